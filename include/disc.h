@@ -24,6 +24,16 @@
  *   disc_accept_resample  Algorithm 1, lines 11-22: K ordered accept tests, then the K-way draw
  *                    over K fresh candidates.
  *
+ * and what the language model around it runs for B queries with K candidates each (line 5's
+ * P = L(a, T) with a model of attention layers):
+ *
+ *   disc_attend_prompt   attention over whole prompts, packed
+ *   disc_cache_*         a key-value cache in pages that the candidates of a query share: fork,
+ *                    extend, write, free, compact
+ *   disc_attend_plan, disc_attend_cached   attention of one new token per candidate over that cache
+ *   disc_logprobs, disc_logprobs_grad   log-probabilities of given tokens, entropy, the most probable
+ *                    alternatives, and the gradient for training on them
+ *
  * Conventions
  *   - Every function returns 0 (DISC_OK) or a negative DISC_ERR_* code.  Return codes cover
  *     argument validation and CUDA launch/allocation errors only; problems of a single row are
@@ -84,10 +94,11 @@ extern "C" {
 #define DISC_ROW_FAULT 16   /* reserved for kernels that wait inside the device; no present kernel sets it
                                (disc_project_step reports a wait that ran out through
                                disc_project_error instead)                                        */
+#define DISC_ROW_NOPAGE 32  /* the cache has no room for the row's new tokens; the row is unchanged   */
 
 typedef struct disc_set disc_set_t; /* opaque; owns its device memory */
 
-typedef enum { DISC_F32 = 0, DISC_BF16 = 1 } disc_dtype_t;
+typedef enum { DISC_F32 = 0, DISC_BF16 = 1, DISC_F16 = 2 /* attention and cache only */ } disc_dtype_t;
 
 #define DISC_MAX_DEPTH 64
 
@@ -357,6 +368,153 @@ int disc_accept_resample(const float* logw, int32_t B, int32_t K, uint64_t seed,
                          int32_t* choice_out, int32_t* first_out, float* logz_out,
                          const int32_t* seq_tokens, int32_t seq_ld, int32_t* tokens_out,
                          uint8_t* status_out, void* stream);
+
+/* ---- log-probabilities ---------------------------------------------------------------------------
+ * For each of n rows, with p = softmax(z / T) over the whole vocabulary:
+ *   logits, dtype, ld   as for disc_step (any alignment of the rows; device memory)
+ *   targets     device, int32[n] (nullable): the token to score; -1 = none (logp 0)
+ *   top         0..64 alternatives per row
+ *   logp_out    device, float[n] (required with targets): log p_target
+ *   entropy_out device, float[n] (nullable): - sum_v p_v log p_v (nats)
+ *   lse_out     device, float[n] (nullable): log sum_v e^{z_v/T}
+ *   top_ids_out device, int32[n][top]: the most probable tokens in descending order; equal logits
+ *               (-0 = +0) by the lower id first, NaN last; -1 beyond the vocabulary
+ *   top_logp_out  device, float[n][top] (nullable): their log-probabilities (-inf beside a -1)
+ *   status_out  device, uint8[n]: DISC_ROW_NOMASS for a row of -inf logits (lse and all
+ *               log-probabilities -inf, entropy 0), DISC_ROW_NONFINITE for NaN or +inf among the logits
+ *               (log-probabilities and entropy are then NaN or unspecified; the ids are not),
+ *               DISC_ROW_DEAD for a target that is neither -1 nor in [0, vocab_size) (logp NaN)
+ * Sums are held in fp32 relative to the row's maximum.
+ * Errors: DISC_ERR_ARG, DISC_ERR_UNSUPPORTED (dtype; top > 64; n > 2^27). */
+int disc_logprobs(const void* logits, disc_dtype_t dtype, int64_t ld, int64_t n, int32_t vocab_size, float inv_temperature,
+                  const int32_t* targets, int32_t top, float* logp_out, float* entropy_out, float* lse_out,
+                  int32_t* top_ids_out, float* top_logp_out, uint8_t* status_out, void* stream);
+
+/* The gradient of sum_i (d_logp[i] logp[i] + d_entropy[i] entropy[i]) with respect to the logits:
+ *   grad[i][v] = (d_logp [v = target] - p_v (d_logp + d_entropy (log p_v + entropy))) / T
+ *   lse, entropy   device, float[n]: what disc_logprobs returned for these logits (entropy nullable
+ *               without d_entropy)
+ *   d_logp      device, float[n] (nullable; needs targets); rows without a target ignore it
+ *   d_entropy   device, float[n] (nullable)
+ *   grad_out    device, n rows of vocab_size values of type `dtype`, row i at element offset
+ *               i*grad_ld; may be `logits` itself (with grad_ld = ld), otherwise must not overlap it
+ * Rows of -inf logits get a zero gradient, rows with a non-finite lse a non-finite one. */
+int disc_logprobs_grad(const void* logits, disc_dtype_t dtype, int64_t ld, int64_t n, int32_t vocab_size, float inv_temperature,
+                       const int32_t* targets, const float* lse, const float* entropy, const float* d_logp, const float* d_entropy,
+                       void* grad_out, int64_t grad_ld, void* stream);
+
+/* ---- attention over whole prompts ------------------------------------------------------------------
+ * Packed sequences: sequence i has the queries cu_q[i] .. cu_q[i+1]-1 and the keys cu_k[i] ..
+ * cu_k[i+1]-1 (lq and lk of them).  Query j of a sequence sees its keys 0 .. j + lk - lq with `causal`
+ * (the last query sees all; a query that sees none gets out = 0, lse = -inf), all lk of them without.
+ * Query head h reads key head h / (n_q_heads / n_kv_heads).
+ *   out = softmax(scale q k^T) v,  lse = log sum e^{scale q k^T}
+ *   q, k, v     device, bf16 or f16; token t, head h at element offset t*token_stride + h*head_stride,
+ *               head_dim values in a row (slices of one fused projection output are fine).  Bases on
+ *               16-byte boundaries, strides multiples of 8
+ *   head_dim    a multiple of 8, at most DISC_MAX_HEAD_DIM
+ *   n_q_heads   a multiple of n_kv_heads, at most 128 times as many
+ *   n_q, n_k    tokens in q and in k / v
+ *   cu_q        device, int32[n_seqs+1], ascending from 0 to n_q;  cu_k the same over n_k (nullable:
+ *               the same sequences)
+ *   max_q       no sequence has more queries than this (sizes the launch)
+ *   out         device, [n_q][n_q_heads][head_dim] contiguous, 16-byte aligned
+ *   lse_out     device, float[n_q][n_q_heads] (nullable)
+ *   error       device, 4 bytes: set to 1 when a bounded wait inside the kernel ran out (results
+ *               invalid), never cleared; read with disc_attend_error
+ * Scores, sums and outputs are accumulated in fp32; the probabilities are rounded to the inputs' type for
+ * the second product, the outputs once at the end.  A non-finite value vector makes the rows of its own
+ * sequence non-finite where they share a block of 128 keys with it, also those that do not see it;
+ * other sequences are not touched by it.
+ * Errors: DISC_ERR_ARG, DISC_ERR_UNSUPPORTED (dtype, head_dim, strides, head counts). */
+#define DISC_MAX_HEAD_DIM 128
+int disc_attend_prompt(const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride,
+                       int64_t k_head_stride, const void* v, int64_t v_token_stride, int64_t v_head_stride, disc_dtype_t dtype,
+                       int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t n_q, int64_t n_k, const int32_t* cu_q,
+                       const int32_t* cu_k, int32_t n_seqs, int32_t max_q, int32_t causal, float scale, void* out, float* lse_out,
+                       uint32_t* error, void* stream);
+
+/* Synchronises `stream`; DISC_ERR_CUDA when an attention kernel has set this error word. */
+int disc_attend_error(const uint32_t* error, void* stream);
+
+/* ---- the key-value cache ---------------------------------------------------------------------------
+ * Rows (sequences) hold their keys and values in pages of page_size tokens; a page may belong to several
+ * rows, which is how the K candidates of a query share its prompt.  All memory is the caller's, on
+ * the device; the struct itself is host memory and may be rebuilt for every call.
+ *   pool    [n_layers][2][n_pages][n_kv_heads][page_size][head_dim] of dtype (index 1: keys, values)
+ *   table   int32[n_rows][table_width]: the pages of row r in order; -1 beyond the last one
+ *   len     int32[n_rows]: tokens of row r; it uses ceil(len / page_size) pages
+ *   ref     int32[n_pages]: number of table entries that name the page; 0 = free
+ *   scratch disc_cache_scratch_bytes() bytes, 16-byte aligned, contents irrelevant between calls
+ * An empty cache has table = -1, len = 0, ref = 0.  The calls below keep the three consistent; new
+ * pages are always the free ones of lowest id.  The calls on one cache must not overlap on the device.
+ * Page sizes: 16, 32, 64, 128.  dtype bf16 or f16, head_dim a multiple of 8 up to 128. */
+typedef struct {
+    void* pool;
+    int32_t* table;
+    int32_t* len;
+    int32_t* ref;
+    void* scratch;
+    int64_t scratch_bytes;
+    int32_t n_layers, n_pages, n_kv_heads, page_size, head_dim, n_rows, table_width, dtype;
+} disc_cache_t;
+
+int64_t disc_cache_scratch_bytes(const disc_cache_t* c);   /* from the sizes alone */
+
+/* Row r becomes what row parent[r] was before the call, sharing its pages (no contents are copied); a
+ * parent outside [0, n_rows) empties the row.  Any mapping is allowed: fork K candidates from
+ * a prompt, reorder, keep the drawn candidate of each query and drop the others.
+ *   parent  device, int32[n_rows]; parent[r] = r leaves the row as it is */
+int disc_cache_fork(const disc_cache_t* c, const int32_t* parent, void* stream);
+
+/* The rows with freed[r] != 0 become empty.  freed: device, uint8[n_rows]. */
+int disc_cache_free(const disc_cache_t* c, const uint8_t* freed, void* stream);
+
+/* Room for add[r] more tokens in row r (add: device, int32[n_rows]; null = one each; <= 0 = none): len
+ * grows, new pages are taken, and a row about to write into a partly filled page that other rows hold too
+ * gets its own copy of the tokens in it, in all layers (when every holder of the page writes on, the lowest
+ * row keeps it).  Rows are served in ascending order: once the pages still needed by a row and those before
+ * it exceed the free ones, that row and later ones that need a page get DISC_ROW_NOPAGE and stay as they
+ * are; so do rows that would outgrow the table.  status_out: device, uint8[n_rows]. */
+int disc_cache_extend(const disc_cache_t* c, const int32_t* add, uint8_t* status_out, void* stream);
+
+/* Keys and values of the newest tokens of some rows into layer `layer`: sequence i of n_seqs is row rows[i]
+ * (null: row i), its tokens t = cu[i] .. cu[i+1]-1 (null cu: one token, t = i) are the last ones
+ * the row was extended by.
+ *   k, v    device, token t, head h at element offset t*token_stride + h*head_stride; bases on
+ *           16-byte boundaries, strides multiples of 8
+ *   status  device, uint8[n_rows] (nullable): rows with a status (disc_cache_extend) are skipped */
+int disc_cache_write(const disc_cache_t* c, int32_t layer, const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v,
+                     int64_t v_token_stride, int64_t v_head_stride, int64_t n_tokens, const int32_t* cu, int32_t n_seqs,
+                     const int32_t* rows, const uint8_t* status, void* stream);
+
+/* The n pages in use move to the ids 0 .. n-1 (those that are there already stay, the others go to
+ * the free ids below n in order), contents of all layers with them.  live_out: device, int32: n. */
+int disc_cache_compact(const disc_cache_t* c, int32_t* live_out, void* stream);
+
+/* ---- attention of one new token per row over the cache -----------------------------------------------
+ * The plan: which pages each group of `group` consecutive rows (K candidates of a query; 1 = unrelated
+ * rows) has in common, and how the work is split.  It depends on the books only: make it once per position, after
+ * disc_cache_extend, and use it for every layer.
+ *   plan    device, disc_attend_plan_bytes() bytes, 16-byte aligned */
+int64_t disc_attend_plan_bytes(const disc_cache_t* c, int32_t n_q_heads, int32_t group);
+int disc_attend_plan(const disc_cache_t* c, int32_t n_q_heads, int32_t group, void* plan, int64_t plan_bytes, void* stream);
+
+/* out[r] = softmax(scale q[r] K^T) V over the len[r] tokens of row r in layer `layer`; a row without tokens
+ * gets out = 0, lse = -inf.  Pages that the rows of a group have in common are read once for all.
+ *   q       device, dtype of the cache; row r, head h at element offset r*q_row_stride + h*q_head_stride;
+ *           base on a 16-byte boundary, strides multiples of 8
+ *   n_q_heads   a multiple of n_kv_heads, at most 64 times as many
+ *   plan    of disc_attend_plan with the same cache sizes, n_q_heads and group; long rows are split and joined in
+ *           it, so calls that share a plan must not overlap
+ *   out     device, [n_rows][n_q_heads][head_dim] contiguous, 16-byte aligned
+ *   lse_out device, float[n_rows][n_q_heads] (nullable)
+ * Scores, sums and outputs are accumulated in fp32; the probabilities are rounded to the inputs' type for
+ * the second product, the outputs once at the end.  The result does not depend on the order in which the parts of
+ * a row finish. */
+int disc_attend_cached(const disc_cache_t* c, int32_t layer, const void* q, int64_t q_row_stride, int64_t q_head_stride,
+                       int32_t n_q_heads, int32_t group, float scale, void* plan, int64_t plan_bytes, void* out, float* lse_out,
+                       void* stream);
 
 /* Diagnostic: the n group-noise uniforms of token groups g0 .. g0+n-1 for (seed, step, row), fp32.
  *   out  device, float[n] */

@@ -16,8 +16,8 @@ import torch
 
 from . import build as _build
 
-DISC_F32, DISC_BF16 = 0, 1
-ROW_DEAD, ROW_NOMASS, ROW_NONFINITE, ROW_DONE, ROW_FAULT = 1, 2, 4, 8, 16
+DISC_F32, DISC_BF16, DISC_F16 = 0, 1, 2
+ROW_DEAD, ROW_NOMASS, ROW_NONFINITE, ROW_DONE, ROW_FAULT, ROW_NOPAGE = 1, 2, 4, 8, 16, 32
 MAX_DEPTH = 64
 
 ERRORS = {-1: "DISC_ERR_ARG", -2: "DISC_ERR_EMPTY", -3: "DISC_ERR_TOKEN", -4: "DISC_ERR_PREFIX",
@@ -27,6 +27,9 @@ EXPORTS = ["disc_build_set", "disc_build_set_eok", "disc_free_set", "disc_set_in
            "disc_mask", "disc_mask_static", "disc_verify", "disc_step", "disc_project_step", "disc_project_scratch_bytes",
            "disc_project_error", "disc_topm", "disc_step_topm", "disc_step_topm_scratch_bytes", "disc_resample", "disc_accept", "disc_accept_resample",
            "disc_sampling_uniforms",
+           "disc_logprobs", "disc_logprobs_grad", "disc_attend_prompt", "disc_attend_error",
+           "disc_cache_scratch_bytes", "disc_cache_fork", "disc_cache_free", "disc_cache_extend", "disc_cache_write",
+           "disc_cache_compact", "disc_attend_plan_bytes", "disc_attend_plan", "disc_attend_cached",
            "disc_error_string", "disc_last_cuda_error"]
 
 
@@ -38,6 +41,13 @@ class DiscError(RuntimeError):
             extra = f" (cudaError {lib().disc_last_cuda_error()})"
         super().__init__(f"{where} failed: {name}{extra}")
         self.code = code
+
+
+class _Cache(C.Structure):
+    _fields_ = [("pool", C.c_void_p), ("table", C.c_void_p), ("len", C.c_void_p), ("ref", C.c_void_p),
+                ("scratch", C.c_void_p), ("scratch_bytes", C.c_int64), ("n_layers", C.c_int32), ("n_pages", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("page_size", C.c_int32), ("head_dim", C.c_int32), ("n_rows", C.c_int32),
+                ("table_width", C.c_int32), ("dtype", C.c_int32)]
 
 
 class _SetInfo(C.Structure):
@@ -82,11 +92,26 @@ def lib():
     L.disc_accept.argtypes = [vp, i32, i32, u64, i64, vp, vp]
     L.disc_accept_resample.argtypes = [vp, i32, i32, u64, i64, vp, vp, vp, vp, i32, vp, vp, vp]
     L.disc_sampling_uniforms.argtypes = [u64, u32, u32, i32, i32, vp, vp]
+    L.disc_logprobs.argtypes = [vp, C.c_int, i64, i64, i32, f32, vp, i32, vp, vp, vp, vp, vp, vp, vp]
+    L.disc_logprobs_grad.argtypes = [vp, C.c_int, i64, i64, i32, f32, vp, vp, vp, vp, vp, vp, i64, vp]
+    L.disc_attend_prompt.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, i64, C.c_int, i32, i32, i32, i64, i64, vp, vp,
+                                     i32, i32, i32, f32, vp, vp, vp, vp]
+    L.disc_attend_error.argtypes = [vp, vp]
+    L.disc_cache_scratch_bytes.argtypes = [vp]
+    L.disc_cache_fork.argtypes = [vp, vp, vp]
+    L.disc_cache_free.argtypes = [vp, vp, vp]
+    L.disc_cache_extend.argtypes = [vp, vp, vp, vp]
+    L.disc_cache_write.argtypes = [vp, i32, vp, i64, i64, vp, i64, i64, i64, vp, i32, vp, vp, vp]
+    L.disc_cache_compact.argtypes = [vp, vp, vp]
+    L.disc_attend_plan_bytes.argtypes = [vp, i32, i32]
+    L.disc_attend_plan.argtypes = [vp, i32, i32, vp, i64, vp]
+    L.disc_attend_cached.argtypes = [vp, i32, vp, i64, i64, i32, i32, f32, vp, i64, vp, vp, vp]
     L.disc_error_string.argtypes = [C.c_int]
     L.disc_error_string.restype = C.c_char_p
     L.disc_last_cuda_error.argtypes = []
     for name in EXPORTS:
-        if name in ("disc_project_scratch_bytes", "disc_step_topm_scratch_bytes"):
+        if name in ("disc_project_scratch_bytes", "disc_step_topm_scratch_bytes", "disc_cache_scratch_bytes",
+                    "disc_attend_plan_bytes"):
             getattr(L, name).restype = C.c_int64
         elif name not in ("disc_free_set", "disc_error_string"):
             getattr(L, name).restype = C.c_int

@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "disc.h"
 
 struct disc_set {
@@ -76,6 +78,27 @@ inline int check_device(const disc_set* s) {
         cudaError_t e__ = (call);                               \
         if (e__ != cudaSuccess) return ::disc::cuda_fail(e__);  \
     } while (0)
+
+// the number of SMs of the current device
+inline int device_sms(int* sms) {
+    int dev = 0;
+    DISC_CUDA(cudaGetDevice(&dev));
+    DISC_CUDA(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev));
+    return DISC_OK;
+}
+
+// More than 48 KB of dynamic shared memory for a kernel, set once per device; `done` is a static of the caller,
+// one per kernel.
+template <class F>
+inline int allow_smem(F* kernel, int bytes, std::atomic<uint64_t>& done) {
+    int dev = 0;
+    DISC_CUDA(cudaGetDevice(&dev));
+    const uint64_t bit = uint64_t(1) << (dev & 63);
+    if (done.load(std::memory_order_acquire) & bit) return DISC_OK;
+    DISC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    done.fetch_or(bit, std::memory_order_release);
+    return DISC_OK;
+}
 
 // ------------------------------------------------------------------ Philox4x32-10
 // Counter-based generator of Salmon et al. (SC'11).  Round keys depend only on the seed.
@@ -153,6 +176,9 @@ int step_with_candidates(const disc_set* s, const void* logits, disc_dtype_t dty
                          int32_t* hi, int32_t* depth, float* logw, uint8_t* done, int32_t* token_out, int32_t* seq_tokens,
                          int32_t seq_ld, float* logq_out, float* logp_out, uint32_t* mask_out, uint8_t* status_out,
                          const int32_t* cand, const uint8_t* valid, int32_t M, const float2* lse, cudaStream_t st);
+
+// the sizes and alignments of a cache, without its books (disc_cache.cu)
+int cache_sizes(const disc_cache_t* c);
 
 // top 23 bits k of a word -> u = (2k+1) * 2^-24, exact in fp32, as is 1-u
 __device__ __forceinline__ float uniform_from_bits(uint32_t r) {

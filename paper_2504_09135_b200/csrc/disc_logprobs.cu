@@ -1,0 +1,665 @@
+// disc_logprobs: per row of logits the log-sum-exp, the entropy of softmax(z / T), the log-probability
+// of a given token and the `top` most probable tokens with theirs; disc_logprobs_grad: the gradient of
+// the log-probabilities and entropies with respect to the logits.
+//
+// With y_v = z_v log2(e) / T and m = max y:   S = sum 2^(y-m),  U = sum (y-m) 2^(y-m),
+//   lse = ln2 (m + log2 S)     H = ln2 (log2 S - U / S)     log p_t = z_t / T - lse
+// so that one pass with a running maximum gives all three.  In units of y - m both sums stay between
+// 0 and the number of tokens, and H loses nothing to a large lse.
+//
+// The pass is bound by the bytes of the logits.  What it may spend per logit is little: at the
+// measured copy rate 11 bf16 logits arrive per SM and clock, and an SM takes 2^x sixteen times and
+// any instruction 128 times per clock.  Hence packed bf16 maxima (half an instruction per logit), one
+// comparison with the running maximum per 32 logits, and nothing in the loop for the alternatives:
+//
+// The alternatives come from what the pass keeps anyway, each thread's own maximum.  The k-th largest
+// of the block's thread maxima (k distinct elements reach it) is at most the k-th largest element.  Only
+// the threads whose maximum reaches it can own one of the k best, as a rule k of them, and their
+// elements, a k-th part of a percent of the row, are looked at again (they are in L2).  What reaches the
+// threshold, typically k and a few, is ranked by counting in the order (larger first, -0 = +0, lower id
+// first, NaN last).  Should more reach it than the list holds (rows of equal logits), or too few (rows of
+// NaN), the block selects by histograms of the order keys over its slice: exact for every input.
+//
+// A row is taken by one block, or, when there are too few rows to fill the device, by a cluster of up to
+// 8 blocks that join their sums and lists over distributed shared memory.
+
+#include <cuda_bf16.h>
+#include <math_constants.h>
+
+#include "disc_internal.cuh"
+
+namespace {
+
+constexpr int NT = 256;               // threads per block
+constexpr int NW = NT / 32;
+constexpr int TOP_MAX = 64;
+constexpr int LIST_CAP = 2048;
+constexpr unsigned FULL = 0xffffffffu;
+constexpr float LOG2E_F = 1.4426950408889634f;
+constexpr float LN2_F = 0.6931471805599453f;
+// 2^y is zero in fp32 (flushed) below -126; clamping y there keeps (y-m) 2^(y-m) at 0 for y = -inf
+constexpr float Y_MIN = -200.f;
+
+struct LogprobParams {
+    const void* logits;
+    int64_t ld;
+    int32_t V, top, split;
+    float inv_t, c2;                  // 1/T, log2(e)/T
+    const int32_t* targets;           // nullable
+    float* logp;                      // nullable
+    float* entropy;                   // nullable
+    float* lse;                       // nullable
+    int32_t* top_ids;                 // [n][top]
+    float* top_logp;                  // [n][top] (nullable)
+    uint8_t* status;
+};
+
+__device__ __forceinline__ float ex2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// the larger of the two, NaN if either is
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+__device__ __forceinline__ uint32_t order_key(float x) {
+    if (x != x) return 0u;
+    uint32_t b = __float_as_uint(x);
+    if (b == 0x80000000u) b = 0u;
+    return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
+}
+__device__ __forceinline__ float key_value(uint32_t k) {
+    if (k == 0u) return CUDART_NAN_F;
+    return (k & 0x80000000u) ? __uint_as_float(k & 0x7fffffffu) : __uint_as_float(~k);
+}
+__device__ __forceinline__ uint4 ld_stream(const uint4* p) {
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "l"(p));
+    return v;
+}
+
+template <int DT>
+struct Vec;
+template <>
+struct Vec<DISC_BF16> {
+    static constexpr int E = 8;
+    static constexpr int SIZE = 2;
+    static __device__ __forceinline__ uint4 lowest() { return make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u); }
+    static __device__ __forceinline__ void unpack(const uint4& v, float* x) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { x[2 * j] = __uint_as_float(w[j] << 16); x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u); }
+    }
+    // the largest of U vectors' elements, NaN only if all are
+    template <int U>
+    static __device__ __forceinline__ float largest(const uint4* v) {
+        __nv_bfloat162 a = *reinterpret_cast<const __nv_bfloat162*>(&v[0].x);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (u) a = __hmax2(a, *reinterpret_cast<const __nv_bfloat162*>(&v[u].x));
+            a = __hmax2(a, *reinterpret_cast<const __nv_bfloat162*>(&v[u].y));
+            a = __hmax2(a, *reinterpret_cast<const __nv_bfloat162*>(&v[u].z));
+            a = __hmax2(a, *reinterpret_cast<const __nv_bfloat162*>(&v[u].w));
+        }
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(&a);
+        return fmaxf(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    }
+    static __device__ __forceinline__ float at(const char* p) { return __uint_as_float(uint32_t(*reinterpret_cast<const unsigned short*>(p)) << 16); }
+    static __device__ __forceinline__ void put(char* p, float x) { *reinterpret_cast<__nv_bfloat16*>(p) = __float2bfloat16_rn(x); }
+    static __device__ __forceinline__ uint4 pack(const float* x) {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * j], x[2 * j + 1]);
+            w[j] = *reinterpret_cast<const uint32_t*>(&b);
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+template <>
+struct Vec<DISC_F32> {
+    static constexpr int E = 4;
+    static constexpr int SIZE = 4;
+    static __device__ __forceinline__ uint4 lowest() { return make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u); }
+    static __device__ __forceinline__ void unpack(const uint4& v, float* x) {
+        x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
+    }
+    template <int U>
+    static __device__ __forceinline__ float largest(const uint4* v) {
+        float a = __uint_as_float(v[0].x);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            a = fmaxf(fmaxf(a, __uint_as_float(v[u].x)), fmaxf(__uint_as_float(v[u].y), fmaxf(__uint_as_float(v[u].z), __uint_as_float(v[u].w))));
+        return a;
+    }
+    static __device__ __forceinline__ float at(const char* p) { return *reinterpret_cast<const float*>(p); }
+    static __device__ __forceinline__ void put(char* p, float x) { *reinterpret_cast<float*>(p) = x; }
+    static __device__ __forceinline__ uint4 pack(const float* x) {
+        return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+    }
+};
+
+// A row as elements before the first 16-byte boundary, whole vectors, and the elements after them.
+template <int DT>
+struct RowShape {
+    const char* base;
+    int32_t head, nvec, tail;
+    __device__ __forceinline__ RowShape(const void* logits, int64_t ld, int64_t row, int32_t V) {
+        constexpr int E = Vec<DT>::E, SIZE = Vec<DT>::SIZE;
+        base = static_cast<const char*>(logits) + row * ld * SIZE;
+        head = min(V, int32_t(((16 - (reinterpret_cast<uintptr_t>(base) & 15)) & 15) / SIZE));
+        nvec = (V - head) / E;
+        tail = V - head - nvec * E;
+    }
+    __device__ __forceinline__ const uint4* vecs() const { return reinterpret_cast<const uint4*>(base + size_t(head) * Vec<DT>::SIZE); }
+};
+
+struct Sums {
+    float m, ref, s, u;               // largest logit, its y; sums relative to ref
+};
+__device__ __forceinline__ void raise(Sums& a, float m_new, float c2) {
+    const float ref = fabsf(m_new) < CUDART_INF_F ? m_new * c2 : 0.f;
+    const float d = a.m > -CUDART_INF_F ? a.ref - ref : Y_MIN;
+    const float f = ex2_approx(d);
+    a.u = f * fmaf(d, a.s, a.u);
+    a.s *= f;
+    a.m = m_new;
+    a.ref = ref;
+}
+__device__ __forceinline__ Sums join(Sums a, Sums b, float c2) {
+    if (b.m > a.m) { const Sums t = a; a = b; b = t; }
+    raise(b, a.m, c2);
+    a.s += b.s;
+    a.u += b.u;
+    return a;
+}
+__device__ __forceinline__ void add(Sums& a, float x, float c2) {
+    const float d = max_nan(fmaf(x, c2, -a.ref), Y_MIN);
+    const float e = ex2_approx(d);
+    a.s += e;
+    a.u = fmaf(d, e, a.u);
+}
+
+// shared memory of a block; the other blocks of the cluster read `part`, `found` and `list`
+struct Smem {
+    unsigned long long list[LIST_CAP];                 // order key << 32 | ~id : larger = better
+    unsigned long long best[TOP_MAX];
+    uint32_t keys[NT];
+    int32_t hot[NT];
+    unsigned int hist[256];
+    Sums warp_sums[NW];
+    Sums part;
+    unsigned int n_hot, n_list, threshold, found;
+    unsigned int prefix, remaining;
+    int scan[NW];
+};
+
+__device__ __forceinline__ unsigned long long entry(uint32_t key, int32_t id) {
+    return (static_cast<unsigned long long>(key) << 32) | uint32_t(~id);
+}
+
+__device__ __forceinline__ uint32_t cluster_ctarank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync_all() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t remote(const void* p, uint32_t rank) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(uint32_t(__cvta_generic_to_shared(p))), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ uint32_t ld_remote32(uint32_t a) {
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ unsigned long long ld_remote64(uint32_t a) {
+    unsigned long long v;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
+    return v;
+}
+
+// Of the cnt entries of sm.list the `want` best, in order, into sm.best.  Entries are distinct.
+__device__ __forceinline__ void rank_list(Smem& sm, unsigned int cnt, unsigned int want) {
+    for (unsigned int i = threadIdx.x; i < cnt; i += NT) {
+        const unsigned long long e = sm.list[i];
+        unsigned int r = 0;
+        for (unsigned int j = 0; j < cnt; ++j) r += sm.list[j] > e;
+        if (r < want) sm.best[r] = e;
+    }
+    __syncthreads();
+}
+
+// The `want` best of the elements [e0, e1) of a row by histograms of the order keys, eight bits at a
+// time, and the lowest ids among the keys equal to the last one.  Called by the whole block.
+template <int DT>
+__device__ __noinline__ void select_slice(const char* base, int32_t e0, int32_t e1, unsigned int want, Smem& sm) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    __syncthreads();
+    if (tid == 0) { sm.prefix = 0u; sm.remaining = want; sm.n_list = 0u; }
+    __syncthreads();
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        for (int b = tid; b < 256; b += NT) sm.hist[b] = 0u;
+        __syncthreads();
+        const uint32_t prefix = sm.prefix;
+        unsigned int bin = 256u, run = 0u;              // equal bins in a row are counted before they are added
+        for (int32_t e = e0 + tid; e < e1; e += NT) {
+            const uint32_t key = order_key(Vec<DT>::at(base + size_t(e) * Vec<DT>::SIZE));
+            if (shift < 24 && (key >> (shift + 8)) != (prefix >> (shift + 8))) continue;
+            const unsigned int b = (key >> shift) & 255u;
+            if (b != bin) {
+                if (run) atomicAdd(&sm.hist[bin], run);
+                bin = b;
+                run = 0u;
+            }
+            ++run;
+        }
+        if (run) atomicAdd(&sm.hist[bin], run);
+        __syncthreads();
+        if (tid == 0) {
+            unsigned int left = sm.remaining;
+            int b = 255;
+            for (; b > 0; --b) {
+                if (sm.hist[b] >= left) break;
+                left -= sm.hist[b];
+            }
+            sm.prefix = prefix | (uint32_t(b) << shift);
+            sm.remaining = left;
+        }
+        __syncthreads();
+    }
+    const uint32_t last = sm.prefix;
+    const unsigned int ties = sm.remaining;
+    for (int32_t e = e0 + tid; e < e1; e += NT) {       // fewer than `want` of them
+        const uint32_t key = order_key(Vec<DT>::at(base + size_t(e) * Vec<DT>::SIZE));
+        if (key > last) sm.list[atomicAdd(&sm.n_list, 1u)] = entry(key, e);
+    }
+    unsigned int taken = 0;
+    for (int32_t b0 = e0; b0 < e1 && taken < ties; b0 += NT) {
+        const int32_t e = b0 + tid;
+        const bool eq = e < e1 && order_key(Vec<DT>::at(base + size_t(e) * Vec<DT>::SIZE)) == last;
+        const unsigned ball = __ballot_sync(FULL, eq);
+        if (lane == 0) sm.scan[warp] = __popc(ball);
+        __syncthreads();
+        unsigned int before = taken, all = 0;
+        for (int w = 0; w < NW; ++w) {
+            if (w < warp) before += sm.scan[w];
+            all += sm.scan[w];
+        }
+        before += __popc(ball & ((1u << lane) - 1u));
+        if (eq && before < ties) sm.list[atomicAdd(&sm.n_list, 1u)] = entry(last, e);
+        taken += all;
+        __syncthreads();
+    }
+    __syncthreads();
+}
+
+constexpr int U = 4;                  // 16-byte loads a thread keeps in flight
+
+template <int DT, bool TOP>
+__global__ void __launch_bounds__(NT, 4) disc_logprobs_kernel(const LogprobParams p) {
+    constexpr int E = Vec<DT>::E, SIZE = Vec<DT>::SIZE;
+    extern __shared__ unsigned char smem_raw[];
+    Smem& sm = *reinterpret_cast<Smem*>(smem_raw);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int64_t row = blockIdx.x / unsigned(p.split);
+    const uint32_t rank = p.split > 1 ? cluster_ctarank() : 0u;
+    const RowShape<DT> r(p.logits, p.ld, row, p.V);
+    const uint4* vecs = r.vecs();
+
+    // this block's vectors [v0, v1); the first block also takes the elements around the vectors, one per thread
+    const int32_t per = (r.nvec + p.split - 1) / p.split;
+    const int32_t v0 = min(r.nvec, int32_t(rank) * per), v1 = min(r.nvec, v0 + per);
+    int32_t extra = -1;
+    if (rank == 0) {
+        if (tid < r.head) extra = tid;
+        else if (tid - r.head < r.tail) extra = r.head + r.nvec * E + tid - r.head;
+    }
+
+    Sums a{-CUDART_INF_F, 0.f, 0.f, 0.f};
+    if (extra >= 0) {
+        const float x = Vec<DT>::at(r.base + size_t(extra) * SIZE);
+        if (x > a.m) raise(a, x, p.c2);
+        add(a, x, p.c2);
+    }
+    for (int32_t v = v0 + tid; v < v1; v += NT * U) {
+        uint4 w[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) w[u] = v + u * NT < v1 ? ld_stream(vecs + v + u * NT) : Vec<DT>::lowest();
+        const float mx = Vec<DT>::template largest<U>(w);
+        if (mx > a.m) raise(a, mx, p.c2);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float x[E];
+            Vec<DT>::unpack(w[u], x);
+#pragma unroll
+            for (int j = 0; j < E; ++j) add(a, x[j], p.c2);
+        }
+    }
+
+    const float own_max = a.m;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        Sums b;
+        b.m = __shfl_xor_sync(FULL, a.m, o);
+        b.ref = __shfl_xor_sync(FULL, a.ref, o);
+        b.s = __shfl_xor_sync(FULL, a.s, o);
+        b.u = __shfl_xor_sync(FULL, a.u, o);
+        a = join(a, b, p.c2);
+    }
+    if (lane == 0) sm.warp_sums[warp] = a;
+    const uint32_t key = v0 + tid < v1 || extra >= 0 ? order_key(own_max) : 0u;
+    unsigned int found = 0;
+    if (TOP) {
+        sm.keys[tid] = key;
+        if (tid == 0) { sm.n_hot = 0u; sm.n_list = 0u; }
+    }
+    __syncthreads();
+    if (TOP) {
+        const int32_t elements = (v1 - v0) * E + (rank == 0 ? r.head + r.tail : 0);
+        const unsigned int want = min(unsigned(p.top), unsigned(elements));
+        // the want-th largest of the threads' maxima
+        unsigned int above = 0;
+        const uint4* k4 = reinterpret_cast<const uint4*>(sm.keys);
+#pragma unroll 8
+        for (int j = 0; j < NT / 4; ++j) {
+            const uint4 k = k4[j];
+            above += (k.x > key || (k.x == key && 4 * j + 0 < tid)) + (k.y > key || (k.y == key && 4 * j + 1 < tid)) +
+                     (k.z > key || (k.z == key && 4 * j + 2 < tid)) + (k.w > key || (k.w == key && 4 * j + 3 < tid));
+        }
+        if (want > 0 && above == want - 1) sm.threshold = key;
+        __syncthreads();
+        if (want > 0) {
+            const uint32_t thr = sm.threshold;
+            const bool hot = v0 + tid < v1 && key >= thr;
+            if (hot) sm.hot[atomicAdd(&sm.n_hot, 1u)] = tid;
+            if (extra >= 0) {
+                const uint32_t k = order_key(Vec<DT>::at(r.base + size_t(extra) * SIZE));
+                if (k >= thr) sm.list[atomicAdd(&sm.n_list, 1u)] = entry(k, extra);
+            }
+            __syncthreads();
+            const int32_t rounds = (v1 - v0 + NT - 1) / NT;
+            const int32_t n_look = int32_t(sm.n_hot) * rounds;
+            for (int32_t i = tid; i < n_look; i += NT) {
+                const int32_t v = v0 + sm.hot[i / rounds] + (i % rounds) * NT;
+                if (v < v1) {
+                    const uint4 w = __ldg(vecs + v);
+                    float x[E];
+                    Vec<DT>::unpack(w, x);
+#pragma unroll
+                    for (int j = 0; j < E; ++j) {
+                        const uint32_t k = order_key(x[j]);
+                        if (k >= thr) {
+                            const unsigned int at = atomicAdd(&sm.n_list, 1u);
+                            if (at < LIST_CAP) sm.list[at] = entry(k, r.head + v * E + j);
+                        }
+                    }
+                }
+            }
+            __syncthreads();
+            unsigned int cnt = sm.n_list;
+            if (cnt > LIST_CAP || cnt < want) {
+                const int32_t e0 = rank == 0 ? 0 : r.head + v0 * E;
+                // the first block's slice is not one run of ids when others lie between it and the row's last
+                // elements; those few are put in by hand
+                const int32_t e1 = p.split == 1 ? p.V : r.head + v1 * E;
+                const bool apart = rank == 0 && p.split > 1 && r.tail > 0;
+                const unsigned int in_run = unsigned(e1 - e0);
+                select_slice<DT>(r.base, e0, e1, min(want, in_run), sm);
+                if (apart && tid < r.tail) {
+                    const int32_t e = r.head + r.nvec * E + tid;
+                    sm.list[atomicAdd(&sm.n_list, 1u)] = entry(order_key(Vec<DT>::at(r.base + size_t(e) * SIZE)), e);
+                }
+                __syncthreads();
+                cnt = sm.n_list;
+            }
+            rank_list(sm, cnt, want);
+        }
+        found = want;
+    }
+    if (tid == 0) {
+        Sums t = sm.warp_sums[0];
+        for (int w = 1; w < NW; ++w) t = join(t, sm.warp_sums[w], p.c2);
+        sm.part = t;
+        sm.found = found;
+    }
+    if (p.split > 1) {
+        cluster_sync_all();
+        if (rank == 0) {
+            if (TOP) {
+                // all blocks' lists together: at most 8 x 64 entries
+                unsigned int at = 0;
+                for (int c = 0; c < p.split; ++c) {
+                    const unsigned int f = ld_remote32(remote(&sm.found, c));
+                    for (unsigned int i = tid; i < f; i += NT) sm.list[at + i] = ld_remote64(remote(&sm.best[i], c));
+                    at += f;
+                }
+                __syncthreads();
+                found = min(unsigned(p.top), at);
+                rank_list(sm, at, found);
+            }
+            if (tid == 0) {
+                Sums t = sm.part;
+                for (int c = 1; c < p.split; ++c) {
+                    const uint32_t q = remote(&sm.part, c);
+                    Sums b{__uint_as_float(ld_remote32(q)), __uint_as_float(ld_remote32(q + 4)), __uint_as_float(ld_remote32(q + 8)), __uint_as_float(ld_remote32(q + 12))};
+                    t = join(t, b, p.c2);
+                }
+                sm.part = t;
+            }
+        }
+        cluster_sync_all();
+        if (rank != 0) return;
+    }
+    __syncthreads();
+
+    const Sums t = sm.part;
+    uint8_t status = 0;
+    float lse, h;
+    if (t.s != t.s || t.u != t.u || t.m == CUDART_INF_F) {
+        status = DISC_ROW_NONFINITE;
+        lse = t.m == CUDART_INF_F && t.s == t.s ? CUDART_INF_F : CUDART_NAN_F;
+        h = CUDART_NAN_F;
+    } else if (!(t.m > -CUDART_INF_F)) {
+        status = DISC_ROW_NOMASS;
+        lse = -CUDART_INF_F;
+        h = 0.f;
+    } else {
+        const float l2 = log2f(t.s);
+        lse = fmaf(t.ref, LN2_F, l2 * LN2_F);
+        h = fmaxf(0.f, LN2_F * (l2 - t.u / t.s));
+    }
+    if (tid == 0) {
+        if (p.lse) p.lse[row] = lse;
+        if (p.entropy) p.entropy[row] = h;
+        if (p.targets) {
+            const int32_t tok = p.targets[row];
+            float lp = 0.f;
+            if (tok >= 0 && tok < p.V) {
+                const float x = Vec<DT>::at(r.base + size_t(tok) * SIZE);
+                lp = status & DISC_ROW_NOMASS ? -CUDART_INF_F : x * p.inv_t - lse;
+            } else if (tok != -1) {
+                lp = CUDART_NAN_F;
+                status |= DISC_ROW_DEAD;
+            }
+            if (p.logp) p.logp[row] = lp;
+        }
+        p.status[row] = status;
+    }
+    if (TOP) {
+        for (unsigned int i = tid; i < unsigned(p.top); i += NT) {
+            int32_t id = -1;
+            float lp = -CUDART_INF_F;
+            if (i < found) {
+                const unsigned long long e = sm.best[i];
+                id = int32_t(~uint32_t(e));
+                if (!(status & DISC_ROW_NOMASS)) lp = key_value(uint32_t(e >> 32)) * p.inv_t - lse;
+            }
+            p.top_ids[row * p.top + i] = id;
+            if (p.top_logp) p.top_logp[row * p.top + i] = lp;
+        }
+    }
+}
+
+// ---- gradient ---------------------------------------------------------------------------------------
+// With a = d logp, b = dH of the row (H = entropy, p_v = 2^(y_v - lse log2e)):
+//   dz_v = (a [v = t] - p_v (a + b (log p_v + H))) / T
+// One read and one write per logit; one 2^x and a handful of multiply-adds, bound by the bytes.
+struct GradParams {
+    const void* logits;
+    int64_t ld;
+    void* grad;
+    int64_t grad_ld;
+    int32_t V, blocks_per_row;
+    float inv_t, c2;
+    const int32_t* targets;           // nullable
+    const float* lse;
+    const float* entropy;             // nullable when d_entropy is
+    const float* d_logp;              // nullable
+    const float* d_entropy;           // nullable
+};
+
+struct RowGrad {
+    float l2, a_bh, b, scale;         // lse in units of y; a + b H; b ln2; 1/T
+    __device__ __forceinline__ float at(float x, float c2) const {
+        const float y = max_nan(fmaf(x, c2, -l2), Y_MIN);
+        return -scale * ex2_approx(y) * fmaf(y, b, a_bh);
+    }
+};
+
+template <int DT>
+__global__ void __launch_bounds__(NT) disc_logprobs_grad_kernel(const GradParams p) {
+    constexpr int E = Vec<DT>::E, SIZE = Vec<DT>::SIZE;
+    const int64_t row = blockIdx.x / unsigned(p.blocks_per_row);
+    const int32_t part = int32_t(blockIdx.x - row * p.blocks_per_row);
+    const int tid = threadIdx.x;
+    const RowShape<DT> r(p.logits, p.ld, row, p.V);
+    char* out = static_cast<char*>(p.grad) + row * p.grad_ld * SIZE;
+    const int32_t tok = p.targets ? p.targets[row] : -1;
+    const float a = p.d_logp && tok >= 0 && tok < p.V ? p.d_logp[row] : 0.f;
+    const float b = p.d_entropy ? p.d_entropy[row] : 0.f;
+    const float lse = p.lse[row];
+    RowGrad g;
+    g.l2 = lse * LOG2E_F;
+    g.a_bh = b != 0.f ? fmaf(b, p.entropy[row], a) : a;
+    g.b = b * LN2_F;
+    g.scale = p.inv_t;
+    if (lse == -CUDART_INF_F) { g.l2 = 0.f; g.scale = 0.f; }      // no mass: nothing to move
+    const float a_t = g.scale * a;
+
+    const bool together = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(r.base)) & 15) == 0;
+    const uint4* vecs = r.vecs();
+    char* out_vecs = out + size_t(r.head) * SIZE;
+    uint4 w[U];
+    const int32_t v0 = part * (NT * U) + tid;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (v0 + u * NT < r.nvec) w[u] = ld_stream(vecs + v0 + u * NT);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int32_t v = v0 + u * NT;
+        if (v < r.nvec) {
+            float x[E];
+            Vec<DT>::unpack(w[u], x);
+            const int32_t at = tok - (r.head + v * E);
+#pragma unroll
+            for (int j = 0; j < E; ++j) x[j] = g.at(x[j], p.c2) + (at == j ? a_t : 0.f);
+            if (together) __stcs(reinterpret_cast<uint4*>(out_vecs) + v, Vec<DT>::pack(x));
+            else
+#pragma unroll
+                for (int j = 0; j < E; ++j) Vec<DT>::put(out_vecs + (size_t(v) * E + j) * SIZE, x[j]);
+        }
+    }
+    if (part == 0) {
+        int32_t e = -1;
+        if (tid < r.head) e = tid;
+        else if (tid - r.head < r.tail) e = r.head + r.nvec * E + tid - r.head;
+        if (e >= 0) Vec<DT>::put(out + size_t(e) * SIZE, g.at(Vec<DT>::at(r.base + size_t(e) * SIZE), p.c2) + (e == tok ? a_t : 0.f));
+    }
+}
+
+template <int DT, bool TOP>
+int launch_logprobs(const LogprobParams& p, int64_t n, cudaStream_t st) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(n * p.split));
+    cfg.blockDim = dim3(NT);
+    cfg.dynamicSmemBytes = sizeof(Smem);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = unsigned(p.split);
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = p.split > 1 ? 1 : 0;
+    DISC_CUDA(cudaLaunchKernelEx(&cfg, disc_logprobs_kernel<DT, TOP>, p));
+    return DISC_OK;
+}
+
+bool bad_logits(const void* logits, int dtype) { return (reinterpret_cast<uintptr_t>(logits) & (dtype == DISC_F32 ? 3u : 1u)) != 0; }
+
+}  // namespace
+
+extern "C" {
+
+int disc_logprobs(const void* logits, disc_dtype_t dtype, int64_t ld, int64_t n, int32_t vocab_size, float inv_temperature,
+                  const int32_t* targets, int32_t top, float* logp_out, float* entropy_out, float* lse_out,
+                  int32_t* top_ids_out, float* top_logp_out, uint8_t* status_out, void* stream) {
+    if (n < 0 || vocab_size <= 0 || ld < vocab_size || top < 0) return DISC_ERR_ARG;
+    if (dtype != DISC_F32 && dtype != DISC_BF16) return DISC_ERR_UNSUPPORTED;
+    if (top > TOP_MAX || n > (int64_t(1) << 27)) return DISC_ERR_UNSUPPORTED;
+    if (!(inv_temperature > 0.f) || !(inv_temperature <= 3.0e38f)) return DISC_ERR_ARG;
+    if (n == 0) return DISC_OK;
+    if (!logits || !status_out || (top > 0 && !top_ids_out) || (targets && !logp_out)) return DISC_ERR_ARG;
+    if (bad_logits(logits, dtype)) return DISC_ERR_ARG;
+    int sms = 0;
+    if (const int rc = disc::device_sms(&sms)) return rc;
+    LogprobParams p;
+    p.logits = logits; p.ld = ld; p.V = vocab_size; p.top = top;
+    p.inv_t = inv_temperature; p.c2 = inv_temperature * LOG2E_F;
+    p.targets = targets; p.logp = logp_out; p.entropy = entropy_out; p.lse = lse_out;
+    p.top_ids = top_ids_out; p.top_logp = top_logp_out; p.status = status_out;
+    // too few rows to put a block on every SM: a row is shared by a cluster, as long as every block still has
+    // some vectors for each of its threads
+    p.split = 1;
+    const int64_t vecs = vocab_size / (dtype == DISC_F32 ? 4 : 8);
+    while (p.split < 8 && n * p.split * 2 <= 2 * sms && vecs / (p.split * 2) >= NT) p.split *= 2;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (dtype == DISC_F32) return top ? launch_logprobs<DISC_F32, true>(p, n, st) : launch_logprobs<DISC_F32, false>(p, n, st);
+    return top ? launch_logprobs<DISC_BF16, true>(p, n, st) : launch_logprobs<DISC_BF16, false>(p, n, st);
+}
+
+int disc_logprobs_grad(const void* logits, disc_dtype_t dtype, int64_t ld, int64_t n, int32_t vocab_size, float inv_temperature,
+                       const int32_t* targets, const float* lse, const float* entropy, const float* d_logp, const float* d_entropy,
+                       void* grad_out, int64_t grad_ld, void* stream) {
+    if (n < 0 || vocab_size <= 0 || ld < vocab_size || grad_ld < vocab_size) return DISC_ERR_ARG;
+    if (dtype != DISC_F32 && dtype != DISC_BF16) return DISC_ERR_UNSUPPORTED;
+    if (!(inv_temperature > 0.f) || !(inv_temperature <= 3.0e38f)) return DISC_ERR_ARG;
+    if (n == 0) return DISC_OK;
+    if (!logits || !lse || !grad_out || (d_logp && !targets) || (d_entropy && !entropy)) return DISC_ERR_ARG;
+    if (bad_logits(logits, dtype) || bad_logits(grad_out, dtype)) return DISC_ERR_ARG;
+    // in place is fine; rows that overlap in any other way are not
+    if (grad_out == logits && grad_ld != ld) return DISC_ERR_ARG;
+    const int64_t vecs = vocab_size / (dtype == DISC_F32 ? 4 : 8);
+    GradParams p;
+    p.logits = logits; p.ld = ld; p.grad = grad_out; p.grad_ld = grad_ld; p.V = vocab_size;
+    p.blocks_per_row = int32_t(vecs / (NT * U) + 1);
+    p.inv_t = inv_temperature; p.c2 = inv_temperature * LOG2E_F;
+    p.targets = targets; p.lse = lse; p.entropy = entropy; p.d_logp = d_logp; p.d_entropy = d_entropy;
+    if (n * p.blocks_per_row > 0x7fffffff) return DISC_ERR_UNSUPPORTED;
+    const unsigned grid = unsigned(n * p.blocks_per_row);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (dtype == DISC_F32) disc_logprobs_grad_kernel<DISC_F32><<<grid, NT, 0, st>>>(p);
+    else disc_logprobs_grad_kernel<DISC_BF16><<<grid, NT, 0, st>>>(p);
+    DISC_CUDA(cudaGetLastError());
+    return DISC_OK;
+}
+
+}  // extern "C"

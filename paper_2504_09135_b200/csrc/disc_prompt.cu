@@ -1,0 +1,496 @@
+// disc_attend_prompt: attention over whole prompts, packed sequences, causal or full, grouped heads.
+//
+//   S = scale Q K^T (masked),  P = softmax(S) row by row,  O = P V
+//
+// 4 D flops per query, key and query head: bound by the tensor cores once a sequence has some
+// hundred tokens.  An SM's tensor cores take 8192 bf16 flops a clock and its special-function units 16
+// exponentials; a block of 128 queries x 128 keys at D = 128 needs 1024 clocks of either, so that both
+// have to be kept busy at once.
+//
+// A block works on two tiles of 128 query vectors against a stream of key/value blocks of 128 tokens.
+// The vectors of a tile are TQ = 128 / G consecutive tokens times the G query heads that read the
+// same key head: K and V are read once for all G, and the staircase of the causal mask costs one masked block
+// per tile whatever G is.
+//   warps 0-3, 4-7   one thread per query vector of tile 0 and tile 1: reads its 128 scores from tensor memory,
+//                    masks, exponentiates relative to a running reference and writes P back as bf16 / f16
+//                    over the scores
+//   warp 8           TMA loads of Q once, then K and V blocks in turn into a ring
+//   warp 9           issues the MMAs (tcgen05, cta_group::1, M 128): S_i = Q_i K^T from shared memory, then
+//                    O_i += P_i V with P_i as the operand in tensor memory.  While the threads of one tile
+//                    exponentiate, the tensor cores run the other tile's P V and next Q K^T.
+// Tensor memory, 512 columns: S_0 | S_1 | O_0 | O_1.
+//
+// The reference a row is exponentiated against moves only when the row's maximum exceeds it by more than 2^8: until then
+// the sums just grow (up to 2^8 times, fp32 has room), and the accumulated O need not be touched.  When it moves, the
+// row's own thread rescales O in tensor memory; the product before has completed by then, since it was issued
+// before the scores the thread has just read.  Sums l are of the unrounded probabilities, in fp32; P is
+// rounded to the inputs' type because the second product takes it in that type; O is rounded once at the end.
+//
+// The rows of V beyond the end of a sequence belong to the next one: P is 0 there, but 0 times a non-finite
+// value is not, so the last block's foreign rows are overwritten with zeros before the product.
+// All waits are bounded; one that runs out sets the error word and every role leaves.
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <math_constants.h>
+
+#include "disc_sm100.cuh"
+
+namespace {
+
+using namespace disc;
+
+constexpr float LN2_F = 0.6931471805599453f;
+constexpr float LOG2E_F = 1.4426950408889634f;
+constexpr int TM = 128;                  // query vectors of a tile
+constexpr int TN = 128;                  // keys of a block
+constexpr int THREADS = 384;
+constexpr int BOX = 64;                  // values of a row in one 128-byte swizzled box
+constexpr float SLACK = 8.f;             // log2 of the growth a row's sums take before the reference moves
+
+template <int DP>
+struct Shape {
+    static constexpr int BOXES = DP / BOX;
+    static constexpr int BOX_BYTES = TN * BOX * 2;                 // 16 KB
+    static constexpr int TILE_BYTES = BOXES * BOX_BYTES;
+    static constexpr int STAGES = DP == 128 ? 4 : 6;
+    static constexpr int SMEM = 2 * TILE_BYTES + STAGES * TILE_BYTES + 1024 + 256;
+};
+
+struct PromptParams {
+    const int32_t* cu_q;
+    const int32_t* cu_k;
+    int32_t n_seqs, hq, hkv, G, TQ, D, causal, tiles;
+    float c2;                             // scale log2(e)
+    unsigned char* out;
+    float* lse;
+    uint32_t* error;
+    uint32_t idesc_qk, idesc_pv;
+};
+
+__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+        : "memory");
+}
+__device__ __forceinline__ void umma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void umma_commit(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+// Descriptor of a [tokens][64 values] box of V read as the N-major operand of P V: along the values 64 to a
+// swizzle row and `lead` bytes to the next 64, along the tokens groups of eight rows 1024 bytes apart.
+__device__ __forceinline__ uint64_t smem_desc_n_major(const void* tile, uint32_t lead) {
+    const uint64_t addr = uint64_t(smem_u32(tile) >> 4) & 0x3FFFu;
+    return addr | (uint64_t(lead >> 4) << 16) | (uint64_t(1024 >> 4) << 32) | (uint64_t(1) << 46) | (uint64_t(2) << 61);
+}
+// 128 consecutive fp32 columns of this thread's TMEM lane.  The wait is part of the statement, so that no use of the
+// registers can move above it.
+__device__ __forceinline__ void tmem_ld128(uint32_t taddr, float* v) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x128.b32 {"
+        "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
+        "%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,"
+        "%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63,"
+        "%64,%65,%66,%67,%68,%69,%70,%71,%72,%73,%74,%75,%76,%77,%78,%79,"
+        "%80,%81,%82,%83,%84,%85,%86,%87,%88,%89,%90,%91,%92,%93,%94,%95,"
+        "%96,%97,%98,%99,%100,%101,%102,%103,%104,%105,%106,%107,%108,%109,%110,%111,"
+        "%112,%113,%114,%115,%116,%117,%118,%119,%120,%121,%122,%123,%124,%125,%126,%127"
+        "}, [%128];\n\ttcgen05.wait::ld.sync.aligned;"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
+          "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]),
+          "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]),
+          "=f"(v[30]), "=f"(v[31]), "=f"(v[32]), "=f"(v[33]), "=f"(v[34]), "=f"(v[35]), "=f"(v[36]), "=f"(v[37]), "=f"(v[38]), "=f"(v[39]),
+          "=f"(v[40]), "=f"(v[41]), "=f"(v[42]), "=f"(v[43]), "=f"(v[44]), "=f"(v[45]), "=f"(v[46]), "=f"(v[47]), "=f"(v[48]), "=f"(v[49]),
+          "=f"(v[50]), "=f"(v[51]), "=f"(v[52]), "=f"(v[53]), "=f"(v[54]), "=f"(v[55]), "=f"(v[56]), "=f"(v[57]), "=f"(v[58]), "=f"(v[59]),
+          "=f"(v[60]), "=f"(v[61]), "=f"(v[62]), "=f"(v[63]), "=f"(v[64]), "=f"(v[65]), "=f"(v[66]), "=f"(v[67]), "=f"(v[68]), "=f"(v[69]),
+          "=f"(v[70]), "=f"(v[71]), "=f"(v[72]), "=f"(v[73]), "=f"(v[74]), "=f"(v[75]), "=f"(v[76]), "=f"(v[77]), "=f"(v[78]), "=f"(v[79]),
+          "=f"(v[80]), "=f"(v[81]), "=f"(v[82]), "=f"(v[83]), "=f"(v[84]), "=f"(v[85]), "=f"(v[86]), "=f"(v[87]), "=f"(v[88]), "=f"(v[89]),
+          "=f"(v[90]), "=f"(v[91]), "=f"(v[92]), "=f"(v[93]), "=f"(v[94]), "=f"(v[95]), "=f"(v[96]), "=f"(v[97]), "=f"(v[98]), "=f"(v[99]),
+          "=f"(v[100]), "=f"(v[101]), "=f"(v[102]), "=f"(v[103]), "=f"(v[104]), "=f"(v[105]), "=f"(v[106]), "=f"(v[107]), "=f"(v[108]), "=f"(v[109]),
+          "=f"(v[110]), "=f"(v[111]), "=f"(v[112]), "=f"(v[113]), "=f"(v[114]), "=f"(v[115]), "=f"(v[116]), "=f"(v[117]), "=f"(v[118]), "=f"(v[119]),
+          "=f"(v[120]), "=f"(v[121]), "=f"(v[122]), "=f"(v[123]), "=f"(v[124]), "=f"(v[125]), "=f"(v[126]), "=f"(v[127])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
+        ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
+          "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]),
+          "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]),
+          "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]), "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi);
+template <>
+__device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi) {
+    const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&b);
+}
+template <>
+__device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi) {
+    const __half2 b = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&b);
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(THREADS, 1)
+attend_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                     const __grid_constant__ CUtensorMap map_v, const PromptParams p) {
+    using S = Shape<DP>;
+    // which tiles: heads fastest, so that blocks that run together share K and V in L2; the tiles late in their
+    // sequences, which see the most keys, first
+    const int head = int(blockIdx.x % unsigned(p.hkv));
+    const unsigned rest = blockIdx.x / unsigned(p.hkv);
+    const int seq = int(rest % unsigned(p.n_seqs));
+    const int first = (p.tiles - 1 - int(rest / unsigned(p.n_seqs))) * 2 * p.TQ;      // first query token
+    const int q0 = p.cu_q[seq], lq = p.cu_q[seq + 1] - q0;
+    if (first >= lq) return;
+    const int k0 = p.cu_k[seq], lk = p.cu_k[seq + 1] - k0;
+    const int shift = lk - lq;                        // query j sees the keys 0 .. j + shift
+
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* tiles = reinterpret_cast<unsigned char*>((uintptr_t(smem_raw) + 1023) & ~uintptr_t(1023));
+    unsigned char* ring = tiles + 2 * S::TILE_BYTES;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(ring + S::STAGES * S::TILE_BYTES);
+    uint64_t* q_full = bars;                          // [2]
+    uint64_t* s_full = bars + 2;                      // [2] scores of a tile (and the product before) done
+    uint64_t* p_full = bars + 4;                      // [2] probabilities of a tile written
+    uint64_t* kv_full = bars + 6;                     // [STAGES]
+    uint64_t* kv_empty = bars + 6 + S::STAGES;        // [STAGES]
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 6 + 2 * S::STAGES);
+    __shared__ int s_abort;
+    volatile int* abort = &s_abort;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        s_abort = 0;
+        for (int i = 0; i < 2; ++i) { mbar_init(q_full + i, 1); mbar_init(s_full + i, 1); mbar_init(p_full + i, TM); }
+        for (int s = 0; s < S::STAGES; ++s) { mbar_init(kv_full + s, 1); mbar_init(kv_empty + s, 1); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(tmem_slot);
+
+    // blocks of keys that each tile sees
+    int nb[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int t0 = first + i * p.TQ, t1 = min(lq, t0 + p.TQ);
+        const int keys = t0 < t1 ? (p.causal ? min(lk, t1 + shift) : lk) : 0;
+        nb[i] = keys > 0 ? (keys + TN - 1) / TN : 0;
+    }
+    const int n_blk = max(nb[0], nb[1]);
+
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        if (warp == 8) {
+            // ---- loads
+            if (lane == 0 && n_blk > 0) {
+                const uint32_t q_bytes = uint32_t(S::BOXES) * p.G * p.TQ * BOX * 2;
+                for (int i = 0; i < 2; ++i)
+                    if (nb[i] > 0) {
+                        mbar_expect_tx(q_full + i, q_bytes);
+                        for (int b = 0; b < S::BOXES; ++b)
+                            tma_load_3d(tiles + i * S::TILE_BYTES + b * S::BOX_BYTES, &map_q, b * BOX, head * p.G, q0 + first + i * p.TQ, q_full + i);
+                    }
+                for (int it = 0; it < 2 * n_blk; ++it) {                 // K_0 V_0 K_1 V_1 ...
+                    const int s = it % S::STAGES, round = it / S::STAGES;
+                    if (round > 0 && !mbar_wait(kv_empty + s, (round - 1) & 1, abort)) break;
+                    mbar_expect_tx(kv_full + s, S::TILE_BYTES);
+                    for (int b = 0; b < S::BOXES; ++b)
+                        tma_load_3d(ring + s * S::TILE_BYTES + b * S::BOX_BYTES, it & 1 ? &map_v : &map_k, b * BOX, head, k0 + (it >> 1) * TN, kv_full + s);
+                }
+            }
+        } else if (warp == 9 && n_blk > 0) {
+            // ---- MMAs
+            uint64_t q_desc[2];
+            for (int i = 0; i < 2; ++i) q_desc[i] = smem_desc_sw128(tiles + i * S::TILE_BYTES);
+            auto scores = [&](int i, int it) {
+                if (lane == 0) {
+                    const uint64_t kd = smem_desc_sw128(ring + (it % S::STAGES) * S::TILE_BYTES);
+#pragma unroll
+                    for (int kk = 0; kk < DP / 16; ++kk) {
+                        const uint64_t off = uint64_t((kk / 4) * (S::BOX_BYTES >> 4) + (kk % 4) * 2);
+                        umma_ss(tmem + i * TN, q_desc[i] + off, kd + off, p.idesc_qk, kk > 0);
+                    }
+                }
+            };
+            bool ok = mbar_wait_warp(kv_full, 0, abort, lane);
+            tc_fence_after();
+            for (int i = 0; i < 2 && ok; ++i)
+                if (nb[i] > 0) {
+                    ok = mbar_wait_warp(q_full + i, 0, abort, lane);
+                    if (!ok) break;
+                    scores(i, 0);
+                    if (lane == 0) umma_commit(s_full + i);
+                }
+            // a place in the ring is reported free only where a load waits for it
+            const int n_loads = 2 * n_blk;
+            if (lane == 0 && S::STAGES < n_loads) umma_commit(kv_empty);
+            for (int j = 0; j < n_blk && ok; ++j) {
+                const int iv = 2 * j + 1, ik = 2 * j + 2;
+                unsigned char* v_tile = ring + (iv % S::STAGES) * S::TILE_BYTES;
+                if (!mbar_wait_warp(kv_full + iv % S::STAGES, (iv / S::STAGES) & 1, abort, lane)) break;
+                const bool more = j + 1 < n_blk;
+                if (more && !mbar_wait_warp(kv_full + ik % S::STAGES, (ik / S::STAGES) & 1, abort, lane)) break;
+                tc_fence_after();
+                const int left = lk - j * TN;
+                if (left < TN) {                       // rows beyond the sequence: zeros
+                    for (int r = left + (lane >> 3); r < TN; r += 4)
+#pragma unroll
+                        for (int b = 0; b < S::BOXES; ++b)
+                            *reinterpret_cast<uint4*>(v_tile + b * S::BOX_BYTES + r * 128 + (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                }
+                for (int i = 0; i < 2 && ok; ++i) {
+                    if (j >= nb[i]) continue;
+                    ok = mbar_wait_warp(p_full + i, j & 1, abort, lane);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (lane == 0) {
+                        const uint64_t vd = smem_desc_n_major(v_tile, S::BOX_BYTES);
+#pragma unroll
+                        for (int kk = 0; kk < TN / 16; ++kk)
+                            umma_ts(tmem + 2 * TN + i * DP, tmem + i * TN + kk * 8, vd + uint64_t(kk * (16 * 128 >> 4)), p.idesc_pv, j > 0 || kk > 0);
+                    }
+                    if (j + 1 < nb[i]) scores(i, ik);
+                    if (lane == 0) umma_commit(s_full + i);
+                }
+                if (lane == 0) {
+                    if (iv + S::STAGES < n_loads) umma_commit(kv_empty + iv % S::STAGES);
+                    if (ik + S::STAGES < n_loads) umma_commit(kv_empty + ik % S::STAGES);
+                }
+            }
+        }
+    } else {
+        // ---- softmax: this thread's query vector
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        const int i = warp >> 2;
+        const int m = (warp & 3) * 32 + lane;
+        const int tok = first + i * p.TQ + m / p.G, g = m % p.G;
+        const bool live = m < p.TQ * p.G && tok < lq;
+        const int sees = live ? (p.causal ? max(0, min(lk, tok + shift + 1)) : lk) : 0;
+        const uint32_t lane_bits = uint32_t((warp & 3) * 32) << 16;
+        const uint32_t s_tm = tmem + lane_bits + i * TN, o_tm = tmem + lane_bits + 2 * TN + i * DP;
+        float ref = -CUDART_INF_F, l = 0.f;           // ref in units of log2
+        bool ok = true;
+        for (int j = 0; j < nb[i]; ++j) {
+            ok = mbar_wait_warp(s_full + i, j & 1, abort, lane);
+            if (!ok) break;
+            tc_fence_after();
+            float s[TN];
+            tmem_ld128(s_tm, s);
+            const int left = sees - j * TN;           // keys of this block that the row sees
+            if (__any_sync(0xffffffffu, left < TN)) {
+#pragma unroll
+                for (int c = 0; c < TN; ++c) s[c] = c < left ? s[c] : -CUDART_INF_F;
+            }
+            float mx0 = s[0], mx1 = s[1], mx2 = s[2], mx3 = s[3];
+#pragma unroll
+            for (int c = 4; c < TN; c += 4) {
+                mx0 = fmaxf(mx0, s[c]);
+                mx1 = fmaxf(mx1, s[c + 1]);
+                mx2 = fmaxf(mx2, s[c + 2]);
+                mx3 = fmaxf(mx3, s[c + 3]);
+            }
+            const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * p.c2;
+            const bool move = mx > ref + SLACK;       // also at the first finite maximum
+            if (__any_sync(0xffffffffu, move)) {
+                const float f = move ? (ref > -CUDART_INF_F ? ex2_approx(ref - mx) : 0.f) : 1.f;
+                if (move) ref = mx;
+                l *= f;
+                if (j > 0) {
+#pragma unroll 1
+                    for (int c = 0; c < DP; c += 32) {
+                        uint32_t o[32];
+                        tmem_ld32(o_tm + c, o);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                        tmem_st32(o_tm + c, o);
+                    }
+                }
+            }
+            const float base = ref > -CUDART_INF_F ? ref : 0.f;
+            float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t pk[32];
+#pragma unroll
+                for (int c = 0; c < 32; ++c) {
+                    const float a = ex2_approx(fmaf(s[h * 64 + 2 * c], p.c2, -base));
+                    const float b = ex2_approx(fmaf(s[h * 64 + 2 * c + 1], p.c2, -base));
+                    l0 += a;
+                    l1 += b;
+                    pk[c] = pack2<T>(a, b);
+                }
+                tmem_st32(s_tm + h * 32, pk);
+            }
+            l += l0 + l1;
+            tmem_wait_st();
+            tc_fence_before();
+            mbar_arrive(p_full + i);
+        }
+        if (ok && nb[i] > 0) {
+            ok = mbar_wait_warp(s_full + i, nb[i] & 1, abort, lane);
+            tc_fence_after();
+        }
+        if (ok) {
+            const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+            const int64_t at = int64_t(q0 + tok) * p.hq + head * p.G + g;
+            unsigned char* dst = p.out + at * p.D * 2;
+#pragma unroll 1
+            for (int c = 0; c < DP; c += 32) {
+                uint32_t o[32];
+                if (nb[i] > 0) tmem_ld32(o_tm + c, o);
+#pragma unroll
+                for (int e = 0; e < 32; e += 8) {
+                    uint4 w = make_uint4(0, 0, 0, 0);
+                    if (sees > 0) {
+                        w.x = pack2<T>(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
+                        w.y = pack2<T>(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
+                        w.z = pack2<T>(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv);
+                        w.w = pack2<T>(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
+                    }
+                    if (live && c + e < p.D) *reinterpret_cast<uint4*>(dst + (c + e) * 2) = w;
+                }
+            }
+            if (live && p.lse) p.lse[at] = l > 0.f ? (ref + log2f(l)) * LN2_F : (l == 0.f ? -CUDART_INF_F : l);
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (s_abort && threadIdx.x == 0) {
+        atomicExch(p.error, 1u);
+        for (int i = 0; i < 200; ++i) __nanosleep(1000);          // copies in flight land before the memory is given up
+    }
+    __syncthreads();
+    if (warp == 9) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
+}
+
+// [tokens][heads][D] as a 3-D tensor map, innermost first
+int make_map3(EncodeTiled enc, CUtensorMap* map, CUtensorMapDataType type, const void* base, int64_t tokens, int32_t heads, int32_t D,
+              int64_t token_stride, int64_t head_stride, int box_heads, int box_tokens) {
+    const cuuint64_t dims[3] = {cuuint64_t(D), cuuint64_t(heads), cuuint64_t(tokens)};
+    const cuuint64_t strides[2] = {cuuint64_t(head_stride) * 2, cuuint64_t(token_stride) * 2};
+    const cuuint32_t box[3] = {cuuint32_t(BOX), cuuint32_t(box_heads), cuuint32_t(box_tokens)};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    const CUresult r = enc(map, type, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? DISC_OK : DISC_ERR_UNSUPPORTED;
+}
+
+template <typename T, int DP>
+int launch_prompt(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const PromptParams& p, unsigned grid, cudaStream_t st) {
+    static std::atomic<uint64_t> done{0};
+    if (const int rc = allow_smem(attend_prompt_kernel<T, DP>, Shape<DP>::SMEM, done)) return rc;
+    attend_prompt_kernel<T, DP><<<grid, THREADS, Shape<DP>::SMEM, st>>>(q, k, v, p);
+    DISC_CUDA(cudaGetLastError());
+    return DISC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int disc_attend_prompt(const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride,
+                       int64_t k_head_stride, const void* v, int64_t v_token_stride, int64_t v_head_stride, disc_dtype_t dtype,
+                       int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t n_q, int64_t n_k, const int32_t* cu_q,
+                       const int32_t* cu_k, int32_t n_seqs, int32_t max_q, int32_t causal, float scale, void* out, float* lse_out,
+                       uint32_t* error, void* stream) {
+    if (n_q_heads <= 0 || n_kv_heads <= 0 || head_dim <= 0 || n_q < 0 || n_k < 0 || n_seqs < 0 || max_q < 0) return DISC_ERR_ARG;
+    if (dtype != DISC_BF16 && dtype != DISC_F16) return DISC_ERR_UNSUPPORTED;
+    if (n_q_heads % n_kv_heads || !(scale > 0.f) || !(scale <= 3.0e38f)) return DISC_ERR_ARG;
+    if (head_dim % 8 || head_dim > DISC_MAX_HEAD_DIM || n_q_heads / n_kv_heads > TM || n_q >= (int64_t(1) << 31) - 512 ||
+        n_k >= (int64_t(1) << 31) - 512)
+        return DISC_ERR_UNSUPPORTED;
+    if (n_q == 0 || n_seqs == 0 || max_q == 0) return DISC_OK;
+    if (!q || !out || !cu_q || !error || (n_k > 0 && (!k || !v))) return DISC_ERR_ARG;
+    if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(out)) & 15u)
+        return DISC_ERR_ARG;
+    // without the keys' own offsets they are the queries'
+    if (!cu_k && n_k != n_q) return DISC_ERR_ARG;
+    // TMA: strides in multiples of 16 bytes.  The stride over an axis of one is never used; any valid one will do.
+    const int64_t fit = (int64_t(head_dim) + 7) / 8 * 8;
+    if (n_q_heads == 1) q_head_stride = fit;
+    if (n_kv_heads == 1) k_head_stride = v_head_stride = fit;
+    if (n_q == 1) q_token_stride = fit * n_q_heads;
+    if (n_k <= 1) k_token_stride = v_token_stride = fit * n_kv_heads;
+    if ((q_token_stride | q_head_stride | k_token_stride | k_head_stride | v_token_stride | v_head_stride) & 7) return DISC_ERR_UNSUPPORTED;
+    if (q_token_stride <= 0 || q_head_stride <= 0 || k_token_stride <= 0 || k_head_stride <= 0 || v_token_stride <= 0 || v_head_stride <= 0)
+        return DISC_ERR_UNSUPPORTED;
+    const int G = n_q_heads / n_kv_heads, TQ = TM / G;
+    PromptParams p;
+    p.cu_q = cu_q; p.cu_k = cu_k ? cu_k : cu_q; p.n_seqs = n_seqs; p.hq = n_q_heads; p.hkv = n_kv_heads; p.G = G; p.TQ = TQ; p.D = head_dim;
+    p.causal = causal != 0; p.c2 = scale * LOG2E_F; p.out = static_cast<unsigned char*>(out); p.lse = lse_out; p.error = error;
+    const int64_t longest = max_q < n_q ? max_q : n_q;
+    p.tiles = int32_t((longest + 2 * TQ - 1) / (2 * TQ));
+    const int64_t grid = int64_t(p.tiles) * n_seqs * n_kv_heads;
+    if (grid > 0x7fffffff) return DISC_ERR_UNSUPPORTED;
+    const int DP = head_dim <= 64 ? 64 : 128;
+    // instruction descriptors: D fp32 (bits 4-5 = 1), A and B f16 = 0 / bf16 = 1 (bits 7-9, 10-12), B of the second
+    // product N-major (bit 16), N >> 3 at bit 17, M >> 4 at bit 24
+    const uint32_t ty = dtype == DISC_BF16 ? 1u : 0u;
+    const uint32_t idesc = (1u << 4) | (ty << 7) | (ty << 10) | (uint32_t(TM >> 4) << 24);
+    p.idesc_qk = idesc | (uint32_t(TN >> 3) << 17);
+    p.idesc_pv = idesc | (uint32_t(DP >> 3) << 17) | (1u << 16);
+
+    EncodeTiled enc = nullptr;
+    if (const int rc = tensor_map_encoder(&enc)) return rc;
+    const CUtensorMapDataType type = dtype == DISC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    alignas(64) CUtensorMap map_q, map_k, map_v;
+    if (const int rc = make_map3(enc, &map_q, type, q, n_q, n_q_heads, head_dim, q_token_stride, q_head_stride, G, TQ)) return rc;
+    // no keys at all: no load is issued, and any valid map will do
+    const bool none = n_k == 0;
+    if (const int rc = make_map3(enc, &map_k, type, none ? q : k, none ? 1 : n_k, n_kv_heads, head_dim, k_token_stride, k_head_stride, 1, TN)) return rc;
+    if (const int rc = make_map3(enc, &map_v, type, none ? q : v, none ? 1 : n_k, n_kv_heads, head_dim, v_token_stride, v_head_stride, 1, TN)) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (dtype == DISC_BF16)
+        return DP == 64 ? launch_prompt<__nv_bfloat16, 64>(map_q, map_k, map_v, p, unsigned(grid), st)
+                        : launch_prompt<__nv_bfloat16, 128>(map_q, map_k, map_v, p, unsigned(grid), st);
+    return DP == 64 ? launch_prompt<__half, 64>(map_q, map_k, map_v, p, unsigned(grid), st)
+                    : launch_prompt<__half, 128>(map_q, map_k, map_v, p, unsigned(grid), st);
+}
+
+int disc_attend_error(const uint32_t* error, void* stream) {
+    if (!error) return DISC_ERR_ARG;
+    uint32_t e = 0;
+    DISC_CUDA(cudaMemcpyAsync(&e, error, 4, cudaMemcpyDeviceToHost, static_cast<cudaStream_t>(stream)));
+    DISC_CUDA(cudaStreamSynchronize(static_cast<cudaStream_t>(stream)));
+    return e ? DISC_ERR_CUDA : DISC_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,272 @@
+"""Binding of the operators the language model around the decoding step runs (include/disc.h):
+attention over prompts, the paged key-value cache and attention over it, log-probabilities.
+
+Argument marshalling only, like binding.py; there is no CPU fallback.
+"""
+from __future__ import annotations
+
+import ctypes as C
+import math
+
+import torch
+
+from .binding import DISC_BF16, DISC_F16, DISC_F32, DiscError, _Cache, _check, _dev, _stream_ptr, lib
+
+_HALF = {torch.bfloat16: DISC_BF16, torch.float16: DISC_F16}
+_LOGIT = {torch.float32: DISC_F32, torch.bfloat16: DISC_BF16}
+
+
+def _vectors(t: torch.Tensor, dtype, name: str):
+    """A CUDA tensor [tokens, heads, head_dim] whose innermost axis is contiguous."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.ndim == 3
+            and (t.stride(2) == 1 or t.shape[2] == 1)):
+        raise TypeError(f"{name}: expected a CUDA tensor [tokens, heads, head_dim] of {dtype} with unit inner stride")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def _rows(t: torch.Tensor, name: str):
+    """Logits [n, V]: (pointer, dtype code, row stride)."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.ndim == 2 and (t.stride(1) == 1 or t.shape[1] == 1)):
+        raise TypeError(f"{name}: expected a CUDA tensor [n, V] with unit inner stride")
+    if t.dtype not in _LOGIT:
+        raise DiscError(-7, name)
+    return t.data_ptr(), _LOGIT[t.dtype], t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _want(t, n: int, name: str):
+    if t is not None and t.numel() != n:
+        raise TypeError(f"{name}: expected {n} entries, got {t.numel()}")
+
+
+# ---- log-probabilities ------------------------------------------------------------------------------
+def disc_logprobs(logits: torch.Tensor, targets: torch.Tensor | None = None, *, top: int = 0, inv_temperature=1.0,
+                  out=None, stream=None):
+    """logits [n, V] float32 or bfloat16 (any row stride), targets int32[n] (-1 = none) ->
+    dict(logp, entropy, lse float[n], top_ids int32[n, top], top_logp float[n, top], status uint8[n])."""
+    ptr, dt, ld = _rows(logits, "disc_logprobs")
+    n, V = logits.shape
+    _want(targets, n, "targets")
+    if out is None:
+        f = dict(dtype=torch.float32, device=logits.device)
+        out = {"logp": torch.empty(n, **f) if targets is not None else None, "entropy": torch.empty(n, **f),
+               "lse": torch.empty(n, **f),
+               "top_ids": torch.empty((n, top), dtype=torch.int32, device=logits.device) if top > 0 else None,
+               "top_logp": torch.empty((n, top), **f) if top > 0 else None,
+               "status": torch.empty(n, dtype=torch.uint8, device=logits.device)}
+    rc = lib().disc_logprobs(ptr, dt, ld, n, V, float(inv_temperature), _dev(targets, torch.int32, "targets"), int(top),
+                             _dev(out["logp"], torch.float32, "logp"), _dev(out["entropy"], torch.float32, "entropy"),
+                             _dev(out["lse"], torch.float32, "lse"), _dev(out["top_ids"], torch.int32, "top_ids"),
+                             _dev(out["top_logp"], torch.float32, "top_logp"), _dev(out["status"], torch.uint8, "status"),
+                             _stream_ptr(stream))
+    _check(rc, "disc_logprobs")
+    return out
+
+
+def disc_logprobs_grad(logits: torch.Tensor, targets, lse: torch.Tensor, entropy, d_logp, d_entropy=None, *,
+                       inv_temperature=1.0, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The gradient of sum(d_logp * logp + d_entropy * entropy) with respect to the logits, in their dtype.
+    lse, entropy: what disc_logprobs gave for these logits.  out may be `logits` itself."""
+    ptr, dt, ld = _rows(logits, "disc_logprobs_grad")
+    n, V = logits.shape
+    for t, name in ((targets, "targets"), (lse, "lse"), (entropy, "entropy"), (d_logp, "d_logp"), (d_entropy, "d_entropy")):
+        _want(t, n, name)
+    if out is None:
+        out = torch.empty((n, V), dtype=logits.dtype, device=logits.device)
+    elif out.shape != logits.shape or out.dtype != logits.dtype:
+        raise TypeError("out: expected the shape and dtype of the logits")
+    optr, _, old = _rows(out, "out")
+    rc = lib().disc_logprobs_grad(ptr, dt, ld, n, V, float(inv_temperature), _dev(targets, torch.int32, "targets"),
+                                  _dev(lse, torch.float32, "lse"), _dev(entropy, torch.float32, "entropy"),
+                                  _dev(d_logp, torch.float32, "d_logp"), _dev(d_entropy, torch.float32, "d_entropy"),
+                                  optr, old, _stream_ptr(stream))
+    _check(rc, "disc_logprobs_grad")
+    return out
+
+
+# ---- attention over prompts -------------------------------------------------------------------------
+_error_words: dict = {}
+
+
+def _error_word(device: torch.device) -> torch.Tensor:
+    """The word an attention kernel sets when a bounded wait ran out, one per device."""
+    w = _error_words.get(device)
+    if w is None:
+        w = _error_words[device] = torch.zeros(1, dtype=torch.int32, device=device)
+        torch.cuda.synchronize(device)          # zero before any other stream uses it
+    return w
+
+
+def disc_attend_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, cu_k=None, *, max_len: int,
+                       scale: float | None = None, causal: bool = True, out=None, lse=None, stream=None):
+    """Attention over packed sequences: q [n_q, Hq, D], k and v [n_k, Hkv, D] (bf16 or f16, slices of a fused projection are
+    fine), cu_q / cu_k int32[n_seqs + 1] on the device (cu_k None: the same sequences), max_len: no sequence
+    has more queries -> (out [n_q, Hq, D], lse float[n_q, Hq])."""
+    dt = _HALF.get(q.dtype)
+    if dt is None:
+        raise DiscError(-7, "disc_attend_prompt")
+    qp, qt, qh = _vectors(q, q.dtype, "q")
+    kp, kt, kh = _vectors(k, q.dtype, "k")
+    vp, vt, vh = _vectors(v, q.dtype, "v")
+    if k.shape != v.shape or k.shape[2] != q.shape[2]:
+        raise TypeError("k, v: expected the same shape [n_k, Hkv, D] with q's head dim")
+    n_seqs = cu_q.numel() - 1
+    if cu_k is not None:
+        _want(cu_k, n_seqs + 1, "cu_k")
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape:
+        raise TypeError("out: expected q's shape")
+    if lse is None:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    elif lse.shape != q.shape[:2]:
+        raise TypeError("lse: expected [n_q, Hq]")
+    rc = lib().disc_attend_prompt(qp, qt, qh, kp, kt, kh, vp, vt, vh, dt, q.shape[1], k.shape[1], q.shape[2], q.shape[0],
+                                  k.shape[0], _dev(cu_q, torch.int32, "cu_q"), _dev(cu_k, torch.int32, "cu_k"), n_seqs,
+                                  int(max_len), int(causal), 1.0 / math.sqrt(q.shape[2]) if scale is None else float(scale),
+                                  _dev(out, q.dtype, "out"), _dev(lse, torch.float32, "lse"), _error_word(q.device).data_ptr(),
+                                  _stream_ptr(stream))
+    _check(rc, "disc_attend_prompt")
+    return out, lse
+
+
+def disc_attend_check(device="cuda", stream=None):
+    """Synchronises and raises DiscError when an attention kernel on the device gave up on one of its bounded waits."""
+    dev = torch.device(device)
+    if dev.index is None:
+        dev = torch.device(dev.type, torch.cuda.current_device())
+    _check(lib().disc_attend_error(_error_word(dev).data_ptr(), _stream_ptr(stream)), "disc_attend_error")
+
+
+# ---- the key-value cache ----------------------------------------------------------------------------
+class DiscCache:
+    """A key-value cache in pages: pool [layers, 2, pages, kv heads, page size, head dim] (bf16 or f16) and its
+    books, one int32 buffer holding the page table [rows, table_width], the lengths [rows] and the reference
+    counts [pages].  Without `book` the cache starts empty; a given buffer is used as it is."""
+
+    def __init__(self, pool: torch.Tensor, n_rows: int, table_width: int, *, book: torch.Tensor | None = None):
+        if not (isinstance(pool, torch.Tensor) and pool.is_cuda and pool.ndim == 6 and pool.shape[1] == 2 and pool.is_contiguous()):
+            raise TypeError("pool: expected a contiguous CUDA tensor [layers, 2, pages, kv heads, page size, head dim]")
+        if pool.dtype not in _HALF:
+            raise DiscError(-7, "DiscCache")
+        self.pool, self.n_rows, self.table_width = pool, int(n_rows), int(table_width)
+        self.n_layers, _, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = pool.shape
+        a, b = self.n_rows * self.table_width, self.n_rows * self.table_width + self.n_rows
+        if book is None:
+            book = torch.zeros(b + self.n_pages, dtype=torch.int32, device=pool.device)
+            book[:a] = -1
+        if not (book.is_cuda and book.dtype == torch.int32 and book.is_contiguous() and book.numel() == b + self.n_pages):
+            raise TypeError(f"book: expected a contiguous int32 CUDA tensor of {b + self.n_pages} entries")
+        self.book = book
+        self.table, self.len, self.ref = book[:a].view(self.n_rows, self.table_width), book[a:b], book[b:]
+        self._c = _Cache(pool.data_ptr(), self.table.data_ptr(), self.len.data_ptr(), self.ref.data_ptr(), None, 0,
+                         self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim, self.n_rows,
+                         self.table_width, _HALF[pool.dtype])
+        self._p = C.addressof(self._c)
+        need = lib().disc_cache_scratch_bytes(self._p)
+        if need < 0:
+            raise DiscError(int(need), "disc_cache_scratch_bytes")
+        self._scratch = torch.empty(int(need), dtype=torch.uint8, device=pool.device)
+        self._c.scratch, self._c.scratch_bytes = self._scratch.data_ptr(), int(need)
+        self._plans: dict = {}
+
+    @staticmethod
+    def empty(n_layers: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, n_rows: int, table_width: int, *,
+              dtype=torch.bfloat16, device="cuda") -> "DiscCache":
+        pool = torch.zeros((n_layers, 2, n_pages, n_kv_heads, page_size, head_dim), dtype=dtype, device=device)
+        return DiscCache(pool, n_rows, table_width)
+
+
+def disc_cache_fork(cache: DiscCache, parent: torch.Tensor, stream=None):
+    """Row r becomes what row parent[r] was (int32[n_rows] on the device; outside [0, n_rows): emptied)."""
+    _want(parent, cache.n_rows, "parent")
+    _check(lib().disc_cache_fork(cache._p, _dev(parent, torch.int32, "parent"), _stream_ptr(stream)), "disc_cache_fork")
+
+
+def disc_cache_free(cache: DiscCache, freed: torch.Tensor, stream=None):
+    """The rows with freed[r] != 0 (uint8[n_rows] on the device) become empty."""
+    _want(freed, cache.n_rows, "freed")
+    _check(lib().disc_cache_free(cache._p, _dev(freed, torch.uint8, "freed"), _stream_ptr(stream)), "disc_cache_free")
+
+
+def disc_cache_extend(cache: DiscCache, add: torch.Tensor | None = None, *, status: torch.Tensor | None = None,
+                      stream=None) -> torch.Tensor:
+    """Room for add[r] more tokens in every row (int32[n_rows] on the device, None: one each) -> status uint8[n_rows]."""
+    _want(add, cache.n_rows, "add")
+    if status is None:
+        status = torch.empty(cache.n_rows, dtype=torch.uint8, device=cache.pool.device)
+    _want(status, cache.n_rows, "status")
+    _check(lib().disc_cache_extend(cache._p, _dev(add, torch.int32, "add"), _dev(status, torch.uint8, "status"),
+                                   _stream_ptr(stream)), "disc_cache_extend")
+    return status
+
+
+def disc_cache_write(cache: DiscCache, layer: int, k: torch.Tensor, v: torch.Tensor, *, cu: torch.Tensor | None = None,
+                     rows: torch.Tensor | None = None, status: torch.Tensor | None = None, stream=None):
+    """k, v [tokens, kv heads, head dim]: the newest tokens of sequence i (row rows[i], None: row i) are
+    cu[i] .. cu[i+1]-1 (None: one token each)."""
+    kp, kt, kh = _vectors(k, cache.pool.dtype, "k")
+    vp, vt, vh = _vectors(v, cache.pool.dtype, "v")
+    if k.shape != v.shape or tuple(k.shape[1:]) != (cache.n_kv_heads, cache.head_dim):
+        raise TypeError("k, v: expected [tokens, kv heads, head dim] of the cache")
+    n_seqs = k.shape[0] if cu is None else cu.numel() - 1
+    if rows is not None:
+        _want(rows, n_seqs, "rows")
+    _want(status, cache.n_rows, "status")
+    _check(lib().disc_cache_write(cache._p, int(layer), kp, kt, kh, vp, vt, vh, k.shape[0], _dev(cu, torch.int32, "cu"), n_seqs,
+                                  _dev(rows, torch.int32, "rows"), _dev(status, torch.uint8, "status"), _stream_ptr(stream)),
+           "disc_cache_write")
+
+
+def disc_cache_compact(cache: DiscCache, *, live: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The n pages in use move to the ids 0 .. n-1 -> n as int32[1] on the device."""
+    if live is None:
+        live = torch.empty(1, dtype=torch.int32, device=cache.pool.device)
+    _check(lib().disc_cache_compact(cache._p, _dev(live, torch.int32, "live"), _stream_ptr(stream)), "disc_cache_compact")
+    return live
+
+
+# ---- attention of one new token per row ---------------------------------------------------------------
+class AttendPlan:
+    """Buffer of a plan (disc_attend_plan) and what it was made for."""
+
+    def __init__(self, cache: DiscCache, n_q_heads: int, group: int):
+        need = lib().disc_attend_plan_bytes(cache._p, int(n_q_heads), int(group))
+        if need < 0:
+            raise DiscError(int(need), "disc_attend_plan_bytes")
+        self.n_q_heads, self.group, self.nbytes = int(n_q_heads), int(group), int(need)
+        self.buf = torch.empty(self.nbytes, dtype=torch.uint8, device=cache.pool.device)
+
+
+def disc_attend_plan(cache: DiscCache, n_q_heads: int, *, group: int = 1, plan: AttendPlan | None = None,
+                     stream=None) -> AttendPlan:
+    """The plan of one position for all layers: `group` consecutive rows (the K candidates of a query) may share
+    leading pages.  Without `plan` the cache's own buffer for these sizes is used (and reused)."""
+    if plan is None:
+        plan = cache._plans.get((n_q_heads, group))
+        if plan is None:
+            plan = cache._plans[(n_q_heads, group)] = AttendPlan(cache, n_q_heads, group)
+    _check(lib().disc_attend_plan(cache._p, plan.n_q_heads, plan.group, plan.buf.data_ptr(), plan.nbytes, _stream_ptr(stream)),
+           "disc_attend_plan")
+    return plan
+
+
+def disc_attend_cached(cache: DiscCache, layer: int, q: torch.Tensor, plan: AttendPlan, *, scale: float | None = None,
+                       out=None, lse=None, stream=None):
+    """One new token per row: q [rows, Hq, D] against the row's tokens in layer `layer` -> (out [rows, Hq, D],
+    lse float[rows, Hq])."""
+    qp, qr, qh = _vectors(q, cache.pool.dtype, "q")
+    if tuple(q.shape) != (cache.n_rows, plan.n_q_heads, cache.head_dim):
+        raise TypeError("q: expected [rows, Hq, head dim] of the cache and the plan")
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape:
+        raise TypeError("out: expected q's shape")
+    if lse is None:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    elif lse.shape != q.shape[:2]:
+        raise TypeError("lse: expected [rows, Hq]")
+    _check(lib().disc_attend_cached(cache._p, int(layer), qp, qr, qh, plan.n_q_heads, plan.group,
+                                    1.0 / math.sqrt(cache.head_dim) if scale is None else float(scale), plan.buf.data_ptr(),
+                                    plan.nbytes, _dev(out, q.dtype, "out"), _dev(lse, torch.float32, "lse"),
+                                    _stream_ptr(stream)), "disc_attend_cached")
+    return out, lse
