@@ -162,9 +162,12 @@ struct RowShape {
 struct Sums {
     float m, ref, s, u;               // largest logit, its y; sums relative to ref
 };
+// A logit so far out that its y has no place in fp32 (a mask of the type's lowest value) counts as FAR: sums relative to
+// such a maximum stay finite, but mean nothing until a nearer one comes.
+constexpr float FAR_Y = 1.0e38f;
 __device__ __forceinline__ void raise(Sums& a, float m_new, float c2) {
-    const float ref = fabsf(m_new) < CUDART_INF_F ? m_new * c2 : 0.f;
-    const float d = a.m > -CUDART_INF_F ? a.ref - ref : Y_MIN;
+    const float ref = fabsf(m_new) < CUDART_INF_F ? fminf(fmaxf(m_new * c2, -FAR_Y), FAR_Y) : 0.f;
+    const float d = a.m > -CUDART_INF_F ? fmaxf(a.ref - ref, Y_MIN) : Y_MIN;
     const float f = ex2_approx(d);
     a.u = f * fmaf(d, a.s, a.u);
     a.s *= f;
@@ -461,7 +464,25 @@ __global__ void __launch_bounds__(NT, 4) disc_logprobs_kernel(const LogprobParam
     }
     __syncthreads();
 
-    const Sums t = sm.part;
+    Sums t = sm.part;
+    bool far = fabsf(t.m) < CUDART_INF_F && fabsf(t.m * p.c2) >= FAR_Y && t.s == t.s;
+    if (far) {                        // the largest logit itself is that far out: once more, with differences of logits
+        Sums b{t.m, 0.f, 0.f, 0.f};
+        for (int32_t e = tid; e < p.V; e += NT) {
+            const float d = max_nan((Vec<DT>::at(r.base + size_t(e) * SIZE) - t.m) * p.c2, Y_MIN), x = ex2_approx(d);
+            b.s += x;
+            b.u = fmaf(d, x, b.u);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            b.s += __shfl_xor_sync(FULL, b.s, o);
+            b.u += __shfl_xor_sync(FULL, b.u, o);
+        }
+        if (lane == 0) sm.warp_sums[warp] = b;
+        __syncthreads();
+        t.s = t.u = 0.f;
+        for (int w = 0; w < NW; ++w) { t.s += sm.warp_sums[w].s; t.u += sm.warp_sums[w].u; }
+    }
     uint8_t status = 0;
     float lse, h;
     if (t.s != t.s || t.u != t.u || t.m == CUDART_INF_F) {
@@ -474,7 +495,7 @@ __global__ void __launch_bounds__(NT, 4) disc_logprobs_kernel(const LogprobParam
         h = 0.f;
     } else {
         const float l2 = log2f(t.s);
-        lse = fmaf(t.ref, LN2_F, l2 * LN2_F);
+        lse = far ? fmaf(t.m, p.inv_t, l2 * LN2_F) : fmaf(t.ref, LN2_F, l2 * LN2_F);
         h = fmaxf(0.f, LN2_F * (l2 - t.u / t.s));
     }
     if (tid == 0) {
@@ -529,8 +550,9 @@ struct GradParams {
 
 struct RowGrad {
     float l2, a_bh, b, scale;         // lse in units of y; a + b H; b ln2; 1/T
+    float far_lse;                    // lse where l2 has no place in fp32, otherwise 0
     __device__ __forceinline__ float at(float x, float c2) const {
-        const float y = max_nan(fmaf(x, c2, -l2), Y_MIN);
+        const float y = max_nan(far_lse == 0.f ? fmaf(x, c2, -l2) : fmaf(x, scale, -far_lse) * LOG2E_F, Y_MIN);
         return -scale * ex2_approx(y) * fmaf(y, b, a_bh);
     }
 };
@@ -552,6 +574,7 @@ __global__ void __launch_bounds__(NT) disc_logprobs_grad_kernel(const GradParams
     g.a_bh = b != 0.f ? fmaf(b, p.entropy[row], a) : a;
     g.b = b * LN2_F;
     g.scale = p.inv_t;
+    g.far_lse = fabsf(g.l2) >= FAR_Y && fabsf(lse) < CUDART_INF_F ? lse : 0.f;
     if (lse == -CUDART_INF_F) { g.l2 = 0.f; g.scale = 0.f; }      // no mass: nothing to move
     const float a_t = g.scale * a;
 
