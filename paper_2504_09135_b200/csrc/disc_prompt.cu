@@ -46,6 +46,7 @@ constexpr int TM = 128;                  // query vectors of a tile
 constexpr int TN = 128;                  // keys of a block
 constexpr int THREADS = 384;
 constexpr int BOX = 64;                  // values of a row in one 128-byte swizzled box
+constexpr int FIRST = 96;                // keys whose probabilities are handed over first
 constexpr float SLACK = 8.f;             // log2 of the growth a row's sums take before the reference moves
 
 template <int DP>
@@ -140,6 +141,13 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* v) {
           "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]), "r"(taddr)
         : "memory");
 }
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+        ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
+          "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(taddr)
+        : "memory");
+}
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 template <typename T>
@@ -153,6 +161,40 @@ template <>
 __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi) {
     const __half2 b = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&b);
+}
+
+// two fp32 operations in one instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(reinterpret_cast<unsigned long long&>(d))
+        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)), "l"(reinterpret_cast<unsigned long long&>(c)));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("add.rn.f32x2 %0, %1, %2;"
+        : "=l"(reinterpret_cast<unsigned long long&>(d))
+        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
+    return d;
+}
+// the largest of three, NaN if any is
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// 32 scores -> probabilities 2^(s c2 + shift): their sum is added to l, 16 packed pairs go to pk
+template <typename T>
+__device__ __forceinline__ void exp_chunk(const float* s, float2 c2, float2 shift, float2& l, uint32_t* pk) {
+#pragma unroll
+    for (int c = 0; c < 16; ++c) {
+        float2 x = fma2(make_float2(s[2 * c], s[2 * c + 1]), c2, shift);
+        x.x = ex2_approx(x.x);
+        x.y = ex2_approx(x.y);
+        l = add2(l, x);
+        pk[c] = pack2<T>(x.x, x.y);
+    }
 }
 
 template <typename T, int DP>
@@ -177,17 +219,17 @@ attend_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     uint64_t* bars = reinterpret_cast<uint64_t*>(ring + S::STAGES * S::TILE_BYTES);
     uint64_t* q_full = bars;                          // [2]
     uint64_t* s_full = bars + 2;                      // [2] scores of a tile (and the product before) done
-    uint64_t* p_full = bars + 4;                      // [2] probabilities of a tile written
-    uint64_t* kv_full = bars + 6;                     // [STAGES]
-    uint64_t* kv_empty = bars + 6 + S::STAGES;        // [STAGES]
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 6 + 2 * S::STAGES);
+    uint64_t* p_full = bars + 4;                      // [2][2] probabilities of a tile written: the first 96 keys, the last 32
+    uint64_t* kv_full = bars + 8;                     // [STAGES]
+    uint64_t* kv_empty = bars + 8 + S::STAGES;        // [STAGES]
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 8 + 2 * S::STAGES);
     __shared__ int s_abort;
     volatile int* abort = &s_abort;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         s_abort = 0;
-        for (int i = 0; i < 2; ++i) { mbar_init(q_full + i, 1); mbar_init(s_full + i, 1); mbar_init(p_full + i, TM); }
+        for (int i = 0; i < 2; ++i) { mbar_init(q_full + i, 1); mbar_init(s_full + i, 1); mbar_init(p_full + 2 * i, TM / 32); mbar_init(p_full + 2 * i + 1, TM / 32); }
         for (int s = 0; s < S::STAGES; ++s) { mbar_init(kv_full + s, 1); mbar_init(kv_empty + s, 1); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -232,39 +274,40 @@ attend_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             }
         } else if (warp == 9 && n_blk > 0) {
             // ---- MMAs
-            uint64_t q_desc[2];
-            for (int i = 0; i < 2; ++i) q_desc[i] = smem_desc_sw128(tiles + i * S::TILE_BYTES);
+            const uint64_t q_desc[2] = {smem_desc_sw128(tiles), smem_desc_sw128(tiles + S::TILE_BYTES)};
+            const uint64_t kv_desc = smem_desc_sw128(ring), v_desc = smem_desc_n_major(ring, S::BOX_BYTES);
+            constexpr uint64_t TILE16 = S::TILE_BYTES >> 4;
+            const int n_loads = 2 * n_blk;
+            // S_i = Q_i K^T with the keys of load `it`
             auto scores = [&](int i, int it) {
-                if (lane == 0) {
-                    const uint64_t kd = smem_desc_sw128(ring + (it % S::STAGES) * S::TILE_BYTES);
+                const uint64_t kd = kv_desc + uint64_t(it % S::STAGES) * TILE16;
 #pragma unroll
-                    for (int kk = 0; kk < DP / 16; ++kk) {
-                        const uint64_t off = uint64_t((kk / 4) * (S::BOX_BYTES >> 4) + (kk % 4) * 2);
-                        umma_ss(tmem + i * TN, q_desc[i] + off, kd + off, p.idesc_qk, kk > 0);
-                    }
+                for (int kk = 0; kk < DP / 16; ++kk) {
+                    const uint64_t off = uint64_t((kk / 4) * (S::BOX_BYTES >> 4) + (kk % 4) * 2);
+                    umma_ss(tmem + i * TN, q_desc[i] + off, kd + off, p.idesc_qk, kk > 0);
                 }
             };
-            bool ok = mbar_wait_warp(kv_full, 0, abort, lane);
-            tc_fence_after();
+            bool ok = mbar_wait_all(kv_full, 0, abort);
             for (int i = 0; i < 2 && ok; ++i)
                 if (nb[i] > 0) {
-                    ok = mbar_wait_warp(q_full + i, 0, abort, lane);
+                    ok = mbar_wait_all(q_full + i, 0, abort);
                     if (!ok) break;
-                    scores(i, 0);
-                    if (lane == 0) umma_commit(s_full + i);
+                    tc_fence_after();
+                    if (elect_one()) {
+                        scores(i, 0);
+                        umma_commit(s_full + i);
+                    }
                 }
             // a place in the ring is reported free only where a load waits for it
-            const int n_loads = 2 * n_blk;
-            if (lane == 0 && S::STAGES < n_loads) umma_commit(kv_empty);
+            if (ok && S::STAGES < n_loads && elect_one()) umma_commit(kv_empty);
             for (int j = 0; j < n_blk && ok; ++j) {
                 const int iv = 2 * j + 1, ik = 2 * j + 2;
-                unsigned char* v_tile = ring + (iv % S::STAGES) * S::TILE_BYTES;
-                if (!mbar_wait_warp(kv_full + iv % S::STAGES, (iv / S::STAGES) & 1, abort, lane)) break;
-                const bool more = j + 1 < n_blk;
-                if (more && !mbar_wait_warp(kv_full + ik % S::STAGES, (ik / S::STAGES) & 1, abort, lane)) break;
-                tc_fence_after();
+                const int v_stage = iv % S::STAGES, k_stage = ik % S::STAGES;
+                if (!mbar_wait_all(kv_full + v_stage, (iv / S::STAGES) & 1, abort)) break;
+                if (ik < n_loads && !mbar_wait_all(kv_full + k_stage, (ik / S::STAGES) & 1, abort)) break;
                 const int left = lk - j * TN;
                 if (left < TN) {                       // rows beyond the sequence: zeros
+                    unsigned char* v_tile = ring + v_stage * S::TILE_BYTES;
                     for (int r = left + (lane >> 3); r < TN; r += 4)
 #pragma unroll
                         for (int b = 0; b < S::BOXES; ++b)
@@ -272,23 +315,32 @@ attend_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                 }
-                for (int i = 0; i < 2 && ok; ++i) {
-                    if (j >= nb[i]) continue;
-                    ok = mbar_wait_warp(p_full + i, j & 1, abort, lane);
-                    if (!ok) break;
-                    tc_fence_after();
-                    if (lane == 0) {
-                        const uint64_t vd = smem_desc_n_major(v_tile, S::BOX_BYTES);
+                const uint64_t vd = v_desc + uint64_t(v_stage) * TILE16;
 #pragma unroll
-                        for (int kk = 0; kk < TN / 16; ++kk)
+                for (int i = 0; i < 2; ++i) {
+                    if (j >= nb[i] || !ok) continue;
+                    auto values = [&](int from, int to) {
+#pragma unroll
+                        for (int kk = from; kk < to; ++kk)
                             umma_ts(tmem + 2 * TN + i * DP, tmem + i * TN + kk * 8, vd + uint64_t(kk * (16 * 128 >> 4)), p.idesc_pv, j > 0 || kk > 0);
+                    };
+                    ok = mbar_wait_all(p_full + 2 * i, j & 1, abort);
+                    if (!ok) continue;
+                    tc_fence_after();
+                    if (elect_one()) values(0, FIRST / 16);
+                    __syncwarp();
+                    ok = mbar_wait_all(p_full + 2 * i + 1, j & 1, abort);
+                    if (!ok) continue;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        values(FIRST / 16, TN / 16);
+                        if (j + 1 < nb[i]) scores(i, ik);
+                        umma_commit(s_full + i);
                     }
-                    if (j + 1 < nb[i]) scores(i, ik);
-                    if (lane == 0) umma_commit(s_full + i);
                 }
-                if (lane == 0) {
-                    if (iv + S::STAGES < n_loads) umma_commit(kv_empty + iv % S::STAGES);
-                    if (ik + S::STAGES < n_loads) umma_commit(kv_empty + ik % S::STAGES);
+                if (ok && elect_one()) {
+                    if (iv + S::STAGES < n_loads) umma_commit(kv_empty + v_stage);
+                    if (ik + S::STAGES < n_loads) umma_commit(kv_empty + k_stage);
                 }
             }
         }
@@ -302,10 +354,13 @@ attend_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         const int sees = live ? (p.causal ? max(0, min(lk, tok + shift + 1)) : lk) : 0;
         const uint32_t lane_bits = uint32_t((warp & 3) * 32) << 16;
         const uint32_t s_tm = tmem + lane_bits + i * TN, o_tm = tmem + lane_bits + 2 * TN + i * DP;
-        float ref = -CUDART_INF_F, l = 0.f;           // ref in units of log2
+        const float2 c2 = make_float2(p.c2, p.c2);
+        float ref = -CUDART_INF_F;                    // in units of log2
+        float2 l = make_float2(0.f, 0.f);
+        bool bad = false;                             // a score is NaN
         bool ok = true;
         for (int j = 0; j < nb[i]; ++j) {
-            ok = mbar_wait_warp(s_full + i, j & 1, abort, lane);
+            ok = mbar_wait_all(s_full + i, j & 1, abort);
             if (!ok) break;
             tc_fence_after();
             float s[TN];
@@ -315,57 +370,71 @@ attend_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
 #pragma unroll
                 for (int c = 0; c < TN; ++c) s[c] = c < left ? s[c] : -CUDART_INF_F;
             }
-            float mx0 = s[0], mx1 = s[1], mx2 = s[2], mx3 = s[3];
+            // The first half is exponentiated against the old reference while the block's maximum is formed: the
+            // maxima fill the issue slots that the special-function unit leaves.  Should the reference have to move, once
+            // more against the new one.
+            uint32_t pk[32];
+            float2 la;
+            bool again;
+            do {
+                const float base = ref > -CUDART_INF_F ? ref : 0.f;
+                const float2 nb2 = make_float2(-base, -base);
+                la = make_float2(0.f, 0.f);
+                float mx0 = s[0], mx1 = s[1];
 #pragma unroll
-            for (int c = 4; c < TN; c += 4) {
-                mx0 = fmaxf(mx0, s[c]);
-                mx1 = fmaxf(mx1, s[c + 1]);
-                mx2 = fmaxf(mx2, s[c + 2]);
-                mx3 = fmaxf(mx3, s[c + 3]);
-            }
-            const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * p.c2;
-            const bool move = mx > ref + SLACK;       // also at the first finite maximum
-            if (__any_sync(0xffffffffu, move)) {
-                const float f = move ? (ref > -CUDART_INF_F ? ex2_approx(ref - mx) : 0.f) : 1.f;
-                if (move) ref = mx;
-                l *= f;
-                if (j > 0) {
-#pragma unroll 1
-                    for (int c = 0; c < DP; c += 32) {
-                        uint32_t o[32];
-                        tmem_ld32(o_tm + c, o);
+                for (int c = 0; c < 2; ++c) {
+                    exp_chunk<T>(s + 32 * c, c2, nb2, la, pk + 16 * c);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                        tmem_st32(o_tm + c, o);
+                    for (int e = c * 64; e < c * 64 + 64; e += 4) {
+                        mx0 = max3(mx0, s[e], s[e + 1]);
+                        mx1 = max3(mx1, s[e + 2], s[e + 3]);
                     }
                 }
-            }
-            const float base = ref > -CUDART_INF_F ? ref : 0.f;
-            float l0 = 0.f, l1 = 0.f;
+                const float mx = max3(mx0, mx1, mx1) * p.c2;
+                bad = bad || mx != mx;
+                const bool move = mx > ref + SLACK;   // also at the first finite maximum
+                again = __any_sync(0xffffffffu, move);
+                if (again) {
+                    const float f = move ? (ref > -CUDART_INF_F ? ex2_approx(ref - mx) : 0.f) : 1.f;
+                    if (move) ref = mx;
+                    l.x *= f;
+                    l.y *= f;
+                    if (j > 0) {
+#pragma unroll 1
+                        for (int c = 0; c < DP; c += 32) {
+                            uint32_t o[32];
+                            tmem_ld32(o_tm + c, o);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t pk[32];
-#pragma unroll
-                for (int c = 0; c < 32; ++c) {
-                    const float a = ex2_approx(fmaf(s[h * 64 + 2 * c], p.c2, -base));
-                    const float b = ex2_approx(fmaf(s[h * 64 + 2 * c + 1], p.c2, -base));
-                    l0 += a;
-                    l1 += b;
-                    pk[c] = pack2<T>(a, b);
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            tmem_st32(o_tm + c, o);
+                        }
+                    }
                 }
-                tmem_st32(s_tm + h * 32, pk);
-            }
-            l += l0 + l1;
+            } while (again);
+            tmem_st32(s_tm, pk);
+            const float base = ref > -CUDART_INF_F ? ref : 0.f;
+            const float2 nb2 = make_float2(-base, -base);
+            exp_chunk<T>(s + 64, c2, nb2, la, pk);
+            tmem_st16(s_tm + 32, pk);
             tmem_wait_st();
             tc_fence_before();
-            mbar_arrive(p_full + i);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_full + 2 * i);
+            exp_chunk<T>(s + 96, c2, nb2, la, pk + 16);
+            tmem_st16(s_tm + 48, pk + 16);
+            l = add2(l, la);
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_full + 2 * i + 1);
         }
+        const float total = bad ? CUDART_NAN_F : l.x + l.y;
         if (ok && nb[i] > 0) {
-            ok = mbar_wait_warp(s_full + i, nb[i] & 1, abort, lane);
+            ok = mbar_wait_all(s_full + i, nb[i] & 1, abort);
             tc_fence_after();
         }
         if (ok) {
-            const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+            const float inv = total > 0.f ? 1.f / total : (total == 0.f ? 0.f : total);
             const int64_t at = int64_t(q0 + tok) * p.hq + head * p.G + g;
             unsigned char* dst = p.out + at * p.D * 2;
 #pragma unroll 1
@@ -384,7 +453,7 @@ attend_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     if (live && c + e < p.D) *reinterpret_cast<uint4*>(dst + (c + e) * 2) = w;
                 }
             }
-            if (live && p.lse) p.lse[at] = l > 0.f ? (ref + log2f(l)) * LN2_F : (l == 0.f ? -CUDART_INF_F : l);
+            if (live && p.lse) p.lse[at] = total > 0.f ? (ref + log2f(total)) * LN2_F : (total == 0.f ? -CUDART_INF_F : total);
         }
     }
 
