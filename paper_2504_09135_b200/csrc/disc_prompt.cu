@@ -61,7 +61,7 @@ struct Shape {
 struct PromptParams {
     const int32_t* cu_q;
     const int32_t* cu_k;
-    int32_t n_seqs, hq, hkv, G, TQ, D, causal, tiles;
+    int32_t n_seqs, hq, hkv, G, TQ, D, causal;
     float c2;                             // scale log2(e)
     unsigned char* out;
     float* lse;
@@ -130,6 +130,12 @@ __device__ __forceinline__ void tmem_ld128(uint32_t taddr, float* v) {
         : "r"(taddr)
         : "memory");
 }
+// 32 bytes to a 32-byte boundary
+__device__ __forceinline__ void st_global32(void* p, const uint32_t* v) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* v) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
@@ -197,263 +203,442 @@ __device__ __forceinline__ void exp_chunk(const float* s, float2 c2, float2 shif
     }
 }
 
+// One item of work, put together by the scheduling warp for the others.
+struct Item {
+    int q0, lq, k0, lk;                   // the sequence's tokens in q and in k / v
+    int first, head;                      // first query token of the two tiles, key head
+    int nb[2];                            // blocks of keys that each tile sees
+    int some;                             // 0: no more items
+};
+constexpr int ITEMS = 2;
+
+// Cluster launch control: a block that is already running takes over the place of one that has not started yet.
+__device__ __forceinline__ void ask_for_block(void* answer, uint64_t* bar) {
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];"
+                 ::"r"(smem_u32(answer)), "r"(smem_u32(bar))
+                 : "memory");
+}
+__device__ __forceinline__ bool taken_block(const void* answer, unsigned& block) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .b128 h;\n\t.reg .pred p;\n\t"
+        "ld.shared.b128 h, [%2];\n\t"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t"
+        "mov.u32 %1, 0;\n\t"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, h;\n\t}"
+        : "=r"(ok), "=r"(block)
+        : "r"(smem_u32(answer))
+        : "memory");
+    return ok != 0;
+}
+
 template <typename T, int DP>
 __global__ void __launch_bounds__(THREADS, 1)
 attend_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                      const __grid_constant__ CUtensorMap map_v, const PromptParams p) {
     using S = Shape<DP>;
-    // which tiles: heads fastest, so that blocks that run together share K and V in L2; the tiles late in their
-    // sequences, which see the most keys, first
-    const int head = int(blockIdx.x % unsigned(p.hkv));
-    const unsigned rest = blockIdx.x / unsigned(p.hkv);
-    const int seq = int(rest % unsigned(p.n_seqs));
-    const int first = (p.tiles - 1 - int(rest / unsigned(p.n_seqs))) * 2 * p.TQ;      // first query token
-    const int q0 = p.cu_q[seq], lq = p.cu_q[seq + 1] - q0;
-    if (first >= lq) return;
-    const int k0 = p.cu_k[seq], lk = p.cu_k[seq + 1] - k0;
-    const int shift = lk - lq;                        // query j sees the keys 0 .. j + shift
-
     extern __shared__ unsigned char smem_raw[];
     unsigned char* tiles = reinterpret_cast<unsigned char*>((uintptr_t(smem_raw) + 1023) & ~uintptr_t(1023));
     unsigned char* ring = tiles + 2 * S::TILE_BYTES;
     uint64_t* bars = reinterpret_cast<uint64_t*>(ring + S::STAGES * S::TILE_BYTES);
     uint64_t* q_full = bars;                          // [2]
-    uint64_t* s_full = bars + 2;                      // [2] scores of a tile (and the product before) done
-    uint64_t* p_full = bars + 4;                      // [2][2] probabilities of a tile written: the first 96 keys, the last 32
-    uint64_t* kv_full = bars + 8;                     // [STAGES]
-    uint64_t* kv_empty = bars + 8 + S::STAGES;        // [STAGES]
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 8 + 2 * S::STAGES);
+    uint64_t* q_empty = bars + 2;                     // [2] the last scores of an item's tile are done
+    uint64_t* s_full = bars + 4;                      // [2] scores of a tile (and the product before) done
+    uint64_t* o_full = bars + 6;                      // [2] the last product of an item's tile done
+    uint64_t* p_full = bars + 8;                      // [2][2] probabilities of a tile written: the first 96 keys, the last 32
+    uint64_t* item_full = bars + 12;                  // [ITEMS]
+    uint64_t* item_empty = bars + 14;                 // [ITEMS]
+    uint64_t* answer_full = bars + 16;
+    uint64_t* kv_full = bars + 17;                    // [STAGES]
+    uint64_t* kv_empty = bars + 17 + S::STAGES;       // [STAGES]
+    static_assert((17 + 2 * S::STAGES) * 8 <= 256, "room for the barriers");
+    __shared__ __align__(16) unsigned char answer[16];
+    __shared__ Item items[ITEMS];
+    __shared__ uint32_t tmem_slot;
     __shared__ int s_abort;
     volatile int* abort = &s_abort;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         s_abort = 0;
-        for (int i = 0; i < 2; ++i) { mbar_init(q_full + i, 1); mbar_init(s_full + i, 1); mbar_init(p_full + 2 * i, TM / 32); mbar_init(p_full + 2 * i + 1, TM / 32); }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(q_full + i, 1); mbar_init(q_empty + i, 1); mbar_init(s_full + i, 1); mbar_init(o_full + i, 1);
+            mbar_init(p_full + 2 * i, TM / 32); mbar_init(p_full + 2 * i + 1, TM / 32);
+        }
+        for (int i = 0; i < ITEMS; ++i) { mbar_init(item_full + i, 1); mbar_init(item_empty + i, 10); }
+        mbar_init(answer_full, 1);
         for (int s = 0; s < S::STAGES; ++s) { mbar_init(kv_full + s, 1); mbar_init(kv_empty + s, 1); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 9) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(tmem_slot);
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&tmem_slot);
 
-    // blocks of keys that each tile sees
-    int nb[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int t0 = first + i * p.TQ, t1 = min(lq, t0 + p.TQ);
-        const int keys = t0 < t1 ? (p.causal ? min(lk, t1 + shift) : lk) : 0;
-        nb[i] = keys > 0 ? (keys + TN - 1) / TN : 0;
-    }
-    const int n_blk = max(nb[0], nb[1]);
+    // the n-th item of this block, null when there is none (or a wait ran out); it stays in its place until the warp lets go of it
+    auto get_item = [&](int n) -> const volatile Item* {
+        if (!mbar_wait_all(item_full + n % ITEMS, (n / ITEMS) & 1, abort)) return nullptr;
+        const volatile Item* it = &items[n % ITEMS];
+        return it->some ? it : nullptr;
+    };
+    auto let_go = [&](int n) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(item_empty + n % ITEMS);
+    };
 
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-        if (warp == 8) {
-            // ---- loads
-            if (lane == 0 && n_blk > 0) {
-                const uint32_t q_bytes = uint32_t(S::BOXES) * p.G * p.TQ * BOX * 2;
-                for (int i = 0; i < 2; ++i)
-                    if (nb[i] > 0) {
-                        mbar_expect_tx(q_full + i, q_bytes);
-                        for (int b = 0; b < S::BOXES; ++b)
-                            tma_load_3d(tiles + i * S::TILE_BYTES + b * S::BOX_BYTES, &map_q, b * BOX, head * p.G, q0 + first + i * p.TQ, q_full + i);
+        if (warp == 10) {
+            // ---- scheduling.  Block b stands for key head b % hkv of the (b / hkv)-th pair of tiles, counted through the
+            // sequences, the tiles late in a sequence, which see the most keys, first; neighbouring blocks share keys
+            // and values.  The launch has room for the most pairs there can be; what lies beyond the last is skipped.
+            unsigned block = blockIdx.x;
+            int base = 0, chunk = 0;                   // pairs before the chunk-th 32 sequences
+            for (int n = 0;; ++n) {
+                Item it;
+                it.some = 0;
+                bool more = true;
+                while (more) {
+                    const int pair = int(block / unsigned(p.hkv));
+                    bool beyond = false;
+                    if (pair < base) base = chunk = 0;
+                    for (;;) {
+                        const int seq = chunk * 32 + lane;
+                        const int q0 = p.cu_q[min(seq, p.n_seqs)], q1 = p.cu_q[min(seq + 1, p.n_seqs)];
+                        const int pairs = (q1 - q0 + 2 * p.TQ - 1) / (2 * p.TQ);
+                        int upto = pairs;
+#pragma unroll
+                        for (int o = 1; o < 32; o <<= 1) {
+                            const int u = __shfl_up_sync(0xffffffffu, upto, o);
+                            if (lane >= o) upto += u;
+                        }
+                        const unsigned in = __ballot_sync(0xffffffffu, pair < base + upto);
+                        if (in) {
+                            const int who = __ffs(in) - 1;
+                            it.q0 = __shfl_sync(0xffffffffu, q0, who);
+                            it.lq = __shfl_sync(0xffffffffu, q1, who) - it.q0;
+                            const int before = base + __shfl_sync(0xffffffffu, upto - pairs, who);
+                            it.first = (__shfl_sync(0xffffffffu, pairs, who) - 1 - (pair - before)) * 2 * p.TQ;
+                            const int seq_of = chunk * 32 + who;
+                            it.k0 = p.cu_k[seq_of];
+                            it.lk = p.cu_k[seq_of + 1] - it.k0;
+                            break;
+                        }
+                        base += __shfl_sync(0xffffffffu, upto, 31);
+                        ++chunk;
+                        if (chunk * 32 >= p.n_seqs) { beyond = true; break; }
                     }
-                for (int it = 0; it < 2 * n_blk; ++it) {                 // K_0 V_0 K_1 V_1 ...
-                    const int s = it % S::STAGES, round = it / S::STAGES;
-                    if (round > 0 && !mbar_wait(kv_empty + s, (round - 1) & 1, abort)) break;
-                    mbar_expect_tx(kv_full + s, S::TILE_BYTES);
-                    for (int b = 0; b < S::BOXES; ++b)
-                        tma_load_3d(ring + s * S::TILE_BYTES + b * S::BOX_BYTES, it & 1 ? &map_v : &map_k, b * BOX, head, k0 + (it >> 1) * TN, kv_full + s);
+                    if (!beyond) {
+                        it.head = int(block % unsigned(p.hkv));
+                        it.some = 1;
+                        const int shift = it.lk - it.lq;          // query j sees the keys 0 .. j + shift
+                        for (int i = 0; i < 2; ++i) {
+                            const int t0 = it.first + i * p.TQ, t1 = min(it.lq, t0 + p.TQ);
+                            const int keys = t0 < t1 ? (p.causal ? min(it.lk, t1 + shift) : it.lk) : 0;
+                            it.nb[i] = keys > 0 ? (keys + TN - 1) / TN : 0;
+                        }
+                    }
+                    // the place in the ring was read by everybody before it is written again
+                    if (it.some) {
+                        if (n >= ITEMS && !mbar_wait_all(item_empty + n % ITEMS, (n / ITEMS - 1) & 1, abort)) { it.some = 0; more = false; break; }
+                        if (lane == 0) {
+                            items[n % ITEMS] = it;
+                            mbar_arrive(item_full + n % ITEMS);
+                        }
+                        __syncwarp();
+                        break;
+                    }
+                    more = false;                      // nothing lies beyond the last pair
+                }
+                if (!it.some) {
+                    if (n >= ITEMS) mbar_wait_all(item_empty + n % ITEMS, (n / ITEMS - 1) & 1, abort);
+                    if (lane == 0) {
+                        items[n % ITEMS].some = 0;
+                        mbar_arrive(item_full + n % ITEMS);
+                    }
+                    break;
+                }
+                if (lane == 0) {
+                    mbar_expect_tx(answer_full, 16);
+                    ask_for_block(answer, answer_full);
+                }
+                __syncwarp();
+                if (!mbar_wait_all(answer_full, n & 1, abort)) break;
+                const bool got = taken_block(answer, block);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (!got) {
+                    ++n;
+                    if (n >= ITEMS) mbar_wait_all(item_empty + n % ITEMS, (n / ITEMS - 1) & 1, abort);
+                    if (lane == 0) {
+                        items[n % ITEMS].some = 0;
+                        mbar_arrive(item_full + n % ITEMS);
+                    }
+                    break;
                 }
             }
-        } else if (warp == 9 && n_blk > 0) {
+        } else if (warp == 8) {
+            // ---- loads
+            int load = 0, uses[2] = {0, 0};
+            bool ok = true;
+            for (int n = 0; ok; ++n) {
+                const volatile Item* it = get_item(n);
+                if (!it) break;
+                if (lane == 0) {
+                    const int n_blk = max(it->nb[0], it->nb[1]), head = it->head, k0 = it->k0;
+                    const uint32_t q_bytes = uint32_t(S::BOXES) * p.G * p.TQ * BOX * 2;
+                    for (int i = 0; i < 2 && ok; ++i)
+                        if (it->nb[i] > 0) {
+                            if (uses[i] > 0) ok = mbar_wait(q_empty + i, (uses[i] - 1) & 1, abort);
+                            if (!ok) break;
+                            ++uses[i];
+                            mbar_expect_tx(q_full + i, q_bytes);
+                            for (int b = 0; b < S::BOXES; ++b)
+                                tma_load_3d(tiles + i * S::TILE_BYTES + b * S::BOX_BYTES, &map_q, b * BOX, head * p.G, it->q0 + it->first + i * p.TQ, q_full + i);
+                        }
+                    for (int j = 0; j < 2 * n_blk && ok; ++j, ++load) {            // K_0 V_0 K_1 V_1 ...
+                        const int s = load % S::STAGES, round = load / S::STAGES;
+                        if (round > 0) ok = mbar_wait(kv_empty + s, (round - 1) & 1, abort);
+                        if (!ok) break;
+                        mbar_expect_tx(kv_full + s, S::TILE_BYTES);
+                        for (int b = 0; b < S::BOXES; ++b)
+                            tma_load_3d(ring + s * S::TILE_BYTES + b * S::BOX_BYTES, j & 1 ? &map_v : &map_k, b * BOX, head, k0 + (j >> 1) * TN, kv_full + s);
+                    }
+                }
+                ok = __shfl_sync(0xffffffffu, ok, 0);
+                let_go(n);
+            }
+        } else if (warp == 9) {
             // ---- MMAs
             const uint64_t q_desc[2] = {smem_desc_sw128(tiles), smem_desc_sw128(tiles + S::TILE_BYTES)};
             const uint64_t kv_desc = smem_desc_sw128(ring), v_desc = smem_desc_n_major(ring, S::BOX_BYTES);
             constexpr uint64_t TILE16 = S::TILE_BYTES >> 4;
-            const int n_loads = 2 * n_blk;
-            // S_i = Q_i K^T with the keys of load `it`
-            auto scores = [&](int i, int it) {
-                const uint64_t kd = kv_desc + uint64_t(it % S::STAGES) * TILE16;
+            // S_i = Q_i K^T with the keys in place `stage` of the ring
+            auto scores = [&](int i, int stage) {
+                const uint64_t kd = kv_desc + uint64_t(stage) * TILE16;
 #pragma unroll
                 for (int kk = 0; kk < DP / 16; ++kk) {
                     const uint64_t off = uint64_t((kk / 4) * (S::BOX_BYTES >> 4) + (kk % 4) * 2);
                     umma_ss(tmem + i * TN, q_desc[i] + off, kd + off, p.idesc_qk, kk > 0);
                 }
             };
-            bool ok = mbar_wait_all(kv_full, 0, abort);
-            for (int i = 0; i < 2 && ok; ++i)
-                if (nb[i] > 0) {
-                    ok = mbar_wait_all(q_full + i, 0, abort);
-                    if (!ok) break;
-                    tc_fence_after();
-                    if (elect_one()) {
-                        scores(i, 0);
-                        umma_commit(s_full + i);
-                    }
-                }
-            // a place in the ring is reported free only where a load waits for it
-            if (ok && S::STAGES < n_loads && elect_one()) umma_commit(kv_empty);
-            for (int j = 0; j < n_blk && ok; ++j) {
-                const int iv = 2 * j + 1, ik = 2 * j + 2;
-                const int v_stage = iv % S::STAGES, k_stage = ik % S::STAGES;
-                if (!mbar_wait_all(kv_full + v_stage, (iv / S::STAGES) & 1, abort)) break;
-                if (ik < n_loads && !mbar_wait_all(kv_full + k_stage, (ik / S::STAGES) & 1, abort)) break;
-                const int left = lk - j * TN;
-                if (left < TN) {                       // rows beyond the sequence: zeros
-                    unsigned char* v_tile = ring + v_stage * S::TILE_BYTES;
-                    for (int r = left + (lane >> 3); r < TN; r += 4)
-#pragma unroll
-                        for (int b = 0; b < S::BOXES; ++b)
-                            *reinterpret_cast<uint4*>(v_tile + b * S::BOX_BYTES + r * 128 + (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                }
-                const uint64_t vd = v_desc + uint64_t(v_stage) * TILE16;
+            int load = 0, uses[2] = {0, 0}, done[2] = {0, 0};      // loads taken; items and blocks of each tile
+            bool ok = true;
+            for (int n = 0; ok; ++n) {
+                const volatile Item* it = get_item(n);
+                if (!it) break;
+                const int nb[2] = {it->nb[0], it->nb[1]}, lk = it->lk;
+                let_go(n);
+                const int n_blk = max(nb[0], nb[1]);
+                if (n_blk == 0) continue;
+                ok = mbar_wait_all(kv_full + load % S::STAGES, (load / S::STAGES) & 1, abort);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    if (j >= nb[i] || !ok) continue;
-                    auto values = [&](int from, int to) {
-#pragma unroll
-                        for (int kk = from; kk < to; ++kk)
-                            umma_ts(tmem + 2 * TN + i * DP, tmem + i * TN + kk * 8, vd + uint64_t(kk * (16 * 128 >> 4)), p.idesc_pv, j > 0 || kk > 0);
-                    };
-                    ok = mbar_wait_all(p_full + 2 * i, j & 1, abort);
+                    if (nb[i] == 0 || !ok) continue;
+                    ok = mbar_wait_all(q_full + i, uses[i] & 1, abort);
                     if (!ok) continue;
-                    tc_fence_after();
-                    if (elect_one()) values(0, FIRST / 16);
-                    __syncwarp();
-                    ok = mbar_wait_all(p_full + 2 * i + 1, j & 1, abort);
-                    if (!ok) continue;
+                    ++uses[i];
                     tc_fence_after();
                     if (elect_one()) {
-                        values(FIRST / 16, TN / 16);
-                        if (j + 1 < nb[i]) scores(i, ik);
+                        scores(i, load % S::STAGES);
                         umma_commit(s_full + i);
+                        if (nb[i] == 1) umma_commit(q_empty + i);
                     }
+                    __syncwarp();
                 }
-                if (ok && elect_one()) {
-                    if (iv + S::STAGES < n_loads) umma_commit(kv_empty + v_stage);
-                    if (ik + S::STAGES < n_loads) umma_commit(kv_empty + k_stage);
+                if (!ok) break;
+                if (elect_one()) umma_commit(kv_empty + load % S::STAGES);
+                __syncwarp();
+                ++load;
+                for (int j = 0; j < n_blk && ok; ++j) {
+                    const bool more = j + 1 < n_blk;
+                    const int v_stage = load % S::STAGES, k_stage = (load + 1) % S::STAGES;
+                    ok = mbar_wait_all(kv_full + v_stage, (load / S::STAGES) & 1, abort);
+                    if (ok && more) ok = mbar_wait_all(kv_full + k_stage, ((load + 1) / S::STAGES) & 1, abort);
+                    if (!ok) break;
+                    const int left = lk - j * TN;
+                    if (left < TN) {                   // rows beyond the sequence: zeros
+                        unsigned char* v_tile = ring + v_stage * S::TILE_BYTES;
+                        for (int r = left + (lane >> 3); r < TN; r += 4)
+#pragma unroll
+                            for (int b = 0; b < S::BOXES; ++b)
+                                *reinterpret_cast<uint4*>(v_tile + b * S::BOX_BYTES + r * 128 + (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                    }
+                    const uint64_t vd = v_desc + uint64_t(v_stage) * TILE16;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        if (j >= nb[i] || !ok) continue;
+                        auto values = [&](int from, int to) {
+#pragma unroll
+                            for (int kk = from; kk < to; ++kk)
+                                umma_ts(tmem + 2 * TN + i * DP, tmem + i * TN + kk * 8, vd + uint64_t(kk * (16 * 128 >> 4)), p.idesc_pv, j > 0 || kk > 0);
+                        };
+                        ok = mbar_wait_all(p_full + 2 * i, done[i] & 1, abort);
+                        if (!ok) continue;
+                        tc_fence_after();
+                        if (elect_one()) values(0, FIRST / 16);
+                        __syncwarp();
+                        ok = mbar_wait_all(p_full + 2 * i + 1, done[i] & 1, abort);
+                        if (!ok) continue;
+                        ++done[i];
+                        tc_fence_after();
+                        if (elect_one()) {
+                            values(FIRST / 16, TN / 16);
+                            if (j + 1 < nb[i]) {
+                                scores(i, k_stage);
+                                umma_commit(s_full + i);
+                                if (j + 2 == nb[i]) umma_commit(q_empty + i);
+                            } else umma_commit(o_full + i);
+                        }
+                        __syncwarp();
+                    }
+                    if (!ok) break;
+                    if (elect_one()) {
+                        umma_commit(kv_empty + v_stage);
+                        if (more) umma_commit(kv_empty + k_stage);
+                    }
+                    __syncwarp();
+                    load += more ? 2 : 1;
                 }
             }
+            // the last reports of free places have arrived before the block leaves
+            for (int back = 0; back < S::STAGES && back < load && ok; ++back)
+                ok = mbar_wait_all(kv_empty + (load - 1 - back) % S::STAGES, ((load - 1 - back) / S::STAGES) & 1, abort);
+            for (int i = 0; i < 2 && ok; ++i)
+                if (uses[i] > 0) ok = mbar_wait_all(q_empty + i, (uses[i] - 1) & 1, abort);
         }
     } else {
         // ---- softmax: this thread's query vector
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         const int i = warp >> 2;
         const int m = (warp & 3) * 32 + lane;
-        const int tok = first + i * p.TQ + m / p.G, g = m % p.G;
-        const bool live = m < p.TQ * p.G && tok < lq;
-        const int sees = live ? (p.causal ? max(0, min(lk, tok + shift + 1)) : lk) : 0;
+        const int row_tok = i * p.TQ + m / p.G, g = m % p.G;
+        const bool used = m < p.TQ * p.G;
         const uint32_t lane_bits = uint32_t((warp & 3) * 32) << 16;
         const uint32_t s_tm = tmem + lane_bits + i * TN, o_tm = tmem + lane_bits + 2 * TN + i * DP;
         const float2 c2 = make_float2(p.c2, p.c2);
-        float ref = -CUDART_INF_F;                    // in units of log2
-        float2 l = make_float2(0.f, 0.f);
-        bool bad = false;                             // a score is NaN
-        bool ok = true;
-        for (int j = 0; j < nb[i]; ++j) {
-            ok = mbar_wait_all(s_full + i, j & 1, abort);
-            if (!ok) break;
-            tc_fence_after();
-            float s[TN];
-            tmem_ld128(s_tm, s);
-            const int left = sees - j * TN;           // keys of this block that the row sees
-            if (__any_sync(0xffffffffu, left < TN)) {
+        // output rows on 32-byte boundaries are written 32 bytes at a time
+        const bool wide = p.D % 16 == 0 && (reinterpret_cast<uintptr_t>(p.out) & 31) == 0;
+        int seen = 0, ends = 0;                       // blocks and items of this tile so far
+        for (int n = 0;; ++n) {
+            const volatile Item* it = get_item(n);
+            if (!it) break;
+            const int nb = it->nb[i];
+            int sees = 0;                             // keys that the row sees
+            if (used && it->first + row_tok < it->lq) sees = p.causal ? max(0, min(it->lk, it->first + row_tok + it->lk - it->lq + 1)) : it->lk;
+            float ref = -CUDART_INF_F;                // in units of log2
+            float2 l = make_float2(0.f, 0.f);
+            bool bad = false;                         // a score is NaN
+            bool ok = true;
+            for (int j = 0; j < nb; ++j) {
+                ok = mbar_wait_all(s_full + i, seen & 1, abort);
+                if (!ok) break;
+                ++seen;
+                tc_fence_after();
+                float s[TN];
+                tmem_ld128(s_tm, s);
+                const int left = sees - j * TN;       // keys of this block that the row sees
+                if (__any_sync(0xffffffffu, left < TN)) {
 #pragma unroll
-                for (int c = 0; c < TN; ++c) s[c] = c < left ? s[c] : -CUDART_INF_F;
-            }
-            // The first half is exponentiated against the old reference while the block's maximum is formed: the
-            // maxima fill the issue slots that the special-function unit leaves.  Should the reference have to move, once
-            // more against the new one.
-            uint32_t pk[32];
-            float2 la;
-            bool again;
-            do {
-                const float base = ref > -CUDART_INF_F ? ref : 0.f;
-                const float2 nb2 = make_float2(-base, -base);
-                la = make_float2(0.f, 0.f);
-                float mx0 = s[0], mx1 = s[1];
+                    for (int c = 0; c < TN; ++c) s[c] = c < left ? s[c] : -CUDART_INF_F;
+                }
+                // The first quarter is exponentiated against the old reference while the block's maximum is formed: the
+                // maxima fill the issue slots that the special-function unit leaves.  Should the reference have to move, once
+                // more against the new one.
+                uint32_t pk[16];
+                float2 la;
+                bool again;
+                do {
+                    const float base = ref > -CUDART_INF_F ? ref : 0.f;
+                    la = make_float2(0.f, 0.f);
+                    exp_chunk<T>(s, c2, make_float2(-base, -base), la, pk);
+                    float mx0 = s[0], mx1 = s[1];
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    exp_chunk<T>(s + 32 * c, c2, nb2, la, pk + 16 * c);
-#pragma unroll
-                    for (int e = c * 64; e < c * 64 + 64; e += 4) {
+                    for (int e = 0; e < TN; e += 4) {
                         mx0 = max3(mx0, s[e], s[e + 1]);
                         mx1 = max3(mx1, s[e + 2], s[e + 3]);
                     }
-                }
-                const float mx = max3(mx0, mx1, mx1) * p.c2;
-                bad = bad || mx != mx;
-                const bool move = mx > ref + SLACK;   // also at the first finite maximum
-                again = __any_sync(0xffffffffu, move);
-                if (again) {
-                    const float f = move ? (ref > -CUDART_INF_F ? ex2_approx(ref - mx) : 0.f) : 1.f;
-                    if (move) ref = mx;
-                    l.x *= f;
-                    l.y *= f;
-                    if (j > 0) {
+                    const float mx = max3(mx0, mx1, mx1) * p.c2;
+                    bad = bad || mx != mx;
+                    const bool move = mx > ref + SLACK;   // also at the first finite maximum
+                    again = __any_sync(0xffffffffu, move);
+                    if (again) {
+                        const float f = move ? (ref > -CUDART_INF_F ? ex2_approx(ref - mx) : 0.f) : 1.f;
+                        if (move) ref = mx;
+                        l.x *= f;
+                        l.y *= f;
+                        if (j > 0) {
 #pragma unroll 1
-                        for (int c = 0; c < DP; c += 32) {
-                            uint32_t o[32];
-                            tmem_ld32(o_tm + c, o);
+                            for (int c = 0; c < DP; c += 32) {
+                                uint32_t o[32];
+                                tmem_ld32(o_tm + c, o);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                            tmem_st32(o_tm + c, o);
+                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                                tmem_st32(o_tm + c, o);
+                            }
                         }
                     }
-                }
-            } while (again);
-            tmem_st32(s_tm, pk);
-            const float base = ref > -CUDART_INF_F ? ref : 0.f;
-            const float2 nb2 = make_float2(-base, -base);
-            exp_chunk<T>(s + 64, c2, nb2, la, pk);
-            tmem_st16(s_tm + 32, pk);
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(p_full + 2 * i);
-            exp_chunk<T>(s + 96, c2, nb2, la, pk + 16);
-            tmem_st16(s_tm + 48, pk + 16);
-            l = add2(l, la);
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(p_full + 2 * i + 1);
-        }
-        const float total = bad ? CUDART_NAN_F : l.x + l.y;
-        if (ok && nb[i] > 0) {
-            ok = mbar_wait_all(s_full + i, nb[i] & 1, abort);
-            tc_fence_after();
-        }
-        if (ok) {
+                } while (again);
+                tmem_st16(s_tm, pk);
+                const float base = ref > -CUDART_INF_F ? ref : 0.f;
+                const float2 down = make_float2(-base, -base);
+                exp_chunk<T>(s + 32, c2, down, la, pk);
+                tmem_st16(s_tm + 16, pk);
+                exp_chunk<T>(s + 64, c2, down, la, pk);
+                tmem_st16(s_tm + 32, pk);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full + 2 * i);
+                exp_chunk<T>(s + 96, c2, down, la, pk);
+                tmem_st16(s_tm + 48, pk);
+                l = add2(l, la);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full + 2 * i + 1);
+            }
+            const float total = bad ? CUDART_NAN_F : l.x + l.y;
+            if (!ok) break;
+            if (nb > 0) {
+                if (!mbar_wait_all(o_full + i, ends & 1, abort)) break;
+                ++ends;
+                tc_fence_after();
+            }
             const float inv = total > 0.f ? 1.f / total : (total == 0.f ? 0.f : total);
-            const int64_t at = int64_t(q0 + tok) * p.hq + head * p.G + g;
+            const int tok = it->first + row_tok;
+            const bool live = used && tok < it->lq;
+            const int64_t at = int64_t(it->q0 + tok) * p.hq + it->head * p.G + g;
+            let_go(n);
             unsigned char* dst = p.out + at * p.D * 2;
 #pragma unroll 1
             for (int c = 0; c < DP; c += 32) {
                 uint32_t o[32];
-                if (nb[i] > 0) tmem_ld32(o_tm + c, o);
+                if (nb > 0) tmem_ld32(o_tm + c, o);
 #pragma unroll
-                for (int e = 0; e < 32; e += 8) {
-                    uint4 w = make_uint4(0, 0, 0, 0);
-                    if (sees > 0) {
-                        w.x = pack2<T>(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
-                        w.y = pack2<T>(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
-                        w.z = pack2<T>(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv);
-                        w.w = pack2<T>(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
+                for (int e = 0; e < 32; e += 16) {
+                    uint32_t w[8];
+#pragma unroll
+                    for (int x = 0; x < 8; ++x)
+                        w[x] = sees > 0 ? pack2<T>(__uint_as_float(o[e + 2 * x]) * inv, __uint_as_float(o[e + 2 * x + 1]) * inv) : 0u;
+                    if (live && c + e < p.D) {
+                        if (wide) st_global32(dst + (c + e) * 2, w);
+                        else {
+                            *reinterpret_cast<uint4*>(dst + (c + e) * 2) = make_uint4(w[0], w[1], w[2], w[3]);
+                            if (c + e + 8 < p.D) *reinterpret_cast<uint4*>(dst + (c + e) * 2 + 16) = make_uint4(w[4], w[5], w[6], w[7]);
+                        }
                     }
-                    if (live && c + e < p.D) *reinterpret_cast<uint4*>(dst + (c + e) * 2) = w;
                 }
             }
             if (live && p.lse) p.lse[at] = total > 0.f ? (ref + log2f(total)) * LN2_F : (total == 0.f ? -CUDART_INF_F : total);
+            tc_fence_before();                        // O has been read before the next item's first probabilities are reported
         }
     }
 
@@ -525,9 +710,10 @@ int disc_attend_prompt(const void* q, int64_t q_token_stride, int64_t q_head_str
     PromptParams p;
     p.cu_q = cu_q; p.cu_k = cu_k ? cu_k : cu_q; p.n_seqs = n_seqs; p.hq = n_q_heads; p.hkv = n_kv_heads; p.G = G; p.TQ = TQ; p.D = head_dim;
     p.causal = causal != 0; p.c2 = scale * LOG2E_F; p.out = static_cast<unsigned char*>(out); p.lse = lse_out; p.error = error;
+    // pairs of tiles: a sequence of n queries has n / (2 TQ) of them, rounded up
     const int64_t longest = max_q < n_q ? max_q : n_q;
-    p.tiles = int32_t((longest + 2 * TQ - 1) / (2 * TQ));
-    const int64_t grid = int64_t(p.tiles) * n_seqs * n_kv_heads;
+    const int64_t by_seq = (longest + 2 * TQ - 1) / (2 * TQ) * n_seqs, by_sum = n_q / (2 * TQ) + n_seqs;
+    const int64_t grid = (by_seq < by_sum ? by_seq : by_sum) * n_kv_heads;
     if (grid > 0x7fffffff) return DISC_ERR_UNSUPPORTED;
     const int DP = head_dim <= 64 ? 64 : 128;
     // instruction descriptors: D fp32 (bits 4-5 = 1), A and B f16 = 0 / bf16 = 1 (bits 7-9, 10-12), B of the second
