@@ -124,9 +124,17 @@ def _check(rc: int, where: str):
         raise DiscError(rc, where)
 
 
+# the current stream's handle without a Stream object around it (3 us a call); present in every torch that has CUDA
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream_ptr(stream=None) -> int:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return int(s.cuda_stream)
+    if stream is not None:
+        return int(stream.cuda_stream)
+    if _raw_stream is not None and _raw_device is not None and torch.cuda.is_initialized():
+        return _raw_stream(_raw_device())
+    return int(torch.cuda.current_stream().cuda_stream)
 
 
 def _dev(t: torch.Tensor, dtype, name: str) -> int:

@@ -9,15 +9,17 @@
 //
 // The pass is bound by the bytes of the logits.  What it may spend per logit is little: at the
 // measured copy rate 11 bf16 logits arrive per SM and clock, and an SM takes 2^x sixteen times and
-// any instruction 128 times per clock.  Hence packed bf16 maxima (half an instruction per logit), one
-// comparison with the running maximum per 32 logits, and nothing in the loop for the alternatives:
+// any instruction 128 times per clock.  Hence packed bf16 maxima and packed fp32 pairs (about 4.5 instructions
+// per logit), one comparison with the running maximum per 32 logits, and next to nothing in the loop for the
+// alternatives:
 //
-// The alternatives come from what the pass keeps anyway, each thread's own maximum.  The k-th largest
-// of the block's thread maxima (k distinct elements reach it) is at most the k-th largest element.  Only
-// the threads whose maximum reaches it can own one of the k best, as a rule k of them, and their
-// elements, a k-th part of a percent of the row, are looked at again (they are in L2).  What reaches the
-// threshold, typically k and a few, is ranked by counting in the order (larger first, -0 = +0, lower id
-// first, NaN last).  Should more reach it than the list holds (rows of equal logits), or too few (rows of
+// The alternatives come from what the pass keeps anyway, the maxima of each thread's portions of the row
+// (32 logits; noted in shared memory).  The k-th largest of the block's thread maxima (k distinct elements
+// reach it) is at most the k-th largest element, so that only portions whose maximum reaches it can hold one
+// of the k best: as a rule k and a few, and only they are looked at again.  (Looking at all of a thread's
+// portions again instead read half of the row a second time from HBM: the rows being worked on do not
+// fit in L2.)  What reaches the threshold is ranked by counting in the order (larger first, -0 = +0, lower
+// id first, NaN last).  Should more reach it than the lists hold (rows of equal logits), or too few (rows of
 // NaN), the block selects by histograms of the order keys over its slice: exact for every input.
 //
 // A row is taken by one block, or, when there are too few rows to fill the device, by a cluster of up to
@@ -34,17 +36,24 @@ constexpr int NT = 256;               // threads per block
 constexpr int NW = NT / 32;
 constexpr int TOP_MAX = 64;
 constexpr int LIST_CAP = 2048;
+constexpr int HOT_CAP = 512;          // portions of the row that are looked at again
+constexpr int SLOTS = 32;             // portions of a thread
 constexpr unsigned FULL = 0xffffffffu;
 constexpr float LOG2E_F = 1.4426950408889634f;
 constexpr float LN2_F = 0.6931471805599453f;
-// 2^y is zero in fp32 (flushed) below -126; clamping y there keeps (y-m) 2^(y-m) at 0 for y = -inf
+// 2^y is zero in fp32 (flushed) below -126
 constexpr float Y_MIN = -200.f;
+// Logits below `low`, y = -10^6, are taken as that: (y-m) 2^(y-m) is then 0 for them, where it would be NaN for -inf.  (y
+// has to stay where fp32 still resolves whole numbers, or y-m of the floor itself would be a large rounding error.)  A row whose
+// largest logit is that far out, a mask of the type's lowest value everywhere, goes through a pass of its own.
+constexpr float FAR_Y = 1.0e6f;
 
 struct LogprobParams {
     const void* logits;
     int64_t ld;
     int32_t V, top, split;
     float inv_t, c2;                  // 1/T, log2(e)/T
+    float low, low_y;                 // the floor of the logits, a bf16 value, and its y
     const int32_t* targets;           // nullable
     float* logp;                      // nullable
     float* entropy;                   // nullable
@@ -109,6 +118,21 @@ struct Vec<DISC_BF16> {
         const uint32_t w = *reinterpret_cast<const uint32_t*>(&a);
         return fmaxf(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
     }
+    // every element at least `low`, NaN kept
+    static __device__ __forceinline__ uint4 floor_at(uint4 v, float low) {
+        const __nv_bfloat162 l = __float2bfloat162_rn(low);
+        uint32_t* w = &v.x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const __nv_bfloat162 m = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(w + j), l);
+            w[j] = *reinterpret_cast<const uint32_t*>(&m);
+        }
+        return v;
+    }
+    // a maximum over elements in 16 bits
+    using Short = unsigned short;
+    static __device__ __forceinline__ Short shorten(float x) { return Short(__float_as_uint(x) >> 16); }
+    static __device__ __forceinline__ float lengthen(Short x) { return __uint_as_float(uint32_t(x) << 16); }
     static __device__ __forceinline__ float at(const char* p) { return __uint_as_float(uint32_t(*reinterpret_cast<const unsigned short*>(p)) << 16); }
     static __device__ __forceinline__ void put(char* p, float x) { *reinterpret_cast<__nv_bfloat16*>(p) = __float2bfloat16_rn(x); }
     static __device__ __forceinline__ uint4 pack(const float* x) {
@@ -137,6 +161,15 @@ struct Vec<DISC_F32> {
             a = fmaxf(fmaxf(a, __uint_as_float(v[u].x)), fmaxf(__uint_as_float(v[u].y), fmaxf(__uint_as_float(v[u].z), __uint_as_float(v[u].w))));
         return a;
     }
+    static __device__ __forceinline__ uint4 floor_at(uint4 v, float low) {
+        uint32_t* w = &v.x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = __float_as_uint(max_nan(__uint_as_float(w[j]), low));
+        return v;
+    }
+    using Short = float;
+    static __device__ __forceinline__ Short shorten(float x) { return x; }
+    static __device__ __forceinline__ float lengthen(Short x) { return x; }
     static __device__ __forceinline__ float at(const char* p) { return *reinterpret_cast<const float*>(p); }
     static __device__ __forceinline__ void put(char* p, float x) { *reinterpret_cast<float*>(p) = x; }
     static __device__ __forceinline__ uint4 pack(const float* x) {
@@ -162,11 +195,29 @@ struct RowShape {
 struct Sums {
     float m, ref, s, u;               // largest logit, its y; sums relative to ref
 };
-// A logit so far out that its y has no place in fp32 (a mask of the type's lowest value) counts as FAR: sums relative to
-// such a maximum stay finite, but mean nothing until a nearer one comes.
-constexpr float FAR_Y = 1.0e38f;
-__device__ __forceinline__ void raise(Sums& a, float m_new, float c2) {
-    const float ref = fabsf(m_new) < CUDART_INF_F ? fminf(fmaxf(m_new * c2, -FAR_Y), FAR_Y) : 0.f;
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(reinterpret_cast<unsigned long long&>(d))
+        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)), "l"(reinterpret_cast<unsigned long long&>(c)));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("add.rn.f32x2 %0, %1, %2;"
+        : "=l"(reinterpret_cast<unsigned long long&>(d))
+        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
+    return d;
+}
+struct Scale {
+    float c2, low_y;
+};
+__device__ __forceinline__ float reference(float m, Scale k) {
+    return fabsf(m) < CUDART_INF_F ? fminf(fmaxf(m * k.c2, k.low_y), FAR_Y) : 0.f;
+}
+// the sums of a, relative to a's reference, seen from another one
+__device__ __forceinline__ void raise(Sums& a, float m_new, Scale k) {
+    const float ref = reference(m_new, k);
     const float d = a.m > -CUDART_INF_F ? fmaxf(a.ref - ref, Y_MIN) : Y_MIN;
     const float f = ex2_approx(d);
     a.u = f * fmaf(d, a.s, a.u);
@@ -174,18 +225,32 @@ __device__ __forceinline__ void raise(Sums& a, float m_new, float c2) {
     a.m = m_new;
     a.ref = ref;
 }
-__device__ __forceinline__ Sums join(Sums a, Sums b, float c2) {
+__device__ __forceinline__ Sums join(Sums a, Sums b, Scale k) {
     if (b.m > a.m) { const Sums t = a; a = b; b = t; }
-    raise(b, a.m, c2);
+    raise(b, a.m, k);
     a.s += b.s;
     a.u += b.u;
     return a;
 }
-__device__ __forceinline__ void add(Sums& a, float x, float c2) {
-    const float d = max_nan(fmaf(x, c2, -a.ref), Y_MIN);
-    const float e = ex2_approx(d);
-    a.s += e;
-    a.u = fmaf(d, e, a.u);
+// a thread's running sums, even and odd elements apart
+struct Running {
+    float m, ref;
+    float2 s, u;
+};
+__device__ __forceinline__ void raise(Running& a, float m_new, Scale k) {
+    const float ref = reference(m_new, k);
+    const float d = a.m > -CUDART_INF_F ? fmaxf(a.ref - ref, Y_MIN) : Y_MIN;
+    const float f = ex2_approx(d);
+    a.u = make_float2(f * fmaf(d, a.s.x, a.u.x), f * fmaf(d, a.s.y, a.u.y));
+    a.s = make_float2(a.s.x * f, a.s.y * f);
+    a.m = m_new;
+    a.ref = ref;
+}
+__device__ __forceinline__ void add(Running& a, float2 x, float2 c2, float2 down) {
+    const float2 d = fma2(x, c2, down);
+    const float2 e = make_float2(ex2_approx(d.x), ex2_approx(d.y));
+    a.s = add2(a.s, e);
+    a.u = fma2(d, e, a.u);
 }
 
 // shared memory of a block; the other blocks of the cluster read `part`, `found` and `list`
@@ -193,13 +258,18 @@ struct Smem {
     unsigned long long list[LIST_CAP];                 // order key << 32 | ~id : larger = better
     unsigned long long best[TOP_MAX];
     uint32_t keys[NT];
-    int32_t hot[NT];
+    int32_t hot[HOT_CAP];                              // portion << 8 | thread
     unsigned int hist[256];
     Sums warp_sums[NW];
     Sums part;
     unsigned int n_hot, n_list, threshold, found;
     unsigned int prefix, remaining;
     int scan[NW];
+};
+
+template <int DT>
+struct PortionMaxima {
+    typename Vec<DT>::Short at[SLOTS][NT];
 };
 
 __device__ __forceinline__ unsigned long long entry(uint32_t key, int32_t id) {
@@ -239,6 +309,23 @@ __device__ __forceinline__ void rank_list(Smem& sm, unsigned int cnt, unsigned i
         if (r < want) sm.best[r] = e;
     }
     __syncthreads();
+}
+
+// The want-th largest (want <= NT) of the block's keys, its lower 16 bits cleared: found bit by bit by one warp.
+__device__ __forceinline__ uint32_t kth_key(const uint32_t* keys, unsigned int want, int lane) {
+    uint32_t k[NT / 32];
+#pragma unroll
+    for (int j = 0; j < NT / 32; ++j) k[j] = keys[j * 32 + lane];
+    uint32_t found = 0u;
+#pragma unroll 1
+    for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
+        const uint32_t t = found | bit;
+        unsigned int n = 0;
+#pragma unroll
+        for (int j = 0; j < NT / 32; ++j) n += k[j] >= t;
+        if (__reduce_add_sync(FULL, n) >= want) found = t;
+    }
+    return found;
 }
 
 // The `want` best of the elements [e0, e1) of a row by histograms of the order keys, eight bits at a
@@ -312,6 +399,7 @@ __global__ void __launch_bounds__(NT, 4) disc_logprobs_kernel(const LogprobParam
     constexpr int E = Vec<DT>::E, SIZE = Vec<DT>::SIZE;
     extern __shared__ unsigned char smem_raw[];
     Smem& sm = *reinterpret_cast<Smem*>(smem_raw);
+    PortionMaxima<DT>& pm = *reinterpret_cast<PortionMaxima<DT>*>(smem_raw + sizeof(Smem));      // only with TOP
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t row = blockIdx.x / unsigned(p.split);
     const uint32_t rank = p.split > 1 ? cluster_ctarank() : 0u;
@@ -327,28 +415,52 @@ __global__ void __launch_bounds__(NT, 4) disc_logprobs_kernel(const LogprobParam
         else if (tid - r.head < r.tail) extra = r.head + r.nvec * E + tid - r.head;
     }
 
-    Sums a{-CUDART_INF_F, 0.f, 0.f, 0.f};
+    Running run{-CUDART_INF_F, 0.f, make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+    const float2 c2 = make_float2(p.c2, p.c2);
+    const Scale k{p.c2, p.low_y};
+    float extra_max = -CUDART_INF_F;
     if (extra >= 0) {
         const float x = Vec<DT>::at(r.base + size_t(extra) * SIZE);
-        if (x > a.m) raise(a, x, p.c2);
-        add(a, x, p.c2);
+        if (x > run.m) raise(run, x, k);
+        extra_max = x;
+        // the same steps as for a pair, on one element
+        const float d = fmaf(max_nan(x, p.low), p.c2, -run.ref), e = ex2_approx(d);
+        run.s.x += e;
+        run.u.x = fmaf(d, e, run.u.x);
     }
-    for (int32_t v = v0 + tid; v < v1; v += NT * U) {
+    // portions of the thread's vectors: U of them, or more when that would make too many
+    const int32_t rounds = (v1 - v0 + NT * U - 1) / (NT * U);
+    const int32_t per_slot = (rounds + SLOTS - 1) / SLOTS;
+    int32_t in_slot = 0, slot = 0;
+    float slot_max = -CUDART_INF_F;
+    for (int32_t v = v0 + tid; v < v0 + rounds * (NT * U); v += NT * U) {
         uint4 w[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) w[u] = v + u * NT < v1 ? ld_stream(vecs + v + u * NT) : Vec<DT>::lowest();
         const float mx = Vec<DT>::template largest<U>(w);
-        if (mx > a.m) raise(a, mx, p.c2);
+        if (mx > run.m) raise(run, mx, k);
+        if (TOP) {
+            slot_max = fmaxf(slot_max, mx);
+            if (++in_slot == per_slot) {
+                pm.at[slot][tid] = Vec<DT>::shorten(slot_max);
+                ++slot;
+                in_slot = 0;
+                slot_max = -CUDART_INF_F;
+            }
+        }
+        const float2 down = make_float2(-run.ref, -run.ref);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float x[E];
-            Vec<DT>::unpack(w[u], x);
+            Vec<DT>::unpack(Vec<DT>::floor_at(w[u], p.low), x);
 #pragma unroll
-            for (int j = 0; j < E; ++j) add(a, x[j], p.c2);
+            for (int j = 0; j < E; j += 2) add(run, make_float2(x[j], x[j + 1]), c2, down);
         }
     }
+    if (TOP && in_slot > 0) pm.at[slot][tid] = Vec<DT>::shorten(slot_max);
+    Sums a{run.m, run.ref, run.s.x + run.s.y, run.u.x + run.u.y};
 
-    const float own_max = a.m;
+    const float own_max = run.m;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         Sums b;
@@ -356,7 +468,7 @@ __global__ void __launch_bounds__(NT, 4) disc_logprobs_kernel(const LogprobParam
         b.ref = __shfl_xor_sync(FULL, a.ref, o);
         b.s = __shfl_xor_sync(FULL, a.s, o);
         b.u = __shfl_xor_sync(FULL, a.u, o);
-        a = join(a, b, p.c2);
+        a = join(a, b, k);
     }
     if (lane == 0) sm.warp_sums[warp] = a;
     const uint32_t key = v0 + tid < v1 || extra >= 0 ? order_key(own_max) : 0u;
@@ -369,30 +481,29 @@ __global__ void __launch_bounds__(NT, 4) disc_logprobs_kernel(const LogprobParam
     if (TOP) {
         const int32_t elements = (v1 - v0) * E + (rank == 0 ? r.head + r.tail : 0);
         const unsigned int want = min(unsigned(p.top), unsigned(elements));
-        // the want-th largest of the threads' maxima
-        unsigned int above = 0;
-        const uint4* k4 = reinterpret_cast<const uint4*>(sm.keys);
-#pragma unroll 8
-        for (int j = 0; j < NT / 4; ++j) {
-            const uint4 k = k4[j];
-            above += (k.x > key || (k.x == key && 4 * j + 0 < tid)) + (k.y > key || (k.y == key && 4 * j + 1 < tid)) +
-                     (k.z > key || (k.z == key && 4 * j + 2 < tid)) + (k.w > key || (k.w == key && 4 * j + 3 < tid));
-        }
-        if (want > 0 && above == want - 1) sm.threshold = key;
-        __syncthreads();
         if (want > 0) {
+            if (warp == 0) {
+                const uint32_t t = kth_key(sm.keys, want, lane);
+                if (lane == 0) sm.threshold = t;
+            }
+            __syncthreads();
             const uint32_t thr = sm.threshold;
-            const bool hot = v0 + tid < v1 && key >= thr;
-            if (hot) sm.hot[atomicAdd(&sm.n_hot, 1u)] = tid;
+            if (v0 + tid < v1 && key >= thr)
+                for (int32_t i = 0; i * per_slot < rounds; ++i)
+                    if (order_key(Vec<DT>::lengthen(pm.at[i][tid])) >= thr) {
+                        const unsigned int at = atomicAdd(&sm.n_hot, 1u);
+                        if (at < HOT_CAP) sm.hot[at] = i << 8 | tid;
+                    }
             if (extra >= 0) {
-                const uint32_t k = order_key(Vec<DT>::at(r.base + size_t(extra) * SIZE));
+                const uint32_t k = order_key(extra_max);
                 if (k >= thr) sm.list[atomicAdd(&sm.n_list, 1u)] = entry(k, extra);
             }
             __syncthreads();
-            const int32_t rounds = (v1 - v0 + NT - 1) / NT;
-            const int32_t n_look = int32_t(sm.n_hot) * rounds;
+            const unsigned int n_hot = sm.n_hot;
+            const int32_t each = per_slot * U, n_look = n_hot <= HOT_CAP ? int32_t(n_hot) * each : 0;
             for (int32_t i = tid; i < n_look; i += NT) {
-                const int32_t v = v0 + sm.hot[i / rounds] + (i % rounds) * NT;
+                const int32_t h = sm.hot[i / each];
+                const int32_t v = v0 + ((h >> 8) * each + i % each) * NT + (h & 255);
                 if (v < v1) {
                     const uint4 w = __ldg(vecs + v);
                     float x[E];
@@ -409,7 +520,7 @@ __global__ void __launch_bounds__(NT, 4) disc_logprobs_kernel(const LogprobParam
             }
             __syncthreads();
             unsigned int cnt = sm.n_list;
-            if (cnt > LIST_CAP || cnt < want) {
+            if (n_hot > HOT_CAP || cnt > LIST_CAP || cnt < want) {
                 const int32_t e0 = rank == 0 ? 0 : r.head + v0 * E;
                 // the first block's slice is not one run of ids when others lie between it and the row's last
                 // elements; those few are put in by hand
@@ -430,7 +541,7 @@ __global__ void __launch_bounds__(NT, 4) disc_logprobs_kernel(const LogprobParam
     }
     if (tid == 0) {
         Sums t = sm.warp_sums[0];
-        for (int w = 1; w < NW; ++w) t = join(t, sm.warp_sums[w], p.c2);
+        for (int w = 1; w < NW; ++w) t = join(t, sm.warp_sums[w], k);
         sm.part = t;
         sm.found = found;
     }
@@ -454,7 +565,7 @@ __global__ void __launch_bounds__(NT, 4) disc_logprobs_kernel(const LogprobParam
                 for (int c = 1; c < p.split; ++c) {
                     const uint32_t q = remote(&sm.part, c);
                     Sums b{__uint_as_float(ld_remote32(q)), __uint_as_float(ld_remote32(q + 4)), __uint_as_float(ld_remote32(q + 8)), __uint_as_float(ld_remote32(q + 12))};
-                    t = join(t, b, p.c2);
+                    t = join(t, b, k);
                 }
                 sm.part = t;
             }
@@ -465,7 +576,7 @@ __global__ void __launch_bounds__(NT, 4) disc_logprobs_kernel(const LogprobParam
     __syncthreads();
 
     Sums t = sm.part;
-    bool far = fabsf(t.m) < CUDART_INF_F && fabsf(t.m * p.c2) >= FAR_Y && t.s == t.s;
+    bool far = fabsf(t.m) < CUDART_INF_F && !(t.m * p.c2 > p.low_y + 256.f && t.m * p.c2 < FAR_Y) && t.s == t.s;
     if (far) {                        // the largest logit itself is that far out: once more, with differences of logits
         Sums b{t.m, 0.f, 0.f, 0.f};
         for (int32_t e = tid; e < p.V; e += NT) {
@@ -614,7 +725,10 @@ int launch_logprobs(const LogprobParams& p, int64_t n, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(n * p.split));
     cfg.blockDim = dim3(NT);
-    cfg.dynamicSmemBytes = sizeof(Smem);
+    constexpr int bytes = sizeof(Smem) + (TOP ? sizeof(PortionMaxima<DT>) : 0);
+    static std::atomic<uint64_t> done{0};
+    if (const int rc = disc::allow_smem(disc_logprobs_kernel<DT, TOP>, bytes, done)) return rc;
+    cfg.dynamicSmemBytes = bytes;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -647,6 +761,8 @@ int disc_logprobs(const void* logits, disc_dtype_t dtype, int64_t ld, int64_t n,
     LogprobParams p;
     p.logits = logits; p.ld = ld; p.V = vocab_size; p.top = top;
     p.inv_t = inv_temperature; p.c2 = inv_temperature * LOG2E_F;
+    p.low = __bfloat162float(__float2bfloat16_rn(fmaxf(-FAR_Y / p.c2, -1.0e37f)));
+    p.low_y = p.low * p.c2;
     p.targets = targets; p.logp = logp_out; p.entropy = entropy_out; p.lse = lse_out;
     p.top_ids = top_ids_out; p.top_logp = top_logp_out; p.status = status_out;
     // too few rows to put a block on every SM: a row is shared by a cluster, as long as every block still has

@@ -33,6 +33,11 @@ def _rows(t: torch.Tensor, name: str):
     return t.data_ptr(), _LOGIT[t.dtype], t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
+def _own(t):
+    """Pointer of an output made here."""
+    return 0 if t is None else t.data_ptr()
+
+
 def _want(t, n: int, name: str):
     if t is not None and t.numel() != n:
         raise TypeError(f"{name}: expected {n} entries, got {t.numel()}")
@@ -53,11 +58,13 @@ def disc_logprobs(logits: torch.Tensor, targets: torch.Tensor | None = None, *, 
                "top_ids": torch.empty((n, top), dtype=torch.int32, device=logits.device) if top > 0 else None,
                "top_logp": torch.empty((n, top), **f) if top > 0 else None,
                "status": torch.empty(n, dtype=torch.uint8, device=logits.device)}
+    else:
+        for k in ("logp", "entropy", "lse", "top_ids", "top_logp", "status"):
+            _want(out[k], n * top if k.startswith("top") else n, k)
+            _dev(out[k], torch.int32 if k == "top_ids" else torch.uint8 if k == "status" else torch.float32, k)
     rc = lib().disc_logprobs(ptr, dt, ld, n, V, float(inv_temperature), _dev(targets, torch.int32, "targets"), int(top),
-                             _dev(out["logp"], torch.float32, "logp"), _dev(out["entropy"], torch.float32, "entropy"),
-                             _dev(out["lse"], torch.float32, "lse"), _dev(out["top_ids"], torch.int32, "top_ids"),
-                             _dev(out["top_logp"], torch.float32, "top_logp"), _dev(out["status"], torch.uint8, "status"),
-                             _stream_ptr(stream))
+                             _own(out["logp"]), _own(out["entropy"]), _own(out["lse"]), _own(out["top_ids"]),
+                             _own(out["top_logp"]), _own(out["status"]), _stream_ptr(stream))
     _check(rc, "disc_logprobs")
     return out
 
@@ -84,6 +91,18 @@ def disc_logprobs_grad(logits: torch.Tensor, targets, lse: torch.Tensor, entropy
 
 
 # ---- attention over prompts -------------------------------------------------------------------------
+def _attend_outputs(q: torch.Tensor, out, lse):
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape or not _dev(out, q.dtype, "out") and out.numel():
+        raise TypeError("out: expected q's shape")
+    if lse is None:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    elif lse.shape != q.shape[:2] or not _dev(lse, torch.float32, "lse") and lse.numel():
+        raise TypeError("lse: expected [tokens, heads] of q")
+    return out, lse
+
+
 _error_words: dict = {}
 
 
@@ -112,18 +131,11 @@ def disc_attend_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: 
     n_seqs = cu_q.numel() - 1
     if cu_k is not None:
         _want(cu_k, n_seqs + 1, "cu_k")
-    if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    elif out.shape != q.shape:
-        raise TypeError("out: expected q's shape")
-    if lse is None:
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-    elif lse.shape != q.shape[:2]:
-        raise TypeError("lse: expected [n_q, Hq]")
+    out, lse = _attend_outputs(q, out, lse)
     rc = lib().disc_attend_prompt(qp, qt, qh, kp, kt, kh, vp, vt, vh, dt, q.shape[1], k.shape[1], q.shape[2], q.shape[0],
                                   k.shape[0], _dev(cu_q, torch.int32, "cu_q"), _dev(cu_k, torch.int32, "cu_k"), n_seqs,
                                   int(max_len), int(causal), 1.0 / math.sqrt(q.shape[2]) if scale is None else float(scale),
-                                  _dev(out, q.dtype, "out"), _dev(lse, torch.float32, "lse"), _error_word(q.device).data_ptr(),
+                                  _own(out), _own(lse), _error_word(q.device).data_ptr(),
                                   _stream_ptr(stream))
     _check(rc, "disc_attend_prompt")
     return out, lse
@@ -194,7 +206,8 @@ def disc_cache_extend(cache: DiscCache, add: torch.Tensor | None = None, *, stat
     _want(add, cache.n_rows, "add")
     if status is None:
         status = torch.empty(cache.n_rows, dtype=torch.uint8, device=cache.pool.device)
-    _want(status, cache.n_rows, "status")
+    else:
+        _want(status, cache.n_rows, "status")
     _check(lib().disc_cache_extend(cache._p, _dev(add, torch.int32, "add"), _dev(status, torch.uint8, "status"),
                                    _stream_ptr(stream)), "disc_cache_extend")
     return status
@@ -257,16 +270,9 @@ def disc_attend_cached(cache: DiscCache, layer: int, q: torch.Tensor, plan: Atte
     qp, qr, qh = _vectors(q, cache.pool.dtype, "q")
     if tuple(q.shape) != (cache.n_rows, plan.n_q_heads, cache.head_dim):
         raise TypeError("q: expected [rows, Hq, head dim] of the cache and the plan")
-    if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    elif out.shape != q.shape:
-        raise TypeError("out: expected q's shape")
-    if lse is None:
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-    elif lse.shape != q.shape[:2]:
-        raise TypeError("lse: expected [rows, Hq]")
+    out, lse = _attend_outputs(q, out, lse)
     _check(lib().disc_attend_cached(cache._p, int(layer), qp, qr, qh, plan.n_q_heads, plan.group,
                                     1.0 / math.sqrt(cache.head_dim) if scale is None else float(scale), plan.buf.data_ptr(),
-                                    plan.nbytes, _dev(out, q.dtype, "out"), _dev(lse, torch.float32, "lse"),
+                                    plan.nbytes, _own(out), _own(lse),
                                     _stream_ptr(stream)), "disc_attend_cached")
     return out, lse
