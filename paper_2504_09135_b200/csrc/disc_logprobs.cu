@@ -35,6 +35,7 @@ namespace {
 constexpr int NT = 256;               // threads per block
 constexpr int NW = NT / 32;
 constexpr int TOP_MAX = 64;
+constexpr int SHORT_ROW = 1024;       // rows up to this long are held in a warp's registers
 constexpr int LIST_CAP = 2048;
 constexpr int HOT_CAP = 512;          // portions of the row that are looked at again
 constexpr int SLOTS = 32;             // portions of a thread
@@ -232,6 +233,20 @@ __device__ __forceinline__ Sums join(Sums a, Sums b, Scale k) {
     a.u += b.u;
     return a;
 }
+// over the first N lanes of the warp (a power of two); called by all of them
+template <int N>
+__device__ __forceinline__ Sums join_lanes(Sums a, Scale k) {
+#pragma unroll
+    for (int o = N / 2; o > 0; o >>= 1) {
+        Sums b;
+        b.m = __shfl_xor_sync(FULL, a.m, o);
+        b.ref = __shfl_xor_sync(FULL, a.ref, o);
+        b.s = __shfl_xor_sync(FULL, a.s, o);
+        b.u = __shfl_xor_sync(FULL, a.u, o);
+        a = join(a, b, k);
+    }
+    return a;
+}
 // a thread's running sums, even and odd elements apart
 struct Running {
     float m, ref;
@@ -255,13 +270,13 @@ __device__ __forceinline__ void add(Running& a, float2 x, float2 c2, float2 down
 
 // shared memory of a block; the other blocks of the cluster read `part`, `found` and `list`
 struct Smem {
-    unsigned long long list[LIST_CAP];                 // order key << 32 | ~id : larger = better
+    unsigned long long list[LIST_CAP + 8];             // order key << 32 | ~id : larger = better
     unsigned long long best[TOP_MAX];
     uint32_t keys[NT];
     int32_t hot[HOT_CAP];                              // portion << 8 | thread
     unsigned int hist[256];
     Sums warp_sums[NW];
-    Sums part;
+    Sums part, row;                                    // of the block; of the row, in a cluster's first block
     unsigned int n_hot, n_list, threshold, found;
     unsigned int prefix, remaining;
     int scan[NW];
@@ -300,12 +315,21 @@ __device__ __forceinline__ unsigned long long ld_remote64(uint32_t a) {
     return v;
 }
 
-// Of the cnt entries of sm.list the `want` best, in order, into sm.best.  Entries are distinct.
+// Of the cnt entries of sm.list the `want` best, in order, into sm.best.  Entries are distinct and not 0.  Called by the
+// whole block.
 __device__ __forceinline__ void rank_list(Smem& sm, unsigned int cnt, unsigned int want) {
+    if (threadIdx.x < 8) sm.list[cnt + threadIdx.x] = 0ull;       // up to a whole number of eights
+    __syncthreads();
     for (unsigned int i = threadIdx.x; i < cnt; i += NT) {
         const unsigned long long e = sm.list[i];
         unsigned int r = 0;
-        for (unsigned int j = 0; j < cnt; ++j) r += sm.list[j] > e;
+        for (unsigned int j = 0; j < cnt; j += 8) {
+#pragma unroll
+            for (int x = 0; x < 8; x += 2) {
+                const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(&sm.list[j + x]);
+                r += (two.x > e) + (two.y > e);
+            }
+        }
         if (r < want) sm.best[r] = e;
     }
     __syncthreads();
@@ -392,10 +416,115 @@ __device__ __noinline__ void select_slice(const char* base, int32_t e0, int32_t 
     __syncthreads();
 }
 
+// ---- what a row's sums give -----------------------------------------------------------------------------
+struct RowResult {
+    float lse, entropy;
+    uint8_t status;
+};
+// far: t's sums are relative to its largest logit itself, not to the clamped reference
+__device__ __forceinline__ RowResult row_result(const LogprobParams& p, const Sums& t, bool far) {
+    if (t.s != t.s || t.u != t.u || t.m == CUDART_INF_F)
+        return {t.m == CUDART_INF_F && t.s == t.s ? CUDART_INF_F : CUDART_NAN_F, CUDART_NAN_F, DISC_ROW_NONFINITE};
+    if (!(t.m > -CUDART_INF_F)) return {-CUDART_INF_F, 0.f, DISC_ROW_NOMASS};
+    const float l2 = log2f(t.s);
+    return {far ? fmaf(t.m, p.inv_t, l2 * LN2_F) : fmaf(t.ref, LN2_F, l2 * LN2_F), fmaxf(0.f, LN2_F * (l2 - t.u / t.s)), 0};
+}
+// one thread
+template <int DT>
+__device__ __forceinline__ void store_row(const LogprobParams& p, int64_t row, const char* base, RowResult r) {
+    if (p.lse) p.lse[row] = r.lse;
+    if (p.entropy) p.entropy[row] = r.entropy;
+    if (p.targets) {
+        const int32_t tok = p.targets[row];
+        float lp = 0.f;
+        if (tok >= 0 && tok < p.V) {
+            const float x = Vec<DT>::at(base + size_t(tok) * Vec<DT>::SIZE);
+            lp = r.status & DISC_ROW_NOMASS ? -CUDART_INF_F : x * p.inv_t - r.lse;
+        } else if (tok != -1) {
+            lp = CUDART_NAN_F;
+            r.status |= DISC_ROW_DEAD;
+        }
+        if (p.logp) p.logp[row] = lp;
+    }
+    p.status[row] = r.status;
+}
+// the i-th alternative; -1 where there is none
+__device__ __forceinline__ void store_top(const LogprobParams& p, int64_t row, unsigned int i, unsigned long long e, bool some, const RowResult& r) {
+    p.top_ids[row * p.top + i] = some ? int32_t(~uint32_t(e)) : -1;
+    if (p.top_logp)
+        p.top_logp[row * p.top + i] = some && !(r.status & DISC_ROW_NOMASS) ? key_value(uint32_t(e >> 32)) * p.inv_t - r.lse : -CUDART_INF_F;
+}
+
+// ---- short rows --------------------------------------------------------------------------------------------
+// Up to 32 EPL logits: a warp per row, the row in registers.  (A block per row would spend its time on barriers.)  The
+// alternatives are taken one after the other, each lane offering its best.
+template <int DT, int EPL>
+__global__ void __launch_bounds__(NT) disc_logprobs_short_kernel(const LogprobParams p, int64_t n) {
+    const int lane = threadIdx.x & 31;
+    const int64_t row = (int64_t(blockIdx.x) * NT + threadIdx.x) >> 5;
+    if (row >= n) return;
+    const char* base = static_cast<const char*>(p.logits) + row * p.ld * Vec<DT>::SIZE;
+    float x[EPL];
+#pragma unroll
+    for (int j = 0; j < EPL; ++j) x[j] = lane + 32 * j < p.V ? Vec<DT>::at(base + size_t(lane + 32 * j) * Vec<DT>::SIZE) : -CUDART_INF_F;
+    float mx = x[0];
+#pragma unroll
+    for (int j = 1; j < EPL; ++j) mx = fmaxf(mx, x[j]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(FULL, mx, o));
+    // relative to the maximum itself: no logit is too far out
+    const float m = fabsf(mx) < CUDART_INF_F ? mx : 0.f;
+    Sums t{mx == mx ? mx : -CUDART_INF_F, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < EPL; ++j) {
+        const float d = max_nan((x[j] - m) * p.c2, Y_MIN), e = ex2_approx(d);
+        t.s += e;
+        t.u = fmaf(d, e, t.u);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        t.s += __shfl_xor_sync(FULL, t.s, o);
+        t.u += __shfl_xor_sync(FULL, t.u, o);
+    }
+    const RowResult res = row_result(p, t, true);
+    if (lane == 0) store_row<DT>(p, row, base, res);
+    if (p.top == 0) return;
+    uint32_t key[EPL];                // + 1: 0 is what has been taken or is not there
+#pragma unroll
+    for (int j = 0; j < EPL; ++j) key[j] = lane + 32 * j < p.V ? max(order_key(x[j]), 1u) : 0u;
+    const int some = min(p.top, p.V);
+    uint32_t best = 0u;
+    int at = -1;
+    auto offer = [&]() {
+        best = 0u;
+        at = -1;
+#pragma unroll
+        for (int j = 0; j < EPL; ++j)
+            if (key[j] > best) { best = key[j]; at = j; }
+    };
+    offer();
+    for (int i = 0; i < p.top; ++i) {
+        unsigned long long e = 0ull;
+        if (i < some) {
+            const uint32_t hi = __reduce_max_sync(FULL, best);
+            const int32_t id = best == hi && at >= 0 ? lane + 32 * at : 0x7fffffff;
+            const int32_t won = __reduce_min_sync(FULL, id);
+            if (id == won) {
+#pragma unroll
+                for (int j = 0; j < EPL; ++j)
+                    if (j == at) key[j] = 0u;
+                offer();
+            }
+            e = entry(hi, won);
+        }
+        if (lane == (i & 31)) store_top(p, row, i, e, i < some, res);
+    }
+}
+
 constexpr int U = 4;                  // 16-byte loads a thread keeps in flight
 
 template <int DT, bool TOP>
-__global__ void __launch_bounds__(NT, 4) disc_logprobs_kernel(const LogprobParams p) {
+__global__ void __launch_bounds__(NT, 5) disc_logprobs_kernel(const LogprobParams p) {
     constexpr int E = Vec<DT>::E, SIZE = Vec<DT>::SIZE;
     extern __shared__ unsigned char smem_raw[];
     Smem& sm = *reinterpret_cast<Smem*>(smem_raw);
@@ -461,15 +590,7 @@ __global__ void __launch_bounds__(NT, 4) disc_logprobs_kernel(const LogprobParam
     Sums a{run.m, run.ref, run.s.x + run.s.y, run.u.x + run.u.y};
 
     const float own_max = run.m;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        Sums b;
-        b.m = __shfl_xor_sync(FULL, a.m, o);
-        b.ref = __shfl_xor_sync(FULL, a.ref, o);
-        b.s = __shfl_xor_sync(FULL, a.s, o);
-        b.u = __shfl_xor_sync(FULL, a.u, o);
-        a = join(a, b, k);
-    }
+    a = join_lanes<32>(a, k);
     if (lane == 0) sm.warp_sums[warp] = a;
     const uint32_t key = v0 + tid < v1 || extra >= 0 ? order_key(own_max) : 0u;
     unsigned int found = 0;
@@ -478,6 +599,10 @@ __global__ void __launch_bounds__(NT, 4) disc_logprobs_kernel(const LogprobParam
         if (tid == 0) { sm.n_hot = 0u; sm.n_list = 0u; }
     }
     __syncthreads();
+    if (warp == 1) {                  // beside the selection, which the first warp begins
+        const Sums t = join_lanes<NW>(sm.warp_sums[lane % NW], k);
+        if (lane == 0) sm.part = t;
+    }
     if (TOP) {
         const int32_t elements = (v1 - v0) * E + (rank == 0 ? r.head + r.tail : 0);
         const unsigned int want = min(unsigned(p.top), unsigned(elements));
@@ -539,35 +664,39 @@ __global__ void __launch_bounds__(NT, 4) disc_logprobs_kernel(const LogprobParam
         }
         found = want;
     }
-    if (tid == 0) {
-        Sums t = sm.warp_sums[0];
-        for (int w = 1; w < NW; ++w) t = join(t, sm.warp_sums[w], k);
-        sm.part = t;
-        sm.found = found;
-    }
+    if (TOP && tid == 0) sm.found = found;
     if (p.split > 1) {
         cluster_sync_all();
         if (rank == 0) {
+            if (warp == 1) {
+                Sums t{-CUDART_INF_F, 0.f, 0.f, 0.f};
+                if (lane < p.split) {
+                    const uint32_t q = remote(&sm.part, lane);
+                    t = Sums{__uint_as_float(ld_remote32(q)), __uint_as_float(ld_remote32(q + 4)), __uint_as_float(ld_remote32(q + 8)), __uint_as_float(ld_remote32(q + 12))};
+                }
+                t = join_lanes<8>(t, k);
+                __syncwarp();
+                if (lane == 0) sm.row = t;
+            }
             if (TOP) {
                 // all blocks' lists together: at most 8 x 64 entries
-                unsigned int at = 0;
-                for (int c = 0; c < p.split; ++c) {
-                    const unsigned int f = ld_remote32(remote(&sm.found, c));
-                    for (unsigned int i = tid; i < f; i += NT) sm.list[at + i] = ld_remote64(remote(&sm.best[i], c));
-                    at += f;
+                const unsigned int f = lane < p.split ? ld_remote32(remote(&sm.found, lane)) : 0u;
+                unsigned int upto = f;
+#pragma unroll
+                for (int o = 1; o < 8; o <<= 1) {
+                    const unsigned int u = __shfl_up_sync(FULL, upto, o);
+                    if (lane >= o) upto += u;
+                }
+                const unsigned int all = __shfl_sync(FULL, upto, 7);
+                for (unsigned int i = tid; i < 8 * TOP_MAX; i += NT) {
+                    const int c = int(i) / TOP_MAX;
+                    const unsigned int j = i % TOP_MAX;
+                    const unsigned int n = __shfl_sync(FULL, f, c), before = __shfl_sync(FULL, upto, c) - n;
+                    if (j < n) sm.list[before + j] = ld_remote64(remote(&sm.best[j], c));
                 }
                 __syncthreads();
-                found = min(unsigned(p.top), at);
-                rank_list(sm, at, found);
-            }
-            if (tid == 0) {
-                Sums t = sm.part;
-                for (int c = 1; c < p.split; ++c) {
-                    const uint32_t q = remote(&sm.part, c);
-                    Sums b{__uint_as_float(ld_remote32(q)), __uint_as_float(ld_remote32(q + 4)), __uint_as_float(ld_remote32(q + 8)), __uint_as_float(ld_remote32(q + 12))};
-                    t = join(t, b, k);
-                }
-                sm.part = t;
+                found = min(unsigned(p.top), all);
+                rank_list(sm, all, found);
             }
         }
         cluster_sync_all();
@@ -575,7 +704,7 @@ __global__ void __launch_bounds__(NT, 4) disc_logprobs_kernel(const LogprobParam
     }
     __syncthreads();
 
-    Sums t = sm.part;
+    Sums t = p.split > 1 ? sm.row : sm.part;
     bool far = fabsf(t.m) < CUDART_INF_F && !(t.m * p.c2 > p.low_y + 256.f && t.m * p.c2 < FAR_Y) && t.s == t.s;
     if (far) {                        // the largest logit itself is that far out: once more, with differences of logits
         Sums b{t.m, 0.f, 0.f, 0.f};
@@ -594,51 +723,10 @@ __global__ void __launch_bounds__(NT, 4) disc_logprobs_kernel(const LogprobParam
         t.s = t.u = 0.f;
         for (int w = 0; w < NW; ++w) { t.s += sm.warp_sums[w].s; t.u += sm.warp_sums[w].u; }
     }
-    uint8_t status = 0;
-    float lse, h;
-    if (t.s != t.s || t.u != t.u || t.m == CUDART_INF_F) {
-        status = DISC_ROW_NONFINITE;
-        lse = t.m == CUDART_INF_F && t.s == t.s ? CUDART_INF_F : CUDART_NAN_F;
-        h = CUDART_NAN_F;
-    } else if (!(t.m > -CUDART_INF_F)) {
-        status = DISC_ROW_NOMASS;
-        lse = -CUDART_INF_F;
-        h = 0.f;
-    } else {
-        const float l2 = log2f(t.s);
-        lse = far ? fmaf(t.m, p.inv_t, l2 * LN2_F) : fmaf(t.ref, LN2_F, l2 * LN2_F);
-        h = fmaxf(0.f, LN2_F * (l2 - t.u / t.s));
-    }
-    if (tid == 0) {
-        if (p.lse) p.lse[row] = lse;
-        if (p.entropy) p.entropy[row] = h;
-        if (p.targets) {
-            const int32_t tok = p.targets[row];
-            float lp = 0.f;
-            if (tok >= 0 && tok < p.V) {
-                const float x = Vec<DT>::at(r.base + size_t(tok) * SIZE);
-                lp = status & DISC_ROW_NOMASS ? -CUDART_INF_F : x * p.inv_t - lse;
-            } else if (tok != -1) {
-                lp = CUDART_NAN_F;
-                status |= DISC_ROW_DEAD;
-            }
-            if (p.logp) p.logp[row] = lp;
-        }
-        p.status[row] = status;
-    }
-    if (TOP) {
-        for (unsigned int i = tid; i < unsigned(p.top); i += NT) {
-            int32_t id = -1;
-            float lp = -CUDART_INF_F;
-            if (i < found) {
-                const unsigned long long e = sm.best[i];
-                id = int32_t(~uint32_t(e));
-                if (!(status & DISC_ROW_NOMASS)) lp = key_value(uint32_t(e >> 32)) * p.inv_t - lse;
-            }
-            p.top_ids[row * p.top + i] = id;
-            if (p.top_logp) p.top_logp[row * p.top + i] = lp;
-        }
-    }
+    const RowResult res = row_result(p, t, far);
+    if (tid == 0) store_row<DT>(p, row, r.base, res);
+    if (TOP)
+        for (unsigned int i = tid; i < unsigned(p.top); i += NT) store_top(p, row, i, i < found ? sm.best[i] : 0ull, i < found, res);
 }
 
 // ---- gradient ---------------------------------------------------------------------------------------
@@ -650,7 +738,7 @@ struct GradParams {
     int64_t ld;
     void* grad;
     int64_t grad_ld;
-    int32_t V, blocks_per_row;
+    int32_t V, teams_per_row;
     float inv_t, c2;
     const int32_t* targets;           // nullable
     const float* lse;
@@ -668,12 +756,15 @@ struct RowGrad {
     }
 };
 
-template <int DT>
-__global__ void __launch_bounds__(NT) disc_logprobs_grad_kernel(const GradParams p) {
+// TEAM threads work on a portion of a row: a block, or a warp where a warp's loads cover the row.
+template <int DT, int TEAM>
+__global__ void __launch_bounds__(NT) disc_logprobs_grad_kernel(const GradParams p, int64_t n) {
     constexpr int E = Vec<DT>::E, SIZE = Vec<DT>::SIZE;
-    const int64_t row = blockIdx.x / unsigned(p.blocks_per_row);
-    const int32_t part = int32_t(blockIdx.x - row * p.blocks_per_row);
-    const int tid = threadIdx.x;
+    const int64_t team = (int64_t(blockIdx.x) * NT + threadIdx.x) / TEAM;
+    const int64_t row = TEAM == NT ? int64_t(blockIdx.x / unsigned(p.teams_per_row)) : team;
+    const int32_t part = TEAM == NT ? int32_t(blockIdx.x - row * p.teams_per_row) : 0;
+    const int tid = threadIdx.x % TEAM;
+    if (row >= n) return;
     const RowShape<DT> r(p.logits, p.ld, row, p.V);
     char* out = static_cast<char*>(p.grad) + row * p.grad_ld * SIZE;
     const int32_t tok = p.targets ? p.targets[row] : -1;
@@ -693,13 +784,13 @@ __global__ void __launch_bounds__(NT) disc_logprobs_grad_kernel(const GradParams
     const uint4* vecs = r.vecs();
     char* out_vecs = out + size_t(r.head) * SIZE;
     uint4 w[U];
-    const int32_t v0 = part * (NT * U) + tid;
+    const int32_t v0 = part * (TEAM * U) + tid;
 #pragma unroll
     for (int u = 0; u < U; ++u)
-        if (v0 + u * NT < r.nvec) w[u] = ld_stream(vecs + v0 + u * NT);
+        if (v0 + u * TEAM < r.nvec) w[u] = ld_stream(vecs + v0 + u * TEAM);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const int32_t v = v0 + u * NT;
+        const int32_t v = v0 + u * TEAM;
         if (v < r.nvec) {
             float x[E];
             Vec<DT>::unpack(w[u], x);
@@ -718,6 +809,17 @@ __global__ void __launch_bounds__(NT) disc_logprobs_grad_kernel(const GradParams
         else if (tid - r.head < r.tail) e = r.head + r.nvec * E + tid - r.head;
         if (e >= 0) Vec<DT>::put(out + size_t(e) * SIZE, g.at(Vec<DT>::at(r.base + size_t(e) * SIZE), p.c2) + (e == tok ? a_t : 0.f));
     }
+}
+
+template <int DT, int EPL>
+int launch_short(const LogprobParams& p, int64_t n, cudaStream_t st) {
+    disc_logprobs_short_kernel<DT, EPL><<<unsigned((n * 32 + NT - 1) / NT), NT, 0, st>>>(p, n);
+    DISC_CUDA(cudaGetLastError());
+    return DISC_OK;
+}
+template <int DT>
+int launch_short(const LogprobParams& p, int64_t n, cudaStream_t st) {
+    return p.V <= 256 ? launch_short<DT, 8>(p, n, st) : launch_short<DT, 32>(p, n, st);
 }
 
 template <int DT, bool TOP>
@@ -771,6 +873,9 @@ int disc_logprobs(const void* logits, disc_dtype_t dtype, int64_t ld, int64_t n,
     const int64_t vecs = vocab_size / (dtype == DISC_F32 ? 4 : 8);
     while (p.split < 8 && n * p.split * 2 <= 2 * sms && vecs / (p.split * 2) >= NT) p.split *= 2;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    // Short rows: 4096 rows of 256 take 19 us with 20 alternatives and 45 with 64 by warps, 41 and 74 by blocks; of 1000, 14 us
+    // with one, 45 with 20 and 115 with 64 by warps, 39, 43 and 51 by blocks.
+    if (vocab_size <= 256 || (vocab_size <= SHORT_ROW && top <= 20)) return dtype == DISC_F32 ? launch_short<DISC_F32>(p, n, st) : launch_short<DISC_BF16>(p, n, st);
     if (dtype == DISC_F32) return top ? launch_logprobs<DISC_F32, true>(p, n, st) : launch_logprobs<DISC_F32, false>(p, n, st);
     return top ? launch_logprobs<DISC_BF16, true>(p, n, st) : launch_logprobs<DISC_BF16, false>(p, n, st);
 }
@@ -789,14 +894,20 @@ int disc_logprobs_grad(const void* logits, disc_dtype_t dtype, int64_t ld, int64
     const int64_t vecs = vocab_size / (dtype == DISC_F32 ? 4 : 8);
     GradParams p;
     p.logits = logits; p.ld = ld; p.grad = grad_out; p.grad_ld = grad_ld; p.V = vocab_size;
-    p.blocks_per_row = int32_t(vecs / (NT * U) + 1);
     p.inv_t = inv_temperature; p.c2 = inv_temperature * LOG2E_F;
     p.targets = targets; p.lse = lse; p.entropy = entropy; p.d_logp = d_logp; p.d_entropy = d_entropy;
-    if (n * p.blocks_per_row > 0x7fffffff) return DISC_ERR_UNSUPPORTED;
-    const unsigned grid = unsigned(n * p.blocks_per_row);
+    const bool warps = vecs <= 32 * U;
+    p.teams_per_row = warps ? 1 : int32_t(vecs / (NT * U) + 1);
+    if (n * p.teams_per_row > 0x7fffffff) return DISC_ERR_UNSUPPORTED;
+    const unsigned grid = warps ? unsigned((n + NW - 1) / NW) : unsigned(n * p.teams_per_row);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (dtype == DISC_F32) disc_logprobs_grad_kernel<DISC_F32><<<grid, NT, 0, st>>>(p);
-    else disc_logprobs_grad_kernel<DISC_BF16><<<grid, NT, 0, st>>>(p);
+    if (dtype == DISC_F32) {
+        if (warps) disc_logprobs_grad_kernel<DISC_F32, 32><<<grid, NT, 0, st>>>(p, n);
+        else disc_logprobs_grad_kernel<DISC_F32, NT><<<grid, NT, 0, st>>>(p, n);
+    } else {
+        if (warps) disc_logprobs_grad_kernel<DISC_BF16, 32><<<grid, NT, 0, st>>>(p, n);
+        else disc_logprobs_grad_kernel<DISC_BF16, NT><<<grid, NT, 0, st>>>(p, n);
+    }
     DISC_CUDA(cudaGetLastError());
     return DISC_OK;
 }
