@@ -9,14 +9,17 @@
 // that a row has for itself follow in the same stream, each with its owner, and the other rows' scores are
 // set to -inf there.  What bounds the kernel is then the bytes of the distinct pages.
 //
+// Two forms, by the number M of query vectors that read the same pages (rows of the group x query heads per
+// key head).  M <= 16, this file: mma.sync m16n8k16 on one tile of 16 rows, far from being the bound.  M > 16,
+// disc_attend_group.cu: tcgen05 on tiles of 128 rows.
+//
 // Plan (one cluster of 8 blocks): per group the number of leading pages its rows share, and the stream as a
 // list of blocks of 16 tokens (page, block in the page, tokens in it, owner); from the lengths of
 // the lists the items: runs of blocks, about as many as there are places for them on the device.
 //
 // Attention: a block of 4 warps per item and key head; blocks of 16 tokens come in through cp.async, three
-// tiles of 64 tokens deep.  M <= 16: every warp takes its own block of 16 tokens of a tile with all the rows, so that the
-// warps need no barrier in the loop; their results are joined at the end.  M <= 64: every warp takes 16 rows
-// and all the tokens.  mma.sync m16n8k16: with M below 64 the bytes take longer than the products.
+// tiles of 64 tokens deep.  Every warp takes its own block of 16 tokens of a tile with all the rows, so that the
+// warps need no barrier in the loop; their results are joined at the end.
 // Running maximum and sum per row in fp32, in units of log2.  An item that is not its group's only one
 // writes its rows' normalised sum and log-sum-exp; the block that finishes last joins them in the
 // order of the items.
@@ -25,7 +28,7 @@
 #include <cuda_fp16.h>
 #include <math_constants.h>
 
-#include "disc_internal.cuh"
+#include "disc_attend.cuh"
 
 namespace {
 
@@ -34,84 +37,13 @@ using namespace disc;
 constexpr unsigned FULL = 0xffffffffu;
 constexpr float LOG2E_F = 1.4426950408889634f;
 constexpr float LN2_F = 0.6931471805599453f;
-constexpr int BLK = 16;                // tokens of a block
 constexpr int TILE_BLKS = 4;           // blocks of a tile
 constexpr int TILE = BLK * TILE_BLKS;
 constexpr int STAGES = 3;
-constexpr int M_MAX = 64;
 constexpr int CLUSTER = 8;
 constexpr int PT = 512;                // threads of a plan block
 
 // ---- the plan ---------------------------------------------------------------------------------------
-struct PlanShape {
-    int32_t G;                         // query heads per key head
-    int32_t per_group;                 // rows of a group as it is worked on
-    int32_t sub;                       // such groups per `group` rows
-    int32_t groups;                    // in all
-    int32_t M;                         // query vectors of a group
-    int32_t blks_per_page;
-    int64_t list_ld;                   // blocks a group's list has room for
-    int32_t max_items, max_slots;
-};
-struct Plan {
-    int32_t* head;                     // [0] items
-    int32_t* count;                    // [groups] blocks
-    int32_t* splits;                   // [groups]
-    int32_t* slot;                     // [groups] first partial result, or -1
-    int32_t* arrived;                  // [groups][kv heads]
-    int4* items;                       // group, first block, one past the last, index among the group's items
-    int2* list;                        // [groups][list_ld]: page; block | tokens << 8 | (owner + 1) << 16
-    float* part;                       // [slots][kv heads][M][head_dim]
-    float* part_lse;                   // [slots][kv heads][M], log2
-};
-constexpr int PLAN_UNITS = 148 * 4;    // items x key heads aimed at: two rounds of the blocks the device has places for
-
-inline int64_t up16(int64_t b) { return (b + 15) & ~int64_t(15); }
-
-inline int plan_shape(const disc_cache_t* c, int32_t hq, int32_t group, PlanShape* s) {
-    if (hq <= 0 || group <= 0 || c->n_kv_heads <= 0 || hq % c->n_kv_heads) return DISC_ERR_ARG;
-    s->G = hq / c->n_kv_heads;
-    if (s->G > M_MAX) return DISC_ERR_UNSUPPORTED;
-    if (group > c->n_rows) group = c->n_rows;
-    s->per_group = group < M_MAX / s->G ? group : M_MAX / s->G;
-    s->sub = (group + s->per_group - 1) / s->per_group;
-    const int64_t groups = (int64_t(c->n_rows) + group - 1) / group * s->sub;
-    if (groups > (1 << 26) || s->per_group > 0x7ffe) return DISC_ERR_UNSUPPORTED;
-    s->groups = int32_t(groups);
-    s->M = s->per_group * s->G;
-    s->blks_per_page = c->page_size / BLK;
-    s->list_ld = int64_t(s->per_group) * c->table_width * s->blks_per_page;
-    const int32_t aim = (PLAN_UNITS + c->n_kv_heads - 1) / c->n_kv_heads;
-    s->max_slots = 2 * aim + 2;
-    s->max_items = s->groups + s->max_slots;
-    return DISC_OK;
-}
-inline int64_t plan_layout(const disc_cache_t* c, const PlanShape& s, void* base_, Plan* p) {
-    unsigned char* base = static_cast<unsigned char*>(base_);
-    int64_t at = 0;
-    auto take = [&](int64_t bytes) { unsigned char* q = base + at; at += up16(bytes); return q; };
-    Plan t;
-    t.head = reinterpret_cast<int32_t*>(take(256));
-    t.count = reinterpret_cast<int32_t*>(take(int64_t(s.groups) * 4));
-    t.splits = reinterpret_cast<int32_t*>(take(int64_t(s.groups) * 4));
-    t.slot = reinterpret_cast<int32_t*>(take(int64_t(s.groups) * 4));
-    t.arrived = reinterpret_cast<int32_t*>(take(int64_t(s.groups) * c->n_kv_heads * 4));
-    t.items = reinterpret_cast<int4*>(take(int64_t(s.max_items) * 16));
-    t.list = reinterpret_cast<int2*>(take(int64_t(s.groups) * s.list_ld * 8));
-    t.part = reinterpret_cast<float*>(take(int64_t(s.max_slots) * c->n_kv_heads * s.M * c->head_dim * 4));
-    t.part_lse = reinterpret_cast<float*>(take(int64_t(s.max_slots) * c->n_kv_heads * s.M * 4));
-    if (p) *p = t;
-    return at;
-}
-
-struct PlanParams {
-    Plan plan;
-    PlanShape shape;
-    const int32_t* table;
-    const int32_t* len;
-    int32_t rows, group, width, page_size, shift, kv_heads, aim;
-};
-
 __device__ __forceinline__ void cluster_sync_all() {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -133,8 +65,8 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(PT) attend_pla
 
     // a warp per group: the leading pages that its rows share, and its list of blocks
     for (int32_t g = blockIdx.x * (PT / 32) + warp; g < sh.groups; g += CLUSTER * (PT / 32)) {
-        const int32_t r0 = g / sh.sub * p.group + g % sh.sub * sh.per_group;
-        const int32_t r1 = min(p.rows, min(r0 + sh.per_group, g / sh.sub * p.group + p.group));
+        const int32_t r0 = g / sh.sub * sh.group + g % sh.sub * sh.per_group;
+        const int32_t r1 = min(p.rows, min(r0 + sh.per_group, g / sh.sub * sh.group + sh.group));
         int2* list = p.plan.list + int64_t(g) * sh.list_ld;
         const int32_t n = r1 - r0;
         int32_t shared = 0;
@@ -180,7 +112,7 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(PT) attend_pla
     int64_t all = 0;
     for (int w = 0; w < PT / 32; ++w) all += warp_sums[w][0];
     __syncthreads();
-    int32_t len = int32_t((all + p.aim - 1) / p.aim);
+    int32_t len = int32_t((all + sh.aim - 1) / sh.aim);
     len = max(TILE_BLKS, (len + TILE_BLKS - 1) / TILE_BLKS * TILE_BLKS);
     int32_t items = 0, slots = 0;
     for (int32_t g0 = 0; g0 < sh.groups; g0 += PT) {
@@ -205,23 +137,10 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(PT) attend_pla
             for (int32_t i = 0; i < splits; ++i) p.plan.items[i0 + i] = make_int4(g, i * len, min(n, (i + 1) * len), i);
         }
     }
-    if (tid == 0) p.plan.head[0] = items;
+    if (tid == 0) { p.plan.head[0] = 0; p.plan.head[1] = items; }
 }
 
 // ---- attention --------------------------------------------------------------------------------------
-struct AttendParams {
-    Plan plan;
-    PlanShape shape;
-    const unsigned char* k;            // this layer's planes
-    const unsigned char* v;
-    const unsigned char* q;
-    int64_t q_row, q_head;             // bytes
-    unsigned char* out;
-    float* lse;
-    int32_t rows, group, kv_heads, D, page_size;
-    float c2;                          // scale log2(e)
-};
-
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return uint32_t(__cvta_generic_to_shared(p)); }
 // 16 bytes into shared memory; zeros when !some
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool some) {
@@ -272,11 +191,11 @@ struct Num<__half> {
 
 constexpr int AT = 128;                // threads of an attention block
 
-template <int DP, int MW>
+template <int DP>
 struct AttendSmem {
     static constexpr int ROW = DP * 2;                             // bytes of a token's vector
     static constexpr int TILE_BYTES = TILE * ROW;                  // keys or values of a tile
-    static constexpr int Q_BYTES = 16 * MW * ROW;
+    static constexpr int Q_BYTES = 16 * ROW;
     static constexpr int BYTES = STAGES * 2 * TILE_BYTES + Q_BYTES + 256;
 };
 
@@ -287,11 +206,10 @@ __device__ __forceinline__ uint32_t chunk_at(int row, int ch) {
     return uint32_t(row * (DP * 2) + ((ch ^ (row & 7)) << 4));
 }
 
-template <typename T, int DP, int MW>
+template <typename T, int DP>
 __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams p) {
-    using S = AttendSmem<DP, MW>;
+    using S = AttendSmem<DP>;
     constexpr int CH = DP / 8;                                     // chunks of a row
-    constexpr int NB = MW == 1 ? 1 : TILE_BLKS;                    // blocks of a tile that a warp works on
     extern __shared__ __align__(128) unsigned char smem[];
     unsigned char* q_smem = smem + STAGES * 2 * S::TILE_BYTES;
     volatile int32_t* meta = reinterpret_cast<volatile int32_t*>(q_smem + S::Q_BYTES);      // [STAGES][TILE_BLKS]
@@ -301,16 +219,15 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const PlanShape& sh = p.shape;
     const int G = sh.G;
-    const int n_units = p.plan.head[0] * p.kv_heads;
-    const int row_lo = (MW == 1 ? 0 : warp * 16) + (lane >> 2);    // this thread's two rows of the tile: row_lo, row_lo + 8
+    const int n_units = p.plan.head[1] * p.kv_heads;
+    const int row_lo = lane >> 2;                                  // this thread's two rows of the tile: row_lo, row_lo + 8
     const int own_lo = row_lo / G + 1, own_hi = (row_lo + 8) / G + 1;
-    const int first_owner = (MW == 1 ? 0 : warp * 16) / G + 1, last_owner = (MW == 1 ? 15 : warp * 16 + 15) / G + 1;
 
     for (int unit = blockIdx.x; unit < n_units; unit += gridDim.x) {
         const int4 item = p.plan.items[unit / p.kv_heads];
         const int head = unit % p.kv_heads, g = item.x;
-        const int32_t r0 = g / sh.sub * p.group + g % sh.sub * sh.per_group;
-        const int32_t n_rows = max(0, min(p.rows, min(r0 + sh.per_group, g / sh.sub * p.group + p.group)) - r0);
+        const int32_t r0 = g / sh.sub * sh.group + g % sh.sub * sh.per_group;
+        const int32_t n_rows = max(0, min(p.rows, min(r0 + sh.per_group, g / sh.sub * sh.group + sh.group)) - r0);
         const int M = n_rows * G;
         const int2* list = p.plan.list + int64_t(g) * sh.list_ld;
         const int n_tiles = (item.z - item.y + TILE_BLKS - 1) / TILE_BLKS;
@@ -342,7 +259,7 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
             cp_commit();
         }
         // query vectors: row m of the tile is row m / G, head m % G of the group's heads
-        for (int i = tid; i < 16 * MW * CH; i += AT) {
+        for (int i = tid; i < 16 * CH; i += AT) {
             const int m = i / CH, ch = i % CH;
             uint4 x = make_uint4(0, 0, 0, 0);
             if (m < M && ch * 8 < p.D)
@@ -353,7 +270,7 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
         uint32_t qf[DP / 16][4];
 #pragma unroll
         for (int kk = 0; kk < DP / 16; ++kk)
-            ldsm4(smem_u32(q_smem) + chunk_at<DP>((MW == 1 ? 0 : warp * 16) + (lane & 15), 2 * kk + (lane >> 4)), qf[kk]);
+            ldsm4(smem_u32(q_smem) + chunk_at<DP>(lane & 15, 2 * kk + (lane >> 4)), qf[kk]);
 
         float o[DP / 8][4];
 #pragma unroll
@@ -362,48 +279,36 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
 
         for (int t = 0; t < n_tiles; ++t) {
             cp_wait<STAGES - 2>();
-            if (MW == 1) __syncwarp(); else __syncthreads();
+            __syncwarp();                                          // a warp works on what it has brought in itself
             if (t + STAGES - 1 < n_tiles) load_tile(t + STAGES - 1);
             cp_commit();
             const int stage = t % STAGES;
             const uint32_t kt = smem_u32(smem + stage * 2 * S::TILE_BYTES), vt = kt + S::TILE_BYTES;
-            float s[NB * 2][4];
-            int tokens[NB], owner[NB];
+            float s[2][4];
+            const int mt = meta[stage * TILE_BLKS + warp], owner = mt >> 8, tokens = mt & 255;
             float mx0 = -CUDART_INF_F, mx1 = -CUDART_INF_F;
+            s[0][0] = s[0][1] = s[0][2] = s[0][3] = s[1][0] = s[1][1] = s[1][2] = s[1][3] = 0.f;
+            if (tokens) {
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                const int blk = MW == 1 ? warp : b;
-                const int mt = meta[stage * TILE_BLKS + blk];
-                owner[b] = mt >> 8;
-                tokens[b] = mt & 255;
-                if (owner[b] && (owner[b] < first_owner || owner[b] > last_owner)) tokens[b] = 0;
-                float* sa = s[2 * b];
-                float* sb = s[2 * b + 1];
-                sa[0] = sa[1] = sa[2] = sa[3] = sb[0] = sb[1] = sb[2] = sb[3] = 0.f;
-                if (tokens[b]) {
-#pragma unroll
-                    for (int kk = 0; kk < DP / 16; ++kk) {
-                        uint32_t kf[4];
-                        // matrices: tokens 0-7 and 8-15 of the block, each k 0-7 and 8-15
-                        ldsm4(kt + chunk_at<DP>(blk * BLK + (lane & 7) + ((lane >> 4) << 3), 2 * kk + ((lane >> 3) & 1)), kf);
-                        Num<T>::mma(sa, qf[kk], kf[0], kf[1]);
-                        Num<T>::mma(sb, qf[kk], kf[2], kf[3]);
-                    }
+                for (int kk = 0; kk < DP / 16; ++kk) {
+                    uint32_t kf[4];
+                    // matrices: tokens 0-7 and 8-15 of the block, each k 0-7 and 8-15
+                    ldsm4(kt + chunk_at<DP>(warp * BLK + (lane & 7) + ((lane >> 4) << 3), 2 * kk + ((lane >> 3) & 1)), kf);
+                    Num<T>::mma(s[0], qf[kk], kf[0], kf[1]);
+                    Num<T>::mma(s[1], qf[kk], kf[2], kf[3]);
                 }
-                const bool in0 = !owner[b] || owner[b] == own_lo, in1 = !owner[b] || owner[b] == own_hi;
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const bool some = h * 8 + (lane & 3) * 2 + e < tokens[b];
-                        float& x0 = s[2 * b + h][e];
-                        float& x1 = s[2 * b + h][2 + e];
-                        x0 = some && in0 ? x0 * p.c2 : -CUDART_INF_F;
-                        x1 = some && in1 ? x1 * p.c2 : -CUDART_INF_F;
-                        mx0 = fmaxf(mx0, x0);
-                        mx1 = fmaxf(mx1, x1);
-                    }
             }
+            const bool in0 = !owner || owner == own_lo, in1 = !owner || owner == own_hi;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const bool some = h * 8 + (lane & 3) * 2 + e < tokens;
+                    s[h][e] = some && in0 ? s[h][e] * p.c2 : -CUDART_INF_F;
+                    s[h][2 + e] = some && in1 ? s[h][2 + e] * p.c2 : -CUDART_INF_F;
+                    mx0 = fmaxf(mx0, s[h][e]);
+                    mx1 = fmaxf(mx1, s[h][2 + e]);
+                }
             mx0 = fmaxf(mx0, __shfl_xor_sync(FULL, mx0, 1));
             mx1 = fmaxf(mx1, __shfl_xor_sync(FULL, mx1, 1));
             mx0 = fmaxf(mx0, __shfl_xor_sync(FULL, mx0, 2));
@@ -419,41 +324,36 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
                 for (int j = 0; j < DP / 8; ++j) { o[j][0] *= f0; o[j][1] *= f0; o[j][2] *= f1; o[j][3] *= f1; }
             }
             const float ref0 = m0 > -CUDART_INF_F ? m0 : 0.f, ref1 = m1 > -CUDART_INF_F ? m1 : 0.f;
+            if (!tokens) continue;
+            uint32_t pf[4];
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                if (!tokens[b]) continue;
-                uint32_t pf[4];
+            for (int h = 0; h < 2; ++h) {
+                float* x = s[h];
+                x[0] = ex2_approx(x[0] - ref0);
+                x[1] = ex2_approx(x[1] - ref0);
+                x[2] = ex2_approx(x[2] - ref1);
+                x[3] = ex2_approx(x[3] - ref1);
+                l0 += x[0] + x[1];
+                l1 += x[2] + x[3];
+                pf[2 * h] = Num<T>::pack(x[0], x[1]);
+                pf[2 * h + 1] = Num<T>::pack(x[2], x[3]);
+            }
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float* x = s[2 * b + h];
-                    x[0] = ex2_approx(x[0] - ref0);
-                    x[1] = ex2_approx(x[1] - ref0);
-                    x[2] = ex2_approx(x[2] - ref1);
-                    x[3] = ex2_approx(x[3] - ref1);
-                    l0 += x[0] + x[1];
-                    l1 += x[2] + x[3];
-                    pf[2 * h] = Num<T>::pack(x[0], x[1]);
-                    pf[2 * h + 1] = Num<T>::pack(x[2], x[3]);
-                }
-                const int blk = MW == 1 ? warp : b;
-                const bool in0 = !owner[b] || owner[b] == own_lo, in1 = !owner[b] || owner[b] == own_hi;
-#pragma unroll
-                for (int j = 0; j < DP / 16; ++j) {
-                    uint32_t vf[4];
-                    // matrices: tokens 0-7, 8-15 of the block at values 16j..16j+7, then at 16j+8..16j+15
-                    ldsm4t(vt + chunk_at<DP>(blk * BLK + (lane & 15), 2 * j + (lane >> 4)), vf);
-                    if (!owner[b]) {
-                        Num<T>::mma(o[2 * j], pf, vf[0], vf[1]);
-                        Num<T>::mma(o[2 * j + 1], pf, vf[2], vf[3]);
-                    } else {
-                        // a row's own tokens: what they add to other rows is 0 * v, which is not 0 for a
-                        // non-finite v, so it is left out
-                        float t0[4] = {0.f, 0.f, 0.f, 0.f}, t1[4] = {0.f, 0.f, 0.f, 0.f};
-                        Num<T>::mma(t0, pf, vf[0], vf[1]);
-                        Num<T>::mma(t1, pf, vf[2], vf[3]);
-                        if (in0) { o[2 * j][0] += t0[0]; o[2 * j][1] += t0[1]; o[2 * j + 1][0] += t1[0]; o[2 * j + 1][1] += t1[1]; }
-                        if (in1) { o[2 * j][2] += t0[2]; o[2 * j][3] += t0[3]; o[2 * j + 1][2] += t1[2]; o[2 * j + 1][3] += t1[3]; }
-                    }
+            for (int j = 0; j < DP / 16; ++j) {
+                uint32_t vf[4];
+                // matrices: tokens 0-7, 8-15 of the block at values 16j..16j+7, then at 16j+8..16j+15
+                ldsm4t(vt + chunk_at<DP>(warp * BLK + (lane & 15), 2 * j + (lane >> 4)), vf);
+                if (!owner) {
+                    Num<T>::mma(o[2 * j], pf, vf[0], vf[1]);
+                    Num<T>::mma(o[2 * j + 1], pf, vf[2], vf[3]);
+                } else {
+                    // a row's own tokens: what they add to other rows is 0 * v, which is not 0 for a
+                    // non-finite v, so it is left out
+                    float t0[4] = {0.f, 0.f, 0.f, 0.f}, t1[4] = {0.f, 0.f, 0.f, 0.f};
+                    Num<T>::mma(t0, pf, vf[0], vf[1]);
+                    Num<T>::mma(t1, pf, vf[2], vf[3]);
+                    if (in0) { o[2 * j][0] += t0[0]; o[2 * j][1] += t0[1]; o[2 * j + 1][0] += t1[0]; o[2 * j + 1][1] += t1[1]; }
+                    if (in1) { o[2 * j][2] += t0[2]; o[2 * j][3] += t0[3]; o[2 * j + 1][2] += t1[2]; o[2 * j + 1][3] += t1[3]; }
                 }
             }
         }
@@ -485,21 +385,14 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
             const int m = i / DV, d = (i % DV) * 4;
             if (d >= p.D) continue;
             float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-            float mm, ll;
-            if (MW == 1) {
-                mm = fmaxf(fmaxf(w_m[0][m], w_m[1][m]), fmaxf(w_m[2][m], w_m[3][m]));
-                ll = 0.f;
+            const float mm = fmaxf(fmaxf(w_m[0][m], w_m[1][m]), fmaxf(w_m[2][m], w_m[3][m]));
+            float ll = 0.f;
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const float f = w_m[w][m] > -CUDART_INF_F ? ex2_approx(w_m[w][m] - mm) : 0.f;
-                    const float4 y = *reinterpret_cast<const float4*>(os + (w * 16 + m) * DP + d);
-                    x.x += f * y.x; x.y += f * y.y; x.z += f * y.z; x.w += f * y.w;
-                    ll += f * w_l[w][m];
-                }
-            } else {
-                mm = w_m[m >> 4][m & 15];
-                ll = w_l[m >> 4][m & 15];
-                x = *reinterpret_cast<const float4*>(os + m * DP + d);
+            for (int w = 0; w < 4; ++w) {
+                const float f = w_m[w][m] > -CUDART_INF_F ? ex2_approx(w_m[w][m] - mm) : 0.f;
+                const float4 y = *reinterpret_cast<const float4*>(os + (w * 16 + m) * DP + d);
+                x.x += f * y.x; x.y += f * y.y; x.z += f * y.z; x.w += f * y.w;
+                ll += f * w_l[w][m];
             }
             const float inv = ll > 0.f ? 1.f / ll : (ll == 0.f ? 0.f : ll);
             x.x *= inv; x.y *= inv; x.z *= inv; x.w *= inv;
@@ -562,19 +455,18 @@ int shift_of(int32_t page_size) {
     return s;
 }
 
-template <typename T, int DP, int MW>
+template <typename T, int DP>
 int launch_attend(const AttendParams& p, unsigned grid, cudaStream_t st) {
-    constexpr int bytes = AttendSmem<DP, MW>::BYTES;
+    constexpr int bytes = AttendSmem<DP>::BYTES;
     static std::atomic<uint64_t> done{0};
-    if (const int rc = allow_smem(attend_cached_kernel<T, DP, MW>, bytes, done)) return rc;
-    attend_cached_kernel<T, DP, MW><<<grid, AT, bytes, st>>>(p);
+    if (const int rc = allow_smem(attend_cached_kernel<T, DP>, bytes, done)) return rc;
+    attend_cached_kernel<T, DP><<<grid, AT, bytes, st>>>(p);
     DISC_CUDA(cudaGetLastError());
     return DISC_OK;
 }
 template <typename T>
 int launch_attend(const AttendParams& p, unsigned grid, cudaStream_t st) {
-    if (p.shape.M <= 16) return p.D <= 64 ? launch_attend<T, 64, 1>(p, grid, st) : launch_attend<T, 128, 1>(p, grid, st);
-    return p.D <= 64 ? launch_attend<T, 64, 4>(p, grid, st) : launch_attend<T, 128, 4>(p, grid, st);
+    return p.D <= 64 ? launch_attend<T, 64>(p, grid, st) : launch_attend<T, 128>(p, grid, st);
 }
 
 }  // namespace
@@ -595,10 +487,11 @@ int disc_attend_plan(const disc_cache_t* c, int32_t n_q_heads, int32_t group, vo
     PlanParams p;
     if (const int rc = plan_shape(c, n_q_heads, group, &p.shape)) return rc;
     if ((reinterpret_cast<uintptr_t>(plan) & 15u) || plan_bytes < plan_layout(c, p.shape, plan, &p.plan)) return DISC_ERR_ARG;
-    p.table = c->table; p.len = c->len; p.rows = c->n_rows; p.group = group < c->n_rows ? group : c->n_rows; p.width = c->table_width;
+    p.table = c->table; p.len = c->len; p.rows = c->n_rows; p.width = c->table_width;
     p.page_size = c->page_size; p.shift = shift_of(c->page_size); p.kv_heads = c->n_kv_heads;
-    p.aim = (PLAN_UNITS + c->n_kv_heads - 1) / c->n_kv_heads;
-    attend_plan_kernel<<<CLUSTER, PT, 0, static_cast<cudaStream_t>(stream)>>>(p);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (p.shape.M > ROWS_M) return disc::plan_groups(p, st);
+    attend_plan_kernel<<<CLUSTER, PT, 0, st>>>(p);
     DISC_CUDA(cudaGetLastError());
     return DISC_OK;
 }
@@ -606,22 +499,28 @@ int disc_attend_plan(const disc_cache_t* c, int32_t n_q_heads, int32_t group, vo
 int disc_attend_cached(const disc_cache_t* c, int32_t layer, const void* q, int64_t q_row_stride, int64_t q_head_stride,
                        int32_t n_q_heads, int32_t group, float scale, void* plan, int64_t plan_bytes, void* out, float* lse_out,
                        void* stream) {
-    if (!c || !c->pool || !q || !plan || !out) return DISC_ERR_ARG;
+    if (!c || !c->pool || !c->table || !c->len || !q || !plan || !out) return DISC_ERR_ARG;
     if (const int rc = disc::cache_sizes(c)) return rc;
-    if (layer < 0 || layer >= c->n_layers || !(scale > -3.0e38f && scale < 3.0e38f)) return DISC_ERR_ARG;
+    if (layer < 0 || layer >= c->n_layers || !(scale > 0.f) || !(scale <= 3.0e38f)) return DISC_ERR_ARG;
     AttendParams p;
     if (const int rc = plan_shape(c, n_q_heads, group, &p.shape)) return rc;
     if ((reinterpret_cast<uintptr_t>(plan) & 15u) || plan_bytes < plan_layout(c, p.shape, plan, &p.plan)) return DISC_ERR_ARG;
     if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15u) return DISC_ERR_ARG;
+    // the stride over an axis of one is never used; any valid one will do
+    if (n_q_heads == 1) q_head_stride = (int64_t(c->head_dim) + 7) / 8 * 8;
+    if (c->n_rows == 1) q_row_stride = (int64_t(c->head_dim) + 7) / 8 * 8 * n_q_heads;
     if ((q_row_stride | q_head_stride) & 7) return DISC_ERR_UNSUPPORTED;
     const int64_t plane = int64_t(c->n_pages) * c->n_kv_heads * c->page_size * c->head_dim * 2;
     p.k = static_cast<const unsigned char*>(c->pool) + 2 * layer * plane;
     p.v = p.k + plane;
     p.q = static_cast<const unsigned char*>(q); p.q_row = q_row_stride * 2; p.q_head = q_head_stride * 2;
+    p.table = c->table; p.len = c->len; p.width = c->table_width; p.pages = c->n_pages;
     p.out = static_cast<unsigned char*>(out); p.lse = lse_out;
-    p.rows = c->n_rows; p.group = group < c->n_rows ? group : c->n_rows; p.kv_heads = c->n_kv_heads; p.D = c->head_dim; p.page_size = c->page_size;
+    p.rows = c->n_rows; p.kv_heads = c->n_kv_heads; p.D = c->head_dim; p.page_size = c->page_size;
     p.c2 = scale * LOG2E_F;
+    p.error = reinterpret_cast<uint32_t*>(p.plan.head);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (p.shape.M > ROWS_M) return disc::attend_groups(p, c->dtype, n_q_heads, st);
     int sms = 0;
     if (const int rc = device_sms(&sms)) return rc;
     const int64_t most = int64_t(p.shape.max_items) * c->n_kv_heads;

@@ -1,0 +1,135 @@
+// What the two forms of the attention over the cache share: the plan's sizes and places (disc_attend.cu, disc_attend_group.cu).
+#pragma once
+
+#include "disc_internal.cuh"
+
+namespace disc {
+
+constexpr int BLK = 16;                // tokens of a block: the smallest page, and the depth of one MMA
+constexpr int ROWS_M = 16;             // up to this many query vectors read the same pages: disc_attend.cu, above it disc_attend_group.cu
+constexpr int GROUP_M = 128;           // query vectors that a group can have at most
+constexpr int G_MAX = 64;              // query heads per key head
+constexpr int PLAN_UNITS = 148 * 4;    // items x key heads aimed at: two rounds of the blocks the device has places for
+
+struct PlanShape {
+    int32_t G;                         // query heads per key head
+    int32_t per_group;                 // rows of a group as it is worked on
+    int32_t sub;                       // such groups per `group` rows
+    int32_t groups;                    // in all
+    int32_t M;                         // query vectors of a group
+    int32_t group;                     // rows that may share pages, as given
+    int32_t blks_per_page;
+    int32_t aim;                       // items aimed at, for each key head
+    int32_t max_items;
+    int64_t list_ld;                   // rows form: blocks a group's list has room for
+    int64_t max_part;                  // partial results: query vectors there is room for
+};
+
+struct GroupItem {                     // rows [row, row + rows) over their blocks [begin, end)
+    int32_t row, rows, begin, end, part, pad[3];
+};
+
+struct Plan {
+    int32_t* head;                     // [0] items
+    float* part;                       // [max_part][head_dim] normalised sums, fp32
+    float* part_lse;                   // [max_part] log-sum-exp in units of log2
+    // rows form
+    int32_t* count;                    // [groups] blocks
+    int32_t* splits;                   // [groups]
+    int32_t* slot;                     // [groups] first partial result, or -1
+    int32_t* arrived;                  // [groups][kv heads]
+    int4* items;                       // group, first block, one past the last, index among the group's items
+    int2* list;                        // [groups][list_ld]: page; block | tokens << 8 | (owner + 1) << 16
+    // group form
+    GroupItem* group_items;
+    int32_t* shared;                   // [groups] leading blocks that its rows share and that are worked on together
+    int32_t* alone;                    // [rows] blocks after those that are worked on as an item of the row's own
+    int2* group_part;                  // [groups] first partial result, number of parts
+    int2* row_part;                    // [rows]
+};
+
+inline int plan_shape(const disc_cache_t* c, int32_t hq, int32_t group, PlanShape* s) {
+    if (hq <= 0 || group <= 0 || c->n_kv_heads <= 0 || hq % c->n_kv_heads) return DISC_ERR_ARG;
+    s->G = hq / c->n_kv_heads;
+    if (s->G > G_MAX) return DISC_ERR_UNSUPPORTED;
+    s->group = group = group < c->n_rows ? group : c->n_rows;
+    const int64_t vectors = int64_t(group) * s->G;
+    s->per_group = vectors <= GROUP_M ? group : GROUP_M / s->G;
+    s->sub = (group + s->per_group - 1) / s->per_group;
+    const int64_t groups = (int64_t(c->n_rows) + group - 1) / group * s->sub;
+    if (groups > (1 << 26)) return DISC_ERR_UNSUPPORTED;
+    s->groups = int32_t(groups);
+    s->M = s->per_group * s->G;
+    s->blks_per_page = c->page_size / BLK;
+    s->aim = (PLAN_UNITS + c->n_kv_heads - 1) / c->n_kv_heads;
+    // a group or row that is cut at all is cut into at most twice its share of the items aimed at
+    if (s->M <= ROWS_M) {
+        s->list_ld = int64_t(s->per_group) * c->table_width * s->blks_per_page;
+        s->max_items = s->groups + 2 * s->aim + 2;
+        s->max_part = int64_t(2 * s->aim + 2) * c->n_kv_heads * s->M;
+    } else {
+        // the K and V planes as tensor maps: rows of a plane are counted in 32 bits
+        if (int64_t(c->n_pages) * c->n_kv_heads * c->page_size >= (int64_t(1) << 31)) return DISC_ERR_UNSUPPORTED;
+        s->list_ld = 0;
+        s->max_items = s->groups + c->n_rows + 2 * s->aim + 2;
+        s->max_part = (int64_t(s->groups) * s->M + int64_t(c->n_rows) * s->G + int64_t(2 * s->aim + 2) * s->M) * c->n_kv_heads;
+        if (s->max_part >= (int64_t(1) << 31)) return DISC_ERR_UNSUPPORTED;
+    }
+    return DISC_OK;
+}
+
+inline int64_t plan_layout(const disc_cache_t* c, const PlanShape& s, void* base_, Plan* p) {
+    unsigned char* base = static_cast<unsigned char*>(base_);
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) { unsigned char* q = base + at; at += (bytes + 31) & ~int64_t(31); return q; };
+    Plan t = {};
+    t.head = reinterpret_cast<int32_t*>(take(256));
+    t.part = reinterpret_cast<float*>(take(s.max_part * c->head_dim * 4));
+    t.part_lse = reinterpret_cast<float*>(take(s.max_part * 4));
+    if (s.M <= ROWS_M) {
+        t.count = reinterpret_cast<int32_t*>(take(int64_t(s.groups) * 4));
+        t.splits = reinterpret_cast<int32_t*>(take(int64_t(s.groups) * 4));
+        t.slot = reinterpret_cast<int32_t*>(take(int64_t(s.groups) * 4));
+        t.arrived = reinterpret_cast<int32_t*>(take(int64_t(s.groups) * c->n_kv_heads * 4));
+        t.items = reinterpret_cast<int4*>(take(int64_t(s.max_items) * 16));
+        t.list = reinterpret_cast<int2*>(take(int64_t(s.groups) * s.list_ld * 8));
+    } else {
+        t.group_items = reinterpret_cast<GroupItem*>(take(int64_t(s.max_items) * sizeof(GroupItem)));
+        t.shared = reinterpret_cast<int32_t*>(take(int64_t(s.groups) * 4));
+        t.alone = reinterpret_cast<int32_t*>(take(int64_t(c->n_rows) * 4));
+        t.group_part = reinterpret_cast<int2*>(take(int64_t(s.groups) * 8));
+        t.row_part = reinterpret_cast<int2*>(take(int64_t(c->n_rows) * 8));
+    }
+    if (p) *p = t;
+    return at;
+}
+
+struct PlanParams {
+    Plan plan;
+    PlanShape shape;
+    const int32_t* table;
+    const int32_t* len;
+    int32_t rows, width, page_size, shift, kv_heads;
+};
+
+struct AttendParams {
+    Plan plan;
+    PlanShape shape;
+    const unsigned char* k;            // this layer's planes
+    const unsigned char* v;
+    const unsigned char* q;
+    int64_t q_row, q_head;             // bytes
+    const int32_t* table;
+    const int32_t* len;
+    unsigned char* out;
+    float* lse;
+    int32_t rows, width, pages, kv_heads, D, page_size;
+    float c2;                          // scale log2(e)
+    uint32_t* error;
+};
+
+// disc_attend_group.cu: more than ROWS_M query vectors read the same pages
+int plan_groups(const PlanParams& p, cudaStream_t st);
+int attend_groups(const AttendParams& p, int32_t dtype, int32_t n_q_heads, cudaStream_t st);
+
+}  // namespace disc

@@ -1,0 +1,645 @@
+// disc_attend_cached where more than 16 query vectors read the same pages: K candidates of a query over its
+// prompt, or many query heads on one key head.
+//
+// Per token and key head there are 4 D bytes to read and 4 M D flops to do, for M = 128 as many flops per
+// byte as the tensor cores can do while the bytes come from HBM at half their rate.  That is tcgen05's work
+// (mma.sync reached a sixth of the bytes' rate here), in two kernels after a plan:
+//
+//   1. A group's rows x query heads, up to 128, are one tile of query vectors.  The blocks of 16 tokens that all
+//      the rows hold in full go through the tensor cores as in the attention over prompts: S = Q K^T, a thread
+//      per query vector for the softmax, O += P V.  A row that has more than 8 full blocks of its own after those
+//      gets items of its own.  Long runs are cut.  Every item leaves normalised sums and log-sum-exps in fp32.
+//   2. A warp per row and key head joins them, in order, with what is left of the row: up to 8 full blocks of its own
+//      and the partly filled one, by mma.sync.  Here, where rows have nothing in common, no row's values come near
+//      another row's sums.
+//
+// Kernel 1: blocks of 6 warps, two to an SM, so that one's softmax runs beside the other's products; 4 warps one
+// thread per query vector, one warp the loads (a TMA box of 16 tokens x 64 values per block, page by page),
+// one the MMAs.  Tensor memory: S 128 columns | O.  A last tile of fewer than 8 blocks takes fewer steps of the
+// second product, and its missing scores are masked, so that nothing stale is ever multiplied.
+
+#include "disc_attend.cuh"
+#include "disc_sm100.cuh"
+
+namespace {
+
+using namespace disc;
+
+constexpr unsigned FULL = 0xffffffffu;
+constexpr float LN2_F = 0.6931471805599453f;
+constexpr int TN = 128;                // tokens of a tile
+constexpr int TILE_BLKS = TN / BLK;
+constexpr int BOX = 64;
+constexpr int MIN_SHARED = 4;          // blocks: less is not worth an item
+constexpr int MAX_TAIL = 8;            // full blocks that kernel 2 takes along
+
+// ---- the plan ---------------------------------------------------------------------------------------
+// A block per group: the leading pages that its rows share, and what rows have left.
+__global__ void __launch_bounds__(256) group_shared_kernel(const PlanParams p) {
+    __shared__ int32_t s_shared;
+    const PlanShape& sh = p.shape;
+    const int g = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int32_t r0 = g / sh.sub * sh.group + g % sh.sub * sh.per_group;
+    const int32_t r1 = min(p.rows, min(r0 + sh.per_group, g / sh.sub * sh.group + sh.group));
+    if (threadIdx.x == 0) s_shared = 0x7fffffff;
+    __syncthreads();
+    const int32_t* first = p.table + int64_t(r0) * p.width;
+    for (int32_t r = r0 + warp; r < r1; r += 8) {
+        const int32_t full = min(p.len[r0], p.len[r]) >> p.shift;
+        int32_t same = full;
+        if (r > r0) {
+            const int32_t* row = p.table + int64_t(r) * p.width;
+            for (int32_t j0 = 0; j0 < full; j0 += 64) {
+                const int32_t j = j0 + lane, j2 = j + 32;
+                const bool a = j >= full || first[j] == row[j], b = j2 >= full || first[j2] == row[j2];
+                const unsigned da = __ballot_sync(FULL, !a), db = __ballot_sync(FULL, !b);
+                if (da | db) {
+                    same = da ? j0 + __ffs(da) - 1 : j0 + 31 + __ffs(db);
+                    break;
+                }
+            }
+        }
+        if (lane == 0) atomicMin(&s_shared, same);
+    }
+    __syncthreads();
+    int32_t blks = r0 < r1 ? s_shared * sh.blks_per_page : 0;
+    if (blks < MIN_SHARED) blks = 0;
+    if (threadIdx.x == 0) p.plan.shared[g] = blks;
+    for (int32_t r = r0 + threadIdx.x; r < r1; r += 256) {
+        const int32_t left = p.len[r] / BLK - blks;
+        p.plan.alone[r] = left > MAX_TAIL ? left : 0;
+    }
+}
+
+// One block: the items' length, and the items, groups first, then rows.
+constexpr int PT = 1024;
+__global__ void __launch_bounds__(PT) group_items_kernel(const PlanParams p) {
+    __shared__ int32_t sums[32][2];
+    __shared__ unsigned long long s_all;
+    const PlanShape& sh = p.shape;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (tid == 0) s_all = 0ull;
+    __syncthreads();
+    unsigned long long mine = 0, alone = 0;
+    for (int32_t g = tid; g < sh.groups; g += PT) mine += p.plan.shared[g];
+    for (int32_t r = tid; r < p.rows; r += PT) alone += p.plan.alone[r];
+    mine += alone;
+    const int any_alone = __syncthreads_or(alone > 0);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(FULL, mine, o);
+    if (lane == 0 && mine) atomicAdd(&s_all, mine);
+    __syncthreads();
+    const int64_t all = int64_t(s_all);
+    int32_t len = int32_t((all + sh.aim - 1) / sh.aim);
+    len = max(TILE_BLKS, (len + TILE_BLKS - 1) / TILE_BLKS * TILE_BLKS);
+    int32_t items = 0, part = 0;
+    for (int kind = 0; kind < 2; ++kind) {
+        const int32_t n = kind == 0 ? sh.groups : p.rows;
+        for (int32_t i0 = 0; i0 < n; i0 += PT) {
+            const int32_t i = i0 + tid;
+            int32_t blks = 0, row = 0, rows = 1, begin = 0;
+            if (i < n && (kind == 0 || any_alone)) {
+                if (kind == 0) {
+                    blks = p.plan.shared[i];
+                    row = i / sh.sub * sh.group + i % sh.sub * sh.per_group;
+                    rows = max(0, min(p.rows, min(row + sh.per_group, i / sh.sub * sh.group + sh.group)) - row);
+                } else {
+                    blks = p.plan.alone[i];
+                    row = i;
+                    if (blks) begin = p.plan.shared[i / sh.group * sh.sub + i % sh.group / sh.per_group];
+                }
+            }
+            const int32_t splits = (blks + len - 1) / len, parts = splits * rows * sh.G * p.kv_heads;
+            int32_t a = splits, b = parts;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int32_t ua = __shfl_up_sync(FULL, a, o), ub = __shfl_up_sync(FULL, b, o);
+                if (lane >= o) { a += ua; b += ub; }
+            }
+            __syncthreads();
+            if (lane == 31) { sums[warp][0] = a; sums[warp][1] = b; }
+            __syncthreads();
+            int32_t wa = sums[lane][0], wb = sums[lane][1];
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int32_t ua = __shfl_up_sync(FULL, wa, o), ub = __shfl_up_sync(FULL, wb, o);
+                if (lane >= o) { wa += ua; wb += ub; }
+            }
+            const int32_t before_a = __shfl_sync(FULL, wa, max(warp - 1, 0)), before_b = __shfl_sync(FULL, wb, max(warp - 1, 0));
+            const int32_t item0 = items + a - splits + (warp ? before_a : 0), part0 = part + b - parts + (warp ? before_b : 0);
+            items += __shfl_sync(FULL, wa, 31);
+            part += __shfl_sync(FULL, wb, 31);
+            if (i < n) (kind == 0 ? p.plan.group_part : p.plan.row_part)[i] = make_int2(part0, splits);
+            for (int32_t x = 0; x < splits; ++x)
+                p.plan.group_items[item0 + x] =
+                    GroupItem{row, rows, begin + x * len, begin + min(blks, (x + 1) * len), part0 + x * rows * sh.G * p.kv_heads, {0, 0, 0}};
+        }
+    }
+    if (tid == 0) { p.plan.head[0] = 0; p.plan.head[1] = items; }
+}
+
+// ---- kernel 1 -----------------------------------------------------------------------------------------
+constexpr int THREADS = 192;
+template <int DP>
+struct Shape {
+    static constexpr int BOXES = DP / BOX;
+    static constexpr int BOX_BYTES = TN * BOX * 2;
+    static constexpr int TILE_BYTES = BOXES * BOX_BYTES;
+    static constexpr int STAGES = DP == 128 ? 2 : 4;
+    static constexpr int TMEM = 256;                               // columns: S 128, O up to 128
+    static constexpr int SMEM = TILE_BYTES + STAGES * TILE_BYTES + 1024 + 128;
+};
+
+struct GroupParams {
+    Plan plan;
+    const int32_t* table;
+    int32_t width, kv_heads, G, per_group, D, page_size, blks_per_page;
+    float c2;
+    uint32_t* error;
+    uint32_t idesc_qk, idesc_pv;
+};
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(THREADS, 2)
+attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                    const __grid_constant__ CUtensorMap map_v, const GroupParams p) {
+    using S = Shape<DP>;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* q_tile = reinterpret_cast<unsigned char*>((uintptr_t(smem_raw) + 1023) & ~uintptr_t(1023));
+    unsigned char* ring = q_tile + S::TILE_BYTES;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(ring + S::STAGES * S::TILE_BYTES);
+    uint64_t* q_full = bars;
+    uint64_t* q_empty = bars + 1;
+    uint64_t* s_full = bars + 2;
+    uint64_t* o_full = bars + 3;
+    uint64_t* p_full = bars + 4;
+    uint64_t* kv_full = bars + 5;
+    uint64_t* kv_empty = bars + 5 + S::STAGES;
+    static_assert((5 + 2 * S::STAGES) * 8 <= 128, "room for the barriers");
+    __shared__ uint32_t tmem_slot;
+    __shared__ int s_abort;
+    volatile int* abort = &s_abort;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        s_abort = 0;
+        mbar_init(q_full, 1); mbar_init(q_empty, 1); mbar_init(s_full, 1); mbar_init(o_full, 1); mbar_init(p_full, 4);
+        for (int s = 0; s < S::STAGES; ++s) { mbar_init(kv_full + s, 1); mbar_init(kv_empty + s, 1); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 5) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(S::TMEM) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&tmem_slot);
+
+    const int n_units = p.plan.head[1] * p.kv_heads;               // neighbouring units: the key heads of an item
+    const int step = int(gridDim.x);
+
+    if (warp >= 4) {
+        if (warp == 4) {
+            // ---- loads
+            int load = 0, n = 0;
+            bool ok = true;
+            for (int unit = blockIdx.x; unit < n_units && ok; unit += step, ++n) {
+                const GroupItem* it = p.plan.group_items + unit / p.kv_heads;
+                const int head = unit % p.kv_heads, row = it->row, begin = it->begin, blks = it->end - begin;
+                const int32_t* table = p.table + int64_t(row) * p.width;
+                if (n > 0) ok = mbar_wait_all(q_empty, (n - 1) & 1, abort);
+                if (ok && lane == 0) {
+                    mbar_expect_tx(q_full, uint32_t(S::BOXES) * p.G * p.per_group * BOX * 2);
+                    for (int b = 0; b < S::BOXES; ++b) tma_load_3d(q_tile + b * S::BOX_BYTES, &map_q, b * BOX, head * p.G, row, q_full);
+                }
+                for (int t = 0; t < blks && ok; t += TILE_BLKS) {
+                    const int here = min(TILE_BLKS, blks - t);
+                    // lane l brings in block l % 8: its keys, then its values
+                    const int b = lane % TILE_BLKS, blk = begin + t + b;
+                    int y = 0;
+                    if (b < here) y = (table[blk / p.blks_per_page] * p.kv_heads + head) * p.page_size + blk % p.blks_per_page * BLK;
+#pragma unroll
+                    for (int kv = 0; kv < 2; ++kv, ++load) {
+                        const int s = load % S::STAGES, round = load / S::STAGES;
+                        if (round > 0 && ok) ok = mbar_wait_all(kv_empty + s, (round - 1) & 1, abort);
+                        if (!ok) continue;
+                        if (lane == 0) mbar_expect_tx(kv_full + s, uint32_t(here) * S::BOXES * BLK * BOX * 2);
+                        __syncwarp();
+                        if (lane < TILE_BLKS && b < here)
+                            for (int x = 0; x < S::BOXES; ++x)
+                                tma_load_2d(ring + s * S::TILE_BYTES + x * S::BOX_BYTES + b * (BLK * BOX * 2), kv ? &map_v : &map_k, x * BOX, y, kv_full + s);
+                        __syncwarp();
+                    }
+                }
+            }
+        } else if (warp == 5) {
+            // ---- MMAs
+            const uint64_t q_desc = smem_desc_sw128(q_tile), kv_desc = smem_desc_sw128(ring), v_desc = smem_desc_n_major(ring, S::BOX_BYTES);
+            constexpr uint64_t TILE16 = S::TILE_BYTES >> 4;
+            auto scores = [&](int stage) {
+                const uint64_t kd = kv_desc + uint64_t(stage) * TILE16;
+#pragma unroll
+                for (int kk = 0; kk < DP / 16; ++kk) {
+                    const uint64_t off = uint64_t((kk / 4) * (S::BOX_BYTES >> 4) + (kk % 4) * 2);
+                    umma_ss(tmem, q_desc + off, kd + off, p.idesc_qk, kk > 0);
+                }
+            };
+            int load = 0, n = 0, tile = 0;
+            bool ok = true;
+            for (int unit = blockIdx.x; unit < n_units && ok; unit += step, ++n) {
+                const GroupItem* it = p.plan.group_items + unit / p.kv_heads;
+                const int blks = it->end - it->begin;
+                ok = mbar_wait_all(q_full, n & 1, abort) && mbar_wait_all(kv_full + load % S::STAGES, (load / S::STAGES) & 1, abort);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    scores(load % S::STAGES);
+                    umma_commit(s_full);
+                    umma_commit(kv_empty + load % S::STAGES);
+                    if (blks <= TILE_BLKS) umma_commit(q_empty);
+                }
+                __syncwarp();
+                ++load;
+                for (int t = 0; t < blks && ok; t += TILE_BLKS, ++tile) {
+                    const int here = min(TILE_BLKS, blks - t);
+                    const bool more = t + TILE_BLKS < blks;
+                    const int v_stage = load % S::STAGES, k_stage = (load + 1) % S::STAGES;
+                    ok = mbar_wait_all(kv_full + v_stage, (load / S::STAGES) & 1, abort);
+                    if (ok) ok = mbar_wait_all(p_full, tile & 1, abort);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint64_t vd = v_desc + uint64_t(v_stage) * TILE16;
+                        for (int kk = 0; kk < here; ++kk)
+                            umma_ts(tmem + TN, tmem + kk * 8, vd + uint64_t(kk * (BLK * 128 >> 4)), p.idesc_pv, t > 0 || kk > 0);
+                        umma_commit(kv_empty + v_stage);
+                        if (!more) umma_commit(o_full);
+                    }
+                    __syncwarp();
+                    ++load;
+                    if (more) {
+                        ok = mbar_wait_all(kv_full + k_stage, (load / S::STAGES) & 1, abort);
+                        if (!ok) break;
+                        tc_fence_after();
+                        if (elect_one()) {
+                            scores(k_stage);
+                            umma_commit(s_full);
+                            umma_commit(kv_empty + k_stage);
+                            if (t + 2 * TILE_BLKS >= blks) umma_commit(q_empty);
+                        }
+                        __syncwarp();
+                        ++load;
+                    }
+                }
+            }
+            // the last reports of free places have arrived before the block leaves
+            for (int back = 0; back < S::STAGES && back < load && ok; ++back)
+                ok = mbar_wait_all(kv_empty + (load - 1 - back) % S::STAGES, ((load - 1 - back) / S::STAGES) & 1, abort);
+            if (ok && n > 0) mbar_wait_all(q_empty, (n - 1) & 1, abort);
+        }
+    } else {
+        // ---- softmax: this thread's query vector
+        const int m = warp * 32 + lane;
+        const uint32_t lane_bits = uint32_t(warp * 32) << 16;
+        const uint32_t s_tm = tmem + lane_bits, o_tm = tmem + lane_bits + TN;
+        const float2 c2 = make_float2(p.c2, p.c2);
+        int tile = 0, n = 0;
+        bool ok = true;
+        for (int unit = blockIdx.x; unit < n_units && ok; unit += step, ++n) {
+            const GroupItem* it = p.plan.group_items + unit / p.kv_heads;
+            const int blks = it->end - it->begin;
+            float ref = -CUDART_INF_F;
+            float2 l = make_float2(0.f, 0.f);
+            bool bad = false;
+            for (int t = 0; t < blks; t += TILE_BLKS, ++tile) {
+                ok = mbar_wait_all(s_full, tile & 1, abort);
+                if (!ok) break;
+                tc_fence_after();
+                float s[TN];
+                tmem_ld128(s_tm, s);
+                const int here = min(TILE_BLKS, blks - t) * BLK;
+                if (here < TN) {
+#pragma unroll
+                    for (int c = 0; c < TN; ++c) s[c] = c < here ? s[c] : -CUDART_INF_F;
+                }
+                uint32_t pk[16];
+                float2 la;
+                first_quarter<T, DP>(s, c2, ref, l, bad, o_tm, t > 0, la, pk);
+                tmem_st16(s_tm, pk);
+                const float base = ref > -CUDART_INF_F ? ref : 0.f;
+                const float2 down = make_float2(-base, -base);
+                exp_chunk<T>(s + 32, c2, down, la, pk);
+                tmem_st16(s_tm + 16, pk);
+                exp_chunk<T>(s + 64, c2, down, la, pk);
+                tmem_st16(s_tm + 32, pk);
+                exp_chunk<T>(s + 96, c2, down, la, pk);
+                tmem_st16(s_tm + 48, pk);
+                l = add2(l, la);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full);
+            }
+            if (!ok) break;
+            ok = mbar_wait_all(o_full, n & 1, abort);
+            if (!ok) break;
+            tc_fence_after();
+            const float total = bad ? CUDART_NAN_F : l.x + l.y;
+            const float inv = total > 0.f ? 1.f / total : (total == 0.f ? 0.f : total);
+            const int rows = it->rows * p.G;
+            const int64_t at = int64_t(it->part) + (unit % p.kv_heads) * rows + m;
+            float* dst = p.plan.part + at * p.D;
+#pragma unroll 1
+            for (int c = 0; c < DP; c += 32) {
+                uint32_t o[32];
+                tmem_ld32(o_tm + c, o);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * inv);
+#pragma unroll
+                for (int e = 0; e < 32; e += 8)
+                    if (m < rows && c + e < p.D) st_global32(dst + c + e, o + e);
+            }
+            if (m < rows) p.plan.part_lse[at] = total > 0.f ? ref + log2f(total) : (total == 0.f ? -CUDART_INF_F : total);
+            tc_fence_before();                        // O has been read before the next unit's first probabilities are reported
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (s_abort && threadIdx.x == 0) {
+        atomicExch(p.error, 1u);
+        for (int i = 0; i < 200; ++i) __nanosleep(1000);          // copies in flight land before the memory is given up
+    }
+    __syncthreads();
+    if (warp == 5) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::TMEM) : "memory");
+    }
+}
+
+// ---- kernel 2 -----------------------------------------------------------------------------------------
+constexpr int JT = 128;                // threads of a block: 4 warps, each with a row and key head of its own
+
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool some) {
+    const int n = some ? 16 : 0;
+    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t a, uint32_t* r) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t a, uint32_t* r) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+template <typename T>
+__device__ __forceinline__ void mma16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void mma16<__nv_bfloat16>(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <>
+__device__ __forceinline__ void mma16<__half>(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// 16-byte chunk ch of row `row` of a block in shared memory; neighbouring rows' chunks lie in different banks
+template <int DP>
+__device__ __forceinline__ uint32_t chunk_at(int row, int ch) {
+    return uint32_t(row * (DP * 2) + ((ch ^ (row & 7)) << 4));
+}
+
+struct JoinRow {                       // two rows' running state: rows lane / 4 and lane / 4 + 8 of the tile
+    float m0, m1, l0, l1;
+};
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(JT, 4) attend_join_kernel(const AttendParams p) {
+    constexpr int CH = DP / 8;
+    constexpr int BLOCK_BYTES = BLK * DP * 2;
+    extern __shared__ __align__(128) unsigned char smem[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t job = int64_t(blockIdx.x) * (JT / 32) + warp;
+    if (job >= int64_t(p.rows) * p.kv_heads) return;
+    const int row = int(job / p.kv_heads), head = int(job % p.kv_heads);
+    const PlanShape& sh = p.shape;
+    const int G = sh.G;
+    const int g = row / sh.group * sh.sub + row % sh.group / sh.per_group, k_row = row % sh.group % sh.per_group;
+    const int first_row = row - k_row;
+    const int group_rows = min(p.rows, min(first_row + sh.per_group, row / sh.group * sh.group + sh.group)) - first_row;
+    const int32_t len = p.len[row];
+    const int2 gp = p.plan.group_part[g], rp = p.plan.row_part[row];
+    const int begin = p.plan.shared[g] + p.plan.alone[row], end = (len + BLK - 1) / BLK;
+    const int32_t* table = p.table + int64_t(row) * p.width;
+    const int64_t head_bytes = int64_t(p.page_size) * p.D * 2;
+    unsigned char* k_sm = smem + warp * 2 * BLOCK_BYTES;
+    const uint32_t k_at = smem_u32(k_sm), v_at = k_at + BLOCK_BYTES;
+    const int64_t out_at = (int64_t(row) * p.kv_heads + head) * G;
+
+    auto load_block = [&](int blk) {
+        const int page = table[blk / sh.blks_per_page], tokens = min(BLK, len - blk * BLK);
+        const int64_t off = (int64_t(page) * p.kv_heads + head) * head_bytes + int64_t(blk % sh.blks_per_page) * (BLK * 2) * p.D;
+#pragma unroll
+        for (int j = 0; j < BLK * CH / 32; ++j) {
+            const int c = j * 32 + lane, r = c / CH, ch = c % CH;
+            const bool some = r < tokens && ch * 8 < p.D;
+            const int64_t src = some ? off + int64_t(r) * p.D * 2 + ch * 16 : 0;
+            const uint32_t dst = chunk_at<DP>(r, ch);
+            cp16(k_at + dst, p.k + src, some);
+            cp16(v_at + dst, p.v + src, some);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+
+    for (int g0 = 0; g0 < G; g0 += 16) {               // query heads g0 .. g0 + 15
+        if (begin < end) load_block(begin);
+        const int r_lo = g0 + (lane >> 2), r_hi = r_lo + 8;
+        const bool lo = r_lo < G, hi = r_hi < G;
+        float o[DP / 8][4];
+#pragma unroll
+        for (int j = 0; j < DP / 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+        JoinRow w{-CUDART_INF_F, -CUDART_INF_F, 0.f, 0.f};
+        // the row's sums so far, seen from new maxima
+        auto move_to = [&](float n0, float n1) {
+            const float f0 = w.m0 > -CUDART_INF_F ? ex2_approx(w.m0 - n0) : 0.f, f1 = w.m1 > -CUDART_INF_F ? ex2_approx(w.m1 - n1) : 0.f;
+            w = JoinRow{n0, n1, w.l0 * f0, w.l1 * f1};
+#pragma unroll
+            for (int j = 0; j < DP / 8; ++j) { o[j][0] *= f0; o[j][1] *= f0; o[j][2] *= f1; o[j][3] *= f1; }
+        };
+        // the parts: the group's items in order, then the row's own
+        auto take_parts = [&](int2 part, int rows, int at_row) {
+            for (int x = 0; x < part.y; ++x) {
+                const int64_t base = int64_t(part.x) + (int64_t(x) * p.kv_heads + head) * rows + at_row;
+                const float a = lo ? p.plan.part_lse[base + r_lo] : -CUDART_INF_F, b = hi ? p.plan.part_lse[base + r_hi] : -CUDART_INF_F;
+                move_to(fmaxf(w.m0, a), fmaxf(w.m1, b));
+                const float f0 = a == -CUDART_INF_F ? 0.f : ex2_approx(a - w.m0), f1 = b == -CUDART_INF_F ? 0.f : ex2_approx(b - w.m1);
+                w.l0 += f0;
+                w.l1 += f1;
+                const float* src0 = p.plan.part + (base + r_lo) * p.D + (lane & 3) * 2;
+                const float* src1 = src0 + 8 * int64_t(p.D);
+#pragma unroll
+                for (int j = 0; j < DP / 8; ++j) {
+                    if (lo && j * 8 < p.D) {
+                        const float2 y = *reinterpret_cast<const float2*>(src0 + j * 8);
+                        o[j][0] = fmaf(f0, y.x, o[j][0]);
+                        o[j][1] = fmaf(f0, y.y, o[j][1]);
+                    }
+                    if (hi && j * 8 < p.D) {
+                        const float2 y = *reinterpret_cast<const float2*>(src1 + j * 8);
+                        o[j][2] = fmaf(f1, y.x, o[j][2]);
+                        o[j][3] = fmaf(f1, y.y, o[j][3]);
+                    }
+                }
+            }
+        };
+        take_parts(gp, group_rows * G, k_row * G);
+        take_parts(rp, G, 0);
+        // query fragments straight from memory: 4 bytes at (row, 16 kk + 2 (lane % 4)) and 8 values further
+        uint32_t qf[DP / 16][4];
+        {
+            const unsigned char* q_lo = p.q + row * p.q_row + (head * G + r_lo) * p.q_head + (lane & 3) * 4;
+            const unsigned char* q_hi = q_lo + 8 * p.q_head;
+#pragma unroll
+            for (int kk = 0; kk < DP / 16; ++kk) {
+                const bool a = kk * 16 < p.D, b = kk * 16 + 8 < p.D;
+                qf[kk][0] = lo && a ? *reinterpret_cast<const uint32_t*>(q_lo + kk * 32) : 0u;
+                qf[kk][1] = hi && a ? *reinterpret_cast<const uint32_t*>(q_hi + kk * 32) : 0u;
+                qf[kk][2] = lo && b ? *reinterpret_cast<const uint32_t*>(q_lo + kk * 32 + 16) : 0u;
+                qf[kk][3] = hi && b ? *reinterpret_cast<const uint32_t*>(q_hi + kk * 32 + 16) : 0u;
+            }
+        }
+        // what is left of the row, a block of 16 tokens at a time
+        for (int blk = begin; blk < end; ++blk) {
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncwarp();
+            const int tokens = min(BLK, len - blk * BLK);
+            float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+            for (int kk = 0; kk < DP / 16; ++kk) {
+                uint32_t kf[4];
+                ldsm4(k_at + chunk_at<DP>((lane & 7) + ((lane >> 4) << 3), 2 * kk + ((lane >> 3) & 1)), kf);
+                mma16<T>(s[0], qf[kk], kf[0], kf[1]);
+                mma16<T>(s[1], qf[kk], kf[2], kf[3]);
+            }
+            float mx0 = -CUDART_INF_F, mx1 = -CUDART_INF_F;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const bool some = h * 8 + (lane & 3) * 2 + e < tokens;
+                    s[h][e] = some ? s[h][e] * p.c2 : -CUDART_INF_F;
+                    s[h][2 + e] = some ? s[h][2 + e] * p.c2 : -CUDART_INF_F;
+                    mx0 = fmaxf(mx0, s[h][e]);
+                    mx1 = fmaxf(mx1, s[h][2 + e]);
+                }
+            mx0 = fmaxf(mx0, __shfl_xor_sync(FULL, mx0, 1));
+            mx1 = fmaxf(mx1, __shfl_xor_sync(FULL, mx1, 1));
+            mx0 = fmaxf(mx0, __shfl_xor_sync(FULL, mx0, 2));
+            mx1 = fmaxf(mx1, __shfl_xor_sync(FULL, mx1, 2));
+            if (__any_sync(FULL, mx0 > w.m0 || mx1 > w.m1)) move_to(fmaxf(w.m0, mx0), fmaxf(w.m1, mx1));
+            const float ref0 = w.m0 > -CUDART_INF_F ? w.m0 : 0.f, ref1 = w.m1 > -CUDART_INF_F ? w.m1 : 0.f;
+            uint32_t pf[4];
+            float a0 = 0.f, a1 = 0.f;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float x0 = ex2_approx(s[h][0] - ref0), x1 = ex2_approx(s[h][1] - ref0), x2 = ex2_approx(s[h][2] - ref1), x3 = ex2_approx(s[h][3] - ref1);
+                a0 += x0 + x1;
+                a1 += x2 + x3;
+                pf[2 * h] = pack2<T>(x0, x1);
+                pf[2 * h + 1] = pack2<T>(x2, x3);
+            }
+            a0 += __shfl_xor_sync(FULL, a0, 1);
+            a1 += __shfl_xor_sync(FULL, a1, 1);
+            a0 += __shfl_xor_sync(FULL, a0, 2);
+            a1 += __shfl_xor_sync(FULL, a1, 2);
+            w.l0 += a0;
+            w.l1 += a1;
+#pragma unroll
+            for (int j = 0; j < DP / 16; ++j) {
+                uint32_t vf[4];
+                ldsm4t(v_at + chunk_at<DP>(lane & 15, 2 * j + (lane >> 4)), vf);
+                mma16<T>(o[2 * j], pf, vf[0], vf[1]);
+                mma16<T>(o[2 * j + 1], pf, vf[2], vf[3]);
+            }
+            __syncwarp();
+            if (blk + 1 < end) load_block(blk + 1);
+        }
+        const float inv0 = w.l0 > 0.f ? 1.f / w.l0 : (w.l0 == 0.f ? 0.f : w.l0), inv1 = w.l1 > 0.f ? 1.f / w.l1 : (w.l1 == 0.f ? 0.f : w.l1);
+#pragma unroll
+        for (int j = 0; j < DP / 8; ++j) {
+            const int d = j * 8 + (lane & 3) * 2;
+            if (lo && d < p.D) *reinterpret_cast<uint32_t*>(p.out + ((out_at + r_lo) * p.D + d) * 2) = pack2<T>(o[j][0] * inv0, o[j][1] * inv0);
+            if (hi && d < p.D) *reinterpret_cast<uint32_t*>(p.out + ((out_at + r_hi) * p.D + d) * 2) = pack2<T>(o[j][2] * inv1, o[j][3] * inv1);
+        }
+        if (p.lse && (lane & 3) == 0) {
+            if (lo) p.lse[out_at + r_lo] = w.l0 > 0.f ? (w.m0 + log2f(w.l0)) * LN2_F : (w.l0 == 0.f ? -CUDART_INF_F : w.l0);
+            if (hi) p.lse[out_at + r_hi] = w.l1 > 0.f ? (w.m1 + log2f(w.l1)) * LN2_F : (w.l1 == 0.f ? -CUDART_INF_F : w.l1);
+        }
+    }
+}
+
+template <typename T, int DP>
+int launch_groups(const AttendParams& a, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const GroupParams& p, unsigned grid, cudaStream_t st) {
+    static std::atomic<uint64_t> done{0}, done2{0};
+    constexpr int join_bytes = JT / 32 * 2 * BLK * DP * 2;
+    if (const int rc = allow_smem(attend_group_kernel<T, DP>, Shape<DP>::SMEM, done)) return rc;
+    attend_group_kernel<T, DP><<<grid, THREADS, Shape<DP>::SMEM, st>>>(q, k, v, p);
+    DISC_CUDA(cudaGetLastError());
+    if (const int rc = allow_smem(attend_join_kernel<T, DP>, join_bytes, done2)) return rc;
+    const int64_t jobs = int64_t(a.rows) * a.kv_heads;
+    attend_join_kernel<T, DP><<<unsigned((jobs + JT / 32 - 1) / (JT / 32)), JT, join_bytes, st>>>(a);
+    DISC_CUDA(cudaGetLastError());
+    return DISC_OK;
+}
+
+int encode(EncodeTiled enc, CUtensorMap* map, CUtensorMapDataType type, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides,
+           const cuuint32_t* box) {
+    const cuuint32_t estr[3] = {1, 1, 1};
+    const CUresult r = enc(map, type, cuuint32_t(rank), const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? DISC_OK : DISC_ERR_UNSUPPORTED;
+}
+
+}  // namespace
+
+int disc::plan_groups(const PlanParams& p, cudaStream_t st) {
+    group_shared_kernel<<<unsigned(p.shape.groups), 256, 0, st>>>(p);
+    group_items_kernel<<<1, PT, 0, st>>>(p);
+    DISC_CUDA(cudaGetLastError());
+    return DISC_OK;
+}
+
+int disc::attend_groups(const AttendParams& a, int32_t dtype, int32_t n_q_heads, cudaStream_t st) {
+    GroupParams p;
+    p.plan = a.plan; p.table = a.table; p.width = a.width; p.kv_heads = a.kv_heads; p.G = a.shape.G; p.per_group = a.shape.per_group;
+    p.D = a.D; p.page_size = a.page_size; p.blks_per_page = a.shape.blks_per_page; p.c2 = a.c2; p.error = a.error;
+    const int DP = a.D <= 64 ? 64 : 128;
+    // instruction descriptors: D fp32 (bits 4-5 = 1), A and B f16 = 0 / bf16 = 1 (bits 7-9, 10-12), B of the second
+    // product N-major (bit 16), N >> 3 at bit 17, M >> 4 at bit 24
+    const uint32_t ty = dtype == DISC_BF16 ? 1u : 0u;
+    const uint32_t idesc = (1u << 4) | (ty << 7) | (ty << 10) | (uint32_t(GROUP_M >> 4) << 24);
+    p.idesc_qk = idesc | (uint32_t(TN >> 3) << 17);
+    p.idesc_pv = idesc | (uint32_t(DP >> 3) << 17) | (1u << 16);
+    EncodeTiled enc = nullptr;
+    if (const int rc = tensor_map_encoder(&enc)) return rc;
+    const CUtensorMapDataType type = dtype == DISC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    alignas(64) CUtensorMap map_q, map_k, map_v;
+    if (a.q_row <= 0 || a.q_head <= 0) return DISC_ERR_UNSUPPORTED;
+    const cuuint64_t q_dims[3] = {cuuint64_t(a.D), cuuint64_t(n_q_heads), cuuint64_t(a.rows)}, q_strides[2] = {cuuint64_t(a.q_head), cuuint64_t(a.q_row)};
+    const cuuint32_t q_box[3] = {cuuint32_t(BOX), cuuint32_t(p.G), cuuint32_t(p.per_group)};
+    if (const int rc = encode(enc, &map_q, type, 3, a.q, q_dims, q_strides, q_box)) return rc;
+    // a plane as [pages x heads x page size][D]
+    const cuuint64_t dims[2] = {cuuint64_t(a.D), cuuint64_t(a.pages) * a.kv_heads * a.page_size}, strides[1] = {cuuint64_t(a.D) * 2};
+    const cuuint32_t box[2] = {cuuint32_t(BOX), cuuint32_t(BLK)};
+    if (const int rc = encode(enc, &map_k, type, 2, a.k, dims, strides, box)) return rc;
+    if (const int rc = encode(enc, &map_v, type, 2, a.v, dims, strides, box)) return rc;
+    int sms = 0;
+    if (const int rc = device_sms(&sms)) return rc;
+    const int64_t most = int64_t(a.shape.max_items) * a.kv_heads;
+    const unsigned grid = unsigned(most < 2 * sms ? most : 2 * sms);
+    if (dtype == DISC_BF16)
+        return DP == 64 ? launch_groups<__nv_bfloat16, 64>(a, map_q, map_k, map_v, p, grid, st) : launch_groups<__nv_bfloat16, 128>(a, map_q, map_k, map_v, p, grid, st);
+    return DP == 64 ? launch_groups<__half, 64>(a, map_q, map_k, map_v, p, grid, st) : launch_groups<__half, 128>(a, map_q, map_k, map_v, p, grid, st);
+}
