@@ -411,14 +411,28 @@ __device__ __forceinline__ uint32_t chunk_at(int row, int ch) {
     return uint32_t(row * (DP * 2) + ((ch ^ (row & 7)) << 4));
 }
 
-struct JoinRow {                       // two rows' running state: rows lane / 4 and lane / 4 + 8 of the tile
-    float m0, m1, l0, l1;
+// an 8 x 8 matrix of 16-bit values across the warp, transposed
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
+template <int DP>
+struct JoinSmem {
+    static constexpr int O_LD = DP + 4;                            // fp32 sums [8 heads][DP], over the block's keys and values
+    static constexpr int BLOCK_BYTES = BLK * DP * 2;
+    static constexpr int WARP_BYTES = 2 * BLOCK_BYTES + 64;        // a block's keys and values; maximum and sum of 8 heads
+    static_assert(8 * O_LD * 4 <= 2 * BLOCK_BYTES, "the sums fit over the block");
 };
 
+// The products are taken the other way round, S^T = K Q^T and O^T = V^T P^T: 8 query heads are then the narrow side of
+// m16n8k16, where rows of queries would leave 12 of 16 rows empty with 4 heads, and hold twice the registers (101 us that
+// way on 4096 rows x 4 key heads).
 template <typename T, int DP>
-__global__ void __launch_bounds__(JT, 4) attend_join_kernel(const AttendParams p) {
+__global__ void __launch_bounds__(JT, 6) attend_join_kernel(const AttendParams p) {
+    using S = JoinSmem<DP>;
     constexpr int CH = DP / 8;
-    constexpr int BLOCK_BYTES = BLK * DP * 2;
     extern __shared__ __align__(128) unsigned char smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t job = int64_t(blockIdx.x) * (JT / 32) + warp;
@@ -434,8 +448,10 @@ __global__ void __launch_bounds__(JT, 4) attend_join_kernel(const AttendParams p
     const int begin = p.plan.shared[g] + p.plan.alone[row], end = (len + BLK - 1) / BLK;
     const int32_t* table = p.table + int64_t(row) * p.width;
     const int64_t head_bytes = int64_t(p.page_size) * p.D * 2;
-    unsigned char* k_sm = smem + warp * 2 * BLOCK_BYTES;
-    const uint32_t k_at = smem_u32(k_sm), v_at = k_at + BLOCK_BYTES;
+    unsigned char* own = smem + warp * S::WARP_BYTES;
+    const uint32_t k_at = smem_u32(own), v_at = k_at + S::BLOCK_BYTES;
+    float* o_sm = reinterpret_cast<float*>(own);
+    float* ml_sm = reinterpret_cast<float*>(own + 2 * S::BLOCK_BYTES);     // [8] maxima, [8] sums
     const int64_t out_at = (int64_t(row) * p.kv_heads + head) * G;
 
     auto load_block = [&](int blk) {
@@ -453,137 +469,133 @@ __global__ void __launch_bounds__(JT, 4) attend_join_kernel(const AttendParams p
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
 
-    for (int g0 = 0; g0 < G; g0 += 16) {               // query heads g0 .. g0 + 15
-        if (begin < end) load_block(begin);
-        const int r_lo = g0 + (lane >> 2), r_hi = r_lo + 8;
-        const bool lo = r_lo < G, hi = r_hi < G;
-        float o[DP / 8][4];
-#pragma unroll
-        for (int j = 0; j < DP / 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
-        JoinRow w{-CUDART_INF_F, -CUDART_INF_F, 0.f, 0.f};
-        // the row's sums so far, seen from new maxima
-        auto move_to = [&](float n0, float n1) {
-            const float f0 = w.m0 > -CUDART_INF_F ? ex2_approx(w.m0 - n0) : 0.f, f1 = w.m1 > -CUDART_INF_F ? ex2_approx(w.m1 - n1) : 0.f;
-            w = JoinRow{n0, n1, w.l0 * f0, w.l1 * f1};
-#pragma unroll
-            for (int j = 0; j < DP / 8; ++j) { o[j][0] *= f0; o[j][1] *= f0; o[j][2] *= f1; o[j][3] *= f1; }
-        };
-        // the parts: the group's items in order, then the row's own
-        auto take_parts = [&](int2 part, int rows, int at_row) {
-            for (int x = 0; x < part.y; ++x) {
-                const int64_t base = int64_t(part.x) + (int64_t(x) * p.kv_heads + head) * rows + at_row;
-                const float a = lo ? p.plan.part_lse[base + r_lo] : -CUDART_INF_F, b = hi ? p.plan.part_lse[base + r_hi] : -CUDART_INF_F;
-                move_to(fmaxf(w.m0, a), fmaxf(w.m1, b));
-                const float f0 = a == -CUDART_INF_F ? 0.f : ex2_approx(a - w.m0), f1 = b == -CUDART_INF_F ? 0.f : ex2_approx(b - w.m1);
-                w.l0 += f0;
-                w.l1 += f1;
-                const float* src0 = p.plan.part + (base + r_lo) * p.D + (lane & 3) * 2;
-                const float* src1 = src0 + 8 * int64_t(p.D);
-#pragma unroll
-                for (int j = 0; j < DP / 8; ++j) {
-                    if (lo && j * 8 < p.D) {
-                        const float2 y = *reinterpret_cast<const float2*>(src0 + j * 8);
-                        o[j][0] = fmaf(f0, y.x, o[j][0]);
-                        o[j][1] = fmaf(f0, y.y, o[j][1]);
-                    }
-                    if (hi && j * 8 < p.D) {
-                        const float2 y = *reinterpret_cast<const float2*>(src1 + j * 8);
-                        o[j][2] = fmaf(f1, y.x, o[j][2]);
-                        o[j][3] = fmaf(f1, y.y, o[j][3]);
-                    }
-                }
-            }
-        };
-        take_parts(gp, group_rows * G, k_row * G);
-        take_parts(rp, G, 0);
-        // query fragments straight from memory: 4 bytes at (row, 16 kk + 2 (lane % 4)) and 8 values further
-        uint32_t qf[DP / 16][4];
-        {
-            const unsigned char* q_lo = p.q + row * p.q_row + (head * G + r_lo) * p.q_head + (lane & 3) * 4;
-            const unsigned char* q_hi = q_lo + 8 * p.q_head;
+    for (int g0 = 0; g0 < G; g0 += 8) {                // query heads g0 .. g0 + 7
+        const int heads = min(8, G - g0);
+        if (begin < end) {
+            load_block(begin);
+            // query fragments: head lane / 4, values 16 kk + 2 (lane % 4) and 8 further
+            uint32_t qf[DP / 16][2];
+            const bool some_head = (lane >> 2) < heads;
+            const unsigned char* q = p.q + row * p.q_row + (head * G + g0 + (lane >> 2)) * p.q_head + (lane & 3) * 4;
 #pragma unroll
             for (int kk = 0; kk < DP / 16; ++kk) {
-                const bool a = kk * 16 < p.D, b = kk * 16 + 8 < p.D;
-                qf[kk][0] = lo && a ? *reinterpret_cast<const uint32_t*>(q_lo + kk * 32) : 0u;
-                qf[kk][1] = hi && a ? *reinterpret_cast<const uint32_t*>(q_hi + kk * 32) : 0u;
-                qf[kk][2] = lo && b ? *reinterpret_cast<const uint32_t*>(q_lo + kk * 32 + 16) : 0u;
-                qf[kk][3] = hi && b ? *reinterpret_cast<const uint32_t*>(q_hi + kk * 32 + 16) : 0u;
+                qf[kk][0] = some_head && kk * 16 < p.D ? *reinterpret_cast<const uint32_t*>(q + kk * 32) : 0u;
+                qf[kk][1] = some_head && kk * 16 + 8 < p.D ? *reinterpret_cast<const uint32_t*>(q + kk * 32 + 16) : 0u;
             }
-        }
-        // what is left of the row, a block of 16 tokens at a time
-        for (int blk = begin; blk < end; ++blk) {
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
-            __syncwarp();
-            const int tokens = min(BLK, len - blk * BLK);
-            float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+            // this thread's two heads: 2 (lane % 4) and the next
+            float o[DP / 16][4];
 #pragma unroll
-            for (int kk = 0; kk < DP / 16; ++kk) {
-                uint32_t kf[4];
-                ldsm4(k_at + chunk_at<DP>((lane & 7) + ((lane >> 4) << 3), 2 * kk + ((lane >> 3) & 1)), kf);
-                mma16<T>(s[0], qf[kk], kf[0], kf[1]);
-                mma16<T>(s[1], qf[kk], kf[2], kf[3]);
-            }
-            float mx0 = -CUDART_INF_F, mx1 = -CUDART_INF_F;
+            for (int j = 0; j < DP / 16; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+            float m0 = -CUDART_INF_F, m1 = -CUDART_INF_F, l0 = 0.f, l1 = 0.f;
+            for (int blk = begin; blk < end; ++blk) {
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+                __syncwarp();
+                const int tokens = min(BLK, len - blk * BLK);
+                float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const bool some = h * 8 + (lane & 3) * 2 + e < tokens;
-                    s[h][e] = some ? s[h][e] * p.c2 : -CUDART_INF_F;
-                    s[h][2 + e] = some ? s[h][2 + e] * p.c2 : -CUDART_INF_F;
-                    mx0 = fmaxf(mx0, s[h][e]);
-                    mx1 = fmaxf(mx1, s[h][2 + e]);
+                for (int kk = 0; kk < DP / 16; ++kk) {
+                    uint32_t kf[4];
+                    ldsm4(k_at + chunk_at<DP>(lane & 15, 2 * kk + (lane >> 4)), kf);
+                    mma16<T>(s, kf, qf[kk][0], qf[kk][1]);
                 }
-            mx0 = fmaxf(mx0, __shfl_xor_sync(FULL, mx0, 1));
-            mx1 = fmaxf(mx1, __shfl_xor_sync(FULL, mx1, 1));
-            mx0 = fmaxf(mx0, __shfl_xor_sync(FULL, mx0, 2));
-            mx1 = fmaxf(mx1, __shfl_xor_sync(FULL, mx1, 2));
-            if (__any_sync(FULL, mx0 > w.m0 || mx1 > w.m1)) move_to(fmaxf(w.m0, mx0), fmaxf(w.m1, mx1));
-            const float ref0 = w.m0 > -CUDART_INF_F ? w.m0 : 0.f, ref1 = w.m1 > -CUDART_INF_F ? w.m1 : 0.f;
-            uint32_t pf[4];
-            float a0 = 0.f, a1 = 0.f;
+                // tokens lane / 4 (s[0], s[1]) and 8 further (s[2], s[3])
+                const bool a = (lane >> 2) < tokens, b = (lane >> 2) + 8 < tokens;
+                s[0] = a ? s[0] * p.c2 : -CUDART_INF_F;
+                s[1] = a ? s[1] * p.c2 : -CUDART_INF_F;
+                s[2] = b ? s[2] * p.c2 : -CUDART_INF_F;
+                s[3] = b ? s[3] * p.c2 : -CUDART_INF_F;
+                float mx0 = fmaxf(s[0], s[2]), mx1 = fmaxf(s[1], s[3]);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float x0 = ex2_approx(s[h][0] - ref0), x1 = ex2_approx(s[h][1] - ref0), x2 = ex2_approx(s[h][2] - ref1), x3 = ex2_approx(s[h][3] - ref1);
-                a0 += x0 + x1;
-                a1 += x2 + x3;
-                pf[2 * h] = pack2<T>(x0, x1);
-                pf[2 * h + 1] = pack2<T>(x2, x3);
+                for (int x = 4; x < 32; x <<= 1) {
+                    mx0 = fmaxf(mx0, __shfl_xor_sync(FULL, mx0, x));
+                    mx1 = fmaxf(mx1, __shfl_xor_sync(FULL, mx1, x));
+                }
+                const float n0 = fmaxf(m0, mx0), n1 = fmaxf(m1, mx1);
+                if (blk > begin && __any_sync(FULL, n0 > m0 || n1 > m1)) {
+                    const float f0 = m0 > -CUDART_INF_F ? ex2_approx(m0 - n0) : 0.f, f1 = m1 > -CUDART_INF_F ? ex2_approx(m1 - n1) : 0.f;
+                    l0 *= f0;
+                    l1 *= f1;
+#pragma unroll
+                    for (int j = 0; j < DP / 16; ++j) { o[j][0] *= f0; o[j][1] *= f1; o[j][2] *= f0; o[j][3] *= f1; }
+                }
+                m0 = n0;
+                m1 = n1;
+                const float ref0 = m0 > -CUDART_INF_F ? m0 : 0.f, ref1 = m1 > -CUDART_INF_F ? m1 : 0.f;
+                s[0] = ex2_approx(s[0] - ref0);
+                s[1] = ex2_approx(s[1] - ref1);
+                s[2] = ex2_approx(s[2] - ref0);
+                s[3] = ex2_approx(s[3] - ref1);
+                l0 += s[0] + s[2];
+                l1 += s[1] + s[3];
+                const uint32_t p0 = transposed(pack2<T>(s[0], s[1])), p1 = transposed(pack2<T>(s[2], s[3]));
+#pragma unroll
+                for (int j = 0; j < DP / 16; ++j) {
+                    uint32_t vf[4];
+                    ldsm4t(v_at + chunk_at<DP>((lane & 7) + ((lane >> 4) << 3), 2 * j + ((lane >> 3) & 1)), vf);
+                    mma16<T>(o[j], vf, p0, p1);
+                }
+                __syncwarp();
+                if (blk + 1 < end) load_block(blk + 1);
             }
-            a0 += __shfl_xor_sync(FULL, a0, 1);
-            a1 += __shfl_xor_sync(FULL, a1, 1);
-            a0 += __shfl_xor_sync(FULL, a0, 2);
-            a1 += __shfl_xor_sync(FULL, a1, 2);
-            w.l0 += a0;
-            w.l1 += a1;
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) {
+                l0 += __shfl_xor_sync(FULL, l0, x);
+                l1 += __shfl_xor_sync(FULL, l1, x);
+            }
+            float* dst = o_sm + (lane & 3) * 2 * S::O_LD + (lane >> 2);
 #pragma unroll
             for (int j = 0; j < DP / 16; ++j) {
-                uint32_t vf[4];
-                ldsm4t(v_at + chunk_at<DP>(lane & 15, 2 * j + (lane >> 4)), vf);
-                mma16<T>(o[2 * j], pf, vf[0], vf[1]);
-                mma16<T>(o[2 * j + 1], pf, vf[2], vf[3]);
+                dst[16 * j] = o[j][0];
+                dst[S::O_LD + 16 * j] = o[j][1];
+                dst[16 * j + 8] = o[j][2];
+                dst[S::O_LD + 16 * j + 8] = o[j][3];
+            }
+            if (lane < 4) {
+                ml_sm[2 * lane] = m0; ml_sm[2 * lane + 1] = m1;
+                ml_sm[8 + 2 * lane] = l0; ml_sm[8 + 2 * lane + 1] = l1;
             }
             __syncwarp();
-            if (blk + 1 < end) load_block(blk + 1);
         }
-        const float inv0 = w.l0 > 0.f ? 1.f / w.l0 : (w.l0 == 0.f ? 0.f : w.l0), inv1 = w.l1 > 0.f ? 1.f / w.l1 : (w.l1 == 0.f ? 0.f : w.l1);
-#pragma unroll
-        for (int j = 0; j < DP / 8; ++j) {
-            const int d = j * 8 + (lane & 3) * 2;
-            if (lo && d < p.D) *reinterpret_cast<uint32_t*>(p.out + ((out_at + r_lo) * p.D + d) * 2) = pack2<T>(o[j][0] * inv0, o[j][1] * inv0);
-            if (hi && d < p.D) *reinterpret_cast<uint32_t*>(p.out + ((out_at + r_hi) * p.D + d) * 2) = pack2<T>(o[j][2] * inv1, o[j][3] * inv1);
+        // the parts, in order: the group's items, then the row's own, then what was just added up
+        for (int i = lane; i < heads * (DP / 4); i += 32) {
+            const int h = i / (DP / 4), d = i % (DP / 4) * 4;
+            if (d >= p.D) continue;
+            const int64_t g_at = int64_t(gp.x) + int64_t(head) * group_rows * G + k_row * G + g0 + h, g_step = int64_t(p.kv_heads) * group_rows * G;
+            const int64_t r_at = int64_t(rp.x) + int64_t(head) * G + g0 + h, r_step = int64_t(p.kv_heads) * G;
+            float m = -CUDART_INF_F, total = 0.f;
+            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+            auto take = [&](int64_t at) {
+                const float lse = p.plan.part_lse[at];
+                const float4 y = *reinterpret_cast<const float4*>(p.plan.part + at * p.D + d);
+                const float n = fmaxf(m, lse);
+                const float f = m > -CUDART_INF_F ? ex2_approx(m - n) : 0.f, w = lse == -CUDART_INF_F ? 0.f : ex2_approx(lse - n);
+                m = n;
+                total = fmaf(total, f, w);
+                x = make_float4(fmaf(w, y.x, x.x * f), fmaf(w, y.y, x.y * f), fmaf(w, y.z, x.z * f), fmaf(w, y.w, x.w * f));
+            };
+            for (int s = 0; s < gp.y; ++s) take(g_at + s * g_step);
+            for (int s = 0; s < rp.y; ++s) take(r_at + s * r_step);
+            if (begin < end) {
+                const float mt = ml_sm[h], lt = ml_sm[8 + h];
+                const float4 y = *reinterpret_cast<const float4*>(o_sm + h * S::O_LD + d);
+                const float n = fmaxf(m, mt);
+                const float f = m > -CUDART_INF_F ? ex2_approx(m - n) : 0.f, w = mt > -CUDART_INF_F ? ex2_approx(mt - n) : (lt == 0.f ? 0.f : lt);
+                m = n;
+                total = fmaf(total, f, w * lt);
+                x = make_float4(fmaf(w, y.x, x.x * f), fmaf(w, y.y, x.y * f), fmaf(w, y.z, x.z * f), fmaf(w, y.w, x.w * f));
+            }
+            const float inv = total > 0.f ? 1.f / total : (total == 0.f ? 0.f : total);
+            *reinterpret_cast<uint2*>(p.out + ((out_at + g0 + h) * p.D + d) * 2) = make_uint2(pack2<T>(x.x * inv, x.y * inv), pack2<T>(x.z * inv, x.w * inv));
+            if (d == 0 && p.lse) p.lse[out_at + g0 + h] = total > 0.f ? (m + log2f(total)) * LN2_F : (total == 0.f ? -CUDART_INF_F : total);
         }
-        if (p.lse && (lane & 3) == 0) {
-            if (lo) p.lse[out_at + r_lo] = w.l0 > 0.f ? (w.m0 + log2f(w.l0)) * LN2_F : (w.l0 == 0.f ? -CUDART_INF_F : w.l0);
-            if (hi) p.lse[out_at + r_hi] = w.l1 > 0.f ? (w.m1 + log2f(w.l1)) * LN2_F : (w.l1 == 0.f ? -CUDART_INF_F : w.l1);
-        }
+        __syncwarp();                                  // the sums have been read before the next heads' block comes in
     }
 }
 
 template <typename T, int DP>
 int launch_groups(const AttendParams& a, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const GroupParams& p, unsigned grid, cudaStream_t st) {
     static std::atomic<uint64_t> done{0}, done2{0};
-    constexpr int join_bytes = JT / 32 * 2 * BLK * DP * 2;
+    constexpr int join_bytes = JT / 32 * JoinSmem<DP>::WARP_BYTES;
     if (const int rc = allow_smem(attend_group_kernel<T, DP>, Shape<DP>::SMEM, done)) return rc;
     attend_group_kernel<T, DP><<<grid, THREADS, Shape<DP>::SMEM, st>>>(q, k, v, p);
     DISC_CUDA(cudaGetLastError());
