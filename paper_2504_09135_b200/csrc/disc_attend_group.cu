@@ -420,24 +420,27 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
 
 template <int DP>
 struct JoinSmem {
-    static constexpr int O_LD = DP + 4;                            // fp32 sums [8 heads][DP], over the block's keys and values
+    static constexpr int O_LD = DP + 4;                            // fp32 sums [8 heads][DP], over keys and values no longer needed
     static constexpr int BLOCK_BYTES = BLK * DP * 2;
-    static constexpr int WARP_BYTES = 2 * BLOCK_BYTES + 64;        // a block's keys and values; maximum and sum of 8 heads
-    static_assert(8 * O_LD * 4 <= 2 * BLOCK_BYTES, "the sums fit over the block");
+    static constexpr int WARP_BYTES = 4 * BLOCK_BYTES + 64;        // keys and values of two blocks; maximum and sum of 8 heads
+    static_assert(8 * O_LD * 4 <= 2 * BLOCK_BYTES, "the sums fit over a block");
 };
 
 // The products are taken the other way round, S^T = K Q^T and O^T = V^T P^T: 8 query heads are then the narrow side of
 // m16n8k16, where rows of queries would leave 12 of 16 rows empty with 4 heads, and hold twice the registers (101 us that
-// way on 4096 rows x 4 key heads).
+// way on 4096 rows x 4 key heads).  A warp goes through several key heads of its row, as many as leave a warp for every
+// place on the device, and has the next block's loads in flight under the present one's products (78 us without).
 template <typename T, int DP>
-__global__ void __launch_bounds__(JT, 6) attend_join_kernel(const AttendParams p) {
+__global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p, int heads_per_job) {
     using S = JoinSmem<DP>;
     constexpr int CH = DP / 8;
     extern __shared__ __align__(128) unsigned char smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int jobs_per_row = (p.kv_heads + heads_per_job - 1) / heads_per_job;
     const int64_t job = int64_t(blockIdx.x) * (JT / 32) + warp;
-    if (job >= int64_t(p.rows) * p.kv_heads) return;
-    const int row = int(job / p.kv_heads), head = int(job % p.kv_heads);
+    if (job >= int64_t(p.rows) * jobs_per_row) return;
+    const int row = int(job / jobs_per_row), head0 = int(job % jobs_per_row) * heads_per_job;
+    const int head1 = min(p.kv_heads, head0 + heads_per_job);
     const PlanShape& sh = p.shape;
     const int G = sh.G;
     const int g = row / sh.group * sh.sub + row % sh.group / sh.per_group, k_row = row % sh.group % sh.per_group;
@@ -445,34 +448,42 @@ __global__ void __launch_bounds__(JT, 6) attend_join_kernel(const AttendParams p
     const int group_rows = min(p.rows, min(first_row + sh.per_group, row / sh.group * sh.group + sh.group)) - first_row;
     const int32_t len = p.len[row];
     const int2 gp = p.plan.group_part[g], rp = p.plan.row_part[row];
-    const int begin = p.plan.shared[g] + p.plan.alone[row], end = (len + BLK - 1) / BLK;
+    const int begin = p.plan.shared[g] + p.plan.alone[row], left = (len + BLK - 1) / BLK - begin;      // blocks
     const int32_t* table = p.table + int64_t(row) * p.width;
     const int64_t head_bytes = int64_t(p.page_size) * p.D * 2;
     unsigned char* own = smem + warp * S::WARP_BYTES;
-    const uint32_t k_at = smem_u32(own), v_at = k_at + S::BLOCK_BYTES;
-    float* o_sm = reinterpret_cast<float*>(own);
-    float* ml_sm = reinterpret_cast<float*>(own + 2 * S::BLOCK_BYTES);     // [8] maxima, [8] sums
-    const int64_t out_at = (int64_t(row) * p.kv_heads + head) * G;
+    float* ml_sm = reinterpret_cast<float*>(own + 4 * S::BLOCK_BYTES);     // [8] maxima, [8] sums
+    const int eights = (G + 7) / 8;                    // a key head's query heads, eight at a time
+    const int steps = (head1 - head0) * eights * left;
 
-    auto load_block = [&](int blk) {
-        const int page = table[blk / sh.blks_per_page], tokens = min(BLK, len - blk * BLK);
-        const int64_t off = (int64_t(page) * p.kv_heads + head) * head_bytes + int64_t(blk % sh.blks_per_page) * (BLK * 2) * p.D;
+    // step: block step % left of the (step / left)-th eight of query heads
+    auto load_step = [&](int step) {
+        if (step < steps) {
+            const int head = head0 + step / left / eights, blk = begin + step % left;
+            const int page = table[blk / sh.blks_per_page], tokens = min(BLK, len - blk * BLK);
+            const int64_t off = (int64_t(page) * p.kv_heads + head) * head_bytes + int64_t(blk % sh.blks_per_page) * (BLK * 2) * p.D;
+            const uint32_t k_at = smem_u32(own) + (step & 1) * 2 * S::BLOCK_BYTES;
 #pragma unroll
-        for (int j = 0; j < BLK * CH / 32; ++j) {
-            const int c = j * 32 + lane, r = c / CH, ch = c % CH;
-            const bool some = r < tokens && ch * 8 < p.D;
-            const int64_t src = some ? off + int64_t(r) * p.D * 2 + ch * 16 : 0;
-            const uint32_t dst = chunk_at<DP>(r, ch);
-            cp16(k_at + dst, p.k + src, some);
-            cp16(v_at + dst, p.v + src, some);
+            for (int j = 0; j < BLK * CH / 32; ++j) {
+                const int c = j * 32 + lane, r = c / CH, ch = c % CH;
+                const bool some = r < tokens && ch * 8 < p.D;
+                const int64_t src = some ? off + int64_t(r) * p.D * 2 + ch * 16 : 0;
+                const uint32_t dst = k_at + chunk_at<DP>(r, ch);
+                cp16(dst, p.k + src, some);
+                cp16(dst + S::BLOCK_BYTES, p.v + src, some);
+            }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
+    load_step(0);
 
-    for (int g0 = 0; g0 < G; g0 += 8) {                // query heads g0 .. g0 + 7
+    int step = 0;
+    for (int unit = 0; unit < (head1 - head0) * eights; ++unit) {
+        const int head = head0 + unit / eights, g0 = unit % eights * 8;
         const int heads = min(8, G - g0);
-        if (begin < end) {
-            load_block(begin);
+        const int64_t out_at = (int64_t(row) * p.kv_heads + head) * G;
+        float* o_sm = reinterpret_cast<float*>(own);
+        if (left > 0) {
             // query fragments: head lane / 4, values 16 kk + 2 (lane % 4) and 8 further
             uint32_t qf[DP / 16][2];
             const bool some_head = (lane >> 2) < heads;
@@ -487,10 +498,13 @@ __global__ void __launch_bounds__(JT, 6) attend_join_kernel(const AttendParams p
 #pragma unroll
             for (int j = 0; j < DP / 16; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
             float m0 = -CUDART_INF_F, m1 = -CUDART_INF_F, l0 = 0.f, l1 = 0.f;
-            for (int blk = begin; blk < end; ++blk) {
-                asm volatile("cp.async.wait_group 0;" ::: "memory");
+            for (int i = 0; i < left; ++i, ++step) {
+                __syncwarp();                          // what the next loads overwrite has been read by all lanes
+                load_step(step + 1);
+                asm volatile("cp.async.wait_group 1;" ::: "memory");
                 __syncwarp();
-                const int tokens = min(BLK, len - blk * BLK);
+                const int tokens = min(BLK, len - (begin + i) * BLK);
+                const uint32_t k_at = smem_u32(own) + (step & 1) * 2 * S::BLOCK_BYTES, v_at = k_at + S::BLOCK_BYTES;
                 float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int kk = 0; kk < DP / 16; ++kk) {
@@ -511,7 +525,7 @@ __global__ void __launch_bounds__(JT, 6) attend_join_kernel(const AttendParams p
                     mx1 = fmaxf(mx1, __shfl_xor_sync(FULL, mx1, x));
                 }
                 const float n0 = fmaxf(m0, mx0), n1 = fmaxf(m1, mx1);
-                if (blk > begin && __any_sync(FULL, n0 > m0 || n1 > m1)) {
+                if (i > 0 && __any_sync(FULL, n0 > m0 || n1 > m1)) {
                     const float f0 = m0 > -CUDART_INF_F ? ex2_approx(m0 - n0) : 0.f, f1 = m1 > -CUDART_INF_F ? ex2_approx(m1 - n1) : 0.f;
                     l0 *= f0;
                     l1 *= f1;
@@ -534,9 +548,9 @@ __global__ void __launch_bounds__(JT, 6) attend_join_kernel(const AttendParams p
                     ldsm4t(v_at + chunk_at<DP>((lane & 7) + ((lane >> 4) << 3), 2 * j + ((lane >> 3) & 1)), vf);
                     mma16<T>(o[j], vf, p0, p1);
                 }
-                __syncwarp();
-                if (blk + 1 < end) load_block(blk + 1);
             }
+            __syncwarp();
+            o_sm = reinterpret_cast<float*>(own + ((step - 1) & 1) * 2 * S::BLOCK_BYTES);
 #pragma unroll
             for (int x = 4; x < 32; x <<= 1) {
                 l0 += __shfl_xor_sync(FULL, l0, x);
@@ -556,39 +570,58 @@ __global__ void __launch_bounds__(JT, 6) attend_join_kernel(const AttendParams p
             }
             __syncwarp();
         }
-        // the parts, in order: the group's items, then the row's own, then what was just added up
-        for (int i = lane; i < heads * (DP / 4); i += 32) {
-            const int h = i / (DP / 4), d = i % (DP / 4) * 4;
-            if (d >= p.D) continue;
-            const int64_t g_at = int64_t(gp.x) + int64_t(head) * group_rows * G + k_row * G + g0 + h, g_step = int64_t(p.kv_heads) * group_rows * G;
-            const int64_t r_at = int64_t(rp.x) + int64_t(head) * G + g0 + h, r_step = int64_t(p.kv_heads) * G;
-            float m = -CUDART_INF_F, total = 0.f;
-            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        // the parts, in order: the group's items, then the row's own, then what was just added up.  A lane takes 4 values of
+        // up to four heads at a time, so that their loads are in flight together.
+        constexpr int AT_ONCE = 4;
+        const int64_t g_at = int64_t(gp.x) + int64_t(head) * group_rows * G + k_row * G + g0, g_step = int64_t(p.kv_heads) * group_rows * G;
+        const int64_t r_at = int64_t(rp.x) + int64_t(head) * G + g0, r_step = int64_t(p.kv_heads) * G;
+        for (int i0 = lane; i0 < heads * (DP / 4); i0 += 32 * AT_ONCE) {
+            float m[AT_ONCE], total[AT_ONCE];
+            float4 x[AT_ONCE];
+            int h[AT_ONCE];
+            bool some[AT_ONCE];
+            const int d = i0 % (DP / 4) * 4;           // the same for all of a lane's heads: 32 is a multiple of DP / 4, or the other way round
+#pragma unroll
+            for (int a = 0; a < AT_ONCE; ++a) {
+                h[a] = (i0 + 32 * a) / (DP / 4);
+                some[a] = h[a] < heads && d < p.D;
+                m[a] = -CUDART_INF_F;
+                total[a] = 0.f;
+                x[a] = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            auto add = [&](int a, float lse, float weight, const float4& y) {
+                const float n = fmaxf(m[a], lse);
+                const float f = m[a] > -CUDART_INF_F ? ex2_approx(m[a] - n) : 0.f, w = lse == -CUDART_INF_F ? 0.f : ex2_approx(lse - n);
+                m[a] = n;
+                total[a] = fmaf(total[a], f, w * weight);
+                x[a] = make_float4(fmaf(w, y.x, x[a].x * f), fmaf(w, y.y, x[a].y * f), fmaf(w, y.z, x[a].z * f), fmaf(w, y.w, x[a].w * f));
+            };
             auto take = [&](int64_t at) {
-                const float lse = p.plan.part_lse[at];
-                const float4 y = *reinterpret_cast<const float4*>(p.plan.part + at * p.D + d);
-                const float n = fmaxf(m, lse);
-                const float f = m > -CUDART_INF_F ? ex2_approx(m - n) : 0.f, w = lse == -CUDART_INF_F ? 0.f : ex2_approx(lse - n);
-                m = n;
-                total = fmaf(total, f, w);
-                x = make_float4(fmaf(w, y.x, x.x * f), fmaf(w, y.y, x.y * f), fmaf(w, y.z, x.z * f), fmaf(w, y.w, x.w * f));
+                float lse[AT_ONCE];
+                float4 y[AT_ONCE];
+#pragma unroll
+                for (int a = 0; a < AT_ONCE; ++a) {
+                    lse[a] = some[a] ? p.plan.part_lse[at + h[a]] : -CUDART_INF_F;
+                    y[a] = some[a] ? *reinterpret_cast<const float4*>(p.plan.part + (at + h[a]) * p.D + d) : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+#pragma unroll
+                for (int a = 0; a < AT_ONCE; ++a) add(a, lse[a], 1.f, y[a]);
             };
             for (int s = 0; s < gp.y; ++s) take(g_at + s * g_step);
             for (int s = 0; s < rp.y; ++s) take(r_at + s * r_step);
-            if (begin < end) {
-                const float mt = ml_sm[h], lt = ml_sm[8 + h];
-                const float4 y = *reinterpret_cast<const float4*>(o_sm + h * S::O_LD + d);
-                const float n = fmaxf(m, mt);
-                const float f = m > -CUDART_INF_F ? ex2_approx(m - n) : 0.f, w = mt > -CUDART_INF_F ? ex2_approx(mt - n) : (lt == 0.f ? 0.f : lt);
-                m = n;
-                total = fmaf(total, f, w * lt);
-                x = make_float4(fmaf(w, y.x, x.x * f), fmaf(w, y.y, x.y * f), fmaf(w, y.z, x.z * f), fmaf(w, y.w, x.w * f));
+#pragma unroll
+            for (int a = 0; a < AT_ONCE; ++a) {
+                if (!some[a]) continue;
+                if (left > 0) {
+                    const float mt = ml_sm[h[a]], lt = ml_sm[8 + h[a]];
+                    if (mt > -CUDART_INF_F || lt != lt) add(a, mt > -CUDART_INF_F ? mt : 0.f, lt, *reinterpret_cast<const float4*>(o_sm + h[a] * S::O_LD + d));
+                }
+                const float inv = total[a] > 0.f ? 1.f / total[a] : (total[a] == 0.f ? 0.f : total[a]);
+                *reinterpret_cast<uint2*>(p.out + ((out_at + g0 + h[a]) * p.D + d) * 2) =
+                    make_uint2(pack2<T>(x[a].x * inv, x[a].y * inv), pack2<T>(x[a].z * inv, x[a].w * inv));
+                if (d == 0 && p.lse) p.lse[out_at + g0 + h[a]] = total[a] > 0.f ? (m[a] + log2f(total[a])) * LN2_F : (total[a] == 0.f ? -CUDART_INF_F : total[a]);
             }
-            const float inv = total > 0.f ? 1.f / total : (total == 0.f ? 0.f : total);
-            *reinterpret_cast<uint2*>(p.out + ((out_at + g0 + h) * p.D + d) * 2) = make_uint2(pack2<T>(x.x * inv, x.y * inv), pack2<T>(x.z * inv, x.w * inv));
-            if (d == 0 && p.lse) p.lse[out_at + g0 + h] = total > 0.f ? (m + log2f(total)) * LN2_F : (total == 0.f ? -CUDART_INF_F : total);
         }
-        __syncwarp();                                  // the sums have been read before the next heads' block comes in
     }
 }
 
@@ -600,8 +633,12 @@ int launch_groups(const AttendParams& a, const CUtensorMap& q, const CUtensorMap
     attend_group_kernel<T, DP><<<grid, THREADS, Shape<DP>::SMEM, st>>>(q, k, v, p);
     DISC_CUDA(cudaGetLastError());
     if (const int rc = allow_smem(attend_join_kernel<T, DP>, join_bytes, done2)) return rc;
-    const int64_t jobs = int64_t(a.rows) * a.kv_heads;
-    attend_join_kernel<T, DP><<<unsigned((jobs + JT / 32 - 1) / (JT / 32)), JT, join_bytes, st>>>(a);
+    int sms = 0;
+    if (const int rc = device_sms(&sms)) return rc;
+    const int64_t places = int64_t(sms) * 3 * (JT / 32), units = int64_t(a.rows) * a.kv_heads;
+    const int heads_per_job = int(units / places < 1 ? 1 : units / places > a.kv_heads ? a.kv_heads : units / places);
+    const int64_t jobs = int64_t(a.rows) * ((a.kv_heads + heads_per_job - 1) / heads_per_job);
+    attend_join_kernel<T, DP><<<unsigned((jobs + JT / 32 - 1) / (JT / 32)), JT, join_bytes, st>>>(a, heads_per_job);
     DISC_CUDA(cudaGetLastError());
     return DISC_OK;
 }
