@@ -15,9 +15,9 @@
 //
 // Plan (one cluster of 8 blocks): per group the number of leading pages its rows share, and the stream as a
 // list of blocks of 16 tokens (page, block in the page, tokens in it, owner); from the lengths of
-// the lists the items: runs of blocks, about as many as there are places for them on the device.
+// the lists the items: every block of threads that runs at a time gets an equal share of all blocks.
 //
-// Attention: a block of 4 warps per item and key head; blocks of 16 tokens come in through cp.async, three
+// Attention: a block of 4 warps per share and key head; blocks of 16 tokens come in through cp.async, three
 // tiles of 64 tokens deep.  Every warp takes its own block of 16 tokens of a tile with all the rows, so that the
 // warps need no barrier in the loop; their results are joined at the end.
 // Running maximum and sum per row in fp32, in units of log2.  An item that is not its group's only one
@@ -103,25 +103,36 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(PT) attend_pla
     cluster_sync_all();
     if (blockIdx.x != 0) return;
 
-    // one block: how long an item is, and the items
+    // one block: how long a lane's share is, and the items
     int32_t sum = 0;
     for (int32_t g = tid; g < sh.groups; g += PT) sum += p.plan.count[g];
     sum = warp_incl_scan(sum, lane);
     if (lane == 31) warp_sums[warp][0] = sum;
+    for (int32_t i = tid; i <= sh.lanes; i += PT) p.plan.first[i] = 0x7fffffff;
     __syncthreads();
     int64_t all = 0;
     for (int w = 0; w < PT / 32; ++w) all += warp_sums[w][0];
     __syncthreads();
-    int32_t len = int32_t((all + sh.aim - 1) / sh.aim);
-    len = max(TILE_BLKS, (len + TILE_BLKS - 1) / TILE_BLKS * TILE_BLKS);
+    const int32_t share = max(TILE_BLKS, int32_t((all + sh.lanes - 1) / sh.lanes + TILE_BLKS - 1) / TILE_BLKS * TILE_BLKS);
+    const int32_t lanes = max(1, int32_t((all + share - 1) / share));
     int32_t items = 0, slots = 0;
+    int64_t blocks = 0;
     for (int32_t g0 = 0; g0 < sh.groups; g0 += PT) {
         const int32_t g = g0 + tid;
         const int32_t n = g < sh.groups ? p.plan.count[g] : 0;
-        const int32_t splits = g < sh.groups ? max(1, (n + len - 1) / len) : 0;
+        const int32_t bs = warp_incl_scan(n, lane);
+        __syncthreads();
+        if (lane == 31) warp_sums[warp][0] = bs;
+        __syncthreads();
+        int64_t at = blocks + bs - n;
+        for (int w = 0; w < PT / 32; ++w) {
+            if (w < warp) at += warp_sums[w][0];
+            blocks += warp_sums[w][0];
+        }
+        const Cut cut = cut_group(at, n, share);
+        const int32_t splits = g < sh.groups ? max(1, cut.splits) : 0;         // an empty group is an item too: its rows get zeros
         const int32_t own_slots = splits > 1 ? splits : 0;
         const int32_t is = warp_incl_scan(splits, lane), ss = warp_incl_scan(own_slots, lane);
-        __syncthreads();
         if (lane == 31) { warp_sums[warp][1] = is; warp_sums[warp][2] = ss; }
         __syncthreads();
         int32_t i0 = items + is - splits, s0 = slots + ss - own_slots;
@@ -134,10 +145,17 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(PT) attend_pla
             p.plan.splits[g] = splits;
             p.plan.slot[g] = splits > 1 ? s0 : -1;
             for (int32_t h = 0; h < p.kv_heads; ++h) p.plan.arrived[int64_t(g) * p.kv_heads + h] = 0;
-            for (int32_t i = 0; i < splits; ++i) p.plan.items[i0 + i] = make_int4(g, i * len, min(n, (i + 1) * len), i);
+            for (int32_t i = 0; i < splits; ++i) {
+                const int64_t border = int64_t(cut.from + i) * share;
+                const int32_t begin = int32_t(max(at, border) - at), end = int32_t(min(at + n, border + share) - at);
+                p.plan.items[i0 + i] = make_int4(g, begin, end, i);
+                // the first item of a lane begins at its border
+                if ((at + begin) % share == 0 && cut.from + i < lanes) atomicMin(p.plan.first + cut.from + i, i0 + i);
+            }
         }
     }
-    if (tid == 0) { p.plan.head[0] = 0; p.plan.head[1] = items; }
+    __syncthreads();
+    if (tid == 0) { p.plan.first[0] = 0; p.plan.first[lanes] = items; p.plan.head[0] = 0; p.plan.head[1] = lanes; }
 }
 
 // ---- attention --------------------------------------------------------------------------------------
@@ -219,13 +237,16 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const PlanShape& sh = p.shape;
     const int G = sh.G;
-    const int n_units = p.plan.head[1] * p.kv_heads;
+    // this block's lane and key head
+    const int lane_of = blockIdx.x / p.kv_heads, head = blockIdx.x % p.kv_heads;
+    if (lane_of >= p.plan.head[1]) return;
+    const int item_end = p.plan.first[lane_of + 1];
     const int row_lo = lane >> 2;                                  // this thread's two rows of the tile: row_lo, row_lo + 8
     const int own_lo = row_lo / G + 1, own_hi = (row_lo + 8) / G + 1;
 
-    for (int unit = blockIdx.x; unit < n_units; unit += gridDim.x) {
-        const int4 item = p.plan.items[unit / p.kv_heads];
-        const int head = unit % p.kv_heads, g = item.x;
+    for (int n = p.plan.first[lane_of]; n < item_end; ++n) {
+        const int4 item = p.plan.items[n];
+        const int g = item.x;
         const int32_t r0 = g / sh.sub * sh.group + g % sh.sub * sh.per_group;
         const int32_t n_rows = max(0, min(p.rows, min(r0 + sh.per_group, g / sh.sub * sh.group + sh.group)) - r0);
         const int M = n_rows * G;
@@ -234,11 +255,13 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
         const int64_t head_bytes = int64_t(p.page_size) * p.D * 2;
 
         __syncthreads();                                           // the unit before is done with the shared memory
-        // a warp brings in block `warp` of a tile
-        auto load_tile = [&](int t) {
-            const int stage = t % STAGES;
+        // a warp brings in block `warp` of a tile; which one that is has been read a tile earlier
+        auto entry = [&](int t) {
             const int i = item.y + t * TILE_BLKS + warp;
-            const int2 e = i < item.z ? __ldg(list + i) : make_int2(0, 0);
+            return i < item.z ? __ldg(list + i) : make_int2(0, 0);
+        };
+        auto load_tile = [&](int t, int2 e) {
+            const int stage = t % STAGES;
             const int tokens = (e.y >> 8) & 255;
             const int64_t off = (int64_t(e.x) * p.kv_heads + head) * head_bytes + int64_t(e.y & 255) * (BLK * 2) * p.D;
             const uint32_t kd = smem_u32(smem + stage * 2 * S::TILE_BYTES), vd = kd + S::TILE_BYTES;
@@ -253,11 +276,15 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
             }
             if (lane == 0) meta[stage * TILE_BLKS + warp] = e.y >> 8;
         };
+        int2 first[STAGES];
+#pragma unroll
+        for (int t = 0; t < STAGES; ++t) first[t] = entry(t);
 #pragma unroll
         for (int t = 0; t < STAGES - 1; ++t) {
-            if (t < n_tiles) load_tile(t);
+            if (t < n_tiles) load_tile(t, first[t]);
             cp_commit();
         }
+        int2 next = first[STAGES - 1];
         // query vectors: row m of the tile is row m / G, head m % G of the group's heads
         for (int i = tid; i < 16 * CH; i += AT) {
             const int m = i / CH, ch = i % CH;
@@ -280,8 +307,9 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
         for (int t = 0; t < n_tiles; ++t) {
             cp_wait<STAGES - 2>();
             __syncwarp();                                          // a warp works on what it has brought in itself
-            if (t + STAGES - 1 < n_tiles) load_tile(t + STAGES - 1);
+            if (t + STAGES - 1 < n_tiles) load_tile(t + STAGES - 1, next);
             cp_commit();
+            next = entry(t + STAGES);
             const int stage = t % STAGES;
             const uint32_t kt = smem_u32(smem + stage * 2 * S::TILE_BYTES), vt = kt + S::TILE_BYTES;
             float s[2][4];
@@ -521,10 +549,7 @@ int disc_attend_cached(const disc_cache_t* c, int32_t layer, const void* q, int6
     p.error = reinterpret_cast<uint32_t*>(p.plan.head);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (p.shape.M > ROWS_M) return disc::attend_groups(p, c->dtype, n_q_heads, st);
-    int sms = 0;
-    if (const int rc = device_sms(&sms)) return rc;
-    const int64_t most = int64_t(p.shape.max_items) * c->n_kv_heads;
-    const unsigned grid = unsigned(most < 2 * sms ? most : 2 * sms);
+    const unsigned grid = unsigned(p.shape.lanes * c->n_kv_heads);
     return c->dtype == DISC_BF16 ? launch_attend<__nv_bfloat16>(p, grid, st) : launch_attend<__half>(p, grid, st);
 }
 

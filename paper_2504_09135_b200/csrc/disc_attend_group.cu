@@ -8,7 +8,7 @@
 //   1. A group's rows x query heads, up to 128, are one tile of query vectors.  The blocks of 16 tokens that all
 //      the rows hold in full go through the tensor cores as in the attention over prompts: S = Q K^T, a thread
 //      per query vector for the softmax, O += P V.  A row that has more than 8 full blocks of its own after those
-//      gets items of its own.  Long runs are cut.  Every item leaves normalised sums and log-sum-exps in fp32.
+//      gets items of its own.  The whole is cut into equal shares.  Every item leaves normalised sums and log-sum-exps in fp32.
 //   2. A warp per row and key head joins them, in order, with what is left of the row: up to 8 full blocks of its own
 //      and the partly filled one, by mma.sync.  Here, where rows have nothing in common, no row's values come near
 //      another row's sums.
@@ -71,14 +71,38 @@ __global__ void __launch_bounds__(256) group_shared_kernel(const PlanParams p) {
     }
 }
 
-// One block: the items' length, and the items, groups first, then rows.
+// Exclusive sums over the block of two numbers; all: the whole sums.  Called by the whole block.
 constexpr int PT = 1024;
+__device__ __forceinline__ int2 block_sums(int32_t a, int32_t b, int2 (*sums), int2* all) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int32_t ia = a, ib = b;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int32_t ua = __shfl_up_sync(FULL, ia, o), ub = __shfl_up_sync(FULL, ib, o);
+        if (lane >= o) { ia += ua; ib += ub; }
+    }
+    __syncthreads();
+    if (lane == 31) sums[warp] = make_int2(ia, ib);
+    __syncthreads();
+    int2 w = sums[lane];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int32_t ua = __shfl_up_sync(FULL, w.x, o), ub = __shfl_up_sync(FULL, w.y, o);
+        if (lane >= o) { w.x += ua; w.y += ub; }
+    }
+    *all = make_int2(__shfl_sync(FULL, w.x, 31), __shfl_sync(FULL, w.y, 31));
+    const int32_t ba = __shfl_sync(FULL, w.x, max(warp - 1, 0)), bb = __shfl_sync(FULL, w.y, max(warp - 1, 0));
+    return make_int2(ia - a + (warp ? ba : 0), ib - b + (warp ? bb : 0));
+}
+
+// One block: a lane's share, and the items, groups first, then rows.
 __global__ void __launch_bounds__(PT) group_items_kernel(const PlanParams p) {
-    __shared__ int32_t sums[32][2];
+    __shared__ int2 sums[32];
     __shared__ unsigned long long s_all;
     const PlanShape& sh = p.shape;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31;
     if (tid == 0) s_all = 0ull;
+    for (int32_t i = tid; i <= sh.lanes; i += PT) p.plan.first[i] = 0x7fffffff;
     __syncthreads();
     unsigned long long mine = 0, alone = 0;
     for (int32_t g = tid; g < sh.groups; g += PT) mine += p.plan.shared[g];
@@ -90,15 +114,20 @@ __global__ void __launch_bounds__(PT) group_items_kernel(const PlanParams p) {
     if (lane == 0 && mine) atomicAdd(&s_all, mine);
     __syncthreads();
     const int64_t all = int64_t(s_all);
-    int32_t len = int32_t((all + sh.aim - 1) / sh.aim);
-    len = max(TILE_BLKS, (len + TILE_BLKS - 1) / TILE_BLKS * TILE_BLKS);
+    const int32_t share = max(TILE_BLKS, int32_t((all + sh.lanes - 1) / sh.lanes + TILE_BLKS - 1) / TILE_BLKS * TILE_BLKS);
+    const int32_t lanes = int32_t((all + share - 1) / share);
     int32_t items = 0, part = 0;
+    int64_t blocks = 0;
     for (int kind = 0; kind < 2; ++kind) {
         const int32_t n = kind == 0 ? sh.groups : p.rows;
         for (int32_t i0 = 0; i0 < n; i0 += PT) {
             const int32_t i = i0 + tid;
-            int32_t blks = 0, row = 0, rows = 1, begin = 0;
-            if (i < n && (kind == 0 || any_alone)) {
+            if (kind == 1 && !any_alone) {
+                if (i < n) p.plan.row_part[i] = make_int2(0, 0);
+                continue;
+            }
+            int32_t blks = 0, row = 0, rows = 1, first = 0;
+            if (i < n) {
                 if (kind == 0) {
                     blks = p.plan.shared[i];
                     row = i / sh.sub * sh.group + i % sh.sub * sh.per_group;
@@ -106,36 +135,29 @@ __global__ void __launch_bounds__(PT) group_items_kernel(const PlanParams p) {
                 } else {
                     blks = p.plan.alone[i];
                     row = i;
-                    if (blks) begin = p.plan.shared[i / sh.group * sh.sub + i % sh.group / sh.per_group];
+                    if (blks) first = p.plan.shared[i / sh.group * sh.sub + i % sh.group / sh.per_group];
                 }
             }
-            const int32_t splits = (blks + len - 1) / len, parts = splits * rows * sh.G * p.kv_heads;
-            int32_t a = splits, b = parts;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int32_t ua = __shfl_up_sync(FULL, a, o), ub = __shfl_up_sync(FULL, b, o);
-                if (lane >= o) { a += ua; b += ub; }
+            int2 total;
+            const int64_t at = blocks + block_sums(blks, 0, sums, &total).x;
+            blocks += total.x;
+            const Cut cut = cut_group(at, blks, share);
+            const int32_t parts = cut.splits * rows * sh.G * p.kv_heads;
+            const int2 before = block_sums(cut.splits, parts, sums, &total);
+            const int32_t item0 = items + before.x, part0 = part + before.y;
+            items += total.x;
+            part += total.y;
+            if (i < n) (kind == 0 ? p.plan.group_part : p.plan.row_part)[i] = make_int2(part0, cut.splits);
+            for (int32_t x = 0; x < cut.splits; ++x) {
+                const int64_t border = int64_t(cut.from + x) * share;
+                const int32_t begin = int32_t(max(at, border) - at), end = int32_t(min(at + blks, border + share) - at);
+                p.plan.group_items[item0 + x] = GroupItem{row, rows, first + begin, first + end, part0 + x * rows * sh.G * p.kv_heads, {0, 0, 0}};
+                if ((at + begin) % share == 0) p.plan.first[cut.from + x] = item0 + x;         // every lane has exactly one item at its border
             }
-            __syncthreads();
-            if (lane == 31) { sums[warp][0] = a; sums[warp][1] = b; }
-            __syncthreads();
-            int32_t wa = sums[lane][0], wb = sums[lane][1];
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int32_t ua = __shfl_up_sync(FULL, wa, o), ub = __shfl_up_sync(FULL, wb, o);
-                if (lane >= o) { wa += ua; wb += ub; }
-            }
-            const int32_t before_a = __shfl_sync(FULL, wa, max(warp - 1, 0)), before_b = __shfl_sync(FULL, wb, max(warp - 1, 0));
-            const int32_t item0 = items + a - splits + (warp ? before_a : 0), part0 = part + b - parts + (warp ? before_b : 0);
-            items += __shfl_sync(FULL, wa, 31);
-            part += __shfl_sync(FULL, wb, 31);
-            if (i < n) (kind == 0 ? p.plan.group_part : p.plan.row_part)[i] = make_int2(part0, splits);
-            for (int32_t x = 0; x < splits; ++x)
-                p.plan.group_items[item0 + x] =
-                    GroupItem{row, rows, begin + x * len, begin + min(blks, (x + 1) * len), part0 + x * rows * sh.G * p.kv_heads, {0, 0, 0}};
         }
     }
-    if (tid == 0) { p.plan.head[0] = 0; p.plan.head[1] = items; }
+    __syncthreads();
+    if (tid == 0) { p.plan.first[lanes] = items; p.plan.head[0] = 0; p.plan.head[1] = lanes; }
 }
 
 // ---- kernel 1 -----------------------------------------------------------------------------------------
@@ -196,17 +218,19 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     tc_fence_after();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&tmem_slot);
 
-    const int n_units = p.plan.head[1] * p.kv_heads;               // neighbouring units: the key heads of an item
-    const int step = int(gridDim.x);
+    // this block's lane and key head
+    const int lane_of = blockIdx.x / p.kv_heads, head = blockIdx.x % p.kv_heads;
+    const bool some = lane_of < p.plan.head[1];
+    const int item0 = some ? p.plan.first[lane_of] : 0, item1 = some ? p.plan.first[lane_of + 1] : 0;
 
     if (warp >= 4) {
         if (warp == 4) {
             // ---- loads
             int load = 0, n = 0;
             bool ok = true;
-            for (int unit = blockIdx.x; unit < n_units && ok; unit += step, ++n) {
-                const GroupItem* it = p.plan.group_items + unit / p.kv_heads;
-                const int head = unit % p.kv_heads, row = it->row, begin = it->begin, blks = it->end - begin;
+            for (; item0 + n < item1 && ok; ++n) {
+                const GroupItem* it = p.plan.group_items + item0 + n;
+                const int row = it->row, begin = it->begin, blks = it->end - begin;
                 const int32_t* table = p.table + int64_t(row) * p.width;
                 if (n > 0) ok = mbar_wait_all(q_empty, (n - 1) & 1, abort);
                 if (ok && lane == 0) {
@@ -247,8 +271,8 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
             };
             int load = 0, n = 0, tile = 0;
             bool ok = true;
-            for (int unit = blockIdx.x; unit < n_units && ok; unit += step, ++n) {
-                const GroupItem* it = p.plan.group_items + unit / p.kv_heads;
+            for (; item0 + n < item1 && ok; ++n) {
+                const GroupItem* it = p.plan.group_items + item0 + n;
                 const int blks = it->end - it->begin;
                 ok = mbar_wait_all(q_full, n & 1, abort) && mbar_wait_all(kv_full + load % S::STAGES, (load / S::STAGES) & 1, abort);
                 if (!ok) break;
@@ -306,8 +330,8 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         const float2 c2 = make_float2(p.c2, p.c2);
         int tile = 0, n = 0;
         bool ok = true;
-        for (int unit = blockIdx.x; unit < n_units && ok; unit += step, ++n) {
-            const GroupItem* it = p.plan.group_items + unit / p.kv_heads;
+        for (; item0 + n < item1 && ok; ++n) {
+            const GroupItem* it = p.plan.group_items + item0 + n;
             const int blks = it->end - it->begin;
             float ref = -CUDART_INF_F;
             float2 l = make_float2(0.f, 0.f);
@@ -348,7 +372,7 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
             const float total = bad ? CUDART_NAN_F : l.x + l.y;
             const float inv = total > 0.f ? 1.f / total : (total == 0.f ? 0.f : total);
             const int rows = it->rows * p.G;
-            const int64_t at = int64_t(it->part) + (unit % p.kv_heads) * rows + m;
+            const int64_t at = int64_t(it->part) + head * rows + m;
             float* dst = p.plan.part + at * p.D;
 #pragma unroll 1
             for (int c = 0; c < DP; c += 32) {
@@ -456,11 +480,16 @@ __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p
     const int eights = (G + 7) / 8;                    // a key head's query heads, eight at a time
     const int steps = (head1 - head0) * eights * left;
 
-    // step: block step % left of the (step / left)-th eight of query heads
+    // step: block step % left of the (step / left)-th eight of query heads; a row's pages are the same for all heads, a lane
+    // holds the page of one of its blocks (there are at most 9)
+    const int my_page = lane < left ? table[(begin + lane) / sh.blks_per_page] : 0;
+    static_assert(MAX_TAIL < 32, "a lane per block");
+    int load_unit = 0, load_blk = 0;                   // of the next step to be loaded
     auto load_step = [&](int step) {
         if (step < steps) {
-            const int head = head0 + step / left / eights, blk = begin + step % left;
-            const int page = table[blk / sh.blks_per_page], tokens = min(BLK, len - blk * BLK);
+            const int head = head0 + load_unit / eights, blk = begin + load_blk;
+            const int page = __shfl_sync(FULL, my_page, load_blk), tokens = min(BLK, len - blk * BLK);
+            if (++load_blk == left) { load_blk = 0; ++load_unit; }
             const int64_t off = (int64_t(page) * p.kv_heads + head) * head_bytes + int64_t(blk % sh.blks_per_page) * (BLK * 2) * p.D;
             const uint32_t k_at = smem_u32(own) + (step & 1) * 2 * S::BLOCK_BYTES;
 #pragma unroll
@@ -684,10 +713,7 @@ int disc::attend_groups(const AttendParams& a, int32_t dtype, int32_t n_q_heads,
     const cuuint32_t box[2] = {cuuint32_t(BOX), cuuint32_t(BLK)};
     if (const int rc = encode(enc, &map_k, type, 2, a.k, dims, strides, box)) return rc;
     if (const int rc = encode(enc, &map_v, type, 2, a.v, dims, strides, box)) return rc;
-    int sms = 0;
-    if (const int rc = device_sms(&sms)) return rc;
-    const int64_t most = int64_t(a.shape.max_items) * a.kv_heads;
-    const unsigned grid = unsigned(most < 2 * sms ? most : 2 * sms);
+    const unsigned grid = unsigned(a.shape.lanes * a.kv_heads);
     if (dtype == DISC_BF16)
         return DP == 64 ? launch_groups<__nv_bfloat16, 64>(a, map_q, map_k, map_v, p, grid, st) : launch_groups<__nv_bfloat16, 128>(a, map_q, map_k, map_v, p, grid, st);
     return DP == 64 ? launch_groups<__half, 64>(a, map_q, map_k, map_v, p, grid, st) : launch_groups<__half, 128>(a, map_q, map_k, map_v, p, grid, st);
