@@ -69,6 +69,10 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(PT) attend_pla
         const int32_t r1 = min(p.rows, min(r0 + sh.per_group, g / sh.sub * sh.group + sh.group));
         int2* list = p.plan.list + int64_t(g) * sh.list_ld;
         const int32_t n = r1 - r0;
+        if (sh.per_group == 1) {
+            if (lane == 0) p.plan.count[g] = (p.len[r0] + BLK - 1) / BLK;
+            continue;
+        }
         int32_t shared = 0;
         if (n > 1) {
             int32_t full = 0x7fffffff;
@@ -110,13 +114,13 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(PT) attend_pla
     if (lane == 31) warp_sums[warp][0] = sum;
     for (int32_t i = tid; i <= sh.lanes; i += PT) p.plan.first[i] = 0x7fffffff;
     __syncthreads();
-    int64_t all = 0;
+    int32_t all = 0;
     for (int w = 0; w < PT / 32; ++w) all += warp_sums[w][0];
     __syncthreads();
-    const int32_t share = max(TILE_BLKS, int32_t((all + sh.lanes - 1) / sh.lanes + TILE_BLKS - 1) / TILE_BLKS * TILE_BLKS);
-    const int32_t lanes = max(1, int32_t((all + share - 1) / share));
+    const int32_t share = max(TILE_BLKS, ((all - 1) / sh.lanes + TILE_BLKS) / TILE_BLKS * TILE_BLKS);
+    const int32_t lanes = max(1, all / share + (all % share > 0));
     int32_t items = 0, slots = 0;
-    int64_t blocks = 0;
+    int32_t blocks = 0;
     for (int32_t g0 = 0; g0 < sh.groups; g0 += PT) {
         const int32_t g = g0 + tid;
         const int32_t n = g < sh.groups ? p.plan.count[g] : 0;
@@ -124,7 +128,7 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(PT) attend_pla
         __syncthreads();
         if (lane == 31) warp_sums[warp][0] = bs;
         __syncthreads();
-        int64_t at = blocks + bs - n;
+        int32_t at = blocks + bs - n;
         for (int w = 0; w < PT / 32; ++w) {
             if (w < warp) at += warp_sums[w][0];
             blocks += warp_sums[w][0];
@@ -146,11 +150,10 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(PT) attend_pla
             p.plan.slot[g] = splits > 1 ? s0 : -1;
             for (int32_t h = 0; h < p.kv_heads; ++h) p.plan.arrived[int64_t(g) * p.kv_heads + h] = 0;
             for (int32_t i = 0; i < splits; ++i) {
-                const int64_t border = int64_t(cut.from + i) * share;
-                const int32_t begin = int32_t(max(at, border) - at), end = int32_t(min(at + n, border + share) - at);
-                p.plan.items[i0 + i] = make_int4(g, begin, end, i);
+                const int32_t border = (cut.from + i) * share - at;            // from the group's first block
+                p.plan.items[i0 + i] = make_int4(g, max(0, border), min(n, border + share), i);
                 // the first item of a lane begins at its border
-                if ((at + begin) % share == 0 && cut.from + i < lanes) atomicMin(p.plan.first + cut.from + i, i0 + i);
+                if (border >= 0 && cut.from + i < lanes) atomicMin(p.plan.first + cut.from + i, i0 + i);
             }
         }
     }
@@ -251,6 +254,8 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
         const int32_t n_rows = max(0, min(p.rows, min(r0 + sh.per_group, g / sh.sub * sh.group + sh.group)) - r0);
         const int M = n_rows * G;
         const int2* list = p.plan.list + int64_t(g) * sh.list_ld;
+        const int32_t* table = p.table + int64_t(r0) * p.width;
+        const int32_t len = p.len[r0];
         const int n_tiles = (item.z - item.y + TILE_BLKS - 1) / TILE_BLKS;
         const int64_t head_bytes = int64_t(p.page_size) * p.D * 2;
 
@@ -258,7 +263,9 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
         // a warp brings in block `warp` of a tile; which one that is has been read a tile earlier
         auto entry = [&](int t) {
             const int i = item.y + t * TILE_BLKS + warp;
-            return i < item.z ? __ldg(list + i) : make_int2(0, 0);
+            if (i >= item.z) return make_int2(0, 0);
+            if (sh.per_group > 1) return __ldg(list + i);
+            return make_int2(__ldg(table + i / sh.blks_per_page), i % sh.blks_per_page | min(BLK, len - i * BLK) << 8);
         };
         auto load_tile = [&](int t, int2 e) {
             const int stage = t % STAGES;

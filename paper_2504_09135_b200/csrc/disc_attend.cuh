@@ -62,10 +62,13 @@ inline int plan_shape(const disc_cache_t* c, int32_t hq, int32_t group, PlanShap
     s->groups = int32_t(groups);
     s->M = s->per_group * s->G;
     s->blks_per_page = c->page_size / BLK;
+    // blocks are counted in 32 bits
+    if (int64_t(c->n_rows) * c->table_width * s->blks_per_page >= (int64_t(1) << 31)) return DISC_ERR_UNSUPPORTED;
     s->lanes = PLACES / c->n_kv_heads > 1 ? PLACES / c->n_kv_heads : 1;
     // every border between two lanes makes one item two
     if (s->M <= ROWS_M) {
-        s->list_ld = int64_t(s->per_group) * c->table_width * s->blks_per_page;
+        // a row alone: its blocks are found through the table
+        s->list_ld = s->per_group == 1 ? 0 : int64_t(s->per_group) * c->table_width * s->blks_per_page;
         s->max_items = s->groups + s->lanes;
         s->max_part = int64_t(2 * s->lanes) * c->n_kv_heads * s->M;
     } else {
@@ -113,9 +116,9 @@ inline int64_t plan_layout(const disc_cache_t* c, const PlanShape& s, void* base
 struct Cut {
     int32_t from, splits;              // lane of the first item; items
 };
-__host__ __device__ inline Cut cut_group(int64_t at, int32_t blocks, int32_t share) {
-    const int32_t from = int32_t(at / share);
-    return {from, blocks > 0 ? int32_t((at + blocks - 1) / share) - from + 1 : 0};
+__host__ __device__ inline Cut cut_group(int32_t at, int32_t blocks, int32_t share) {
+    const int32_t from = at / share;
+    return {from, blocks > 0 ? (at + blocks - 1) / share - from + 1 : 0};
 }
 
 struct PlanParams {

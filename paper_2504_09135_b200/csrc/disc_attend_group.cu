@@ -98,13 +98,13 @@ __device__ __forceinline__ int2 block_sums(int32_t a, int32_t b, int2 (*sums), i
 // One block: a lane's share, and the items, groups first, then rows.
 __global__ void __launch_bounds__(PT) group_items_kernel(const PlanParams p) {
     __shared__ int2 sums[32];
-    __shared__ unsigned long long s_all;
+    __shared__ int32_t s_all;
     const PlanShape& sh = p.shape;
     const int tid = threadIdx.x, lane = tid & 31;
-    if (tid == 0) s_all = 0ull;
+    if (tid == 0) s_all = 0;
     for (int32_t i = tid; i <= sh.lanes; i += PT) p.plan.first[i] = 0x7fffffff;
     __syncthreads();
-    unsigned long long mine = 0, alone = 0;
+    int32_t mine = 0, alone = 0;
     for (int32_t g = tid; g < sh.groups; g += PT) mine += p.plan.shared[g];
     for (int32_t r = tid; r < p.rows; r += PT) alone += p.plan.alone[r];
     mine += alone;
@@ -113,11 +113,10 @@ __global__ void __launch_bounds__(PT) group_items_kernel(const PlanParams p) {
     for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(FULL, mine, o);
     if (lane == 0 && mine) atomicAdd(&s_all, mine);
     __syncthreads();
-    const int64_t all = int64_t(s_all);
-    const int32_t share = max(TILE_BLKS, int32_t((all + sh.lanes - 1) / sh.lanes + TILE_BLKS - 1) / TILE_BLKS * TILE_BLKS);
-    const int32_t lanes = int32_t((all + share - 1) / share);
-    int32_t items = 0, part = 0;
-    int64_t blocks = 0;
+    const int32_t all = s_all;
+    const int32_t share = max(TILE_BLKS, ((all - 1) / sh.lanes + TILE_BLKS) / TILE_BLKS * TILE_BLKS);
+    const int32_t lanes = all / share + (all % share > 0);
+    int32_t items = 0, part = 0, blocks = 0;
     for (int kind = 0; kind < 2; ++kind) {
         const int32_t n = kind == 0 ? sh.groups : p.rows;
         for (int32_t i0 = 0; i0 < n; i0 += PT) {
@@ -139,7 +138,7 @@ __global__ void __launch_bounds__(PT) group_items_kernel(const PlanParams p) {
                 }
             }
             int2 total;
-            const int64_t at = blocks + block_sums(blks, 0, sums, &total).x;
+            const int32_t at = blocks + block_sums(blks, 0, sums, &total).x;
             blocks += total.x;
             const Cut cut = cut_group(at, blks, share);
             const int32_t parts = cut.splits * rows * sh.G * p.kv_heads;
@@ -149,10 +148,9 @@ __global__ void __launch_bounds__(PT) group_items_kernel(const PlanParams p) {
             part += total.y;
             if (i < n) (kind == 0 ? p.plan.group_part : p.plan.row_part)[i] = make_int2(part0, cut.splits);
             for (int32_t x = 0; x < cut.splits; ++x) {
-                const int64_t border = int64_t(cut.from + x) * share;
-                const int32_t begin = int32_t(max(at, border) - at), end = int32_t(min(at + blks, border + share) - at);
+                const int32_t border = (cut.from + x) * share - at, begin = max(0, border), end = min(blks, border + share);
                 p.plan.group_items[item0 + x] = GroupItem{row, rows, first + begin, first + end, part0 + x * rows * sh.G * p.kv_heads, {0, 0, 0}};
-                if ((at + begin) % share == 0) p.plan.first[cut.from + x] = item0 + x;         // every lane has exactly one item at its border
+                if (border >= 0) p.plan.first[cut.from + x] = item0 + x;         // every lane has exactly one item at its border
             }
         }
     }
