@@ -105,7 +105,35 @@ __global__ void __launch_bounds__(256) cache_settle_kernel(Books b, const int32_
 }
 
 // ---- extend ------------------------------------------------------------------------------------------
+// The calls that decide by order, extend and compact, run as one cluster of 8 blocks: their steps hang on one another, and a
+// cluster's barrier costs less than a launch.  One block alone takes 38 us to extend 4096 rows over 27,000 pages, the
+// cluster 13, most of it waiting for one load after the other; but 16 rows over some hundred pages take 10 us in the
+// cluster and 6 in one block, which is what small caches get.
 constexpr int XT = 1024;
+constexpr int CLUSTER = 8;
+constexpr int ONE_BLOCK = 8192;        // up to this many pages (and XT rows): one block
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync_all() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ int32_t remote_int(const int32_t* p, uint32_t rank) {
+    uint32_t a;
+    int32_t v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(uint32_t(__cvta_generic_to_shared(p))), "r"(rank));
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+
+// the barrier of CL blocks
+template <int CL>
+__device__ __forceinline__ void sync_blocks() {
+    if (CL == 1) __syncthreads(); else cluster_sync_all();
+}
 
 // exclusive sum over the block of v; *total gets the whole sum.  Called by the whole block.
 __device__ __forceinline__ int32_t block_scan(int32_t v, int32_t* warp_sums, int32_t* total) {
@@ -119,22 +147,49 @@ __device__ __forceinline__ int32_t block_scan(int32_t v, int32_t* warp_sums, int
     __syncthreads();
     if (lane == 31) warp_sums[warp] = incl;
     __syncthreads();
-    if (warp == 0) {
-        int32_t w = warp_sums[lane];
+    int32_t w = warp_sums[lane];
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int32_t u = __shfl_up_sync(FULL, w, o);
-            if (lane >= o) w += u;
-        }
-        warp_sums[lane] = w;
+    for (int o = 1; o < 32; o <<= 1) {
+        const int32_t u = __shfl_up_sync(FULL, w, o);
+        if (lane >= o) w += u;
     }
-    __syncthreads();
-    *total = warp_sums[31];
-    return incl - v + (warp ? warp_sums[warp - 1] : 0);
+    *total = __shfl_sync(FULL, w, 31);
+    const int32_t before = __shfl_sync(FULL, w, max(warp - 1, 0));
+    return incl - v + (warp ? before : 0);
+}
+
+// The blocks' own numbers, one each, exchanged: the sum over the blocks before this one, and over all.  `mine` is shared
+// memory that stays as it is until the next barrier of the cluster.  Begins with a barrier of the cluster.
+template <int CL>
+__device__ __forceinline__ void cluster_sums(const int32_t* mine, uint32_t rank, int32_t* before, int32_t* all) {
+    sync_blocks<CL>();
+    int32_t b = 0, t = 0;
+#pragma unroll
+    for (uint32_t c = 0; c < CL; ++c) {
+        const int32_t v = CL == 1 ? *mine : remote_int(mine, c);
+        if (c < rank) b += v;
+        t += v;
+    }
+    *before = b;
+    *all = t;
+}
+
+// this block's share [a, b) of n things, in runs of 4
+template <int CL>
+__device__ __forceinline__ void share_of(int32_t n, uint32_t rank, int32_t* a, int32_t* b) {
+    const int32_t per = ((n + CL - 1) / CL + 3) & ~3;
+    *a = min(n, int32_t(rank) * per);
+    *b = min(n, *a + per);
+}
+// four consecutive reference counts from p (a multiple of 4); 1 beyond the last
+__device__ __forceinline__ int4 four_refs(const int32_t* ref, int32_t p, int32_t end) {
+    if (p + 4 <= end && (reinterpret_cast<uintptr_t>(ref) & 15) == 0) return *reinterpret_cast<const int4*>(ref + p);
+    return make_int4(p < end ? ref[p] : 1, p + 1 < end ? ref[p + 1] : 1, p + 2 < end ? ref[p + 2] : 1, p + 3 < end ? ref[p + 3] : 1);
 }
 
 struct Need {
-    int32_t add, len, first, last, page, copy, pages;      // table positions [first, last) are new; page: the partial last one or -1
+    int32_t add, len, first, last, page;                   // table positions [first, last) are new; page: the partial last one or -1
+    bool too_long;                                         // the table has no room for the row's pages
 };
 __device__ __forceinline__ Need row_need(const Books& b, const int32_t* add, int32_t row) {
     Need n;
@@ -142,119 +197,168 @@ __device__ __forceinline__ Need row_need(const Books& b, const int32_t* add, int
     n.len = b.len[row];
     n.first = (n.len + b.page_size - 1) >> b.shift;
     n.page = -1;
-    n.copy = 0;
     n.last = n.first;
-    if (n.add > 0) {
-        n.last = int32_t((int64_t(n.len) + n.add + b.page_size - 1) >> b.shift);
+    n.too_long = n.add > 0 && int64_t(n.len) + n.add > (int64_t(b.width) << b.shift);
+    if (n.add > 0 && !n.too_long) {
+        n.last = (n.len + n.add + b.page_size - 1) >> b.shift;
         if (n.len & (b.page_size - 1)) n.page = b.table[size_t(row) * b.width + n.first - 1];
     }
-    n.pages = n.last - n.first;
     return n;
 }
-// no room in the table for the row's pages
-__device__ __forceinline__ bool too_long(const Books& b, const Need& n) {
-    return int64_t(n.len) + n.add > (int64_t(b.width) << b.shift);
-}
 
-// One block: the arrays are small and every step hangs on the one before.
 //  1. Rows that go on writing into a partly filled page mark it: how many rows do (sharers), and the lowest of
 //     them (keeper).  If they are all the rows that hold the page, the keeper writes on in place; the others, and
 //     all of them where a row that stays behind holds the page too, get a copy.
 //  2. Prefix sums over the rows of the pages they need; rows beyond the number of free pages get nothing.
 //  3. The free pages of lowest id, in order, as many as are needed, and from them each row's share.
-__global__ void __launch_bounds__(XT) cache_extend_kernel(Books b, const int32_t* __restrict__ add, Scratch s, uint8_t* __restrict__ status) {
+// A thread has ROWS consecutive rows, in registers from the first step to the last, or, where there are more of them, reads
+// them again in every step.
+template <int CL, int ROWS>
+__global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(XT) cache_extend_kernel(Books b, const int32_t* __restrict__ add, Scratch s,
+                                                                                       uint8_t* __restrict__ status) {
     __shared__ int32_t warp_sums[32];
-    const int tid = threadIdx.x;
-    for (int32_t row = tid; row < b.rows; row += XT) {
-        const Need n = row_need(b, add, row);
-        if (n.page >= 0 && !too_long(b, n)) { s.sharers[n.page] = 0; s.keeper[n.page] = 0x7fffffff; }
-    }
-    __syncthreads();
-    for (int32_t row = tid; row < b.rows; row += XT) {
-        const Need n = row_need(b, add, row);
-        if (n.page >= 0 && !too_long(b, n)) { atomicAdd(s.sharers + n.page, 1); atomicMin(s.keeper + n.page, row); }
-    }
-    __syncthreads();
+    __shared__ int32_t own_need, own_free;
+    const int tid = threadIdx.x, lane = tid & 31;
+    const uint32_t rank = cluster_rank();
+    int32_t a0, a1;
+    share_of<CL>(b.rows, rank, &a0, &a1);
+    const int32_t per = ROWS ? ROWS : (a1 - a0 + XT - 1) / XT;
+    const int32_t r0 = min(a1, a0 + tid * per), n_rows = min(a1, r0 + per) - r0;
+    constexpr int HELD = ROWS ? ROWS : 1;
+    Need held[HELD];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i)
+        if (i < n_rows) held[i] = row_need(b, add, r0 + i);
+    // f(row's number, what it needs) for the thread's rows
+    auto each = [&](auto f) {
+        if (ROWS) {
+#pragma unroll
+            for (int i = 0; i < HELD; ++i)
+                if (i < n_rows) f(r0 + i, held[i]);
+        } else {
+            for (int32_t i = 0; i < n_rows; ++i) f(r0 + i, row_need(b, add, r0 + i));
+        }
+    };
+    each([&](int32_t, const Need& n) { if (n.page >= 0) { s.sharers[n.page] = 0; s.keeper[n.page] = 0x7fffffff; } });
+    if (rank == 0 && tid == 0) s.head[0] = 0;
 
-    // pages needed in all
+    // the free pages of this block's share
+    int32_t p0, p1, n_free = 0;
+    share_of<CL>(b.pages, rank, &p0, &p1);
     int32_t mine = 0;
-    const int32_t per = (b.rows + XT - 1) / XT;            // rows of a thread: consecutive
-    const int32_t r0 = min(b.rows, tid * per), r1 = min(b.rows, r0 + per);
+    for (int32_t p = p0 + tid * 4; p < p1; p += XT * 4) {
+        const int4 r = four_refs(b.ref, p, p1);
+        mine += (r.x == 0) + (r.y == 0) + (r.z == 0) + (r.w == 0);
+    }
+    block_scan(mine, warp_sums, &n_free);
+    if (tid == 0) own_free = n_free;
+
+    sync_blocks<CL>();
+    each([&](int32_t row, const Need& n) { if (n.page >= 0) { atomicAdd(s.sharers + n.page, 1); atomicMin(s.keeper + n.page, row); } });
+    sync_blocks<CL>();
+
     auto copies = [&](const Need& n, int32_t row) {
         if (n.page < 0) return 0;
         const int32_t ref = b.ref[n.page];
         if (ref <= 1) return 0;
         return s.sharers[n.page] == ref && s.keeper[n.page] == row ? 0 : 1;
     };
-    for (int32_t row = r0; row < r1; ++row) {
-        const Need n = row_need(b, add, row);
-        if (n.add > 0 && !too_long(b, n)) mine += n.pages + copies(n, row);
+    int32_t held_copy[HELD];
+    mine = 0;
+    if (ROWS) {
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) held_copy[i] = i < n_rows ? copies(held[i], r0 + i) : 0;
+#pragma unroll
+        for (int i = 0; i < HELD; ++i)
+            if (i < n_rows) mine += held[i].last - held[i].first + held_copy[i];
+    } else {
+        each([&](int32_t row, const Need& n) {
+            const int32_t cp = copies(n, row);
+            s.len[row] = cp;
+            mine += n.last - n.first + cp;
+        });
     }
-    int32_t needed = 0;
-    const int32_t before = block_scan(mine, warp_sums, &needed);
+    int32_t total = 0;
+    int32_t at = block_scan(mine, warp_sums, &total);
+    if (tid == 0) own_need = total;
+    int32_t before, needed, free_before, free_all;
+    cluster_sums<CL>(&own_need, rank, &before, &needed);
+    at += before;
+    free_before = 0;
+    free_all = 0;
+#pragma unroll
+    for (uint32_t c = 0; c < CL; ++c) {
+        const int32_t v = CL == 1 ? own_free : remote_int(&own_free, c);
+        if (c < rank) free_before += v;
+        free_all += v;
+    }
 
     // the free pages, lowest first, as far as they are needed
-    int32_t n_free = 0;
-    if (needed > 0) {
-        for (int32_t p0 = 0; p0 < b.pages && n_free < needed; p0 += XT * 4) {
-            int32_t mask = 0;
+    for (int32_t q = p0; q < p1 && free_before < needed; q += XT * 4) {
+        const int32_t p = q + tid * 4;
+        const int4 r = p < p1 ? four_refs(b.ref, p, p1) : make_int4(1, 1, 1, 1);
+        const int32_t mask = (r.x == 0) | (r.y == 0) << 1 | (r.z == 0) << 2 | (r.w == 0) << 3;
+        int32_t got = 0;
+        int32_t x = free_before + block_scan(__popc(mask), warp_sums, &got);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int32_t p = p0 + tid * 4 + j;
-                if (p < b.pages && b.ref[p] == 0) mask |= 1 << j;
+        for (int j = 0; j < 4; ++j)
+            if ((mask >> j) & 1) {
+                if (x < needed) s.list[x] = p + j;
+                ++x;
             }
-            int32_t got = 0;
-            int32_t at = n_free + block_scan(__popc(mask), warp_sums, &got);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if ((mask >> j) & 1) s.list[at++] = p0 + tid * 4 + j;
-            n_free += got;
-        }
+        free_before += got;
     }
-    if (tid == 0) s.head[0] = 0;
-    __syncthreads();
-
-    int32_t at = before, n_copy = 0;
-    // two rounds over the thread's rows: the decisions read the reference counts and marks, then the counts change
-    for (int32_t row = r0; row < r1; ++row) {
-        const Need n = row_need(b, add, row);
+    // every decision has been made on the counts as they were, the list is complete; then the counts change
+    sync_blocks<CL>();
+    auto settle = [&](int32_t row, const Need& n, int32_t cp) {
         uint8_t st = 0;
-        int32_t share = -1;                                // where the row's pages start in the list, + copy bit
+        bool copy = false;
+        int32_t to = 0;
         if (n.add > 0) {
-            if (too_long(b, n)) st = DISC_ROW_NOPAGE;
+            const int32_t pages = n.last - n.first + cp;
+            if (n.too_long || (pages > 0 && at + pages > free_all)) st = DISC_ROW_NOPAGE;
             else {
-                const int32_t cp = copies(n, row), pages = n.pages + cp;
-                if (pages > 0 && at + pages > n_free) st = DISC_ROW_NOPAGE;
-                else { share = at * 2 + cp; n_copy += cp; }
-                at += pages;
+                int32_t from = at;
+                int32_t* t = b.table + size_t(row) * b.width;
+                if (cp) {
+                    copy = true;
+                    to = s.list[from++];
+                    t[n.first - 1] = to;
+                    b.ref[to] = 1;
+                    atomicAdd(b.ref + n.page, -1);
+                }
+                for (int32_t j = n.first; j < n.last; ++j) {
+                    const int32_t page = s.list[from++];
+                    t[j] = page;
+                    b.ref[page] = 1;
+                }
+                b.len[row] = n.len + n.add;
             }
+            if (!n.too_long) at += pages;
         }
-        s.len[row] = share;
         status[row] = st;
-    }
-    int32_t all = 0;
-    int32_t slot = block_scan(n_copy, warp_sums, &all);
-    for (int32_t row = r0; row < r1; ++row) {
-        const int32_t share = s.len[row];
-        if (share < 0) continue;
-        const Need n = row_need(b, add, row);
-        int32_t from = share >> 1;
-        int32_t* t = b.table + size_t(row) * b.width;
-        if (share & 1) {
-            const int32_t to = s.list[from++];
-            s.copy[slot++] = make_int4(n.page, to, n.len & (b.page_size - 1), 0);
-            t[n.first - 1] = to;
-            b.ref[to] = 1;
-            atomicAdd(b.ref + n.page, -1);
+        // a place in the list of copies, whose order does not matter
+        const unsigned who = __activemask(), some = __ballot_sync(who, copy);
+        if (some) {
+            const int first = __ffs(some) - 1;
+            int32_t base = 0;
+            if (lane == first) base = atomicAdd(s.head, __popc(some));
+            base = __shfl_sync(who, base, first);
+            if (copy) s.copy[base + __popc(some & ((1u << lane) - 1u))] = make_int4(n.page, to, n.len & (b.page_size - 1), 0);
         }
-        for (int32_t j = n.first; j < n.last; ++j) {
-            const int32_t to = s.list[from++];
-            t[j] = to;
-            b.ref[to] = 1;
+    };
+    if (ROWS) {
+#pragma unroll
+        for (int i = 0; i < HELD; ++i)
+            if (i < n_rows) settle(r0 + i, held[i], held_copy[i]);
+    } else {
+        // the copies are decided by counts that other rows are changing: they were noted with the decision
+        for (int32_t i = 0; i < n_rows; ++i) {
+            const Need n = row_need(b, add, r0 + i);
+            settle(r0 + i, n, s.len[r0 + i]);
         }
-        b.len[row] = n.len + n.add;
     }
-    if (tid == 0) s.head[0] = all;
+    sync_blocks<CL>();                                    // no block leaves while another may still read its shared memory
 }
 
 // The copies of the partly filled pages: a warp per copy, plane and head, which is one run of tokens x head dim.
@@ -271,7 +375,15 @@ __global__ void __launch_bounds__(256) cache_copy_kernel(unsigned char* __restri
         const uint4* from = reinterpret_cast<const uint4*>(pool + pl * plane_bytes + (int64_t(c.x) * heads + h) * head_bytes);
         uint4* to = reinterpret_cast<uint4*>(pool + pl * plane_bytes + (int64_t(c.y) * heads + h) * head_bytes);
         const int32_t vecs = c.z * token_bytes / 16;
-        for (int32_t v = lane; v < vecs; v += 32) to[v] = from[v];
+        for (int32_t v0 = lane; v0 < vecs; v0 += 32 * 4) {         // four loads in flight
+            uint4 x[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (v0 + u * 32 < vecs) x[u] = from[v0 + u * 32];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (v0 + u * 32 < vecs) __stcs(to + v0 + u * 32, x[u]);
+        }
     }
 }
 
@@ -321,36 +433,78 @@ __global__ void __launch_bounds__(256) cache_write_kernel(Books b, WriteParams w
 }
 
 // ---- compact -----------------------------------------------------------------------------------------
-// One block: the number n of live pages; the live pages at n and above, in order, are to go to the free pages below
+// One cluster: the number n of live pages; the live pages at n and above, in order, are to go to the free pages below
 // n, in order; their reference counts go along.
-__global__ void __launch_bounds__(XT) cache_plan_compact_kernel(Books b, Scratch s, int32_t* __restrict__ live_out) {
+template <int CL>
+__global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(XT) cache_plan_compact_kernel(Books b, Scratch s, int32_t* __restrict__ live_out) {
     __shared__ int32_t warp_sums[32];
+    __shared__ int32_t own_live, own_holes, own_movers;
     const int tid = threadIdx.x;
-    int32_t mine = 0;
-    for (int32_t p = tid; p < b.pages; p += XT) mine += b.ref[p] > 0;
-    int32_t live = 0;
-    block_scan(mine, warp_sums, &live);
-    int32_t holes = 0, movers = 0;
-    for (int32_t p0 = 0; p0 < b.pages; p0 += XT) {
-        const int32_t p = p0 + tid;
-        const int32_t ref = p < b.pages ? b.ref[p] : 0;
-        const bool hole = p < live && ref <= 0, mover = p >= live && p < b.pages && ref > 0;
+    const uint32_t rank = cluster_rank();
+    int32_t p0, p1;
+    share_of<CL>(b.pages, rank, &p0, &p1);
+    int32_t mine = 0, total = 0;
+    for (int32_t p = p0 + tid * 4; p < p1; p += XT * 4) {
+        const int4 r = four_refs(b.ref, p, p1);
+        const int32_t here = min(4, p1 - p);
+        mine += (r.x > 0) + (here > 1 && r.y > 0) + (here > 2 && r.z > 0) + (here > 3 && r.w > 0);
+    }
+    block_scan(mine, warp_sums, &total);
+    if (tid == 0) own_live = total;
+    int32_t before, live;
+    cluster_sums<CL>(&own_live, rank, &before, &live);
+    // holes of this share: its places below n that no live page has; movers: its live pages from n on
+    const int32_t below = max(0, min(p1, live) - p0);
+    int32_t live_below = 0;
+    mine = 0;
+    for (int32_t p = p0 + tid * 4; p < min(p1, live); p += XT * 4) {
+        const int4 r = four_refs(b.ref, p, p1);
+        const int32_t here = min(4, min(p1, live) - p);
+        mine += (r.x > 0) + (here > 1 && r.y > 0) + (here > 2 && r.z > 0) + (here > 3 && r.w > 0);
+    }
+    block_scan(mine, warp_sums, &live_below);
+    if (tid == 0) { own_holes = below - live_below; own_movers = total - live_below; }
+    int32_t holes, movers, n_holes, n_movers;
+    cluster_sums<CL>(&own_holes, rank, &holes, &n_holes);
+    movers = 0;
+    n_movers = 0;
+#pragma unroll
+    for (uint32_t c = 0; c < CL; ++c) {
+        const int32_t v = CL == 1 ? own_movers : remote_int(&own_movers, c);
+        if (c < rank) movers += v;
+        n_movers += v;
+    }
+    for (int32_t q = p0; q < p1; q += XT * 4) {
+        const int32_t p = q + tid * 4;
+        const int4 r4 = p < p1 ? four_refs(b.ref, p, p1) : make_int4(1, 1, 1, 1);
+        const int32_t r[4] = {r4.x, r4.y, r4.z, r4.w};
+        int32_t h = 0, m = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const bool in = p + j < p1;
+            h |= int32_t(in && p + j < live && r[j] <= 0) << j;
+            m |= int32_t(in && p + j >= live && r[j] > 0) << j;
+        }
         int32_t n = 0;
-        const int32_t at = block_scan(hole | (mover << 16), warp_sums, &n);
-        if (hole) s.move[holes + (at & 0xffff)].y = p;
-        if (mover) s.move[movers + (at >> 16)].x = p;
-        if (p < b.pages) s.list[p] = p;
+        const int32_t at = block_scan(__popc(h) | (__popc(m) << 16), warp_sums, &n);
+        int32_t ih = holes + (at & 0xffff), im = movers + (at >> 16);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if ((h >> j) & 1) s.move[ih++].y = p + j;
+            if ((m >> j) & 1) s.move[im++].x = p + j;
+            if (p + j < p1) s.list[p + j] = p + j;
+        }
         holes += n & 0xffff;
         movers += n >> 16;
     }
-    __syncthreads();
-    for (int32_t i = tid; i < movers; i += XT) {
+    sync_blocks<CL>();
+    for (int32_t i = int32_t(rank) * XT + tid; i < n_movers; i += CL * XT) {
         const int2 m = s.move[i];
         s.list[m.x] = m.y;
         b.ref[m.y] = b.ref[m.x];
         b.ref[m.x] = 0;
     }
-    if (tid == 0) { s.head[1] = live; s.head[2] = movers; *live_out = live; }
+    if (rank == 0 && tid == 0) { s.head[1] = live; s.head[2] = n_movers; *live_out = live; }
 }
 // The moves, a block per page and plane, and the new page numbers in the table.
 __global__ void __launch_bounds__(256) cache_move_kernel(Books b, unsigned char* __restrict__ pool, Scratch s, int32_t planes,
@@ -367,7 +521,15 @@ __global__ void __launch_bounds__(256) cache_move_kernel(Books b, unsigned char*
         unsigned char* plane = pool + (i % planes) * plane_bytes;
         const uint4* from = reinterpret_cast<const uint4*>(plane + int64_t(m.x) * page_bytes);
         uint4* to = reinterpret_cast<uint4*>(plane + int64_t(m.y) * page_bytes);
-        for (int32_t v = threadIdx.x; v < vecs; v += blockDim.x) to[v] = from[v];
+        for (int32_t v0 = threadIdx.x; v0 < vecs; v0 += 256 * 4) {
+            uint4 x[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (v0 + u * 256 < vecs) x[u] = __ldcs(from + v0 + u * 256);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (v0 + u * 256 < vecs) __stcs(to + v0 + u * 256, x[u]);
+        }
     }
 }
 
@@ -439,7 +601,12 @@ int disc_cache_extend(const disc_cache_t* c, const int32_t* add, uint8_t* status
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     int sms = 0;
     if (const int rc = device_sms(&sms)) return rc;
-    cache_extend_kernel<<<1, XT, 0, st>>>(books(c), add, s, status_out);
+    // rows of a thread: up to 4 are held in registers
+    const int64_t share = ((int64_t(c->n_rows) + CLUSTER - 1) / CLUSTER + 3) & ~int64_t(3), per = (share + XT - 1) / XT;
+    if (c->n_rows <= XT && c->n_pages <= ONE_BLOCK) cache_extend_kernel<1, 1><<<1, XT, 0, st>>>(books(c), add, s, status_out);
+    else if (per <= 1) cache_extend_kernel<CLUSTER, 1><<<CLUSTER, XT, 0, st>>>(books(c), add, s, status_out);
+    else if (per <= 4) cache_extend_kernel<CLUSTER, 4><<<CLUSTER, XT, 0, st>>>(books(c), add, s, status_out);
+    else cache_extend_kernel<CLUSTER, 0><<<CLUSTER, XT, 0, st>>>(books(c), add, s, status_out);
     const int32_t planes = c->n_layers * 2, token_bytes = c->head_dim * 2, head_bytes = c->page_size * token_bytes;
     const int64_t most = (int64_t(c->n_rows) * planes * c->n_kv_heads + 7) / 8;
     const unsigned grid = unsigned(most < sms * 8 ? most : sms * 8);
@@ -482,7 +649,8 @@ int disc_cache_compact(const disc_cache_t* c, int32_t* live_out, void* stream) {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     int sms = 0;
     if (const int rc = device_sms(&sms)) return rc;
-    cache_plan_compact_kernel<<<1, XT, 0, st>>>(books(c), s, live_out);
+    if (c->n_pages <= ONE_BLOCK) cache_plan_compact_kernel<1><<<1, XT, 0, st>>>(books(c), s, live_out);
+    else cache_plan_compact_kernel<CLUSTER><<<CLUSTER, XT, 0, st>>>(books(c), s, live_out);
     const int32_t page_bytes = c->n_kv_heads * c->page_size * c->head_dim * 2;
     cache_move_kernel<<<unsigned(sms * 8), 256, 0, st>>>(books(c), static_cast<unsigned char*>(c->pool), s, c->n_layers * 2,
                                                          int64_t(c->n_pages) * page_bytes, page_bytes);

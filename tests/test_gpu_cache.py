@@ -135,6 +135,24 @@ def test_rows_beyond_the_free_pages_are_left_alone():
         x.check()
 
 
+@pytest.mark.parametrize("rows,pages", [(9000, 12000), (40000, 45000)])
+def test_many_rows(rows, pages):
+    """More rows than threads: four of a thread in registers, and more."""
+    b = Both(1, pages, 16, 1, 8, rows, 3, torch.bfloat16, rows)
+    b.extend((b.rng.integers(0, 24, rows) * (b.rng.random(rows) < 0.6)).astype(np.int32))
+    b.check()
+    parent = np.arange(rows)
+    pick = b.rng.random(rows) < 0.4
+    parent[pick] = b.rng.integers(-1, rows, int(pick.sum()))
+    b.fork([int(x) for x in parent])
+    b.check()
+    b.extend((b.rng.integers(0, 10, rows)).astype(np.int32))
+    b.check()
+    b.free(np.nonzero(b.rng.random(rows) < 0.5)[0])
+    b.compact()
+    b.check()
+
+
 def test_one_token_each_without_offsets_and_skipped_rows():
     b = Both(1, 16, 16, 2, 8, 4, 2, torch.float16, 7)
     b.extend([3, 0, 16, 1])
