@@ -17,11 +17,12 @@ _LOGIT = {torch.float32: DISC_F32, torch.bfloat16: DISC_BF16}
 
 
 def _vectors(t: torch.Tensor, dtype, name: str):
-    """A CUDA tensor [tokens, heads, head_dim] whose innermost axis is contiguous."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.ndim == 3
-            and (t.stride(2) == 1 or t.shape[2] == 1)):
-        raise TypeError(f"{name}: expected a CUDA tensor [tokens, heads, head_dim] of {dtype} with unit inner stride")
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    """A CUDA tensor [tokens, heads, head_dim] whose innermost axis is contiguous: (pointer, the two strides)."""
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype:
+        st = t.stride()
+        if len(st) == 3 and (st[2] == 1 or t.shape[2] == 1):
+            return t.data_ptr(), st[0], st[1]
+    raise TypeError(f"{name}: expected a CUDA tensor [tokens, heads, head_dim] of {dtype} with unit inner stride")
 
 
 def _rows(t: torch.Tensor, name: str):
@@ -52,12 +53,12 @@ def disc_logprobs(logits: torch.Tensor, targets: torch.Tensor | None = None, *, 
     n, V = logits.shape
     _want(targets, n, "targets")
     if out is None:
-        f = dict(dtype=torch.float32, device=logits.device)
-        out = {"logp": torch.empty(n, **f) if targets is not None else None, "entropy": torch.empty(n, **f),
-               "lse": torch.empty(n, **f),
-               "top_ids": torch.empty((n, top), dtype=torch.int32, device=logits.device) if top > 0 else None,
-               "top_logp": torch.empty((n, top), **f) if top > 0 else None,
-               "status": torch.empty(n, dtype=torch.uint8, device=logits.device)}
+        dev, f = logits.device, torch.float32
+        out = {"logp": torch.empty(n, dtype=f, device=dev) if targets is not None else None,
+               "entropy": torch.empty(n, dtype=f, device=dev), "lse": torch.empty(n, dtype=f, device=dev),
+               "top_ids": torch.empty_strided((n, top), (top, 1), dtype=torch.int32, device=dev) if top > 0 else None,
+               "top_logp": torch.empty_strided((n, top), (top, 1), dtype=f, device=dev) if top > 0 else None,
+               "status": torch.empty(n, dtype=torch.uint8, device=dev)}
     else:
         for k in ("logp", "entropy", "lse", "top_ids", "top_logp", "status"):
             _want(out[k], n * top if k.startswith("top") else n, k)
@@ -91,14 +92,18 @@ def disc_logprobs_grad(logits: torch.Tensor, targets, lse: torch.Tensor, entropy
 
 
 # ---- attention over prompts -------------------------------------------------------------------------
+_F32, _DENSE = torch.float32, torch.contiguous_format
+
+
 def _attend_outputs(q: torch.Tensor, out, lse):
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = torch.empty_like(q, memory_format=_DENSE)
     elif out.shape != q.shape or not _dev(out, q.dtype, "out") and out.numel():
         raise TypeError("out: expected q's shape")
     if lse is None:
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-    elif lse.shape != q.shape[:2] or not _dev(lse, torch.float32, "lse") and lse.numel():
+        n, h, _ = q.shape
+        lse = torch.empty_strided((n, h), (h, 1), dtype=_F32, device=q.device)
+    elif lse.shape != q.shape[:2] or not _dev(lse, _F32, "lse") and lse.numel():
         raise TypeError("lse: expected [tokens, heads] of q")
     return out, lse
 
@@ -126,15 +131,16 @@ def disc_attend_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: 
     qp, qt, qh = _vectors(q, q.dtype, "q")
     kp, kt, kh = _vectors(k, q.dtype, "k")
     vp, vt, vh = _vectors(v, q.dtype, "v")
-    if k.shape != v.shape or k.shape[2] != q.shape[2]:
+    n_q, hq, d = q.shape
+    n_k, hkv, dk = k.shape
+    if v.shape != k.shape or dk != d:
         raise TypeError("k, v: expected the same shape [n_k, Hkv, D] with q's head dim")
     n_seqs = cu_q.numel() - 1
     if cu_k is not None:
         _want(cu_k, n_seqs + 1, "cu_k")
     out, lse = _attend_outputs(q, out, lse)
-    rc = lib().disc_attend_prompt(qp, qt, qh, kp, kt, kh, vp, vt, vh, dt, q.shape[1], k.shape[1], q.shape[2], q.shape[0],
-                                  k.shape[0], _dev(cu_q, torch.int32, "cu_q"), _dev(cu_k, torch.int32, "cu_k"), n_seqs,
-                                  int(max_len), int(causal), 1.0 / math.sqrt(q.shape[2]) if scale is None else float(scale),
+    rc = lib().disc_attend_prompt(qp, qt, qh, kp, kt, kh, vp, vt, vh, dt, hq, hkv, d, n_q, n_k, _dev(cu_q, torch.int32, "cu_q"), _dev(cu_k, torch.int32, "cu_k"), n_seqs,
+                                  int(max_len), int(causal), 1.0 / math.sqrt(d) if scale is None else float(scale),
                                   _own(out), _own(lse), _error_word(q.device).data_ptr(),
                                   _stream_ptr(stream))
     _check(rc, "disc_attend_prompt")
