@@ -8,12 +8,15 @@ Three ways to take a step: with the exact valid set (disc_step, the default), in
 mode (`top_m=M`: disc_step_topm - the M most probable tokens are verified in the sorted array and the
 token is drawn among the verified ones; a row without a valid candidate ends as a dead end), and
 from the model's final hidden vectors with the projection fused in (`step_hidden`,
-disc_project_step).
+disc_project_step).  `decode_cached` runs the whole decode of a model of attention layers over a paged key-value
+cache: every query's prompt once, its K candidates on the prompt's shared pages, and at the end the
+drawn candidate alone.
 """
 from __future__ import annotations
 
 import torch
 
+from .model_ops import DiscCache, disc_attend_plan, disc_cache_compact, disc_cache_extend, disc_cache_fork
 from .binding import (DiscSet, DiscState, StepOutputs, disc_accept_resample, disc_project_scratch, disc_project_step,
                       disc_resample, disc_state_init, disc_step, disc_step_topm, lib)
 
@@ -115,6 +118,54 @@ class DiscDecoder:
             o = self.step(logits, t, seed=seed, inv_temperature=inv_temperature)
             prev = torch.where(o.token >= 0, o.token.to(torch.int64), prev)
         return self.finish(seed=seed)
+
+    def decode_cached(self, lm, cache: DiscCache, prompts: torch.Tensor, cu: torch.Tensor, max_len: int, *, seed=0,
+                      inv_temperature=1.0, on_step=None):
+        """Decode of a model of attention layers.
+
+        cache: B*K rows, empty; row b*K + k is candidate k of query b.  prompts: the queries' prompt tokens, packed; cu
+        int32[B+1] on the device, max_len: no prompt is longer.  lm.prefill(prompts, cu, max_len, cache, rows, status) and
+        lm.step(tokens, cache, plan, status) give hidden vectors, lm.logits(hidden) their logits, lm.hq is the number of
+        query heads.  Every prompt runs once, into row b*K; the candidates fork from it and share its pages.  Each position
+        then extends the candidates that are not complete by the token just drawn.  After the K-way draw row b*K
+        holds the drawn candidate, the other rows are empty and the pages in use have moved together.
+
+        Returns disc_resample's results with `cache_status` (uint8[B*K]: ROW_NOPAGE where the cache had no room for a
+        token, whose row is then not to be used) and `live_pages`.  on_step(t, logits, outputs) is called after every
+        position.  The host waits for nothing."""
+        B, K, R = self.B, self.K, self.R
+        if cache.n_rows != R:
+            raise ValueError(f"decode_cached: the cache has {cache.n_rows} rows, the decoder {R}")
+        dev = self.device
+        first = torch.arange(B, dtype=torch.int32, device=dev) * K
+        heads = first.repeat_interleave(K)
+        self.reset()
+        add = torch.zeros(R, dtype=torch.int32, device=dev)
+        add[::K] = cu[1:] - cu[:-1]
+        status = disc_cache_extend(cache, add)
+        hidden = lm.prefill(prompts, cu, max_len, cache, first, status)
+        disc_cache_fork(cache, heads)
+        # a prompt without room leaves its whole group unusable
+        status = status.view(B, K)[:, :1].expand(B, K).reshape(R).contiguous()
+        hidden = hidden.index_select(0, cu[1:].long() - 1).repeat_interleave(K, dim=0)
+        prev = None
+        for t in range(self.set.l_max):
+            if t > 0:
+                add = ((self.state.done == 0) & (status == 0)).to(torch.int32)
+                status = status | disc_cache_extend(cache, add)
+                plan = disc_attend_plan(cache, lm.hq, group=K)
+                # rows that stay as they are must not be written to: their newest token is an old one
+                hidden = lm.step(prev, cache, plan, status | (add == 0).to(torch.uint8))
+            logits = lm.logits(hidden)
+            o = self.step(logits, t, seed=seed, inv_temperature=inv_temperature)
+            if on_step is not None:
+                on_step(t, logits, o)
+            prev = o.token.clamp(min=0) if prev is None else torch.where(o.token >= 0, o.token, prev)
+        res = self.finish(seed=seed)
+        keep = torch.full((R,), -1, dtype=torch.int32, device=dev)
+        keep[::K] = first + res["idx"].clamp(min=0)
+        disc_cache_fork(cache, keep)
+        return {**res, "cache_status": status, "live_pages": disc_cache_compact(cache)}
 
     def replay(self, logits_per_step, *, seed=0, inv_temperature=1.0):
         """Decode over logits that are already resident on the device, one tensor per step."""
