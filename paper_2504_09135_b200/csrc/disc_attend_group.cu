@@ -15,7 +15,8 @@
 //
 // Kernel 1: blocks of 6 warps, two to an SM, so that one's softmax runs beside the other's products; 4 warps one
 // thread per query vector, one warp the loads (a TMA box of 16 tokens x 64 values per block, page by page),
-// one the MMAs.  Tensor memory: S 128 columns | O.  A last tile of fewer than 8 blocks takes fewer steps of the
+// one the MMAs.  Tensor memory: S 64 columns | O.  Tiles of 64 tokens, so that five of keys or values are on their way at a
+// time (with two of 128 tokens the loads came too late: 54 us against 50 on 128 prompts of 500 to 1024 tokens).  A last tile of fewer than 4 blocks takes fewer steps of the
 // second product, and its missing scores are masked, so that nothing stale is ever multiplied.
 
 #include "disc_attend.cuh"
@@ -27,9 +28,10 @@ using namespace disc;
 
 constexpr unsigned FULL = 0xffffffffu;
 constexpr float LN2_F = 0.6931471805599453f;
-constexpr int TN = 128;                // tokens of a tile
+constexpr int TN = 64;                 // tokens of a tile
 constexpr int TILE_BLKS = TN / BLK;
 constexpr int BOX = 64;
+constexpr int Q_BOX_BYTES = GROUP_M * BOX * 2;
 constexpr int MIN_SHARED = 4;          // blocks: less is not worth an item
 constexpr int MAX_TAIL = 8;            // full blocks that kernel 2 takes along
 
@@ -165,9 +167,11 @@ struct Shape {
     static constexpr int BOXES = DP / BOX;
     static constexpr int BOX_BYTES = TN * BOX * 2;
     static constexpr int TILE_BYTES = BOXES * BOX_BYTES;
-    static constexpr int STAGES = DP == 128 ? 2 : 4;
-    static constexpr int TMEM = 256;                               // columns: S 128, O up to 128
-    static constexpr int SMEM = TILE_BYTES + STAGES * TILE_BYTES + 1024 + 128;
+    static constexpr int Q_BYTES = BOXES * Q_BOX_BYTES;
+    static constexpr int STAGES = DP == 128 ? 5 : 10;              // with Q as much as two blocks fit into an SM
+    static constexpr int TMEM = 256;                               // columns: S 64, O up to 128
+    static constexpr int BARRIERS = 5 + 2 * STAGES;
+    static constexpr int SMEM = Q_BYTES + STAGES * TILE_BYTES + BARRIERS * 8 + 16;
 };
 
 struct GroupParams {
@@ -184,9 +188,8 @@ __global__ void __launch_bounds__(THREADS, 2)
 attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                     const __grid_constant__ CUtensorMap map_v, const GroupParams p) {
     using S = Shape<DP>;
-    extern __shared__ unsigned char smem_raw[];
-    unsigned char* q_tile = reinterpret_cast<unsigned char*>((uintptr_t(smem_raw) + 1023) & ~uintptr_t(1023));
-    unsigned char* ring = q_tile + S::TILE_BYTES;
+    extern __shared__ __align__(1024) unsigned char q_tile[];      // nothing else is in shared memory: it begins on a swizzle atom
+    unsigned char* ring = q_tile + S::Q_BYTES;
     uint64_t* bars = reinterpret_cast<uint64_t*>(ring + S::STAGES * S::TILE_BYTES);
     uint64_t* q_full = bars;
     uint64_t* q_empty = bars + 1;
@@ -195,9 +198,8 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     uint64_t* p_full = bars + 4;
     uint64_t* kv_full = bars + 5;
     uint64_t* kv_empty = bars + 5 + S::STAGES;
-    static_assert((5 + 2 * S::STAGES) * 8 <= 128, "room for the barriers");
-    __shared__ uint32_t tmem_slot;
-    __shared__ int s_abort;
+    uint32_t& tmem_slot = *reinterpret_cast<uint32_t*>(bars + S::BARRIERS);
+    int& s_abort = *reinterpret_cast<int*>(bars + S::BARRIERS + 1);
     volatile int* abort = &s_abort;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -233,7 +235,7 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                 if (n > 0) ok = mbar_wait_all(q_empty, (n - 1) & 1, abort);
                 if (ok && lane == 0) {
                     mbar_expect_tx(q_full, uint32_t(S::BOXES) * p.G * p.per_group * BOX * 2);
-                    for (int b = 0; b < S::BOXES; ++b) tma_load_3d(q_tile + b * S::BOX_BYTES, &map_q, b * BOX, head * p.G, row, q_full);
+                    for (int b = 0; b < S::BOXES; ++b) tma_load_3d(q_tile + b * Q_BOX_BYTES, &map_q, b * BOX, head * p.G, row, q_full);
                 }
                 for (int t = 0; t < blks && ok; t += TILE_BLKS) {
                     const int here = min(TILE_BLKS, blks - t);
@@ -263,8 +265,8 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                 const uint64_t kd = kv_desc + uint64_t(stage) * TILE16;
 #pragma unroll
                 for (int kk = 0; kk < DP / 16; ++kk) {
-                    const uint64_t off = uint64_t((kk / 4) * (S::BOX_BYTES >> 4) + (kk % 4) * 2);
-                    umma_ss(tmem, q_desc + off, kd + off, p.idesc_qk, kk > 0);
+                    umma_ss(tmem, q_desc + uint64_t((kk / 4) * (Q_BOX_BYTES >> 4) + (kk % 4) * 2), kd + uint64_t((kk / 4) * (S::BOX_BYTES >> 4) + (kk % 4) * 2),
+                            p.idesc_qk, kk > 0);
                 }
             };
             int load = 0, n = 0, tile = 0;
@@ -339,7 +341,7 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                 if (!ok) break;
                 tc_fence_after();
                 float s[TN];
-                tmem_ld128(s_tm, s);
+                tmem_ld64(s_tm, s);
                 const int here = min(TILE_BLKS, blks - t) * BLK;
                 if (here < TN) {
 #pragma unroll
@@ -347,16 +349,11 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                 }
                 uint32_t pk[16];
                 float2 la;
-                first_quarter<T, DP>(s, c2, ref, l, bad, o_tm, t > 0, la, pk);
+                first_scores<T, DP, TN>(s, c2, ref, l, bad, o_tm, t > 0, la, pk);
                 tmem_st16(s_tm, pk);
                 const float base = ref > -CUDART_INF_F ? ref : 0.f;
-                const float2 down = make_float2(-base, -base);
-                exp_chunk<T>(s + 32, c2, down, la, pk);
+                exp_chunk<T>(s + 32, c2, make_float2(-base, -base), la, pk);
                 tmem_st16(s_tm + 16, pk);
-                exp_chunk<T>(s + 64, c2, down, la, pk);
-                tmem_st16(s_tm + 32, pk);
-                exp_chunk<T>(s + 96, c2, down, la, pk);
-                tmem_st16(s_tm + 48, pk);
                 l = add2(l, la);
                 tmem_wait_st();
                 tc_fence_before();

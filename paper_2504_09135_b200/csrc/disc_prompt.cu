@@ -416,7 +416,7 @@ attend_prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 }
                 uint32_t pk[16];
                 float2 la;
-                first_quarter<T, DP>(s, c2, ref, l, bad, o_tm, j > 0, la, pk);
+                first_scores<T, DP, TN>(s, c2, ref, l, bad, o_tm, j > 0, la, pk);
                 tmem_st16(s_tm, pk);
                 const float base = ref > -CUDART_INF_F ? ref : 0.f;
                 const float2 down = make_float2(-base, -base);

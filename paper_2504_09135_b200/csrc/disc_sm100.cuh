@@ -176,6 +176,24 @@ __device__ __forceinline__ void tmem_ld128(uint32_t taddr, float* v) {
         : "r"(taddr)
         : "memory");
 }
+__device__ __forceinline__ void tmem_ld64(uint32_t taddr, float* v) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+        "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
+        "%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,"
+        "%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63"
+        "}, [%64];\n\ttcgen05.wait::ld.sync.aligned;"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
+          "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]),
+          "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]),
+          "=f"(v[30]), "=f"(v[31]), "=f"(v[32]), "=f"(v[33]), "=f"(v[34]), "=f"(v[35]), "=f"(v[36]), "=f"(v[37]), "=f"(v[38]), "=f"(v[39]),
+          "=f"(v[40]), "=f"(v[41]), "=f"(v[42]), "=f"(v[43]), "=f"(v[44]), "=f"(v[45]), "=f"(v[46]), "=f"(v[47]), "=f"(v[48]), "=f"(v[49]),
+          "=f"(v[50]), "=f"(v[51]), "=f"(v[52]), "=f"(v[53]), "=f"(v[54]), "=f"(v[55]), "=f"(v[56]), "=f"(v[57]), "=f"(v[58]), "=f"(v[59]),
+          "=f"(v[60]), "=f"(v[61]), "=f"(v[62]), "=f"(v[63])
+        : "r"(taddr)
+        : "memory");
+}
 // 32 bytes to a 32-byte boundary
 __device__ __forceinline__ void st_global32(void* p, const uint32_t* v) {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
@@ -251,14 +269,14 @@ __device__ __forceinline__ void exp_chunk(const float* s, float2 c2, float2 shif
 
 constexpr float SLACK = 8.f;             // log2 of the growth a row's sums take before the reference moves
 
-// The first 32 of a block's 128 scores -> probabilities against the row's reference `ref` (in units of log2), their sum to
+// The first 32 of a block's N scores -> probabilities against the row's reference `ref` (in units of log2), their sum to
 // la and 16 packed pairs to pk.  They are exponentiated against the old reference while the block's maximum is formed: the
 // maxima fill the issue slots that the special-function unit leaves.  Should the reference have to move (the maximum
 // exceeds it by more than SLACK, or it is the first finite one), the sums so far, l and the DP columns of O, are
-// rescaled, and the quarter is done once more.  bad is set when a score is NaN.  Called by whole warps.
-template <typename T, int DP>
-__device__ __forceinline__ void first_quarter(const float* s, float2 c2, float& ref, float2& l, bool& bad, uint32_t o_tm, bool has_o,
-                                              float2& la, uint32_t* pk) {
+// rescaled, and the 32 are done once more.  bad is set when a score is NaN.  Called by whole warps.
+template <typename T, int DP, int N>
+__device__ __forceinline__ void first_scores(const float* s, float2 c2, float& ref, float2& l, bool& bad, uint32_t o_tm, bool has_o,
+                                             float2& la, uint32_t* pk) {
     bool again;
     do {
         const float base = ref > -CUDART_INF_F ? ref : 0.f;
@@ -266,7 +284,7 @@ __device__ __forceinline__ void first_quarter(const float* s, float2 c2, float& 
         exp_chunk<T>(s, c2, make_float2(-base, -base), la, pk);
         float mx0 = s[0], mx1 = s[1];
 #pragma unroll
-        for (int e = 0; e < 128; e += 4) {
+        for (int e = 0; e < N; e += 4) {
             mx0 = max3(mx0, s[e], s[e + 1]);
             mx1 = max3(mx1, s[e + 2], s[e + 3]);
         }
