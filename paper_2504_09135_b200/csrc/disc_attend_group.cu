@@ -441,7 +441,7 @@ template <int DP>
 struct JoinSmem {
     static constexpr int O_LD = DP + 4;                            // fp32 sums [8 heads][DP], over keys and values no longer needed
     static constexpr int BLOCK_BYTES = BLK * DP * 2;
-    static constexpr int WARP_BYTES = 4 * BLOCK_BYTES + 64;        // keys and values of two blocks; maximum and sum of 8 heads
+    static constexpr int WARP_BYTES = 4 * BLOCK_BYTES + 256;       // keys and values of two blocks; maximum and sum of 8 heads
     static_assert(8 * O_LD * 4 <= 2 * BLOCK_BYTES, "the sums fit over a block");
 };
 
@@ -449,11 +449,13 @@ struct JoinSmem {
 // m16n8k16, where rows of queries would leave 12 of 16 rows empty with 4 heads, and hold twice the registers (101 us that
 // way on 4096 rows x 4 key heads).  A warp goes through several key heads of its row, as many as leave a warp for every
 // place on the device, and has the next block's loads in flight under the present one's products (78 us without).
-template <typename T, int DP>
+// EXACT: the head dim is DP itself, and all strides and ends along it are known.
+template <typename T, int DP, bool EXACT>
 __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p, int heads_per_job) {
     using S = JoinSmem<DP>;
     constexpr int CH = DP / 8;
-    extern __shared__ __align__(128) unsigned char smem[];
+    const int D = EXACT ? DP : p.D;
+    extern __shared__ __align__(1024) unsigned char smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int jobs_per_row = (p.kv_heads + heads_per_job - 1) / heads_per_job;
     const int64_t job = int64_t(blockIdx.x) * (JT / 32) + warp;
@@ -469,7 +471,7 @@ __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p
     const int2 gp = p.plan.group_part[g], rp = p.plan.row_part[row];
     const int begin = p.plan.shared[g] + p.plan.alone[row], left = (len + BLK - 1) / BLK - begin;      // blocks
     const int32_t* table = p.table + int64_t(row) * p.width;
-    const int64_t head_bytes = int64_t(p.page_size) * p.D * 2;
+    const int64_t head_bytes = int64_t(p.page_size) * D * 2;
     unsigned char* own = smem + warp * S::WARP_BYTES;
     float* ml_sm = reinterpret_cast<float*>(own + 4 * S::BLOCK_BYTES);     // [8] maxima, [8] sums
     const int eights = (G + 7) / 8;                    // a key head's query heads, eight at a time
@@ -479,22 +481,25 @@ __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p
     // holds the page of one of its blocks (there are at most 9)
     const int my_page = lane < left ? table[(begin + lane) / sh.blks_per_page] : 0;
     static_assert(MAX_TAIL < 32, "a lane per block");
+    const int lane_src = lane / CH * (D * 2) + lane % CH * 16;
+    const uint32_t lane_dst = chunk_at<DP>(lane / CH, lane % CH);
     int load_unit = 0, load_blk = 0;                   // of the next step to be loaded
     auto load_step = [&](int step) {
         if (step < steps) {
             const int head = head0 + load_unit / eights, blk = begin + load_blk;
             const int page = __shfl_sync(FULL, my_page, load_blk), tokens = min(BLK, len - blk * BLK);
             if (++load_blk == left) { load_blk = 0; ++load_unit; }
-            const int64_t off = (int64_t(page) * p.kv_heads + head) * head_bytes + int64_t(blk % sh.blks_per_page) * (BLK * 2) * p.D;
+            const int64_t off = (int64_t(page) * p.kv_heads + head) * head_bytes + int64_t(blk % sh.blks_per_page) * (BLK * 2) * D + lane_src;
+            const unsigned char* k_src = p.k + off;
+            const unsigned char* v_src = p.v + off;
             const uint32_t k_at = smem_u32(own) + (step & 1) * 2 * S::BLOCK_BYTES;
 #pragma unroll
             for (int j = 0; j < BLK * CH / 32; ++j) {
-                const int c = j * 32 + lane, r = c / CH, ch = c % CH;
-                const bool some = r < tokens && ch * 8 < p.D;
-                const int64_t src = some ? off + int64_t(r) * p.D * 2 + ch * 16 : 0;
-                const uint32_t dst = k_at + chunk_at<DP>(r, ch);
-                cp16(dst, p.k + src, some);
-                cp16(dst + S::BLOCK_BYTES, p.v + src, some);
+                const bool some = j * (32 / CH) + lane / CH < tokens && (EXACT || lane % CH * 8 < D);
+                // rows j (32 / CH) + lane / CH: what chunk_at() mixes in from the row is the lane's and j's part apart
+                const uint32_t dst = k_at + (lane_dst ^ uint32_t(((j * (32 / CH)) & 7) << 4)) + j * 512;
+                cp16(dst, some ? k_src + j * (32 / CH) * (D * 2) : p.k, some);
+                cp16(dst + S::BLOCK_BYTES, some ? v_src + j * (32 / CH) * (D * 2) : p.v, some);
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -514,8 +519,8 @@ __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p
             const unsigned char* q = p.q + row * p.q_row + (head * G + g0 + (lane >> 2)) * p.q_head + (lane & 3) * 4;
 #pragma unroll
             for (int kk = 0; kk < DP / 16; ++kk) {
-                qf[kk][0] = some_head && kk * 16 < p.D ? *reinterpret_cast<const uint32_t*>(q + kk * 32) : 0u;
-                qf[kk][1] = some_head && kk * 16 + 8 < p.D ? *reinterpret_cast<const uint32_t*>(q + kk * 32 + 16) : 0u;
+                qf[kk][0] = some_head && kk * 16 < D ? *reinterpret_cast<const uint32_t*>(q + kk * 32) : 0u;
+                qf[kk][1] = some_head && kk * 16 + 8 < D ? *reinterpret_cast<const uint32_t*>(q + kk * 32 + 16) : 0u;
             }
             // this thread's two heads: 2 (lane % 4) and the next
             float o[DP / 16][4];
@@ -533,7 +538,7 @@ __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p
 #pragma unroll
                 for (int kk = 0; kk < DP / 16; ++kk) {
                     uint32_t kf[4];
-                    ldsm4(k_at + chunk_at<DP>(lane & 15, 2 * kk + (lane >> 4)), kf);
+                    ldsm4((k_at + chunk_at<DP>(lane & 15, lane >> 4)) ^ uint32_t(kk << 5), kf);
                     mma16<T>(s, kf, qf[kk][0], qf[kk][1]);
                 }
                 // tokens lane / 4 (s[0], s[1]) and 8 further (s[2], s[3])
@@ -569,7 +574,7 @@ __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p
 #pragma unroll
                 for (int j = 0; j < DP / 16; ++j) {
                     uint32_t vf[4];
-                    ldsm4t(v_at + chunk_at<DP>((lane & 7) + ((lane >> 4) << 3), 2 * j + ((lane >> 3) & 1)), vf);
+                    ldsm4t((v_at + chunk_at<DP>((lane & 7) + ((lane >> 4) << 3), (lane >> 3) & 1)) ^ uint32_t(j << 5), vf);
                     mma16<T>(o[j], vf, p0, p1);
                 }
             }
@@ -608,7 +613,7 @@ __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p
 #pragma unroll
             for (int a = 0; a < AT_ONCE; ++a) {
                 h[a] = (i0 + 32 * a) / (DP / 4);
-                some[a] = h[a] < heads && d < p.D;
+                some[a] = h[a] < heads && d < D;
                 m[a] = -CUDART_INF_F;
                 total[a] = 0.f;
                 x[a] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -626,7 +631,7 @@ __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p
 #pragma unroll
                 for (int a = 0; a < AT_ONCE; ++a) {
                     lse[a] = some[a] ? p.plan.part_lse[at + h[a]] : -CUDART_INF_F;
-                    y[a] = some[a] ? *reinterpret_cast<const float4*>(p.plan.part + (at + h[a]) * p.D + d) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    y[a] = some[a] ? *reinterpret_cast<const float4*>(p.plan.part + (at + h[a]) * D + d) : make_float4(0.f, 0.f, 0.f, 0.f);
                 }
 #pragma unroll
                 for (int a = 0; a < AT_ONCE; ++a) add(a, lse[a], 1.f, y[a]);
@@ -641,7 +646,7 @@ __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p
                     if (mt > -CUDART_INF_F || lt != lt) add(a, mt > -CUDART_INF_F ? mt : 0.f, lt, *reinterpret_cast<const float4*>(o_sm + h[a] * S::O_LD + d));
                 }
                 const float inv = total[a] > 0.f ? 1.f / total[a] : (total[a] == 0.f ? 0.f : total[a]);
-                *reinterpret_cast<uint2*>(p.out + ((out_at + g0 + h[a]) * p.D + d) * 2) =
+                *reinterpret_cast<uint2*>(p.out + ((out_at + g0 + h[a]) * D + d) * 2) =
                     make_uint2(pack2<T>(x[a].x * inv, x[a].y * inv), pack2<T>(x[a].z * inv, x[a].w * inv));
                 if (d == 0 && p.lse) p.lse[out_at + g0 + h[a]] = total[a] > 0.f ? (m[a] + log2f(total[a])) * LN2_F : (total[a] == 0.f ? -CUDART_INF_F : total[a]);
             }
@@ -651,18 +656,21 @@ __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p
 
 template <typename T, int DP>
 int launch_groups(const AttendParams& a, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const GroupParams& p, unsigned grid, cudaStream_t st) {
-    static std::atomic<uint64_t> done{0}, done2{0};
+    static std::atomic<uint64_t> done{0}, done2{0}, done3{0};
     constexpr int join_bytes = JT / 32 * JoinSmem<DP>::WARP_BYTES;
     if (const int rc = allow_smem(attend_group_kernel<T, DP>, Shape<DP>::SMEM, done)) return rc;
     attend_group_kernel<T, DP><<<grid, THREADS, Shape<DP>::SMEM, st>>>(q, k, v, p);
     DISC_CUDA(cudaGetLastError());
-    if (const int rc = allow_smem(attend_join_kernel<T, DP>, join_bytes, done2)) return rc;
+    if (const int rc = allow_smem(attend_join_kernel<T, DP, true>, join_bytes, done2)) return rc;
+    if (const int rc = allow_smem(attend_join_kernel<T, DP, false>, join_bytes, done3)) return rc;
     int sms = 0;
     if (const int rc = device_sms(&sms)) return rc;
     const int64_t places = int64_t(sms) * 3 * (JT / 32), units = int64_t(a.rows) * a.kv_heads;
     const int heads_per_job = int(units / places < 1 ? 1 : units / places > a.kv_heads ? a.kv_heads : units / places);
     const int64_t jobs = int64_t(a.rows) * ((a.kv_heads + heads_per_job - 1) / heads_per_job);
-    attend_join_kernel<T, DP><<<unsigned((jobs + JT / 32 - 1) / (JT / 32)), JT, join_bytes, st>>>(a, heads_per_job);
+    const unsigned join_grid = unsigned((jobs + JT / 32 - 1) / (JT / 32));
+    if (a.D == DP) attend_join_kernel<T, DP, true><<<join_grid, JT, join_bytes, st>>>(a, heads_per_job);
+    else attend_join_kernel<T, DP, false><<<join_grid, JT, join_bytes, st>>>(a, heads_per_job);
     DISC_CUDA(cudaGetLastError());
     return DISC_OK;
 }
