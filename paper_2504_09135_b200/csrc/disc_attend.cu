@@ -57,14 +57,15 @@ __device__ __forceinline__ int32_t warp_incl_scan(int32_t v, int lane) {
     return v;
 }
 
-__global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(PT) attend_plan_kernel(const PlanParams p) {
+template <int CL>
+__global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(PT) attend_plan_kernel(const PlanParams p) {
     __shared__ int32_t warp_sums[32][3];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const PlanShape& sh = p.shape;
     const int32_t bpp = sh.blks_per_page;
 
     // a warp per group: the leading pages that its rows share, and its list of blocks
-    for (int32_t g = blockIdx.x * (PT / 32) + warp; g < sh.groups; g += CLUSTER * (PT / 32)) {
+    for (int32_t g = blockIdx.x * (PT / 32) + warp; g < sh.groups; g += CL * (PT / 32)) {
         const int32_t r0 = g / sh.sub * sh.group + g % sh.sub * sh.per_group;
         const int32_t r1 = min(p.rows, min(r0 + sh.per_group, g / sh.sub * sh.group + sh.group));
         int2* list = p.plan.list + int64_t(g) * sh.list_ld;
@@ -104,31 +105,31 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(PT) attend_pla
         }
         if (lane == 0) p.plan.count[g] = at;
     }
-    cluster_sync_all();
+    if (CL == 1) __syncthreads(); else cluster_sync_all();
     if (blockIdx.x != 0) return;
 
     // one block: how long a lane's share is, and the items
     int32_t sum = 0;
-    for (int32_t g = tid; g < sh.groups; g += PT) sum += p.plan.count[g];
+    for (int32_t g = tid; g < sh.groups; g += PT) sum += p.plan.count[g] + START;
     sum = warp_incl_scan(sum, lane);
     if (lane == 31) warp_sums[warp][0] = sum;
-    for (int32_t i = tid; i <= sh.lanes; i += PT) p.plan.first[i] = 0x7fffffff;
     __syncthreads();
     int32_t all = 0;
     for (int w = 0; w < PT / 32; ++w) all += warp_sums[w][0];
     __syncthreads();
     const int32_t share = max(TILE_BLKS, ((all - 1) / sh.lanes + TILE_BLKS) / TILE_BLKS * TILE_BLKS);
-    const int32_t lanes = max(1, all / share + (all % share > 0));
+    const int32_t lanes = all / share + (all % share > 0);
     int32_t items = 0, slots = 0;
     int32_t blocks = 0;
     for (int32_t g0 = 0; g0 < sh.groups; g0 += PT) {
         const int32_t g = g0 + tid;
         const int32_t n = g < sh.groups ? p.plan.count[g] : 0;
-        const int32_t bs = warp_incl_scan(n, lane);
+        const int32_t place = g < sh.groups ? n + START : 0;
+        const int32_t bs = warp_incl_scan(place, lane);
         __syncthreads();
         if (lane == 31) warp_sums[warp][0] = bs;
         __syncthreads();
-        int32_t at = blocks + bs - n;
+        int32_t at = blocks + bs - place;
         for (int w = 0; w < PT / 32; ++w) {
             if (w < warp) at += warp_sums[w][0];
             blocks += warp_sums[w][0];
@@ -152,13 +153,11 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(PT) attend_pla
             for (int32_t i = 0; i < splits; ++i) {
                 const int32_t border = (cut.from + i) * share - at;            // from the group's first block
                 p.plan.items[i0 + i] = make_int4(g, max(0, border), min(n, border + share), i);
-                // the first item of a lane begins at its border
-                if (border >= 0 && cut.from + i < lanes) atomicMin(p.plan.first + cut.from + i, i0 + i);
             }
+            first_items(p.plan.first, at, n, share, cut, i0, splits);
         }
     }
-    __syncthreads();
-    if (tid == 0) { p.plan.first[0] = 0; p.plan.first[lanes] = items; p.plan.head[0] = 0; p.plan.head[1] = lanes; }
+    if (tid == 0) { p.plan.first[lanes] = items; p.plan.head[0] = 0; p.plan.head[1] = lanes; }
 }
 
 // ---- attention --------------------------------------------------------------------------------------
@@ -457,27 +456,34 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
                 for (int i = tid; i < M * DV; i += AT) {
                     const int m = i / DV, d = (i % DV) * 4;
                     if (d >= p.D) continue;
-                    float top = -CUDART_INF_F;
-                    bool bad = false;
-                    for (int j = 0; j < splits; ++j) {
-                        const float y = __ldcg(p.plan.part_lse + slot0 + j * step + m);
-                        top = fmaxf(top, y);
-                        bad |= y != y;
-                    }
-                    const float ref = top > -CUDART_INF_F ? top : 0.f;
-                    float total = bad ? CUDART_NAN_F : 0.f;
+                    // one pass in the order of the parts, eight of them on their way at a time
+                    float top = -CUDART_INF_F, total = 0.f;
                     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-                    for (int j = 0; j < splits; ++j) {
-                        const float f = ex2_approx(__ldcg(p.plan.part_lse + slot0 + j * step + m) - ref);
-                        const float4 y = __ldcg(reinterpret_cast<const float4*>(p.plan.part + (slot0 + j * step + m) * p.D + d));
-                        total += f;
-                        x.x += f * y.x; x.y += f * y.y; x.z += f * y.z; x.w += f * y.w;
+                    for (int j0 = 0; j0 < splits; j0 += 8) {
+                        float lse[8];
+                        float4 y[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (j0 + j < splits) {
+                                const int64_t part = slot0 + (j0 + j) * step + m;
+                                lse[j] = __ldcg(p.plan.part_lse + part);
+                                y[j] = __ldcg(reinterpret_cast<const float4*>(p.plan.part + part * p.D + d));
+                            }
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (j0 + j < splits) {
+                                const float n = fmaxf(top, lse[j]);
+                                const float f = top > -CUDART_INF_F ? ex2_approx(top - n) : 0.f, w = lse[j] == -CUDART_INF_F ? 0.f : ex2_approx(lse[j] - n);
+                                top = n;
+                                total = fmaf(total, f, w);
+                                x = make_float4(fmaf(w, y[j].x, x.x * f), fmaf(w, y[j].y, x.y * f), fmaf(w, y[j].z, x.z * f), fmaf(w, y[j].w, x.w * f));
+                            }
                     }
                     const float inv = total > 0.f ? 1.f / total : (total == 0.f ? 0.f : total);
                     const int64_t at = int64_t(r0 + m / G) * p.kv_heads * G + head * G + m % G;
                     *reinterpret_cast<uint2*>(p.out + (at * p.D + d) * 2) =
                         make_uint2(Num<T>::pack(x.x * inv, x.y * inv), Num<T>::pack(x.z * inv, x.w * inv));
-                    if (d == 0 && p.lse) p.lse[at] = total > 0.f ? (ref + log2f(total)) * LN2_F : (total == 0.f ? -CUDART_INF_F : total);
+                    if (d == 0 && p.lse) p.lse[at] = total > 0.f ? (top + log2f(total)) * LN2_F : (total == 0.f ? -CUDART_INF_F : total);
                 }
             }
         }
@@ -526,7 +532,9 @@ int disc_attend_plan(const disc_cache_t* c, int32_t n_q_heads, int32_t group, vo
     p.page_size = c->page_size; p.shift = shift_of(c->page_size); p.kv_heads = c->n_kv_heads;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (p.shape.M > ROWS_M) return disc::plan_groups(p, st);
-    attend_plan_kernel<<<CLUSTER, PT, 0, st>>>(p);
+    // few groups: one block does without the cluster's barrier
+    if (p.shape.groups <= PT / 32) attend_plan_kernel<1><<<1, PT, 0, st>>>(p);
+    else attend_plan_kernel<CLUSTER><<<CLUSTER, PT, 0, st>>>(p);
     DISC_CUDA(cudaGetLastError());
     return DISC_OK;
 }

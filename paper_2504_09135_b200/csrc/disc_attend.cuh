@@ -9,6 +9,7 @@ constexpr int BLK = 16;                // tokens of a block: the smallest page, 
 constexpr int ROWS_M = 16;             // up to this many query vectors read the same pages: disc_attend.cu, above it disc_attend_group.cu
 constexpr int GROUP_M = 128;           // query vectors that a group can have at most
 constexpr int G_MAX = 64;              // query heads per key head
+constexpr int START = 8;               // what beginning an item costs, in blocks
 constexpr int PLACES = 148 * 2;        // blocks that run at a time: two to an SM
 
 struct PlanShape {
@@ -63,7 +64,7 @@ inline int plan_shape(const disc_cache_t* c, int32_t hq, int32_t group, PlanShap
     s->M = s->per_group * s->G;
     s->blks_per_page = c->page_size / BLK;
     // blocks are counted in 32 bits
-    if (int64_t(c->n_rows) * c->table_width * s->blks_per_page >= (int64_t(1) << 31)) return DISC_ERR_UNSUPPORTED;
+    if (int64_t(c->n_rows) * (int64_t(c->table_width) * s->blks_per_page + START) >= (int64_t(1) << 30)) return DISC_ERR_UNSUPPORTED;
     s->lanes = PLACES / c->n_kv_heads > 1 ? PLACES / c->n_kv_heads : 1;
     // every border between two lanes makes one item two
     if (s->M <= ROWS_M) {
@@ -112,13 +113,19 @@ inline int64_t plan_layout(const disc_cache_t* c, const PlanShape& s, void* base
 // How the work of a key head is cut, the same way for every key head: all blocks in a row, group after group, in equal
 // shares ("lanes") for the blocks of threads that run at a time.  An item is what a lane has of one group.  (Items of equal
 // length dealt out in turn left the device waiting for the last ones: 196 us against 185 with 1.5 times as many, 213 with four
-// times, on 64 rows of 1 to 8191 tokens and 8 key heads.)
+// times, 159 with shares, on 64 rows of 1 to 8191 tokens and 8 key heads.)  Behind its blocks a group takes up START more,
+// for what beginning an item costs, so that a lane of many short rows is not the last.
 struct Cut {
     int32_t from, splits;              // lane of the first item; items
 };
 __host__ __device__ inline Cut cut_group(int32_t at, int32_t blocks, int32_t share) {
     const int32_t from = at / share;
     return {from, blocks > 0 ? (at + blocks - 1) / share - from + 1 : 0};
+}
+// The lanes that begin within a group's place [at, at + blocks + START): their first items.  One thread.
+__device__ inline void first_items(int32_t* first, int32_t at, int32_t blocks, int32_t share, const Cut& cut, int32_t item0, int32_t items) {
+    for (int32_t lane = (at + share - 1) / share; lane * share < at + blocks + START; ++lane)
+        first[lane] = item0 + (lane * share < at + blocks ? lane - cut.from : lane * share == at ? 0 : items);
 }
 
 struct PlanParams {

@@ -104,11 +104,11 @@ __global__ void __launch_bounds__(PT) group_items_kernel(const PlanParams p) {
     const PlanShape& sh = p.shape;
     const int tid = threadIdx.x, lane = tid & 31;
     if (tid == 0) s_all = 0;
-    for (int32_t i = tid; i <= sh.lanes; i += PT) p.plan.first[i] = 0x7fffffff;
     __syncthreads();
     int32_t mine = 0, alone = 0;
-    for (int32_t g = tid; g < sh.groups; g += PT) mine += p.plan.shared[g];
-    for (int32_t r = tid; r < p.rows; r += PT) alone += p.plan.alone[r];
+    auto place = [](int32_t blks) { return blks > 0 ? blks + START : 0; };
+    for (int32_t g = tid; g < sh.groups; g += PT) mine += place(p.plan.shared[g]);
+    for (int32_t r = tid; r < p.rows; r += PT) alone += place(p.plan.alone[r]);
     mine += alone;
     const int any_alone = __syncthreads_or(alone > 0);
 #pragma unroll
@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(PT) group_items_kernel(const PlanParams p) {
                 }
             }
             int2 total;
-            const int32_t at = blocks + block_sums(blks, 0, sums, &total).x;
+            const int32_t at = blocks + block_sums(place(blks), 0, sums, &total).x;
             blocks += total.x;
             const Cut cut = cut_group(at, blks, share);
             const int32_t parts = cut.splits * rows * sh.G * p.kv_heads;
@@ -152,8 +152,8 @@ __global__ void __launch_bounds__(PT) group_items_kernel(const PlanParams p) {
             for (int32_t x = 0; x < cut.splits; ++x) {
                 const int32_t border = (cut.from + x) * share - at, begin = max(0, border), end = min(blks, border + share);
                 p.plan.group_items[item0 + x] = GroupItem{row, rows, first + begin, first + end, part0 + x * rows * sh.G * p.kv_heads, {0, 0, 0}};
-                if (border >= 0) p.plan.first[cut.from + x] = item0 + x;         // every lane has exactly one item at its border
             }
+            if (blks > 0) first_items(p.plan.first, at, blks, share, cut, item0, cut.splits);
         }
     }
     __syncthreads();
