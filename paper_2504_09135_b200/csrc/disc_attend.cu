@@ -59,6 +59,8 @@ __device__ __forceinline__ int32_t warp_incl_scan(int32_t v, int lane) {
 
 template <int CL>
 __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(PT) attend_plan_kernel(const PlanParams p) {
+    let_later_in();
+    wait_for_earlier();
     __shared__ int32_t warp_sums[32][3];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const PlanShape& sh = p.shape;
@@ -228,6 +230,8 @@ __device__ __forceinline__ uint32_t chunk_at(int row, int ch) {
 
 template <typename T, int DP>
 __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams p) {
+    let_later_in();
+    wait_for_earlier();
     using S = AttendSmem<DP>;
     constexpr int CH = DP / 8;                                     // chunks of a row
     extern __shared__ __align__(128) unsigned char smem[];
@@ -501,9 +505,7 @@ int launch_attend(const AttendParams& p, unsigned grid, cudaStream_t st) {
     constexpr int bytes = AttendSmem<DP>::BYTES;
     static std::atomic<uint64_t> done{0};
     if (const int rc = allow_smem(attend_cached_kernel<T, DP>, bytes, done)) return rc;
-    attend_cached_kernel<T, DP><<<grid, AT, bytes, st>>>(p);
-    DISC_CUDA(cudaGetLastError());
-    return DISC_OK;
+    return launch_after(attend_cached_kernel<T, DP>, grid, AT, bytes, st, p);
 }
 template <typename T>
 int launch_attend(const AttendParams& p, unsigned grid, cudaStream_t st) {
@@ -533,10 +535,8 @@ int disc_attend_plan(const disc_cache_t* c, int32_t n_q_heads, int32_t group, vo
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (p.shape.M > ROWS_M) return disc::plan_groups(p, st);
     // few groups: one block does without the cluster's barrier
-    if (p.shape.groups <= PT / 32) attend_plan_kernel<1><<<1, PT, 0, st>>>(p);
-    else attend_plan_kernel<CLUSTER><<<CLUSTER, PT, 0, st>>>(p);
-    DISC_CUDA(cudaGetLastError());
-    return DISC_OK;
+    const bool one = p.shape.groups <= PT / 32;
+    return launch_after(one ? attend_plan_kernel<1> : attend_plan_kernel<CLUSTER>, one ? 1 : CLUSTER, PT, 0, st, p);
 }
 
 int disc_attend_cached(const disc_cache_t* c, int32_t layer, const void* q, int64_t q_row_stride, int64_t q_head_stride,

@@ -38,6 +38,8 @@ constexpr int MAX_TAIL = 8;            // full blocks that kernel 2 takes along
 // ---- the plan ---------------------------------------------------------------------------------------
 // A block per group: the leading pages that its rows share, and what rows have left.
 __global__ void __launch_bounds__(256) group_shared_kernel(const PlanParams p) {
+    let_later_in();
+    wait_for_earlier();
     __shared__ int32_t s_shared;
     const PlanShape& sh = p.shape;
     const int g = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -99,6 +101,8 @@ __device__ __forceinline__ int2 block_sums(int32_t a, int32_t b, int2 (*sums), i
 
 // One block: a lane's share, and the items, groups first, then rows.
 __global__ void __launch_bounds__(PT) group_items_kernel(const PlanParams p) {
+    let_later_in();
+    wait_for_earlier();
     __shared__ int2 sums[32];
     __shared__ int32_t s_all;
     const PlanShape& sh = p.shape;
@@ -218,6 +222,8 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     tc_fence_after();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&tmem_slot);
 
+    let_later_in();
+    wait_for_earlier();
     // this block's lane and key head
     const int lane_of = blockIdx.x / p.kv_heads, head = blockIdx.x % p.kv_heads;
     const bool some = lane_of < p.plan.head[1];
@@ -452,6 +458,8 @@ struct JoinSmem {
 // EXACT: the head dim is DP itself, and all strides and ends along it are known.
 template <typename T, int DP, bool EXACT>
 __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p, int heads_per_job) {
+    let_later_in();
+    wait_for_earlier();
     using S = JoinSmem<DP>;
     constexpr int CH = DP / 8;
     const int D = EXACT ? DP : p.D;
@@ -659,8 +667,7 @@ int launch_groups(const AttendParams& a, const CUtensorMap& q, const CUtensorMap
     static std::atomic<uint64_t> done{0}, done2{0}, done3{0};
     constexpr int join_bytes = JT / 32 * JoinSmem<DP>::WARP_BYTES;
     if (const int rc = allow_smem(attend_group_kernel<T, DP>, Shape<DP>::SMEM, done)) return rc;
-    attend_group_kernel<T, DP><<<grid, THREADS, Shape<DP>::SMEM, st>>>(q, k, v, p);
-    DISC_CUDA(cudaGetLastError());
+    if (const int rc = launch_after(attend_group_kernel<T, DP>, grid, THREADS, Shape<DP>::SMEM, st, q, k, v, p)) return rc;
     if (const int rc = allow_smem(attend_join_kernel<T, DP, true>, join_bytes, done2)) return rc;
     if (const int rc = allow_smem(attend_join_kernel<T, DP, false>, join_bytes, done3)) return rc;
     int sms = 0;
@@ -669,10 +676,7 @@ int launch_groups(const AttendParams& a, const CUtensorMap& q, const CUtensorMap
     const int heads_per_job = int(units / places < 1 ? 1 : units / places > a.kv_heads ? a.kv_heads : units / places);
     const int64_t jobs = int64_t(a.rows) * ((a.kv_heads + heads_per_job - 1) / heads_per_job);
     const unsigned join_grid = unsigned((jobs + JT / 32 - 1) / (JT / 32));
-    if (a.D == DP) attend_join_kernel<T, DP, true><<<join_grid, JT, join_bytes, st>>>(a, heads_per_job);
-    else attend_join_kernel<T, DP, false><<<join_grid, JT, join_bytes, st>>>(a, heads_per_job);
-    DISC_CUDA(cudaGetLastError());
-    return DISC_OK;
+    return launch_after(a.D == DP ? attend_join_kernel<T, DP, true> : attend_join_kernel<T, DP, false>, join_grid, JT, join_bytes, st, a, heads_per_job);
 }
 
 int encode(EncodeTiled enc, CUtensorMap* map, CUtensorMapDataType type, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides,
@@ -686,10 +690,8 @@ int encode(EncodeTiled enc, CUtensorMap* map, CUtensorMapDataType type, int rank
 }  // namespace
 
 int disc::plan_groups(const PlanParams& p, cudaStream_t st) {
-    group_shared_kernel<<<unsigned(p.shape.groups), 256, 0, st>>>(p);
-    group_items_kernel<<<1, PT, 0, st>>>(p);
-    DISC_CUDA(cudaGetLastError());
-    return DISC_OK;
+    if (const int rc = launch_after(group_shared_kernel, unsigned(p.shape.groups), 256, 0, st, p)) return rc;
+    return launch_after(group_items_kernel, 1, PT, 0, st, p);
 }
 
 int disc::attend_groups(const AttendParams& a, int32_t dtype, int32_t n_q_heads, cudaStream_t st) {

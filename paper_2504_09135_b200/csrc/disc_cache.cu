@@ -68,6 +68,8 @@ struct Books {
 // the second writes the table.  Two launches, because a row that changes may be another row's parent.
 __global__ void __launch_bounds__(256) cache_take_kernel(Books b, const int32_t* __restrict__ parent, const uint8_t* __restrict__ freed,
                                                          Scratch s) {
+    let_later_in();
+    wait_for_earlier();
     const int32_t row = int32_t((blockIdx.x * blockDim.x + threadIdx.x) >> 5);
     const int lane = threadIdx.x & 31;
     if (row >= b.rows) return;
@@ -91,6 +93,8 @@ __global__ void __launch_bounds__(256) cache_take_kernel(Books b, const int32_t*
 }
 __global__ void __launch_bounds__(256) cache_settle_kernel(Books b, const int32_t* __restrict__ parent, const uint8_t* __restrict__ freed,
                                                            Scratch s) {
+    let_later_in();
+    wait_for_earlier();
     const int32_t row = int32_t((blockIdx.x * blockDim.x + threadIdx.x) >> 5);
     const int lane = threadIdx.x & 31;
     if (row >= b.rows) return;
@@ -216,6 +220,8 @@ __device__ __forceinline__ Need row_need(const Books& b, const int32_t* add, int
 template <int CL, int ROWS>
 __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(XT) cache_extend_kernel(Books b, const int32_t* __restrict__ add, Scratch s,
                                                                                        uint8_t* __restrict__ status) {
+    let_later_in();
+    wait_for_earlier();
     __shared__ int32_t warp_sums[32];
     __shared__ int32_t own_need, own_free;
     const int tid = threadIdx.x, lane = tid & 31;
@@ -364,6 +370,8 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(XT) cache_extend_ke
 // The copies of the partly filled pages: a warp per copy, plane and head, which is one run of tokens x head dim.
 __global__ void __launch_bounds__(256) cache_copy_kernel(unsigned char* __restrict__ pool, Scratch s, int32_t planes, int32_t heads,
                                                          int64_t plane_bytes, int32_t head_bytes, int32_t token_bytes) {
+    let_later_in();
+    wait_for_earlier();
     const int lane = threadIdx.x & 31;
     const int64_t n = int64_t(s.head[0]) * planes * heads;
     const int64_t step = int64_t(gridDim.x) * (blockDim.x >> 5);
@@ -402,6 +410,8 @@ struct WriteParams {
 };
 // one warp per new token: its keys and values of all heads
 __global__ void __launch_bounds__(256) cache_write_kernel(Books b, WriteParams w) {
+    let_later_in();
+    wait_for_earlier();
     const int32_t t = int32_t((blockIdx.x * blockDim.x + threadIdx.x) >> 5);
     const int lane = threadIdx.x & 31;
     if (t >= w.tokens) return;
@@ -437,6 +447,8 @@ __global__ void __launch_bounds__(256) cache_write_kernel(Books b, WriteParams w
 // n, in order; their reference counts go along.
 template <int CL>
 __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(XT) cache_plan_compact_kernel(Books b, Scratch s, int32_t* __restrict__ live_out) {
+    let_later_in();
+    wait_for_earlier();
     __shared__ int32_t warp_sums[32];
     __shared__ int32_t own_live, own_holes, own_movers;
     const int tid = threadIdx.x;
@@ -509,6 +521,8 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(XT) cache_plan_comp
 // The moves, a block per page and plane, and the new page numbers in the table.
 __global__ void __launch_bounds__(256) cache_move_kernel(Books b, unsigned char* __restrict__ pool, Scratch s, int32_t planes,
                                                          int64_t plane_bytes, int32_t page_bytes) {
+    let_later_in();
+    wait_for_earlier();
     const int64_t entries = int64_t(b.rows) * b.width;
     for (int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; i < entries; i += int64_t(gridDim.x) * blockDim.x) {
         const int32_t p = b.table[i];
@@ -553,10 +567,8 @@ int take(const disc_cache_t* c, const int32_t* parent, const uint8_t* freed, cud
     Scratch s;
     scratch_layout(c, &s);
     const unsigned grid = unsigned((int64_t(c->n_rows) * 32 + 255) / 256);
-    cache_take_kernel<<<grid, 256, 0, st>>>(books(c), parent, freed, s);
-    cache_settle_kernel<<<grid, 256, 0, st>>>(books(c), parent, freed, s);
-    DISC_CUDA(cudaGetLastError());
-    return DISC_OK;
+    if (const int rc = launch_after(cache_take_kernel, grid, 256, 0, st, books(c), parent, freed, s)) return rc;
+    return launch_after(cache_settle_kernel, grid, 256, 0, st, books(c), parent, freed, s);
 }
 
 }  // namespace
@@ -603,17 +615,14 @@ int disc_cache_extend(const disc_cache_t* c, const int32_t* add, uint8_t* status
     if (const int rc = device_sms(&sms)) return rc;
     // rows of a thread: up to 4 are held in registers
     const int64_t share = ((int64_t(c->n_rows) + CLUSTER - 1) / CLUSTER + 3) & ~int64_t(3), per = (share + XT - 1) / XT;
-    if (c->n_rows <= XT && c->n_pages <= ONE_BLOCK) cache_extend_kernel<1, 1><<<1, XT, 0, st>>>(books(c), add, s, status_out);
-    else if (per <= 1) cache_extend_kernel<CLUSTER, 1><<<CLUSTER, XT, 0, st>>>(books(c), add, s, status_out);
-    else if (per <= 4) cache_extend_kernel<CLUSTER, 4><<<CLUSTER, XT, 0, st>>>(books(c), add, s, status_out);
-    else cache_extend_kernel<CLUSTER, 0><<<CLUSTER, XT, 0, st>>>(books(c), add, s, status_out);
+    const bool one = c->n_rows <= XT && c->n_pages <= ONE_BLOCK;
+    auto extend = one ? cache_extend_kernel<1, 1> : per <= 1 ? cache_extend_kernel<CLUSTER, 1> : per <= 4 ? cache_extend_kernel<CLUSTER, 4> : cache_extend_kernel<CLUSTER, 0>;
+    if (const int rc = launch_after(extend, one ? 1 : CLUSTER, XT, 0, st, books(c), add, s, status_out)) return rc;
     const int32_t planes = c->n_layers * 2, token_bytes = c->head_dim * 2, head_bytes = c->page_size * token_bytes;
     const int64_t most = (int64_t(c->n_rows) * planes * c->n_kv_heads + 7) / 8;
     const unsigned grid = unsigned(most < sms * 8 ? most : sms * 8);
-    cache_copy_kernel<<<grid, 256, 0, st>>>(static_cast<unsigned char*>(c->pool), s, planes, c->n_kv_heads,
-                                            int64_t(c->n_pages) * c->n_kv_heads * head_bytes, head_bytes, token_bytes);
-    DISC_CUDA(cudaGetLastError());
-    return DISC_OK;
+    return launch_after(cache_copy_kernel, grid, 256, 0, st, static_cast<unsigned char*>(c->pool), s, planes, c->n_kv_heads,
+                        int64_t(c->n_pages) * c->n_kv_heads * head_bytes, head_bytes, token_bytes);
 }
 
 int disc_cache_write(const disc_cache_t* c, int32_t layer, const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v,
@@ -636,9 +645,7 @@ int disc_cache_write(const disc_cache_t* c, int32_t layer, const void* k, int64_
     const int64_t plane = int64_t(c->n_pages) * w.heads * w.head_bytes;
     w.k_plane = static_cast<unsigned char*>(c->pool) + 2 * int64_t(layer) * plane;
     w.v_plane = w.k_plane + plane;
-    cache_write_kernel<<<unsigned((n_tokens * 32 + 255) / 256), 256, 0, static_cast<cudaStream_t>(stream)>>>(books(c), w);
-    DISC_CUDA(cudaGetLastError());
-    return DISC_OK;
+    return launch_after(cache_write_kernel, unsigned((n_tokens * 32 + 255) / 256), 256, 0, static_cast<cudaStream_t>(stream), books(c), w);
 }
 
 int disc_cache_compact(const disc_cache_t* c, int32_t* live_out, void* stream) {
@@ -649,13 +656,12 @@ int disc_cache_compact(const disc_cache_t* c, int32_t* live_out, void* stream) {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     int sms = 0;
     if (const int rc = device_sms(&sms)) return rc;
-    if (c->n_pages <= ONE_BLOCK) cache_plan_compact_kernel<1><<<1, XT, 0, st>>>(books(c), s, live_out);
-    else cache_plan_compact_kernel<CLUSTER><<<CLUSTER, XT, 0, st>>>(books(c), s, live_out);
+    const bool one = c->n_pages <= ONE_BLOCK;
+    auto plan = one ? cache_plan_compact_kernel<1> : cache_plan_compact_kernel<CLUSTER>;
+    if (const int rc = launch_after(plan, one ? 1 : CLUSTER, XT, 0, st, books(c), s, live_out)) return rc;
     const int32_t page_bytes = c->n_kv_heads * c->page_size * c->head_dim * 2;
-    cache_move_kernel<<<unsigned(sms * 8), 256, 0, st>>>(books(c), static_cast<unsigned char*>(c->pool), s, c->n_layers * 2,
-                                                         int64_t(c->n_pages) * page_bytes, page_bytes);
-    DISC_CUDA(cudaGetLastError());
-    return DISC_OK;
+    return launch_after(cache_move_kernel, unsigned(sms * 8), 256, 0, st, books(c), static_cast<unsigned char*>(c->pool), s, c->n_layers * 2,
+                        int64_t(c->n_pages) * page_bytes, page_bytes);
 }
 
 }  // extern "C"

@@ -100,6 +100,27 @@ inline int allow_smem(F* kernel, int bytes, std::atomic<uint64_t>& done) {
     return DISC_OK;
 }
 
+// Launches that follow one another closely: the kernel's blocks may move in while the last ones of the kernel before are still
+// at work (programmatic stream serialisation), which hides a launch's latency.  Such a kernel begins with
+// wait_for_earlier(), before it touches global memory, and lets its own successor in with let_later_in().
+template <class... P, class... A>
+inline int launch_after(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, cudaStream_t st, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    DISC_CUDA(cudaLaunchKernelEx(&cfg, kernel, P(args)...));
+    return DISC_OK;
+}
+__device__ __forceinline__ void wait_for_earlier() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_later_in() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // ------------------------------------------------------------------ Philox4x32-10
 // Counter-based generator of Salmon et al. (SC'11).  Round keys depend only on the seed.
 struct PhiloxKey {
