@@ -64,17 +64,13 @@ struct Books {
 };
 
 // ---- fork / free ------------------------------------------------------------------------------------
-// One warp per row.  The first kernel notes every changing row's new pages and moves the reference counts;
-// the second writes the table.  Two launches, because a row that changes may be another row's parent.
-__global__ void __launch_bounds__(256) cache_take_kernel(Books b, const int32_t* __restrict__ parent, const uint8_t* __restrict__ freed,
-                                                         Scratch s) {
-    let_later_in();
-    wait_for_earlier();
-    const int32_t row = int32_t((blockIdx.x * blockDim.x + threadIdx.x) >> 5);
-    const int lane = threadIdx.x & 31;
-    if (row >= b.rows) return;
-    const int32_t p = parent ? parent[row] : (freed[row] ? -1 : row);
-    if (p == row) return;
+// One warp per row, two steps.  The first notes every changing row's new pages and moves the reference counts;
+// the second writes the table.  All rows take the first before any takes the second, because a row that changes may be another
+// row's parent: two launches, or, for up to 32 rows, one block with a barrier.
+__device__ __forceinline__ int32_t parent_of(int32_t row, const int32_t* parent, const uint8_t* freed) {
+    return parent ? parent[row] : (freed[row] ? -1 : row);
+}
+__device__ __forceinline__ void take_row(const Books& b, const Scratch& s, int32_t row, int32_t p, int lane) {
     const bool some = p >= 0 && p < b.rows;
     const int32_t len = some ? b.len[p] : 0;
     const int32_t used = (len + b.page_size - 1) >> b.shift, old = (b.len[row] + b.page_size - 1) >> b.shift;
@@ -91,21 +87,27 @@ __global__ void __launch_bounds__(256) cache_take_kernel(Books b, const int32_t*
     }
     if (lane == 0) s.len[row] = len;
 }
-__global__ void __launch_bounds__(256) cache_settle_kernel(Books b, const int32_t* __restrict__ parent, const uint8_t* __restrict__ freed,
-                                                           Scratch s) {
-    let_later_in();
-    wait_for_earlier();
-    const int32_t row = int32_t((blockIdx.x * blockDim.x + threadIdx.x) >> 5);
-    const int lane = threadIdx.x & 31;
-    if (row >= b.rows) return;
-    const int32_t p = parent ? parent[row] : (freed[row] ? -1 : row);
-    if (p == row) return;
-    const int32_t used = (s.len[row] + b.page_size - 1) >> b.shift, old = (b.len[row] + b.page_size - 1) >> b.shift;
+__device__ __forceinline__ void settle_row(const Books& b, const Scratch& s, int32_t row, int lane) {
+    const int32_t len = s.len[row];
+    const int32_t used = (len + b.page_size - 1) >> b.shift, old = (b.len[row] + b.page_size - 1) >> b.shift;
     const int32_t* from = s.table + size_t(row) * b.width;
     int32_t* to = b.table + size_t(row) * b.width;
     for (int32_t j = lane; j < max(used, old); j += 32) to[j] = j < used ? from[j] : -1;
     __syncwarp();
-    if (lane == 0) b.len[row] = s.len[row];
+    if (lane == 0) b.len[row] = len;
+}
+// step 0: the first, 1: the second, 2: both, in one block
+template <int STEP>
+__global__ void __launch_bounds__(STEP == 2 ? 1024 : 256) cache_fork_kernel(Books b, const int32_t* __restrict__ parent,
+                                                                           const uint8_t* __restrict__ freed, Scratch s) {
+    let_later_in();
+    wait_for_earlier();
+    const int32_t row = int32_t((blockIdx.x * blockDim.x + threadIdx.x) >> 5);
+    const int lane = threadIdx.x & 31;
+    const int32_t p = row < b.rows ? parent_of(row, parent, freed) : row;
+    if (STEP != 1 && p != row) take_row(b, s, row, p, lane);
+    if (STEP == 2) __syncthreads();
+    if (STEP != 0 && p != row) settle_row(b, s, row, lane);
 }
 
 // ---- extend ------------------------------------------------------------------------------------------
@@ -191,6 +193,42 @@ __device__ __forceinline__ int4 four_refs(const int32_t* ref, int32_t p, int32_t
     return make_int4(p < end ? ref[p] : 1, p + 1 < end ? ref[p + 1] : 1, p + 2 < end ? ref[p + 2] : 1, p + 3 < end ? ref[p + 3] : 1);
 }
 
+struct Pool {
+    unsigned char* base;
+    int32_t planes, heads;
+    int64_t plane_bytes;
+    int32_t head_bytes, token_bytes;
+};
+// Copies of the tokens in partly filled pages: a warp per copy, plane and head, which is one run of tokens x head dim.
+// This warp's units: first, first + step, ... below n.
+__device__ __forceinline__ void copy_units(const Pool& o, const Scratch& s, int64_t first, int64_t step, int64_t n) {
+    const int lane = threadIdx.x & 31;
+    for (int64_t i = first; i < n; i += step) {
+        const int32_t h = int32_t(i % o.heads);
+        const int64_t j = i / o.heads;
+        const int32_t pl = int32_t(j % o.planes);
+        const int4 c = s.copy[j / o.planes];
+        const uint4* from = reinterpret_cast<const uint4*>(o.base + pl * o.plane_bytes + (int64_t(c.x) * o.heads + h) * o.head_bytes);
+        uint4* to = reinterpret_cast<uint4*>(o.base + pl * o.plane_bytes + (int64_t(c.y) * o.heads + h) * o.head_bytes);
+        const int32_t vecs = c.z * o.token_bytes / 16;
+        for (int32_t v0 = lane; v0 < vecs; v0 += 32 * 4) {         // four loads in flight
+            uint4 x[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (v0 + u * 32 < vecs) x[u] = from[v0 + u * 32];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (v0 + u * 32 < vecs) __stcs(to + v0 + u * 32, x[u]);
+        }
+    }
+}
+__global__ void __launch_bounds__(256) cache_copy_kernel(Pool o, Scratch s) {
+    let_later_in();
+    wait_for_earlier();
+    copy_units(o, s, (int64_t(blockIdx.x) * blockDim.x + threadIdx.x) >> 5, int64_t(gridDim.x) * (blockDim.x >> 5),
+               int64_t(s.head[0]) * o.planes * o.heads);
+}
+
 struct Need {
     int32_t add, len, first, last, page;                   // table positions [first, last) are new; page: the partial last one or -1
     bool too_long;                                         // the table has no room for the row's pages
@@ -219,7 +257,7 @@ __device__ __forceinline__ Need row_need(const Books& b, const int32_t* add, int
 // them again in every step.
 template <int CL, int ROWS>
 __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(XT) cache_extend_kernel(Books b, const int32_t* __restrict__ add, Scratch s,
-                                                                                       uint8_t* __restrict__ status) {
+                                                                                  uint8_t* __restrict__ status, Pool o, bool copy_here) {
     let_later_in();
     wait_for_earlier();
     __shared__ int32_t warp_sums[32];
@@ -365,34 +403,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(XT) cache_extend_ke
         }
     }
     sync_blocks<CL>();                                    // no block leaves while another may still read its shared memory
-}
-
-// The copies of the partly filled pages: a warp per copy, plane and head, which is one run of tokens x head dim.
-__global__ void __launch_bounds__(256) cache_copy_kernel(unsigned char* __restrict__ pool, Scratch s, int32_t planes, int32_t heads,
-                                                         int64_t plane_bytes, int32_t head_bytes, int32_t token_bytes) {
-    let_later_in();
-    wait_for_earlier();
-    const int lane = threadIdx.x & 31;
-    const int64_t n = int64_t(s.head[0]) * planes * heads;
-    const int64_t step = int64_t(gridDim.x) * (blockDim.x >> 5);
-    for (int64_t i = (int64_t(blockIdx.x) * blockDim.x + threadIdx.x) >> 5; i < n; i += step) {
-        const int32_t h = int32_t(i % heads);
-        const int64_t j = i / heads;
-        const int32_t pl = int32_t(j % planes);
-        const int4 c = s.copy[j / planes];
-        const uint4* from = reinterpret_cast<const uint4*>(pool + pl * plane_bytes + (int64_t(c.x) * heads + h) * head_bytes);
-        uint4* to = reinterpret_cast<uint4*>(pool + pl * plane_bytes + (int64_t(c.y) * heads + h) * head_bytes);
-        const int32_t vecs = c.z * token_bytes / 16;
-        for (int32_t v0 = lane; v0 < vecs; v0 += 32 * 4) {         // four loads in flight
-            uint4 x[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (v0 + u * 32 < vecs) x[u] = from[v0 + u * 32];
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (v0 + u * 32 < vecs) __stcs(to + v0 + u * 32, x[u]);
-        }
-    }
+    if (CL == 1 && copy_here) copy_units(o, s, tid >> 5, XT / 32, int64_t(s.head[0]) * o.planes * o.heads);
 }
 
 // ---- write -------------------------------------------------------------------------------------------
@@ -566,9 +577,10 @@ Books books(const disc_cache_t* c) {
 int take(const disc_cache_t* c, const int32_t* parent, const uint8_t* freed, cudaStream_t st) {
     Scratch s;
     scratch_layout(c, &s);
+    if (c->n_rows <= 32) return launch_after(cache_fork_kernel<2>, 1, unsigned(c->n_rows) * 32, 0, st, books(c), parent, freed, s);
     const unsigned grid = unsigned((int64_t(c->n_rows) * 32 + 255) / 256);
-    if (const int rc = launch_after(cache_take_kernel, grid, 256, 0, st, books(c), parent, freed, s)) return rc;
-    return launch_after(cache_settle_kernel, grid, 256, 0, st, books(c), parent, freed, s);
+    if (const int rc = launch_after(cache_fork_kernel<0>, grid, 256, 0, st, books(c), parent, freed, s)) return rc;
+    return launch_after(cache_fork_kernel<1>, grid, 256, 0, st, books(c), parent, freed, s);
 }
 
 }  // namespace
@@ -616,13 +628,18 @@ int disc_cache_extend(const disc_cache_t* c, const int32_t* add, uint8_t* status
     // rows of a thread: up to 4 are held in registers
     const int64_t share = ((int64_t(c->n_rows) + CLUSTER - 1) / CLUSTER + 3) & ~int64_t(3), per = (share + XT - 1) / XT;
     const bool one = c->n_rows <= XT && c->n_pages <= ONE_BLOCK;
+    Pool o;
+    o.base = static_cast<unsigned char*>(c->pool); o.planes = c->n_layers * 2; o.heads = c->n_kv_heads;
+    o.token_bytes = c->head_dim * 2; o.head_bytes = c->page_size * o.token_bytes;
+    o.plane_bytes = int64_t(c->n_pages) * c->n_kv_heads * o.head_bytes;
+    // copies that the one block can make itself, up to 8 a warp, are not worth a launch
+    const int64_t units = int64_t(c->n_rows) * o.planes * o.heads;
+    const bool copy_here = one && units <= XT / 32 * 8;
     auto extend = one ? cache_extend_kernel<1, 1> : per <= 1 ? cache_extend_kernel<CLUSTER, 1> : per <= 4 ? cache_extend_kernel<CLUSTER, 4> : cache_extend_kernel<CLUSTER, 0>;
-    if (const int rc = launch_after(extend, one ? 1 : CLUSTER, XT, 0, st, books(c), add, s, status_out)) return rc;
-    const int32_t planes = c->n_layers * 2, token_bytes = c->head_dim * 2, head_bytes = c->page_size * token_bytes;
-    const int64_t most = (int64_t(c->n_rows) * planes * c->n_kv_heads + 7) / 8;
-    const unsigned grid = unsigned(most < sms * 8 ? most : sms * 8);
-    return launch_after(cache_copy_kernel, grid, 256, 0, st, static_cast<unsigned char*>(c->pool), s, planes, c->n_kv_heads,
-                        int64_t(c->n_pages) * c->n_kv_heads * head_bytes, head_bytes, token_bytes);
+    if (const int rc = launch_after(extend, one ? 1 : CLUSTER, XT, 0, st, books(c), add, s, status_out, o, copy_here)) return rc;
+    if (copy_here) return DISC_OK;
+    const int64_t most = (units + 7) / 8;
+    return launch_after(cache_copy_kernel, unsigned(most < sms * 8 ? most : sms * 8), 256, 0, st, o, s);
 }
 
 int disc_cache_write(const disc_cache_t* c, int32_t layer, const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v,
