@@ -496,7 +496,10 @@ int disc_cache_compact(const disc_cache_t* c, int32_t* live_out, void* stream);
  * The plan: which pages each group of `group` consecutive rows (K candidates of a query; 1 = unrelated
  * rows) has in common, and how the work is split.  It depends on the books only: make it once per position, after
  * disc_cache_extend, and use it for every layer.
- *   plan    device, disc_attend_plan_bytes() bytes, 16-byte aligned */
+ *   plan    device, disc_attend_plan_bytes() bytes, 32-byte aligned.  Its first 4 bytes are an error word as
+ *           disc_attend_prompt's, cleared here and set by disc_attend_cached; read with disc_attend_error
+ * Errors: DISC_ERR_ARG; DISC_ERR_UNSUPPORTED for more than 64 query heads per key head, or tables of more than 2^30 blocks of
+ * 16 tokens. */
 int64_t disc_attend_plan_bytes(const disc_cache_t* c, int32_t n_q_heads, int32_t group);
 int disc_attend_plan(const disc_cache_t* c, int32_t n_q_heads, int32_t group, void* plan, int64_t plan_bytes, void* stream);
 
@@ -505,13 +508,14 @@ int disc_attend_plan(const disc_cache_t* c, int32_t n_q_heads, int32_t group, vo
  *   q       device, dtype of the cache; row r, head h at element offset r*q_row_stride + h*q_head_stride;
  *           base on a 16-byte boundary, strides multiples of 8
  *   n_q_heads   a multiple of n_kv_heads, at most 64 times as many
+ *   scale   > 0
  *   plan    of disc_attend_plan with the same cache sizes, n_q_heads and group; long rows are split and joined in
  *           it, so calls that share a plan must not overlap
  *   out     device, [n_rows][n_q_heads][head_dim] contiguous, 16-byte aligned
  *   lse_out device, float[n_rows][n_q_heads] (nullable)
  * Scores, sums and outputs are accumulated in fp32; the probabilities are rounded to the inputs' type for
  * the second product, the outputs once at the end.  The result does not depend on the order in which the parts of
- * a row finish. */
+ * a row finish, and a row's non-finite values do not reach the other rows of its group. */
 int disc_attend_cached(const disc_cache_t* c, int32_t layer, const void* q, int64_t q_row_stride, int64_t q_head_stride,
                        int32_t n_q_heads, int32_t group, float scale, void* plan, int64_t plan_bytes, void* out, float* lse_out,
                        void* stream);

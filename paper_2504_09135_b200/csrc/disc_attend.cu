@@ -149,17 +149,18 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(PT) attend_plan_ker
             slots += warp_sums[w][2];
         }
         if (g < sh.groups) {
-            p.plan.splits[g] = splits;
-            p.plan.slot[g] = splits > 1 ? s0 : -1;
+            const int32_t r0 = g / sh.sub * sh.group + g % sh.sub * sh.per_group;
+            const int32_t rows = max(0, min(p.rows, min(r0 + sh.per_group, g / sh.sub * sh.group + sh.group)) - r0);
             for (int32_t h = 0; h < p.kv_heads; ++h) p.plan.arrived[int64_t(g) * p.kv_heads + h] = 0;
             for (int32_t i = 0; i < splits; ++i) {
                 const int32_t border = (cut.from + i) * share - at;            // from the group's first block
-                p.plan.items[i0 + i] = make_int4(g, max(0, border), min(n, border + share), i);
+                p.plan.items[i0 + i] = RowItem{g, max(0, border), min(n, border + share), i, r0, rows, splits, splits > 1 ? s0 : -1};
             }
             first_items(p.plan.first, at, n, share, cut, i0, splits);
         }
     }
-    if (tid == 0) { p.plan.first[lanes] = items; p.plan.head[0] = 0; p.plan.head[1] = lanes; }
+    for (int32_t i = lanes + tid; i <= sh.lanes; i += PT) p.plan.first[i] = items;
+    if (tid == 0) p.plan.head[0] = 0;
 }
 
 // ---- attention --------------------------------------------------------------------------------------
@@ -245,16 +246,13 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
     const int G = sh.G;
     // this block's lane and key head
     const int lane_of = blockIdx.x / p.kv_heads, head = blockIdx.x % p.kv_heads;
-    if (lane_of >= p.plan.head[1]) return;
     const int item_end = p.plan.first[lane_of + 1];
     const int row_lo = lane >> 2;                                  // this thread's two rows of the tile: row_lo, row_lo + 8
     const int own_lo = row_lo / G + 1, own_hi = (row_lo + 8) / G + 1;
 
     for (int n = p.plan.first[lane_of]; n < item_end; ++n) {
-        const int4 item = p.plan.items[n];
-        const int g = item.x;
-        const int32_t r0 = g / sh.sub * sh.group + g % sh.sub * sh.per_group;
-        const int32_t n_rows = max(0, min(p.rows, min(r0 + sh.per_group, g / sh.sub * sh.group + sh.group)) - r0);
+        const int4 item = *reinterpret_cast<const int4*>(p.plan.items + n), more = *(reinterpret_cast<const int4*>(p.plan.items + n) + 1);
+        const int g = item.x, r0 = more.x, n_rows = more.y, splits = more.z;
         const int M = n_rows * G;
         const int2* list = p.plan.list + int64_t(g) * sh.list_ld;
         const int32_t* table = p.table + int64_t(r0) * p.width;
@@ -416,8 +414,7 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
         }
         __syncthreads();
 
-        const int splits = p.plan.splits[g];
-        const int64_t slot = splits > 1 ? (int64_t(p.plan.slot[g] + item.w) * p.kv_heads + head) * sh.M : 0;
+        const int64_t slot = splits > 1 ? (int64_t(more.w + item.w) * p.kv_heads + head) * sh.M : 0;
         constexpr int DV = DP / 4;
         for (int i = tid; i < M * DV; i += AT) {
             const int m = i / DV, d = (i % DV) * 4;
@@ -456,7 +453,7 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
             __syncthreads();
             if (s_last) {
                 __threadfence();
-                const int64_t slot0 = (int64_t(p.plan.slot[g]) * p.kv_heads + head) * sh.M, step = int64_t(p.kv_heads) * sh.M;
+                const int64_t slot0 = (int64_t(more.w) * p.kv_heads + head) * sh.M, step = int64_t(p.kv_heads) * sh.M;
                 for (int i = tid; i < M * DV; i += AT) {
                     const int m = i / DV, d = (i % DV) * 4;
                     if (d >= p.D) continue;
@@ -529,7 +526,7 @@ int disc_attend_plan(const disc_cache_t* c, int32_t n_q_heads, int32_t group, vo
     if (const int rc = disc::cache_sizes(c)) return rc;
     PlanParams p;
     if (const int rc = plan_shape(c, n_q_heads, group, &p.shape)) return rc;
-    if ((reinterpret_cast<uintptr_t>(plan) & 15u) || plan_bytes < plan_layout(c, p.shape, plan, &p.plan)) return DISC_ERR_ARG;
+    if ((reinterpret_cast<uintptr_t>(plan) & 31u) || plan_bytes < plan_layout(c, p.shape, plan, &p.plan)) return DISC_ERR_ARG;
     p.table = c->table; p.len = c->len; p.rows = c->n_rows; p.width = c->table_width;
     p.page_size = c->page_size; p.shift = shift_of(c->page_size); p.kv_heads = c->n_kv_heads;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -547,7 +544,7 @@ int disc_attend_cached(const disc_cache_t* c, int32_t layer, const void* q, int6
     if (layer < 0 || layer >= c->n_layers || !(scale > 0.f) || !(scale <= 3.0e38f)) return DISC_ERR_ARG;
     AttendParams p;
     if (const int rc = plan_shape(c, n_q_heads, group, &p.shape)) return rc;
-    if ((reinterpret_cast<uintptr_t>(plan) & 15u) || plan_bytes < plan_layout(c, p.shape, plan, &p.plan)) return DISC_ERR_ARG;
+    if ((reinterpret_cast<uintptr_t>(plan) & 31u) || plan_bytes < plan_layout(c, p.shape, plan, &p.plan)) return DISC_ERR_ARG;
     if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15u) return DISC_ERR_ARG;
     // the stride over an axis of one is never used; any valid one will do
     if (n_q_heads == 1) q_head_stride = (int64_t(c->head_dim) + 7) / 8 * 8;

@@ -30,17 +30,20 @@ struct GroupItem {                     // rows [row, row + rows) over their bloc
     int32_t row, rows, begin, end, part, pad[3];
 };
 
+struct RowItem {                       // rows [row, row + rows) of group g over the blocks [begin, end) of its list
+    int32_t g, begin, end, index;      // index among the group's items
+    int32_t row, rows, items, slot;    // the group's items; its first partial result, or -1
+};
+
 struct Plan {
-    int32_t* head;                     // [0] error word, [1] lanes in use
-    int32_t* first;                    // [lanes + 1] first item of a lane
+    int32_t* head;                     // [0] error word
+    int32_t* first;                    // [lanes + 1] first item of a lane; lanes without work begin where all items end
     float* part;                       // [max_part][head_dim] normalised sums, fp32
     float* part_lse;                   // [max_part] log-sum-exp in units of log2
     // rows form
     int32_t* count;                    // [groups] blocks
-    int32_t* splits;                   // [groups]
-    int32_t* slot;                     // [groups] first partial result, or -1
     int32_t* arrived;                  // [groups][kv heads]
-    int4* items;                       // group, first block, one past the last, index among the group's items
+    RowItem* items;
     int2* list;                        // [groups][list_ld]: page; block | tokens << 8 | (owner + 1) << 16
     // group form
     GroupItem* group_items;
@@ -94,10 +97,8 @@ inline int64_t plan_layout(const disc_cache_t* c, const PlanShape& s, void* base
     t.part_lse = reinterpret_cast<float*>(take(s.max_part * 4));
     if (s.M <= ROWS_M) {
         t.count = reinterpret_cast<int32_t*>(take(int64_t(s.groups) * 4));
-        t.splits = reinterpret_cast<int32_t*>(take(int64_t(s.groups) * 4));
-        t.slot = reinterpret_cast<int32_t*>(take(int64_t(s.groups) * 4));
         t.arrived = reinterpret_cast<int32_t*>(take(int64_t(s.groups) * c->n_kv_heads * 4));
-        t.items = reinterpret_cast<int4*>(take(int64_t(s.max_items) * 16));
+        t.items = reinterpret_cast<RowItem*>(take(int64_t(s.max_items) * sizeof(RowItem)));
         t.list = reinterpret_cast<int2*>(take(int64_t(s.groups) * s.list_ld * 8));
     } else {
         t.group_items = reinterpret_cast<GroupItem*>(take(int64_t(s.max_items) * sizeof(GroupItem)));

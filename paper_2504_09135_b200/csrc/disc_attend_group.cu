@@ -161,7 +161,8 @@ __global__ void __launch_bounds__(PT) group_items_kernel(const PlanParams p) {
         }
     }
     __syncthreads();
-    if (tid == 0) { p.plan.first[lanes] = items; p.plan.head[0] = 0; p.plan.head[1] = lanes; }
+    for (int32_t i = lanes + tid; i <= sh.lanes; i += PT) p.plan.first[i] = items;
+    if (tid == 0) p.plan.head[0] = 0;
 }
 
 // ---- kernel 1 -----------------------------------------------------------------------------------------
@@ -226,8 +227,7 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     wait_for_earlier();
     // this block's lane and key head
     const int lane_of = blockIdx.x / p.kv_heads, head = blockIdx.x % p.kv_heads;
-    const bool some = lane_of < p.plan.head[1];
-    const int item0 = some ? p.plan.first[lane_of] : 0, item1 = some ? p.plan.first[lane_of + 1] : 0;
+    const int item0 = p.plan.first[lane_of], item1 = p.plan.first[lane_of + 1];
 
     if (warp >= 4) {
         if (warp == 4) {

@@ -147,8 +147,12 @@ def disc_attend_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: 
     return out, lse
 
 
-def disc_attend_check(device="cuda", stream=None):
-    """Synchronises and raises DiscError when an attention kernel on the device gave up on one of its bounded waits."""
+def disc_attend_check(device="cuda", stream=None, *, plan: "AttendPlan | None" = None):
+    """Synchronises and raises DiscError when a prompt attention on the device, or a cached attention with this plan, gave up on
+    one of its bounded waits."""
+    if plan is not None:
+        _check(lib().disc_attend_error(plan.buf.data_ptr(), _stream_ptr(stream)), "disc_attend_error")
+        return
     dev = torch.device(device)
     if dev.index is None:
         dev = torch.device(dev.type, torch.cuda.current_device())

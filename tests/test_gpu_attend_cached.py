@@ -62,6 +62,7 @@ def check(cache, table, lens, hq, group, *, layer=0, rows=None, q=None, seed=1, 
     scale = 1 / math.sqrt(d) if scale is None else scale
     plan = disc.disc_attend_plan(cache, hq, group=group)
     out, lse = disc.disc_attend_cached(cache, layer, q, plan, scale=scale)
+    disc.disc_attend_check(plan=plan)
     again, lse2 = disc.disc_attend_cached(cache, layer, q, plan, scale=scale)       # the plan serves every layer, and the bits are the same
     assert torch.equal(out, again) and torch.equal(lse, lse2)
     for r in range(len(lens)) if rows is None else rows:
@@ -179,6 +180,8 @@ def test_refusals():
         disc.disc_attend_plan(cache, 4, group=0)
     plan = disc.disc_attend_plan(cache, 4)
     q = torch.zeros((2, 4, 64), dtype=torch.bfloat16, device=DEV)
+    with pytest.raises(disc.DiscError):
+        disc.disc_attend_cached(cache, 0, q, plan, scale=0.0)
     with pytest.raises(TypeError):
         disc.disc_attend_cached(cache, 0, q.half(), plan)
     with pytest.raises(TypeError):
