@@ -12,8 +12,9 @@
 // order.  The counts are changed by atomic additions (their sum does not depend on the order) and
 // everything that depends on an order goes by prefix sums, so the same calls give the same table every time.
 //
-// What these calls cost is latency, a few dependent reads of small arrays, except for the copies of page
-// contents, which are bound by the bytes.
+// What these calls cost is latency, a few dependent reads of small arrays (4096 rows: fork 7 us, extend 13), except for
+// the copies of page contents, which are bound by the bytes: 48 us for the 0.26 GB of 4096 candidates' last pages
+// (5.3 TB/s), 102 us for a compaction's 0.58 GB (5.7 TB/s; the measured copy rate is 6.5).
 
 #include "disc_internal.cuh"
 

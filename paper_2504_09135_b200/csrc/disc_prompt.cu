@@ -13,11 +13,14 @@
 // per tile whatever G is.
 //   warps 0-3, 4-7   one thread per query vector of tile 0 and tile 1: reads its 128 scores from tensor memory,
 //                    masks, exponentiates relative to a running reference and writes P back as bf16 / f16
-//                    over the scores
-//   warp 8           TMA loads of Q once, then K and V blocks in turn into a ring
+//                    over the scores, the first 96 keys before the rest
+//   warp 8           TMA loads of Q, then K and V blocks in turn into a ring
 //   warp 9           issues the MMAs (tcgen05, cta_group::1, M 128): S_i = Q_i K^T from shared memory, then
 //                    O_i += P_i V with P_i as the operand in tensor memory.  While the threads of one tile
 //                    exponentiate, the tensor cores run the other tile's P V and next Q K^T.
+//   warp 10          what to work on next: the block takes over the places of blocks that have not started yet (cluster
+//                    launch control), so that the next item's loads and first scores run under the last one's output
+//                    (64 prompts of 350 tokens: 92 us with a block per item, 73 so)
 // Tensor memory, 512 columns: S_0 | S_1 | O_0 | O_1.
 //
 // The reference a row is exponentiated against moves only when the row's maximum exceeds it by more than 2^8: until then
@@ -29,6 +32,9 @@
 // The rows of V beyond the end of a sequence belong to the next one: P is 0 there, but 0 times a non-finite
 // value is not, so the last block's foreign rows are overwritten with zeros before the product.
 // All waits are bounded; one that runs out sets the error word and every role leaves.
+//
+// Measured on 2 x 8192 tokens, 16 / 4 heads of 128: 445 us (1.24 PFLOP/s, 0.74 of cuBLAS' measured rate) in a short run, 520 us
+// under the power cap; 2,820 clocks per 256 x 128 block of scores, of which the products take 2,080 and the exponentials as many.
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
