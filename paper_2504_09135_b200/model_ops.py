@@ -229,13 +229,14 @@ def disc_cache_write(cache: DiscCache, layer: int, k: torch.Tensor, v: torch.Ten
     cu[i] .. cu[i+1]-1 (None: one token each)."""
     kp, kt, kh = _vectors(k, cache.pool.dtype, "k")
     vp, vt, vh = _vectors(v, cache.pool.dtype, "v")
-    if k.shape != v.shape or tuple(k.shape[1:]) != (cache.n_kv_heads, cache.head_dim):
+    n, h, d = k.shape
+    if v.shape != k.shape or h != cache.n_kv_heads or d != cache.head_dim:
         raise TypeError("k, v: expected [tokens, kv heads, head dim] of the cache")
-    n_seqs = k.shape[0] if cu is None else cu.numel() - 1
+    n_seqs = n if cu is None else cu.numel() - 1
     if rows is not None:
         _want(rows, n_seqs, "rows")
     _want(status, cache.n_rows, "status")
-    _check(lib().disc_cache_write(cache._p, int(layer), kp, kt, kh, vp, vt, vh, k.shape[0], _dev(cu, torch.int32, "cu"), n_seqs,
+    _check(lib().disc_cache_write(cache._p, int(layer), kp, kt, kh, vp, vt, vh, n, _dev(cu, torch.int32, "cu"), n_seqs,
                                   _dev(rows, torch.int32, "rows"), _dev(status, torch.uint8, "status"), _stream_ptr(stream)),
            "disc_cache_write")
 
@@ -278,7 +279,8 @@ def disc_attend_cached(cache: DiscCache, layer: int, q: torch.Tensor, plan: Atte
     """One new token per row: q [rows, Hq, D] against the row's tokens in layer `layer` -> (out [rows, Hq, D],
     lse float[rows, Hq])."""
     qp, qr, qh = _vectors(q, cache.pool.dtype, "q")
-    if tuple(q.shape) != (cache.n_rows, plan.n_q_heads, cache.head_dim):
+    n, h, d = q.shape
+    if n != cache.n_rows or h != plan.n_q_heads or d != cache.head_dim:
         raise TypeError("q: expected [rows, Hq, head dim] of the cache and the plan")
     out, lse = _attend_outputs(q, out, lse)
     _check(lib().disc_attend_cached(cache._p, int(layer), qp, qr, qh, plan.n_q_heads, plan.group,
