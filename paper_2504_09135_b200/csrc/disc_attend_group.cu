@@ -453,8 +453,8 @@ struct JoinSmem {
 
 // The products are taken the other way round, S^T = K Q^T and O^T = V^T P^T: 8 query heads are then the narrow side of
 // m16n8k16, where rows of queries would leave 12 of 16 rows empty with 4 heads, and hold twice the registers (101 us that
-// way on 4096 rows x 4 key heads).  A warp goes through several key heads of its row, as many as leave a warp for every
-// place on the device, and has the next block's loads in flight under the present one's products (78 us without).
+// way on 4096 rows x 4 key heads).  A warp goes through one or two key heads of its row (the launch says why) and has the
+// next block's loads in flight under the present one's products (78 us without).
 // EXACT: the head dim is DP itself, and all strides and ends along it are known.
 template <typename T, int DP, bool EXACT>
 __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p, int heads_per_job) {
@@ -673,7 +673,10 @@ int launch_groups(const AttendParams& a, const CUtensorMap& q, const CUtensorMap
     int sms = 0;
     if (const int rc = device_sms(&sms)) return rc;
     const int64_t places = int64_t(sms) * 3 * (JT / 32), units = int64_t(a.rows) * a.kv_heads;
-    const int heads_per_job = int(units / places < 1 ? 1 : units / places > a.kv_heads ? a.kv_heads : units / places);
+    // a warp takes two key heads of a row if that leaves a job for every warp that runs at a time: the row's books are read once
+    // and the second head's blocks come in under the first's sums (4096 rows of 4 heads: 120.4 us for plan and attention; one
+    // head 124.3, all four 123.4, as the warps are then through 2.3 times)
+    const int heads_per_job = units >= 2 * places && a.kv_heads > 1 ? 2 : 1;
     const int64_t jobs = int64_t(a.rows) * ((a.kv_heads + heads_per_job - 1) / heads_per_job);
     const unsigned join_grid = unsigned((jobs + JT / 32 - 1) / (JT / 32));
     return launch_after(a.D == DP ? attend_join_kernel<T, DP, true> : attend_join_kernel<T, DP, false>, join_grid, JT, join_bytes, st, a, heads_per_job);
