@@ -1,7 +1,9 @@
 """Binding of the operators the language model around the decoding step runs (include/disc.h):
 attention over prompts, the paged key-value cache and attention over it, log-probabilities.
 
-Argument marshalling only, like binding.py; there is no CPU fallback.
+Argument marshalling only, like binding.py; there is no CPU fallback.  Outputs made here belong to the stream the call is
+given (None: the current one).  A cache, a plan or an output used on another stream than the call before needs an event between
+the two.
 """
 from __future__ import annotations
 
@@ -44,7 +46,28 @@ def _want(t, n: int, name: str):
         raise TypeError(f"{name}: expected {n} entries, got {t.numel()}")
 
 
+def _empty(shape, dtype, device):
+    return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _alloc(stream, make, *args):
+    """make(*args) with its memory from the stream the kernel runs on: memory of another stream may still be in use there."""
+    if stream is None:
+        return make(*args)
+    with torch.cuda.stream(stream):
+        return make(*args)
+
+
 # ---- log-probabilities ------------------------------------------------------------------------------
+def _logprobs_outputs(n: int, top: int, targets: bool, dev):
+    f = torch.float32
+    return {"logp": torch.empty(n, dtype=f, device=dev) if targets else None,
+            "entropy": torch.empty(n, dtype=f, device=dev), "lse": torch.empty(n, dtype=f, device=dev),
+            "top_ids": torch.empty_strided((n, top), (top, 1), dtype=torch.int32, device=dev) if top > 0 else None,
+            "top_logp": torch.empty_strided((n, top), (top, 1), dtype=f, device=dev) if top > 0 else None,
+            "status": torch.empty(n, dtype=torch.uint8, device=dev)}
+
+
 def disc_logprobs(logits: torch.Tensor, targets: torch.Tensor | None = None, *, top: int = 0, inv_temperature=1.0,
                   out=None, stream=None):
     """logits [n, V] float32 or bfloat16 (any row stride), targets int32[n] (-1 = none) ->
@@ -53,12 +76,7 @@ def disc_logprobs(logits: torch.Tensor, targets: torch.Tensor | None = None, *, 
     n, V = logits.shape
     _want(targets, n, "targets")
     if out is None:
-        dev, f = logits.device, torch.float32
-        out = {"logp": torch.empty(n, dtype=f, device=dev) if targets is not None else None,
-               "entropy": torch.empty(n, dtype=f, device=dev), "lse": torch.empty(n, dtype=f, device=dev),
-               "top_ids": torch.empty_strided((n, top), (top, 1), dtype=torch.int32, device=dev) if top > 0 else None,
-               "top_logp": torch.empty_strided((n, top), (top, 1), dtype=f, device=dev) if top > 0 else None,
-               "status": torch.empty(n, dtype=torch.uint8, device=dev)}
+        out = _alloc(stream, _logprobs_outputs, n, top, targets is not None, logits.device)
     else:
         for k in ("logp", "entropy", "lse", "top_ids", "top_logp", "status"):
             _want(out[k], n * top if k.startswith("top") else n, k)
@@ -79,7 +97,7 @@ def disc_logprobs_grad(logits: torch.Tensor, targets, lse: torch.Tensor, entropy
     for t, name in ((targets, "targets"), (lse, "lse"), (entropy, "entropy"), (d_logp, "d_logp"), (d_entropy, "d_entropy")):
         _want(t, n, name)
     if out is None:
-        out = torch.empty((n, V), dtype=logits.dtype, device=logits.device)
+        out = _alloc(stream, _empty, (n, V), logits.dtype, logits.device)
     elif out.shape != logits.shape or out.dtype != logits.dtype:
         raise TypeError("out: expected the shape and dtype of the logits")
     optr, _, old = _rows(out, "out")
@@ -124,7 +142,8 @@ def disc_attend_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: 
                        scale: float | None = None, causal: bool = True, out=None, lse=None, stream=None):
     """Attention over packed sequences: q [n_q, Hq, D], k and v [n_k, Hkv, D] (bf16 or f16, slices of a fused projection are
     fine), cu_q / cu_k int32[n_seqs + 1] on the device (cu_k None: the same sequences), max_len: no sequence
-    has more queries -> (out [n_q, Hq, D], lse float[n_q, Hq])."""
+    has more queries -> (out [n_q, Hq, D], lse float[n_q, Hq]).  The first call on a device makes the word that
+    disc_attend_check reads and waits for it: it comes before any stream capture."""
     dt = _HALF.get(q.dtype)
     if dt is None:
         raise DiscError(-7, "disc_attend_prompt")
@@ -138,7 +157,7 @@ def disc_attend_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: 
     n_seqs = cu_q.numel() - 1
     if cu_k is not None:
         _want(cu_k, n_seqs + 1, "cu_k")
-    out, lse = _attend_outputs(q, out, lse)
+    out, lse = _alloc(stream, _attend_outputs, q, out, lse)
     rc = lib().disc_attend_prompt(qp, qt, qh, kp, kt, kh, vp, vt, vh, dt, hq, hkv, d, n_q, n_k, _dev(cu_q, torch.int32, "cu_q"), _dev(cu_k, torch.int32, "cu_k"), n_seqs,
                                   int(max_len), int(causal), 1.0 / math.sqrt(d) if scale is None else float(scale),
                                   _own(out), _own(lse), _error_word(q.device).data_ptr(),
@@ -215,7 +234,7 @@ def disc_cache_extend(cache: DiscCache, add: torch.Tensor | None = None, *, stat
     """Room for add[r] more tokens in every row (int32[n_rows] on the device, None: one each) -> status uint8[n_rows]."""
     _want(add, cache.n_rows, "add")
     if status is None:
-        status = torch.empty(cache.n_rows, dtype=torch.uint8, device=cache.pool.device)
+        status = _alloc(stream, _empty, cache.n_rows, torch.uint8, cache.pool.device)
     else:
         _want(status, cache.n_rows, "status")
     _check(lib().disc_cache_extend(cache._p, _dev(add, torch.int32, "add"), _dev(status, torch.uint8, "status"),
@@ -244,7 +263,7 @@ def disc_cache_write(cache: DiscCache, layer: int, k: torch.Tensor, v: torch.Ten
 def disc_cache_compact(cache: DiscCache, *, live: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """The n pages in use move to the ids 0 .. n-1 -> n as int32[1] on the device."""
     if live is None:
-        live = torch.empty(1, dtype=torch.int32, device=cache.pool.device)
+        live = _alloc(stream, _empty, 1, torch.int32, cache.pool.device)
     _check(lib().disc_cache_compact(cache._p, _dev(live, torch.int32, "live"), _stream_ptr(stream)), "disc_cache_compact")
     return live
 
@@ -268,7 +287,7 @@ def disc_attend_plan(cache: DiscCache, n_q_heads: int, *, group: int = 1, plan: 
     if plan is None:
         plan = cache._plans.get((n_q_heads, group))
         if plan is None:
-            plan = cache._plans[(n_q_heads, group)] = AttendPlan(cache, n_q_heads, group)
+            plan = cache._plans[(n_q_heads, group)] = _alloc(stream, AttendPlan, cache, n_q_heads, group)
     _check(lib().disc_attend_plan(cache._p, plan.n_q_heads, plan.group, plan.buf.data_ptr(), plan.nbytes, _stream_ptr(stream)),
            "disc_attend_plan")
     return plan
@@ -282,7 +301,7 @@ def disc_attend_cached(cache: DiscCache, layer: int, q: torch.Tensor, plan: Atte
     n, h, d = q.shape
     if n != cache.n_rows or h != plan.n_q_heads or d != cache.head_dim:
         raise TypeError("q: expected [rows, Hq, head dim] of the cache and the plan")
-    out, lse = _attend_outputs(q, out, lse)
+    out, lse = _alloc(stream, _attend_outputs, q, out, lse)
     _check(lib().disc_attend_cached(cache._p, int(layer), qp, qr, qh, plan.n_q_heads, plan.group,
                                     1.0 / math.sqrt(cache.head_dim) if scale is None else float(scale), plan.buf.data_ptr(),
                                     plan.nbytes, _own(out), _own(lse),
