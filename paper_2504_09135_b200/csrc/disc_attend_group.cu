@@ -9,7 +9,7 @@
 //      the rows hold in full go through the tensor cores as in the attention over prompts: S = Q K^T, a thread
 //      per query vector for the softmax, O += P V.  A row that has more than 8 full blocks of its own after those
 //      gets items of its own.  The whole is cut into equal shares.  Every item leaves normalised sums and log-sum-exps in fp32.
-//   2. A warp per row and key head joins them, in order, with what is left of the row: up to 8 full blocks of its own
+//   2. A warp per row and one or two key heads joins them, in order, with what is left of the row: up to 8 full blocks of its own
 //      and the partly filled one, by mma.sync.  Here, where rows have nothing in common, no row's values come near
 //      another row's sums.
 //
