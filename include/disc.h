@@ -472,8 +472,8 @@ int disc_cache_free(const disc_cache_t* c, const uint8_t* freed, void* stream);
 
 /* Room for add[r] more tokens in row r (add: device, int32[n_rows]; null = one each; <= 0 = none): len
  * grows, new pages are taken, and a row about to write into a partly filled page that other rows hold too
- * gets its own copy of the tokens in it, in all layers (when every holder of the page writes on, the lowest
- * row keeps it).  Rows are served in ascending order: once the pages still needed by a row and those before
+ * gets its own copy of the tokens in it, in all layers (when every holder of the page writes on, the longest of
+ * them, of equally long ones the lowest row, keeps it).  Rows are served in ascending order: once the pages still needed by a row and those before
  * it exceed the free ones, that row and later ones that need a page get DISC_ROW_NOPAGE and stay as they
  * are; so do rows that would outgrow the table.  status_out: device, uint8[n_rows]. */
 int disc_cache_extend(const disc_cache_t* c, const int32_t* add, uint8_t* status_out, void* stream);

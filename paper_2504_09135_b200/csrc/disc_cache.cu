@@ -30,7 +30,7 @@ struct Scratch {
     int32_t* len;         // [rows]
     int32_t* table;       // [rows][width]
     int32_t* sharers;     // [pages]
-    int32_t* keeper;      // [pages]
+    unsigned long long* keeper;   // [pages]
     int32_t* list;        // [pages] free pages in order / [pages] where a page goes
     int4* copy;           // [rows] source page, copy, tokens
     int2* move;           // [pages] from, to
@@ -50,7 +50,7 @@ inline int64_t scratch_layout(const disc_cache_t* c, Scratch* s) {
     t.len = reinterpret_cast<int32_t*>(take(rows * 4));
     t.table = reinterpret_cast<int32_t*>(take(rows * c->table_width * 4));
     t.sharers = reinterpret_cast<int32_t*>(take(pages * 4));
-    t.keeper = reinterpret_cast<int32_t*>(take(pages * 4));
+    t.keeper = reinterpret_cast<unsigned long long*>(take(pages * 8));
     t.list = reinterpret_cast<int32_t*>(take(pages * 4));
     if (s) *s = t;
     return at;
@@ -249,9 +249,16 @@ __device__ __forceinline__ Need row_need(const Books& b, const int32_t* add, int
     return n;
 }
 
-//  1. Rows that go on writing into a partly filled page mark it: how many rows do (sharers), and the lowest of
+// the longer row has the smaller key, of equally long ones the lower
+__device__ __forceinline__ unsigned long long keeper_key(const Books& b, const Need& n, int32_t row) {
+    return static_cast<unsigned long long>(b.page_size - (n.len & (b.page_size - 1))) << 32 | uint32_t(row);
+}
+
+//  1. Rows that go on writing into a partly filled page mark it: how many rows do (sharers), and the lowest of the longest of
 //     them (keeper).  If they are all the rows that hold the page, the keeper writes on in place; the others, and
-//     all of them where a row that stays behind holds the page too, get a copy.
+//     all of them where a row that stays behind holds the page too, get a copy.  The longest, because the rows of a page can differ in
+//     length (one that found no page stays behind the others), and one that finds no page for its copy now keeps its tokens
+//     only if nobody writes before its end.
 //  2. Prefix sums over the rows of the pages they need; rows beyond the number of free pages get nothing.
 //  3. The free pages of lowest id, in order, as many as are needed, and from them each row's share.
 // A thread has ROWS consecutive rows, in registers from the first step to the last, or, where there are more of them, reads
@@ -284,7 +291,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(XT) cache_extend_ke
             for (int32_t i = 0; i < n_rows; ++i) f(r0 + i, row_need(b, add, r0 + i));
         }
     };
-    each([&](int32_t, const Need& n) { if (n.page >= 0) { s.sharers[n.page] = 0; s.keeper[n.page] = 0x7fffffff; } });
+    each([&](int32_t, const Need& n) { if (n.page >= 0) { s.sharers[n.page] = 0; s.keeper[n.page] = ~0ull; } });
     if (rank == 0 && tid == 0) s.head[0] = 0;
 
     // the free pages of this block's share
@@ -299,14 +306,14 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(XT) cache_extend_ke
     if (tid == 0) own_free = n_free;
 
     sync_blocks<CL>();
-    each([&](int32_t row, const Need& n) { if (n.page >= 0) { atomicAdd(s.sharers + n.page, 1); atomicMin(s.keeper + n.page, row); } });
+    each([&](int32_t row, const Need& n) { if (n.page >= 0) { atomicAdd(s.sharers + n.page, 1); atomicMin(s.keeper + n.page, keeper_key(b, n, row)); } });
     sync_blocks<CL>();
 
     auto copies = [&](const Need& n, int32_t row) {
         if (n.page < 0) return 0;
         const int32_t ref = b.ref[n.page];
         if (ref <= 1) return 0;
-        return s.sharers[n.page] == ref && s.keeper[n.page] == row ? 0 : 1;
+        return s.sharers[n.page] == ref && s.keeper[n.page] == keeper_key(b, n, row) ? 0 : 1;
     };
     int32_t held_copy[HELD];
     mine = 0;
