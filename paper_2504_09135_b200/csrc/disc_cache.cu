@@ -431,7 +431,7 @@ struct WriteParams {
 __global__ void __launch_bounds__(256) cache_write_kernel(Books b, WriteParams w) {
     let_later_in();
     wait_for_earlier();
-    const int32_t t = int32_t((blockIdx.x * blockDim.x + threadIdx.x) >> 5);
+    const int32_t t = int32_t((int64_t(blockIdx.x) * blockDim.x + threadIdx.x) >> 5);       // up to 2^30 tokens: 2^35 threads
     const int lane = threadIdx.x & 31;
     if (t >= w.tokens) return;
     int32_t seq = t, back = 1;                  // the token is the back-th from the end of its sequence

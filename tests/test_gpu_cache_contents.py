@@ -92,3 +92,13 @@ def test_a_random_life_in_few_pages(rows, pages, width, seed):
             x.fork([int(a) for a in rng.permutation(rows)])
         else:
             x.fork([int(a) for a in np.where(rng.random(rows) < 0.2, -1, rng.integers(0, rows, rows))])
+
+
+def test_writing_more_tokens_than_threads_can_be_counted_in_32_bits():
+    """2^27 tokens take 2^32 threads.  The row holds the last 16 of them; the tokens before have no place and are skipped."""
+    n = (1 << 27) + 16
+    cache = disc.DiscCache.empty(1, 1, P, 1, 8, 1, 1)
+    disc.disc_cache_extend(cache, torch.tensor([16], dtype=torch.int32, device=DEV))
+    k = torch.full((1, 1, 8), 3.0, dtype=torch.bfloat16, device=DEV).expand(n, 1, 8)
+    disc.disc_cache_write(cache, 0, k, k, cu=torch.tensor([0, n], dtype=torch.int32, device=DEV))
+    assert torch.all(cache.pool == 3.0)
