@@ -3,9 +3,10 @@
 // the log-probabilities and entropies with respect to the logits.
 //
 // With y_v = z_v log2(e) / T and m = max y:   S = sum 2^(y-m),  U = sum (y-m) 2^(y-m),
-//   lse = ln2 (m + log2 S)     H = ln2 (log2 S - U / S)     log p_t = z_t / T - lse
+//   lse = ln2 (m + log2 S)     H = ln2 (log2 S - U / S)     log p_t = (z_t - max z) / T - ln2 log2 S
 // so that one pass with a running maximum gives all three.  In units of y - m both sums stay between
-// 0 and the number of tokens, and H loses nothing to a large lse.
+// 0 and the number of tokens, and neither H nor a log-probability loses anything to a large lse, which fp32 holds only to 2^-24 of
+// its size (2e-3 for logits near 30 at T = 1/1000; log S altogether for rows masked with a finite value).
 //
 // The pass is bound by the bytes of the logits.  What it may spend per logit is little: at the
 // measured copy rate 11 bf16 logits arrive per SM and clock, and an SM takes 2^x sixteen times and
@@ -422,15 +423,25 @@ __device__ __noinline__ void select_slice(const char* base, int32_t e0, int32_t 
 // ---- what a row's sums give -----------------------------------------------------------------------------
 struct RowResult {
     float lse, entropy;
+    float m, log_sum;                 // the largest logit; ln of the sum relative to it
     uint8_t status;
 };
-// far: t's sums are relative to its largest logit itself, not to the clamped reference
+// far: t's sums are relative to its largest logit itself, not to the clamped and rounded reference
 __device__ __forceinline__ RowResult row_result(const LogprobParams& p, const Sums& t, bool far) {
     if (t.s != t.s || t.u != t.u || t.m == CUDART_INF_F)
-        return {t.m == CUDART_INF_F && t.s == t.s ? CUDART_INF_F : CUDART_NAN_F, CUDART_NAN_F, DISC_ROW_NONFINITE};
-    if (!(t.m > -CUDART_INF_F)) return {-CUDART_INF_F, 0.f, DISC_ROW_NOMASS};
+        return {t.m == CUDART_INF_F && t.s == t.s ? CUDART_INF_F : CUDART_NAN_F, CUDART_NAN_F, 0.f, 0.f, DISC_ROW_NONFINITE};
+    if (!(t.m > -CUDART_INF_F)) return {-CUDART_INF_F, 0.f, 0.f, 0.f, DISC_ROW_NOMASS};
     const float l2 = log2f(t.s);
-    return {far ? fmaf(t.m, p.inv_t, l2 * LN2_F) : fmaf(t.ref, LN2_F, l2 * LN2_F), fmaxf(0.f, LN2_F * (l2 - t.u / t.s)), 0};
+    // the reference is m c2 rounded; what the rounding took is exact in one multiply-add
+    const float log_sum = LN2_F * (far ? l2 : l2 - fmaf(t.m, p.c2, -t.ref));
+    return {fmaf(t.m, p.inv_t, log_sum), fmaxf(0.f, LN2_F * (l2 - t.u / t.s)), t.m, log_sum, 0};
+}
+// the log-probability of a logit of the row
+__device__ __forceinline__ float log_prob(const LogprobParams& p, const RowResult& r, float x) {
+    if (r.status & DISC_ROW_NOMASS) return -CUDART_INF_F;
+    if (r.status & DISC_ROW_NONFINITE) return x * p.inv_t - r.lse;
+    const float lp = fmaf(x - r.m, p.inv_t, -r.log_sum);
+    return lp > 0.f ? 0.f : lp;       // roundings of the largest one's
 }
 // one thread
 template <int DT>
@@ -440,10 +451,8 @@ __device__ __forceinline__ void store_row(const LogprobParams& p, int64_t row, c
     if (p.targets) {
         const int32_t tok = p.targets[row];
         float lp = 0.f;
-        if (tok >= 0 && tok < p.V) {
-            const float x = Vec<DT>::at(base + size_t(tok) * Vec<DT>::SIZE);
-            lp = r.status & DISC_ROW_NOMASS ? -CUDART_INF_F : x * p.inv_t - r.lse;
-        } else if (tok != -1) {
+        if (tok >= 0 && tok < p.V) lp = log_prob(p, r, Vec<DT>::at(base + size_t(tok) * Vec<DT>::SIZE));
+        else if (tok != -1) {
             lp = CUDART_NAN_F;
             r.status |= DISC_ROW_DEAD;
         }
@@ -455,7 +464,7 @@ __device__ __forceinline__ void store_row(const LogprobParams& p, int64_t row, c
 __device__ __forceinline__ void store_top(const LogprobParams& p, int64_t row, unsigned int i, unsigned long long e, bool some, const RowResult& r) {
     p.top_ids[row * p.top + i] = some ? int32_t(~uint32_t(e)) : -1;
     if (p.top_logp)
-        p.top_logp[row * p.top + i] = some && !(r.status & DISC_ROW_NOMASS) ? key_value(uint32_t(e >> 32)) * p.inv_t - r.lse : -CUDART_INF_F;
+        p.top_logp[row * p.top + i] = some ? log_prob(p, r, key_value(uint32_t(e >> 32))) : -CUDART_INF_F;
 }
 
 // ---- short rows --------------------------------------------------------------------------------------------

@@ -1,0 +1,73 @@
+"""Log-probabilities of rows whose log-sum-exp is large: masks of a finite value, low temperatures.  fp32 holds such a
+log-sum-exp only to some 2^-24 of its size, but log-probabilities hang on differences of logits."""
+import math
+
+import pytest
+import torch
+
+import paper_2504_09135_b200 as disc
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def reference(z, inv_t):
+    """log p, p and entropy in 64 bits, from differences to the row's maximum."""
+    d = (z.double() - z.double().amax(dim=1, keepdim=True)) * float(torch.tensor(inv_t, dtype=torch.float32))
+    lp = d - torch.logsumexp(d, dim=1, keepdim=True)
+    p = lp.exp()
+    return lp, p, -(p * torch.where(p > 0, lp, 0.0)).sum(dim=1)
+
+
+def base(V):
+    """What fp32 sums of V terms in 256 threads and 2^x to 2^-22 allow, whatever the size of the logits."""
+    return 2.0 ** -20 + (V / 256 + 40) * 2.0 ** -24
+
+
+def check(z, t, inv_t, top):
+    """A log-probability is log2(e)/T times a difference of logits (three roundings of 2^-24, twice) plus the logarithm of the sum."""
+    n, V = z.shape
+    r = disc.disc_logprobs(z, t, top=top, inv_temperature=inv_t)
+    lp, p, H = reference(z, inv_t)
+    assert torch.all(r["status"] == 0)
+    want = lp.gather(1, t.long()[:, None])[:, 0]
+    assert torch.all((r["logp"].double() - want).abs() <= base(V) + 2.0 ** -21 * want.abs())
+    assert torch.all(r["logp"] <= 0)
+    assert torch.all((r["entropy"].double() - H).abs() <= base(V) * (2 + 2 * math.log(V + 1)))
+    want = lp.gather(1, r["top_ids"].long())
+    assert torch.all((r["top_logp"].double() - want).abs() <= base(V) + 2.0 ** -21 * want.abs())
+    return r
+
+
+SIZES = [(3, 7), (5, 300), (4, 1000), (3, 3000), (2, 32001), (200, 20000), (1, 128256)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,V", SIZES)
+@pytest.mark.parametrize("value", [-1e9, "lowest", -2e4, 1e6])
+def test_rows_of_one_large_value(dtype, n, V, value):
+    z = torch.full((n, V), torch.finfo(dtype).min if value == "lowest" else value, dtype=dtype, device=DEV)
+    t = torch.randint(0, V, (n,), dtype=torch.int32, device=DEV)
+    r = check(z, t, 1.0, min(4, V))
+    assert torch.all((r["logp"] + math.log(V)).abs() <= base(V) + 2.0 ** -21 * math.log(V))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,V", SIZES)
+def test_masks_of_a_finite_value_beside_logits(dtype, n, V):
+    z = (torch.randn((n, V), device=DEV) * 3).to(dtype)
+    z[:, ::2] = -1e9
+    z[n // 2] = -1e9                                    # nothing left of one row
+    t = (torch.randint(0, V // 2, (n,), device=DEV) * 2 + 1).to(torch.int32)
+    check(z, t, 1.0, min(3, V))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,V", SIZES)
+@pytest.mark.parametrize("inv_t", [1000.0, 40.0])
+def test_low_temperatures(dtype, n, V, inv_t):
+    """Logits near 30 that differ by hundredths: at T = 1/1000 their log-sum-exp is some 3e4."""
+    z = (30 + torch.randn((n, V), device=DEV) * 0.02).to(dtype)
+    z[0] = (torch.randn(V, device=DEV) * 3).to(dtype)
+    t = torch.randint(0, V, (n,), dtype=torch.int32, device=DEV)
+    check(z, t, inv_t, min(5, V))
