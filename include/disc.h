@@ -394,6 +394,7 @@ int disc_logprobs(const void* logits, disc_dtype_t dtype, int64_t ld, int64_t n,
  *   grad[i][v] = (d_logp [v = target] - p_v (d_logp + d_entropy (log p_v + entropy))) / T
  *   lse, entropy   device, float[n]: what disc_logprobs returned for these logits (entropy nullable
  *               without d_entropy)
+ *               (rows with |lse| >= 128, which fp32 holds too coarsely, have their sum formed anew)
  *   d_logp      device, float[n] (nullable; needs targets); rows without a target ignore it
  *   d_entropy   device, float[n] (nullable)
  *   grad_out    device, n rows of vocab_size values of type `dtype`, row i at element offset

@@ -761,13 +761,62 @@ struct GradParams {
 };
 
 struct RowGrad {
-    float l2, a_bh, b, scale;         // lse in units of y; a + b H; b ln2; 1/T
-    float far_lse;                    // lse where l2 has no place in fp32, otherwise 0
+    float m, l2;                      // y - log2 sum = (x - m) c2 - l2: m = 0 and the log-sum-exp, or the row's maximum and its own sum
+    float a_bh, b, scale;             // a + b H; b ln2; 1/T
     __device__ __forceinline__ float at(float x, float c2) const {
-        const float y = max_nan(far_lse == 0.f ? fmaf(x, c2, -l2) : fmaf(x, scale, -far_lse) * LOG2E_F, Y_MIN);
+        const float y = max_nan(fmaf(x - m, c2, -l2), Y_MIN);
         return -scale * ex2_approx(y) * fmaf(y, b, a_bh);
     }
 };
+// A log-sum-exp is given rounded to fp32, which puts a factor 1 +- |lse| 2^-24 on all probabilities of the row: 8e-6 up to this
+// limit.  For rows beyond it (low temperatures, rows masked with a finite value, where log S would be lost) one team takes the
+// whole row, forms maximum and sum anew and then the gradient; the row's other teams have nothing to do.  (4096 x 32000 bf16: 88 us
+// when all rows are within the limit, 128 when all are beyond it; 16 x 128256: 12 and 29.)
+constexpr float LSE_LIMIT = 128.f;
+
+// the row's maximum and log2 of its sum of 2^((x - m) c2); called by the whole team
+template <int DT, int TEAM>
+__device__ __noinline__ float2 row_norm(const RowShape<DT>& r, int tid, int32_t extra, float c2) {
+    constexpr int E = Vec<DT>::E, SIZE = Vec<DT>::SIZE, UN = 2;
+    float m = -CUDART_INF_F, s = 0.f;
+    auto up_to = [&](float mx) {
+        if (mx > m) { s *= ex2_approx((m - mx) * c2); m = mx; }
+        return m > -CUDART_INF_F ? m : 0.f;
+    };
+    if (extra >= 0) {
+        const float x = Vec<DT>::at(r.base + size_t(extra) * SIZE), ref = up_to(x);
+        s += ex2_approx((x - ref) * c2);
+    }
+    for (int32_t v = tid; v < r.nvec; v += UN * TEAM) {
+        uint4 w[UN];
+#pragma unroll
+        for (int u = 0; u < UN; ++u) w[u] = v + u * TEAM < r.nvec ? r.vecs()[v + u * TEAM] : Vec<DT>::lowest();
+        const float ref = up_to(Vec<DT>::template largest<UN>(w));
+#pragma unroll
+        for (int u = 0; u < UN; ++u) {
+            float x[E];
+            Vec<DT>::unpack(w[u], x);
+#pragma unroll
+            for (int j = 0; j < E; ++j) s += ex2_approx((x[j] - ref) * c2);
+        }
+    }
+    auto join = [&](float m2, float s2) {
+        const float top = fmaxf(m, m2), ref = top > -CUDART_INF_F ? top : 0.f;
+        s = s * ex2_approx((m - ref) * c2) + s2 * ex2_approx((m2 - ref) * c2);
+        m = top;
+    };
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) join(__shfl_xor_sync(FULL, m, o), __shfl_xor_sync(FULL, s, o));
+    if (TEAM == NT) {
+        __shared__ float2 warps[NW];
+        if ((tid & 31) == 0) warps[tid >> 5] = make_float2(m, s);
+        __syncthreads();
+        m = -CUDART_INF_F;
+        s = 0.f;
+        for (int w = 0; w < NW; ++w) join(warps[w].x, warps[w].y);
+    }
+    return make_float2(m, log2f(s));
+}
 
 // TEAM threads work on a portion of a row: a block, or a warp where a warp's loads cover the row.
 template <int DT, int TEAM>
@@ -784,44 +833,54 @@ __global__ void __launch_bounds__(NT) disc_logprobs_grad_kernel(const GradParams
     const float a = p.d_logp && tok >= 0 && tok < p.V ? p.d_logp[row] : 0.f;
     const float b = p.d_entropy ? p.d_entropy[row] : 0.f;
     const float lse = p.lse[row];
+    int32_t extra = -1;               // a thread's element before or after the vectors
+    if (part == 0) {
+        if (tid < r.head) extra = tid;
+        else if (tid - r.head < r.tail) extra = r.head + r.nvec * E + tid - r.head;
+    }
     RowGrad g;
+    g.m = 0.f;
     g.l2 = lse * LOG2E_F;
     g.a_bh = b != 0.f ? fmaf(b, p.entropy[row], a) : a;
     g.b = b * LN2_F;
     g.scale = p.inv_t;
-    g.far_lse = fabsf(g.l2) >= FAR_Y && fabsf(lse) < CUDART_INF_F ? lse : 0.f;
     if (lse == -CUDART_INF_F) { g.l2 = 0.f; g.scale = 0.f; }      // no mass: nothing to move
+    const bool anew = fabsf(lse) >= LSE_LIMIT && fabsf(lse) < CUDART_INF_F;
+    if (anew) {
+        if (part != 0) return;
+        const float2 norm = row_norm<DT, TEAM>(r, tid, extra, p.c2);
+        g.m = norm.x;
+        g.l2 = norm.y;
+    }
     const float a_t = g.scale * a;
 
     const bool together = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(r.base)) & 15) == 0;
     const uint4* vecs = r.vecs();
     char* out_vecs = out + size_t(r.head) * SIZE;
-    uint4 w[U];
-    const int32_t v0 = part * (TEAM * U) + tid;
+    int32_t v0 = part * (TEAM * U) + tid;
+    do {
+        uint4 w[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-        if (v0 + u * TEAM < r.nvec) w[u] = ld_stream(vecs + v0 + u * TEAM);
+        for (int u = 0; u < U; ++u)
+            if (v0 + u * TEAM < r.nvec) w[u] = ld_stream(vecs + v0 + u * TEAM);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int32_t v = v0 + u * TEAM;
-        if (v < r.nvec) {
-            float x[E];
-            Vec<DT>::unpack(w[u], x);
-            const int32_t at = tok - (r.head + v * E);
+        for (int u = 0; u < U; ++u) {
+            const int32_t v = v0 + u * TEAM;
+            if (v < r.nvec) {
+                float x[E];
+                Vec<DT>::unpack(w[u], x);
+                const int32_t at = tok - (r.head + v * E);
 #pragma unroll
-            for (int j = 0; j < E; ++j) x[j] = g.at(x[j], p.c2) + (at == j ? a_t : 0.f);
-            if (together) __stcs(reinterpret_cast<uint4*>(out_vecs) + v, Vec<DT>::pack(x));
-            else
+                for (int j = 0; j < E; ++j) x[j] = g.at(x[j], p.c2) + (at == j ? a_t : 0.f);
+                if (together) __stcs(reinterpret_cast<uint4*>(out_vecs) + v, Vec<DT>::pack(x));
+                else
 #pragma unroll
-                for (int j = 0; j < E; ++j) Vec<DT>::put(out_vecs + (size_t(v) * E + j) * SIZE, x[j]);
+                    for (int j = 0; j < E; ++j) Vec<DT>::put(out_vecs + (size_t(v) * E + j) * SIZE, x[j]);
+            }
         }
-    }
-    if (part == 0) {
-        int32_t e = -1;
-        if (tid < r.head) e = tid;
-        else if (tid - r.head < r.tail) e = r.head + r.nvec * E + tid - r.head;
-        if (e >= 0) Vec<DT>::put(out + size_t(e) * SIZE, g.at(Vec<DT>::at(r.base + size_t(e) * SIZE), p.c2) + (e == tok ? a_t : 0.f));
-    }
+        v0 += TEAM * U;
+    } while (anew && v0 < r.nvec);
+    if (extra >= 0) Vec<DT>::put(out + size_t(extra) * SIZE, g.at(Vec<DT>::at(r.base + size_t(extra) * SIZE), p.c2) + (extra == tok ? a_t : 0.f));
 }
 
 template <int DT, int EPL>

@@ -1,5 +1,5 @@
-"""Log-probabilities of rows whose log-sum-exp is large: masks of a finite value, low temperatures.  fp32 holds such a
-log-sum-exp only to some 2^-24 of its size, but log-probabilities hang on differences of logits."""
+"""Log-probabilities and gradients of rows whose log-sum-exp is large: masks of a finite value, low temperatures.  fp32 holds such a
+log-sum-exp only to some 2^-24 of its size, but log-probabilities, probabilities and gradients hang on differences of logits."""
 import math
 
 import pytest
@@ -9,6 +9,7 @@ import paper_2504_09135_b200 as disc
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
+UNIT = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
 
 
 def reference(z, inv_t):
@@ -36,6 +37,24 @@ def check(z, t, inv_t, top):
     assert torch.all((r["entropy"].double() - H).abs() <= base(V) * (2 + 2 * math.log(V + 1)))
     want = lp.gather(1, r["top_ids"].long())
     assert torch.all((r["top_logp"].double() - want).abs() <= base(V) + 2.0 ** -21 * want.abs())
+    a, b = torch.randn(n, device=DEV), torch.randn(n, device=DEV)
+    one = torch.zeros_like(lp)
+    one.scatter_(1, t.long()[:, None], 1.0)
+    for db in (None, b):
+        a64 = a.double()[:, None]
+        b64 = torch.zeros_like(a64) if db is None else db.double()[:, None]
+        step = torch.where(p > 0, lp, 0.0)
+        want = ((one - p) * a64 - p * (step + H[:, None]) * b64) * inv_t
+        # of a probability: its own log's error; of the entropy's part the errors of log p and H
+        rel = base(V) + 2.0 ** -21 * step.abs()
+        tol = inv_t * p * (rel * (a64.abs() + b64.abs() * (step.abs() + H[:, None])) + b64.abs() * (rel + base(V) * (2 + 2 * math.log(V + 1))))
+        tol = tol + UNIT[z.dtype] * want.abs() + 2.0 ** -23 * inv_t * a64.abs() * one + 1e-30
+        g = disc.disc_logprobs_grad(z, t, r["lse"], r["entropy"], a, db, inv_temperature=inv_t)
+        err = (g.double() - want).abs()
+        assert torch.all(err <= tol), float((err - tol).max())
+        same = z.clone()                                # in place
+        disc.disc_logprobs_grad(same, t, r["lse"], r["entropy"], a, db, inv_temperature=inv_t, out=same)
+        assert torch.equal(same, g)
     return r
 
 
@@ -50,6 +69,8 @@ def test_rows_of_one_large_value(dtype, n, V, value):
     t = torch.randint(0, V, (n,), dtype=torch.int32, device=DEV)
     r = check(z, t, 1.0, min(4, V))
     assert torch.all((r["logp"] + math.log(V)).abs() <= base(V) + 2.0 ** -21 * math.log(V))
+    g = disc.disc_logprobs_grad(z, t, r["lse"], r["entropy"], torch.ones(n, device=DEV))
+    assert torch.all(g.double().sum(dim=1).abs() <= 2 * (UNIT[dtype] + base(V)))
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
