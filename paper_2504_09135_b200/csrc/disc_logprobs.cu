@@ -845,6 +845,7 @@ __global__ void __launch_bounds__(NT) disc_logprobs_grad_kernel(const GradParams
     g.b = b * LN2_F;
     g.scale = p.inv_t;
     if (lse == -CUDART_INF_F) { g.l2 = 0.f; g.scale = 0.f; }      // no mass: nothing to move
+    else if (!(lse < CUDART_INF_F)) g.l2 = CUDART_NAN_F;          // +inf or NaN among the logits: no gradient is finite
     const bool anew = fabsf(lse) >= LSE_LIMIT && fabsf(lse) < CUDART_INF_F;
     if (anew) {
         if (part != 0) return;

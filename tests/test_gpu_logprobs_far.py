@@ -92,3 +92,18 @@ def test_low_temperatures(dtype, n, V, inv_t):
     z[0] = (torch.randn(V, device=DEV) * 3).to(dtype)
     t = torch.randint(0, V, (n,), dtype=torch.int32, device=DEV)
     check(z, t, inv_t, min(5, V))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [50, 5000, 40000])
+def test_rows_without_a_finite_sum_have_no_finite_gradient(dtype, V):
+    z = torch.randn((4, V), device=DEV).to(dtype)
+    z[0, V // 2] = math.inf
+    z[1, V // 3] = math.nan
+    z[2] = -math.inf
+    t = torch.zeros(4, dtype=torch.int32, device=DEV)
+    r = disc.disc_logprobs(z, t)
+    for b in (None, torch.ones(4, device=DEV)):
+        g = disc.disc_logprobs_grad(z, t, r["lse"], r["entropy"], torch.ones(4, device=DEV), b)
+        assert not torch.isfinite(g[:2]).any()
+        assert torch.all(g[2] == 0) and torch.isfinite(g[3]).all()
