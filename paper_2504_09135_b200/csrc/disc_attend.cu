@@ -266,8 +266,8 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
         auto entry = [&](int t) {
             const int i = item.y + t * TILE_BLKS + warp;
             if (i >= item.z) return make_int2(0, 0);
-            if (sh.per_group > 1) return __ldg(list + i);
-            return make_int2(__ldg(table + i / sh.blks_per_page), i % sh.blks_per_page | min(BLK, len - i * BLK) << 8);
+            if (sh.per_group > 1) return list[i];
+            return make_int2(table[i / sh.blks_per_page], i % sh.blks_per_page | min(BLK, len - i * BLK) << 8);
         };
         auto load_tile = [&](int t, int2 e) {
             const int stage = t % STAGES;

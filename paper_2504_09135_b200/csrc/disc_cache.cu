@@ -99,8 +99,8 @@ __device__ __forceinline__ void settle_row(const Books& b, const Scratch& s, int
 }
 // step 0: the first, 1: the second, 2: both, in one block
 template <int STEP>
-__global__ void __launch_bounds__(STEP == 2 ? 1024 : 256) cache_fork_kernel(Books b, const int32_t* __restrict__ parent,
-                                                                           const uint8_t* __restrict__ freed, Scratch s) {
+__global__ void __launch_bounds__(STEP == 2 ? 1024 : 256) cache_fork_kernel(Books b, const int32_t* parent,
+                                                                           const uint8_t* freed, Scratch s) {
     let_later_in();
     wait_for_earlier();
     const int32_t row = int32_t((blockIdx.x * blockDim.x + threadIdx.x) >> 5);
@@ -264,8 +264,8 @@ __device__ __forceinline__ unsigned long long keeper_key(const Books& b, const N
 // A thread has ROWS consecutive rows, in registers from the first step to the last, or, where there are more of them, reads
 // them again in every step.
 template <int CL, int ROWS>
-__global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(XT) cache_extend_kernel(Books b, const int32_t* __restrict__ add, Scratch s,
-                                                                                  uint8_t* __restrict__ status, Pool o, bool copy_here) {
+__global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(XT) cache_extend_kernel(Books b, const int32_t* add, Scratch s,
+                                                                                  uint8_t* status, Pool o, bool copy_here) {
     let_later_in();
     wait_for_earlier();
     __shared__ int32_t warp_sums[32];
@@ -465,7 +465,7 @@ __global__ void __launch_bounds__(256) cache_write_kernel(Books b, WriteParams w
 // One cluster: the number n of live pages; the live pages at n and above, in order, are to go to the free pages below
 // n, in order; their reference counts go along.
 template <int CL>
-__global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(XT) cache_plan_compact_kernel(Books b, Scratch s, int32_t* __restrict__ live_out) {
+__global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(XT) cache_plan_compact_kernel(Books b, Scratch s, int32_t* live_out) {
     let_later_in();
     wait_for_earlier();
     __shared__ int32_t warp_sums[32];
@@ -538,7 +538,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(XT) cache_plan_comp
     if (rank == 0 && tid == 0) { s.head[1] = live; s.head[2] = n_movers; *live_out = live; }
 }
 // The moves, a block per page and plane, and the new page numbers in the table.
-__global__ void __launch_bounds__(256) cache_move_kernel(Books b, unsigned char* __restrict__ pool, Scratch s, int32_t planes,
+__global__ void __launch_bounds__(256) cache_move_kernel(Books b, unsigned char* pool, Scratch s, int32_t planes,
                                                          int64_t plane_bytes, int32_t page_bytes) {
     let_later_in();
     wait_for_earlier();

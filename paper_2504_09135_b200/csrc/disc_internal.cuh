@@ -103,6 +103,9 @@ inline int allow_smem(F* kernel, int bytes, std::atomic<uint64_t>& done) {
 // Launches that follow one another closely: the kernel's blocks may move in while the last ones of the kernel before are still
 // at work (programmatic stream serialisation), which hides a launch's latency.  Such a kernel begins with
 // wait_for_earlier(), before it touches global memory, and lets its own successor in with let_later_in().
+// It may be resident while the kernels before it still write what it is to read, and so takes none of its pointers as const
+// __restrict__ and reads nothing with __ldg: such loads (ld.global.nc) are for memory that nobody writes while the kernel
+// lives, and the compiler may move them above the wait.
 template <class... P, class... A>
 inline int launch_after(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, cudaStream_t st, A... args) {
     cudaLaunchConfig_t cfg = {};
