@@ -96,6 +96,15 @@ __device__ __forceinline__ uint4 ld_stream(const uint4* p) {
                  : "l"(p));
     return v;
 }
+// the same for memory that the kernel itself may write: a gradient over its own logits
+__device__ __forceinline__ uint4 ld_stream_own(const uint4* p) {
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "l"(p)
+                 : "memory");
+    return v;
+}
 
 template <int DT>
 struct Vec;
@@ -863,7 +872,7 @@ __global__ void __launch_bounds__(NT) disc_logprobs_grad_kernel(const GradParams
         uint4 w[U];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (v0 + u * TEAM < r.nvec) w[u] = ld_stream(vecs + v0 + u * TEAM);
+            if (v0 + u * TEAM < r.nvec) w[u] = ld_stream_own(vecs + v0 + u * TEAM);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int32_t v = v0 + u * TEAM;
