@@ -167,15 +167,21 @@ def disc_attend_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: 
 
 
 def disc_attend_check(device="cuda", stream=None, *, plan: "AttendPlan | None" = None):
-    """Synchronises and raises DiscError when a prompt attention on the device, or a cached attention with this plan, gave up on
-    one of its bounded waits."""
+    """Synchronises and raises DiscError when a prompt attention on the device, or a cached attention with this plan, has given up
+    on one of its bounded waits since the last check."""
     if plan is not None:
-        _check(lib().disc_attend_error(plan.buf.data_ptr(), _stream_ptr(stream)), "disc_attend_error")
-        return
-    dev = torch.device(device)
-    if dev.index is None:
-        dev = torch.device(dev.type, torch.cuda.current_device())
-    _check(lib().disc_attend_error(_error_word(dev).data_ptr(), _stream_ptr(stream)), "disc_attend_error")
+        word = plan.buf[:4].view(torch.int32)
+    else:
+        dev = torch.device(device)
+        if dev.index is None:
+            dev = torch.device(dev.type, torch.cuda.current_device())
+        word = _error_word(dev)
+    rc = lib().disc_attend_error(word.data_ptr(), _stream_ptr(stream))
+    try:
+        if rc:
+            _alloc(stream, word.zero_)          # reported once
+    finally:
+        _check(rc, "disc_attend_error")
 
 
 # ---- the key-value cache ----------------------------------------------------------------------------
