@@ -498,7 +498,8 @@ int disc_cache_compact(const disc_cache_t* c, int32_t* live_out, void* stream);
  * rows) has in common, and how the work is split.  It depends on the books only: make it once per position, after
  * disc_cache_extend, and use it for every layer.
  *   plan    device, disc_attend_plan_bytes() bytes, 32-byte aligned.  Its first 4 bytes are an error word as
- *           disc_attend_prompt's, cleared here and set by disc_attend_cached; read with disc_attend_error
+ *           disc_attend_prompt's: the caller sets it to 0 before the first plan is made in the buffer, disc_attend_cached sets
+ *           it to 1, and no call clears it, so that it can be read (disc_attend_error) once after many positions
  * Errors: DISC_ERR_ARG; DISC_ERR_UNSUPPORTED for more than 64 query heads per key head, or tables of more than 2^30 blocks of
  * 16 tokens. */
 int64_t disc_attend_plan_bytes(const disc_cache_t* c, int32_t n_q_heads, int32_t group);

@@ -161,7 +161,6 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(PT) attend_plan_ker
         }
     }
     for (int32_t i = lanes + tid; i <= sh.lanes; i += PT) p.plan.first[i] = items;
-    if (tid == 0) p.plan.head[0] = 0;
 }
 
 // ---- attention --------------------------------------------------------------------------------------

@@ -36,7 +36,7 @@ struct RowItem {                       // rows [row, row + rows) of group g over
 };
 
 struct Plan {
-    int32_t* head;                     // [0] error word
+    int32_t* head;                     // [0] error word: the caller's to clear, no kernel does
     int32_t* first;                    // [lanes + 1] first item of a lane; lanes without work begin where all items end
     float* part;                       // [max_part][head_dim] normalised sums, fp32
     float* part_lse;                   // [max_part] log-sum-exp in units of log2

@@ -162,7 +162,6 @@ __global__ void __launch_bounds__(PT) group_items_kernel(const PlanParams p) {
     }
     __syncthreads();
     for (int32_t i = lanes + tid; i <= sh.lanes; i += PT) p.plan.first[i] = items;
-    if (tid == 0) p.plan.head[0] = 0;
 }
 
 // ---- kernel 1 -----------------------------------------------------------------------------------------

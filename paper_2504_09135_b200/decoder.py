@@ -16,7 +16,7 @@ from __future__ import annotations
 
 import torch
 
-from .model_ops import DiscCache, disc_attend_plan, disc_cache_compact, disc_cache_extend, disc_cache_fork
+from .model_ops import DiscCache, attend_error_word, disc_attend_plan, disc_cache_compact, disc_cache_extend, disc_cache_fork
 from .binding import (DiscSet, DiscState, StepOutputs, disc_accept_resample, disc_project_scratch, disc_project_step,
                       disc_resample, disc_state_init, disc_step, disc_step_topm, lib)
 
@@ -131,8 +131,9 @@ class DiscDecoder:
         holds the drawn candidate, the other rows are empty and the pages in use have moved together.
 
         Returns disc_resample's results with `cache_status` (uint8[B*K]: ROW_NOPAGE where the cache had no room for a
-        token, whose row is then not to be used) and `live_pages`.  on_step(t, logits, outputs) is called after every
-        position.  The host waits for nothing."""
+        token, whose row is then not to be used), `live_pages` and `attend_error` (int32[1]: not 0 when a bounded wait of an
+        attention kernel ran out at any position, or since the last disc_attend_check; the results are then invalid).
+        on_step(t, logits, outputs) is called after every position.  The host waits for nothing."""
         B, K, R = self.B, self.K, self.R
         if cache.n_rows != R:
             raise ValueError(f"decode_cached: the cache has {cache.n_rows} rows, the decoder {R}")
@@ -149,6 +150,7 @@ class DiscDecoder:
         status = status.view(B, K)[:, :1].expand(B, K).reshape(R).contiguous()
         hidden = hidden.index_select(0, cu[1:].long() - 1).repeat_interleave(K, dim=0)
         prev = None
+        error = attend_error_word(prompts.device)
         for t in range(self.set.l_max):
             if t > 0:
                 add = ((self.state.done == 0) & (status == 0)).to(torch.int32)
@@ -161,11 +163,12 @@ class DiscDecoder:
             if on_step is not None:
                 on_step(t, logits, o)
             prev = o.token.clamp(min=0) if prev is None else torch.where(o.token >= 0, o.token, prev)
+        error = error | plan.error if self.set.l_max > 1 else error.clone()
         res = self.finish(seed=seed)
         keep = torch.full((R,), -1, dtype=torch.int32, device=dev)
         keep[::K] = first + res["idx"].clamp(min=0)
         disc_cache_fork(cache, keep)
-        return {**res, "cache_status": status, "live_pages": disc_cache_compact(cache)}
+        return {**res, "cache_status": status, "live_pages": disc_cache_compact(cache), "attend_error": error}
 
     def replay(self, logits_per_step, *, seed=0, inv_temperature=1.0):
         """Decode over logits that are already resident on the device, one tensor per step."""

@@ -129,7 +129,7 @@ def _attend_outputs(q: torch.Tensor, out, lse):
 _error_words: dict = {}
 
 
-def _error_word(device: torch.device) -> torch.Tensor:
+def attend_error_word(device: torch.device) -> torch.Tensor:
     """The word an attention kernel sets when a bounded wait ran out, one per device."""
     w = _error_words.get(device)
     if w is None:
@@ -160,7 +160,7 @@ def disc_attend_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: 
     out, lse = _alloc(stream, _attend_outputs, q, out, lse)
     rc = lib().disc_attend_prompt(qp, qt, qh, kp, kt, kh, vp, vt, vh, dt, hq, hkv, d, n_q, n_k, _dev(cu_q, torch.int32, "cu_q"), _dev(cu_k, torch.int32, "cu_k"), n_seqs,
                                   int(max_len), int(causal), 1.0 / math.sqrt(d) if scale is None else float(scale),
-                                  _own(out), _own(lse), _error_word(q.device).data_ptr(),
+                                  _own(out), _own(lse), attend_error_word(q.device).data_ptr(),
                                   _stream_ptr(stream))
     _check(rc, "disc_attend_prompt")
     return out, lse
@@ -170,12 +170,12 @@ def disc_attend_check(device="cuda", stream=None, *, plan: "AttendPlan | None" =
     """Synchronises and raises DiscError when a prompt attention on the device, or a cached attention with this plan, has given up
     on one of its bounded waits since the last check."""
     if plan is not None:
-        word = plan.buf[:4].view(torch.int32)
+        word = plan.error
     else:
         dev = torch.device(device)
         if dev.index is None:
             dev = torch.device(dev.type, torch.cuda.current_device())
-        word = _error_word(dev)
+        word = attend_error_word(dev)
     rc = lib().disc_attend_error(word.data_ptr(), _stream_ptr(stream))
     try:
         if rc:
@@ -276,14 +276,17 @@ def disc_cache_compact(cache: DiscCache, *, live: torch.Tensor | None = None, st
 
 # ---- attention of one new token per row ---------------------------------------------------------------
 class AttendPlan:
-    """Buffer of a plan (disc_attend_plan) and what it was made for."""
+    """Buffer of a plan (disc_attend_plan) and what it was made for; error: int32[1], not 0 once a cached attention with this
+    plan gave up on a bounded wait, until disc_attend_check reports it."""
 
     def __init__(self, cache: DiscCache, n_q_heads: int, group: int):
         need = lib().disc_attend_plan_bytes(cache._p, int(n_q_heads), int(group))
         if need < 0:
             raise DiscError(int(need), "disc_attend_plan_bytes")
         self.n_q_heads, self.group, self.nbytes = int(n_q_heads), int(group), int(need)
-        self.buf = torch.empty(self.nbytes, dtype=torch.uint8, device=cache.pool.device)
+        # zeros: no error yet, and no work in a plan that has not been made
+        self.buf = torch.zeros(self.nbytes, dtype=torch.uint8, device=cache.pool.device)
+        self.error = self.buf[:4].view(torch.int32)
 
 
 def disc_attend_plan(cache: DiscCache, n_q_heads: int, *, group: int = 1, plan: AttendPlan | None = None,
