@@ -17,7 +17,7 @@ from __future__ import annotations
 import torch
 
 from .model_ops import DiscCache, attend_error_word, disc_attend_plan, disc_cache_compact, disc_cache_extend, disc_cache_fork
-from .binding import (DiscSet, DiscState, StepOutputs, disc_accept_resample, disc_project_scratch, disc_project_step,
+from .binding import (ROW_DEAD, DiscSet, DiscState, StepOutputs, disc_accept_resample, disc_project_scratch, disc_project_step,
                       disc_resample, disc_state_init, disc_step, disc_step_topm, lib)
 
 
@@ -131,24 +131,29 @@ class DiscDecoder:
         holds the drawn candidate, the other rows are empty and the pages in use have moved together.
 
         Returns disc_resample's results with `cache_status` (uint8[B*K]: ROW_NOPAGE where the cache had no room for a
-        token, whose row is then not to be used), `live_pages` and `attend_error` (int32[1]: not 0 when a bounded wait of an
+        token, ROW_DEAD for the candidates of an empty prompt, which gives no logits; such a row is not to be used), `live_pages` and `attend_error` (int32[1]: not 0 when a bounded wait of an
         attention kernel ran out at any position, or since the last disc_attend_check; the results are then invalid).
         on_step(t, logits, outputs) is called after every position.  The host waits for nothing."""
         B, K, R = self.B, self.K, self.R
         if cache.n_rows != R:
             raise ValueError(f"decode_cached: the cache has {cache.n_rows} rows, the decoder {R}")
+        if prompts.numel() == 0:
+            raise ValueError("decode_cached: no prompt has a token")
         dev = self.device
         first = torch.arange(B, dtype=torch.int32, device=dev) * K
         heads = first.repeat_interleave(K)
         self.reset()
         add = torch.zeros(R, dtype=torch.int32, device=dev)
         add[::K] = cu[1:] - cu[:-1]
+        empty = cu[1:] == cu[:-1]
         status = disc_cache_extend(cache, add)
         hidden = lm.prefill(prompts, cu, max_len, cache, first, status)
         disc_cache_fork(cache, heads)
-        # a prompt without room leaves its whole group unusable
-        status = status.view(B, K)[:, :1].expand(B, K).reshape(R).contiguous()
-        hidden = hidden.index_select(0, cu[1:].long() - 1).repeat_interleave(K, dim=0)
+        # a prompt without room leaves its whole group unusable, and so does one without tokens: it has no last hidden vector, and
+        # the place before its end is another prompt's, or none
+        status = status.view(B, K)[:, 0] | empty.to(torch.uint8) * ROW_DEAD
+        status = status[:, None].expand(B, K).reshape(R).contiguous()
+        hidden = hidden.index_select(0, (cu[1:].long() - 1).clamp(min=0)).masked_fill(empty[:, None], 0).repeat_interleave(K, dim=0)
         prev = None
         error = attend_error_word(prompts.device)
         for t in range(self.set.l_max):
