@@ -46,6 +46,7 @@ constexpr int PT = 512;                // threads of a plan block
 
 // ---- the plan ---------------------------------------------------------------------------------------
 __device__ __forceinline__ void cluster_sync_all() {
+    __syncwarp();                     // .aligned: the whole warp at once, also after a loop that its lanes left apart
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 

@@ -126,6 +126,7 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     return r;
 }
 __device__ __forceinline__ void cluster_sync_all() {
+    __syncwarp();                     // .aligned: the whole warp at once, also after a loop that its lanes left apart
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ int32_t remote_int(const int32_t* p, uint32_t rank) {
@@ -277,7 +278,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(XT) cache_extend_ke
     const int32_t per = ROWS ? ROWS : (a1 - a0 + XT - 1) / XT;
     const int32_t r0 = min(a1, a0 + tid * per), n_rows = min(a1, r0 + per) - r0;
     constexpr int HELD = ROWS ? ROWS : 1;
-    Need held[HELD];
+    Need held[HELD] = {};
 #pragma unroll
     for (int i = 0; i < ROWS; ++i)
         if (i < n_rows) held[i] = row_need(b, add, r0 + i);
@@ -362,11 +363,12 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(XT) cache_extend_ke
     }
     // every decision has been made on the counts as they were, the list is complete; then the counts change
     sync_blocks<CL>();
-    auto settle = [&](int32_t row, const Need& n, int32_t cp) {
+    // by whole warps, also for lanes without a row
+    auto settle = [&](bool some, int32_t row, const Need& n, int32_t cp) {
         uint8_t st = 0;
         bool copy = false;
         int32_t to = 0;
-        if (n.add > 0) {
+        if (some && n.add > 0) {
             const int32_t pages = n.last - n.first + cp;
             if (n.too_long || (pages > 0 && at + pages > free_all)) st = DISC_ROW_NOPAGE;
             else {
@@ -388,26 +390,27 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(XT) cache_extend_ke
             }
             if (!n.too_long) at += pages;
         }
-        status[row] = st;
+        if (some) status[row] = st;
         // a place in the list of copies, whose order does not matter
-        const unsigned who = __activemask(), some = __ballot_sync(who, copy);
-        if (some) {
-            const int first = __ffs(some) - 1;
+        const unsigned copying = __ballot_sync(FULL, copy);
+        if (copying) {
+            const int first = __ffs(copying) - 1;
             int32_t base = 0;
-            if (lane == first) base = atomicAdd(s.head, __popc(some));
-            base = __shfl_sync(who, base, first);
-            if (copy) s.copy[base + __popc(some & ((1u << lane) - 1u))] = make_int4(n.page, to, n.len & (b.page_size - 1), 0);
+            if (lane == first) base = atomicAdd(s.head, __popc(copying));
+            base = __shfl_sync(FULL, base, first);
+            if (copy) s.copy[base + __popc(copying & ((1u << lane) - 1u))] = make_int4(n.page, to, n.len & (b.page_size - 1), 0);
         }
     };
     if (ROWS) {
 #pragma unroll
-        for (int i = 0; i < HELD; ++i)
-            if (i < n_rows) settle(r0 + i, held[i], held_copy[i]);
+        for (int i = 0; i < HELD; ++i) settle(i < n_rows, r0 + i, held[i], held_copy[i]);
     } else {
         // the copies are decided by counts that other rows are changing: they were noted with the decision
-        for (int32_t i = 0; i < n_rows; ++i) {
-            const Need n = row_need(b, add, r0 + i);
-            settle(r0 + i, n, s.len[r0 + i]);
+        for (int32_t i = 0; i < per; ++i) {
+            const bool some = i < n_rows;
+            Need n = {};
+            if (some) n = row_need(b, add, r0 + i);
+            settle(some, r0 + i, n, some ? s.len[r0 + i] : 0);
         }
     }
     sync_blocks<CL>();                                    // no block leaves while another may still read its shared memory

@@ -310,6 +310,7 @@ __device__ __forceinline__ uint32_t cluster_ctarank() {
     return r;
 }
 __device__ __forceinline__ void cluster_sync_all() {
+    __syncwarp();                     // .aligned: the whole warp at once, also after a loop that its lanes left apart
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ uint32_t remote(const void* p, uint32_t rank) {
