@@ -215,6 +215,7 @@ class DiscCache:
         self._scratch = torch.empty(int(need), dtype=torch.uint8, device=pool.device)
         self._c.scratch, self._c.scratch_bytes = self._scratch.data_ptr(), int(need)
         self._plans: dict = {}
+        self._sizes = tuple(pool.shape) + (self.n_rows, self.table_width, pool.dtype)
 
     @staticmethod
     def empty(n_layers: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, n_rows: int, table_width: int, *,
@@ -283,10 +284,16 @@ class AttendPlan:
         need = lib().disc_attend_plan_bytes(cache._p, int(n_q_heads), int(group))
         if need < 0:
             raise DiscError(int(need), "disc_attend_plan_bytes")
-        self.n_q_heads, self.group, self.nbytes = int(n_q_heads), int(group), int(need)
+        self.n_q_heads, self.group, self.nbytes, self.sizes = int(n_q_heads), int(group), int(need), cache._sizes
         # zeros: no error yet, and no work in a plan that has not been made
         self.buf = torch.zeros(self.nbytes, dtype=torch.uint8, device=cache.pool.device)
         self.error = self.buf[:4].view(torch.int32)
+
+
+def _of_cache(plan: AttendPlan, cache: DiscCache):
+    # what lies where in the buffer hangs on the sizes: another layout would be read as page numbers
+    if plan.sizes != cache._sizes:
+        raise TypeError("plan: made for a cache of other sizes")
 
 
 def disc_attend_plan(cache: DiscCache, n_q_heads: int, *, group: int = 1, plan: AttendPlan | None = None,
@@ -297,6 +304,7 @@ def disc_attend_plan(cache: DiscCache, n_q_heads: int, *, group: int = 1, plan: 
         plan = cache._plans.get((n_q_heads, group))
         if plan is None:
             plan = cache._plans[(n_q_heads, group)] = _alloc(stream, AttendPlan, cache, n_q_heads, group)
+    _of_cache(plan, cache)
     _check(lib().disc_attend_plan(cache._p, plan.n_q_heads, plan.group, plan.buf.data_ptr(), plan.nbytes, _stream_ptr(stream)),
            "disc_attend_plan")
     return plan
@@ -310,6 +318,7 @@ def disc_attend_cached(cache: DiscCache, layer: int, q: torch.Tensor, plan: Atte
     n, h, d = q.shape
     if n != cache.n_rows or h != plan.n_q_heads or d != cache.head_dim:
         raise TypeError("q: expected [rows, Hq, head dim] of the cache and the plan")
+    _of_cache(plan, cache)
     out, lse = _alloc(stream, _attend_outputs, q, out, lse)
     _check(lib().disc_attend_cached(cache._p, int(layer), qp, qr, qh, plan.n_q_heads, plan.group,
                                     1.0 / math.sqrt(cache.head_dim) if scale is None else float(scale), plan.buf.data_ptr(),
