@@ -267,10 +267,12 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
             const int i = item.y + t * TILE_BLKS + warp;
             if (i >= item.z) return make_int2(0, 0);
             if (sh.per_group > 1) return list[i];
-            return make_int2(table[i / sh.blks_per_page], i % sh.blks_per_page | min(BLK, len - i * BLK) << 8);
+            return make_int2(table[i / sh.blks_per_page], i % sh.blks_per_page | max(0, min(BLK, len - i * BLK)) << 8);
         };
         auto load_tile = [&](int t, int2 e) {
             const int stage = t % STAGES;
+            // a plan older than the books: rows may have let go of their pages since, and -1 is no place to read from
+            if (unsigned(e.x) >= unsigned(p.pages)) e = make_int2(0, 0);
             const int tokens = (e.y >> 8) & 255;
             const int64_t off = (int64_t(e.x) * p.kv_heads + head) * head_bytes + int64_t(e.y & 255) * (BLK * 2) * p.D;
             const uint32_t kd = smem_u32(smem + stage * 2 * S::TILE_BYTES), vd = kd + S::TILE_BYTES;

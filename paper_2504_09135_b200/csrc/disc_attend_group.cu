@@ -486,7 +486,8 @@ __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p
 
     // step: block step % left of the (step / left)-th eight of query heads; a row's pages are the same for all heads, a lane
     // holds the page of one of its blocks (there are at most 9)
-    const int my_page = lane < left ? table[(begin + lane) / sh.blks_per_page] : 0;
+    int my_page = lane < left ? table[(begin + lane) / sh.blks_per_page] : 0;
+    if (unsigned(my_page) >= unsigned(p.pages)) my_page = 0;      // a plan older than the books: no place outside the pool is read
     static_assert(MAX_TAIL < 32, "a lane per block");
     const int lane_src = lane / CH * (D * 2) + lane % CH * 16;
     const uint32_t lane_dst = chunk_at<DP>(lane / CH, lane % CH);

@@ -38,3 +38,21 @@ def test_a_plan_that_was_never_made_holds_no_work(group):
     plan = disc.AttendPlan(cache, 24, group)
     disc.disc_attend_cached(cache, 0, torch.randn((6, 24, 64), device=DEV).bfloat16(), plan)
     disc.disc_attend_check(plan=plan)
+
+
+@pytest.mark.parametrize("group,hq", [(1, 4), (6, 4), (6, 24), (1, 64)])
+def test_a_plan_older_than_the_books_reads_nothing_outside_the_pool(group, hq):
+    """Rows that have let go of their pages since the plan was made: their results mean nothing, and the others are as they were."""
+    cache = filled()
+    q = torch.randn((6, hq, 64), device=DEV).bfloat16()
+    plan = disc.disc_attend_plan(cache, hq, group=group)
+    want, _ = disc.disc_attend_cached(cache, 0, q, plan)
+    freed = torch.tensor([1, 0, 0, 1, 0, 1], dtype=torch.uint8, device=DEV)
+    disc.disc_cache_free(cache, freed)
+    old, _ = disc.disc_attend_cached(cache, 0, q, plan)
+    new, lse = disc.disc_attend_cached(cache, 0, q, disc.disc_attend_plan(cache, hq, group=group))
+    torch.cuda.synchronize()
+    disc.disc_attend_check(plan=plan)
+    kept = freed == 0
+    assert torch.equal(old[kept], want[kept])
+    assert torch.all(new[~kept] == 0) and torch.isinf(lse[~kept]).all()
