@@ -137,12 +137,19 @@ def _stream_ptr(stream=None) -> int:
     return int(torch.cuda.current_stream().cuda_stream)
 
 
+def _here(t: torch.Tensor, name: str) -> int:
+    """Pointer of a CUDA tensor, which has to be on the current device: that is where the kernels are launched."""
+    if t.get_device() != (torch.cuda.current_device() if _raw_device is None else _raw_device()):
+        raise TypeError(f"{name}: on {t.device}, which is not the current device")
+    return t.data_ptr()
+
+
 def _dev(t: torch.Tensor, dtype, name: str) -> int:
     if t is None:
         return 0
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()):
         raise TypeError(f"{name}: expected a contiguous CUDA tensor of {dtype}")
-    return t.data_ptr()
+    return _here(t, name)
 
 
 class DiscSet:

@@ -12,7 +12,7 @@ import math
 
 import torch
 
-from .binding import DISC_BF16, DISC_F16, DISC_F32, DiscError, _Cache, _check, _dev, _stream_ptr, lib
+from .binding import DISC_BF16, DISC_F16, DISC_F32, DiscError, _Cache, _check, _dev, _here, _stream_ptr, lib
 
 _HALF = {torch.bfloat16: DISC_BF16, torch.float16: DISC_F16}
 _LOGIT = {torch.float32: DISC_F32, torch.bfloat16: DISC_BF16}
@@ -23,7 +23,7 @@ def _vectors(t: torch.Tensor, dtype, name: str):
     if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype:
         st = t.stride()
         if len(st) == 3 and (st[2] == 1 or t.shape[2] == 1):
-            return t.data_ptr(), st[0], st[1]
+            return _here(t, name), st[0], st[1]
     raise TypeError(f"{name}: expected a CUDA tensor [tokens, heads, head_dim] of {dtype} with unit inner stride")
 
 
@@ -33,7 +33,7 @@ def _rows(t: torch.Tensor, name: str):
         raise TypeError(f"{name}: expected a CUDA tensor [n, V] with unit inner stride")
     if t.dtype not in _LOGIT:
         raise DiscError(-7, name)
-    return t.data_ptr(), _LOGIT[t.dtype], t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return _here(t, name), _LOGIT[t.dtype], t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
 def _own(t):
@@ -224,16 +224,22 @@ class DiscCache:
         return DiscCache(pool, n_rows, table_width)
 
 
+def _books(cache: DiscCache) -> int:
+    """Address of the cache's sizes and pointers; its memory is on one device."""
+    _here(cache.pool, "cache")
+    return cache._p
+
+
 def disc_cache_fork(cache: DiscCache, parent: torch.Tensor, stream=None):
     """Row r becomes what row parent[r] was (int32[n_rows] on the device; outside [0, n_rows): emptied)."""
     _want(parent, cache.n_rows, "parent")
-    _check(lib().disc_cache_fork(cache._p, _dev(parent, torch.int32, "parent"), _stream_ptr(stream)), "disc_cache_fork")
+    _check(lib().disc_cache_fork(_books(cache), _dev(parent, torch.int32, "parent"), _stream_ptr(stream)), "disc_cache_fork")
 
 
 def disc_cache_free(cache: DiscCache, freed: torch.Tensor, stream=None):
     """The rows with freed[r] != 0 (uint8[n_rows] on the device) become empty."""
     _want(freed, cache.n_rows, "freed")
-    _check(lib().disc_cache_free(cache._p, _dev(freed, torch.uint8, "freed"), _stream_ptr(stream)), "disc_cache_free")
+    _check(lib().disc_cache_free(_books(cache), _dev(freed, torch.uint8, "freed"), _stream_ptr(stream)), "disc_cache_free")
 
 
 def disc_cache_extend(cache: DiscCache, add: torch.Tensor | None = None, *, status: torch.Tensor | None = None,
@@ -244,7 +250,7 @@ def disc_cache_extend(cache: DiscCache, add: torch.Tensor | None = None, *, stat
         status = _alloc(stream, _empty, cache.n_rows, torch.uint8, cache.pool.device)
     else:
         _want(status, cache.n_rows, "status")
-    _check(lib().disc_cache_extend(cache._p, _dev(add, torch.int32, "add"), _dev(status, torch.uint8, "status"),
+    _check(lib().disc_cache_extend(_books(cache), _dev(add, torch.int32, "add"), _dev(status, torch.uint8, "status"),
                                    _stream_ptr(stream)), "disc_cache_extend")
     return status
 
@@ -262,7 +268,7 @@ def disc_cache_write(cache: DiscCache, layer: int, k: torch.Tensor, v: torch.Ten
     if rows is not None:
         _want(rows, n_seqs, "rows")
     _want(status, cache.n_rows, "status")
-    _check(lib().disc_cache_write(cache._p, int(layer), kp, kt, kh, vp, vt, vh, n, _dev(cu, torch.int32, "cu"), n_seqs,
+    _check(lib().disc_cache_write(_books(cache), int(layer), kp, kt, kh, vp, vt, vh, n, _dev(cu, torch.int32, "cu"), n_seqs,
                                   _dev(rows, torch.int32, "rows"), _dev(status, torch.uint8, "status"), _stream_ptr(stream)),
            "disc_cache_write")
 
@@ -271,7 +277,7 @@ def disc_cache_compact(cache: DiscCache, *, live: torch.Tensor | None = None, st
     """The n pages in use move to the ids 0 .. n-1 -> n as int32[1] on the device."""
     if live is None:
         live = _alloc(stream, _empty, 1, torch.int32, cache.pool.device)
-    _check(lib().disc_cache_compact(cache._p, _dev(live, torch.int32, "live"), _stream_ptr(stream)), "disc_cache_compact")
+    _check(lib().disc_cache_compact(_books(cache), _dev(live, torch.int32, "live"), _stream_ptr(stream)), "disc_cache_compact")
     return live
 
 
@@ -305,7 +311,7 @@ def disc_attend_plan(cache: DiscCache, n_q_heads: int, *, group: int = 1, plan: 
         if plan is None:
             plan = cache._plans[(n_q_heads, group)] = _alloc(stream, AttendPlan, cache, n_q_heads, group)
     _of_cache(plan, cache)
-    _check(lib().disc_attend_plan(cache._p, plan.n_q_heads, plan.group, plan.buf.data_ptr(), plan.nbytes, _stream_ptr(stream)),
+    _check(lib().disc_attend_plan(_books(cache), plan.n_q_heads, plan.group, plan.buf.data_ptr(), plan.nbytes, _stream_ptr(stream)),
            "disc_attend_plan")
     return plan
 
@@ -320,7 +326,7 @@ def disc_attend_cached(cache: DiscCache, layer: int, q: torch.Tensor, plan: Atte
         raise TypeError("q: expected [rows, Hq, head dim] of the cache and the plan")
     _of_cache(plan, cache)
     out, lse = _alloc(stream, _attend_outputs, q, out, lse)
-    _check(lib().disc_attend_cached(cache._p, int(layer), qp, qr, qh, plan.n_q_heads, plan.group,
+    _check(lib().disc_attend_cached(_books(cache), int(layer), qp, qr, qh, plan.n_q_heads, plan.group,
                                     1.0 / math.sqrt(cache.head_dim) if scale is None else float(scale), plan.buf.data_ptr(),
                                     plan.nbytes, _own(out), _own(lse),
                                     _stream_ptr(stream)), "disc_attend_cached")
