@@ -18,9 +18,15 @@ _HALF = {torch.bfloat16: DISC_BF16, torch.float16: DISC_F16}
 _LOGIT = {torch.float32: DISC_F32, torch.bfloat16: DISC_BF16}
 
 
+def _without_grad(t, name: str):
+    if t is not None and t.requires_grad and torch.is_grad_enabled():
+        raise TypeError(f"{name}: requires a gradient, which this call does not give; detach it, or call under torch.no_grad()")
+
+
 def _vectors(t: torch.Tensor, dtype, name: str):
     """A CUDA tensor [tokens, heads, head_dim] whose innermost axis is contiguous: (pointer, the two strides)."""
     if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype:
+        _without_grad(t, name)
         st = t.stride()
         if len(st) == 3 and (st[2] == 1 or t.shape[2] == 1):
             return _here(t, name), st[0], st[1]
@@ -59,6 +65,29 @@ def _alloc(stream, make, *args):
 
 
 # ---- log-probabilities ------------------------------------------------------------------------------
+_LOGPROBS = ("logp", "entropy", "lse", "top_ids", "top_logp", "status")
+
+
+class _Logprobs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, targets, top, inv_temperature, stream):
+        r = disc_logprobs(logits, targets, top=top, inv_temperature=inv_temperature, stream=stream)
+        ctx.set_materialize_grads(False)
+        ctx.mark_non_differentiable(*(r[k] for k in ("lse", "top_ids", "top_logp", "status") if r[k] is not None))
+        ctx.save_for_backward(logits, targets, r["lse"], r["entropy"])
+        ctx.inv_temperature = inv_temperature
+        return tuple(r[k] for k in _LOGPROBS)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_logp, d_entropy, *_):
+        logits, targets, lse, entropy = ctx.saved_tensors
+        if d_logp is None and d_entropy is None:
+            return (None,) * 5
+        d_logp, d_entropy = (None if d is None else d.contiguous() for d in (d_logp, d_entropy))
+        return disc_logprobs_grad(logits, targets, lse, entropy, d_logp, d_entropy, inv_temperature=ctx.inv_temperature), None, None, None, None
+
+
 def _logprobs_outputs(n: int, top: int, targets: bool, dev):
     f = torch.float32
     return {"logp": torch.empty(n, dtype=f, device=dev) if targets else None,
@@ -71,14 +100,20 @@ def _logprobs_outputs(n: int, top: int, targets: bool, dev):
 def disc_logprobs(logits: torch.Tensor, targets: torch.Tensor | None = None, *, top: int = 0, inv_temperature=1.0,
                   out=None, stream=None):
     """logits [n, V] float32 or bfloat16 (any row stride), targets int32[n] (-1 = none) ->
-    dict(logp, entropy, lse float[n], top_ids int32[n, top], top_logp float[n, top], status uint8[n])."""
+    dict(logp, entropy, lse float[n], top_ids int32[n, top], top_logp float[n, top], status uint8[n]).
+    Where logits require a gradient, logp and entropy have one (disc_logprobs_grad; its call goes to the current stream of
+    this one); lse and the alternatives have none, and `out` is refused."""
+    if isinstance(logits, torch.Tensor) and logits.requires_grad and torch.is_grad_enabled():
+        if out is not None:
+            _without_grad(logits, "logits with out")
+        return dict(zip(_LOGPROBS, _Logprobs.apply(logits, targets, top, inv_temperature, stream)))
     ptr, dt, ld = _rows(logits, "disc_logprobs")
     n, V = logits.shape
     _want(targets, n, "targets")
     if out is None:
         out = _alloc(stream, _logprobs_outputs, n, top, targets is not None, logits.device)
     else:
-        for k in ("logp", "entropy", "lse", "top_ids", "top_logp", "status"):
+        for k in _LOGPROBS:
             _want(out[k], n * top if k.startswith("top") else n, k)
             _dev(out[k], torch.int32 if k == "top_ids" else torch.uint8 if k == "status" else torch.float32, k)
     rc = lib().disc_logprobs(ptr, dt, ld, n, V, float(inv_temperature), _dev(targets, torch.int32, "targets"), int(top),
@@ -94,8 +129,10 @@ def disc_logprobs_grad(logits: torch.Tensor, targets, lse: torch.Tensor, entropy
     lse, entropy: what disc_logprobs gave for these logits.  out may be `logits` itself."""
     ptr, dt, ld = _rows(logits, "disc_logprobs_grad")
     n, V = logits.shape
+    _without_grad(logits, "logits")
     for t, name in ((targets, "targets"), (lse, "lse"), (entropy, "entropy"), (d_logp, "d_logp"), (d_entropy, "d_entropy")):
         _want(t, n, name)
+        _without_grad(t, name)
     if out is None:
         out = _alloc(stream, _empty, (n, V), logits.dtype, logits.device)
     elif out.shape != logits.shape or out.dtype != logits.dtype:
