@@ -412,7 +412,7 @@ int disc_logprobs_grad(const void* logits, disc_dtype_t dtype, int64_t ld, int64
  *   out = softmax(scale q k^T) v,  lse = log sum e^{scale q k^T}
  *   q, k, v     device, bf16 or f16; token t, head h at element offset t*token_stride + h*head_stride,
  *               head_dim values in a row (slices of one fused projection output are fine).  Bases on
- *               16-byte boundaries, strides multiples of 8
+ *               16-byte boundaries, strides multiples of 8 and above 0
  *   head_dim    a multiple of 8, at most DISC_MAX_HEAD_DIM
  *   n_q_heads   a multiple of n_kv_heads, at most 128 times as many
  *   n_q, n_k    tokens in q and in k / v
@@ -508,7 +508,8 @@ int disc_attend_plan(const disc_cache_t* c, int32_t n_q_heads, int32_t group, vo
 /* out[r] = softmax(scale q[r] K^T) V over the len[r] tokens of row r in layer `layer`; a row without tokens
  * gets out = 0, lse = -inf.  Pages that the rows of a group have in common are read once for all.
  *   q       device, dtype of the cache; row r, head h at element offset r*q_row_stride + h*q_head_stride;
- *           base on a 16-byte boundary, strides multiples of 8
+ *           base on a 16-byte boundary, strides multiples of 8 and above 0 (up to 16 query vectors per group, min(group, n_rows) times
+ *           the query heads of a key head, any multiples)
  *   n_q_heads   a multiple of n_kv_heads, at most 64 times as many
  *   scale   > 0
  *   plan    of disc_attend_plan with the same cache sizes, n_q_heads and group; long rows are split and joined in

@@ -662,6 +662,9 @@ int disc_cache_write(const disc_cache_t* c, int32_t layer, const void* k, int64_
     if (!rows && n_seqs > c->n_rows) return DISC_ERR_ARG;
     if (n_tokens == 0 || n_seqs == 0) return DISC_OK;
     if (!k || !v) return DISC_ERR_ARG;
+    // the stride over an axis of one is never used
+    if (n_tokens == 1) k_token_stride = v_token_stride = 0;
+    if (c->n_kv_heads == 1) k_head_stride = v_head_stride = 0;
     // 16-byte reads: the bases on 16-byte boundaries, the strides multiples of 8 values
     if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15u) return DISC_ERR_ARG;
     if ((k_token_stride | k_head_stride | v_token_stride | v_head_stride) & 7) return DISC_ERR_UNSUPPORTED;

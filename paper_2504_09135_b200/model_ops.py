@@ -33,6 +33,13 @@ def _vectors(t: torch.Tensor, dtype, name: str):
     raise TypeError(f"{name}: expected a CUDA tensor [tokens, heads, head_dim] of {dtype} with unit inner stride")
 
 
+def _spread(t: torch.Tensor, stream) -> torch.Tensor:
+    """t itself, or a copy where one vector stands for several tokens or heads (a stride of 0), which tensor maps do not take."""
+    if t.numel() and 0 in t.stride():
+        return _alloc(stream, t.contiguous)
+    return t
+
+
 def _rows(t: torch.Tensor, name: str):
     """Logits [n, V]: (pointer, dtype code, row stride)."""
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.ndim == 2 and (t.stride(1) == 1 or t.shape[1] == 1)):
@@ -184,6 +191,7 @@ def disc_attend_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: 
     dt = _HALF.get(q.dtype)
     if dt is None:
         raise DiscError(-7, "disc_attend_prompt")
+    q, k, v = _spread(q, stream), _spread(k, stream), _spread(v, stream)
     qp, qt, qh = _vectors(q, q.dtype, "q")
     kp, kt, kh = _vectors(k, q.dtype, "k")
     vp, vt, vh = _vectors(v, q.dtype, "v")
@@ -357,6 +365,7 @@ def disc_attend_cached(cache: DiscCache, layer: int, q: torch.Tensor, plan: Atte
                        out=None, lse=None, stream=None):
     """One new token per row: q [rows, Hq, D] against the row's tokens in layer `layer` -> (out [rows, Hq, D],
     lse float[rows, Hq])."""
+    q = _spread(q, stream)
     qp, qr, qh = _vectors(q, cache.pool.dtype, "q")
     n, h, d = q.shape
     if n != cache.n_rows or h != plan.n_q_heads or d != cache.head_dim:
