@@ -506,7 +506,8 @@ int64_t disc_attend_plan_bytes(const disc_cache_t* c, int32_t n_q_heads, int32_t
 int disc_attend_plan(const disc_cache_t* c, int32_t n_q_heads, int32_t group, void* plan, int64_t plan_bytes, void* stream);
 
 /* out[r] = softmax(scale q[r] K^T) V over the len[r] tokens of row r in layer `layer`; a row without tokens
- * gets out = 0, lse = -inf.  Pages that the rows of a group have in common are read once for all.
+ * gets out = 0, lse = -inf.  Pages that the rows with tokens of a group have in common are read once for all of them (for groups
+ * of more than 128 query vectors, rows times the query heads of a key head, once for each 128 or so).
  *   q       device, dtype of the cache; row r, head h at element offset r*q_row_stride + h*q_head_stride;
  *           base on a 16-byte boundary, strides multiples of 8 and above 0 (up to 16 query vectors per group, min(group, n_rows) times
  *           the query heads of a key head, any multiples)

@@ -80,17 +80,23 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(PT) attend_plan_ker
         }
         int32_t shared = 0;
         if (n > 1) {
-            int32_t full = 0x7fffffff;
-            for (int32_t r = r0 + lane; r < r1; r += 32) full = min(full, p.len[r] >> p.shift);
+            // rows without tokens need no pages: the first that has some is what the others are compared with
+            int32_t full = 0x7fffffff, lead = r1;
+            for (int32_t r = r0 + lane; r < r1; r += 32) {
+                const int32_t len = p.len[r];
+                if (len > 0) { full = min(full, len >> p.shift); lead = min(lead, r); }
+            }
             full = __reduce_min_sync(FULL, full);
-            const int32_t* first = p.table + int64_t(r0) * p.width;
+            lead = __reduce_min_sync(FULL, lead);
+            if (lead == r1) full = 0;
+            const int32_t* first = p.table + int64_t(lead < r1 ? lead : r0) * p.width;
             shared = full;
             for (int32_t j0 = 0; j0 < full && shared == full; j0 += 32) {
                 const int32_t j = j0 + lane;
                 bool same = true;
                 if (j < full) {
                     const int32_t page = first[j];
-                    for (int32_t r = 1; r < n; ++r) same = same && first[int64_t(r) * p.width + j] == page;
+                    for (int32_t r = lead + 1; r < r1; ++r) same = same && (p.len[r] == 0 || p.table[int64_t(r) * p.width + j] == page);
                 }
                 const unsigned differ = __ballot_sync(FULL, !same);
                 if (differ) shared = j0 + __ffs(differ) - 1;
@@ -434,7 +440,11 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
             }
             const float inv = ll > 0.f ? 1.f / ll : (ll == 0.f ? 0.f : ll);
             x.x *= inv; x.y *= inv; x.z *= inv; x.w *= inv;
-            const float lse2 = ll > 0.f ? mm + log2f(ll) : (ll == 0.f ? -CUDART_INF_F : ll);
+            float lse2 = ll > 0.f ? mm + log2f(ll) : (ll == 0.f ? -CUDART_INF_F : ll);
+            if (n_rows > 1 && p.len[r0 + m / G] == 0) {           // beside rows whose shared pages it does not hold
+                x = make_float4(0.f, 0.f, 0.f, 0.f);
+                lse2 = -CUDART_INF_F;
+            }
             if (splits > 1) {
                 *reinterpret_cast<float4*>(p.plan.part + (slot + m) * p.D + d) = x;
                 if (d == 0) p.plan.part_lse[slot + m] = lse2;

@@ -26,8 +26,8 @@ struct PlanShape {
     int64_t max_part;                  // partial results: query vectors there is room for
 };
 
-struct GroupItem {                     // rows [row, row + rows) over their blocks [begin, end)
-    int32_t row, rows, begin, end, part, pad[3];
+struct GroupItem {                     // rows [row, row + rows) over the blocks [begin, end) of row `lead`
+    int32_t row, rows, begin, end, part, lead, pad[2];
 };
 
 struct RowItem {                       // rows [row, row + rows) of group g over the blocks [begin, end) of its list
@@ -48,6 +48,7 @@ struct Plan {
     // group form
     GroupItem* group_items;
     int32_t* shared;                   // [groups] leading blocks that its rows share and that are worked on together
+    int32_t* lead;                     // [groups] the first row with tokens, whose pages these are
     int32_t* alone;                    // [rows] blocks after those that are worked on as an item of the row's own
     int2* group_part;                  // [groups] first partial result, number of parts
     int2* row_part;                    // [rows]
@@ -103,6 +104,7 @@ inline int64_t plan_layout(const disc_cache_t* c, const PlanShape& s, void* base
     } else {
         t.group_items = reinterpret_cast<GroupItem*>(take(int64_t(s.max_items) * sizeof(GroupItem)));
         t.shared = reinterpret_cast<int32_t*>(take(int64_t(s.groups) * 4));
+        t.lead = reinterpret_cast<int32_t*>(take(int64_t(s.groups) * 4));
         t.alone = reinterpret_cast<int32_t*>(take(int64_t(c->n_rows) * 4));
         t.group_part = reinterpret_cast<int2*>(take(int64_t(s.groups) * 8));
         t.row_part = reinterpret_cast<int2*>(take(int64_t(c->n_rows) * 8));

@@ -36,22 +36,30 @@ constexpr int MIN_SHARED = 4;          // blocks: less is not worth an item
 constexpr int MAX_TAIL = 8;            // full blocks that kernel 2 takes along
 
 // ---- the plan ---------------------------------------------------------------------------------------
-// A block per group: the leading pages that its rows share, and what rows have left.
+// A block per group: the leading pages that its rows share, and what rows have left.  Rows without tokens need no pages and are
+// left out; what the tile of the group adds up for them is not joined.
 __global__ void __launch_bounds__(256) group_shared_kernel(const PlanParams p) {
     let_later_in();
     wait_for_earlier();
-    __shared__ int32_t s_shared;
+    __shared__ int32_t s_shared, s_lead[8], s_len[GROUP_M];
     const PlanShape& sh = p.shape;
     const int g = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int32_t r0 = g / sh.sub * sh.group + g % sh.sub * sh.per_group;
     const int32_t r1 = min(p.rows, min(r0 + sh.per_group, g / sh.sub * sh.group + sh.group));
     if (threadIdx.x == 0) s_shared = 0x7fffffff;
+    const int32_t own = r0 + int32_t(threadIdx.x), own_len = own < r1 ? p.len[own] : 0;      // at most GROUP_M rows
+    if (own < r1) s_len[threadIdx.x] = own_len;
+    const int32_t warp_lead = __reduce_min_sync(FULL, own_len > 0 ? own : max(r0, r1));
+    if (lane == 0) s_lead[warp] = warp_lead;
     __syncthreads();
-    const int32_t* first = p.table + int64_t(r0) * p.width;
+    const int32_t lead = __reduce_min_sync(FULL, s_lead[lane & 7]);
+    const int32_t* first = p.table + int64_t(lead) * p.width;
     for (int32_t r = r0 + warp; r < r1; r += 8) {
-        const int32_t full = min(p.len[r0], p.len[r]) >> p.shift;
+        const int32_t len = s_len[r - r0];
+        if (len == 0) continue;
+        const int32_t full = min(s_len[lead - r0], len) >> p.shift;
         int32_t same = full;
-        if (r > r0) {
+        if (r > lead) {
             const int32_t* row = p.table + int64_t(r) * p.width;
             for (int32_t j0 = 0; j0 < full; j0 += 64) {
                 const int32_t j = j0 + lane, j2 = j + 32;
@@ -66,12 +74,12 @@ __global__ void __launch_bounds__(256) group_shared_kernel(const PlanParams p) {
         if (lane == 0) atomicMin(&s_shared, same);
     }
     __syncthreads();
-    int32_t blks = r0 < r1 ? s_shared * sh.blks_per_page : 0;
+    int32_t blks = lead < r1 ? s_shared * sh.blks_per_page : 0;
     if (blks < MIN_SHARED) blks = 0;
-    if (threadIdx.x == 0) p.plan.shared[g] = blks;
-    for (int32_t r = r0 + threadIdx.x; r < r1; r += 256) {
-        const int32_t left = p.len[r] / BLK - blks;
-        p.plan.alone[r] = left > MAX_TAIL ? left : 0;
+    if (threadIdx.x == 0) { p.plan.shared[g] = blks; p.plan.lead[g] = lead; }
+    if (own < r1) {
+        const int32_t left = own_len / BLK - blks;
+        p.plan.alone[own] = left > MAX_TAIL ? left : 0;
     }
 }
 
@@ -131,15 +139,16 @@ __global__ void __launch_bounds__(PT) group_items_kernel(const PlanParams p) {
                 if (i < n) p.plan.row_part[i] = make_int2(0, 0);
                 continue;
             }
-            int32_t blks = 0, row = 0, rows = 1, first = 0;
+            int32_t blks = 0, row = 0, rows = 1, first = 0, lead = 0;
             if (i < n) {
                 if (kind == 0) {
                     blks = p.plan.shared[i];
+                    lead = p.plan.lead[i];
                     row = i / sh.sub * sh.group + i % sh.sub * sh.per_group;
                     rows = max(0, min(p.rows, min(row + sh.per_group, i / sh.sub * sh.group + sh.group)) - row);
                 } else {
                     blks = p.plan.alone[i];
-                    row = i;
+                    row = lead = i;
                     if (blks) first = p.plan.shared[i / sh.group * sh.sub + i % sh.group / sh.per_group];
                 }
             }
@@ -155,7 +164,7 @@ __global__ void __launch_bounds__(PT) group_items_kernel(const PlanParams p) {
             if (i < n) (kind == 0 ? p.plan.group_part : p.plan.row_part)[i] = make_int2(part0, cut.splits);
             for (int32_t x = 0; x < cut.splits; ++x) {
                 const int32_t border = (cut.from + x) * share - at, begin = max(0, border), end = min(blks, border + share);
-                p.plan.group_items[item0 + x] = GroupItem{row, rows, first + begin, first + end, part0 + x * rows * sh.G * p.kv_heads, {0, 0, 0}};
+                p.plan.group_items[item0 + x] = GroupItem{row, rows, first + begin, first + end, part0 + x * rows * sh.G * p.kv_heads, lead, {0, 0}};
             }
             if (blks > 0) first_items(p.plan.first, at, blks, share, cut, item0, cut.splits);
         }
@@ -236,7 +245,7 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
             for (; item0 + n < item1 && ok; ++n) {
                 const GroupItem* it = p.plan.group_items + item0 + n;
                 const int row = it->row, begin = it->begin, blks = it->end - begin;
-                const int32_t* table = p.table + int64_t(row) * p.width;
+                const int32_t* table = p.table + int64_t(it->lead) * p.width;
                 if (n > 0) ok = mbar_wait_all(q_empty, (n - 1) & 1, abort);
                 if (ok && lane == 0) {
                     mbar_expect_tx(q_full, uint32_t(S::BOXES) * p.G * p.per_group * BOX * 2);
@@ -244,7 +253,7 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                 }
                 for (int t = 0; t < blks && ok; t += TILE_BLKS) {
                     const int here = min(TILE_BLKS, blks - t);
-                    // lane l brings in block l % 8: its keys, then its values
+                    // lane l brings in block l % 4: its keys, then its values
                     const int b = lane % TILE_BLKS, blk = begin + t + b;
                     int y = 0;
                     if (b < here) y = (table[blk / p.blks_per_page] * p.kv_heads + head) * p.page_size + blk % p.blks_per_page * BLK;
@@ -476,7 +485,7 @@ __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p
     const int group_rows = min(p.rows, min(first_row + sh.per_group, row / sh.group * sh.group + sh.group)) - first_row;
     const int32_t len = p.len[row];
     const int2 gp = p.plan.group_part[g], rp = p.plan.row_part[row];
-    const int begin = p.plan.shared[g] + p.plan.alone[row], left = (len + BLK - 1) / BLK - begin;      // blocks
+    const int begin = p.plan.shared[g] + p.plan.alone[row], left = (len + BLK - 1) / BLK - begin;      // blocks; none without tokens
     const int32_t* table = p.table + int64_t(row) * p.width;
     const int64_t head_bytes = int64_t(p.page_size) * D * 2;
     unsigned char* own = smem + warp * S::WARP_BYTES;
@@ -644,7 +653,7 @@ __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p
 #pragma unroll
                 for (int a = 0; a < AT_ONCE; ++a) add(a, lse[a], 1.f, y[a]);
             };
-            for (int s = 0; s < gp.y; ++s) take(g_at + s * g_step);
+            for (int s = 0; s < gp.y && len > 0; ++s) take(g_at + s * g_step);
             for (int s = 0; s < rp.y; ++s) take(r_at + s * r_step);
 #pragma unroll
             for (int a = 0; a < AT_ONCE; ++a) {
