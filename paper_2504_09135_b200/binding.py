@@ -126,22 +126,25 @@ def _check(rc: int, where: str):
 
 # the current stream's handle without a Stream object around it (3 us a call); present in every torch that has CUDA
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-_raw_device = getattr(torch._C, "_cuda_getDevice", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_initialized = False
 
 
 def _stream_ptr(stream=None) -> int:
     if stream is not None:
         return int(stream.cuda_stream)
-    if _raw_stream is not None and _raw_device is not None and torch.cuda.is_initialized():
+    global _initialized
+    if _raw_stream is not None and (_initialized or torch.cuda.is_initialized()):
+        _initialized = True
         return _raw_stream(_raw_device())
     return int(torch.cuda.current_stream().cuda_stream)
 
 
 def _here(t: torch.Tensor, name: str) -> int:
     """Pointer of a CUDA tensor, which has to be on the current device: that is where the kernels are launched."""
-    if t.get_device() != (torch.cuda.current_device() if _raw_device is None else _raw_device()):
-        raise TypeError(f"{name}: on {t.device}, which is not the current device")
-    return t.data_ptr()
+    if t.get_device() == _raw_device():
+        return t.data_ptr()
+    raise TypeError(f"{name}: on {t.device}, which is not the current device")
 
 
 def _dev(t: torch.Tensor, dtype, name: str) -> int:
@@ -149,7 +152,7 @@ def _dev(t: torch.Tensor, dtype, name: str) -> int:
         return 0
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()):
         raise TypeError(f"{name}: expected a contiguous CUDA tensor of {dtype}")
-    return _here(t, name)
+    return t.data_ptr() if t.get_device() == _raw_device() else _here(t, name)
 
 
 class DiscSet:

@@ -12,6 +12,7 @@ import math
 
 import torch
 
+from . import binding
 from .binding import DISC_BF16, DISC_F16, DISC_F32, DiscError, _Cache, _check, _dev, _here, _stream_ptr, lib
 
 _HALF = {torch.bfloat16: DISC_BF16, torch.float16: DISC_F16}
@@ -26,7 +27,8 @@ def _without_grad(t, name: str):
 def _vectors(t: torch.Tensor, dtype, name: str):
     """A CUDA tensor [tokens, heads, head_dim] whose innermost axis is contiguous: (pointer, the two strides)."""
     if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype:
-        _without_grad(t, name)
+        if t.requires_grad:
+            _without_grad(t, name)
         st = t.stride()
         if len(st) == 3 and (st[2] == 1 or t.shape[2] == 1):
             return _here(t, name), st[0], st[1]
@@ -34,10 +36,8 @@ def _vectors(t: torch.Tensor, dtype, name: str):
 
 
 def _spread(t: torch.Tensor, stream) -> torch.Tensor:
-    """t itself, or a copy where one vector stands for several tokens or heads (a stride of 0), which tensor maps do not take."""
-    if t.numel() and 0 in t.stride():
-        return _alloc(stream, t.contiguous)
-    return t
+    """A copy where one vector stands for several tokens or heads (a stride of 0), which tensor maps do not take."""
+    return _alloc(stream, t.contiguous) if 0 in t.stride() else t
 
 
 def _rows(t: torch.Tensor, name: str):
@@ -188,13 +188,16 @@ def disc_attend_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: 
     fine), cu_q / cu_k int32[n_seqs + 1] on the device (cu_k None: the same sequences), max_len: no sequence
     has more queries -> (out [n_q, Hq, D], lse float[n_q, Hq]).  The first call on a device makes the word that
     disc_attend_check reads and waits for it: it comes before any stream capture."""
-    dt = _HALF.get(q.dtype)
+    dtype = q.dtype
+    dt = _HALF.get(dtype)
     if dt is None:
         raise DiscError(-7, "disc_attend_prompt")
-    q, k, v = _spread(q, stream), _spread(k, stream), _spread(v, stream)
-    qp, qt, qh = _vectors(q, q.dtype, "q")
-    kp, kt, kh = _vectors(k, q.dtype, "k")
-    vp, vt, vh = _vectors(v, q.dtype, "v")
+    qp, qt, qh = _vectors(q, dtype, "q")
+    kp, kt, kh = _vectors(k, dtype, "k")
+    vp, vt, vh = _vectors(v, dtype, "v")
+    if not (qt and qh and kt and kh and vt and vh):
+        q, k, v = _spread(q, stream), _spread(k, stream), _spread(v, stream)
+        (qp, qt, qh), (kp, kt, kh), (vp, vt, vh) = _vectors(q, dtype, "q"), _vectors(k, dtype, "k"), _vectors(v, dtype, "v")
     n_q, hq, d = q.shape
     n_k, hkv, dk = k.shape
     if v.shape != k.shape or dk != d:
@@ -260,6 +263,7 @@ class DiscCache:
         self._scratch = torch.empty(int(need), dtype=torch.uint8, device=pool.device)
         self._c.scratch, self._c.scratch_bytes = self._scratch.data_ptr(), int(need)
         self._plans: dict = {}
+        self._device = pool.get_device()
         self._sizes = tuple(pool.shape) + (self.n_rows, self.table_width, pool.dtype)
 
     @staticmethod
@@ -271,7 +275,8 @@ class DiscCache:
 
 def _books(cache: DiscCache) -> int:
     """Address of the cache's sizes and pointers; its memory is on one device."""
-    _here(cache.pool, "cache")
+    if cache._device != binding._raw_device():
+        _here(cache.pool, "cache")
     return cache._p
 
 
@@ -355,7 +360,8 @@ def disc_attend_plan(cache: DiscCache, n_q_heads: int, *, group: int = 1, plan: 
         plan = cache._plans.get((n_q_heads, group))
         if plan is None:
             plan = cache._plans[(n_q_heads, group)] = _alloc(stream, AttendPlan, cache, n_q_heads, group)
-    _of_cache(plan, cache)
+    else:
+        _of_cache(plan, cache)
     _check(lib().disc_attend_plan(_books(cache), plan.n_q_heads, plan.group, plan.buf.data_ptr(), plan.nbytes, _stream_ptr(stream)),
            "disc_attend_plan")
     return plan
@@ -365,8 +371,10 @@ def disc_attend_cached(cache: DiscCache, layer: int, q: torch.Tensor, plan: Atte
                        out=None, lse=None, stream=None):
     """One new token per row: q [rows, Hq, D] against the row's tokens in layer `layer` -> (out [rows, Hq, D],
     lse float[rows, Hq])."""
-    q = _spread(q, stream)
     qp, qr, qh = _vectors(q, cache.pool.dtype, "q")
+    if not (qr and qh):
+        q = _spread(q, stream)
+        qp, qr, qh = _vectors(q, cache.pool.dtype, "q")
     n, h, d = q.shape
     if n != cache.n_rows or h != plan.n_q_heads or d != cache.head_dim:
         raise TypeError("q: expected [rows, Hq, head dim] of the cache and the plan")
