@@ -956,9 +956,15 @@ int disc_logprobs(const void* logits, disc_dtype_t dtype, int64_t ld, int64_t n,
     const int64_t vecs = vocab_size / (dtype == DISC_F32 ? 4 : 8);
     while (p.split < 8 && n * p.split * 2 <= 2 * sms && vecs / (p.split * 2) >= NT) p.split *= 2;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    // Short rows: 4096 rows of 256 take 19 us with 20 alternatives and 45 with 64 by warps, 41 and 74 by blocks; of 1000, 14 us
-    // with one, 45 with 20 and 115 with 64 by warps, 39, 43 and 51 by blocks.
-    if (vocab_size <= 256 || (vocab_size <= SHORT_ROW && top <= 20)) return dtype == DISC_F32 ? launch_short<DISC_F32>(p, n, st) : launch_short<DISC_BF16>(p, n, st);
+    // Short rows, a warp per row or a block per row (us, bf16, warps / blocks; f32 crosses at the same places):
+    //   4096 rows of 256    1 alternative  5 / 37    20  17 / 40    64   45 / 74
+    //   4096 rows of 1000   1             14 / 37    16  39 / 40    20   45 / 41    64  116 / 50
+    //   32 rows of 256      8              5 / 6     12   6 / 6     20    8 / 6     64   19 / 7
+    //   32 rows of 1000     1              6 / 6      4   8 / 6     20   16 / 6     64   37 / 7
+    // Alternatives cost a warp 0.25 to 0.6 us each, one after the other, whatever the number of rows, and blocks next to
+    // nothing as long as all of them run at once.
+    const bool wave = n <= int64_t(sms) * 5;
+    if (vocab_size <= 256 ? !wave || top <= 12 : vocab_size <= SHORT_ROW && !wave && top <= 16) return dtype == DISC_F32 ? launch_short<DISC_F32>(p, n, st) : launch_short<DISC_BF16>(p, n, st);
     if (dtype == DISC_F32) return top ? launch_logprobs<DISC_F32, true>(p, n, st) : launch_logprobs<DISC_F32, false>(p, n, st);
     return top ? launch_logprobs<DISC_BF16, true>(p, n, st) : launch_logprobs<DISC_BF16, false>(p, n, st);
 }
