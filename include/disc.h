@@ -518,7 +518,8 @@ int disc_attend_plan(const disc_cache_t* c, int32_t n_q_heads, int32_t group, vo
  *   out     device, [n_rows][n_q_heads][head_dim] contiguous, 16-byte aligned
  *   lse_out device, float[n_rows][n_q_heads] (nullable)
  * Scores, sums and outputs are accumulated in fp32; the probabilities are rounded to the inputs' type for
- * the second product, the outputs once at the end.  The result does not depend on the order in which the parts of
+ * the second product (up to 8 query vectors per group, min(group, n_rows) times the query heads of a key head: to twice its
+ * digits), the outputs once at the end.  The result does not depend on the order in which the parts of
  * a row finish, and a row's non-finite values do not reach the other rows of its group. */
 int disc_attend_cached(const disc_cache_t* c, int32_t layer, const void* q, int64_t q_row_stride, int64_t q_head_stride,
                        int32_t n_q_heads, int32_t group, float scale, void* plan, int64_t plan_bytes, void* out, float* lse_out,

@@ -205,6 +205,7 @@ struct Num<__nv_bfloat16> {
         const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
         return *reinterpret_cast<const uint32_t*>(&b);
     }
+    static __device__ __forceinline__ float2 unpack(uint32_t x) { return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); }
 };
 template <>
 struct Num<__half> {
@@ -217,6 +218,7 @@ struct Num<__half> {
         const __half2 b = __floats2half2_rn(lo, hi);
         return *reinterpret_cast<const uint32_t*>(&b);
     }
+    static __device__ __forceinline__ float2 unpack(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
 };
 
 constexpr int AT = 128;                // threads of an attention block
@@ -236,7 +238,12 @@ __device__ __forceinline__ uint32_t chunk_at(int row, int ch) {
     return uint32_t(row * (DP * 2) + ((ch ^ (row & 7)) << 4));
 }
 
-template <typename T, int DP>
+// The second product takes the probabilities in the inputs' type.  EIGHT: up to 8 query vectors, which leaves rows 8-15 of its
+// tile free.  They take what the rounding left out, and V is multiplied with the probabilities to 2^-17 (bf16; f16 2^-22) at no
+// cost: a thread's second row holds the remainders of its first.  They have sums of their own until the end, where a sum that is not
+// finite is dropped: the remainder of a probability can be 0, and 0 times an infinite value is none of the result.  With 9 to 16
+// vectors the probabilities are rounded once; a second product there cost 7 % (64 ragged rows: 182 us against 170).
+template <typename T, int DP, bool EIGHT>
 __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams p) {
     let_later_in();
     wait_for_earlier();
@@ -350,17 +357,17 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
                 for (int e = 0; e < 2; ++e) {
                     const bool some = h * 8 + (lane & 3) * 2 + e < tokens;
                     s[h][e] = some && in0 ? s[h][e] * p.c2 : -CUDART_INF_F;
-                    s[h][2 + e] = some && in1 ? s[h][2 + e] * p.c2 : -CUDART_INF_F;
+                    s[h][2 + e] = !EIGHT && some && in1 ? s[h][2 + e] * p.c2 : -CUDART_INF_F;
                     mx0 = fmaxf(mx0, s[h][e]);
-                    mx1 = fmaxf(mx1, s[h][2 + e]);
+                    if (!EIGHT) mx1 = fmaxf(mx1, s[h][2 + e]);
                 }
             mx0 = fmaxf(mx0, __shfl_xor_sync(FULL, mx0, 1));
-            mx1 = fmaxf(mx1, __shfl_xor_sync(FULL, mx1, 1));
+            if (!EIGHT) mx1 = fmaxf(mx1, __shfl_xor_sync(FULL, mx1, 1));
             mx0 = fmaxf(mx0, __shfl_xor_sync(FULL, mx0, 2));
-            mx1 = fmaxf(mx1, __shfl_xor_sync(FULL, mx1, 2));
-            if (__any_sync(FULL, mx0 > m0 || mx1 > m1)) {
+            if (!EIGHT) mx1 = fmaxf(mx1, __shfl_xor_sync(FULL, mx1, 2));
+            if (__any_sync(FULL, mx0 > m0 || (!EIGHT && mx1 > m1))) {
                 const float n0 = fmaxf(m0, mx0), n1 = fmaxf(m1, mx1);
-                const float f0 = m0 > -CUDART_INF_F ? ex2_approx(m0 - n0) : 0.f, f1 = m1 > -CUDART_INF_F ? ex2_approx(m1 - n1) : 0.f;
+                const float f0 = m0 > -CUDART_INF_F ? ex2_approx(m0 - n0) : 0.f, f1 = EIGHT ? f0 : m1 > -CUDART_INF_F ? ex2_approx(m1 - n1) : 0.f;
                 m0 = n0;
                 m1 = n1;
                 l0 *= f0;
@@ -376,11 +383,17 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
                 float* x = s[h];
                 x[0] = ex2_approx(x[0] - ref0);
                 x[1] = ex2_approx(x[1] - ref0);
-                x[2] = ex2_approx(x[2] - ref1);
-                x[3] = ex2_approx(x[3] - ref1);
                 l0 += x[0] + x[1];
-                l1 += x[2] + x[3];
                 pf[2 * h] = Num<T>::pack(x[0], x[1]);
+                if (EIGHT) {
+                    const float2 r = Num<T>::unpack(pf[2 * h]);
+                    x[2] = x[0] - r.x;
+                    x[3] = x[1] - r.y;
+                } else {
+                    x[2] = ex2_approx(x[2] - ref1);
+                    x[3] = ex2_approx(x[3] - ref1);
+                    l1 += x[2] + x[3];
+                }
                 pf[2 * h + 1] = Num<T>::pack(x[2], x[3]);
             }
 #pragma unroll
@@ -398,7 +411,7 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
                     Num<T>::mma(t0, pf, vf[0], vf[1]);
                     Num<T>::mma(t1, pf, vf[2], vf[3]);
                     if (in0) { o[2 * j][0] += t0[0]; o[2 * j][1] += t0[1]; o[2 * j + 1][0] += t1[0]; o[2 * j + 1][1] += t1[1]; }
-                    if (in1) { o[2 * j][2] += t0[2]; o[2 * j][3] += t0[3]; o[2 * j + 1][2] += t1[2]; o[2 * j + 1][3] += t1[3]; }
+                    if (EIGHT ? in0 : in1) { o[2 * j][2] += t0[2]; o[2 * j][3] += t0[3]; o[2 * j + 1][2] += t1[2]; o[2 * j + 1][3] += t1[3]; }
                 }
             }
         }
@@ -414,6 +427,11 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
 #pragma unroll
         for (int j = 0; j < DP / 8; ++j) {
             float* a = os + (warp * 16 + (lane >> 2)) * DP + j * 8 + (lane & 3) * 2;
+            if (EIGHT) {
+                const float r0 = fabsf(o[j][2]) < CUDART_INF_F ? o[j][2] : 0.f, r1 = fabsf(o[j][3]) < CUDART_INF_F ? o[j][3] : 0.f;
+                *reinterpret_cast<float2*>(a) = make_float2(o[j][0] + r0, o[j][1] + r1);
+                continue;
+            }
             *reinterpret_cast<float2*>(a) = make_float2(o[j][0], o[j][1]);
             *reinterpret_cast<float2*>(a + 8 * DP) = make_float2(o[j][2], o[j][3]);
         }
@@ -510,16 +528,17 @@ int shift_of(int32_t page_size) {
     return s;
 }
 
-template <typename T, int DP>
+template <typename T, int DP, bool EIGHT>
 int launch_attend(const AttendParams& p, unsigned grid, cudaStream_t st) {
     constexpr int bytes = AttendSmem<DP>::BYTES;
     static std::atomic<uint64_t> done{0};
-    if (const int rc = allow_smem(attend_cached_kernel<T, DP>, bytes, done)) return rc;
-    return launch_after(attend_cached_kernel<T, DP>, grid, AT, bytes, st, p);
+    if (const int rc = allow_smem(attend_cached_kernel<T, DP, EIGHT>, bytes, done)) return rc;
+    return launch_after(attend_cached_kernel<T, DP, EIGHT>, grid, AT, bytes, st, p);
 }
 template <typename T>
 int launch_attend(const AttendParams& p, unsigned grid, cudaStream_t st) {
-    return p.D <= 64 ? launch_attend<T, 64>(p, grid, st) : launch_attend<T, 128>(p, grid, st);
+    if (p.shape.M <= 8) return p.D <= 64 ? launch_attend<T, 64, true>(p, grid, st) : launch_attend<T, 128, true>(p, grid, st);
+    return p.D <= 64 ? launch_attend<T, 64, false>(p, grid, st) : launch_attend<T, 128, false>(p, grid, st);
 }
 
 }  // namespace
