@@ -25,10 +25,6 @@
 // order of the items.
 // Measured on 64 rows of 1 to 8191 tokens, 32 / 8 heads of 128, bf16: 159 us for 1.04 GB, the measured copy rate.
 
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-#include <math_constants.h>
-
 #include "disc_attend.cuh"
 
 namespace {
@@ -45,10 +41,6 @@ constexpr int CLUSTER = 8;
 constexpr int PT = 512;                // threads of a plan block
 
 // ---- the plan ---------------------------------------------------------------------------------------
-__device__ __forceinline__ void cluster_sync_all() {
-    __syncwarp();                     // .aligned: the whole warp at once, also after a loop that its lanes left apart
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 
 __device__ __forceinline__ int32_t warp_incl_scan(int32_t v, int lane) {
 #pragma unroll
@@ -171,56 +163,9 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(PT) attend_plan_ker
 }
 
 // ---- attention --------------------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return uint32_t(__cvta_generic_to_shared(p)); }
-// 16 bytes into shared memory; zeros when !some
-__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool some) {
-    const int n = some ? 16 : 0;
-    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-}
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ void ldsm4(uint32_t a, uint32_t* r) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
-}
-__device__ __forceinline__ void ldsm4t(uint32_t a, uint32_t* r) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
-}
-__device__ __forceinline__ float ex2_approx(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-template <typename T>
-struct Num;
-template <>
-struct Num<__nv_bfloat16> {
-    static __device__ __forceinline__ void mma(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    }
-    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
-        const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
-        return *reinterpret_cast<const uint32_t*>(&b);
-    }
-    static __device__ __forceinline__ float2 unpack(uint32_t x) { return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); }
-};
-template <>
-struct Num<__half> {
-    static __device__ __forceinline__ void mma(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    }
-    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
-        const __half2 b = __floats2half2_rn(lo, hi);
-        return *reinterpret_cast<const uint32_t*>(&b);
-    }
-    static __device__ __forceinline__ float2 unpack(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
-};
-
 constexpr int AT = 128;                // threads of an attention block
 
 template <int DP>
@@ -230,13 +175,6 @@ struct AttendSmem {
     static constexpr int Q_BYTES = 16 * ROW;
     static constexpr int BYTES = STAGES * 2 * TILE_BYTES + Q_BYTES + 256;
 };
-
-// 16-byte chunk `ch` of row `row` of a tile whose rows are DP values long: neighbouring rows' chunks lie in
-// different banks, so that ldmatrix reads eight rows at once without conflicts
-template <int DP>
-__device__ __forceinline__ uint32_t chunk_at(int row, int ch) {
-    return uint32_t(row * (DP * 2) + ((ch ^ (row & 7)) << 4));
-}
 
 // The second product takes the probabilities in the inputs' type.  EIGHT: up to 8 query vectors, which leaves rows 8-15 of its
 // tile free.  They take what the rounding left out, and V is multiplied with the probabilities to 2^-17 (bf16; f16 2^-22) at no
@@ -346,8 +284,8 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
                     uint32_t kf[4];
                     // matrices: tokens 0-7 and 8-15 of the block, each k 0-7 and 8-15
                     ldsm4(kt + chunk_at<DP>(warp * BLK + (lane & 7) + ((lane >> 4) << 3), 2 * kk + ((lane >> 3) & 1)), kf);
-                    Num<T>::mma(s[0], qf[kk], kf[0], kf[1]);
-                    Num<T>::mma(s[1], qf[kk], kf[2], kf[3]);
+                    mma16<T>(s[0], qf[kk], kf[0], kf[1]);
+                    mma16<T>(s[1], qf[kk], kf[2], kf[3]);
                 }
             }
             const bool in0 = !owner || owner == own_lo, in1 = !owner || owner == own_hi;
@@ -384,9 +322,9 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
                 x[0] = ex2_approx(x[0] - ref0);
                 x[1] = ex2_approx(x[1] - ref0);
                 l0 += x[0] + x[1];
-                pf[2 * h] = Num<T>::pack(x[0], x[1]);
+                pf[2 * h] = pack2<T>(x[0], x[1]);
                 if (EIGHT) {
-                    const float2 r = Num<T>::unpack(pf[2 * h]);
+                    const float2 r = unpack2<T>(pf[2 * h]);
                     x[2] = x[0] - r.x;
                     x[3] = x[1] - r.y;
                 } else {
@@ -394,7 +332,7 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
                     x[3] = ex2_approx(x[3] - ref1);
                     l1 += x[2] + x[3];
                 }
-                pf[2 * h + 1] = Num<T>::pack(x[2], x[3]);
+                pf[2 * h + 1] = pack2<T>(x[2], x[3]);
             }
 #pragma unroll
             for (int j = 0; j < DP / 16; ++j) {
@@ -402,14 +340,14 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
                 // matrices: tokens 0-7, 8-15 of the block at values 16j..16j+7, then at 16j+8..16j+15
                 ldsm4t(vt + chunk_at<DP>(warp * BLK + (lane & 15), 2 * j + (lane >> 4)), vf);
                 if (!owner) {
-                    Num<T>::mma(o[2 * j], pf, vf[0], vf[1]);
-                    Num<T>::mma(o[2 * j + 1], pf, vf[2], vf[3]);
+                    mma16<T>(o[2 * j], pf, vf[0], vf[1]);
+                    mma16<T>(o[2 * j + 1], pf, vf[2], vf[3]);
                 } else {
                     // a row's own tokens: what they add to other rows is 0 * v, which is not 0 for a
                     // non-finite v, so it is left out
                     float t0[4] = {0.f, 0.f, 0.f, 0.f}, t1[4] = {0.f, 0.f, 0.f, 0.f};
-                    Num<T>::mma(t0, pf, vf[0], vf[1]);
-                    Num<T>::mma(t1, pf, vf[2], vf[3]);
+                    mma16<T>(t0, pf, vf[0], vf[1]);
+                    mma16<T>(t1, pf, vf[2], vf[3]);
                     if (in0) { o[2 * j][0] += t0[0]; o[2 * j][1] += t0[1]; o[2 * j + 1][0] += t1[0]; o[2 * j + 1][1] += t1[1]; }
                     if (EIGHT ? in0 : in1) { o[2 * j][2] += t0[2]; o[2 * j][3] += t0[3]; o[2 * j + 1][2] += t1[2]; o[2 * j + 1][3] += t1[3]; }
                 }
@@ -468,7 +406,7 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
                 if (d == 0) p.plan.part_lse[slot + m] = lse2;
             } else {
                 const int64_t at = int64_t(r0 + m / G) * p.kv_heads * G + head * G + m % G;
-                *reinterpret_cast<uint2*>(p.out + (at * p.D + d) * 2) = make_uint2(Num<T>::pack(x.x, x.y), Num<T>::pack(x.z, x.w));
+                *reinterpret_cast<uint2*>(p.out + (at * p.D + d) * 2) = make_uint2(pack2<T>(x.x, x.y), pack2<T>(x.z, x.w));
                 if (d == 0 && p.lse) p.lse[at] = lse2 * LN2_F;
             }
         }
@@ -514,7 +452,7 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
                     const float inv = total > 0.f ? 1.f / total : (total == 0.f ? 0.f : total);
                     const int64_t at = int64_t(r0 + m / G) * p.kv_heads * G + head * G + m % G;
                     *reinterpret_cast<uint2*>(p.out + (at * p.D + d) * 2) =
-                        make_uint2(Num<T>::pack(x.x * inv, x.y * inv), Num<T>::pack(x.z * inv, x.w * inv));
+                        make_uint2(pack2<T>(x.x * inv, x.y * inv), pack2<T>(x.z * inv, x.w * inv));
                     if (d == 0 && p.lse) p.lse[at] = total > 0.f ? (top + log2f(total)) * LN2_F : (total == 0.f ? -CUDART_INF_F : total);
                 }
             }

@@ -1,7 +1,7 @@
 // What the two forms of the attention over the cache share: the plan's sizes and places (disc_attend.cu, disc_attend_group.cu).
 #pragma once
 
-#include "disc_internal.cuh"
+#include "disc_sm100.cuh"
 
 namespace disc {
 
@@ -129,6 +129,41 @@ __host__ __device__ inline Cut cut_group(int32_t at, int32_t blocks, int32_t sha
 __device__ inline void first_items(int32_t* first, int32_t at, int32_t blocks, int32_t share, const Cut& cut, int32_t item0, int32_t items) {
     for (int32_t lane = (at + share - 1) / share; lane * share < at + blocks + START; ++lane)
         first[lane] = item0 + (lane * share < at + blocks ? lane - cut.from : lane * share == at ? 0 : items);
+}
+
+// ---- loads and products by mma.sync -------------------------------------------------------------------
+// 16 bytes into shared memory; zeros when !some
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool some) {
+    const int n = some ? 16 : 0;
+    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t a, uint32_t* r) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t a, uint32_t* r) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+// d += a b, 16 x 16 by 16 x 8
+template <typename T>
+__device__ __forceinline__ void mma16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void mma16<__nv_bfloat16>(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <>
+__device__ __forceinline__ void mma16<__half>(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// 16-byte chunk `ch` of row `row` of a tile whose rows are DP values long: neighbouring rows' chunks lie in
+// different banks, so that ldmatrix reads eight rows at once without conflicts
+template <int DP>
+__device__ __forceinline__ uint32_t chunk_at(int row, int ch) {
+    return uint32_t(row * (DP * 2) + ((ch ^ (row & 7)) << 4));
 }
 
 struct PlanParams {

@@ -20,7 +20,6 @@
 // second product, and its missing scores are masked, so that nothing stale is ever multiplied.
 
 #include "disc_attend.cuh"
-#include "disc_sm100.cuh"
 
 namespace {
 
@@ -413,36 +412,6 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
 
 // ---- kernel 2 -----------------------------------------------------------------------------------------
 constexpr int JT = 128;                // threads of a block: 4 warps, each with a row and key head of its own
-
-__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool some) {
-    const int n = some ? 16 : 0;
-    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-}
-__device__ __forceinline__ void ldsm4(uint32_t a, uint32_t* r) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
-}
-__device__ __forceinline__ void ldsm4t(uint32_t a, uint32_t* r) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
-}
-template <typename T>
-__device__ __forceinline__ void mma16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1);
-template <>
-__device__ __forceinline__ void mma16<__nv_bfloat16>(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-template <>
-__device__ __forceinline__ void mma16<__half>(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// 16-byte chunk ch of row `row` of a block in shared memory; neighbouring rows' chunks lie in different banks
-template <int DP>
-__device__ __forceinline__ uint32_t chunk_at(int row, int ch) {
-    return uint32_t(row * (DP * 2) + ((ch ^ (row & 7)) << 4));
-}
 
 // an 8 x 8 matrix of 16-bit values across the warp, transposed
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {

@@ -120,15 +120,6 @@ constexpr int XT = 1024;
 constexpr int CLUSTER = 8;
 constexpr int ONE_BLOCK = 8192;        // up to this many pages (and XT rows): one block
 
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync_all() {
-    __syncwarp();                     // .aligned: the whole warp at once, also after a loop that its lanes left apart
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 __device__ __forceinline__ int32_t remote_int(const int32_t* p, uint32_t rank) {
     uint32_t a;
     int32_t v;

@@ -124,6 +124,17 @@ inline int launch_after(void (*kernel)(P...), unsigned grid, unsigned block, siz
 __device__ __forceinline__ void wait_for_earlier() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void let_later_in() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+// the block's number in its cluster, and the barrier of the cluster
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync_all() {
+    __syncwarp();                     // .aligned: the whole warp at once, also after a loop that its lanes left apart
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
 // ------------------------------------------------------------------ Philox4x32-10
 // Counter-based generator of Salmon et al. (SC'11).  Round keys depend only on the seed.
 struct PhiloxKey {

@@ -32,9 +32,15 @@
 #include <cuda_bf16.h>
 #include <math_constants.h>
 
-#include "disc_internal.cuh"
+#include "disc_sm100.cuh"
 
 namespace {
+
+using disc::add2;
+using disc::cluster_rank;
+using disc::cluster_sync_all;
+using disc::ex2_approx;
+using disc::fma2;
 
 constexpr int NT = 256;               // threads per block
 constexpr int NW = NT / 32;
@@ -68,11 +74,6 @@ struct LogprobParams {
     uint8_t* status;
 };
 
-__device__ __forceinline__ float ex2_approx(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 // the larger of the two, NaN if either is
 __device__ __forceinline__ float max_nan(float a, float b) {
     float y;
@@ -209,20 +210,6 @@ struct RowShape {
 struct Sums {
     float m, ref, s, u;               // largest logit, its y; sums relative to ref
 };
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    float2 d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;"
-        : "=l"(reinterpret_cast<unsigned long long&>(d))
-        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)), "l"(reinterpret_cast<unsigned long long&>(c)));
-    return d;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-    float2 d;
-    asm("add.rn.f32x2 %0, %1, %2;"
-        : "=l"(reinterpret_cast<unsigned long long&>(d))
-        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
-    return d;
-}
 struct Scale {
     float c2, low_y;
 };
@@ -304,15 +291,6 @@ __device__ __forceinline__ unsigned long long entry(uint32_t key, int32_t id) {
     return (static_cast<unsigned long long>(key) << 32) | uint32_t(~id);
 }
 
-__device__ __forceinline__ uint32_t cluster_ctarank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync_all() {
-    __syncwarp();                     // .aligned: the whole warp at once, also after a loop that its lanes left apart
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 __device__ __forceinline__ uint32_t remote(const void* p, uint32_t rank) {
     uint32_t a;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(uint32_t(__cvta_generic_to_shared(p))), "r"(rank));
@@ -553,7 +531,7 @@ __global__ void __launch_bounds__(NT, 5) disc_logprobs_kernel(const LogprobParam
     PortionMaxima<DT>& pm = *reinterpret_cast<PortionMaxima<DT>*>(smem_raw + sizeof(Smem));      // only with TOP
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t row = blockIdx.x / unsigned(p.split);
-    const uint32_t rank = p.split > 1 ? cluster_ctarank() : 0u;
+    const uint32_t rank = p.split > 1 ? cluster_rank() : 0u;
     const RowShape<DT> r(p.logits, p.ld, row, p.V);
     const uint4* vecs = r.vecs();
 

@@ -111,21 +111,11 @@ __device__ __forceinline__ bool taken_block(const void* answer, unsigned& block)
     return ok != 0;
 }
 
-__device__ __forceinline__ void unpack8(const unsigned char* src, float* x, const __nv_bfloat16*) {
+template <typename T>
+__device__ __forceinline__ void unpack8(const unsigned char* src, float* x) {
     const uint4 w = *reinterpret_cast<const uint4*>(src);
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) { x[2 * j] = __uint_as_float(u[j] << 16); x[2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u); }
-}
-__device__ __forceinline__ void unpack8(const unsigned char* src, float* x, const __half*) {
-    const uint4 w = *reinterpret_cast<const uint4*>(src);
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[j]));
-        x[2 * j] = f.x;
-        x[2 * j + 1] = f.y;
-    }
+    const float2 a = unpack2<T>(w.x), b = unpack2<T>(w.y), c = unpack2<T>(w.z), d = unpack2<T>(w.w);
+    x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y; x[4] = c.x; x[5] = c.y; x[6] = d.x; x[7] = d.y;
 }
 // A query's output that is not finite.  Its blocks of keys end at `end`, and it sees the first `sees` of them.  If a token in its
 // last blocks that it does not see has a non-finite value vector and none there that it sees, the output is formed again from what
@@ -133,13 +123,12 @@ __device__ __forceinline__ void unpack8(const unsigned char* src, float* x, cons
 template <typename T>
 __device__ __noinline__ void row_alone(const PromptParams& p, int64_t q_tok, int q_head, int k_head, int64_t k0, int sees, int end, float ref, float inv,
                                        unsigned char* dst) {
-    const T* type = nullptr;
     const unsigned char* v = p.v + k0 * p.v_token + k_head * p.v_head;
     float hidden = 0.f, seen = 0.f;                    // NaN once a value is not finite
     for (int j = sees / TN * TN; j < end; ++j)
         for (int c = 0; c < p.D; c += 8) {
             float x[8];
-            unpack8(v + j * p.v_token + c * 2, x, type);
+            unpack8<T>(v + j * p.v_token + c * 2, x);
             for (int e = 0; e < 8; ++e) (j < sees ? seen : hidden) += 0.f * x[e];
         }
     if (hidden == 0.f || seen != 0.f) return;
@@ -150,13 +139,13 @@ __device__ __noinline__ void row_alone(const PromptParams& p, int64_t q_tok, int
         for (int j = 0; j < sees; ++j) {
             float s = 0.f, x[8], y[8];
             for (int d = 0; d < p.D; d += 8) {
-                unpack8(q + d * 2, x, type);
-                unpack8(k + j * p.k_token + d * 2, y, type);
+                unpack8<T>(q + d * 2, x);
+                unpack8<T>(k + j * p.k_token + d * 2, y);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) s = fmaf(x[e], y[e], s);
             }
             const float pr = ex2_approx(fmaf(s, p.c2, -ref));
-            unpack8(v + j * p.v_token + c * 2, x, type);
+            unpack8<T>(v + j * p.v_token + c * 2, x);
 #pragma unroll
             for (int e = 0; e < 8; ++e) o[e] = fmaf(pr, x[e], o[e]);
         }
