@@ -732,8 +732,8 @@ __global__ void __launch_bounds__(NT, 5) disc_logprobs_kernel(const LogprobParam
 // ---- gradient ---------------------------------------------------------------------------------------
 // With a = d logp, b = dH of the row (H = entropy, p_v = 2^(y_v - lse log2e)):
 //   dz_v = (a [v = t] - p_v (a + b (log p_v + H))) / T
-// One read and one write per logit; one 2^x and a handful of multiply-adds, bound by the bytes: 45 us for
-// 2047 x 32000 bf16 (0.26 GB, 5.8 TB/s).
+// One read and one write per logit; one 2^x and a handful of multiply-adds, bound by the bytes: 44 us for
+// 2047 x 32000 bf16 (0.26 GB, 6.0 TB/s).
 struct GradParams {
     const void* logits;
     int64_t ld;
@@ -749,22 +749,67 @@ struct GradParams {
 };
 
 struct RowGrad {
-    float m, l2;                      // y - log2 sum = (x - m) c2 - l2: m = 0 and the log-sum-exp, or the row's maximum and its own sum
-    float a_bh, b, scale;             // a + b H; b ln2; 1/T
+    float l2, a_bh, b, scale, a_t;    // lse in units of y; a + b H; b ln2; 1/T; a / T
+    float m;                          // ANEW: the row's maximum, and l2 its sum relative to that
+    int32_t tok;
+    template <bool ANEW>
     __device__ __forceinline__ float at(float x, float c2) const {
-        const float y = max_nan(fmaf(x - m, c2, -l2), Y_MIN);
+        const float y = max_nan(fmaf(ANEW ? x - m : x, c2, -l2), Y_MIN);
         return -scale * ex2_approx(y) * fmaf(y, b, a_bh);
     }
 };
+// a thread's vectors v0, v0 + TEAM, ... of a row
+template <int DT, int TEAM>
+__device__ __forceinline__ void load_vectors(const RowShape<DT>& r, int32_t v0, uint4* w) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (v0 + u * TEAM < r.nvec) w[u] = ld_stream_own(r.vecs() + v0 + u * TEAM);
+}
+template <int DT, int TEAM, bool ANEW>
+__device__ __forceinline__ void grad_vectors(const RowShape<DT>& r, char* out, const RowGrad& g, float c2, int32_t v0, const uint4* w) {
+    constexpr int E = Vec<DT>::E, SIZE = Vec<DT>::SIZE;
+    const bool together = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(r.base)) & 15) == 0;
+    char* out_vecs = out + size_t(r.head) * SIZE;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int32_t v = v0 + u * TEAM;
+        if (v < r.nvec) {
+            float x[E];
+            Vec<DT>::unpack(w[u], x);
+            const int32_t at = g.tok - (r.head + v * E);
+#pragma unroll
+            for (int j = 0; j < E; ++j) x[j] = g.template at<ANEW>(x[j], c2) + (at == j ? g.a_t : 0.f);
+            if (together) __stcs(reinterpret_cast<uint4*>(out_vecs) + v, Vec<DT>::pack(x));
+            else
+#pragma unroll
+                for (int j = 0; j < E; ++j) Vec<DT>::put(out_vecs + (size_t(v) * E + j) * SIZE, x[j]);
+        }
+    }
+}
+// a thread's element before or after the vectors, -1: none
+template <int DT>
+__device__ __forceinline__ int32_t around_vectors(const RowShape<DT>& r, int tid) {
+    if (tid < r.head) return tid;
+    return tid - r.head < r.tail ? r.head + r.nvec * Vec<DT>::E + tid - r.head : -1;
+}
+template <int DT, bool ANEW>
+__device__ __forceinline__ void grad_element(const RowShape<DT>& r, char* out, const RowGrad& g, float c2, int32_t e) {
+    constexpr int SIZE = Vec<DT>::SIZE;
+    if (e >= 0) Vec<DT>::put(out + size_t(e) * SIZE, g.template at<ANEW>(Vec<DT>::at(r.base + size_t(e) * SIZE), c2) + (e == g.tok ? g.a_t : 0.f));
+}
+
 // A log-sum-exp is given rounded to fp32, which puts a factor 1 +- |lse| 2^-24 on all probabilities of the row: 8e-6 up to this
 // limit.  For rows beyond it (low temperatures, rows masked with a finite value, where log S would be lost) one team takes the
-// whole row, forms maximum and sum anew and then the gradient; the row's other teams have nothing to do.  (4096 x 32000 bf16: 88 us
-// when all rows are within the limit, 128 when all are beyond it; 16 x 128256: 12 and 29.)
+// whole row, forms maximum and sum anew and then the gradient; the row's other teams have nothing to do.  (4096 x 32000 bf16: 82 us
+// when all rows are within the limit, 140 when all are beyond it; 16 x 128256: 12 and 28.)
 constexpr float LSE_LIMIT = 128.f;
 
-// the row's maximum and log2 of its sum of 2^((x - m) c2); called by the whole team
+// Called by the whole team.
 template <int DT, int TEAM>
-__device__ __noinline__ float2 row_norm(const RowShape<DT>& r, int tid, int32_t extra, float c2) {
+__device__ __noinline__ void row_anew(const void* logits, int64_t ld, char* out, int32_t V, int64_t row, int tid, RowGrad g, float c2) {
+    const RowShape<DT> r(logits, ld, row, V);
+    const int32_t extra = around_vectors(r, tid);
+    // the row's maximum m and its sum s of 2^((x - m) c2)
     constexpr int E = Vec<DT>::E, SIZE = Vec<DT>::SIZE, UN = 2;
     float m = -CUDART_INF_F, s = 0.f;
     auto up_to = [&](float mx) {
@@ -803,73 +848,47 @@ __device__ __noinline__ float2 row_norm(const RowShape<DT>& r, int tid, int32_t 
         s = 0.f;
         for (int w = 0; w < NW; ++w) join(warps[w].x, warps[w].y);
     }
-    return make_float2(m, log2f(s));
+    g.m = m;
+    g.l2 = log2f(s);
+    for (int32_t v = tid; v < r.nvec; v += TEAM * U) {
+        uint4 w[U];
+        load_vectors<DT, TEAM>(r, v, w);
+        grad_vectors<DT, TEAM, true>(r, out, g, c2, v, w);
+    }
+    grad_element<DT, true>(r, out, g, c2, extra);
 }
 
 // TEAM threads work on a portion of a row: a block, or a warp where a warp's loads cover the row.
 template <int DT, int TEAM>
-__global__ void __launch_bounds__(NT) disc_logprobs_grad_kernel(const GradParams p, int64_t n) {
-    constexpr int E = Vec<DT>::E, SIZE = Vec<DT>::SIZE;
+__global__ void __launch_bounds__(NT, TEAM == NT ? 6 : 5) disc_logprobs_grad_kernel(const GradParams p, int64_t n) {
     const int64_t team = (int64_t(blockIdx.x) * NT + threadIdx.x) / TEAM;
     const int64_t row = TEAM == NT ? int64_t(blockIdx.x / unsigned(p.teams_per_row)) : team;
     const int32_t part = TEAM == NT ? int32_t(blockIdx.x - row * p.teams_per_row) : 0;
     const int tid = threadIdx.x % TEAM;
     if (row >= n) return;
     const RowShape<DT> r(p.logits, p.ld, row, p.V);
-    char* out = static_cast<char*>(p.grad) + row * p.grad_ld * SIZE;
-    const int32_t tok = p.targets ? p.targets[row] : -1;
-    const float a = p.d_logp && tok >= 0 && tok < p.V ? p.d_logp[row] : 0.f;
+    char* out = static_cast<char*>(p.grad) + row * p.grad_ld * Vec<DT>::SIZE;
+    const int32_t v0 = part * (TEAM * U) + tid;
+    uint4 w[U];
+    load_vectors<DT, TEAM>(r, v0, w);  // under way while the row's numbers come in
+    RowGrad g;
+    g.tok = p.targets ? p.targets[row] : -1;
+    const float a = p.d_logp && g.tok >= 0 && g.tok < p.V ? p.d_logp[row] : 0.f;
     const float b = p.d_entropy ? p.d_entropy[row] : 0.f;
     const float lse = p.lse[row];
-    int32_t extra = -1;               // a thread's element before or after the vectors
-    if (part == 0) {
-        if (tid < r.head) extra = tid;
-        else if (tid - r.head < r.tail) extra = r.head + r.nvec * E + tid - r.head;
-    }
-    RowGrad g;
-    g.m = 0.f;
     g.l2 = lse * LOG2E_F;
     g.a_bh = b != 0.f ? fmaf(b, p.entropy[row], a) : a;
     g.b = b * LN2_F;
     g.scale = p.inv_t;
     if (lse == -CUDART_INF_F) { g.l2 = 0.f; g.scale = 0.f; }      // no mass: nothing to move
     else if (!(lse < CUDART_INF_F)) g.l2 = CUDART_NAN_F;          // +inf or NaN among the logits: no gradient is finite
-    const bool anew = fabsf(lse) >= LSE_LIMIT && fabsf(lse) < CUDART_INF_F;
-    if (anew) {
-        if (part != 0) return;
-        const float2 norm = row_norm<DT, TEAM>(r, tid, extra, p.c2);
-        g.m = norm.x;
-        g.l2 = norm.y;
+    g.a_t = g.scale * a;
+    if (fabsf(lse) >= LSE_LIMIT && fabsf(lse) < CUDART_INF_F) {
+        if (part == 0) row_anew<DT, TEAM>(p.logits, p.ld, out, p.V, row, tid, g, p.c2);
+        return;
     }
-    const float a_t = g.scale * a;
-
-    const bool together = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(r.base)) & 15) == 0;
-    const uint4* vecs = r.vecs();
-    char* out_vecs = out + size_t(r.head) * SIZE;
-    int32_t v0 = part * (TEAM * U) + tid;
-    do {
-        uint4 w[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (v0 + u * TEAM < r.nvec) w[u] = ld_stream_own(vecs + v0 + u * TEAM);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int32_t v = v0 + u * TEAM;
-            if (v < r.nvec) {
-                float x[E];
-                Vec<DT>::unpack(w[u], x);
-                const int32_t at = tok - (r.head + v * E);
-#pragma unroll
-                for (int j = 0; j < E; ++j) x[j] = g.at(x[j], p.c2) + (at == j ? a_t : 0.f);
-                if (together) __stcs(reinterpret_cast<uint4*>(out_vecs) + v, Vec<DT>::pack(x));
-                else
-#pragma unroll
-                    for (int j = 0; j < E; ++j) Vec<DT>::put(out_vecs + (size_t(v) * E + j) * SIZE, x[j]);
-            }
-        }
-        v0 += TEAM * U;
-    } while (anew && v0 < r.nvec);
-    if (extra >= 0) Vec<DT>::put(out + size_t(extra) * SIZE, g.at(Vec<DT>::at(r.base + size_t(extra) * SIZE), p.c2) + (extra == tok ? a_t : 0.f));
+    grad_vectors<DT, TEAM, false>(r, out, g, p.c2, v0, w);
+    if (part == 0) grad_element<DT, false>(r, out, g, p.c2, around_vectors(r, tid));
 }
 
 template <int DT, int EPL>
