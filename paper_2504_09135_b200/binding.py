@@ -128,6 +128,7 @@ def _check(rc: int, where: str):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _initialized = False
+_several = torch.cuda.device_count() > 1        # otherwise there is no other device to be on
 
 
 def _stream_ptr(stream=None) -> int:
@@ -142,9 +143,9 @@ def _stream_ptr(stream=None) -> int:
 
 def _here(t: torch.Tensor, name: str) -> int:
     """Pointer of a CUDA tensor, which has to be on the current device: that is where the kernels are launched."""
-    if t.get_device() == _raw_device():
-        return t.data_ptr()
-    raise TypeError(f"{name}: on {t.device}, which is not the current device")
+    if _several and t.get_device() != _raw_device():
+        raise TypeError(f"{name}: on {t.device}, which is not the current device")
+    return t.data_ptr()
 
 
 def _dev(t: torch.Tensor, dtype, name: str) -> int:
@@ -152,7 +153,7 @@ def _dev(t: torch.Tensor, dtype, name: str) -> int:
         return 0
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()):
         raise TypeError(f"{name}: expected a contiguous CUDA tensor of {dtype}")
-    return t.data_ptr() if t.get_device() == _raw_device() else _here(t, name)
+    return _here(t, name) if _several else t.data_ptr()
 
 
 class DiscSet:

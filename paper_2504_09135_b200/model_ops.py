@@ -12,7 +12,6 @@ import math
 
 import torch
 
-from . import binding
 from .binding import DISC_BF16, DISC_F16, DISC_F32, DiscError, _Cache, _check, _dev, _here, _stream_ptr, lib
 
 _HALF = {torch.bfloat16: DISC_BF16, torch.float16: DISC_F16}
@@ -20,7 +19,7 @@ _LOGIT = {torch.float32: DISC_F32, torch.bfloat16: DISC_BF16}
 
 
 def _without_grad(t, name: str):
-    if t is not None and t.requires_grad and torch.is_grad_enabled():
+    if t.requires_grad and torch.is_grad_enabled():
         raise TypeError(f"{name}: requires a gradient, which this call does not give; detach it, or call under torch.no_grad()")
 
 
@@ -112,7 +111,7 @@ def disc_logprobs(logits: torch.Tensor, targets: torch.Tensor | None = None, *, 
     this one); lse and the alternatives have none, and `out` is refused."""
     if isinstance(logits, torch.Tensor) and logits.requires_grad and torch.is_grad_enabled():
         if out is not None:
-            _without_grad(logits, "logits with out")
+            raise TypeError("out: given buffers have no history; detach the logits, or call under torch.no_grad()")
         return dict(zip(_LOGPROBS, _Logprobs.apply(logits, targets, top, inv_temperature, stream)))
     ptr, dt, ld = _rows(logits, "disc_logprobs")
     n, V = logits.shape
@@ -136,10 +135,12 @@ def disc_logprobs_grad(logits: torch.Tensor, targets, lse: torch.Tensor, entropy
     lse, entropy: what disc_logprobs gave for these logits.  out may be `logits` itself."""
     ptr, dt, ld = _rows(logits, "disc_logprobs_grad")
     n, V = logits.shape
-    _without_grad(logits, "logits")
+    if logits.requires_grad:
+        _without_grad(logits, "logits")
     for t, name in ((targets, "targets"), (lse, "lse"), (entropy, "entropy"), (d_logp, "d_logp"), (d_entropy, "d_entropy")):
-        _want(t, n, name)
-        _without_grad(t, name)
+        if t is not None and (t.requires_grad or t.numel() != n):
+            _want(t, n, name)
+            _without_grad(t, name)
     if out is None:
         out = _alloc(stream, _empty, (n, V), logits.dtype, logits.device)
     elif out.shape != logits.shape or out.dtype != logits.dtype:
@@ -263,7 +264,6 @@ class DiscCache:
         self._scratch = torch.empty(int(need), dtype=torch.uint8, device=pool.device)
         self._c.scratch, self._c.scratch_bytes = self._scratch.data_ptr(), int(need)
         self._plans: dict = {}
-        self._device = pool.get_device()
         self._sizes = tuple(pool.shape) + (self.n_rows, self.table_width, pool.dtype)
 
     @staticmethod
@@ -275,8 +275,7 @@ class DiscCache:
 
 def _books(cache: DiscCache) -> int:
     """Address of the cache's sizes and pointers; its memory is on one device."""
-    if cache._device != binding._raw_device():
-        _here(cache.pool, "cache")
+    _here(cache.pool, "cache")
     return cache._p
 
 

@@ -25,6 +25,9 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
     plan = disc.disc_attend_plan(cache, 4)
     for call in calls[:5]:
         call()
+    monkeypatch.setattr(binding, "_several", True)
+    for call in calls[:5]:
+        call()
     monkeypatch.setattr(binding, "_raw_device", lambda: 1)
     for call in calls:
         with pytest.raises(TypeError, match="current device"):
