@@ -17,7 +17,9 @@
 // thread per query vector, one warp the loads (a TMA box of 16 tokens x 64 values per block, page by page),
 // one the MMAs.  Tensor memory: S 64 columns | O.  Tiles of 64 tokens, so that five of keys or values are on their way at a
 // time (with two of 128 tokens the loads came too late: 54 us against 50 on 128 prompts of 500 to 1024 tokens).  A last tile of fewer than 4 blocks takes fewer steps of the
-// second product, and its missing scores are masked, so that nothing stale is ever multiplied.
+// second product, and its missing scores are masked, so that nothing stale is ever multiplied.  P is rounded to the inputs' type, the
+// operand type of the second product; sums of the remainders apart from O, as the rows form has them, would need 320 of the 256
+// columns of tensor memory that a block can have with two to an SM.
 
 #include "disc_attend.cuh"
 

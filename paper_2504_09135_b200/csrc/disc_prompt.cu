@@ -36,7 +36,7 @@
 // against 88.0, 2 x 8192 tokens 513 against 510).
 // All waits are bounded; one that runs out sets the error word and every role leaves.
 //
-// Measured on 2 x 8192 tokens, 16 / 4 heads of 128: 445 us (1.24 PFLOP/s, 0.74 of cuBLAS' measured rate) in a short run, 520 us
+// Measured on 2 x 8192 tokens, 16 / 4 heads of 128: 457 us (1.20 PFLOP/s, 0.71 of cuBLAS' measured rate) in a short run, 515 us
 // under the power cap; 2,820 clocks per 256 x 128 block of scores, of which the products take 2,080 and the exponentials as many.
 
 #include <cuda_bf16.h>
