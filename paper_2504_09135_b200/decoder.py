@@ -119,6 +119,7 @@ class DiscDecoder:
             prev = torch.where(o.token >= 0, o.token.to(torch.int64), prev)
         return self.finish(seed=seed)
 
+    @torch.no_grad()
     def decode_cached(self, lm, cache: DiscCache, prompts: torch.Tensor, cu: torch.Tensor, max_len: int, *, seed=0,
                       inv_temperature=1.0, on_step=None):
         """Decode of a model of attention layers.

@@ -53,3 +53,34 @@ def test_no_prompt_tokens_at_all():
     with pytest.raises(ValueError):
         disc.DiscDecoder(G, 2, 4).decode_cached(lm, cache, torch.empty(0, dtype=torch.int32, device=DEV), cu, 0)
     G.close()
+
+
+def test_a_model_whose_weights_require_gradients():
+    """A decode has no backward pass: it is not recorded, whatever the caller's mode."""
+    w = scaled("tiny")
+    tok, off = make_set(w)
+    G = disc.disc_build_set(tok, off, w.V)
+    runs = []
+    for grad in (False, True):
+        lm = AttentionLM(w.V, 1, 4, 2, 32)
+
+        class Model:
+            hq = lm.hq
+
+            def prefill(self, *args):
+                return AttentionLM.prefill.__wrapped__(lm, *args)
+
+            def step(self, *args):
+                return AttentionLM.step.__wrapped__(lm, *args)
+
+            def logits(self, hidden):
+                return lm.logits(hidden)
+
+        for m in [lm.embed, lm.head] + [x for b in lm.blocks for x in b.values()]:
+            m.requires_grad_(grad)
+        cache = lm.new_cache(8, 64, n_pages=40)
+        dec = disc.DiscDecoder(G, 2, 4)
+        r = dec.decode_cached(Model(), cache, torch.arange(20, dtype=torch.int32, device=DEV), torch.tensor([0, 7, 20], dtype=torch.int32, device=DEV), 13, seed=3)
+        runs.append((dec.seq.clone(), r["idx"]))
+    assert all(torch.equal(a, b) for a, b in zip(*runs))
+    G.close()
