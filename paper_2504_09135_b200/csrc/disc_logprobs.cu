@@ -806,7 +806,7 @@ constexpr float LSE_LIMIT = 128.f;
 
 // Called by the whole team.
 template <int DT, int TEAM>
-__device__ __noinline__ void row_anew(const void* logits, int64_t ld, char* out, int32_t V, int64_t row, int tid, RowGrad g, float c2) {
+__device__ __noinline__ void row_anew(const void* logits, int64_t ld, char* out, int32_t V, int64_t row, int tid, float lse, RowGrad g, float c2) {
     const RowShape<DT> r(logits, ld, row, V);
     const int32_t extra = around_vectors(r, tid);
     // the row's maximum m and its sum s of 2^((x - m) c2)
@@ -848,8 +848,10 @@ __device__ __noinline__ void row_anew(const void* logits, int64_t ld, char* out,
         s = 0.f;
         for (int w = 0; w < NW; ++w) join(warps[w].x, warps[w].y);
     }
+    // A log-sum-exp that is not these logits' own, of a row that lies here only in part, say, is taken as it is given.
+    const float log_sum = log2f(s), given = fmaf(-m, g.scale, lse);
     g.m = m;
-    g.l2 = log2f(s);
+    g.l2 = fabsf(fmaf(log_sum, -LN2_F, given)) <= fabsf(lse) * 4.76837158203125e-7f ? log_sum : given * LOG2E_F;      // 2^-21
     for (int32_t v = tid; v < r.nvec; v += TEAM * U) {
         uint4 w[U];
         load_vectors<DT, TEAM>(r, v, w);
@@ -884,7 +886,7 @@ __global__ void __launch_bounds__(NT, TEAM == NT ? 6 : 5) disc_logprobs_grad_ker
     else if (!(lse < CUDART_INF_F)) g.l2 = CUDART_NAN_F;          // +inf or NaN among the logits: no gradient is finite
     g.a_t = g.scale * a;
     if (fabsf(lse) >= LSE_LIMIT && fabsf(lse) < CUDART_INF_F) {
-        if (part == 0) row_anew<DT, TEAM>(p.logits, p.ld, out, p.V, row, tid, g, p.c2);
+        if (part == 0) row_anew<DT, TEAM>(p.logits, p.ld, out, p.V, row, tid, lse, g, p.c2);
         return;
     }
     grad_vectors<DT, TEAM, false>(r, out, g, p.c2, v0, w);

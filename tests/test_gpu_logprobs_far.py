@@ -107,3 +107,23 @@ def test_rows_without_a_finite_sum_have_no_finite_gradient(dtype, V):
         g = disc.disc_logprobs_grad(z, t, r["lse"], r["entropy"], torch.ones(4, device=DEV), b)
         assert not torch.isfinite(g[:2]).any()
         assert torch.all(g[2] == 0) and torch.isfinite(g[3]).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V,cut", [(200, 77), (9000, 4000), (40001, 8)])
+@pytest.mark.parametrize("inv_t", [1.0, 40.0])
+def test_a_row_in_two_parts_with_the_whole_rows_log_sum_exp(dtype, V, cut, inv_t):
+    """Each part's gradient is its part of the whole row's: the log-sum-exp that is given counts, not the part's own.  It is held to
+    2^-24 of its size, as is its product with log2(e)."""
+    z = (torch.randn((6, V), device=DEV) * 4).to(dtype)
+    t = torch.full((6,), -1, dtype=torch.int32, device=DEV)
+    r = disc.disc_logprobs(z, inv_temperature=inv_t)
+    lp, p, H = reference(z, inv_t)
+    b = torch.randn(6, device=DEV)
+    for part, q, l in ((z[:, :cut], p[:, :cut], lp[:, :cut]), (z[:, cut:], p[:, cut:], lp[:, cut:])):
+        step = torch.where(q > 0, l, 0.0)
+        want = -q * (step + H[:, None]) * b.double()[:, None] * inv_t
+        got = disc.disc_logprobs_grad(part, t, r["lse"], r["entropy"], None, b, inv_temperature=inv_t)
+        rel = base(V) + 2.0 ** -21 * step.abs() + 2.0 ** -22 * r["lse"].double().abs()[:, None]
+        tol = inv_t * q * b.double().abs()[:, None] * (rel * (step.abs() + H[:, None] + 1) + base(V) * (2 + 2 * math.log(V + 1))) + UNIT[dtype] * want.abs() + 1e-30
+        assert torch.all((got.double() - want).abs() <= tol)
