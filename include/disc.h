@@ -425,7 +425,7 @@ int disc_logprobs_grad(const void* logits, disc_dtype_t dtype, int64_t ld, int64
  *               invalid), never cleared; read with disc_attend_error
  * Scores, sums and outputs are accumulated in fp32; the probabilities are rounded to the inputs' type for
  * the second product, the outputs once at the end.  Non-finite keys and values do not reach queries that do not see
- * them, of the same sequence or another.
+ * them, of the same sequence or another (but for an output that a value it sees makes infinite: it may come out as NaN).
  * Errors: DISC_ERR_ARG, DISC_ERR_UNSUPPORTED (dtype, head_dim, strides, head counts). */
 #define DISC_MAX_HEAD_DIM 128
 int disc_attend_prompt(const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride,

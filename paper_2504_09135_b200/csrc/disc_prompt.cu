@@ -117,24 +117,27 @@ __device__ __forceinline__ void unpack8(const unsigned char* src, float* x) {
     const float2 a = unpack2<T>(w.x), b = unpack2<T>(w.y), c = unpack2<T>(w.z), d = unpack2<T>(w.w);
     x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y; x[4] = c.x; x[5] = c.y; x[6] = d.x; x[7] = d.y;
 }
-// A query's output that is not finite.  Its blocks of keys end at `end`, and it sees the first `sees` of them.  If a token in its
-// last blocks that it does not see has a non-finite value vector and none there that it sees, the output is formed again from what
-// it sees: by one thread, 8 values at a time, against the reference and the sum that are known.
+// A query's output that is not finite.  Its blocks of keys end at `end`, and it sees the first `sees` of them.  Values that a
+// token of its last blocks makes non-finite which it does not see, and none there that it sees, are formed again from what it
+// sees: by one thread, 8 at a time, against the reference and the sum that are known.
 template <typename T>
 __device__ __noinline__ void row_alone(const PromptParams& p, int64_t q_tok, int q_head, int k_head, int64_t k0, int sees, int end, float ref, float inv,
                                        unsigned char* dst) {
-    const unsigned char* v = p.v + k0 * p.v_token + k_head * p.v_head;
-    float hidden = 0.f, seen = 0.f;                    // NaN once a value is not finite
-    for (int j = sees / TN * TN; j < end; ++j)
-        for (int c = 0; c < p.D; c += 8) {
-            float x[8];
-            unpack8<T>(v + j * p.v_token + c * 2, x);
-            for (int e = 0; e < 8; ++e) (j < sees ? seen : hidden) += 0.f * x[e];
-        }
-    if (hidden == 0.f || seen != 0.f) return;
     const unsigned char* q = p.q + q_tok * p.q_token + q_head * p.q_head;
     const unsigned char* k = p.k + k0 * p.k_token + k_head * p.k_head;
+    const unsigned char* v = p.v + k0 * p.v_token + k_head * p.v_head;
     for (int c = 0; c < p.D; c += 8) {
+        unsigned hidden = 0u, seen = 0u;               // a bit per value
+        for (int j = sees / TN * TN; j < end; ++j) {
+            float x[8];
+            unpack8<T>(v + j * p.v_token + c * 2, x);
+            unsigned bad = 0u;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) bad |= unsigned(!(fabsf(x[e]) < CUDART_INF_F)) << e;
+            if (j < sees) seen |= bad;
+            else hidden |= bad;
+        }
+        if (!(hidden & ~seen)) continue;
         float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         for (int j = 0; j < sees; ++j) {
             float s = 0.f, x[8], y[8];

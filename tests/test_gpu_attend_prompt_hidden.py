@@ -70,3 +70,26 @@ def test_a_sequence_of_nothing_but_nan_ends():
     disc.disc_attend_check()
     assert torch.isnan(out).all() and torch.isfinite(out2[0]).all() and not torch.isfinite(out2[1:]).any()
     assert torch.all((out3[:n // 2].float() - 1).abs() <= 2.0 ** -8) and torch.isnan(out3[n // 2:]).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_values_beside_infinite_ones_that_are_seen(dtype):
+    """Token 20 has an infinite value at place 5, token 40 at places 9 and 100, and token 41 a NaN at place 5: query 30 sees the first
+    only, and all its values but the one at place 5 are finite."""
+    n, hq, hkv, d = 200, 4, 2, 128
+    q, k, v = make(n, hq, d, dtype, 1), make(n, hkv, d, dtype, 2), make(n, hkv, d, dtype, 3)
+    bad = v.clone()
+    bad[20, :, 5] = math.inf
+    bad[40, :, 9] = -math.inf
+    bad[40, :, 100] = math.inf
+    bad[41, :, 5] = math.nan
+    out, lse = disc.disc_attend_prompt(q, k, bad, cu_of([n]), max_len=n)
+    rest = torch.ones(d, dtype=torch.bool, device=DEV)
+    rest[[5, 9, 100]] = False
+    o, l, to, tl = attend64(q, k, v, 1 / math.sqrt(d), list(range(1, n + 1)))
+    assert torch.all((lse.double() - l).abs() <= tl)
+    err = (out.double() - o).abs()
+    assert torch.all(err[:20] <= to[:20])
+    assert torch.all(err[:, :, rest] <= to[:, :, rest])
+    assert torch.all(err[:40, :, 9] <= to[:40, :, 9]) and torch.all(err[:40, :, 100] <= to[:40, :, 100])
+    assert not torch.isfinite(out[20:, :, 5]).any() and not torch.isfinite(out[40:, :, 9]).any() and not torch.isfinite(out[40:, :, 100]).any()
