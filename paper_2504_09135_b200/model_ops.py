@@ -340,9 +340,9 @@ class AttendPlan:
         if need < 0:
             raise DiscError(int(need), "disc_attend_plan_bytes")
         self.n_q_heads, self.group, self.nbytes, self.sizes = int(n_q_heads), int(group), int(need), cache._sizes
-        # zeros: no error yet, and no work in a plan that has not been made
-        self.buf = torch.zeros(self.nbytes, dtype=torch.uint8, device=cache.pool.device)
-        self.error = self.buf[:4].view(torch.int32)
+        self.buf = torch.empty(self.nbytes, dtype=torch.uint8, device=cache.pool.device)
+        self.error = self.buf[:4].view(torch.int32).zero_()
+        self.made = False
 
 
 def _of_cache(plan: AttendPlan, cache: DiscCache):
@@ -363,6 +363,7 @@ def disc_attend_plan(cache: DiscCache, n_q_heads: int, *, group: int = 1, plan: 
         _of_cache(plan, cache)
     _check(lib().disc_attend_plan(_books(cache), plan.n_q_heads, plan.group, plan.buf.data_ptr(), plan.nbytes, _stream_ptr(stream)),
            "disc_attend_plan")
+    plan.made = True
     return plan
 
 
@@ -378,6 +379,8 @@ def disc_attend_cached(cache: DiscCache, layer: int, q: torch.Tensor, plan: Atte
     if n != cache.n_rows or h != plan.n_q_heads or d != cache.head_dim:
         raise TypeError("q: expected [rows, Hq, head dim] of the cache and the plan")
     _of_cache(plan, cache)
+    if not plan.made:
+        raise TypeError("plan: not made yet (disc_attend_plan)")
     out, lse = _alloc(stream, _attend_outputs, q, out, lse)
     _check(lib().disc_attend_cached(_books(cache), int(layer), qp, qr, qh, plan.n_q_heads, plan.group,
                                     1.0 / math.sqrt(cache.head_dim) if scale is None else float(scale), plan.buf.data_ptr(),

@@ -33,11 +33,15 @@ def test_a_plan_of_another_cache_is_refused(group, other):
 
 
 @pytest.mark.parametrize("group", [1, 6])
-def test_a_plan_that_was_never_made_holds_no_work(group):
+def test_a_plan_that_was_never_made_is_refused(group):
     cache = filled()
     plan = disc.AttendPlan(cache, 24, group)
-    disc.disc_attend_cached(cache, 0, torch.randn((6, 24, 64), device=DEV).bfloat16(), plan)
+    q = torch.randn((6, 24, 64), device=DEV).bfloat16()
+    with pytest.raises(TypeError):
+        disc.disc_attend_cached(cache, 0, q, plan)
     disc.disc_attend_check(plan=plan)
+    assert disc.disc_attend_plan(cache, 24, group=group, plan=plan) is plan
+    disc.disc_attend_cached(cache, 0, q, plan)
 
 
 @pytest.mark.parametrize("group,hq", [(1, 4), (6, 4), (6, 24), (1, 64)])
