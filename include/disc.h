@@ -394,7 +394,8 @@ int disc_logprobs(const void* logits, disc_dtype_t dtype, int64_t ld, int64_t n,
  *   grad[i][v] = (d_logp [v = target] - p_v (d_logp + d_entropy (log p_v + entropy))) / T
  *   lse, entropy   device, float[n]: what disc_logprobs returned for these logits (entropy nullable
  *               without d_entropy)
- *               (rows with |lse| >= 128, which fp32 holds too coarsely, have their sum formed anew)
+ *               (rows with |lse| >= 128, which fp32 holds too coarsely, have their sum formed anew; an lse
+ *               that differs from it by more than 2^-21 of its size, a longer row's say, is taken as given)
  *   d_logp      device, float[n] (nullable; needs targets); rows without a target ignore it
  *   d_entropy   device, float[n] (nullable)
  *   grad_out    device, n rows of vocab_size values of type `dtype`, row i at element offset
@@ -473,8 +474,8 @@ int disc_cache_free(const disc_cache_t* c, const uint8_t* freed, void* stream);
 /* Room for add[r] more tokens in row r (add: device, int32[n_rows]; null = one each; <= 0 = none): len
  * grows, new pages are taken, and a row about to write into a partly filled page that other rows hold too
  * gets its own copy of the tokens in it, in all layers (when every holder of the page writes on, the longest of
- * them, of equally long ones the lowest row, keeps it).  Rows are served in ascending order: once the pages still needed by a row and those before
- * it exceed the free ones, that row and later ones that need a page get DISC_ROW_NOPAGE and stay as they
+ * them, of equally long ones the lowest row, keeps it).  Rows are served in ascending order: once the pages still
+ * needed by a row and those before it exceed the free ones, that row and later ones that need a page get DISC_ROW_NOPAGE and stay as they
  * are; so do rows that would outgrow the table.  status_out: device, uint8[n_rows]. */
 int disc_cache_extend(const disc_cache_t* c, const int32_t* add, uint8_t* status_out, void* stream);
 
