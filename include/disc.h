@@ -28,8 +28,10 @@
  * P = L(a, T) with a model of attention layers):
  *
  *   disc_attend_prompt   attention over whole prompts, packed
+ *   disc_norm_rope, disc_norm_rope_grad   head norms and rotation of queries and keys, and their gradient
  *   disc_cache_*         a key-value cache in pages that the candidates of a query share: fork,
- *                    extend, write, free, compact
+ *                    extend, write, read, free, compact; its vectors as they are or held in 8 bits
+ *   disc_norm_rope_write  norm, rotation and the way into the cache in one launch
  *   disc_attend_plan, disc_attend_cached   attention of one new token per candidate over that cache
  *   disc_logprobs, disc_logprobs_grad   log-probabilities of given tokens, entropy, the most probable
  *                    alternatives, and the gradient for training on them
@@ -438,6 +440,46 @@ int disc_attend_prompt(const void* q, int64_t q_token_stride, int64_t q_head_str
 /* Synchronises `stream`; DISC_ERR_CUDA when an attention kernel has set this error word. */
 int disc_attend_error(const uint32_t* error, void* stream);
 
+/* ---- head norms and rotation of queries and keys ---------------------------------------------------
+ * For every vector x of D = head_dim values, w = q_weight or k_weight:
+ *   u = w x / sqrt(mean(x^2) + eps) with `norm` (a null weight counts as 1), u = x without
+ *   y_a = u_a cos t_i - u_b sin t_i,  y_b = u_b cos t_i + u_a sin t_i,   t_i = position * inv_freq[i],  i < rot / 2
+ * with (a, b) = (i, i + rot/2), or (2i, 2i + 1) with `interleaved`; values from rot on are not rotated.  Rounded once, at the end.
+ * Angles are formed in 64 bits less their whole turns: as exact at position 10^6 as at 10. */
+typedef struct {
+    const float* inv_freq;     /* device, float[rot / 2] (nullable with rot = 0)                        */
+    const void* q_weight;      /* device, head_dim values (nullable), 16-byte aligned                    */
+    const void* k_weight;
+    float eps;                 /* >= 0                                                                   */
+    int32_t rot;               /* a multiple of 8, at most head_dim; 0: no rotation                      */
+    int32_t interleaved, norm; /* 0 or 1                                                                 */
+    int32_t weight_dtype;      /* DISC_F32 or the vectors' type                                          */
+} disc_rope_t;
+
+/* q [n_tokens][n_q_heads][head_dim] -> q_out, k [n_tokens][n_kv_heads][head_dim] -> k_out, by the tokens' positions.
+ *   q, k, q_out, k_out   device, bf16 or f16; token t, head h at element offset t*token_stride + h*head_stride; bases on
+ *               16-byte boundaries, strides multiples of 8.  An output may be its input (same strides), otherwise must
+ *               not overlap it.  Either of q and k may be left out with 0 heads
+ *   head_dim    a multiple of 8, at most DISC_MAX_HEAD_DIM
+ *   positions   device, int32[n_tokens] (nullable with rot = 0)
+ * Sums of squares are held in fp32: |x| up to about 10^18.
+ * Errors: DISC_ERR_ARG, DISC_ERR_UNSUPPORTED (dtype, head_dim, rot, strides, weight_dtype). */
+int disc_norm_rope(const disc_rope_t* how, const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride,
+                   int64_t k_head_stride, disc_dtype_t dtype, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t n_tokens,
+                   const int32_t* positions, void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride, void* k_out,
+                   int64_t k_out_token_stride, int64_t k_out_head_stride, void* stream);
+
+/* Its gradient: from d_q_out, d_k_out (strides as above, 0 allowed) those of q and k and, where not null, of the weights.
+ *   d_q, d_k    device, [n_tokens][heads][head_dim] contiguous, 16-byte aligned, of the vectors' type; must not overlap any input
+ *   d_q_weight, d_k_weight   device, float[head_dim] (nullable; need `norm`): sums in fp32, the same every time
+ *   scratch     device, disc_norm_rope_scratch_bytes() bytes, 4-byte aligned (nullable without weight gradients) */
+int64_t disc_norm_rope_scratch_bytes(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t n_tokens);
+int disc_norm_rope_grad(const disc_rope_t* how, const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride,
+                        int64_t k_head_stride, disc_dtype_t dtype, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t n_tokens,
+                        const int32_t* positions, const void* d_q_out, int64_t dq_token_stride, int64_t dq_head_stride, const void* d_k_out,
+                        int64_t dk_token_stride, int64_t dk_head_stride, void* d_q, void* d_k, float* d_q_weight, float* d_k_weight, void* scratch,
+                        int64_t scratch_bytes, void* stream);
+
 /* ---- the key-value cache ---------------------------------------------------------------------------
  * Rows (sequences) hold their keys and values in pages of page_size tokens; a page may belong to several
  * rows, which is how the K candidates of a query share its prompt.  All memory is the caller's, on
@@ -449,7 +491,20 @@ int disc_attend_error(const uint32_t* error, void* stream);
  *   scratch disc_cache_scratch_bytes() bytes, 16-byte aligned, contents irrelevant between calls
  * An empty cache has table = -1, len = 0, ref = 0.  The calls below keep the three consistent; new
  * pages are always the free ones of lowest id.  The calls on one cache must not overlap on the device.
- * Page sizes: 16, 32, 64, 128.  dtype bf16 or f16, head_dim a multiple of 8 up to 128. */
+ * Page sizes: 16, 32, 64, 128.  dtype bf16 or f16, head_dim a multiple of 8 up to 128.
+ *
+ * With dtype | DISC_HELD_E4M3 or | DISC_HELD_I8 the vectors, of type bf16 or f16 where they are given and returned, are held in 8
+ * bits: one code per value and a power of two, 2^e, per vector.  head_dim is then a multiple of 16 and
+ *   pool    [n_layers][2][n_pages][n_kv_heads] parts of page_size * (head_dim + 1) bytes: the codes [page_size][head_dim], then
+ *           the exponents, one signed byte per token
+ *   e4m3    e = floor(log2 amax) - 8, one more where amax 2^-e > 448;  amax: the vector's largest |value|
+ *   i8      e = floor(log2 amax) - 6, one more where amax 2^-e rounds to more than 127;  two's complement
+ *   code    value * 2^-e rounded to the nearest, ties to even;  e is at least -126
+ * so that an e4m3 code is off by at most 2^-4 of its value (or 2^-10 2^e), an i8 code by half of 2^e.  A held value, code * 2^e, is exact in the
+ * vectors' type; one that exceeds the type's largest finite value (an e4m3 code rounded up) is given back as that.  A vector
+ * with an infinite value or a NaN is held as e = -128 and reads as NaN throughout. */
+#define DISC_HELD_E4M3 0x10
+#define DISC_HELD_I8 0x20
 typedef struct {
     void* pool;
     int32_t* table;
@@ -488,6 +543,23 @@ int disc_cache_extend(const disc_cache_t* c, const int32_t* add, uint8_t* status
 int disc_cache_write(const disc_cache_t* c, int32_t layer, const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v,
                      int64_t v_token_stride, int64_t v_head_stride, int64_t n_tokens, const int32_t* cu, int32_t n_seqs,
                      const int32_t* rows, const uint8_t* status, void* stream);
+
+/* Tokens of some rows out of layer `layer`, packed: token t = cu[i] + j of sequence i (row rows[i]; null: row i) is token
+ * start[i] + j (null start: j) of its row; places before cu[0] and from cu[n_seqs] on are left as they are.
+ *   cu       device, int32[n_seqs+1], ascending, cu[n_seqs] <= n_tokens
+ *   k_out, v_out   device, [n_tokens][n_kv_heads][head_dim] contiguous, 32-byte aligned; zeros for tokens the row does not have */
+int disc_cache_read(const disc_cache_t* c, int32_t layer, const int32_t* cu, int32_t n_seqs, const int32_t* rows, const int32_t* start, int64_t n_tokens,
+                    void* k_out, void* v_out, void* stream);
+
+/* disc_norm_rope on the newest tokens' queries and keys with the cache's head_dim and type, and disc_cache_write of the resulting
+ * keys and of v as they are, in one launch and bit for bit what the two give.
+ *   positions   device, int32[n_tokens] (nullable: each token's place in its row, 0 for one that has none)
+ *   n_q_heads   may be 0 (no queries)
+ * cu, n_seqs, rows, status as for disc_cache_write; the queries of tokens that are not written are formed all the same. */
+int disc_norm_rope_write(const disc_cache_t* c, int32_t layer, const disc_rope_t* how, const void* q, int64_t q_token_stride, int64_t q_head_stride,
+                         int32_t n_q_heads, const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,
+                         int64_t v_head_stride, int64_t n_tokens, const int32_t* positions, const int32_t* cu, int32_t n_seqs, const int32_t* rows,
+                         const uint8_t* status, void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride, void* stream);
 
 /* The n pages in use move to the ids 0 .. n-1 (those that are there already stay, the others go to
  * the free ids below n in order), contents of all layers with them.  live_out: device, int32: n. */

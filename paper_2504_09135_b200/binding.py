@@ -17,6 +17,7 @@ import torch
 from . import build as _build
 
 DISC_F32, DISC_BF16, DISC_F16 = 0, 1, 2
+DISC_HELD_E4M3, DISC_HELD_I8 = 0x10, 0x20
 ROW_DEAD, ROW_NOMASS, ROW_NONFINITE, ROW_DONE, ROW_FAULT, ROW_NOPAGE = 1, 2, 4, 8, 16, 32
 MAX_DEPTH = 64
 
@@ -29,7 +30,8 @@ EXPORTS = ["disc_build_set", "disc_build_set_eok", "disc_free_set", "disc_set_in
            "disc_sampling_uniforms",
            "disc_logprobs", "disc_logprobs_grad", "disc_attend_prompt", "disc_attend_error",
            "disc_cache_scratch_bytes", "disc_cache_fork", "disc_cache_free", "disc_cache_extend", "disc_cache_write",
-           "disc_cache_compact", "disc_attend_plan_bytes", "disc_attend_plan", "disc_attend_cached",
+           "disc_cache_compact", "disc_cache_read", "disc_norm_rope", "disc_norm_rope_grad", "disc_norm_rope_scratch_bytes", "disc_norm_rope_write",
+           "disc_attend_plan_bytes", "disc_attend_plan", "disc_attend_cached",
            "disc_error_string", "disc_last_cuda_error"]
 
 
@@ -48,6 +50,11 @@ class _Cache(C.Structure):
                 ("scratch", C.c_void_p), ("scratch_bytes", C.c_int64), ("n_layers", C.c_int32), ("n_pages", C.c_int32),
                 ("n_kv_heads", C.c_int32), ("page_size", C.c_int32), ("head_dim", C.c_int32), ("n_rows", C.c_int32),
                 ("table_width", C.c_int32), ("dtype", C.c_int32)]
+
+
+class _Rope(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("eps", C.c_float), ("rot", C.c_int32),
+                ("interleaved", C.c_int32), ("norm", C.c_int32), ("weight_dtype", C.c_int32)]
 
 
 class _SetInfo(C.Structure):
@@ -103,6 +110,12 @@ def lib():
     L.disc_cache_extend.argtypes = [vp, vp, vp, vp]
     L.disc_cache_write.argtypes = [vp, i32, vp, i64, i64, vp, i64, i64, i64, vp, i32, vp, vp, vp]
     L.disc_cache_compact.argtypes = [vp, vp, vp]
+    L.disc_cache_read.argtypes = [vp, i32, vp, i32, vp, vp, i64, vp, vp, vp]
+    L.disc_norm_rope.argtypes = [vp, vp, i64, i64, vp, i64, i64, C.c_int, i32, i32, i32, i64, vp, vp, i64, i64, vp, i64, i64, vp]
+    L.disc_norm_rope_scratch_bytes.argtypes = [i32, i32, i32, i64]
+    L.disc_norm_rope_grad.argtypes = [vp, vp, i64, i64, vp, i64, i64, C.c_int, i32, i32, i32, i64, vp, vp, i64, i64, vp, i64, i64, vp, vp, vp, vp,
+                                      vp, i64, vp]
+    L.disc_norm_rope_write.argtypes = [vp, i32, vp, vp, i64, i64, i32, vp, i64, i64, vp, i64, i64, i64, vp, vp, i32, vp, vp, vp, i64, i64, vp]
     L.disc_attend_plan_bytes.argtypes = [vp, i32, i32]
     L.disc_attend_plan.argtypes = [vp, i32, i32, vp, i64, vp]
     L.disc_attend_cached.argtypes = [vp, i32, vp, i64, i64, i32, i32, f32, vp, i64, vp, vp, vp]
@@ -111,7 +124,7 @@ def lib():
     L.disc_last_cuda_error.argtypes = []
     for name in EXPORTS:
         if name in ("disc_project_scratch_bytes", "disc_step_topm_scratch_bytes", "disc_cache_scratch_bytes",
-                    "disc_attend_plan_bytes"):
+                    "disc_norm_rope_scratch_bytes", "disc_attend_plan_bytes"):
             getattr(L, name).restype = C.c_int64
         elif name not in ("disc_free_set", "disc_error_string"):
             getattr(L, name).restype = C.c_int

@@ -21,7 +21,7 @@ LIB = os.path.join(PKG, "libdisc_b200.so")
 STAMP = LIB + ".sha256"
 
 SOURCES = ["disc_build.cu", "disc_mask.cu", "disc_step.cu", "disc_resample.cu", "disc_verify.cu", "disc_project.cu", "disc_topm.cu",
-           "disc_logprobs.cu", "disc_cache.cu", "disc_attend.cu", "disc_attend_group.cu", "disc_prompt.cu"]
+           "disc_logprobs.cu", "disc_cache.cu", "disc_attend.cu", "disc_attend_group.cu", "disc_attend_held.cu", "disc_prompt.cu", "disc_rope.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
 

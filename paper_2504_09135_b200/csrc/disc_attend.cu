@@ -11,7 +11,7 @@
 //
 // Two forms, by the number M of query vectors that read the same pages (rows of the group x query heads per
 // key head).  M <= 16, this file: mma.sync m16n8k16 on one tile of 16 rows, far from being the bound.  M > 16,
-// disc_attend_group.cu: tcgen05 on tiles of 128 rows.
+// disc_attend_group.cu: tcgen05 on tiles of 128 rows.  M <= 16 over a cache held in 8 bits: disc_attend_held.cu, by the plan made here.
 //
 // Plan (one cluster of 8 blocks): per group the number of leading pages its rows share, and the stream as a
 // list of blocks of 16 tokens (page, block in the page, tokens in it, owner); from the lengths of
@@ -33,7 +33,6 @@ using namespace disc;
 
 constexpr unsigned FULL = 0xffffffffu;
 constexpr float LOG2E_F = 1.4426950408889634f;
-constexpr float LN2_F = 0.6931471805599453f;
 constexpr int TILE_BLKS = 4;           // blocks of a tile
 constexpr int TILE = BLK * TILE_BLKS;
 constexpr int STAGES = 3;
@@ -163,9 +162,6 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(PT) attend_plan_ker
 }
 
 // ---- attention --------------------------------------------------------------------------------------
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 constexpr int AT = 128;                // threads of an attention block
 
 template <int DP>
@@ -422,39 +418,7 @@ __global__ void __launch_bounds__(AT, 2) attend_cached_kernel(const AttendParams
             __syncthreads();
             if (s_last) {
                 __threadfence();
-                const int64_t slot0 = (int64_t(more.w) * p.kv_heads + head) * sh.M, step = int64_t(p.kv_heads) * sh.M;
-                for (int i = tid; i < M * DV; i += AT) {
-                    const int m = i / DV, d = (i % DV) * 4;
-                    if (d >= p.D) continue;
-                    // one pass in the order of the parts, eight of them on their way at a time
-                    float top = -CUDART_INF_F, total = 0.f;
-                    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-                    for (int j0 = 0; j0 < splits; j0 += 8) {
-                        float lse[8];
-                        float4 y[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            if (j0 + j < splits) {
-                                const int64_t part = slot0 + (j0 + j) * step + m;
-                                lse[j] = __ldcg(p.plan.part_lse + part);
-                                y[j] = __ldcg(reinterpret_cast<const float4*>(p.plan.part + part * p.D + d));
-                            }
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            if (j0 + j < splits) {
-                                const float n = fmaxf(top, lse[j]);
-                                const float f = top > -CUDART_INF_F ? ex2_approx(top - n) : 0.f, w = lse[j] == -CUDART_INF_F ? 0.f : ex2_approx(lse[j] - n);
-                                top = n;
-                                total = fmaf(total, f, w);
-                                x = make_float4(fmaf(w, y[j].x, x.x * f), fmaf(w, y[j].y, x.y * f), fmaf(w, y[j].z, x.z * f), fmaf(w, y[j].w, x.w * f));
-                            }
-                    }
-                    const float inv = total > 0.f ? 1.f / total : (total == 0.f ? 0.f : total);
-                    const int64_t at = int64_t(r0 + m / G) * p.kv_heads * G + head * G + m % G;
-                    *reinterpret_cast<uint2*>(p.out + (at * p.D + d) * 2) =
-                        make_uint2(pack2<T>(x.x * inv, x.y * inv), pack2<T>(x.z * inv, x.w * inv));
-                    if (d == 0 && p.lse) p.lse[at] = total > 0.f ? (top + log2f(total)) * LN2_F : (total == 0.f ? -CUDART_INF_F : total);
-                }
+                join_items<T, DP, AT>(p, more.w, splits, head, M, r0);
             }
         }
     }
@@ -520,17 +484,19 @@ int disc_attend_cached(const disc_cache_t* c, int32_t layer, const void* q, int6
     if (n_q_heads == 1) q_head_stride = (int64_t(c->head_dim) + 7) / 8 * 8;
     if (c->n_rows == 1) q_row_stride = (int64_t(c->head_dim) + 7) / 8 * 8 * n_q_heads;
     if ((q_row_stride | q_head_stride) & 7) return DISC_ERR_UNSUPPORTED;
-    const int64_t plane = int64_t(c->n_pages) * c->n_kv_heads * c->page_size * c->head_dim * 2;
+    const int64_t plane = disc::cache_plane_bytes(c);
     p.k = static_cast<const unsigned char*>(c->pool) + 2 * layer * plane;
     p.v = p.k + plane;
     p.q = static_cast<const unsigned char*>(q); p.q_row = q_row_stride * 2; p.q_head = q_head_stride * 2;
     p.table = c->table; p.len = c->len; p.width = c->table_width; p.pages = c->n_pages;
     p.out = static_cast<unsigned char*>(out); p.lse = lse_out;
     p.rows = c->n_rows; p.kv_heads = c->n_kv_heads; p.D = c->head_dim; p.page_size = c->page_size;
+    p.head_bytes = disc::cache_head_bytes(c);
     p.c2 = scale * LOG2E_F;
     p.error = reinterpret_cast<uint32_t*>(p.plan.head);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (p.shape.M > ROWS_M) return disc::attend_groups(p, c->dtype, n_q_heads, st);
+    if (disc::cache_held(c)) return disc::attend_held(p, c->dtype, st);
     const unsigned grid = unsigned(p.shape.lanes * c->n_kv_heads);
     return c->dtype == DISC_BF16 ? launch_attend<__nv_bfloat16>(p, grid, st) : launch_attend<__half>(p, grid, st);
 }

@@ -143,6 +143,15 @@ __device__ __forceinline__ void ldsm4(uint32_t a, uint32_t* r) {
 __device__ __forceinline__ void ldsm4t(uint32_t a, uint32_t* r) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
 }
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// an 8 x 8 matrix of 16-bit values across the warp, transposed
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
 // d += a b, 16 x 16 by 16 x 8
 template <typename T>
 __device__ __forceinline__ void mma16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1);
@@ -186,12 +195,57 @@ struct AttendParams {
     unsigned char* out;
     float* lse;
     int32_t rows, width, pages, kv_heads, D, page_size;
+    int32_t head_bytes;                // of a page and key head
     float c2;                          // scale log2(e)
     uint32_t* error;
 };
 
-// disc_attend_group.cu: more than ROWS_M query vectors read the same pages
+constexpr float LN2_F = 0.6931471805599453f;
+
+// The items of a group, joined in their order by the block of threads that finished last: one pass, eight parts on their way at
+// a time.  slot: the group's first part; M query vectors of the rows from r0 on, DP >= D values.
+template <typename T, int DP, int THREADS>
+__device__ __forceinline__ void join_items(const AttendParams& p, int32_t slot, int splits, int head, int M, int r0) {
+    const PlanShape& sh = p.shape;
+    const int G = sh.G;
+    constexpr int DV = DP / 4;
+    const int64_t slot0 = (int64_t(slot) * p.kv_heads + head) * sh.M, step = int64_t(p.kv_heads) * sh.M;
+    for (int i = threadIdx.x; i < M * DV; i += THREADS) {
+        const int m = i / DV, d = (i % DV) * 4;
+        if (d >= p.D) continue;
+        float top = -CUDART_INF_F, total = 0.f;
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int j0 = 0; j0 < splits; j0 += 8) {
+            float lse[8];
+            float4 y[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j0 + j < splits) {
+                    const int64_t part = slot0 + (j0 + j) * step + m;
+                    lse[j] = __ldcg(p.plan.part_lse + part);
+                    y[j] = __ldcg(reinterpret_cast<const float4*>(p.plan.part + part * p.D + d));
+                }
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j0 + j < splits) {
+                    const float n = fmaxf(top, lse[j]);
+                    const float f = top > -CUDART_INF_F ? ex2_approx(top - n) : 0.f, w = lse[j] == -CUDART_INF_F ? 0.f : ex2_approx(lse[j] - n);
+                    top = n;
+                    total = fmaf(total, f, w);
+                    x = make_float4(fmaf(w, y[j].x, x.x * f), fmaf(w, y[j].y, x.y * f), fmaf(w, y[j].z, x.z * f), fmaf(w, y[j].w, x.w * f));
+                }
+        }
+        const float inv = total > 0.f ? 1.f / total : (total == 0.f ? 0.f : total);
+        const int64_t at = int64_t(r0 + m / G) * p.kv_heads * G + head * G + m % G;
+        *reinterpret_cast<uint2*>(p.out + (at * p.D + d) * 2) = make_uint2(pack2<T>(x.x * inv, x.y * inv), pack2<T>(x.z * inv, x.w * inv));
+        if (d == 0 && p.lse) p.lse[at] = total > 0.f ? (top + log2f(total)) * LN2_F : (total == 0.f ? -CUDART_INF_F : total);
+    }
+}
+
+// disc_attend_group.cu: more than ROWS_M query vectors read the same pages; dtype as in disc_cache_t
 int plan_groups(const PlanParams& p, cudaStream_t st);
 int attend_groups(const AttendParams& p, int32_t dtype, int32_t n_q_heads, cudaStream_t st);
+// disc_attend_held.cu: up to ROWS_M, over a cache held in 8 bits
+int attend_held(const AttendParams& p, int32_t dtype, cudaStream_t st);
 
 }  // namespace disc

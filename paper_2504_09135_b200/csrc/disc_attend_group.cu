@@ -28,7 +28,6 @@ namespace {
 using namespace disc;
 
 constexpr unsigned FULL = 0xffffffffu;
-constexpr float LN2_F = 0.6931471805599453f;
 constexpr int TN = 64;                 // tokens of a tile
 constexpr int TILE_BLKS = TN / BLK;
 constexpr int BOX = 64;
@@ -415,13 +414,6 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
 // ---- kernel 2 -----------------------------------------------------------------------------------------
 constexpr int JT = 128;                // threads of a block: 4 warps, each with a row and key head of its own
 
-// an 8 x 8 matrix of 16-bit values across the warp, transposed
-__device__ __forceinline__ uint32_t transposed(uint32_t x) {
-    uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-    return y;
-}
-
 template <int DP>
 struct JoinSmem {
     static constexpr int O_LD = DP + 4;                            // fp32 sums [8 heads][DP], over keys and values no longer needed
@@ -678,6 +670,7 @@ int disc::plan_groups(const PlanParams& p, cudaStream_t st) {
 }
 
 int disc::attend_groups(const AttendParams& a, int32_t dtype, int32_t n_q_heads, cudaStream_t st) {
+    if (dtype >> 4) return DISC_ERR_UNSUPPORTED;
     GroupParams p;
     p.plan = a.plan; p.table = a.table; p.width = a.width; p.kv_heads = a.kv_heads; p.G = a.shape.G; p.per_group = a.shape.per_group;
     p.D = a.D; p.page_size = a.page_size; p.blks_per_page = a.shape.blks_per_page; p.c2 = a.c2; p.error = a.error;

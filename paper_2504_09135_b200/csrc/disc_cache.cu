@@ -3,7 +3,8 @@
 //   disc_cache_fork     row r becomes what row parent[r] was, sharing its pages
 //   disc_cache_free     rows let go of their pages
 //   disc_cache_extend   room for new tokens: free pages, and private copies of shared last pages
-//   disc_cache_write    keys and values of new tokens into the pages
+//   disc_cache_write    keys and values of new tokens into the pages (in 8 bits: disc_rope.cu)
+//   disc_cache_read     tokens of a row back as packed keys and values
 //   disc_cache_compact  the live pages move to the front of the pool
 //
 // The books are whole numbers on the device (page table, lengths, reference counts) and nothing is
@@ -16,7 +17,7 @@
 // the copies of page contents, which are bound by the bytes: 48 us for the 0.26 GB of 4096 candidates' last pages
 // (5.3 TB/s), 102 us for a compaction's 0.58 GB (5.7 TB/s; the measured copy rate is 6.5).
 
-#include "disc_internal.cuh"
+#include "disc_held.cuh"
 
 namespace {
 
@@ -191,6 +192,7 @@ struct Pool {
     int32_t planes, heads;
     int64_t plane_bytes;
     int32_t head_bytes, token_bytes;
+    int32_t exps;                      // 16-byte vectors at the end of a head's page that go along with every copy: its exponents
 };
 // Copies of the tokens in partly filled pages: a warp per copy, plane and head, which is one run of tokens x head dim.
 // This warp's units: first, first + step, ... below n.
@@ -203,15 +205,19 @@ __device__ __forceinline__ void copy_units(const Pool& o, const Scratch& s, int6
         const int4 c = s.copy[j / o.planes];
         const uint4* from = reinterpret_cast<const uint4*>(o.base + pl * o.plane_bytes + (int64_t(c.x) * o.heads + h) * o.head_bytes);
         uint4* to = reinterpret_cast<uint4*>(o.base + pl * o.plane_bytes + (int64_t(c.y) * o.heads + h) * o.head_bytes);
-        const int32_t vecs = c.z * o.token_bytes / 16;
+        const int32_t codes = c.z * o.token_bytes / 16, vecs = codes + o.exps, gap = o.head_bytes / 16 - vecs;
         for (int32_t v0 = lane; v0 < vecs; v0 += 32 * 4) {         // four loads in flight
             uint4 x[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (v0 + u * 32 < vecs) x[u] = from[v0 + u * 32];
+            for (int u = 0; u < 4; ++u) {
+                const int32_t v = v0 + u * 32;
+                if (v < vecs) x[u] = from[v < codes ? v : v + gap];
+            }
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (v0 + u * 32 < vecs) __stcs(to + v0 + u * 32, x[u]);
+            for (int u = 0; u < 4; ++u) {
+                const int32_t v = v0 + u * 32;
+                if (v < vecs) __stcs(to + (v < codes ? v : v + gap), x[u]);
+            }
         }
     }
 }
@@ -455,6 +461,75 @@ __global__ void __launch_bounds__(256) cache_write_kernel(Books b, WriteParams w
     }
 }
 
+// ---- read --------------------------------------------------------------------------------------------
+struct ReadParams {
+    const unsigned char* k_plane;
+    const unsigned char* v_plane;
+    unsigned char* k;
+    unsigned char* v;
+    const int32_t* cu;                          // [n+1]
+    const int32_t* rows;                        // [n] nullable: sequence i is row i
+    const int32_t* start;                       // [n] nullable: from the row's first token
+    int32_t n, tokens, heads, D, head_bytes;
+};
+// One warp per token: 16 values of a lane at a time, out of 16 codes, or 8 as they are.  Bound by the bytes.
+template <typename T, int HELD>
+__global__ void __launch_bounds__(256) cache_read_kernel(Books b, ReadParams r) {
+    let_later_in();
+    wait_for_earlier();
+    const int32_t t = int32_t((int64_t(blockIdx.x) * blockDim.x + threadIdx.x) >> 5);
+    const int lane = threadIdx.x & 31;
+    if (t >= r.tokens) return;
+    int32_t page = -1, off = 0;
+    bool asked = false;
+    if (t >= r.cu[0] && t < r.cu[r.n]) {
+        asked = true;
+        int32_t lo = 0, hi = r.n;               // cu[lo] <= t < cu[hi]
+        while (hi - lo > 1) {
+            const int32_t m = lo + (hi - lo) / 2;
+            if (r.cu[m] <= t) lo = m; else hi = m;
+        }
+        const int32_t row = r.rows ? r.rows[lo] : lo;
+        const int64_t pos = int64_t(r.start ? r.start[lo] : 0) + (t - r.cu[lo]);
+        if (row >= 0 && row < b.rows && pos >= 0 && pos < b.len[row] && (pos >> b.shift) < b.width) {
+            page = b.table[size_t(row) * b.width + (pos >> b.shift)];
+            off = int32_t(pos) & (b.page_size - 1);
+            if (page >= b.pages) page = -1;
+        }
+    }
+    if (!asked) return;
+    constexpr int RUN = HELD ? 16 : 8;          // values of a lane
+    const int runs = r.D / RUN, all = runs * r.heads;
+    const int64_t out0 = int64_t(t) * r.heads * r.D * 2, in0 = int64_t(max(page, 0)) * r.heads * r.head_bytes;
+    for (int i0 = lane; i0 < 2 * all; i0 += 32 * 4) {          // four loads in flight
+        uint4 c[4];
+        int e[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int i = i0 + u * 32, j = i >= all ? i - all : i, h = j / runs, x = j - h * runs;
+            c[u] = make_uint4(0, 0, 0, 0);
+            e[u] = 0;
+            if (i >= 2 * all || page < 0) continue;
+            const unsigned char* from = (i >= all ? r.v_plane : r.k_plane) + in0 + int64_t(h) * r.head_bytes;
+            c[u] = *reinterpret_cast<const uint4*>(from + (off * r.D * (HELD ? 1 : 2)) + x * 16);
+            if (HELD) e[u] = reinterpret_cast<const signed char*>(from)[b.page_size * r.D + off];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int i = i0 + u * 32, j = i >= all ? i - all : i;
+            if (i >= 2 * all) continue;
+            unsigned char* to = (i >= all ? r.v : r.k) + out0 + int64_t(j) * RUN * 2;
+            if (HELD) {
+                uint32_t x[8];
+                values16<T, HELD>(c[u], page < 0 ? 0.f : exponent_scale(e[u]), x);
+                st_global32(to, x);
+            } else {
+                *reinterpret_cast<uint4*>(to) = c[u];
+            }
+        }
+    }
+}
+
 // ---- compact -----------------------------------------------------------------------------------------
 // One cluster: the number n of live pages; the live pages at n and above, in order, are to go to the free pages below
 // n, in order; their reference counts go along.
@@ -590,8 +665,9 @@ int take(const disc_cache_t* c, const int32_t* parent, const uint8_t* freed, cud
 // the sizes of a cache alone
 int disc::cache_sizes(const disc_cache_t* c) {
     if (c->n_layers <= 0 || c->n_pages <= 0 || c->n_kv_heads <= 0 || c->head_dim <= 0 || c->n_rows <= 0 || c->table_width <= 0) return DISC_ERR_ARG;
-    if (c->dtype != DISC_BF16 && c->dtype != DISC_F16) return DISC_ERR_UNSUPPORTED;
-    if (c->head_dim % 8 || c->head_dim > DISC_MAX_HEAD_DIM) return DISC_ERR_UNSUPPORTED;
+    if ((disc::cache_type(c) != DISC_BF16 && disc::cache_type(c) != DISC_F16) || disc::cache_held(c) < 0 || disc::cache_held(c) > HELD_I8) return DISC_ERR_UNSUPPORTED;
+    // vectors lie on 16-byte boundaries
+    if (c->head_dim % (disc::cache_held(c) ? 16 : 8) || c->head_dim > DISC_MAX_HEAD_DIM) return DISC_ERR_UNSUPPORTED;
     if (c->page_size < 16 || c->page_size > 128 || (c->page_size & (c->page_size - 1))) return DISC_ERR_UNSUPPORTED;
     // a row's tokens are counted in 32 bits, pages and rows in 2^26 at most
     if (c->n_pages > (1 << 26) || c->n_rows > (1 << 26) || int64_t(c->table_width) * c->page_size >= (int64_t(1) << 31) ||
@@ -632,8 +708,9 @@ int disc_cache_extend(const disc_cache_t* c, const int32_t* add, uint8_t* status
     const bool one = c->n_rows <= XT && c->n_pages <= ONE_BLOCK;
     Pool o;
     o.base = static_cast<unsigned char*>(c->pool); o.planes = c->n_layers * 2; o.heads = c->n_kv_heads;
-    o.token_bytes = c->head_dim * 2; o.head_bytes = c->page_size * o.token_bytes;
-    o.plane_bytes = int64_t(c->n_pages) * c->n_kv_heads * o.head_bytes;
+    o.token_bytes = cache_token_bytes(c); o.head_bytes = cache_head_bytes(c);
+    o.plane_bytes = cache_plane_bytes(c);
+    o.exps = cache_held(c) ? c->page_size / 16 : 0;
     // copies that the one block can make itself, up to 8 a warp, are not worth a launch
     const int64_t units = int64_t(c->n_rows) * o.planes * o.heads;
     const bool copy_here = one && units <= XT / 32 * 8;
@@ -659,6 +736,9 @@ int disc_cache_write(const disc_cache_t* c, int32_t layer, const void* k, int64_
     // 16-byte reads: the bases on 16-byte boundaries, the strides multiples of 8 values
     if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15u) return DISC_ERR_ARG;
     if ((k_token_stride | k_head_stride | v_token_stride | v_head_stride) & 7) return DISC_ERR_UNSUPPORTED;
+    if (cache_held(c))
+        return disc::write_held(c, layer, k, k_token_stride, k_head_stride, v, v_token_stride, v_head_stride, int32_t(n_tokens), cu, n_seqs, rows, status,
+                                static_cast<cudaStream_t>(stream));
     WriteParams w;
     w.k = static_cast<const unsigned char*>(k); w.v = static_cast<const unsigned char*>(v);
     w.k_token = k_token_stride * 2; w.k_head = k_head_stride * 2; w.v_token = v_token_stride * 2; w.v_head = v_head_stride * 2;
@@ -668,6 +748,27 @@ int disc_cache_write(const disc_cache_t* c, int32_t layer, const void* k, int64_
     w.k_plane = static_cast<unsigned char*>(c->pool) + 2 * int64_t(layer) * plane;
     w.v_plane = w.k_plane + plane;
     return launch_after(cache_write_kernel, unsigned((n_tokens * 32 + 255) / 256), 256, 0, static_cast<cudaStream_t>(stream), books(c), w);
+}
+
+int disc_cache_read(const disc_cache_t* c, int32_t layer, const int32_t* cu, int32_t n_seqs, const int32_t* rows, const int32_t* start, int64_t n_tokens,
+                    void* k_out, void* v_out, void* stream) {
+    if (!c || !c->pool || !c->table || !c->len) return DISC_ERR_ARG;
+    if (const int rc = disc::cache_sizes(c)) return rc;
+    if (layer < 0 || layer >= c->n_layers || n_tokens < 0 || n_seqs < 0 || n_tokens > (int64_t(1) << 30)) return DISC_ERR_ARG;
+    if (!rows && n_seqs > c->n_rows) return DISC_ERR_ARG;
+    if (n_tokens == 0 || n_seqs == 0) return DISC_OK;
+    if (!cu || !k_out || !v_out || ((reinterpret_cast<uintptr_t>(k_out) | reinterpret_cast<uintptr_t>(v_out)) & 31u)) return DISC_ERR_ARG;
+    ReadParams r;
+    r.k_plane = static_cast<const unsigned char*>(c->pool) + 2 * int64_t(layer) * cache_plane_bytes(c);
+    r.v_plane = r.k_plane + cache_plane_bytes(c);
+    r.k = static_cast<unsigned char*>(k_out); r.v = static_cast<unsigned char*>(v_out);
+    r.cu = cu; r.rows = rows; r.start = start; r.n = n_seqs; r.tokens = int32_t(n_tokens);
+    r.heads = c->n_kv_heads; r.D = c->head_dim; r.head_bytes = cache_head_bytes(c);
+    const bool bf = cache_type(c) == DISC_BF16;
+    auto kernel = cache_held(c) == HELD_PLAIN ? cache_read_kernel<__nv_bfloat16, HELD_PLAIN>
+                  : cache_held(c) == HELD_E4M3 ? (bf ? cache_read_kernel<__nv_bfloat16, HELD_E4M3> : cache_read_kernel<__half, HELD_E4M3>)
+                                               : (bf ? cache_read_kernel<__nv_bfloat16, HELD_I8> : cache_read_kernel<__half, HELD_I8>);
+    return launch_after(kernel, unsigned((n_tokens * 32 + 255) / 256), 256, 0, static_cast<cudaStream_t>(stream), books(c), r);
 }
 
 int disc_cache_compact(const disc_cache_t* c, int32_t* live_out, void* stream) {
@@ -681,7 +782,7 @@ int disc_cache_compact(const disc_cache_t* c, int32_t* live_out, void* stream) {
     const bool one = c->n_pages <= ONE_BLOCK;
     auto plan = one ? cache_plan_compact_kernel<1> : cache_plan_compact_kernel<CLUSTER>;
     if (const int rc = launch_after(plan, one ? 1 : CLUSTER, XT, 0, st, books(c), s, live_out)) return rc;
-    const int32_t page_bytes = c->n_kv_heads * c->page_size * c->head_dim * 2;
+    const int32_t page_bytes = c->n_kv_heads * cache_head_bytes(c);
     return launch_after(cache_move_kernel, unsigned(sms * 8), 256, 0, st, books(c), static_cast<unsigned char*>(c->pool), s, c->n_layers * 2,
                         int64_t(c->n_pages) * page_bytes, page_bytes);
 }

@@ -1,0 +1,223 @@
+// Attention of up to NT * 8 query vectors to a block of 16 tokens held in 8 bits, by one warp with mma.sync: what the kernels of
+// disc_attend_held.cu and of disc_attend_group.cu's second step share.  The products and the reasons: disc_attend_held.cu.
+#pragma once
+
+#include "disc_attend.cuh"
+#include "disc_held.cuh"
+
+namespace disc {
+
+// shared memory of a block: keys [16][DP] | values [16][DP] | exponents of the keys [16] | of the values [16]
+template <int DP>
+__host__ __device__ constexpr int held_stage_bytes() { return 2 * BLK * DP + 2 * BLK; }
+
+// 16-byte chunk `ch` of token `row`: neighbouring tokens' chunks lie in different banks, so that ldmatrix reads eight of them at once
+// without conflicts
+template <int DP>
+__device__ __forceinline__ uint32_t held_chunk_at(int row, int ch) {
+    return DP == 128 ? uint32_t(row * 128 + ((ch ^ (row & 7)) << 4)) : uint32_t(row * 64 + ((ch ^ ((row >> 1) & 3)) << 4));
+}
+
+// Block `blk` of a page of which k and v are this head's parts; zeros beyond its tokens and its D values.  By a whole warp.
+template <int DP>
+__device__ __forceinline__ void load_held_block(uint32_t stage, const unsigned char* k, const unsigned char* v, int blk, int tokens, int D, int page_size, int lane) {
+    constexpr int CH = DP / 16;
+    const int at = blk * BLK * D;
+#pragma unroll
+    for (int j = 0; j < BLK * CH / 32; ++j) {
+        const int c = j * 32 + lane, row = c / CH, ch = c % CH;
+        const bool some = row < tokens && ch * 16 < D;
+        const int src = some ? at + row * D + ch * 16 : 0;
+        const uint32_t dst = stage + held_chunk_at<DP>(row, ch);
+        cp16(dst, k + src, some);
+        cp16(dst + BLK * DP, v + src, some);
+    }
+    if (lane < 2) cp16(stage + 2 * BLK * DP + lane * BLK, (lane ? v : k) + page_size * D + blk * BLK, true);
+}
+
+// Four codes as f16, exactly: those of bytes 0 and 2, and of bytes 1 and 3.  An e4m3 code's exponent and mantissa, moved to an
+// f16's places, stand for 2^-8 of its value (the biases are 7 and 15), denormal codes included.  An i8 code, its top bit
+// turned over, is the last byte of the f16 1024 + 128 + code.
+template <int HELD>
+__device__ __forceinline__ void codes_f16(uint32_t c, uint32_t& even, uint32_t& odd) {
+    if (HELD == HELD_E4M3) {
+        const uint32_t d = c << 8;
+        even = (d & 0x80008000u) | ((d >> 1) & 0x3f803f80u);
+        odd = (c & 0x80008000u) | ((c >> 1) & 0x3f803f80u);
+    } else {
+        const __half2 bias = __half2half2(__ushort_as_half(0x6480));           // 1152
+        const uint32_t a = (c & 0x00ff00ffu) ^ 0x64806480u, b = ((c >> 8) & 0x00ff00ffu) ^ 0x64806480u;
+        const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), bias), y = __hsub2(*reinterpret_cast<const __half2*>(&b), bias);
+        even = *reinterpret_cast<const uint32_t*>(&x);
+        odd = *reinterpret_cast<const uint32_t*>(&y);
+    }
+}
+template <int HELD>
+__device__ __forceinline__ constexpr float held_shift() { return HELD == HELD_E4M3 ? 8.f : 0.f; }      // log2 of code / f16
+
+template <int DP, int NT>
+struct HeldQueries {
+    uint32_t f[NT][DP / 16][2];        // vector lane / 4; values 16 kk + 4 (lane % 4) + {0, 2} and + {1, 3}, as the codes come
+    float c2[NT][2];                   // what a score of this thread's vectors, 2 (lane % 4) and the next, is multiplied with: units of log2
+};
+// q: this lane's vector (lane / 4 of the eight), `some`: there is one
+template <typename T, int DP, int HELD, int NT>
+__device__ __forceinline__ void load_held_queries(HeldQueries<DP, NT>& qs, int nt, const unsigned char* q, bool some, int D, float c2, int lane) {
+    float x[DP / 16][4];
+    uint32_t amax = 0;
+#pragma unroll
+    for (int kk = 0; kk < DP / 16; ++kk) {
+        uint2 w = make_uint2(0, 0);
+        if (some && kk * 16 < D) w = *reinterpret_cast<const uint2*>(q + kk * 32 + (lane & 3) * 8);
+        const float2 a = unpack2<T>(w.x), b = unpack2<T>(w.y);
+        x[kk][0] = a.x; x[kk][1] = a.y; x[kk][2] = b.x; x[kk][3] = b.y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) amax = max(amax, __float_as_uint(x[kk][i]) & 0x7fffffffu);
+    }
+    int up = 0;                        // what the vector is multiplied with, as a power of two
+    if (!is_half<T>()) {
+        amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+        amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+        if (amax > 0 && amax < 0x7f800000u) up = 8 - max(int(amax >> 23) - 127, -110);
+    }
+    const float f = pow2f(up);
+#pragma unroll
+    for (int kk = 0; kk < DP / 16; ++kk) {
+        qs.f[nt][kk][0] = pack2<__half>(x[kk][0] * f, x[kk][2] * f);
+        qs.f[nt][kk][1] = pack2<__half>(x[kk][1] * f, x[kk][3] * f);
+    }
+    const float back = c2 * pow2f(-up) * (HELD == HELD_E4M3 ? 256.f : 1.f);
+    qs.c2[nt][0] = __shfl_sync(0xffffffffu, back, (lane & 3) * 8);
+    qs.c2[nt][1] = __shfl_sync(0xffffffffu, back, (lane & 3) * 8 + 4);
+}
+
+template <int DP, int NT>
+struct HeldSums {                      // this thread's vectors: 2 (lane % 4) and the next of each eight
+    float o[NT][DP / 16][4];           // dims 16 j + 2 (lane / 4) of the two vectors, then the next dim of both, times 2^-t
+    float m[NT][2], l[NT][2];          // reference and sum of the probabilities
+    float t[NT][2];                    // reference of probability times the values' power of two
+};
+template <int DP, int NT>
+__device__ __forceinline__ void clear_held(HeldSums<DP, NT>& a) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int j = 0; j < DP / 16; ++j) a.o[nt][j][0] = a.o[nt][j][1] = a.o[nt][j][2] = a.o[nt][j][3] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) { a.m[nt][e] = a.t[nt][e] = -CUDART_INF_F; a.l[nt][e] = 0.f; }
+    }
+}
+template <int DP, int NT>
+__device__ __forceinline__ void finish_held(HeldSums<DP, NT>& a) {
+#pragma unroll
+    for (int x = 4; x < 32; x <<= 1)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) a.l[nt][e] += __shfl_xor_sync(0xffffffffu, a.l[nt][e], x);
+}
+
+// in[nt][e]: the block's tokens are seen by this thread's vectors.  Probabilities are rounded to f16 for the second product; where T is
+// f16 what that leaves out goes through a second one, so that the outputs' own rounding stays the larger.
+template <typename T, int DP, int HELD, int NT>
+__device__ __forceinline__ void add_held_block(HeldSums<DP, NT>& acc, const HeldQueries<DP, NT>& qs, uint32_t stage, int tokens, const bool (&in)[NT][2], int lane) {
+    constexpr bool TWO = is_half<T>();
+    // tokens lane / 4 (s[0], s[1]) and 8 further (s[2], s[3]); two chains of products
+    float s[NT][4], s2[NT][4];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = s2[nt][0] = s2[nt][1] = s2[nt][2] = s2[nt][3] = 0.f;
+#pragma unroll
+    for (int c = 0; c < DP / 32; ++c) {
+        uint32_t kf[4], a[4], b[4];
+        // matrices: tokens 0-7 and 8-15 at chunk 2 c, then at chunk 2 c + 1
+        ldsm4(stage + held_chunk_at<DP>(lane & 15, 2 * c + (lane >> 4)), kf);
+        codes_f16<HELD>(kf[0], a[0], a[2]);
+        codes_f16<HELD>(kf[1], a[1], a[3]);
+        codes_f16<HELD>(kf[2], b[0], b[2]);
+        codes_f16<HELD>(kf[3], b[1], b[3]);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            mma16<__half>(s[nt], a, qs.f[nt][2 * c][0], qs.f[nt][2 * c][1]);
+            mma16<__half>(s2[nt], b, qs.f[nt][2 * c + 1][0], qs.f[nt][2 * c + 1][1]);
+        }
+    }
+    const uint32_t exps = stage + 2 * BLK * DP + (lane >> 2);
+    int e[4];                          // keys, values; token lane / 4, 8 further
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm volatile("ld.shared.s8 %0, [%1];" : "=r"(e[i]) : "r"(exps + i * 8) : "memory");
+    const float k0 = exponent_scale(e[0]), k1 = exponent_scale(e[1]);
+    const float v0 = e[2] == NAN_EXP ? CUDART_NAN_F : float(e[2]), v1 = e[3] == NAN_EXP ? CUDART_NAN_F : float(e[3]);
+    const bool some0 = (lane >> 2) < tokens, some1 = (lane >> 2) + 8 < tokens;
+    float w[NT][4];
+    bool move = false;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float x = (s[nt][i] + s2[nt][i]) * (qs.c2[nt][i] * k0), y = (s[nt][2 + i] + s2[nt][2 + i]) * (qs.c2[nt][i] * k1);
+            const bool a = some0 && in[nt][i], b = some1 && in[nt][i];
+            s[nt][i] = a ? x : -CUDART_INF_F;
+            s[nt][2 + i] = b ? y : -CUDART_INF_F;
+            w[nt][i] = a ? x + v0 : -CUDART_INF_F;
+            w[nt][2 + i] = b ? y + v1 : -CUDART_INF_F;
+            move = move || fmaxf(s[nt][i], s[nt][2 + i]) > acc.m[nt][i] + SLACK || fmaxf(w[nt][i], w[nt][2 + i]) > acc.t[nt][i] + SLACK;
+        }
+    if (__any_sync(0xffffffffu, move)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                float ms = fmaxf(acc.m[nt][i], fmaxf(s[nt][i], s[nt][2 + i])), mw = fmaxf(acc.t[nt][i], fmaxf(w[nt][i], w[nt][2 + i]));
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) {
+                    ms = fmaxf(ms, __shfl_xor_sync(0xffffffffu, ms, x));
+                    mw = fmaxf(mw, __shfl_xor_sync(0xffffffffu, mw, x));
+                }
+                // sums without a finite reference so far are 0, or NaN
+                if (acc.m[nt][i] > -CUDART_INF_F) acc.l[nt][i] *= ex2_approx(acc.m[nt][i] - ms);
+                const float f = acc.t[nt][i] > -CUDART_INF_F ? ex2_approx(acc.t[nt][i] - mw) : 1.f;
+                acc.m[nt][i] = ms;
+                acc.t[nt][i] = mw;
+#pragma unroll
+                for (int j = 0; j < DP / 16; ++j) { acc.o[nt][j][i] *= f; acc.o[nt][j][2 + i] *= f; }
+            }
+    }
+    uint32_t p0[NT], p1[NT], r0[NT], r1[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const float m0 = acc.m[nt][0] > -CUDART_INF_F ? acc.m[nt][0] : 0.f, m1 = acc.m[nt][1] > -CUDART_INF_F ? acc.m[nt][1] : 0.f;
+        const float t0 = acc.t[nt][0] > -CUDART_INF_F ? acc.t[nt][0] : 0.f, t1 = acc.t[nt][1] > -CUDART_INF_F ? acc.t[nt][1] : 0.f;
+        acc.l[nt][0] += ex2_approx(s[nt][0] - m0) + ex2_approx(s[nt][2] - m0);
+        acc.l[nt][1] += ex2_approx(s[nt][1] - m1) + ex2_approx(s[nt][3] - m1);
+        const float x0 = ex2_approx(w[nt][0] - t0), x1 = ex2_approx(w[nt][1] - t1), x2 = ex2_approx(w[nt][2] - t0), x3 = ex2_approx(w[nt][3] - t1);
+        const uint32_t a = pack2<__half>(x0, x1), b = pack2<__half>(x2, x3);
+        p0[nt] = transposed(a);
+        p1[nt] = transposed(b);
+        if (TWO) {
+            const float2 ra = unpack2<__half>(a), rb = unpack2<__half>(b);
+            r0[nt] = transposed(pack2<__half>(x0 - ra.x, x1 - ra.y));
+            r1[nt] = transposed(pack2<__half>(x2 - rb.x, x3 - rb.y));
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < DP / 32; ++j) {
+        uint32_t vf[4], a[4], b[4];
+        // matrices: tokens 0-7 at chunks 2 j and 2 j + 1, then tokens 8-15; each register two dims of two tokens
+        ldsm4t(stage + BLK * DP + held_chunk_at<DP>((lane & 7) + ((lane >> 4) << 3), 2 * j + ((lane >> 3) & 1)), vf);
+        codes_f16<HELD>(vf[0], a[0], a[1]);
+        codes_f16<HELD>(vf[2], a[2], a[3]);
+        codes_f16<HELD>(vf[1], b[0], b[1]);
+        codes_f16<HELD>(vf[3], b[2], b[3]);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            mma16<__half>(acc.o[nt][2 * j], a, p0[nt], p1[nt]);
+            mma16<__half>(acc.o[nt][2 * j + 1], b, p0[nt], p1[nt]);
+            if (TWO) {
+                mma16<__half>(acc.o[nt][2 * j], a, r0[nt], r1[nt]);
+                mma16<__half>(acc.o[nt][2 * j + 1], b, r0[nt], r1[nt]);
+            }
+        }
+    }
+}
+
+}  // namespace disc

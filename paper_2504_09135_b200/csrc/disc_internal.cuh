@@ -215,6 +215,18 @@ int step_with_candidates(const disc_set* s, const void* logits, disc_dtype_t dty
 // the sizes and alignments of a cache, without its books (disc_cache.cu)
 int cache_sizes(const disc_cache_t* c);
 
+// How a cache lays out a page and key head: the tokens' vectors, and behind them, where they are held in 8 bits, an exponent per token.
+enum Held { HELD_PLAIN = 0, HELD_E4M3 = 1, HELD_I8 = 2 };
+inline int cache_held(const disc_cache_t* c) { return c->dtype >> 4; }
+inline int cache_type(const disc_cache_t* c) { return c->dtype & 15; }        // of the vectors given and returned
+inline int32_t cache_token_bytes(const disc_cache_t* c) { return cache_held(c) ? c->head_dim : c->head_dim * 2; }
+inline int32_t cache_head_bytes(const disc_cache_t* c) { return c->page_size * (cache_token_bytes(c) + (cache_held(c) ? 1 : 0)); }
+inline int64_t cache_plane_bytes(const disc_cache_t* c) { return int64_t(c->n_pages) * c->n_kv_heads * cache_head_bytes(c); }
+
+// Keys and values of new tokens into a cache held in 8 bits (disc_rope.cu); the arguments have been checked.  Strides in values.
+int write_held(const disc_cache_t* c, int32_t layer, const void* k, int64_t k_token, int64_t k_head, const void* v, int64_t v_token, int64_t v_head,
+               int32_t n_tokens, const int32_t* cu, int32_t n_seqs, const int32_t* rows, const uint8_t* status, cudaStream_t st);
+
 // top 23 bits k of a word -> u = (2k+1) * 2^-24, exact in fp32, as is 1-u
 __device__ __forceinline__ float uniform_from_bits(uint32_t r) {
     return float((r >> 9) * 2u + 1u) * 5.9604644775390625e-08f;

@@ -1,5 +1,5 @@
 """Binding of the operators the language model around the decoding step runs (include/disc.h):
-attention over prompts, the paged key-value cache and attention over it, log-probabilities.
+head norms and rotation, attention over prompts, the paged key-value cache and attention over it, log-probabilities.
 
 Argument marshalling only, like binding.py; there is no CPU fallback.  Outputs made here belong to the stream the call is
 given (None: the current one).  A cache, a plan or an output used on another stream than the call before needs an event between
@@ -12,7 +12,7 @@ import math
 
 import torch
 
-from .binding import DISC_BF16, DISC_F16, DISC_F32, DiscError, _Cache, _check, _dev, _here, _stream_ptr, lib
+from .binding import DISC_BF16, DISC_F16, DISC_F32, DISC_HELD_E4M3, DISC_HELD_I8, DiscError, _Cache, _Rope, _check, _dev, _here, _stream_ptr, lib
 
 _HALF = {torch.bfloat16: DISC_BF16, torch.float16: DISC_F16}
 _LOGIT = {torch.float32: DISC_F32, torch.bfloat16: DISC_BF16}
@@ -154,6 +154,158 @@ def disc_logprobs_grad(logits: torch.Tensor, targets, lse: torch.Tensor, entropy
     return out
 
 
+# ---- head norms and rotation --------------------------------------------------------------------------
+def _how(dtype, d: int, inv_freq, norm, q_weight, k_weight, eps, interleaved) -> _Rope:
+    """What is done to the vectors, with the checks that need the tensors."""
+    rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+    wt = torch.float32
+    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is None:
+            continue
+        if not norm:
+            raise TypeError(f"{name}: the weights are the norm's; there is none")
+        _want(w, d, name)
+        if w.dtype is dtype:
+            wt = dtype
+    if q_weight is not None and k_weight is not None and q_weight.dtype is not k_weight.dtype:
+        raise TypeError("q_weight, k_weight: expected the same type")
+    return _Rope(_dev(inv_freq, torch.float32, "inv_freq"), _dev(q_weight, wt, "q_weight"), _dev(k_weight, wt, "k_weight"), float(eps), rot,
+                 int(bool(interleaved)), int(bool(norm)), DISC_F32 if wt is torch.float32 else _HALF[wt])
+
+
+def _positions(positions, n: int, inv_freq):
+    if positions is None:
+        if inv_freq is not None:
+            raise TypeError("positions: expected one per token")
+        return 0
+    _want(positions, n, "positions")
+    return _dev(positions, torch.int32, "positions")
+
+
+def _heads(q, k, where: str):
+    """Shapes of q [n, Hq, D] and k [n, Hkv, D], either of which may be None: (dtype, n, Hq, Hkv, D)."""
+    t = q if q is not None else k
+    if t is None:
+        raise TypeError(f"{where}: neither queries nor keys")
+    if t.dtype not in _HALF:
+        raise DiscError(-7, where)
+    if t.dim() != 3 or (k is not None and q is not None and (k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2])):
+        raise TypeError("q, k: expected [tokens, heads, head_dim] with the same tokens and head_dim")
+    return t.dtype, t.shape[0], 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], t.shape[2]
+
+
+_NONE = (0, 0, 0)
+
+
+def _like(t, out, name: str, stream):
+    """An output for vectors t: made here, or the given one of the same shape (which may be strided)."""
+    if t is None:
+        return None, _NONE
+    if out is None:
+        out = _alloc(stream, _empty, t.shape, t.dtype, t.device)
+        return out, (out.data_ptr(), out.shape[1] * out.shape[2], out.shape[2])
+    if out.shape != t.shape:
+        raise TypeError(f"{name}: expected the shape of the vectors")
+    v = _vectors(out, t.dtype, name)
+    for size, stride in zip(out.shape[:2], v[1:]):
+        if size > 1 and stride == 0:
+            raise TypeError(f"{name}: one place for several tokens or heads")
+    return out, v
+
+
+def _aligned(t, stream):
+    """Gradients come as autograd makes them: a copy where strides or base are not what the kernels take."""
+    if t is not None and (t.stride(2) != 1 or (t.stride(0) | t.stride(1)) & 7 or t.data_ptr() & 15):
+        t = _alloc(stream, lambda: t.clone(memory_format=torch.contiguous_format))
+    return t
+
+
+class _NormRope(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, positions, inv_freq, q_weight, k_weight, norm, eps, interleaved, stream):
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(q, k, positions, inv_freq, q_weight, k_weight)
+        ctx.how = (norm, eps, interleaved)
+        return disc_norm_rope(q, k, positions, inv_freq, norm=norm, q_weight=q_weight, k_weight=k_weight, eps=eps, interleaved=interleaved, stream=stream)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_q, d_k):
+        q, k, positions, inv_freq, qw, kw = ctx.saved_tensors
+        norm, eps, interleaved = ctx.how
+        if d_q is None:
+            q = qw = None
+        if d_k is None:
+            k = kw = None
+        if q is None and k is None:
+            return (None,) * 10
+        d_q, d_k, d_qw, d_kw = disc_norm_rope_grad(q, k, positions, inv_freq, d_q, d_k, norm=norm, q_weight=qw, k_weight=kw, eps=eps, interleaved=interleaved)
+        if d_qw is not None:
+            d_qw = d_qw.to(qw.dtype)
+        if d_kw is not None:
+            d_kw = d_kw.to(kw.dtype)
+        return d_q, d_k, None, None, d_qw, d_kw, None, None, None, None
+
+
+def disc_norm_rope(q, k, positions, inv_freq=None, *, norm: bool = True, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False,
+                   out=None, stream=None):
+    """Each head's RMS norm and the rotation by the token's position: q [n, Hq, D], k [n, Hkv, D] (bf16 or f16, slices of a fused
+    projection are fine; either may be None), positions int32[n] -> (q', k').  inv_freq float32[rot / 2]: the first `rot` values
+    of a vector are rotated (None: none); q_weight, k_weight [D] float32 or the vectors' type (None: 1).
+    out: a pair of buffers of the same shapes, which may be q and k themselves.  Where an input or a weight requires a gradient the
+    results have one (disc_norm_rope_grad; its call goes to the current stream of this one), and `out` is refused."""
+    if torch.is_grad_enabled():
+        if inv_freq is not None and inv_freq.requires_grad:
+            _without_grad(inv_freq, "inv_freq")
+        if any(t is not None and t.requires_grad for t in (q, k, q_weight, k_weight)):
+            if out is not None:
+                raise TypeError("out: given buffers have no history; detach the inputs, or call under torch.no_grad()")
+            return _NormRope.apply(q, k, positions, inv_freq, q_weight, k_weight, norm, eps, interleaved, stream)
+    dtype, n, hq, hkv, d = _heads(q, k, "disc_norm_rope")
+    qv = _NONE if q is None else _vectors(q, dtype, "q")
+    kv = _NONE if k is None else _vectors(k, dtype, "k")
+    how = _how(dtype, d, inv_freq, norm, q_weight, k_weight, eps, interleaved)
+    pos = _positions(positions, n, inv_freq)
+    q_out, k_out = (None, None) if out is None else out
+    q_out, qo = _like(q, q_out, "out", stream)
+    k_out, ko = _like(k, k_out, "out", stream)
+    _check(lib().disc_norm_rope(C.addressof(how), *qv, *kv, _HALF[dtype], hq, hkv, d, n, pos, *qo, *ko, _stream_ptr(stream)), "disc_norm_rope")
+    return q_out, k_out
+
+
+def disc_norm_rope_grad(q, k, positions, inv_freq, d_q, d_k, *, norm: bool = True, q_weight=None, k_weight=None, eps: float = 1e-6,
+                        interleaved: bool = False, stream=None):
+    """From the gradients d_q, d_k of disc_norm_rope's results those of its inputs: (dq, dk, dq_weight, dk_weight), the weights' in
+    float32 (None for a weight that is not given)."""
+    dtype, n, hq, hkv, d = _heads(q, k, "disc_norm_rope_grad")
+    for t, x, name in ((q, d_q, "d_q"), (k, d_k, "d_k")):
+        if (t is None) != (x is None) or (t is not None and x.shape != t.shape):
+            raise TypeError(f"{name}: expected the shape of the vectors")
+    d_q, d_k = _aligned(d_q, stream), _aligned(d_k, stream)
+    vec = [_NONE if t is None else _vectors(t, dtype, name) for t, name in ((q, "q"), (k, "k"), (d_q, "d_q"), (d_k, "d_k"))]
+    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight"), (inv_freq, "inv_freq")):
+        if w is not None and w.requires_grad:
+            _without_grad(w, name)
+    how = _how(dtype, d, inv_freq, norm, q_weight, k_weight, eps, interleaved)
+    pos = _positions(positions, n, inv_freq)
+    dev = (q if q is not None else k).device
+    need = 0
+    if q_weight is not None or k_weight is not None:
+        need = lib().disc_norm_rope_scratch_bytes(hq, hkv, d, n)
+        if need < 0:
+            raise DiscError(int(need), "disc_norm_rope_scratch_bytes")
+
+    def outputs():
+        return (None if q is None else torch.empty(q.shape, dtype=dtype, device=dev), None if k is None else torch.empty(k.shape, dtype=dtype, device=dev),
+                None if q_weight is None else torch.empty(d, dtype=_F32, device=dev), None if k_weight is None else torch.empty(d, dtype=_F32, device=dev),
+                torch.empty(need, dtype=torch.uint8, device=dev) if need else None)
+
+    gq, gk, gqw, gkw, scratch = _alloc(stream, outputs)
+    _check(lib().disc_norm_rope_grad(C.addressof(how), *vec[0], *vec[1], _HALF[dtype], hq, hkv, d, n, pos, *vec[2], *vec[3], _own(gq), _own(gk), _own(gqw),
+                                     _own(gkw), _own(scratch), need, _stream_ptr(stream)), "disc_norm_rope_grad")
+    return gq, gk, gqw, gkw
+
+
 # ---- attention over prompts -------------------------------------------------------------------------
 _F32, _DENSE = torch.float32, torch.contiguous_format
 
@@ -234,18 +386,37 @@ def disc_attend_check(device="cuda", stream=None, *, plan: "AttendPlan | None" =
 
 
 # ---- the key-value cache ----------------------------------------------------------------------------
+_HELD = {None: 0, "e4m3": DISC_HELD_E4M3, "i8": DISC_HELD_I8}
+
+
 class DiscCache:
     """A key-value cache in pages: pool [layers, 2, pages, kv heads, page size, head dim] (bf16 or f16) and its
     books, one int32 buffer holding the page table [rows, table_width], the lengths [rows] and the reference
-    counts [pages].  Without `book` the cache starts empty; a given buffer is used as it is."""
+    counts [pages].  Without `book` the cache starts empty; a given buffer is used as it is.
 
-    def __init__(self, pool: torch.Tensor, n_rows: int, table_width: int, *, book: torch.Tensor | None = None):
-        if not (isinstance(pool, torch.Tensor) and pool.is_cuda and pool.ndim == 6 and pool.shape[1] == 2 and pool.is_contiguous()):
-            raise TypeError("pool: expected a contiguous CUDA tensor [layers, 2, pages, kv heads, page size, head dim]")
-        if pool.dtype not in _HALF:
+    held="e4m3" or "i8": vectors of type `dtype` held in 8 bits, one code per value and a power of two per vector; the pool is then
+    uint8 [layers, 2, pages, kv heads, page_size * (head dim + 1)], a page and head's codes and behind them its exponents."""
+
+    def __init__(self, pool: torch.Tensor, n_rows: int, table_width: int, *, book: torch.Tensor | None = None, held: str | None = None,
+                 dtype: torch.dtype | None = None, page_size: int | None = None):
+        if held not in _HELD:
+            raise TypeError(f"held: expected None, 'e4m3' or 'i8', got {held!r}")
+        if not (isinstance(pool, torch.Tensor) and pool.is_cuda and pool.ndim == (5 if held else 6) and pool.shape[1] == 2 and pool.is_contiguous()):
+            raise TypeError("pool: expected a contiguous CUDA tensor [layers, 2, pages, kv heads, " + ("page size * (head dim + 1)]" if held else "page size, head dim]"))
+        self.pool, self.n_rows, self.table_width, self.held = pool, int(n_rows), int(table_width), held
+        if held:
+            self.dtype = torch.bfloat16 if dtype is None else dtype
+            if pool.dtype != torch.uint8 or not page_size or pool.shape[4] % page_size:
+                raise TypeError("pool: expected uint8, with page_size tokens to a page")
+            self.n_layers, _, self.n_pages, self.n_kv_heads, part = pool.shape
+            self.page_size, self.head_dim = int(page_size), part // int(page_size) - 1
+        else:
+            self.dtype = pool.dtype
+            self.n_layers, _, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = pool.shape
+            if (dtype or pool.dtype) != pool.dtype or (page_size or self.page_size) != self.page_size:
+                raise TypeError("pool: not of this dtype or page_size")
+        if self.dtype not in _HALF:
             raise DiscError(-7, "DiscCache")
-        self.pool, self.n_rows, self.table_width = pool, int(n_rows), int(table_width)
-        self.n_layers, _, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = pool.shape
         a, b = self.n_rows * self.table_width, self.n_rows * self.table_width + self.n_rows
         if book is None:
             book = torch.zeros(b + self.n_pages, dtype=torch.int32, device=pool.device)
@@ -256,7 +427,7 @@ class DiscCache:
         self.table, self.len, self.ref = book[:a].view(self.n_rows, self.table_width), book[a:b], book[b:]
         self._c = _Cache(pool.data_ptr(), self.table.data_ptr(), self.len.data_ptr(), self.ref.data_ptr(), None, 0,
                          self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim, self.n_rows,
-                         self.table_width, _HALF[pool.dtype])
+                         self.table_width, _HALF[self.dtype] | _HELD[held])
         self._p = C.addressof(self._c)
         need = lib().disc_cache_scratch_bytes(self._p)
         if need < 0:
@@ -264,13 +435,16 @@ class DiscCache:
         self._scratch = torch.empty(int(need), dtype=torch.uint8, device=pool.device)
         self._c.scratch, self._c.scratch_bytes = self._scratch.data_ptr(), int(need)
         self._plans: dict = {}
-        self._sizes = tuple(pool.shape) + (self.n_rows, self.table_width, pool.dtype)
+        self._sizes = tuple(pool.shape) + (self.n_rows, self.table_width, self.dtype, held, self.page_size)
 
     @staticmethod
     def empty(n_layers: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, n_rows: int, table_width: int, *,
-              dtype=torch.bfloat16, device="cuda") -> "DiscCache":
-        pool = torch.zeros((n_layers, 2, n_pages, n_kv_heads, page_size, head_dim), dtype=dtype, device=device)
-        return DiscCache(pool, n_rows, table_width)
+              dtype=torch.bfloat16, device="cuda", held: str | None = None) -> "DiscCache":
+        if held:
+            pool = torch.zeros((n_layers, 2, n_pages, n_kv_heads, page_size * (head_dim + 1)), dtype=torch.uint8, device=device)
+        else:
+            pool = torch.zeros((n_layers, 2, n_pages, n_kv_heads, page_size, head_dim), dtype=dtype, device=device)
+        return DiscCache(pool, n_rows, table_width, held=held, dtype=dtype, page_size=page_size)
 
 
 def _books(cache: DiscCache) -> int:
@@ -308,8 +482,8 @@ def disc_cache_write(cache: DiscCache, layer: int, k: torch.Tensor, v: torch.Ten
                      rows: torch.Tensor | None = None, status: torch.Tensor | None = None, stream=None):
     """k, v [tokens, kv heads, head dim]: the newest tokens of sequence i (row rows[i], None: row i) are
     cu[i] .. cu[i+1]-1 (None: one token each)."""
-    kp, kt, kh = _vectors(k, cache.pool.dtype, "k")
-    vp, vt, vh = _vectors(v, cache.pool.dtype, "v")
+    kp, kt, kh = _vectors(k, cache.dtype, "k")
+    vp, vt, vh = _vectors(v, cache.dtype, "v")
     n, h, d = k.shape
     if v.shape != k.shape or h != cache.n_kv_heads or d != cache.head_dim:
         raise TypeError("k, v: expected [tokens, kv heads, head dim] of the cache")
@@ -320,6 +494,57 @@ def disc_cache_write(cache: DiscCache, layer: int, k: torch.Tensor, v: torch.Ten
     _check(lib().disc_cache_write(_books(cache), int(layer), kp, kt, kh, vp, vt, vh, n, _dev(cu, torch.int32, "cu"), n_seqs,
                                   _dev(rows, torch.int32, "rows"), _dev(status, torch.uint8, "status"), _stream_ptr(stream)),
            "disc_cache_write")
+
+
+def disc_norm_rope_write(cache: DiscCache, layer: int, q, k: torch.Tensor, v: torch.Tensor, inv_freq=None, *, positions=None, norm: bool = True,
+                         q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False, cu: torch.Tensor | None = None,
+                         rows: torch.Tensor | None = None, status: torch.Tensor | None = None, out=None, stream=None):
+    """disc_norm_rope of the newest tokens' q (None: no queries) and k, and disc_cache_write of the resulting keys and of v, in one
+    launch -> q'.  positions None: each token's place in its row.  out: a buffer for q', which may be q itself."""
+    hq = 0 if q is None else q.shape[1]
+    qv = _NONE if q is None else _vectors(q, cache.dtype, "q")
+    kv, vv = _vectors(k, cache.dtype, "k"), _vectors(v, cache.dtype, "v")
+    n, h, d = k.shape
+    if v.shape != k.shape or h != cache.n_kv_heads or d != cache.head_dim:
+        raise TypeError("k, v: expected [tokens, kv heads, head dim] of the cache")
+    if q is not None and (q.shape[0] != n or q.shape[2] != d):
+        raise TypeError("q: expected [tokens, Hq, head dim] with the keys' tokens")
+    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight"), (inv_freq, "inv_freq")):
+        if w is not None and w.requires_grad:
+            _without_grad(w, name)
+    how = _how(cache.dtype, d, inv_freq, norm, q_weight, k_weight, eps, interleaved)
+    n_seqs = n if cu is None else cu.numel() - 1
+    if rows is not None:
+        _want(rows, n_seqs, "rows")
+    _want(status, cache.n_rows, "status")
+    _want(positions, n, "positions")
+    out, qo = _like(q, out, "out", stream)
+    _check(lib().disc_norm_rope_write(_books(cache), int(layer), C.addressof(how), *qv, hq, *kv, *vv, n, _dev(positions, torch.int32, "positions"),
+                                      _dev(cu, torch.int32, "cu"), n_seqs, _dev(rows, torch.int32, "rows"), _dev(status, torch.uint8, "status"), *qo,
+                                      _stream_ptr(stream)), "disc_norm_rope_write")
+    return out
+
+
+def disc_cache_read(cache: DiscCache, layer: int, cu: torch.Tensor, n_tokens: int, *, rows: torch.Tensor | None = None,
+                    start: torch.Tensor | None = None, out=None, stream=None):
+    """Tokens of some rows, packed, in the cache's type: token cu[i] + j of the result is token start[i] + j (None: j) of row rows[i]
+    (None: row i) -> (k, v) [n_tokens, kv heads, head dim]; zeros for tokens the row does not have.  n_tokens: cu[-1], or more
+    (what lies behind is left as it is).  out: a pair of contiguous buffers of that shape."""
+    n_seqs = cu.numel() - 1
+    for t, name in ((rows, "rows"), (start, "start")):
+        _want(t, n_seqs, name)
+    shape = (int(n_tokens), cache.n_kv_heads, cache.head_dim)
+    if out is None:
+        k, v = _alloc(stream, lambda: (_empty(shape, cache.dtype, cache.pool.device), _empty(shape, cache.dtype, cache.pool.device)))
+    else:
+        k, v = out
+        for t, name in ((k, "k"), (v, "v")):
+            _dev(t, cache.dtype, name)
+            if t.shape != shape:
+                raise TypeError(f"{name}: expected [n_tokens, kv heads, head dim]")
+    _check(lib().disc_cache_read(_books(cache), int(layer), _dev(cu, torch.int32, "cu"), n_seqs, _dev(rows, torch.int32, "rows"),
+                                 _dev(start, torch.int32, "start"), int(n_tokens), k.data_ptr(), v.data_ptr(), _stream_ptr(stream)), "disc_cache_read")
+    return k, v
 
 
 def disc_cache_compact(cache: DiscCache, *, live: torch.Tensor | None = None, stream=None) -> torch.Tensor:
@@ -371,10 +596,10 @@ def disc_attend_cached(cache: DiscCache, layer: int, q: torch.Tensor, plan: Atte
                        out=None, lse=None, stream=None):
     """One new token per row: q [rows, Hq, D] against the row's tokens in layer `layer` -> (out [rows, Hq, D],
     lse float[rows, Hq])."""
-    qp, qr, qh = _vectors(q, cache.pool.dtype, "q")
+    qp, qr, qh = _vectors(q, cache.dtype, "q")
     if not (qr and qh):
         q = _spread(q, stream)
-        qp, qr, qh = _vectors(q, cache.pool.dtype, "q")
+        qp, qr, qh = _vectors(q, cache.dtype, "q")
     n, h, d = q.shape
     if n != cache.n_rows or h != plan.n_q_heads or d != cache.head_dim:
         raise TypeError("q: expected [rows, Hq, head dim] of the cache and the plan")
