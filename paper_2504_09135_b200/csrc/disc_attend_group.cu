@@ -21,7 +21,13 @@
 // operand type of the second product; sums of the remainders apart from O, as the rows form has them, would need 320 of the 256
 // columns of tensor memory that a block can have with two to an SM.
 
+//
+// A cache held in 8 bits: the loads bring codes and exponents, and two more warps make of them the tiles that the products read, in
+// the vectors' type and exactly the values that are held; the products and the softmax are the same.  Kernel 2 takes its blocks as
+// disc_attend_held.cu does.
+
 #include "disc_attend.cuh"
+#include "disc_held_mma.cuh"
 
 namespace {
 
@@ -174,17 +180,19 @@ __global__ void __launch_bounds__(PT) group_items_kernel(const PlanParams p) {
 }
 
 // ---- kernel 1 -----------------------------------------------------------------------------------------
-constexpr int THREADS = 192;
-template <int DP>
+template <int DP, int HELD>
 struct Shape {
+    static constexpr int THREADS = HELD ? 256 : 192;
     static constexpr int BOXES = DP / BOX;
     static constexpr int BOX_BYTES = TN * BOX * 2;
     static constexpr int TILE_BYTES = BOXES * BOX_BYTES;
     static constexpr int Q_BYTES = BOXES * Q_BOX_BYTES;
-    static constexpr int STAGES = DP == 128 ? 5 : 10;              // with Q as much as two blocks fit into an SM
+    static constexpr int STAGES = HELD ? (DP == 128 ? 3 : 4) : DP == 128 ? 5 : 10;          // with Q as much as two blocks fit into an SM
+    static constexpr int CODE_STAGES = HELD ? (DP == 128 ? 4 : 8) : 0;
+    static constexpr int CODE_BYTES = TN * DP + TN;                // codes of a tile, its exponents
     static constexpr int TMEM = 256;                               // columns: S 64, O up to 128
-    static constexpr int BARRIERS = 5 + 2 * STAGES;
-    static constexpr int SMEM = Q_BYTES + STAGES * TILE_BYTES + BARRIERS * 8 + 16;
+    static constexpr int BARRIERS = 5 + 2 * STAGES + 2 * CODE_STAGES;
+    static constexpr int SMEM = Q_BYTES + STAGES * TILE_BYTES + CODE_STAGES * CODE_BYTES + BARRIERS * 8 + 16;
 };
 
 struct GroupParams {
@@ -194,16 +202,55 @@ struct GroupParams {
     float c2;
     uint32_t* error;
     uint32_t idesc_qk, idesc_pv;
+    const unsigned char* k;            // held in 8 bits: the planes, which no tensor map describes
+    const unsigned char* v;
+    int32_t pages, head_bytes;
 };
 
-template <typename T, int DP>
-__global__ void __launch_bounds__(THREADS, 2)
+// `bytes`, a multiple of 16, to shared memory, both on 16-byte boundaries
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
+}
+
+// The first `tokens` rows of a tile out of their codes, by 64 threads: a thread per token.  The codes lie D to a token, the tile as the
+// swizzle of 128 bytes wants it.  Neighbouring threads begin at different chunks: reads and writes then go to different banks.  Dims from D on
+// are zeros (Q is 0 there, and 0 times whatever the memory held may be NaN).
+template <typename T, int DP, int HELD>
+__device__ __forceinline__ void expand_tile(unsigned char* tile, const unsigned char* codes, int tokens, int D, int box_bytes, int t) {
+    if (t >= tokens) return;
+    const int e = reinterpret_cast<const signed char*>(codes)[TN * DP + t];
+    uint32_t scale2;
+    const bool fast = fast_scale<T, HELD>(e, &scale2);
+    const float scale = exponent_scale(e);
+    unsigned char* row = tile + t * (BOX * 2);
+    const unsigned char* from = codes + t * D;
+    constexpr int CH = DP / 16;
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        const int c = (j + t) % CH;
+        uint32_t x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (c * 16 < D) {
+            const uint4 w = *reinterpret_cast<const uint4*>(from + c * 16);
+            if (fast) fast_values16<T, HELD>(w, scale2, x); else values16<T, HELD>(w, scale, x);
+        }
+        unsigned char* box = row + c / 4 * box_bytes;
+        const int at = c % 4 * 2;
+        *reinterpret_cast<uint4*>(box + ((at ^ (t & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
+        *reinterpret_cast<uint4*>(box + (((at + 1) ^ (t & 7)) << 4)) = make_uint4(x[4], x[5], x[6], x[7]);
+    }
+}
+
+template <typename T, int DP, int HELD>
+__global__ void __launch_bounds__(Shape<DP, HELD>::THREADS, 2)
 attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                     const __grid_constant__ CUtensorMap map_v, const GroupParams p) {
-    using S = Shape<DP>;
+    using S = Shape<DP, HELD>;
     extern __shared__ __align__(1024) unsigned char q_tile[];      // nothing else is in shared memory: it begins on a swizzle atom
     unsigned char* ring = q_tile + S::Q_BYTES;
-    uint64_t* bars = reinterpret_cast<uint64_t*>(ring + S::STAGES * S::TILE_BYTES);
+    unsigned char* code_ring = ring + S::STAGES * S::TILE_BYTES;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(code_ring + S::CODE_STAGES * S::CODE_BYTES);
     uint64_t* q_full = bars;
     uint64_t* q_empty = bars + 1;
     uint64_t* s_full = bars + 2;
@@ -211,6 +258,8 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     uint64_t* p_full = bars + 4;
     uint64_t* kv_full = bars + 5;
     uint64_t* kv_empty = bars + 5 + S::STAGES;
+    uint64_t* code_full = bars + 5 + 2 * S::STAGES;
+    uint64_t* code_empty = code_full + S::CODE_STAGES;
     uint32_t& tmem_slot = *reinterpret_cast<uint32_t*>(bars + S::BARRIERS);
     int& s_abort = *reinterpret_cast<int*>(bars + S::BARRIERS + 1);
     volatile int* abort = &s_abort;
@@ -219,7 +268,8 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     if (threadIdx.x == 0) {
         s_abort = 0;
         mbar_init(q_full, 1); mbar_init(q_empty, 1); mbar_init(s_full, 1); mbar_init(o_full, 1); mbar_init(p_full, 4);
-        for (int s = 0; s < S::STAGES; ++s) { mbar_init(kv_full + s, 1); mbar_init(kv_empty + s, 1); }
+        for (int s = 0; s < S::STAGES; ++s) { mbar_init(kv_full + s, HELD ? 2 : 1); mbar_init(kv_empty + s, 1); }
+        for (int s = 0; s < S::CODE_STAGES; ++s) { mbar_init(code_full + s, 1); mbar_init(code_empty + s, 2); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 5) {
@@ -255,6 +305,28 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                     const int here = min(TILE_BLKS, blks - t);
                     // lane l brings in block l % 4: its keys, then its values
                     const int b = lane % TILE_BLKS, blk = begin + t + b;
+                    if constexpr (HELD != 0) {
+                        int page = b < here ? table[blk / p.blks_per_page] : 0;
+                        if (unsigned(page) >= unsigned(p.pages)) page = 0;      // a plan older than the books: no place outside the pool is read
+                        const int64_t part = (int64_t(page) * p.kv_heads + head) * p.head_bytes;
+                        const int in_page = blk % p.blks_per_page * BLK;
+#pragma unroll
+                        for (int kv = 0; kv < 2; ++kv, ++load) {
+                            const int s = load % S::CODE_STAGES, round = load / S::CODE_STAGES;
+                            if (round > 0 && ok) ok = mbar_wait_all(code_empty + s, (round - 1) & 1, abort);
+                            if (!ok) continue;
+                            if (lane == 0) mbar_expect_tx(code_full + s, uint32_t(here) * (BLK * p.D + BLK));
+                            __syncwarp();
+                            if (lane < TILE_BLKS && b < here) {
+                                unsigned char* to = code_ring + s * S::CODE_BYTES;
+                                const unsigned char* from = (kv ? p.v : p.k) + part;
+                                bulk_load(to + b * BLK * p.D, from + in_page * p.D, BLK * p.D, code_full + s);
+                                bulk_load(to + TN * DP + b * BLK, from + p.page_size * p.D + in_page, BLK, code_full + s);
+                            }
+                            __syncwarp();
+                        }
+                        continue;
+                    }
                     int y = 0;
                     if (b < here) y = (table[blk / p.blks_per_page] * p.kv_heads + head) * p.page_size + blk % p.blks_per_page * BLK;
 #pragma unroll
@@ -335,6 +407,28 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
             for (int back = 0; back < S::STAGES && back < load && ok; ++back)
                 ok = mbar_wait_all(kv_empty + (load - 1 - back) % S::STAGES, ((load - 1 - back) / S::STAGES) & 1, abort);
             if (ok && n > 0) mbar_wait_all(q_empty, (n - 1) & 1, abort);
+        } else if constexpr (HELD != 0) {
+            // ---- tiles out of codes
+            int load = 0;
+            bool ok = true;
+            for (int n = item0; n < item1 && ok; ++n) {
+                const GroupItem* it = p.plan.group_items + n;
+                const int blks = it->end - it->begin;
+                for (int t = 0; t < blks && ok; t += TILE_BLKS) {
+                    const int tokens = min(TILE_BLKS, blks - t) * BLK;
+#pragma unroll 1
+                    for (int kv = 0; kv < 2 && ok; ++kv, ++load) {
+                        const int c = load % S::CODE_STAGES, s = load % S::STAGES, round = load / S::STAGES;
+                        ok = mbar_wait_all(code_full + c, (load / S::CODE_STAGES) & 1, abort);
+                        if (ok && round > 0) ok = mbar_wait_all(kv_empty + s, (round - 1) & 1, abort);
+                        if (!ok) break;
+                        expand_tile<T, DP, HELD>(ring + s * S::TILE_BYTES, code_ring + c * S::CODE_BYTES, tokens, p.D, S::BOX_BYTES, threadIdx.x - 192);
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the products read what has just been written
+                        __syncwarp();
+                        if (lane == 0) { mbar_arrive(kv_full + s); mbar_arrive(code_empty + c); }
+                    }
+                }
+            }
         }
     } else {
         // ---- softmax: this thread's query vector
@@ -414,12 +508,14 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
 // ---- kernel 2 -----------------------------------------------------------------------------------------
 constexpr int JT = 128;                // threads of a block: 4 warps, each with a row and key head of its own
 
-template <int DP>
+template <int DP, int HELD>
 struct JoinSmem {
     static constexpr int O_LD = DP + 4;                            // fp32 sums [8 heads][DP], over keys and values no longer needed
     static constexpr int BLOCK_BYTES = BLK * DP * 2;
-    static constexpr int WARP_BYTES = 4 * BLOCK_BYTES + 256;       // keys and values of two blocks; maximum and sum of 8 heads
-    static_assert(8 * O_LD * 4 <= 2 * BLOCK_BYTES, "the sums fit over a block");
+    static constexpr int STEP_BYTES = HELD ? held_stage_bytes<DP>() : 2 * BLOCK_BYTES;     // keys and values of a block
+    static constexpr int O_BYTES = HELD ? 8 * O_LD * 4 : 0;        // held in 8 bits a block is smaller than the sums: they have a place of their own
+    static constexpr int WARP_BYTES = 2 * STEP_BYTES + O_BYTES + 256;      // two blocks; maximum and sum of 8 heads
+    static_assert(HELD || 8 * O_LD * 4 <= 2 * BLOCK_BYTES, "the sums fit over a block");
 };
 
 // The products are taken the other way round, S^T = K Q^T and O^T = V^T P^T: 8 query heads are then the narrow side of
@@ -427,11 +523,11 @@ struct JoinSmem {
 // way on 4096 rows x 4 key heads).  A warp goes through one or two key heads of its row (the launch says why) and has the
 // next block's loads in flight under the present one's products (78 us without).
 // EXACT: the head dim is DP itself, and all strides and ends along it are known.
-template <typename T, int DP, bool EXACT>
+template <typename T, int DP, bool EXACT, int HELD>
 __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p, int heads_per_job) {
     let_later_in();
     wait_for_earlier();
-    using S = JoinSmem<DP>;
+    using S = JoinSmem<DP, HELD>;
     constexpr int CH = DP / 8;
     const int D = EXACT ? DP : p.D;
     extern __shared__ __align__(1024) unsigned char smem[];
@@ -452,7 +548,7 @@ __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p
     const int32_t* table = p.table + int64_t(row) * p.width;
     const int64_t head_bytes = int64_t(p.page_size) * D * 2;
     unsigned char* own = smem + warp * S::WARP_BYTES;
-    float* ml_sm = reinterpret_cast<float*>(own + 4 * S::BLOCK_BYTES);     // [8] maxima, [8] sums
+    float* ml_sm = reinterpret_cast<float*>(own + 2 * S::STEP_BYTES + S::O_BYTES);         // [8] maxima, [8] sums
     const int eights = (G + 7) / 8;                    // a key head's query heads, eight at a time
     const int steps = (head1 - head0) * eights * left;
 
@@ -469,6 +565,12 @@ __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p
             const int head = head0 + load_unit / eights, blk = begin + load_blk;
             const int page = __shfl_sync(FULL, my_page, load_blk), tokens = min(BLK, len - blk * BLK);
             if (++load_blk == left) { load_blk = 0; ++load_unit; }
+            if constexpr (HELD != 0) {
+                const int64_t part = (int64_t(page) * p.kv_heads + head) * p.head_bytes;
+                load_held_block<DP>(smem_u32(own) + (step & 1) * S::STEP_BYTES, p.k + part, p.v + part, blk % sh.blks_per_page, tokens, D, p.page_size, lane);
+                cp_commit();
+                return;
+            }
             const int64_t off = (int64_t(page) * p.kv_heads + head) * head_bytes + int64_t(blk % sh.blks_per_page) * (BLK * 2) * D + lane_src;
             const unsigned char* k_src = p.k + off;
             const unsigned char* v_src = p.v + off;
@@ -491,8 +593,33 @@ __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p
         const int head = head0 + unit / eights, g0 = unit % eights * 8;
         const int heads = min(8, G - g0);
         const int64_t out_at = (int64_t(row) * p.kv_heads + head) * G;
-        float* o_sm = reinterpret_cast<float*>(own);
-        if (left > 0) {
+        float* o_sm = reinterpret_cast<float*>(own + (HELD ? 2 * S::STEP_BYTES : 0));
+        if constexpr (HELD != 0) {
+            if (left > 0) {
+                HeldQueries<DP, 1> qs;
+                load_held_queries<T, DP, HELD>(qs, 0, p.q + row * p.q_row + (head * G + g0 + (lane >> 2)) * p.q_head, (lane >> 2) < heads, D, p.c2, lane);
+                HeldSums<DP, 1> acc;
+                clear_held(acc);
+                const bool in[1][2] = {{true, true}};
+                for (int i = 0; i < left; ++i, ++step) {
+                    __syncwarp();                      // what the next loads overwrite has been read by all lanes
+                    load_step(step + 1);
+                    cp_wait<1>();
+                    __syncwarp();
+                    add_held_block<T, DP, HELD, 1>(acc, qs, smem_u32(own) + (step & 1) * S::STEP_BYTES, min(BLK, len - (begin + i) * BLK), in, lane);
+                }
+                finish_held(acc);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float* dst = o_sm + ((lane & 3) * 2 + e) * S::O_LD + (lane >> 2) * 2;
+                    const float f = acc.t[0][e] > -CUDART_INF_F && acc.m[0][e] > -CUDART_INF_F ? exp2f(acc.t[0][e] - acc.m[0][e] + held_shift<HELD>()) : 1.f;
+#pragma unroll
+                    for (int j = 0; j < DP / 16; ++j) *reinterpret_cast<float2*>(dst + 16 * j) = make_float2(acc.o[0][j][e] * f, acc.o[0][j][2 + e] * f);
+                    if (lane < 4) { ml_sm[2 * lane + e] = acc.m[0][e]; ml_sm[8 + 2 * lane + e] = acc.l[0][e]; }
+                }
+                __syncwarp();
+            }
+        } else if (left > 0) {
             // query fragments: head lane / 4, values 16 kk + 2 (lane % 4) and 8 further
             uint32_t qf[DP / 16][2];
             const bool some_head = (lane >> 2) < heads;
@@ -634,14 +761,15 @@ __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p
     }
 }
 
-template <typename T, int DP>
+template <typename T, int DP, int HELD>
 int launch_groups(const AttendParams& a, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const GroupParams& p, unsigned grid, cudaStream_t st) {
     static std::atomic<uint64_t> done{0}, done2{0}, done3{0};
-    constexpr int join_bytes = JT / 32 * JoinSmem<DP>::WARP_BYTES;
-    if (const int rc = allow_smem(attend_group_kernel<T, DP>, Shape<DP>::SMEM, done)) return rc;
-    if (const int rc = launch_after(attend_group_kernel<T, DP>, grid, THREADS, Shape<DP>::SMEM, st, q, k, v, p)) return rc;
-    if (const int rc = allow_smem(attend_join_kernel<T, DP, true>, join_bytes, done2)) return rc;
-    if (const int rc = allow_smem(attend_join_kernel<T, DP, false>, join_bytes, done3)) return rc;
+    using S = Shape<DP, HELD>;
+    constexpr int join_bytes = JT / 32 * JoinSmem<DP, HELD>::WARP_BYTES;
+    if (const int rc = allow_smem(attend_group_kernel<T, DP, HELD>, S::SMEM, done)) return rc;
+    if (const int rc = launch_after(attend_group_kernel<T, DP, HELD>, grid, S::THREADS, S::SMEM, st, q, k, v, p)) return rc;
+    if (const int rc = allow_smem(attend_join_kernel<T, DP, true, HELD>, join_bytes, done2)) return rc;
+    if (const int rc = allow_smem(attend_join_kernel<T, DP, false, HELD>, join_bytes, done3)) return rc;
     int sms = 0;
     if (const int rc = device_sms(&sms)) return rc;
     const int64_t places = int64_t(sms) * 3 * (JT / 32), units = int64_t(a.rows) * a.kv_heads;
@@ -651,7 +779,13 @@ int launch_groups(const AttendParams& a, const CUtensorMap& q, const CUtensorMap
     const int heads_per_job = units >= 2 * places && a.kv_heads > 1 ? 2 : 1;
     const int64_t jobs = int64_t(a.rows) * ((a.kv_heads + heads_per_job - 1) / heads_per_job);
     const unsigned join_grid = unsigned((jobs + JT / 32 - 1) / (JT / 32));
-    return launch_after(a.D == DP ? attend_join_kernel<T, DP, true> : attend_join_kernel<T, DP, false>, join_grid, JT, join_bytes, st, a, heads_per_job);
+    return launch_after(a.D == DP ? attend_join_kernel<T, DP, true, HELD> : attend_join_kernel<T, DP, false, HELD>, join_grid, JT, join_bytes, st, a, heads_per_job);
+}
+
+template <typename T>
+int launch_held(const AttendParams& a, const CUtensorMap& q, const GroupParams& p, int DP, int held, unsigned grid, cudaStream_t st) {
+    if (held == HELD_E4M3) return DP == 64 ? launch_groups<T, 64, HELD_E4M3>(a, q, q, q, p, grid, st) : launch_groups<T, 128, HELD_E4M3>(a, q, q, q, p, grid, st);
+    return DP == 64 ? launch_groups<T, 64, HELD_I8>(a, q, q, q, p, grid, st) : launch_groups<T, 128, HELD_I8>(a, q, q, q, p, grid, st);
 }
 
 int encode(EncodeTiled enc, CUtensorMap* map, CUtensorMapDataType type, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides,
@@ -670,9 +804,11 @@ int disc::plan_groups(const PlanParams& p, cudaStream_t st) {
 }
 
 int disc::attend_groups(const AttendParams& a, int32_t dtype, int32_t n_q_heads, cudaStream_t st) {
-    if (dtype >> 4) return DISC_ERR_UNSUPPORTED;
+    const int held = dtype >> 4;
+    dtype &= 15;
     GroupParams p;
     p.plan = a.plan; p.table = a.table; p.width = a.width; p.kv_heads = a.kv_heads; p.G = a.shape.G; p.per_group = a.shape.per_group;
+    p.k = a.k; p.v = a.v; p.pages = a.pages; p.head_bytes = a.head_bytes;
     p.D = a.D; p.page_size = a.page_size; p.blks_per_page = a.shape.blks_per_page; p.c2 = a.c2; p.error = a.error;
     const int DP = a.D <= 64 ? 64 : 128;
     // instruction descriptors: D fp32 (bits 4-5 = 1), A and B f16 = 0 / bf16 = 1 (bits 7-9, 10-12), B of the second
@@ -689,13 +825,17 @@ int disc::attend_groups(const AttendParams& a, int32_t dtype, int32_t n_q_heads,
     const cuuint64_t q_dims[3] = {cuuint64_t(a.D), cuuint64_t(n_q_heads), cuuint64_t(a.rows)}, q_strides[2] = {cuuint64_t(a.q_head), cuuint64_t(a.q_row)};
     const cuuint32_t q_box[3] = {cuuint32_t(BOX), cuuint32_t(p.G), cuuint32_t(p.per_group)};
     if (const int rc = encode(enc, &map_q, type, 3, a.q, q_dims, q_strides, q_box)) return rc;
+    const unsigned grid = unsigned(a.shape.lanes * a.kv_heads);
+    if (held) {
+        // no maps of the planes: codes and exponents come in as runs of bytes
+        return dtype == DISC_BF16 ? launch_held<__nv_bfloat16>(a, map_q, p, DP, held, grid, st) : launch_held<__half>(a, map_q, p, DP, held, grid, st);
+    }
     // a plane as [pages x heads x page size][D]
     const cuuint64_t dims[2] = {cuuint64_t(a.D), cuuint64_t(a.pages) * a.kv_heads * a.page_size}, strides[1] = {cuuint64_t(a.D) * 2};
     const cuuint32_t box[2] = {cuuint32_t(BOX), cuuint32_t(BLK)};
     if (const int rc = encode(enc, &map_k, type, 2, a.k, dims, strides, box)) return rc;
     if (const int rc = encode(enc, &map_v, type, 2, a.v, dims, strides, box)) return rc;
-    const unsigned grid = unsigned(a.shape.lanes * a.kv_heads);
     if (dtype == DISC_BF16)
-        return DP == 64 ? launch_groups<__nv_bfloat16, 64>(a, map_q, map_k, map_v, p, grid, st) : launch_groups<__nv_bfloat16, 128>(a, map_q, map_k, map_v, p, grid, st);
-    return DP == 64 ? launch_groups<__half, 64>(a, map_q, map_k, map_v, p, grid, st) : launch_groups<__half, 128>(a, map_q, map_k, map_v, p, grid, st);
+        return DP == 64 ? launch_groups<__nv_bfloat16, 64, HELD_PLAIN>(a, map_q, map_k, map_v, p, grid, st) : launch_groups<__nv_bfloat16, 128, HELD_PLAIN>(a, map_q, map_k, map_v, p, grid, st);
+    return DP == 64 ? launch_groups<__half, 64, HELD_PLAIN>(a, map_q, map_k, map_v, p, grid, st) : launch_groups<__half, 128, HELD_PLAIN>(a, map_q, map_k, map_v, p, grid, st);
 }

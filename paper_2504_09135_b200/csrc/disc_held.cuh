@@ -59,8 +59,8 @@ __device__ __forceinline__ void codes4(uint32_t c, float* x) {
 }
 __device__ __forceinline__ float exponent_scale(int e) { return e == NAN_EXP ? CUDART_NAN_F : pow2f(max(e, MIN_EXP)); }
 
-template <typename T> __device__ __forceinline__ constexpr bool is_half() { return false; }
-template <> __device__ __forceinline__ constexpr bool is_half<__half>() { return true; }
+template <typename T> __host__ __device__ constexpr bool is_half() { return false; }
+template <> __host__ __device__ constexpr bool is_half<__half>() { return true; }
 
 // the largest finite value of a type, beyond which held values are cut off when they are given back in it (an e4m3 code can
 // round the largest 4 % of a type's range up to the next power of two)
@@ -84,6 +84,62 @@ __device__ __forceinline__ void values16(const uint4& c, float scale, uint32_t* 
         }
         out[2 * i] = pack2<T>(x[0], x[1]);
         out[2 * i + 1] = pack2<T>(x[2], x[3]);
+    }
+}
+
+// The same by 16-bit arithmetic, two values at a time: an e4m3 code's exponent and mantissa, moved to a bf16's or f16's places, stand
+// for 2^-120 or 2^-8 of its value, denormal codes included; an i8 code is the f16 1152 + code, less 1152, or as a bf16 its lower seven bits
+// on 128, less 128 or, with its top bit, 256.  Then one exact product with the power of two, while that product and its factor are
+// normal values of the type; the rest goes through fp32.
+template <typename T, int HELD>
+struct FastScale {
+    static constexpr int CODE = HELD == HELD_I8 ? 0 : is_half<T>() ? 8 : 120;             // log2 of value / pattern
+    static constexpr int LOW = is_half<T>() ? -14 - CODE : MIN_EXP;
+    static constexpr int HIGH = is_half<T>() ? (HELD == HELD_I8 ? 9 : 7) : HELD == HELD_I8 ? 120 : 7;
+};
+template <typename T>
+__device__ __forceinline__ uint32_t mul16x2(uint32_t a, uint32_t b);
+template <>
+__device__ __forceinline__ uint32_t mul16x2<__nv_bfloat16>(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 c = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&c);
+}
+template <>
+__device__ __forceinline__ uint32_t mul16x2<__half>(uint32_t a, uint32_t b) {
+    const __half2 c = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&c);
+}
+template <typename T, int HELD>
+__device__ __forceinline__ uint32_t pattern2(uint32_t c, uint32_t pick) {
+    if (HELD == HELD_E4M3) {
+        constexpr int SHIFT = is_half<T>() ? 1 : 4;
+        const uint32_t w = __byte_perm(c, 0, pick & 0xf0f0u | 0x0404u);                   // the two codes as upper bytes
+        return (w & 0x80008000u) | ((w & 0x7f007f00u) >> SHIFT);
+    }
+    if (is_half<T>()) {
+        const uint32_t w = __byte_perm(c ^ 0x80808080u, 0x64646464u, pick >> 4 & 0x0f0fu | 0x4040u);
+        const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&w), __half2half2(__ushort_as_half(0x6480)));
+        return *reinterpret_cast<const uint32_t*>(&x);
+    }
+    const uint32_t w = __byte_perm(c, 0x43434343u, pick >> 4 & 0x0f0fu | 0x4040u), a = w & 0xff7fff7fu, b = w & 0xff80ff80u;
+    const __nv_bfloat162 x = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&x);
+}
+template <typename T, int HELD>
+__device__ __forceinline__ bool fast_scale(int e, uint32_t* scale2) {
+    using F = FastScale<T, HELD>;
+    const int x = max(F::LOW, min(F::HIGH, e)) + F::CODE;
+    const uint32_t one = is_half<T>() ? uint32_t(x + 15) << 10 : uint32_t(x + 127) << 7;
+    *scale2 = one | one << 16;
+    return e >= F::LOW && e <= F::HIGH;
+}
+template <typename T, int HELD>
+__device__ __forceinline__ void fast_values16(const uint4& c, uint32_t scale2, uint32_t* out) {
+    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        out[2 * i] = mul16x2<T>(pattern2<T, HELD>(w[i], 0x1000u), scale2);                // codes 0 and 1 of the word
+        out[2 * i + 1] = mul16x2<T>(pattern2<T, HELD>(w[i], 0x3020u), scale2);            // 2 and 3
     }
 }
 
