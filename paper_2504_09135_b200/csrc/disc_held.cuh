@@ -30,19 +30,19 @@ __device__ __forceinline__ int hold_exponent(uint32_t amax_bits, float* inv) {
     *inv = pow2f(-e);
     return e;
 }
-// four codes; x with NAN_EXP's inv = 0 may be anything
+// four codes; x with NAN_EXP's inv = 0 may be anything.  i8: added to 1.5 2^23, a value is rounded to a whole number, to the nearest, ties to
+// even, and its last byte is the code.
 template <int HELD>
-__device__ __forceinline__ uint32_t hold4(const float* x, float inv) {
+__device__ __forceinline__ uint32_t hold4(float2 a, float2 b, float inv) {
     if (inv == 0.f) return 0;
     if (HELD == HELD_E4M3) {
-        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(x[0] * inv, x[1] * inv), __NV_SATFINITE, __NV_E4M3);
-        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(x[2] * inv, x[3] * inv), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a.x * inv, a.y * inv), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(b.x * inv, b.y * inv), __NV_SATFINITE, __NV_E4M3);
         return lo | hi << 16;
     }
-    uint32_t c = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c |= (uint32_t(__float2int_rn(x[i] * inv)) & 255u) << (8 * i);
-    return c;
+    const float2 i2 = make_float2(inv, inv), magic = make_float2(12582912.f, 12582912.f);
+    const float2 x = fma2(a, i2, magic), y = fma2(b, i2, magic);
+    return __byte_perm(__byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x0040), __byte_perm(__float_as_uint(y.x), __float_as_uint(y.y), 0x0040), 0x5410);
 }
 
 // the values of four codes, without the power of two, in fp32

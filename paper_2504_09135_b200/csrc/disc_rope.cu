@@ -7,11 +7,17 @@
 //
 // Backward, with g = dy rotated by -t and c = w g:  dw = sum g x r,  dx = r c - x r^3 mean(c x).
 //
-// Bound by the bytes: every vector is read once and written once.  8 or 16 lanes hold a vector, 8 values each, so that a pair
-// that is rotated lies in one lane and the sum of squares is three or four shuffles; a warp has the vectors of one token, four
-// loads of each lane in flight.  The angles of a lane's four pairs are formed once for the token's vectors: position x
-// inv_freq / 2 pi in 64 bits, less its whole turns, so that a position of a million is as exact as one of ten (in 32 bits its
-// angle is off by 0.03), then sin and cos of a fraction of a turn in 32 bits.
+// Bound by the bytes: every vector is read once and written once, and what stands in the way are the instructions around them.  So a
+// lane holds 16 values of a vector, two runs of 8 that are rotated into one another (8 or 4 lanes a vector, 4 or 8 vectors side by side
+// in a warp; vectors that cannot be cut like that have runs of 4): loads and stores of 16 bytes, three or two shuffles for a sum of
+// squares.  A warp's vectors are all of one kind, queries, keys or values, and it goes from token to token, the next ones on their way
+// into a ring in shared memory, of which every lane fills and reads places of its own, while the present ones are worked on.  What a token's vectors have in common, weight times cosine and weight times sine, is formed once for
+// all of them: y = r (P x + Q x'), x' the other value of the pair.
+//
+// Angles: the fraction of a turn, position x inv_freq / 2 pi less its whole turns, is the product of two whole numbers modulo 2^64 (the
+// frequency as a 64-bit fraction of a turn, which wraps by itself), so that a position of a million is as exact as one of ten; an fp32
+// product would be off by 0.03 there.  Then sin and cos of that fraction in fp32, each pair's by one lane, and through shared memory to the lanes
+// that turn it.
 
 #include "disc_held.cuh"
 
@@ -21,8 +27,14 @@ using namespace disc;
 
 constexpr unsigned FULL = 0xffffffffu;
 constexpr int THREADS = 128;
-constexpr int AT_ONCE = 4;             // vectors of a lane in flight
-constexpr int MAX_BLOCKS = 148 * 8;    // of the gradient, whose blocks each leave sums of their own
+constexpr int WARPS = THREADS / 32;
+constexpr int DEPTH = 6;               // steps of a warp in flight, and the one it is at
+constexpr int GRAD_DEPTH = 4;
+constexpr int BLOCKS = 5;              // on an SM
+constexpr int GRAD_BLOCKS = 3;
+constexpr int SMS = 148;
+constexpr int MAX_GRAD_BLOCKS = SMS * GRAD_BLOCKS;     // which each leave sums of their own
+constexpr int MOST_TOKENS = 8;         // of a warp
 
 struct Vectors {                       // strides in bytes
     unsigned char* at;
@@ -32,6 +44,7 @@ struct RopeParams {
     Vectors x[3];                      // queries, keys; values, which are only written
     Vectors y[2];
     int32_t n, D, rot, interleaved, norm, weights_f32;
+    float inv_D;
     int32_t heads[3];
     const void* w[2];
     float eps;
@@ -50,69 +63,190 @@ struct CacheParams {
 };
 
 // Queries, keys or values: by selection, as an index into the parameters would put them on the stack.
-__device__ __forceinline__ Vectors pick(const Vectors* v, int which) { return which == 0 ? v[0] : which == 1 ? v[1] : v[2]; }
-__device__ __forceinline__ Vectors pick2(const Vectors* v, int which) { return which == 0 ? v[0] : v[1]; }
+__device__ __forceinline__ Vectors pick(const Vectors* v, int kind) { return kind == 0 ? v[0] : kind == 1 ? v[1] : v[2]; }
+__device__ __forceinline__ Vectors pick2(const Vectors* v, int kind) { return kind == 0 ? v[0] : v[1]; }
 
-// Where a lane's two runs of four values begin.  Rotated: the four pairs (a + i, b + i), or (a, a+1), (a+2, a+3), (b, b+1), (b+2, b+3).
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;"
+        : "=l"(reinterpret_cast<unsigned long long&>(d))
+        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
+    return d;
+}
+__device__ __forceinline__ float2 swapped(float2 a) { return make_float2(a.y, a.x); }
+
+// Where a lane's two runs of RUN values begin.  Rotated: the pairs (a + i, b + i), i < RUN, or, interleaved, neighbours in both.
 struct Place {
     int32_t a, b;
     bool some, turned;
 };
+template <int RUN>
 __device__ __forceinline__ Place place_of(const RopeParams& p, int c) {
     Place at;
-    at.some = c * 8 < p.D;
-    at.turned = c * 8 < p.rot;
+    at.some = c * 2 * RUN < p.D;
+    at.turned = c * 2 * RUN < p.rot;
     const bool split = at.turned && !p.interleaved;
-    at.a = split ? 4 * c : 8 * c;
-    at.b = split ? p.rot / 2 + 4 * c : 8 * c + 4;
+    at.a = split ? RUN * c : 2 * RUN * c;
+    at.b = split ? p.rot / 2 + RUN * c : 2 * RUN * c + RUN;
     return at;
 }
-__device__ __forceinline__ void angles(const RopeParams& p, int32_t pos, int c, float* cs, float* sn) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        double turns = double(pos) * (double(p.inv_freq[4 * c + i]) * 0.15915494309189533577);
-        turns -= rint(turns);
-        sincospif(2.f * float(turns), sn + i, cs + i);
+// A lane's values: 16-bit words as they lie in memory, or pairs of neighbours in fp32, run a, then run b.
+template <int RUN>
+struct Raw {
+    uint32_t w[RUN];
+};
+template <int RUN>
+__device__ __forceinline__ Raw<RUN> load_raw(const unsigned char* a_run, const unsigned char* b_run) {
+    Raw<RUN> r;
+    if constexpr (RUN == 8) {
+        const uint4 a = *reinterpret_cast<const uint4*>(a_run), b = *reinterpret_cast<const uint4*>(b_run);
+        r.w[0] = a.x; r.w[1] = a.y; r.w[2] = a.z; r.w[3] = a.w; r.w[4] = b.x; r.w[5] = b.y; r.w[6] = b.z; r.w[7] = b.w;
+    } else {
+        const uint2 a = *reinterpret_cast<const uint2*>(a_run), b = *reinterpret_cast<const uint2*>(b_run);
+        r.w[0] = a.x; r.w[1] = a.y; r.w[2] = b.x; r.w[3] = b.y;
+    }
+    return r;
+}
+// a lane's two runs of a vector into its places of a step in shared memory; zeros when !some
+template <int RUN>
+__host__ __device__ constexpr int step_bytes() { return 32 * RUN * 4; }
+template <int RUN>
+__device__ __forceinline__ void copy_in(uint32_t step, const unsigned char* v, const Place& at, bool some, int lane) {
+    const uint32_t to = step + lane * (RUN * 2);
+    const int n = some ? RUN * 2 : 0;
+    const unsigned char *a = v + at.a * 2, *b = v + at.b * 2;
+    if constexpr (RUN == 8) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(a), "r"(n) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + 32 * 16), "l"(b), "r"(n) : "memory");
+    } else {
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(to), "l"(a), "r"(n) : "memory");
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(to + 32 * 8), "l"(b), "r"(n) : "memory");
     }
 }
-// by the angles, or back with sign = -1
-__device__ __forceinline__ void turn(float* x, const float* cs, const float* sn, bool interleaved, float sign) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float s = sign * sn[i];
-        float* a = interleaved ? x + 2 * i : x + i;
-        float* b = interleaved ? x + 2 * i + 1 : x + 4 + i;
-        const float u = *a, v = *b;
-        *a = u * cs[i] - v * s;
-        *b = v * cs[i] + u * s;
+__device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void wait_for_all_but() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+template <int RUN>
+__device__ __forceinline__ void store_raw(unsigned char* v, const Place& at, const Raw<RUN>& r) {
+    if constexpr (RUN == 8) {
+        *reinterpret_cast<uint4*>(v + at.a * 2) = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
+        *reinterpret_cast<uint4*>(v + at.b * 2) = make_uint4(r.w[4], r.w[5], r.w[6], r.w[7]);
+    } else {
+        *reinterpret_cast<uint2*>(v + at.a * 2) = make_uint2(r.w[0], r.w[1]);
+        *reinterpret_cast<uint2*>(v + at.b * 2) = make_uint2(r.w[2], r.w[3]);
     }
 }
-template <typename T>
-__device__ __forceinline__ void load8(const unsigned char* v, const Place& at, float* x) {
-    const uint2 a = at.some ? *reinterpret_cast<const uint2*>(v + at.a * 2) : make_uint2(0, 0), b = at.some ? *reinterpret_cast<const uint2*>(v + at.b * 2) : make_uint2(0, 0);
-    const float2 f[4] = {unpack2<T>(a.x), unpack2<T>(a.y), unpack2<T>(b.x), unpack2<T>(b.y)};
+template <typename T, int RUN>
+__device__ __forceinline__ void unpack(const Raw<RUN>& r, float2* x) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { x[2 * i] = f[i].x; x[2 * i + 1] = f[i].y; }
+    for (int i = 0; i < RUN; ++i) x[i] = unpack2<T>(r.w[i]);
 }
-template <typename T>
-__device__ __forceinline__ void store8(unsigned char* v, const Place& at, const float* x) {
-    if (!at.some) return;
-    *reinterpret_cast<uint2*>(v + at.a * 2) = make_uint2(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]));
-    *reinterpret_cast<uint2*>(v + at.b * 2) = make_uint2(pack2<T>(x[4], x[5]), pack2<T>(x[6], x[7]));
-}
-template <typename T>
-__device__ __forceinline__ void load_weights(const RopeParams& p, int which, const Place& at, float* w) {
+template <typename T, int RUN>
+__device__ __forceinline__ Raw<RUN> pack(const float2* x) {
+    Raw<RUN> r;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = 1.f;
-    const void* from = which ? p.w[1] : p.w[0];
+    for (int i = 0; i < RUN; ++i) r.w[i] = pack2<T>(x[i].x, x[i].y);
+    return r;
+}
+template <typename T, int RUN>
+__device__ __forceinline__ void load_weights(const RopeParams& p, int kind, const Place& at, float2* w) {
+#pragma unroll
+    for (int i = 0; i < RUN; ++i) w[i] = make_float2(1.f, 1.f);
+    const void* from = kind ? p.w[1] : p.w[0];
     if (!from || !at.some) return;
     if (p.weights_f32) {
         const float* f = static_cast<const float*>(from);
-        const float4 a = *reinterpret_cast<const float4*>(f + at.a), b = *reinterpret_cast<const float4*>(f + at.b);
-        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
-        w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+#pragma unroll
+        for (int i = 0; i < RUN; i += 2) {
+            const float4 v = *reinterpret_cast<const float4*>(f + (i < RUN / 2 ? at.a + 2 * i : at.b + 2 * i - RUN));
+            w[i] = make_float2(v.x, v.y);
+            w[i + 1] = make_float2(v.z, v.w);
+        }
     } else {
-        load8<T>(static_cast<const unsigned char*>(from), at, w);
+        const unsigned char* v = static_cast<const unsigned char*>(from);
+        unpack<T, RUN>(load_raw<RUN>(v + at.a * 2, v + at.b * 2), w);
+    }
+}
+
+// Cosines and sines of a warp's token: each of the rot / 2 <= 64 pairs by one lane, through shared memory.
+struct Turns {
+    float c[64], s[64];
+};
+struct Frequencies {
+    uint64_t f[2];                     // of pairs lane and lane + 32, as 64-bit fractions of a turn
+};
+__device__ __forceinline__ Frequencies frequencies_of(const RopeParams& p, int lane) {
+    Frequencies q;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        q.f[i] = 0;
+        if (2 * (lane + 32 * i) >= p.rot) continue;
+        const double turns = double(p.inv_freq[lane + 32 * i]) * 0.15915494309189533577;          // 1 / 2 pi
+        q.f[i] = uint64_t((turns - floor(turns)) * 18446744073709551616.0);
+    }
+    return q;
+}
+__device__ __forceinline__ void turn_to(const RopeParams& p, int32_t pos, const Frequencies& q, Turns& out, int lane) {
+    __syncwarp();                      // the token before has been read by all lanes
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (64 * i >= p.rot) break;
+        const int32_t part = int32_t(uint32_t((uint64_t(int64_t(pos)) * q.f[i]) >> 32));          // of 2^32, from -1/2 to 1/2 of a turn
+        float s, c;
+        sincospif(float(part) * 0x1p-31f, &s, &c);
+        out.c[lane + 32 * i] = c;
+        out.s[lane + 32 * i] = s;
+    }
+    __syncwarp();
+}
+// the lane's RUN pairs
+template <int RUN>
+__device__ __forceinline__ void read_turns(const Turns& t, int c, float* cs, float* sn) {
+#pragma unroll
+    for (int i = 0; i < RUN; i += 4) {
+        const float4 a = *reinterpret_cast<const float4*>(t.c + RUN * c + i), b = *reinterpret_cast<const float4*>(t.s + RUN * c + i);
+        cs[i] = a.x; cs[i + 1] = a.y; cs[i + 2] = a.z; cs[i + 3] = a.w;
+        sn[i] = b.x; sn[i + 1] = b.y; sn[i + 2] = b.z; sn[i + 3] = b.w;
+    }
+}
+// y_i = x_i P_i + x'_i Q_i, x' the pairs' other values: of the other run, or, interleaved, the neighbours
+template <int RUN>
+__device__ __forceinline__ void turn(float2* x, const float2* P, const float2* Q, bool interleaved) {
+    if (interleaved) {
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) x[i] = fma2(x[i], P[i], mul2(swapped(x[i]), Q[i]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < RUN / 2; ++i) {
+            const float2 u = x[i], v = x[i + RUN / 2];
+            x[i] = fma2(u, P[i], mul2(v, Q[i]));
+            x[i + RUN / 2] = fma2(v, P[i + RUN / 2], mul2(u, Q[i + RUN / 2]));
+        }
+    }
+}
+// P and Q for weights w: forward, sign 1: y_a = w_a x_a c - w_b x_b s, y_b = w_b x_b c + w_a x_a s; back, sign -1
+template <int RUN>
+__device__ __forceinline__ void coefficients(const Turns& t, int c, const float2* w, bool interleaved, float sign, float2* P, float2* Q) {
+    float cs[RUN], sn[RUN];
+    read_turns<RUN>(t, c, cs, sn);
+    if (interleaved) {
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) {
+            const float s = sign * sn[i];
+            P[i] = make_float2(w[i].x * cs[i], w[i].y * cs[i]);
+            Q[i] = make_float2(-w[i].y * s, w[i].x * s);
+        }
+    } else {
+        constexpr int H = RUN / 2;
+#pragma unroll
+        for (int i = 0; i < H; ++i) {
+            const float2 cc = make_float2(cs[2 * i], cs[2 * i + 1]), ss = make_float2(sign * sn[2 * i], sign * sn[2 * i + 1]);
+            P[i] = mul2(w[i], cc);
+            P[i + H] = mul2(w[i + H], cc);
+            Q[i] = mul2(w[i + H], make_float2(-ss.x, -ss.y));
+            Q[i + H] = mul2(w[i], ss);
+        }
     }
 }
 template <int LPV>
@@ -121,238 +255,402 @@ __device__ __forceinline__ float sum_of(float x) {
     for (int o = 1; o < LPV; o <<= 1) x += __shfl_xor_sync(FULL, x, o);
     return x;
 }
-template <int LPV>
-__device__ __forceinline__ float inverse_norm(const RopeParams& p, const float* x) {
-    float s = 0.f;
+template <int LPV, int RUN>
+__device__ __forceinline__ float inverse_norm(const RopeParams& p, const float2* x) {
+    float2 s = mul2(x[0], x[0]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], s);
-    return rsqrtf(sum_of<LPV>(s) / float(p.D) + p.eps);
+    for (int i = 1; i < RUN; ++i) s = fma2(x[i], x[i], s);
+    return rsqrtf(fmaf(sum_of<LPV>(s.x + s.y), p.inv_D, p.eps));
 }
 
-// the last i with cu[i] <= t, for cu[0] <= t < cu[n]; by a whole warp, 32 places at a time
-__device__ __forceinline__ int32_t sequence_of(const int32_t* cu, int32_t n, int32_t t, int lane) {
-    int32_t lo = 0, hi = n;
-    while (hi - lo > 1) {
-        const int32_t step = int32_t((uint32_t(hi - lo) + 31) / 32);
-        const int64_t at = lo + int64_t(lane + 1) * step;
-        const unsigned before = __ballot_sync(FULL, at < hi && cu[min(at, int64_t(n))] <= t);
-        lo += __popc(before) * step;
-        hi = hi - lo > step ? lo + step : hi;
+// The page of a token and its place in it (page -1: it is not written), and its position.  A lane per token.
+struct Spot {
+    int32_t page, off, pos;
+};
+__device__ __forceinline__ Spot spot_of(const CacheParams& w, int32_t t) {
+    Spot at = {-1, 0, 0};
+    int32_t seq = t, back = 1;                         // the token is the back-th from the end of its sequence
+    if (w.cu) {
+        if (t < w.cu[0] || t >= w.cu[w.n_seqs]) return at;
+        int32_t lo = 0, hi = w.n_seqs;                 // cu[lo] <= t < cu[hi]
+        while (hi - lo > 1) {
+            const int32_t m = lo + (hi - lo) / 2;
+            if (w.cu[m] <= t) lo = m; else hi = m;
+        }
+        seq = lo;
+        back = w.cu[lo + 1] - t;
     }
-    return lo;
+    const int32_t row = w.seq_rows ? w.seq_rows[seq] : seq;
+    if (row < 0 || row >= w.rows) return at;
+    const int32_t place = w.len[row] - back;
+    at.pos = max(place, 0);
+    if (place < 0 || (place >> w.shift) >= w.width || (w.status && w.status[row])) return at;
+    at.page = w.table[size_t(row) * w.width + (place >> w.shift)];
+    at.off = place & (w.page_size - 1);
+    if (at.page >= w.pages) at.page = -1;
+    return at;
 }
 
-// A warp per token and LOADS x 32 / LPV of its vectors: queries, then keys, then (with a cache) values.
-template <typename T, int LPV, bool CACHE>
-__global__ void __launch_bounds__(THREADS) norm_rope_kernel(const RopeParams p, const CacheParams w, int chunks) {
+// How the vectors are dealt out: warp `id` has `per` steps (of SIDE vectors each) of one kind of `tokens` tokens.
+struct Cut {
+    int64_t end[3];                    // warps up to the last of queries, keys, values
+    int32_t per[3], chunks[3], tokens;
+};
+struct Share {
+    int kind, h0, h1;                  // vectors h0 .. h1-1 of it
+    int32_t t0, t1;
+};
+__device__ __forceinline__ bool share_of(const Cut& cut, const RopeParams& p, int64_t id, int side_by_side, Share* s) {
+    const int kind = id < cut.end[0] ? 0 : id < cut.end[1] ? 1 : 2;
+    if (id >= cut.end[2]) return false;
+    id -= kind == 0 ? 0 : kind == 1 ? cut.end[0] : cut.end[1];
+    const int chunks = kind == 0 ? cut.chunks[0] : kind == 1 ? cut.chunks[1] : cut.chunks[2];
+    const int per = (kind == 0 ? cut.per[0] : kind == 1 ? cut.per[1] : cut.per[2]) * side_by_side;
+    s->kind = kind;
+    s->t0 = int32_t(id / chunks * cut.tokens);
+    s->t1 = min(p.n, s->t0 + cut.tokens);
+    s->h0 = int(id % chunks) * per;
+    s->h1 = min(kind == 0 ? p.heads[0] : kind == 1 ? p.heads[1] : p.heads[2], s->h0 + per);
+    return true;
+}
+
+// HELD: -1 without a cache, else how it holds its vectors.  The largest |value| of a vector is found among the 16-bit patterns
+// themselves, two at a time: without their signs they are in order, and infinities and NaN come last.
+template <typename T, int LPV, int RUN, int HELD>
+__global__ void __launch_bounds__(THREADS, BLOCKS) norm_rope_kernel(const RopeParams p, const CacheParams w, const Cut cut) {
     let_later_in();
     wait_for_earlier();
+    constexpr int STEP = step_bytes<RUN>();
+    __shared__ __align__(16) unsigned char s_ring[WARPS][DEPTH * STEP];
+    __shared__ Turns s_turns[WARPS];
     constexpr int SIDE = 32 / LPV;     // vectors side by side
-    const int lane = threadIdx.x & 31, c = lane % LPV;
-    const int64_t id = int64_t(blockIdx.x) * (THREADS / 32) + (threadIdx.x >> 5);
-    const int32_t t = int32_t(id / chunks);
-    if (t >= p.n) return;
-    const int first = int(id % chunks) * (AT_ONCE * SIDE) + lane / LPV;
-    const int hq = p.heads[0], hk = hq + p.heads[1], all = CACHE ? hk + p.heads[2] : hk;
-    const Place at = place_of(p, c);
+    constexpr bool CACHE = HELD >= 0;
+    const int lane = threadIdx.x & 31, c = lane % LPV, side = lane / LPV;
+    Turns& turns = s_turns[threadIdx.x >> 5];
+    Share sh;
+    if (!share_of(cut, p, int64_t(blockIdx.x) * WARPS + (threadIdx.x >> 5), SIDE, &sh)) return;
+    const int kind = sh.kind;
+    const Place at = place_of<RUN>(p, c);
+    const bool rotated = p.rot > 0 && kind < 2, normed = p.norm && kind < 2;
+    const int steps = (sh.h1 - sh.h0 + SIDE - 1) / SIDE;           // of a token
 
-    float x[AT_ONCE][8];
+    // loads, DEPTH - 1 steps ahead
+    unsigned char* ring = s_ring[threadIdx.x >> 5];
+    const uint32_t ring_at = smem_u32(ring);
+    const Vectors src = CACHE ? pick(p.x, kind) : pick2(p.x, kind);
+    const unsigned char* in = src.at + sh.t0 * src.token + (sh.h0 + side) * src.head;
+    const int64_t in_step = SIDE * src.head, in_token = src.token - steps * in_step;
+    int in_h = sh.h0 + side, left = (sh.t1 - sh.t0) * steps;       // steps not yet asked for
+    uint32_t in_at = 0, at_step = 0;   // places in the ring
+    auto fetch = [&]() {
+        if (left > 0) {
+            // for lanes without a vector any address will do: nothing is read
+            const bool some = at.some && in_h < sh.h1;
+            copy_in<RUN>(ring_at + in_at, some ? in : src.at, at, some, lane);
+            --left;
+            in += in_step;
+            in_h += SIDE;
+            if (in_h - side >= sh.h1) {
+                in += in_token;
+                in_h = sh.h0 + side;
+            }
+        }
+        commit();
+        in_at = in_at == (DEPTH - 1) * STEP ? 0 : in_at + STEP;
+    };
 #pragma unroll
-    for (int i = 0; i < AT_ONCE; ++i) {
-        const int h = first + i * SIDE, which = h < hq ? 0 : h < hk ? 1 : 2;
-        const Vectors v = CACHE ? pick(p.x, which) : pick2(p.x, which);
-        Place here = at;
-        here.some = at.some && h < all;
-        load8<T>(v.at + t * v.token + (h - (which == 0 ? 0 : which == 1 ? hq : hk)) * v.head, here, x[i]);
+    for (int i = 0; i < DEPTH - 1; ++i) fetch();
+
+    Spot spots = {-1, 0, 0};           // of token t0 + lane
+    if (sh.t0 + lane < sh.t1) {
+        if (CACHE) spots = spot_of(w, sh.t0 + lane);
+        if (rotated && p.pos) spots.pos = p.pos[sh.t0 + lane];
     }
+    Frequencies freq;
+    if (rotated) freq = frequencies_of(p, lane);
 
-    int32_t pos = 0, page = -1, off = 0;
-    if (CACHE) {
-        int32_t seq = t, back = 1;                     // the token is the back-th from the end of its sequence
-        bool some = true;
-        if (w.cu) {
-            some = t >= w.cu[0] && t < w.cu[w.n_seqs];
-            if (some) {
-                seq = sequence_of(w.cu, w.n_seqs, t, lane);
-                back = w.cu[seq + 1] - t;
-            }
-        }
-        const int32_t row = !some ? -1 : w.seq_rows ? w.seq_rows[seq] : seq;
-        if (row >= 0 && row < w.rows) {
-            const int32_t place = w.len[row] - back;
-            pos = max(place, 0);
-            if (place >= 0 && !(w.status && w.status[row])) {
-                page = w.table[size_t(row) * w.width + (place >> w.shift)];
-                off = place & (w.page_size - 1);
-                if (page >= w.pages) page = -1;
-            }
-        }
-    }
-    if (!CACHE || p.pos) pos = p.pos ? p.pos[t] : 0;
-    float cs[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};
-    if (at.turned) angles(p, pos, c, cs, sn);
-
+    float2 P[RUN], Q[RUN];
+    const bool to_cache = CACHE && kind > 0;
+    const Vectors dst = CACHE ? p.y[0] : pick2(p.y, kind);
+    const int64_t out_step = to_cache ? int64_t(SIDE) * w.head_bytes : SIDE * dst.head;
+    unsigned char* out = nullptr;
+    int32_t off = 0, page = -1;
+    int h = sh.h1 + side;              // at a token's end: the next begins
+    int32_t t = sh.t0 - 1;
+    for (int todo = (sh.t1 - sh.t0) * steps; todo > 0; --todo) {
+        {
+            if (h - side >= sh.h1) {
+                ++t;
+                h = sh.h0 + side;
+                const int from = t - sh.t0;
+                if (to_cache) {
+                    page = __shfl_sync(FULL, spots.page, from);
+                    off = __shfl_sync(FULL, spots.off, from);
+                    out = (kind == 2 ? w.plane[1] : w.plane[0]) + (int64_t(max(page, 0)) * p.heads[1] + h) * w.head_bytes;
+                } else {
+                    out = dst.at + t * dst.token + h * dst.head;
+                }
+                if (rotated) turn_to(p, __shfl_sync(FULL, spots.pos, from), freq, turns, lane);
+                // what the weights and the angles come to, where they change
+                if (rotated || (normed && t == sh.t0)) {
+                    float2 f[RUN];
+                    load_weights<T, RUN>(p, kind, at, f);
+                    if (at.turned) {
+                        coefficients<RUN>(turns, c, f, p.interleaved, 1.f, P, Q);
+                    } else {
 #pragma unroll
-    for (int i = 0; i < AT_ONCE; ++i) {
-        const int h = first + i * SIDE, which = h < hq ? 0 : h < hk ? 1 : 2;
-        if (__all_sync(FULL, h >= all)) break;
-        if (p.norm) {
-            const float r = inverse_norm<LPV>(p, x[i]);
-            float f[8];
-            if (which < 2) {
-                load_weights<T>(p, which, at, f);
+                        for (int j = 0; j < RUN; ++j) P[j] = f[j];
+                    }
+                }
+            }
+            wait_for_all_but<DEPTH - 2>();
+            Raw<RUN> y = load_raw<RUN>(ring + at_step + lane * (RUN * 2), ring + at_step + (32 + lane) * (RUN * 2));
+            at_step = at_step == (DEPTH - 1) * STEP ? 0 : at_step + STEP;
+            fetch();
+            if (normed || rotated) {
+                float2 x[RUN];
+                unpack<T, RUN>(y, x);
+                if (normed) {
+                    const float r = inverse_norm<LPV, RUN>(p, x);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) x[i][j] = x[i][j] * r * f[j];
-            }
-        }
-        if (at.turned && which < 2) {
-            if (p.interleaved) turn(x[i], cs, sn, true, 1.f); else turn(x[i], cs, sn, false, 1.f);
-        }
-        const int head = h - (which == 0 ? 0 : which == 1 ? hq : hk);
-        if (!CACHE || which == 0) {
-            const Vectors v = CACHE ? p.y[0] : pick2(p.y, which);
-            if (h < all) store8<T>(v.at + t * v.token + head * v.head, at, x[i]);
-        }
-        if (CACHE) {
-            // by all lanes, also those whose vector is a query: the maximum is formed by shuffles
-            const bool to_page = which > 0 && h < all && page >= 0;
-            unsigned char* to = (which == 2 ? w.plane[1] : w.plane[0]) + (int64_t(max(page, 0)) * p.heads[1] + head) * w.head_bytes;
-            if (w.held == HELD_PLAIN) {
-                if (to_page) store8<T>(to + int64_t(off) * w.token_bytes, at, x[i]);
-                continue;
-            }
-            // what is held is a vector of the type T
-            uint32_t amax = 0;
+                    for (int j = 0; j < RUN; ++j) x[j] = mul2(x[j], make_float2(r, r));
+                }
+                if (at.turned && rotated) {
+                    turn<RUN>(x, P, Q, p.interleaved);
+                } else if (normed) {
 #pragma unroll
-            for (int j = 0; j < 8; j += 2) {
-                const float2 r = unpack2<T>(pack2<T>(x[i][j], x[i][j + 1]));
-                x[i][j] = r.x;
-                x[i][j + 1] = r.y;
-                amax = max(amax, max(__float_as_uint(r.x) & 0x7fffffffu, __float_as_uint(r.y) & 0x7fffffffu));
+                    for (int j = 0; j < RUN; ++j) x[j] = mul2(x[j], P[j]);
+                }
+                y = pack<T, RUN>(x);
             }
+            const bool real = h < sh.h1 && at.some;
+            if (!to_cache) {
+                if (real) store_raw<RUN>(out, at, y);
+            } else if (HELD <= HELD_PLAIN) {
+                if (real && page >= 0) store_raw<RUN>(out + off * w.token_bytes, at, y);
+            } else {
+                // what is held is a vector of the type T
+                constexpr uint32_t ABS = 0x7fff7fffu;
+                uint32_t top = y.w[0] & ABS;
 #pragma unroll
-            for (int o = 1; o < LPV; o <<= 1) amax = max(amax, __shfl_xor_sync(FULL, amax, o));
-            float inv;
-            const int e = w.held == HELD_E4M3 ? hold_exponent<HELD_E4M3>(amax, &inv) : hold_exponent<HELD_I8>(amax, &inv);
-            const uint32_t lo = w.held == HELD_E4M3 ? hold4<HELD_E4M3>(x[i], inv) : hold4<HELD_I8>(x[i], inv);
-            const uint32_t hi = w.held == HELD_E4M3 ? hold4<HELD_E4M3>(x[i] + 4, inv) : hold4<HELD_I8>(x[i] + 4, inv);
-            if (to_page && at.some) {
-                *reinterpret_cast<uint32_t*>(to + off * p.D + at.a) = lo;
-                *reinterpret_cast<uint32_t*>(to + off * p.D + at.b) = hi;
-                if (c == 0) to[w.page_size * p.D + off] = uint8_t(e);
+                for (int j = 1; j < RUN; ++j) top = __vmaxu2(top, y.w[j] & ABS);
+#pragma unroll
+                for (int o = 1; o < LPV; o <<= 1) top = __vmaxu2(top, __shfl_xor_sync(FULL, top, o));
+                const float2 tops = unpack2<T>(top);
+                float inv;
+                const int e = hold_exponent<HELD>(max(__float_as_uint(tops.x), __float_as_uint(tops.y)), &inv);
+                float2 x[RUN];
+                unpack<T, RUN>(y, x);
+                uint32_t code[RUN / 2];
+#pragma unroll
+                for (int j = 0; j < RUN / 2; ++j) code[j] = hold4<HELD>(x[2 * j], x[2 * j + 1], inv);
+                if (real && page >= 0) {
+                    unsigned char* to = out + off * p.D;
+                    if constexpr (RUN == 8) {
+                        *reinterpret_cast<uint2*>(to + at.a) = make_uint2(code[0], code[1]);
+                        *reinterpret_cast<uint2*>(to + at.b) = make_uint2(code[2], code[3]);
+                    } else {
+                        *reinterpret_cast<uint32_t*>(to + at.a) = code[0];
+                        *reinterpret_cast<uint32_t*>(to + at.b) = code[1];
+                    }
+                    if (c == 0) out[w.page_size * p.D + off] = uint8_t(e);
+                }
             }
+            h += SIDE;
+            out += out_step;
         }
     }
 }
 
 // ---- gradient ------------------------------------------------------------------------------------------
-// x: the inputs, y: the gradient of the outputs, dx: contiguous.  Warps go through the tokens' vectors in a fixed order and keep the
-// weights' gradients of their lanes; a block leaves one sum for each weight in part[block][2][D].
-template <typename T, int LPV>
-__global__ void __launch_bounds__(THREADS) norm_rope_grad_kernel(const RopeParams p, unsigned char* dq, unsigned char* dk, float* part, int chunks) {
+// x: the inputs, y: the gradient of the outputs, dx: contiguous.  A block's warps work on one kind, go through its tokens' vectors in a
+// fixed order and keep the weights' gradients of their lanes; a block leaves one sum for each weight in part[block][D].
+template <typename T, int LPV, int RUN>
+__global__ void __launch_bounds__(THREADS, GRAD_BLOCKS) norm_rope_grad_kernel(const RopeParams p, unsigned char* dq, unsigned char* dk, float* part, int q_blocks,
+                                                                           const Cut cut) {
     let_later_in();
     wait_for_earlier();
-    constexpr int SIDE = 32 / LPV, WARPS = THREADS / 32, STEPS = 2;
-    __shared__ float sums[WARPS][2][128];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane % LPV;
-    const int hq = p.heads[0], all = hq + p.heads[1];
-    const Place at = place_of(p, c);
-    float acc[2][8];
+    constexpr int STEP = step_bytes<RUN>();
+    __shared__ __align__(16) unsigned char s_ring[WARPS][GRAD_DEPTH * 2 * STEP];
+    __shared__ Turns s_turns[WARPS];
+    __shared__ float sums[WARPS][128];
+    constexpr int SIDE = 32 / LPV;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane % LPV, side = lane / LPV;
+    Turns& turns = s_turns[warp];
+    const Place at = place_of<RUN>(p, c);
+    const int kind = int(blockIdx.x) < q_blocks ? 0 : 1, heads = kind ? p.heads[1] : p.heads[0];
+    const int chunks = kind ? cut.chunks[1] : cut.chunks[0], per = (kind ? cut.per[1] : cut.per[0]) * SIDE;
+    const int64_t items = int64_t(p.n) * chunks, stride = int64_t(kind ? gridDim.x - q_blocks : q_blocks) * WARPS;
+    const int64_t first = int64_t(kind ? blockIdx.x - q_blocks : blockIdx.x) * WARPS + warp;
+    const Vectors xs = pick2(p.x, kind), gs = pick2(p.y, kind);
+    const bool rotated = p.rot > 0;
+    Frequencies freq;
+    if (rotated) freq = frequencies_of(p, lane);
+    float2 f[RUN], acc[RUN];
+    load_weights<T, RUN>(p, kind, at, f);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) acc[0][j] = acc[1][j] = 0.f;
-    for (int64_t id = int64_t(blockIdx.x) * WARPS + warp; id < int64_t(p.n) * chunks; id += int64_t(gridDim.x) * WARPS) {
+    for (int j = 0; j < RUN; ++j) acc[j] = make_float2(0.f, 0.f);
+
+    // loads, GRAD_DEPTH - 1 steps ahead: vectors and gradients
+    unsigned char* ring = s_ring[warp];
+    const uint32_t ring_at = smem_u32(ring);
+    int64_t in_id = first;
+    const unsigned char *in_x = xs.at, *in_g = gs.at;
+    int in_h = 0, in_last = 0;
+    uint32_t in_at = 0, at_step = 0;
+    auto begin = [&]() {
+        in_last = 0;
+        if (in_id < items) {
+            const int32_t t = int32_t(in_id / chunks);
+            in_h = int(in_id % chunks) * per;
+            in_last = min(heads, in_h + per);
+            in_h += side;
+            in_x = xs.at + t * xs.token + in_h * xs.head;
+            in_g = gs.at + t * gs.token + in_h * gs.head;
+        }
+    };
+    auto fetch = [&]() {
+        if (in_last > 0) {             // by the whole warp
+            const bool some = at.some && in_h < in_last;
+            copy_in<RUN>(ring_at + in_at, some ? in_x : xs.at, at, some, lane);
+            copy_in<RUN>(ring_at + in_at + STEP, some ? in_g : gs.at, at, some, lane);
+            in_h += SIDE;
+            in_x += SIDE * xs.head;
+            in_g += SIDE * gs.head;
+            if (in_h - side >= in_last) {
+                in_id += stride;
+                begin();
+            }
+        }
+        commit();
+        in_at = in_at == (GRAD_DEPTH - 1) * 2 * STEP ? 0 : in_at + 2 * STEP;
+    };
+    begin();
+#pragma unroll
+    for (int i = 0; i < GRAD_DEPTH - 1; ++i) fetch();
+    for (int64_t id = first; id < items; id += stride) {
         const int32_t t = int32_t(id / chunks);
-        const int first = int(id % chunks) * (AT_ONCE * SIDE) + lane / LPV;
-        float cs[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};
-        if (at.turned) angles(p, p.pos ? p.pos[t] : 0, c, cs, sn);
+        const int h0 = int(id % chunks) * per, h1 = min(heads, h0 + per);
+        float2 P[RUN], Q[RUN];
+        if (rotated) {
+            turn_to(p, p.pos[t], freq, turns, lane);
+            if (at.turned) {
+                float2 one[RUN];
 #pragma unroll
-        for (int i0 = 0; i0 < AT_ONCE; i0 += STEPS) {
-            float x[STEPS][8], g[STEPS][8];
-#pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
-                const int h = first + (i0 + i) * SIDE, which = h < hq ? 0 : 1;
-                Place here = at;
-                here.some = at.some && h < all;
-                const Vectors xv = pick2(p.x, which), gv = pick2(p.y, which);
-                load8<T>(xv.at + t * xv.token + (h - which * hq) * xv.head, here, x[i]);
-                load8<T>(gv.at + t * gv.token + (h - which * hq) * gv.head, here, g[i]);
+                for (int j = 0; j < RUN; ++j) one[j] = make_float2(1.f, 1.f);
+                coefficients<RUN>(turns, c, one, p.interleaved, -1.f, P, Q);
             }
+        }
+        unsigned char* to = (kind ? dk : dq) + (int64_t(t) * heads + h0 + side) * p.D * 2;
+        for (int h = h0 + side; h - side < h1; h += SIDE, to += SIDE * p.D * 2) {
+            float2 x[RUN], g[RUN];
+            wait_for_all_but<GRAD_DEPTH - 2>();
+            const unsigned char* mine = ring + at_step + lane * (RUN * 2);
+            unpack<T, RUN>(load_raw<RUN>(mine, mine + 32 * RUN * 2), x);
+            unpack<T, RUN>(load_raw<RUN>(mine + STEP, mine + STEP + 32 * RUN * 2), g);
+            at_step = at_step == (GRAD_DEPTH - 1) * 2 * STEP ? 0 : at_step + 2 * STEP;
+            fetch();
+            if (rotated && at.turned) turn<RUN>(g, P, Q, p.interleaved);
+            if (p.norm) {
+                const float r = inverse_norm<LPV, RUN>(p, x);
+                // vectors that are not there are zeros, but 0 times an infinite r (eps = 0) is not
+                const float ra = h < h1 ? r : 0.f;
+                float2 dot = make_float2(0.f, 0.f);
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
-                const int h = first + (i0 + i) * SIDE, which = h < hq ? 0 : 1, head = h - which * hq;
-                if (at.turned) {
-                    if (p.interleaved) turn(g[i], cs, sn, true, -1.f); else turn(g[i], cs, sn, false, -1.f);
+                for (int j = 0; j < RUN; ++j) {
+                    const float2 gx = mul2(g[j], x[j]);
+                    acc[j] = fma2(gx, make_float2(ra, ra), acc[j]);
+                    dot = fma2(gx, f[j], dot);
+                    g[j] = mul2(g[j], f[j]);
                 }
-                if (p.norm) {
-                    const float r = inverse_norm<LPV>(p, x[i]);
-                    float f[8];
-                    load_weights<T>(p, which, at, f);
-                    float dot = 0.f;
+                const float m = -sum_of<LPV>(dot.x + dot.y) * p.inv_D * (r * r * r);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float dw = h < all ? g[i][j] * x[i][j] * r : 0.f;
-                        if (which == 0) acc[0][j] += dw; else acc[1][j] += dw;
-                        g[i][j] *= f[j];
-                        dot = fmaf(g[i][j], x[i][j], dot);
-                    }
-                    const float m = sum_of<LPV>(dot) / float(p.D) * (r * r * r);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) g[i][j] = r * g[i][j] - x[i][j] * m;
-                }
-                if (h < all) store8<T>((which ? dk : dq) + (int64_t(t) * (which ? p.heads[1] : hq) + head) * p.D * 2, at, g[i]);
+                for (int j = 0; j < RUN; ++j) g[j] = fma2(x[j], make_float2(m, m), mul2(g[j], make_float2(r, r)));
             }
+            if (h < h1 && at.some) store_raw<RUN>(to, at, pack<T, RUN>(g));
         }
     }
     if (!part) return;
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+    for (int j = 0; j < RUN; ++j) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-#pragma unroll
-            for (int o = LPV; o < 32; o <<= 1) acc[k][j] += __shfl_xor_sync(FULL, acc[k][j], o);
-            if (lane < LPV && at.some) sums[warp][k][j < 4 ? at.a + j : at.b + j - 4] = acc[k][j];
+        for (int o = LPV; o < 32; o <<= 1) {
+            acc[j].x += __shfl_xor_sync(FULL, acc[j].x, o);
+            acc[j].y += __shfl_xor_sync(FULL, acc[j].y, o);
         }
+        if (lane < LPV && at.some) {
+            const int d = j < RUN / 2 ? at.a + 2 * j : at.b + 2 * j - RUN;
+            sums[warp][d] = acc[j].x;
+            sums[warp][d + 1] = acc[j].y;
+        }
+    }
     __syncthreads();
-    for (int i = threadIdx.x; i < 2 * p.D; i += THREADS) {
-        const int k = i / p.D, d = i % p.D;
+    for (int d = threadIdx.x; d < p.D; d += THREADS) {
         float s = 0.f;
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) s += sums[w][k][d];
-        part[(int64_t(blockIdx.x) * 2 + k) * p.D + d] = s;
+        for (int w = 0; w < WARPS; ++w) s += sums[w][d];
+        part[int64_t(blockIdx.x) * p.D + d] = s;
     }
 }
 // the blocks' sums, in a fixed order: a block of threads per 32 weights, 32 runs of blocks side by side
-__global__ void __launch_bounds__(1024) weight_grad_kernel(const float* part, int blocks, int D, float* dqw, float* dkw) {
+__global__ void __launch_bounds__(1024) weight_grad_kernel(const float* part, int q_blocks, int blocks, int D, float* dqw, float* dkw) {
     let_later_in();
     wait_for_earlier();
     __shared__ float sums[32][33];
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, i = blockIdx.x * 32 + x;
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, groups = (D + 31) / 32, kind = blockIdx.x / groups, d = blockIdx.x % groups * 32 + x;
     float s = 0.f;
-    if (i < 2 * D)
-        for (int b = y; b < blocks; b += 32) s += part[int64_t(b) * 2 * D + i];
+    if (d < D)
+        for (int b = (kind ? q_blocks : 0) + y; b < (kind ? blocks : q_blocks); b += 32) s += part[int64_t(b) * D + d];
     sums[y][x] = s;
     __syncthreads();
-    if (y == 0 && i < 2 * D) {
+    if (y == 0 && d < D) {
         s = 0.f;
 #pragma unroll
         for (int r = 0; r < 32; ++r) s += sums[r][x];
-        float* to = i < D ? dqw : dkw;
-        if (to) to[i % D] = s;
+        float* to = kind ? dkw : dqw;
+        if (to) to[d] = s;
     }
 }
 
 // ---- launches ------------------------------------------------------------------------------------------
-int chunks_of(int vectors, int D) {
-    const int per = AT_ONCE * (D <= 64 ? 4 : 2);
-    return (vectors + per - 1) / per;
+// Runs of 8 values where both halves of what is rotated and the whole vector are made of them.
+bool long_runs(int32_t D, int32_t rot) { return D % 16 == 0 && rot % 16 == 0; }
+int side_by_side(int32_t D, int32_t rot) { return (D <= 64 ? 4 : 2) * (long_runs(D, rot) ? 2 : 1); }
+
+// A warp takes all of a token's vectors of a kind while that leaves as many warps as run at a time; with fewer tokens the vectors are
+// dealt out, two steps to a warp at least, and with many a warp takes several tokens.
+Cut cut_of(int64_t n, const int32_t* heads, int side, int64_t warps, int most_tokens) {
+    Cut cut = {};
+    int64_t end = 0, tokens = n / warps;
+    cut.tokens = int32_t(tokens < 1 ? 1 : tokens > most_tokens ? most_tokens : tokens);
+    for (int k = 0; k < 3; ++k) {
+        const int steps = (heads[k] + side - 1) / side;
+        int64_t chunks = n > 0 ? (warps + n - 1) / n : 1;
+        if (chunks > (steps + 1) / 2) chunks = (steps + 1) / 2;
+        cut.per[k] = chunks ? int32_t((steps + chunks - 1) / chunks) : 1;
+        cut.chunks[k] = (steps + cut.per[k] - 1) / cut.per[k];
+        end += (n + cut.tokens - 1) / cut.tokens * cut.chunks[k];
+        cut.end[k] = end;
+    }
+    return cut;
 }
-template <typename T, bool CACHE>
+
+template <typename T, int HELD>
 int launch(const RopeParams& p, const CacheParams& w, cudaStream_t st) {
-    const int chunks = chunks_of(p.heads[0] + p.heads[1] + (CACHE ? p.heads[2] : 0), p.D);
-    const int64_t blocks = (int64_t(p.n) * chunks + THREADS / 32 - 1) / (THREADS / 32);
+    const Cut cut = cut_of(p.n, p.heads, side_by_side(p.D, p.rot), SMS * BLOCKS * WARPS, MOST_TOKENS);
+    const int64_t blocks = (cut.end[2] + WARPS - 1) / WARPS;
     if (blocks >= (int64_t(1) << 31)) return DISC_ERR_UNSUPPORTED;
-    if (p.D <= 64) return launch_after(norm_rope_kernel<T, 8, CACHE>, unsigned(blocks), THREADS, 0, st, p, w, chunks);
-    return launch_after(norm_rope_kernel<T, 16, CACHE>, unsigned(blocks), THREADS, 0, st, p, w, chunks);
+    auto kernel = long_runs(p.D, p.rot) ? (p.D <= 64 ? norm_rope_kernel<T, 4, 8, HELD> : norm_rope_kernel<T, 8, 8, HELD>)
+                                        : (p.D <= 64 ? norm_rope_kernel<T, 8, 4, HELD> : norm_rope_kernel<T, 16, 4, HELD>);
+    return launch_after(kernel, unsigned(blocks), THREADS, 0, st, p, w, cut);
+}
+template <int HELD>
+int launch(int type, const RopeParams& p, const CacheParams& w, cudaStream_t st) {
+    return type == DISC_BF16 ? launch<__nv_bfloat16, HELD>(p, w, st) : launch<__half, HELD>(p, w, st);
+}
+int launch_cache(const disc_cache_t* c, const RopeParams& p, const CacheParams& w, cudaStream_t st) {
+    const int held = cache_held(c), type = cache_type(c);
+    return held == HELD_PLAIN ? launch<HELD_PLAIN>(type, p, w, st) : held == HELD_E4M3 ? launch<HELD_E4M3>(type, p, w, st) : launch<HELD_I8>(type, p, w, st);
 }
 
 bool misaligned(const void* x) { return (reinterpret_cast<uintptr_t>(x) & 15u) != 0; }
@@ -370,6 +668,7 @@ int check_how(const disc_rope_t* how, disc_dtype_t dtype, int32_t D, RopeParams*
     p->D = D; p->rot = how->rot; p->interleaved = how->interleaved != 0; p->norm = how->norm != 0;
     p->weights_f32 = how->weight_dtype == DISC_F32;
     p->w[0] = p->norm ? how->q_weight : nullptr; p->w[1] = p->norm ? how->k_weight : nullptr;
+    p->inv_D = 1.f / float(D);
     p->eps = how->eps; p->inv_freq = how->inv_freq;
     return DISC_OK;
 }
@@ -396,9 +695,27 @@ void cache_params(const disc_cache_t* c, int32_t layer, const int32_t* cu, int32
     w->cu = cu; w->seq_rows = rows; w->status = status; w->n_seqs = n_seqs;
 }
 
-int64_t grad_blocks(int64_t n, int32_t vectors, int32_t D) {
-    const int64_t need = (n * chunks_of(vectors, D) + THREADS / 32 - 1) / (THREADS / 32);
-    return need < MAX_BLOCKS ? need : MAX_BLOCKS;
+// The gradient's blocks, in proportion to the vectors of each kind.
+struct GradCut {
+    Cut cut;
+    int q_blocks, blocks;
+};
+GradCut grad_cut(int64_t n, int32_t hq, int32_t hkv, int side) {
+    GradCut g;
+    const int32_t heads[3] = {hq, hkv, 0};
+    // four times as many items as warps, so that the last ones are short
+    g.cut = cut_of(n, heads, side, int64_t(MAX_GRAD_BLOCKS) * WARPS * 4, 1);
+    const int64_t all = int64_t(hq) + hkv;
+    int64_t q = hq ? (MAX_GRAD_BLOCKS * int64_t(hq) + all / 2) / all : 0;
+    if (hq && q < 1) q = 1;
+    if (hkv && q > MAX_GRAD_BLOCKS - 1) q = MAX_GRAD_BLOCKS - 1;
+    int64_t k = hkv ? MAX_GRAD_BLOCKS - q : 0;
+    const int64_t need_q = (n * g.cut.chunks[0] + WARPS - 1) / WARPS, need_k = (n * g.cut.chunks[1] + WARPS - 1) / WARPS;
+    if (q > need_q) q = need_q;
+    if (k > need_k) k = need_k;
+    g.q_blocks = int(q);
+    g.blocks = int(q + k);
+    return g;
 }
 
 }  // namespace
@@ -407,12 +724,12 @@ int disc::write_held(const disc_cache_t* c, int32_t layer, const void* k, int64_
                      int32_t n_tokens, const int32_t* cu, int32_t n_seqs, const int32_t* rows, const uint8_t* status, cudaStream_t st) {
     RopeParams p = {};
     CacheParams w;
-    p.n = n_tokens; p.D = c->head_dim;
+    p.n = n_tokens; p.D = c->head_dim; p.inv_D = 1.f / float(p.D);
     p.heads[1] = p.heads[2] = c->n_kv_heads;
     p.x[1] = Vectors{static_cast<unsigned char*>(const_cast<void*>(k)), k_token * 2, k_head * 2};
     p.x[2] = Vectors{static_cast<unsigned char*>(const_cast<void*>(v)), v_token * 2, v_head * 2};
     cache_params(c, layer, cu, n_seqs, rows, status, &w);
-    return cache_type(c) == DISC_BF16 ? launch<__nv_bfloat16, true>(p, w, st) : launch<__half, true>(p, w, st);
+    return launch_cache(c, p, w, st);
 }
 
 extern "C" {
@@ -431,9 +748,7 @@ int disc_norm_rope(const disc_rope_t* how, const void* q, int64_t q_token_stride
     if (const int rc = check_vectors(q_out, q_out_token_stride, q_out_head_stride, n_tokens, n_q_heads, &p.y[0])) return rc;
     if (const int rc = check_vectors(k_out, k_out_token_stride, k_out_head_stride, n_tokens, n_kv_heads, &p.y[1])) return rc;
     p.n = int32_t(n_tokens); p.heads[0] = n_q_heads; p.heads[1] = n_kv_heads; p.pos = positions;
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const CacheParams none = {};
-    return dtype == DISC_BF16 ? launch<__nv_bfloat16, false>(p, none, st) : launch<__half, false>(p, none, st);
+    return launch<-1>(dtype, p, CacheParams{}, static_cast<cudaStream_t>(stream));
 }
 
 int disc_norm_rope_write(const disc_cache_t* c, int32_t layer, const disc_rope_t* how, const void* q, int64_t q_token_stride, int64_t q_head_stride,
@@ -455,14 +770,14 @@ int disc_norm_rope_write(const disc_cache_t* c, int32_t layer, const disc_rope_t
     p.n = int32_t(n_tokens); p.heads[0] = n_q_heads; p.heads[1] = p.heads[2] = c->n_kv_heads; p.pos = positions;
     CacheParams w;
     cache_params(c, layer, cu, n_seqs, rows, status, &w);
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return cache_type(c) == DISC_BF16 ? launch<__nv_bfloat16, true>(p, w, st) : launch<__half, true>(p, w, st);
+    return launch_cache(c, p, w, static_cast<cudaStream_t>(stream));
 }
 
 int64_t disc_norm_rope_scratch_bytes(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t n_tokens) {
-    if (n_q_heads < 0 || n_kv_heads < 0 || n_q_heads > (1 << 16) || n_kv_heads > (1 << 16) || head_dim <= 0 || head_dim > DISC_MAX_HEAD_DIM || n_tokens < 0 || n_tokens > (int64_t(1) << 30))
+    if (n_q_heads < 0 || n_kv_heads < 0 || n_q_heads > (1 << 16) || n_kv_heads > (1 << 16) || n_q_heads + n_kv_heads == 0 || head_dim <= 0 || head_dim > DISC_MAX_HEAD_DIM || n_tokens < 0 || n_tokens > (int64_t(1) << 30))
         return DISC_ERR_ARG;
-    return grad_blocks(n_tokens, n_q_heads + n_kv_heads, head_dim) * 2 * head_dim * 4;
+    const int a = grad_cut(n_tokens, n_q_heads, n_kv_heads, side_by_side(head_dim, 0)).blocks, b = grad_cut(n_tokens, n_q_heads, n_kv_heads, side_by_side(head_dim, 8)).blocks;
+    return int64_t(a > b ? a : b) * head_dim * 4;
 }
 
 int disc_norm_rope_grad(const disc_rope_t* how, const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride,
@@ -474,7 +789,7 @@ int disc_norm_rope_grad(const disc_rope_t* how, const void* q, int64_t q_token_s
     if (const int rc = check_how(how, dtype, head_dim, &p)) return rc;
     const int64_t need = disc_norm_rope_scratch_bytes(n_q_heads, n_kv_heads, head_dim, n_tokens);
     if (need < 0) return int(need);
-    if (n_q_heads + n_kv_heads == 0 || (n_tokens > 0 && p.rot > 0 && !positions)) return DISC_ERR_ARG;
+    if (n_tokens > 0 && p.rot > 0 && !positions) return DISC_ERR_ARG;
     const bool weights = d_q_weight || d_k_weight;
     if (weights && (!p.norm || (n_tokens > 0 && (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 3u) || scratch_bytes < need)))) return DISC_ERR_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -489,13 +804,16 @@ int disc_norm_rope_grad(const disc_rope_t* how, const void* q, int64_t q_token_s
     if (const int rc = check_vectors(d_k_out, dk_token_stride, dk_head_stride, n_tokens, n_kv_heads, &p.y[1])) return rc;
     if ((n_q_heads && (!d_q || misaligned(d_q))) || (n_kv_heads && (!d_k || misaligned(d_k)))) return DISC_ERR_ARG;
     p.n = int32_t(n_tokens); p.heads[0] = n_q_heads; p.heads[1] = n_kv_heads; p.pos = positions;
-    const int chunks = chunks_of(n_q_heads + n_kv_heads, head_dim), blocks = int(grad_blocks(n_tokens, n_q_heads + n_kv_heads, head_dim));
+    const GradCut g = grad_cut(n_tokens, n_q_heads, n_kv_heads, side_by_side(head_dim, p.rot));
     float* part = weights ? static_cast<float*>(scratch) : nullptr;
-    auto kernel = dtype == DISC_BF16 ? (head_dim <= 64 ? norm_rope_grad_kernel<__nv_bfloat16, 8> : norm_rope_grad_kernel<__nv_bfloat16, 16>)
-                                     : (head_dim <= 64 ? norm_rope_grad_kernel<__half, 8> : norm_rope_grad_kernel<__half, 16>);
-    if (const int rc = launch_after(kernel, unsigned(blocks), THREADS, 0, st, p, static_cast<unsigned char*>(d_q), static_cast<unsigned char*>(d_k), part, chunks)) return rc;
+    const bool bf = dtype == DISC_BF16, small = head_dim <= 64;
+    auto kernel = long_runs(head_dim, p.rot) ? (bf ? (small ? norm_rope_grad_kernel<__nv_bfloat16, 4, 8> : norm_rope_grad_kernel<__nv_bfloat16, 8, 8>)
+                                                   : (small ? norm_rope_grad_kernel<__half, 4, 8> : norm_rope_grad_kernel<__half, 8, 8>))
+                                             : (bf ? (small ? norm_rope_grad_kernel<__nv_bfloat16, 8, 4> : norm_rope_grad_kernel<__nv_bfloat16, 16, 4>)
+                                                   : (small ? norm_rope_grad_kernel<__half, 8, 4> : norm_rope_grad_kernel<__half, 16, 4>));
+    if (const int rc = launch_after(kernel, unsigned(g.blocks), THREADS, 0, st, p, static_cast<unsigned char*>(d_q), static_cast<unsigned char*>(d_k), part, g.q_blocks, g.cut)) return rc;
     if (!weights) return DISC_OK;
-    return launch_after(weight_grad_kernel, unsigned((2 * head_dim + 31) / 32), 1024, 0, st, static_cast<const float*>(part), blocks, int(head_dim), d_q_weight, d_k_weight);
+    return launch_after(weight_grad_kernel, unsigned(2 * ((head_dim + 31) / 32)), 1024, 0, st, static_cast<const float*>(part), g.q_blocks, g.blocks, int(head_dim), d_q_weight, d_k_weight);
 }
 
 }  // extern "C"
