@@ -612,7 +612,7 @@ __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     float* dst = o_sm + ((lane & 3) * 2 + e) * S::O_LD + (lane >> 2) * 2;
-                    const float f = acc.t[0][e] > -CUDART_INF_F && acc.m[0][e] > -CUDART_INF_F ? exp2f(acc.t[0][e] - acc.m[0][e] + held_shift<HELD>()) : 1.f;
+                    const float f = acc.t[0][e] > -CUDART_INF_F && acc.m[0][e] > -CUDART_INF_F ? exp2f(acc.t[0][e] - acc.m[0][e]) : 1.f;
 #pragma unroll
                     for (int j = 0; j < DP / 16; ++j) *reinterpret_cast<float2*>(dst + 16 * j) = make_float2(acc.o[0][j][e] * f, acc.o[0][j][2 + e] * f);
                     if (lane < 4) { ml_sm[2 * lane + e] = acc.m[0][e]; ml_sm[8 + 2 * lane + e] = acc.l[0][e]; }

@@ -28,20 +28,21 @@ using namespace disc;
 
 constexpr int AT = 128;
 constexpr int WARPS = AT / 32;
-constexpr int STAGES = 6;              // blocks of 16 tokens on their way to a warp
+constexpr int STAGES = 4;              // blocks of 16 tokens on their way to a warp, and the one it is at
 
 template <int DP, int NT>
 struct HeldSmem {
-    static constexpr int RING = STAGES * held_stage_bytes<DP>();   // of a warp
+    static constexpr int STAGE = held_stage_bytes<DP>() + 16;      // behind the block: its tokens and owner
+    static constexpr int RING = STAGES * STAGE;                    // of a warp
     static constexpr int SUMS = WARPS * NT * 8 * DP * 4;           // at the end, over the rings
     static constexpr int BYTES = WARPS * RING > SUMS ? WARPS * RING : SUMS;
 };
 
 template <typename T, int DP, int HELD, int NT>
-__global__ void __launch_bounds__(AT, 2) attend_held_kernel(const AttendParams p) {
+__global__ void __launch_bounds__(AT, HELD_BLOCKS) attend_held_kernel(const AttendParams p) {
     let_later_in();
     wait_for_earlier();
-    constexpr int STAGE_BYTES = held_stage_bytes<DP>();
+    constexpr int STAGE = HeldSmem<DP, NT>::STAGE;
     constexpr int CH = DP / 16;                                    // 16-byte chunks of a token's codes
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ float w_m[WARPS][NT * 8], w_l[WARPS][NT * 8], w_t[WARPS][NT * 8];
@@ -52,7 +53,8 @@ __global__ void __launch_bounds__(AT, 2) attend_held_kernel(const AttendParams p
     const int G = sh.G;
     const int lane_of = blockIdx.x / p.kv_heads, head = blockIdx.x % p.kv_heads;
     const int item_end = p.plan.first[lane_of + 1];
-    const uint32_t ring = smem_u32(smem) + warp * HeldSmem<DP, NT>::RING;
+    unsigned char* const ring = smem + warp * HeldSmem<DP, NT>::RING;
+    const uint32_t ring_at = smem_u32(ring);
 
     for (int n = p.plan.first[lane_of]; n < item_end; ++n) {
         const int4 item = *reinterpret_cast<const int4*>(p.plan.items + n), more = *(reinterpret_cast<const int4*>(p.plan.items + n) + 1);
@@ -70,25 +72,22 @@ __global__ void __launch_bounds__(AT, 2) attend_held_kernel(const AttendParams p
             if (sh.per_group > 1) return list[i];
             return make_int2(table[i / sh.blks_per_page], i % sh.blks_per_page | max(0, min(BLK, len - i * BLK)) << 8);
         };
-        int meta[STAGES];                                          // tokens and owner of the blocks in flight; a register each
-        auto load_block = [&](int stage, int2 e) {
+        auto load_block = [&](uint32_t stage, int2 e) {
             // a plan older than the books: rows may have let go of their pages since, and -1 is no place to read from
             if (unsigned(e.x) >= unsigned(p.pages)) e = make_int2(0, 0);
             const int tokens = (e.y >> 8) & 255;
             const int64_t off = (int64_t(e.x) * p.kv_heads + head) * p.head_bytes;
-            load_held_block<DP>(ring + stage * STAGE_BYTES, p.k + off, p.v + off, e.y & 255, tokens, p.D, p.page_size, lane);
-            return e.y >> 8;
+            load_held_block<DP>(ring_at + stage, p.k + off, p.v + off, e.y & 255, tokens, p.D, p.page_size, lane);
+            if (lane == 0) *reinterpret_cast<volatile int*>(ring + stage + held_stage_bytes<DP>()) = e.y >> 8;
         };
         int2 first[STAGES];
 #pragma unroll
         for (int t = 0; t < STAGES; ++t) first[t] = entry(t);
 #pragma unroll
         for (int t = 0; t < STAGES - 1; ++t) {
-            meta[t] = 0;
-            if (t < blocks) meta[t] = load_block(t, first[t]);
+            if (t < blocks) load_block(t * STAGE, first[t]);
             cp_commit();
         }
-        meta[STAGES - 1] = 0;
         int2 next = first[STAGES - 1];
 
         // query vectors: vector m is head m % G of row m / G
@@ -106,26 +105,23 @@ __global__ void __launch_bounds__(AT, 2) attend_held_kernel(const AttendParams p
 #pragma unroll
             for (int e = 0; e < 2; ++e) owner_of[nt][e] = (nt * 8 + (lane & 3) * 2 + e) / G + 1;
 
-        for (int t0 = 0; t0 < blocks; t0 += STAGES) {
+        uint32_t stage = 0;
+#pragma unroll 1
+        for (int t = 0; t < blocks; ++t) {
+            cp_wait<STAGES - 2>();
+            __syncwarp();                                          // a warp works on what it has brought in itself
+            const uint32_t before = stage == 0 ? (STAGES - 1) * STAGE : stage - STAGE;
+            if (t + STAGES - 1 < blocks) load_block(before, next);
+            cp_commit();
+            next = entry(t + STAGES);
+            const int meta = *reinterpret_cast<volatile int*>(ring + stage + held_stage_bytes<DP>()), owner = meta >> 8, tokens = meta & 255;
+            bool in[NT][2];
 #pragma unroll
-            for (int st = 0; st < STAGES; ++st) {
-                const int t = t0 + st;
-                if (t >= blocks) break;
-                cp_wait<STAGES - 2>();
-                __syncwarp();                                      // a warp works on what it has brought in itself
-                constexpr int AHEAD = STAGES - 1;
-                if (t + AHEAD < blocks) meta[(st + AHEAD) % STAGES] = load_block((st + AHEAD) % STAGES, next);
-                cp_commit();
-                next = entry(t + STAGES);
-                const int owner = meta[st] >> 8, tokens = meta[st] & 255;
-                if (tokens == 0) continue;
-                bool in[NT][2];
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) in[nt][e] = !owner || owner == owner_of[nt][e];
-                add_held_block<T, DP, HELD, NT>(acc, qs, ring + st * STAGE_BYTES, tokens, in, lane);
-            }
+                for (int e = 0; e < 2; ++e) in[nt][e] = !owner || owner == owner_of[nt][e];
+            if (tokens) add_held_block<T, DP, HELD, NT>(acc, qs, ring_at + stage, tokens, in, lane);
+            stage = stage == (STAGES - 1) * STAGE ? 0 : stage + STAGE;
         }
         finish_held(acc);
         cp_wait<0>();
@@ -164,7 +160,7 @@ __global__ void __launch_bounds__(AT, 2) attend_held_kernel(const AttendParams p
                 ll += w_m[w][m] > -CUDART_INF_F ? ex2_approx(w_m[w][m] - mm) * w_l[w][m] : w_l[w][m];
             }
             float inv = ll > 0.f ? 1.f / ll : (ll == 0.f ? 0.f : ll);
-            if (tt > -CUDART_INF_F && ll > 0.f) inv *= exp2f(tt - mm + held_shift<HELD>());
+            if (tt > -CUDART_INF_F && ll > 0.f) inv *= exp2f(tt - mm);
             x.x *= inv; x.y *= inv; x.z *= inv; x.w *= inv;
             float lse2 = ll > 0.f ? mm + log2f(ll) : (ll == 0.f ? -CUDART_INF_F : ll);
             if (n_rows > 1 && p.len[r0 + m / G] == 0) {           // beside rows whose shared pages it does not hold

@@ -30,17 +30,30 @@ __device__ __forceinline__ int hold_exponent(uint32_t amax_bits, float* inv) {
     *inv = pow2f(-e);
     return e;
 }
-// four codes; x with NAN_EXP's inv = 0 may be anything.  i8: added to 1.5 2^23, a value is rounded to a whole number, to the nearest, ties to
-// even, and its last byte is the code.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;"
+        : "=l"(reinterpret_cast<unsigned long long&>(d))
+        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
+    return d;
+}
+// Four codes of x 2^-e; what they are with NAN_EXP's inv = 0 does not matter (the caller writes zeros).  i8: added to 1.5 2^23, a value is
+// rounded to a whole number, to the nearest, ties to even, and its last byte is the code.
 template <int HELD>
 __device__ __forceinline__ uint32_t hold4(float2 a, float2 b, float inv) {
-    if (inv == 0.f) return 0;
+    const float2 i2 = make_float2(inv, inv);
     if (HELD == HELD_E4M3) {
-        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a.x * inv, a.y * inv), __NV_SATFINITE, __NV_E4M3);
-        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(b.x * inv, b.y * inv), __NV_SATFINITE, __NV_E4M3);
-        return lo | hi << 16;
+        const float2 x = mul2(a, i2), y = mul2(b, i2);
+        uint32_t c;
+        asm("{\n\t.reg .b16 lo, hi;\n\t"
+            "cvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\t"
+            "cvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\t"
+            "mov.b32 %0, {lo, hi};\n\t}"
+            : "=r"(c)
+            : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
+        return c;
     }
-    const float2 i2 = make_float2(inv, inv), magic = make_float2(12582912.f, 12582912.f);
+    const float2 magic = make_float2(12582912.f, 12582912.f);
     const float2 x = fma2(a, i2, magic), y = fma2(b, i2, magic);
     return __byte_perm(__byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x0040), __byte_perm(__float_as_uint(y.x), __float_as_uint(y.y), 0x0040), 0x5410);
 }

@@ -35,29 +35,53 @@ __device__ __forceinline__ void load_held_block(uint32_t stage, const unsigned c
     if (lane < 2) cp16(stage + 2 * BLK * DP + lane * BLK, (lane ? v : k) + page_size * D + blk * BLK, true);
 }
 
-// Four codes as f16, exactly: those of bytes 0 and 2, and of bytes 1 and 3.  An e4m3 code's exponent and mantissa, moved to an
-// f16's places, stand for 2^-8 of its value (the biases are 7 and 15), denormal codes included.  An i8 code, its top bit
-// turned over, is the last byte of the f16 1024 + 128 + code.
+// Codes as f16, exactly.  e4m3: the conversion instruction takes two neighbouring codes, 49 of them a clock and SM (with shifts and masks,
+// seven operations for four codes, the 64 ragged rows took 183 us).  i8: a code, its top bit turned over, is the last byte of the f16
+// 1024 + 128 + code; that gives codes 0 and 2, and 1 and 3.
+__device__ __forceinline__ uint32_t e4m3_f16(uint32_t two) {
+    uint32_t x;
+    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\t}" : "=r"(x) : "r"(two));
+    return x;
+}
+__device__ __forceinline__ uint32_t e4m3_f16_upper(uint32_t two) {
+    uint32_t x;
+    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, hi;\n\t}" : "=r"(x) : "r"(two));
+    return x;
+}
+__device__ __forceinline__ void i8_f16(uint32_t c, uint32_t& even, uint32_t& odd) {
+    const __half2 bias = __half2half2(__ushort_as_half(0x6480));               // 1152
+    const uint32_t a = (c & 0x00ff00ffu) ^ 0x64806480u, b = ((c >> 8) & 0x00ff00ffu) ^ 0x64806480u;
+    const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), bias), y = __hsub2(*reinterpret_cast<const __half2*>(&b), bias);
+    even = *reinterpret_cast<const uint32_t*>(&x);
+    odd = *reinterpret_cast<const uint32_t*>(&y);
+}
+// Keys: four values of a token, in the order in which the queries lie too (held_dim).
 template <int HELD>
-__device__ __forceinline__ void codes_f16(uint32_t c, uint32_t& even, uint32_t& odd) {
+__device__ __forceinline__ void key_codes(uint32_t c, uint32_t& first, uint32_t& second) {
     if (HELD == HELD_E4M3) {
-        const uint32_t d = c << 8;
-        even = (d & 0x80008000u) | ((d >> 1) & 0x3f803f80u);
-        odd = (c & 0x80008000u) | ((c >> 1) & 0x3f803f80u);
+        first = e4m3_f16(c);
+        second = e4m3_f16_upper(c);
     } else {
-        const __half2 bias = __half2half2(__ushort_as_half(0x6480));           // 1152
-        const uint32_t a = (c & 0x00ff00ffu) ^ 0x64806480u, b = ((c >> 8) & 0x00ff00ffu) ^ 0x64806480u;
-        const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), bias), y = __hsub2(*reinterpret_cast<const __half2*>(&b), bias);
-        even = *reinterpret_cast<const uint32_t*>(&x);
-        odd = *reinterpret_cast<const uint32_t*>(&y);
+        i8_f16(c, first, second);
     }
 }
 template <int HELD>
-__device__ __forceinline__ constexpr float held_shift() { return HELD == HELD_E4M3 ? 8.f : 0.f; }      // log2 of code / f16
+__device__ __forceinline__ constexpr int held_dim(int i) { return HELD == HELD_E4M3 || i == 0 || i == 3 ? i : 3 - i; }       // 0 1 2 3, or 0 2 1 3
+// Values: two neighbouring dims of two tokens -> both tokens' first dim, both tokens' second.
+template <int HELD>
+__device__ __forceinline__ void value_codes(uint32_t c, uint32_t& first, uint32_t& second) {
+    if (HELD == HELD_E4M3) {
+        const uint32_t a = e4m3_f16(c), b = e4m3_f16_upper(c);
+        first = __byte_perm(a, b, 0x5410);
+        second = __byte_perm(a, b, 0x7632);
+    } else {
+        i8_f16(c, first, second);
+    }
+}
 
 template <int DP, int NT>
 struct HeldQueries {
-    uint32_t f[NT][DP / 16][2];        // vector lane / 4; values 16 kk + 4 (lane % 4) + {0, 2} and + {1, 3}, as the codes come
+    uint32_t f[NT][DP / 16][2];        // vector lane / 4; values 16 kk + 4 (lane % 4) + held_dim(0, 1) and (2, 3)
     float c2[NT][2];                   // what a score of this thread's vectors, 2 (lane % 4) and the next, is multiplied with: units of log2
 };
 // q: this lane's vector (lane / 4 of the eight), `some`: there is one
@@ -83,10 +107,10 @@ __device__ __forceinline__ void load_held_queries(HeldQueries<DP, NT>& qs, int n
     const float f = pow2f(up);
 #pragma unroll
     for (int kk = 0; kk < DP / 16; ++kk) {
-        qs.f[nt][kk][0] = pack2<__half>(x[kk][0] * f, x[kk][2] * f);
-        qs.f[nt][kk][1] = pack2<__half>(x[kk][1] * f, x[kk][3] * f);
+        qs.f[nt][kk][0] = pack2<__half>(x[kk][held_dim<HELD>(0)] * f, x[kk][held_dim<HELD>(1)] * f);
+        qs.f[nt][kk][1] = pack2<__half>(x[kk][held_dim<HELD>(2)] * f, x[kk][held_dim<HELD>(3)] * f);
     }
-    const float back = c2 * pow2f(-up) * (HELD == HELD_E4M3 ? 256.f : 1.f);
+    const float back = c2 * pow2f(-up);
     qs.c2[nt][0] = __shfl_sync(0xffffffffu, back, (lane & 3) * 8);
     qs.c2[nt][1] = __shfl_sync(0xffffffffu, back, (lane & 3) * 8 + 4);
 }
@@ -131,10 +155,10 @@ __device__ __forceinline__ void add_held_block(HeldSums<DP, NT>& acc, const Held
         uint32_t kf[4], a[4], b[4];
         // matrices: tokens 0-7 and 8-15 at chunk 2 c, then at chunk 2 c + 1
         ldsm4(stage + held_chunk_at<DP>(lane & 15, 2 * c + (lane >> 4)), kf);
-        codes_f16<HELD>(kf[0], a[0], a[2]);
-        codes_f16<HELD>(kf[1], a[1], a[3]);
-        codes_f16<HELD>(kf[2], b[0], b[2]);
-        codes_f16<HELD>(kf[3], b[1], b[3]);
+        key_codes<HELD>(kf[0], a[0], a[2]);
+        key_codes<HELD>(kf[1], a[1], a[3]);
+        key_codes<HELD>(kf[2], b[0], b[2]);
+        key_codes<HELD>(kf[3], b[1], b[3]);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             mma16<__half>(s[nt], a, qs.f[nt][2 * c][0], qs.f[nt][2 * c][1]);
@@ -204,10 +228,10 @@ __device__ __forceinline__ void add_held_block(HeldSums<DP, NT>& acc, const Held
         uint32_t vf[4], a[4], b[4];
         // matrices: tokens 0-7 at chunks 2 j and 2 j + 1, then tokens 8-15; each register two dims of two tokens
         ldsm4t(stage + BLK * DP + held_chunk_at<DP>((lane & 7) + ((lane >> 4) << 3), 2 * j + ((lane >> 3) & 1)), vf);
-        codes_f16<HELD>(vf[0], a[0], a[1]);
-        codes_f16<HELD>(vf[2], a[2], a[3]);
-        codes_f16<HELD>(vf[1], b[0], b[1]);
-        codes_f16<HELD>(vf[3], b[2], b[3]);
+        value_codes<HELD>(vf[0], a[0], a[1]);
+        value_codes<HELD>(vf[2], a[2], a[3]);
+        value_codes<HELD>(vf[1], b[0], b[1]);
+        value_codes<HELD>(vf[3], b[2], b[3]);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             mma16<__half>(acc.o[nt][2 * j], a, p0[nt], p1[nt]);

@@ -34,7 +34,7 @@ constexpr int BLOCKS = 5;              // on an SM
 constexpr int GRAD_BLOCKS = 3;
 constexpr int SMS = 148;
 constexpr int MAX_GRAD_BLOCKS = SMS * GRAD_BLOCKS;     // which each leave sums of their own
-constexpr int MOST_TOKENS = 8;         // of a warp
+constexpr int MOST_TOKENS = 32;        // of a warp, whose lanes look up one each
 
 struct Vectors {                       // strides in bytes
     unsigned char* at;
@@ -66,13 +66,6 @@ struct CacheParams {
 __device__ __forceinline__ Vectors pick(const Vectors* v, int kind) { return kind == 0 ? v[0] : kind == 1 ? v[1] : v[2]; }
 __device__ __forceinline__ Vectors pick2(const Vectors* v, int kind) { return kind == 0 ? v[0] : v[1]; }
 
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-    float2 d;
-    asm("mul.rn.f32x2 %0, %1, %2;"
-        : "=l"(reinterpret_cast<unsigned long long&>(d))
-        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
-    return d;
-}
 __device__ __forceinline__ float2 swapped(float2 a) { return make_float2(a.y, a.x); }
 
 // Where a lane's two runs of RUN values begin.  Rotated: the pairs (a + i, b + i), i < RUN, or, interleaved, neighbours in both.
@@ -265,7 +258,7 @@ __device__ __forceinline__ float inverse_norm(const RopeParams& p, const float2*
 
 // The page of a token and its place in it (page -1: it is not written), and its position.  A lane per token.
 struct Spot {
-    int32_t page, off, pos;
+    int32_t page, off, pos;            // page -1: not written
 };
 __device__ __forceinline__ Spot spot_of(const CacheParams& w, int32_t t) {
     Spot at = {-1, 0, 0};
@@ -291,14 +284,14 @@ __device__ __forceinline__ Spot spot_of(const CacheParams& w, int32_t t) {
     return at;
 }
 
-// How the vectors are dealt out: warp `id` has `per` steps (of SIDE vectors each) of one kind of `tokens` tokens.
+// How the vectors are dealt out: a warp has `per` steps (of SIDE vectors each) of one kind of `tokens` tokens.
 struct Cut {
     int64_t end[3];                    // warps up to the last of queries, keys, values
-    int32_t per[3], chunks[3], tokens;
+    int32_t per[3], chunks[3], tokens[3];
 };
 struct Share {
     int kind, h0, h1;                  // vectors h0 .. h1-1 of it
-    int32_t t0, t1;
+    int32_t t0, tokens;                // of tokens t0, t0 + 1, ...
 };
 __device__ __forceinline__ bool share_of(const Cut& cut, const RopeParams& p, int64_t id, int side_by_side, Share* s) {
     const int kind = id < cut.end[0] ? 0 : id < cut.end[1] ? 1 : 2;
@@ -307,17 +300,21 @@ __device__ __forceinline__ bool share_of(const Cut& cut, const RopeParams& p, in
     const int chunks = kind == 0 ? cut.chunks[0] : kind == 1 ? cut.chunks[1] : cut.chunks[2];
     const int per = (kind == 0 ? cut.per[0] : kind == 1 ? cut.per[1] : cut.per[2]) * side_by_side;
     s->kind = kind;
-    s->t0 = int32_t(id / chunks * cut.tokens);
-    s->t1 = min(p.n, s->t0 + cut.tokens);
+    const int tokens = kind == 0 ? cut.tokens[0] : kind == 1 ? cut.tokens[1] : cut.tokens[2];
+    s->t0 = int32_t(id / chunks * tokens);
+    s->tokens = min(tokens, p.n - s->t0);
     s->h0 = int(id % chunks) * per;
     s->h1 = min(kind == 0 ? p.heads[0] : kind == 1 ? p.heads[1] : p.heads[2], s->h0 + per);
     return true;
 }
 
-// HELD: -1 without a cache, else how it holds its vectors.  The largest |value| of a vector is found among the 16-bit patterns
+// HELD: -1 without a cache, else how it holds its vectors.  ROPE: there is a norm or a rotation; without, the kernel needs half the registers, and twice
+// as many warps run at a time (65,000 tokens x 16 vectors of 128 into 8 bits: MEASURED).  The largest |value| of a vector is found among the 16-bit patterns
 // themselves, two at a time: without their signs they are in order, and infinities and NaN come last.
-template <typename T, int LPV, int RUN, int HELD>
-__global__ void __launch_bounds__(THREADS, BLOCKS) norm_rope_kernel(const RopeParams p, const CacheParams w, const Cut cut) {
+template <bool ROPE>
+__host__ __device__ constexpr int blocks_of() { return ROPE ? BLOCKS : 9; }
+template <typename T, int LPV, int RUN, int HELD, bool ROPE>
+__global__ void __launch_bounds__(THREADS, blocks_of<ROPE>()) norm_rope_kernel(const RopeParams p, const CacheParams w, const Cut cut) {
     let_later_in();
     wait_for_earlier();
     constexpr int STEP = step_bytes<RUN>();
@@ -331,7 +328,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_rope_kernel(const RopePa
     if (!share_of(cut, p, int64_t(blockIdx.x) * WARPS + (threadIdx.x >> 5), SIDE, &sh)) return;
     const int kind = sh.kind;
     const Place at = place_of<RUN>(p, c);
-    const bool rotated = p.rot > 0 && kind < 2, normed = p.norm && kind < 2;
+    const bool rotated = ROPE && p.rot > 0 && kind < 2, normed = ROPE && p.norm && kind < 2;
     const int steps = (sh.h1 - sh.h0 + SIDE - 1) / SIDE;           // of a token
 
     // loads, DEPTH - 1 steps ahead
@@ -340,7 +337,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_rope_kernel(const RopePa
     const Vectors src = CACHE ? pick(p.x, kind) : pick2(p.x, kind);
     const unsigned char* in = src.at + sh.t0 * src.token + (sh.h0 + side) * src.head;
     const int64_t in_step = SIDE * src.head, in_token = src.token - steps * in_step;
-    int in_h = sh.h0 + side, left = (sh.t1 - sh.t0) * steps;       // steps not yet asked for
+    int in_h = sh.h0 + side, left = sh.tokens * steps;             // steps not yet asked for
     uint32_t in_at = 0, at_step = 0;   // places in the ring
     auto fetch = [&]() {
         if (left > 0) {
@@ -361,10 +358,11 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_rope_kernel(const RopePa
 #pragma unroll
     for (int i = 0; i < DEPTH - 1; ++i) fetch();
 
-    Spot spots = {-1, 0, 0};           // of token t0 + lane
-    if (sh.t0 + lane < sh.t1) {
-        if (CACHE) spots = spot_of(w, sh.t0 + lane);
-        if (rotated && p.pos) spots.pos = p.pos[sh.t0 + lane];
+    Spot spots = {-1, 0, 0};           // of the lane-th token
+    if (lane < sh.tokens) {
+        const int32_t t = sh.t0 + lane;
+        if (CACHE) spots = spot_of(w, t);
+        if (rotated && p.pos) spots.pos = p.pos[t];
     }
     Frequencies freq;
     if (rotated) freq = frequencies_of(p, lane);
@@ -374,25 +372,28 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_rope_kernel(const RopePa
     const Vectors dst = CACHE ? p.y[0] : pick2(p.y, kind);
     const int64_t out_step = to_cache ? int64_t(SIDE) * w.head_bytes : SIDE * dst.head;
     unsigned char* out = nullptr;
-    int32_t off = 0, page = -1;
+    int32_t off = 0;
+    bool written = true;
+    const int64_t page_bytes = to_cache ? int64_t(p.heads[1]) * w.head_bytes : 0, first_out = to_cache ? int64_t(sh.h0 + side) * w.head_bytes : (sh.h0 + side) * dst.head;
+    unsigned char* const plane = CACHE ? (kind == 2 ? w.plane[1] : w.plane[0]) : nullptr;
     int h = sh.h1 + side;              // at a token's end: the next begins
-    int32_t t = sh.t0 - 1;
-    for (int todo = (sh.t1 - sh.t0) * steps; todo > 0; --todo) {
+    int from = -1;                     // which of the warp's tokens
+    for (int todo = sh.tokens * steps; todo > 0; --todo) {
         {
             if (h - side >= sh.h1) {
-                ++t;
+                ++from;
                 h = sh.h0 + side;
-                const int from = t - sh.t0;
                 if (to_cache) {
-                    page = __shfl_sync(FULL, spots.page, from);
+                    const int32_t page = __shfl_sync(FULL, spots.page, from);
                     off = __shfl_sync(FULL, spots.off, from);
-                    out = (kind == 2 ? w.plane[1] : w.plane[0]) + (int64_t(max(page, 0)) * p.heads[1] + h) * w.head_bytes;
+                    written = page >= 0;
+                    out = plane + max(page, 0) * page_bytes + first_out;
                 } else {
-                    out = dst.at + t * dst.token + h * dst.head;
+                    out = dst.at + (int64_t(sh.t0) + from) * dst.token + first_out;
                 }
                 if (rotated) turn_to(p, __shfl_sync(FULL, spots.pos, from), freq, turns, lane);
                 // what the weights and the angles come to, where they change
-                if (rotated || (normed && t == sh.t0)) {
+                if (rotated || (normed && from == 0)) {
                     float2 f[RUN];
                     load_weights<T, RUN>(p, kind, at, f);
                     if (at.turned) {
@@ -427,7 +428,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_rope_kernel(const RopePa
             if (!to_cache) {
                 if (real) store_raw<RUN>(out, at, y);
             } else if (HELD <= HELD_PLAIN) {
-                if (real && page >= 0) store_raw<RUN>(out + off * w.token_bytes, at, y);
+                if (real && written) store_raw<RUN>(out + off * w.token_bytes, at, y);
             } else {
                 // what is held is a vector of the type T
                 constexpr uint32_t ABS = 0x7fff7fffu;
@@ -444,7 +445,11 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_rope_kernel(const RopePa
                 uint32_t code[RUN / 2];
 #pragma unroll
                 for (int j = 0; j < RUN / 2; ++j) code[j] = hold4<HELD>(x[2 * j], x[2 * j + 1], inv);
-                if (real && page >= 0) {
+                if (e == NAN_EXP) {
+#pragma unroll
+                    for (int j = 0; j < RUN / 2; ++j) code[j] = 0;
+                }
+                if (real && written) {
                     unsigned char* to = out + off * p.D;
                     if constexpr (RUN == 8) {
                         *reinterpret_cast<uint2*>(to + at.a) = make_uint2(code[0], code[1]);
@@ -617,19 +622,26 @@ __global__ void __launch_bounds__(1024) weight_grad_kernel(const float* part, in
 bool long_runs(int32_t D, int32_t rot) { return D % 16 == 0 && rot % 16 == 0; }
 int side_by_side(int32_t D, int32_t rot) { return (D <= 64 ? 4 : 2) * (long_runs(D, rot) ? 2 : 1); }
 
-// A warp takes all of a token's vectors of a kind while that leaves as many warps as run at a time; with fewer tokens the vectors are
-// dealt out, two steps to a warp at least, and with many a warp takes several tokens.
-Cut cut_of(int64_t n, const int32_t* heads, int side, int64_t warps, int most_tokens) {
+// Equal shares of all steps for the warps that run at a time, as long as that is at least two steps and at most `most` (then several
+// shares one after the other): a second round of warps that only few take part in would cost as much as the first (65,000 tokens written
+// in 8 bits by 1.1 times as many warps as run at a time: 129 us).  A share is several tokens, or a part of one.  With norm or
+// rotation small shares in several rounds are better (16 steps: 60 us for 16384 tokens of 40 heads; one round of 55: 69 us); without,
+// where a token is less work than looking up its place, large ones (64 steps: 128 us; 4: 139).
+Cut cut_of(int64_t n, const int32_t* heads, int side, int64_t warps, int64_t most) {
     Cut cut = {};
-    int64_t end = 0, tokens = n / warps;
-    cut.tokens = int32_t(tokens < 1 ? 1 : tokens > most_tokens ? most_tokens : tokens);
+    int64_t steps[3], all = 0, end = 0;
+    for (int k = 0; k < 3; ++k) all += n * (steps[k] = (heads[k] + side - 1) / side);
+    int64_t share = (all + warps - 1) / warps;
+    share = share < 2 ? 2 : share > most ? most : share;
     for (int k = 0; k < 3; ++k) {
-        const int steps = (heads[k] + side - 1) / side;
-        int64_t chunks = n > 0 ? (warps + n - 1) / n : 1;
-        if (chunks > (steps + 1) / 2) chunks = (steps + 1) / 2;
-        cut.per[k] = chunks ? int32_t((steps + chunks - 1) / chunks) : 1;
-        cut.chunks[k] = (steps + cut.per[k] - 1) / cut.per[k];
-        end += (n + cut.tokens - 1) / cut.tokens * cut.chunks[k];
+        cut.tokens[k] = cut.per[k] = 1;
+        if (steps[k] > 0) {
+            const int64_t chunks = steps[k] / share > 1 ? steps[k] / share : 1, tokens = (share + steps[k] - 1) / steps[k];
+            cut.tokens[k] = int32_t(chunks > 1 ? 1 : tokens > MOST_TOKENS ? MOST_TOKENS : tokens);
+            cut.per[k] = int32_t((steps[k] + chunks - 1) / chunks);
+        }
+        cut.chunks[k] = int32_t((steps[k] + cut.per[k] - 1) / cut.per[k]);
+        end += (n + cut.tokens[k] - 1) / cut.tokens[k] * cut.chunks[k];
         cut.end[k] = end;
     }
     return cut;
@@ -637,11 +649,17 @@ Cut cut_of(int64_t n, const int32_t* heads, int side, int64_t warps, int most_to
 
 template <typename T, int HELD>
 int launch(const RopeParams& p, const CacheParams& w, cudaStream_t st) {
-    const Cut cut = cut_of(p.n, p.heads, side_by_side(p.D, p.rot), SMS * BLOCKS * WARPS, MOST_TOKENS);
+    const bool plain = HELD > HELD_PLAIN && !p.norm && p.rot == 0;
+    const Cut cut = cut_of(p.n, p.heads, side_by_side(p.D, p.rot), SMS * WARPS * (plain ? blocks_of<false>() : blocks_of<true>()), plain ? 64 : 16);
     const int64_t blocks = (cut.end[2] + WARPS - 1) / WARPS;
     if (blocks >= (int64_t(1) << 31)) return DISC_ERR_UNSUPPORTED;
-    auto kernel = long_runs(p.D, p.rot) ? (p.D <= 64 ? norm_rope_kernel<T, 4, 8, HELD> : norm_rope_kernel<T, 8, 8, HELD>)
-                                        : (p.D <= 64 ? norm_rope_kernel<T, 8, 4, HELD> : norm_rope_kernel<T, 16, 4, HELD>);
+    if (plain) {
+        // held vectors are made of 16 values
+        auto kernel = p.D <= 64 ? norm_rope_kernel<T, 4, 8, HELD, false> : norm_rope_kernel<T, 8, 8, HELD, false>;
+        return launch_after(kernel, unsigned(blocks), THREADS, 0, st, p, w, cut);
+    }
+    auto kernel = long_runs(p.D, p.rot) ? (p.D <= 64 ? norm_rope_kernel<T, 4, 8, HELD, true> : norm_rope_kernel<T, 8, 8, HELD, true>)
+                                        : (p.D <= 64 ? norm_rope_kernel<T, 8, 4, HELD, true> : norm_rope_kernel<T, 16, 4, HELD, true>);
     return launch_after(kernel, unsigned(blocks), THREADS, 0, st, p, w, cut);
 }
 template <int HELD>
@@ -702,9 +720,15 @@ struct GradCut {
 };
 GradCut grad_cut(int64_t n, int32_t hq, int32_t hkv, int side) {
     GradCut g;
-    const int32_t heads[3] = {hq, hkv, 0};
-    // four times as many items as warps, so that the last ones are short
-    g.cut = cut_of(n, heads, side, int64_t(MAX_GRAD_BLOCKS) * WARPS * 4, 1);
+    const int32_t heads[2] = {hq, hkv};
+    // an item: the vectors of a kind of a token, or, with few tokens, a part of them, so that there are four items for a warp
+    const int64_t wanted = n > 0 ? (int64_t(MAX_GRAD_BLOCKS) * WARPS * 4 + n - 1) / n : 1;
+    g.cut = {};
+    for (int k = 0; k < 2; ++k) {
+        const int64_t steps = (heads[k] + side - 1) / side, chunks = wanted < (steps + 1) / 2 ? wanted : (steps + 1) / 2;
+        g.cut.per[k] = chunks ? int32_t((steps + chunks - 1) / chunks) : 1;
+        g.cut.chunks[k] = int32_t((steps + g.cut.per[k] - 1) / g.cut.per[k]);
+    }
     const int64_t all = int64_t(hq) + hkv;
     int64_t q = hq ? (MAX_GRAD_BLOCKS * int64_t(hq) + all / 2) / all : 0;
     if (hq && q < 1) q = 1;

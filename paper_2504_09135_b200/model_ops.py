@@ -154,23 +154,27 @@ def disc_logprobs_grad(logits: torch.Tensor, targets, lse: torch.Tensor, entropy
     return out
 
 
+_F32, _DENSE = torch.float32, torch.contiguous_format
+
+
 # ---- head norms and rotation --------------------------------------------------------------------------
+def _weights(dtype, d: int, norm, q_weight, k_weight):
+    """Pointers of the norm's weights and their type."""
+    if not norm:
+        raise TypeError("q_weight, k_weight: the weights are the norm's; there is none")
+    w = k_weight if q_weight is None else q_weight
+    wt = dtype if w.dtype is dtype else _F32
+    _want(q_weight, d, "q_weight")
+    _want(k_weight, d, "k_weight")
+    return _dev(q_weight, wt, "q_weight"), _dev(k_weight, wt, "k_weight"), DISC_F32 if wt is _F32 else _HALF[wt]
+
+
 def _how(dtype, d: int, inv_freq, norm, q_weight, k_weight, eps, interleaved) -> _Rope:
     """What is done to the vectors, with the checks that need the tensors."""
-    rot = 0 if inv_freq is None else 2 * inv_freq.numel()
-    wt = torch.float32
-    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if w is None:
-            continue
-        if not norm:
-            raise TypeError(f"{name}: the weights are the norm's; there is none")
-        _want(w, d, name)
-        if w.dtype is dtype:
-            wt = dtype
-    if q_weight is not None and k_weight is not None and q_weight.dtype is not k_weight.dtype:
-        raise TypeError("q_weight, k_weight: expected the same type")
-    return _Rope(_dev(inv_freq, torch.float32, "inv_freq"), _dev(q_weight, wt, "q_weight"), _dev(k_weight, wt, "k_weight"), float(eps), rot,
-                 int(bool(interleaved)), int(bool(norm)), DISC_F32 if wt is torch.float32 else _HALF[wt])
+    qw, kw, wt = (0, 0, 0) if q_weight is None and k_weight is None else _weights(dtype, d, norm, q_weight, k_weight)
+    if inv_freq is None:
+        return _Rope(None, qw, kw, eps, 0, 0, 1 if norm else 0, wt)
+    return _Rope(_dev(inv_freq, _F32, "inv_freq"), qw, kw, eps, 2 * inv_freq.numel(), 1 if interleaved else 0, 1 if norm else 0, wt)
 
 
 def _positions(positions, n: int, inv_freq):
@@ -178,44 +182,58 @@ def _positions(positions, n: int, inv_freq):
         if inv_freq is not None:
             raise TypeError("positions: expected one per token")
         return 0
-    _want(positions, n, "positions")
+    if positions.numel() != n:
+        _want(positions, n, "positions")
     return _dev(positions, torch.int32, "positions")
 
 
 def _heads(q, k, where: str):
     """Shapes of q [n, Hq, D] and k [n, Hkv, D], either of which may be None: (dtype, n, Hq, Hkv, D)."""
-    t = q if q is not None else k
+    t = k if q is None else q
     if t is None:
         raise TypeError(f"{where}: neither queries nor keys")
-    if t.dtype not in _HALF:
+    dtype, shape = t.dtype, t.shape
+    if dtype not in _HALF:
         raise DiscError(-7, where)
-    if t.dim() != 3 or (k is not None and q is not None and (k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2])):
-        raise TypeError("q, k: expected [tokens, heads, head_dim] with the same tokens and head_dim")
-    return t.dtype, t.shape[0], 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], t.shape[2]
+    if len(shape) != 3:
+        raise TypeError("q, k: expected [tokens, heads, head_dim]")
+    n, hq, d = shape
+    if q is None:
+        return dtype, n, 0, hq, d
+    if k is None:
+        return dtype, n, hq, 0, d
+    if k.dim() != 3 or k.shape[0] != n or k.shape[2] != d:
+        raise TypeError("q, k: expected the same tokens and head_dim")
+    return dtype, n, hq, k.shape[1], d
 
 
 _NONE = (0, 0, 0)
 
 
-def _like(t, out, name: str, stream):
-    """An output for vectors t: made here, or the given one of the same shape (which may be strided)."""
-    if t is None:
-        return None, _NONE
-    if out is None:
-        out = _alloc(stream, _empty, t.shape, t.dtype, t.device)
-        return out, (out.data_ptr(), out.shape[1] * out.shape[2], out.shape[2])
+def _given(t, out, name: str):
+    """Pointer and strides of a given output for vectors t, which may be strided."""
     if out.shape != t.shape:
         raise TypeError(f"{name}: expected the shape of the vectors")
     v = _vectors(out, t.dtype, name)
     for size, stride in zip(out.shape[:2], v[1:]):
         if size > 1 and stride == 0:
             raise TypeError(f"{name}: one place for several tokens or heads")
-    return out, v
+    return v
+
+
+def _dense(t, stream):
+    """An output for vectors t, made here: the tensor, its pointer and strides."""
+    o = torch.empty_like(t, memory_format=_DENSE) if stream is None else _alloc(stream, lambda: torch.empty_like(t, memory_format=_DENSE))
+    _, h, d = t.shape
+    return o, (o.data_ptr(), h * d, d)
 
 
 def _aligned(t, stream):
     """Gradients come as autograd makes them: a copy where strides or base are not what the kernels take."""
-    if t is not None and (t.stride(2) != 1 or (t.stride(0) | t.stride(1)) & 7 or t.data_ptr() & 15):
+    if t is None:
+        return t
+    a, b, c = t.stride()
+    if c != 1 or (a | b) & 7 or t.data_ptr() & 15:
         t = _alloc(stream, lambda: t.clone(memory_format=torch.contiguous_format))
     return t
 
@@ -266,11 +284,15 @@ def disc_norm_rope(q, k, positions, inv_freq=None, *, norm: bool = True, q_weigh
     kv = _NONE if k is None else _vectors(k, dtype, "k")
     how = _how(dtype, d, inv_freq, norm, q_weight, k_weight, eps, interleaved)
     pos = _positions(positions, n, inv_freq)
-    q_out, k_out = (None, None) if out is None else out
-    q_out, qo = _like(q, q_out, "out", stream)
-    k_out, ko = _like(k, k_out, "out", stream)
-    _check(lib().disc_norm_rope(C.addressof(how), *qv, *kv, _HALF[dtype], hq, hkv, d, n, pos, *qo, *ko, _stream_ptr(stream)), "disc_norm_rope")
-    return q_out, k_out
+    if out is None:
+        q_out, qo = (None, _NONE) if q is None else _dense(q, stream)
+        k_out, ko = (None, _NONE) if k is None else _dense(k, stream)
+    else:
+        q_out, k_out = out
+        qo, ko = _NONE if q is None else _given(q, q_out, "out"), _NONE if k is None else _given(k, k_out, "out")
+    rc = lib().disc_norm_rope(C.addressof(how), *qv, *kv, _HALF[dtype], hq, hkv, d, n, pos, *qo, *ko, _stream_ptr(stream))
+    _check(rc, "disc_norm_rope")
+    return (q_out if q is not None else None), (k_out if k is not None else None)
 
 
 def disc_norm_rope_grad(q, k, positions, inv_freq, d_q, d_k, *, norm: bool = True, q_weight=None, k_weight=None, eps: float = 1e-6,
@@ -278,38 +300,38 @@ def disc_norm_rope_grad(q, k, positions, inv_freq, d_q, d_k, *, norm: bool = Tru
     """From the gradients d_q, d_k of disc_norm_rope's results those of its inputs: (dq, dk, dq_weight, dk_weight), the weights' in
     float32 (None for a weight that is not given)."""
     dtype, n, hq, hkv, d = _heads(q, k, "disc_norm_rope_grad")
-    for t, x, name in ((q, d_q, "d_q"), (k, d_k, "d_k")):
-        if (t is None) != (x is None) or (t is not None and x.shape != t.shape):
-            raise TypeError(f"{name}: expected the shape of the vectors")
+    if (q is None) != (d_q is None) or (q is not None and d_q.shape != q.shape):
+        raise TypeError("d_q: expected the shape of the queries")
+    if (k is None) != (d_k is None) or (k is not None and d_k.shape != k.shape):
+        raise TypeError("d_k: expected the shape of the keys")
     d_q, d_k = _aligned(d_q, stream), _aligned(d_k, stream)
-    vec = [_NONE if t is None else _vectors(t, dtype, name) for t, name in ((q, "q"), (k, "k"), (d_q, "d_q"), (d_k, "d_k"))]
-    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight"), (inv_freq, "inv_freq")):
-        if w is not None and w.requires_grad:
-            _without_grad(w, name)
+    qv, gqv = (_NONE, _NONE) if q is None else (_vectors(q, dtype, "q"), _vectors(d_q, dtype, "d_q"))
+    kv, gkv = (_NONE, _NONE) if k is None else (_vectors(k, dtype, "k"), _vectors(d_k, dtype, "d_k"))
+    if torch.is_grad_enabled():
+        for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight"), (inv_freq, "inv_freq")):
+            if w is not None and w.requires_grad:
+                _without_grad(w, name)
     how = _how(dtype, d, inv_freq, norm, q_weight, k_weight, eps, interleaved)
     pos = _positions(positions, n, inv_freq)
-    dev = (q if q is not None else k).device
     need = 0
     if q_weight is not None or k_weight is not None:
         need = lib().disc_norm_rope_scratch_bytes(hq, hkv, d, n)
         if need < 0:
             raise DiscError(int(need), "disc_norm_rope_scratch_bytes")
-
-    def outputs():
-        return (None if q is None else torch.empty(q.shape, dtype=dtype, device=dev), None if k is None else torch.empty(k.shape, dtype=dtype, device=dev),
-                None if q_weight is None else torch.empty(d, dtype=_F32, device=dev), None if k_weight is None else torch.empty(d, dtype=_F32, device=dev),
-                torch.empty(need, dtype=torch.uint8, device=dev) if need else None)
-
-    gq, gk, gqw, gkw, scratch = _alloc(stream, outputs)
-    _check(lib().disc_norm_rope_grad(C.addressof(how), *vec[0], *vec[1], _HALF[dtype], hq, hkv, d, n, pos, *vec[2], *vec[3], _own(gq), _own(gk), _own(gqw),
-                                     _own(gkw), _own(scratch), need, _stream_ptr(stream)), "disc_norm_rope_grad")
+    gq, gk, gqw, gkw, scratch = _alloc(stream, _grad_outputs, q, k, q_weight, k_weight, need)
+    _check(lib().disc_norm_rope_grad(C.addressof(how), *qv, *kv, _HALF[dtype], hq, hkv, d, n, pos, *gqv, *gkv, _own(gq), _own(gk), _own(gqw), _own(gkw),
+                                     _own(scratch), need, _stream_ptr(stream)), "disc_norm_rope_grad")
     return gq, gk, gqw, gkw
 
 
+def _grad_outputs(q, k, q_weight, k_weight, need: int):
+    like = torch.empty_like
+    return (None if q is None else like(q, memory_format=_DENSE), None if k is None else like(k, memory_format=_DENSE),
+            None if q_weight is None else like(q_weight, dtype=_F32), None if k_weight is None else like(k_weight, dtype=_F32),
+            torch.empty(need, dtype=torch.uint8, device=(k if q is None else q).device) if need else None)
+
+
 # ---- attention over prompts -------------------------------------------------------------------------
-_F32, _DENSE = torch.float32, torch.contiguous_format
-
-
 def _attend_outputs(q: torch.Tensor, out, lse):
     if out is None:
         out = torch.empty_like(q, memory_format=_DENSE)
@@ -509,16 +531,22 @@ def disc_norm_rope_write(cache: DiscCache, layer: int, q, k: torch.Tensor, v: to
         raise TypeError("k, v: expected [tokens, kv heads, head dim] of the cache")
     if q is not None and (q.shape[0] != n or q.shape[2] != d):
         raise TypeError("q: expected [tokens, Hq, head dim] with the keys' tokens")
-    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight"), (inv_freq, "inv_freq")):
-        if w is not None and w.requires_grad:
-            _without_grad(w, name)
+    if torch.is_grad_enabled():
+        for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight"), (inv_freq, "inv_freq")):
+            if w is not None and w.requires_grad:
+                _without_grad(w, name)
     how = _how(cache.dtype, d, inv_freq, norm, q_weight, k_weight, eps, interleaved)
     n_seqs = n if cu is None else cu.numel() - 1
     if rows is not None:
         _want(rows, n_seqs, "rows")
     _want(status, cache.n_rows, "status")
     _want(positions, n, "positions")
-    out, qo = _like(q, out, "out", stream)
+    if q is None:
+        out, qo = None, _NONE
+    elif out is None:
+        out, qo = _dense(q, stream)
+    else:
+        qo = _given(q, out, "out")
     _check(lib().disc_norm_rope_write(_books(cache), int(layer), C.addressof(how), *qv, hq, *kv, *vv, n, _dev(positions, torch.int32, "positions"),
                                       _dev(cu, torch.int32, "cu"), n_seqs, _dev(rows, torch.int32, "rows"), _dev(status, torch.uint8, "status"), *qo,
                                       _stream_ptr(stream)), "disc_norm_rope_write")
