@@ -22,7 +22,7 @@
 // columns of tensor memory that a block can have with two to an SM.
 
 //
-// A cache held in 8 bits: the loads bring codes and exponents, and two more warps make of them the tiles that the products read, in
+// A cache held in 8 bits: the loads bring codes and exponents, and four more warps make of them the tiles that the products read, in
 // the vectors' type and exactly the values that are held; the products and the softmax are the same.  Kernel 2 takes its blocks as
 // disc_attend_held.cu does.
 
@@ -182,7 +182,10 @@ __global__ void __launch_bounds__(PT) group_items_kernel(const PlanParams p) {
 // ---- kernel 1 -----------------------------------------------------------------------------------------
 template <int DP, int HELD>
 struct Shape {
-    static constexpr int THREADS = HELD ? 256 : 192;
+    // 4 warps of softmax, and one of loads and one of products; held in 8 bits, 4 warps that make tiles come between them, and each four
+    // warps have as many registers as they need: 80 at the launch, then 128, 64 and 48
+    static constexpr int THREADS = HELD ? 384 : 192;
+    static constexpr int LOAD_WARP = HELD ? 8 : 4, MMA_WARP = LOAD_WARP + 1;
     static constexpr int BOXES = DP / BOX;
     static constexpr int BOX_BYTES = TN * BOX * 2;
     static constexpr int TILE_BYTES = BOXES * BOX_BYTES;
@@ -214,11 +217,12 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                  : "memory");
 }
 
-// The first `tokens` rows of a tile out of their codes, by 64 threads: a thread per token.  The codes lie D to a token, the tile as the
-// swizzle of 128 bytes wants it.  Neighbouring threads begin at different chunks: reads and writes then go to different banks.  Dims from D on
-// are zeros (Q is 0 there, and 0 times whatever the memory held may be NaN).
+// The first `tokens` rows of a tile out of their codes, by 128 threads: two to a token, each every other 16 codes.  The codes lie D to a
+// token, the tile as the swizzle of 128 bytes wants it.  In which order a thread takes its codes goes by the token, so that eight
+// neighbouring threads read, and write, all banks.  Dims from D on are zeros (Q is 0 there, and 0 times whatever the memory held may be NaN).
 template <typename T, int DP, int HELD>
-__device__ __forceinline__ void expand_tile(unsigned char* tile, const unsigned char* codes, int tokens, int D, int box_bytes, int t) {
+__device__ __forceinline__ void expand_tile(unsigned char* tile, const unsigned char* codes, int tokens, int D, int box_bytes, int thread) {
+    const int t = thread >> 1, half = thread & 1;
     if (t >= tokens) return;
     const int e = reinterpret_cast<const signed char*>(codes)[TN * DP + t];
     uint32_t scale2;
@@ -226,10 +230,10 @@ __device__ __forceinline__ void expand_tile(unsigned char* tile, const unsigned 
     const float scale = exponent_scale(e);
     unsigned char* row = tile + t * (BOX * 2);
     const unsigned char* from = codes + t * D;
-    constexpr int CH = DP / 16;
+    const int turn = DP == 128 ? (t & 1) << 1 | (t >> 1 & 1) : t >> 1 & 1;
 #pragma unroll
-    for (int j = 0; j < CH; ++j) {
-        const int c = (j + t) % CH;
+    for (int j = 0; j < DP / 32; ++j) {
+        const int c = 2 * (j ^ turn) + half;
         uint32_t x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         if (c * 16 < D) {
             const uint4 w = *reinterpret_cast<const uint4*>(from + c * 16);
@@ -268,11 +272,11 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     if (threadIdx.x == 0) {
         s_abort = 0;
         mbar_init(q_full, 1); mbar_init(q_empty, 1); mbar_init(s_full, 1); mbar_init(o_full, 1); mbar_init(p_full, 4);
-        for (int s = 0; s < S::STAGES; ++s) { mbar_init(kv_full + s, HELD ? 2 : 1); mbar_init(kv_empty + s, 1); }
-        for (int s = 0; s < S::CODE_STAGES; ++s) { mbar_init(code_full + s, 1); mbar_init(code_empty + s, 2); }
+        for (int s = 0; s < S::STAGES; ++s) { mbar_init(kv_full + s, HELD ? 4 : 1); mbar_init(kv_empty + s, 1); }
+        for (int s = 0; s < S::CODE_STAGES; ++s) { mbar_init(code_full + s, 1); mbar_init(code_empty + s, 4); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 5) {
+    if (warp == S::MMA_WARP) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(S::TMEM) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -287,8 +291,9 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     const int lane_of = blockIdx.x / p.kv_heads, head = blockIdx.x % p.kv_heads;
     const int item0 = p.plan.first[lane_of], item1 = p.plan.first[lane_of + 1];
 
-    if (warp >= 4) {
-        if (warp == 4) {
+    if (warp >= S::LOAD_WARP) {
+        if (HELD) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        if (warp == S::LOAD_WARP) {
             // ---- loads
             int load = 0, n = 0;
             bool ok = true;
@@ -343,7 +348,7 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                     }
                 }
             }
-        } else if (warp == 5) {
+        } else if (warp == S::MMA_WARP) {
             // ---- MMAs
             const uint64_t q_desc = smem_desc_sw128(q_tile), kv_desc = smem_desc_sw128(ring), v_desc = smem_desc_n_major(ring, S::BOX_BYTES);
             constexpr uint64_t TILE16 = S::TILE_BYTES >> 4;
@@ -407,30 +412,33 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
             for (int back = 0; back < S::STAGES && back < load && ok; ++back)
                 ok = mbar_wait_all(kv_empty + (load - 1 - back) % S::STAGES, ((load - 1 - back) / S::STAGES) & 1, abort);
             if (ok && n > 0) mbar_wait_all(q_empty, (n - 1) & 1, abort);
-        } else if constexpr (HELD != 0) {
-            // ---- tiles out of codes
-            int load = 0;
-            bool ok = true;
-            for (int n = item0; n < item1 && ok; ++n) {
-                const GroupItem* it = p.plan.group_items + n;
-                const int blks = it->end - it->begin;
-                for (int t = 0; t < blks && ok; t += TILE_BLKS) {
-                    const int tokens = min(TILE_BLKS, blks - t) * BLK;
+        }
+    } else if (HELD != 0 && warp >= 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        // ---- tiles out of codes
+        int load = 0;
+        bool ok = true;
+        for (int n = item0; n < item1 && ok; ++n) {
+            const GroupItem* it = p.plan.group_items + n;
+            const int blks = it->end - it->begin;
+            for (int t = 0; t < blks && ok; t += TILE_BLKS) {
+                const int tokens = min(TILE_BLKS, blks - t) * BLK;
 #pragma unroll 1
-                    for (int kv = 0; kv < 2 && ok; ++kv, ++load) {
-                        const int c = load % S::CODE_STAGES, s = load % S::STAGES, round = load / S::STAGES;
-                        ok = mbar_wait_all(code_full + c, (load / S::CODE_STAGES) & 1, abort);
-                        if (ok && round > 0) ok = mbar_wait_all(kv_empty + s, (round - 1) & 1, abort);
-                        if (!ok) break;
-                        expand_tile<T, DP, HELD>(ring + s * S::TILE_BYTES, code_ring + c * S::CODE_BYTES, tokens, p.D, S::BOX_BYTES, threadIdx.x - 192);
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the products read what has just been written
-                        __syncwarp();
-                        if (lane == 0) { mbar_arrive(kv_full + s); mbar_arrive(code_empty + c); }
-                    }
+                for (int kv = 0; kv < 2 && ok; ++kv, ++load) {
+                    constexpr int CODE_STAGES = HELD ? S::CODE_STAGES : 1;
+                    const int c = load % CODE_STAGES, s = load % S::STAGES, round = load / S::STAGES;
+                    ok = mbar_wait_all(code_full + c, (load / CODE_STAGES) & 1, abort);
+                    if (ok && round > 0) ok = mbar_wait_all(kv_empty + s, (round - 1) & 1, abort);
+                    if (!ok) break;
+                    expand_tile<T, DP, HELD>(ring + s * S::TILE_BYTES, code_ring + c * S::CODE_BYTES, tokens, p.D, S::BOX_BYTES, threadIdx.x - 128);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the products read what has just been written
+                    __syncwarp();
+                    if (lane == 0) { mbar_arrive(kv_full + s); mbar_arrive(code_empty + c); }
                 }
             }
         }
     } else {
+        if (HELD) asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
         // ---- softmax: this thread's query vector
         const int m = warp * 32 + lane;
         const uint32_t lane_bits = uint32_t(warp * 32) << 16;
@@ -449,7 +457,12 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                 if (!ok) break;
                 tc_fence_after();
                 float s[TN];
-                tmem_ld64(s_tm, s);
+                if (HELD) {            // the compiler counts the launch's registers for a single load of 64
+                    tmem_ld32(s_tm, reinterpret_cast<uint32_t*>(s));
+                    tmem_ld32(s_tm + 32, reinterpret_cast<uint32_t*>(s) + 32);
+                } else {
+                    tmem_ld64(s_tm, s);
+                }
                 const int here = min(TILE_BLKS, blks - t) * BLK;
                 if (here < TN) {
 #pragma unroll
@@ -499,7 +512,7 @@ attend_group_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         for (int i = 0; i < 200; ++i) __nanosleep(1000);          // copies in flight land before the memory is given up
     }
     __syncthreads();
-    if (warp == 5) {
+    if (warp == S::MMA_WARP) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::TMEM) : "memory");
     }
@@ -514,7 +527,7 @@ struct JoinSmem {
     static constexpr int BLOCK_BYTES = BLK * DP * 2;
     static constexpr int STEP_BYTES = HELD ? held_stage_bytes<DP>() : 2 * BLOCK_BYTES;     // keys and values of a block
     static constexpr int O_BYTES = HELD ? 8 * O_LD * 4 : 0;        // held in 8 bits a block is smaller than the sums: they have a place of their own
-    static constexpr int WARP_BYTES = 2 * STEP_BYTES + O_BYTES + 256;      // two blocks; maximum and sum of 8 heads
+    static constexpr int WARP_BYTES = (2 * STEP_BYTES + O_BYTES + 256 + 127) / 128 * 128;  // two blocks; maximum and sum of 8 heads
     static_assert(HELD || 8 * O_LD * 4 <= 2 * BLOCK_BYTES, "the sums fit over a block");
 };
 
@@ -600,13 +613,15 @@ __global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p
                 load_held_queries<T, DP, HELD>(qs, 0, p.q + row * p.q_row + (head * G + g0 + (lane >> 2)) * p.q_head, (lane >> 2) < heads, D, p.c2, lane);
                 HeldSums<DP, 1> acc;
                 clear_held(acc);
-                const bool in[1][2] = {{true, true}};
+                const bool in[1][1][2] = {{{true, true}}};
                 for (int i = 0; i < left; ++i, ++step) {
                     __syncwarp();                      // what the next loads overwrite has been read by all lanes
                     load_step(step + 1);
                     cp_wait<1>();
                     __syncwarp();
-                    add_held_block<T, DP, HELD, 1>(acc, qs, smem_u32(own) + (step & 1) * S::STEP_BYTES, min(BLK, len - (begin + i) * BLK), in, lane);
+                    const uint32_t stage[1] = {smem_u32(own) + (step & 1) * S::STEP_BYTES};
+                    const int tokens[1] = {min(BLK, len - (begin + i) * BLK)};
+                    add_held_blocks<T, DP, HELD, 1, 1>(acc, qs, stage, tokens, in, lane);
                 }
                 finish_held(acc);
 #pragma unroll

@@ -7,9 +7,10 @@
 
 namespace disc {
 
-// shared memory of a block: keys [16][DP] | values [16][DP] | exponents of the keys [16] | of the values [16]
+// shared memory of a block: keys [16][DP] | values [16][DP] | exponents of the keys [16] | of the values [16] | the user's, from HELD_SPARE on
+constexpr int HELD_SPARE = 2 * BLK;
 template <int DP>
-__host__ __device__ constexpr int held_stage_bytes() { return 2 * BLK * DP + 2 * BLK; }
+__host__ __device__ constexpr int held_stage_bytes() { return 2 * BLK * DP + 128; }        // on 128-byte boundaries
 
 // 16-byte chunk `ch` of token `row`: neighbouring tokens' chunks lie in different banks, so that ldmatrix reads eight of them at once
 // without conflicts
@@ -18,19 +19,31 @@ __device__ __forceinline__ uint32_t held_chunk_at(int row, int ch) {
     return DP == 128 ? uint32_t(row * 128 + ((ch ^ (row & 7)) << 4)) : uint32_t(row * 64 + ((ch ^ ((row >> 1) & 3)) << 4));
 }
 
-// Block `blk` of a page of which k and v are this head's parts; zeros beyond its tokens and its D values.  By a whole warp.
+// Block `blk` of a page of which k and v are this head's parts; zeros beyond its tokens and its D values.  By a whole warp.  A block's codes
+// are one run of bytes: where it is full and D is DP itself, lane l takes 16 of every 512 bytes.
 template <int DP>
 __device__ __forceinline__ void load_held_block(uint32_t stage, const unsigned char* k, const unsigned char* v, int blk, int tokens, int D, int page_size, int lane) {
     constexpr int CH = DP / 16;
     const int at = blk * BLK * D;
+    const uint32_t to = stage + held_chunk_at<DP>(lane / CH, lane % CH);
+    if (tokens == BLK && D == DP) {
+        const unsigned char *ks = k + at + lane * 16, *vs = v + at + lane * 16;
 #pragma unroll
-    for (int j = 0; j < BLK * CH / 32; ++j) {
-        const int c = j * 32 + lane, row = c / CH, ch = c % CH;
-        const bool some = row < tokens && ch * 16 < D;
-        const int src = some ? at + row * D + ch * 16 : 0;
-        const uint32_t dst = stage + held_chunk_at<DP>(row, ch);
-        cp16(dst, k + src, some);
-        cp16(dst + BLK * DP, v + src, some);
+        for (int j = 0; j < BLK * CH / 32; ++j) {
+            const uint32_t dst = (to ^ (DP == 128 ? uint32_t(j & 1) << 6 : 0u)) + j * 512;        // four tokens on, the banks' turn is 4 further
+            cp16(dst, ks + j * 512, true);
+            cp16(dst + BLK * DP, vs + j * 512, true);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < BLK * CH / 32; ++j) {
+            const int row = (j * 32 + lane) / CH, ch = lane % CH;
+            const bool some = row < tokens && ch * 16 < D;
+            const int src = some ? at + row * D + ch * 16 : 0;
+            const uint32_t dst = (to ^ (DP == 128 ? uint32_t(j & 1) << 6 : 0u)) + j * 512;
+            cp16(dst, k + src, some);
+            cp16(dst + BLK * DP, v + src, some);
+        }
     }
     if (lane < 2) cp16(stage + 2 * BLK * DP + lane * BLK, (lane ? v : k) + page_size * D + blk * BLK, true);
 }
@@ -141,104 +154,131 @@ __device__ __forceinline__ void finish_held(HeldSums<DP, NT>& a) {
             for (int e = 0; e < 2; ++e) a.l[nt][e] += __shfl_xor_sync(0xffffffffu, a.l[nt][e], x);
 }
 
-// in[nt][e]: the block's tokens are seen by this thread's vectors.  Probabilities are rounded to f16 for the second product; where T is
-// f16 what that leaves out goes through a second one, so that the outputs' own rounding stays the larger.
-template <typename T, int DP, int HELD, int NT>
-__device__ __forceinline__ void add_held_block(HeldSums<DP, NT>& acc, const HeldQueries<DP, NT>& qs, uint32_t stage, int tokens, const bool (&in)[NT][2], int lane) {
+// B blocks at a time, of tokens[b] tokens each (none: the block is left out); in[b][nt][e]: the block's tokens are seen by this thread's
+// vectors.  Probabilities are rounded to f16 for the second product; where T is f16 what that leaves out goes through a second one,
+// so that the outputs' own rounding stays the larger.
+template <typename T, int DP, int HELD, int NT, int B>
+__device__ __forceinline__ void add_held_blocks(HeldSums<DP, NT>& acc, const HeldQueries<DP, NT>& qs, const uint32_t (&stage)[B], const int (&tokens)[B],
+                                                const bool (&in)[B][NT][2], int lane) {
     constexpr bool TWO = is_half<T>();
-    // tokens lane / 4 (s[0], s[1]) and 8 further (s[2], s[3]); two chains of products
-    float s[NT][4], s2[NT][4];
+    // scores, and with the values' power of two; tokens lane / 4 ([0], [1]) and 8 further ([2], [3])
+    float s[B][NT][4], w[B][NT][4];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = s2[nt][0] = s2[nt][1] = s2[nt][2] = s2[nt][3] = 0.f;
+    for (int b = 0; b < B; ++b) {
+        float s2[NT][4];               // two chains of products
 #pragma unroll
-    for (int c = 0; c < DP / 32; ++c) {
-        uint32_t kf[4], a[4], b[4];
-        // matrices: tokens 0-7 and 8-15 at chunk 2 c, then at chunk 2 c + 1
-        ldsm4(stage + held_chunk_at<DP>(lane & 15, 2 * c + (lane >> 4)), kf);
-        key_codes<HELD>(kf[0], a[0], a[2]);
-        key_codes<HELD>(kf[1], a[1], a[3]);
-        key_codes<HELD>(kf[2], b[0], b[2]);
-        key_codes<HELD>(kf[3], b[1], b[3]);
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            mma16<__half>(s[nt], a, qs.f[nt][2 * c][0], qs.f[nt][2 * c][1]);
-            mma16<__half>(s2[nt], b, qs.f[nt][2 * c + 1][0], qs.f[nt][2 * c + 1][1]);
+            for (int i = 0; i < 4; ++i) s[b][nt][i] = s2[nt][i] = 0.f;
+#pragma unroll
+        for (int c = 0; c < DP / 32; ++c) {
+            uint32_t kf[4], x[4], y[4];
+            // matrices: tokens 0-7 and 8-15 at chunk 2 c, then at chunk 2 c + 1
+            ldsm4((stage[b] + held_chunk_at<DP>(lane & 15, lane >> 4)) ^ uint32_t(c << 5), kf);
+            key_codes<HELD>(kf[0], x[0], x[2]);
+            key_codes<HELD>(kf[1], x[1], x[3]);
+            key_codes<HELD>(kf[2], y[0], y[2]);
+            key_codes<HELD>(kf[3], y[1], y[3]);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                mma16<__half>(s[b][nt], x, qs.f[nt][2 * c][0], qs.f[nt][2 * c][1]);
+                mma16<__half>(s2[nt], y, qs.f[nt][2 * c + 1][0], qs.f[nt][2 * c + 1][1]);
+            }
         }
-    }
-    const uint32_t exps = stage + 2 * BLK * DP + (lane >> 2);
-    int e[4];                          // keys, values; token lane / 4, 8 further
+        const uint32_t exps = stage[b] + 2 * BLK * DP + (lane >> 2);
+        int e[4];                      // keys, values; token lane / 4, 8 further
 #pragma unroll
-    for (int i = 0; i < 4; ++i) asm volatile("ld.shared.s8 %0, [%1];" : "=r"(e[i]) : "r"(exps + i * 8) : "memory");
-    const float k0 = exponent_scale(e[0]), k1 = exponent_scale(e[1]);
-    const float v0 = e[2] == NAN_EXP ? CUDART_NAN_F : float(e[2]), v1 = e[3] == NAN_EXP ? CUDART_NAN_F : float(e[3]);
-    const bool some0 = (lane >> 2) < tokens, some1 = (lane >> 2) + 8 < tokens;
-    float w[NT][4];
+        for (int i = 0; i < 4; ++i) asm volatile("ld.shared.s8 %0, [%1];" : "=r"(e[i]) : "r"(exps + i * 8) : "memory");
+        const float k0 = exponent_scale(e[0]), k1 = exponent_scale(e[1]);
+        const float v0 = e[2] == NAN_EXP ? CUDART_NAN_F : float(e[2]), v1 = e[3] == NAN_EXP ? CUDART_NAN_F : float(e[3]);
+        const bool some0 = (lane >> 2) < tokens[b], some1 = (lane >> 2) + 8 < tokens[b];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float x = (s[b][nt][i] + s2[nt][i]) * (qs.c2[nt][i] * k0), y = (s[b][nt][2 + i] + s2[nt][2 + i]) * (qs.c2[nt][i] * k1);
+                const bool p = some0 && in[b][nt][i], q = some1 && in[b][nt][i];
+                s[b][nt][i] = p ? x : -CUDART_INF_F;
+                s[b][nt][2 + i] = q ? y : -CUDART_INF_F;
+                w[b][nt][i] = p ? x + v0 : -CUDART_INF_F;
+                w[b][nt][2 + i] = q ? y + v1 : -CUDART_INF_F;
+            }
+    }
     bool move = false;
+    float ms[NT][2], mw[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const float x = (s[nt][i] + s2[nt][i]) * (qs.c2[nt][i] * k0), y = (s[nt][2 + i] + s2[nt][2 + i]) * (qs.c2[nt][i] * k1);
-            const bool a = some0 && in[nt][i], b = some1 && in[nt][i];
-            s[nt][i] = a ? x : -CUDART_INF_F;
-            s[nt][2 + i] = b ? y : -CUDART_INF_F;
-            w[nt][i] = a ? x + v0 : -CUDART_INF_F;
-            w[nt][2 + i] = b ? y + v1 : -CUDART_INF_F;
-            move = move || fmaxf(s[nt][i], s[nt][2 + i]) > acc.m[nt][i] + SLACK || fmaxf(w[nt][i], w[nt][2 + i]) > acc.t[nt][i] + SLACK;
+            ms[nt][i] = fmaxf(s[0][nt][i], s[0][nt][2 + i]);
+            mw[nt][i] = fmaxf(w[0][nt][i], w[0][nt][2 + i]);
+#pragma unroll
+            for (int b = 1; b < B; ++b) {
+                ms[nt][i] = fmaxf(ms[nt][i], fmaxf(s[b][nt][i], s[b][nt][2 + i]));
+                mw[nt][i] = fmaxf(mw[nt][i], fmaxf(w[b][nt][i], w[b][nt][2 + i]));
+            }
+            move = move || ms[nt][i] > acc.m[nt][i] + SLACK || mw[nt][i] > acc.t[nt][i] + SLACK;
         }
     if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                float ms = fmaxf(acc.m[nt][i], fmaxf(s[nt][i], s[nt][2 + i])), mw = fmaxf(acc.t[nt][i], fmaxf(w[nt][i], w[nt][2 + i]));
+                float a = fmaxf(acc.m[nt][i], ms[nt][i]), t = fmaxf(acc.t[nt][i], mw[nt][i]);
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) {
-                    ms = fmaxf(ms, __shfl_xor_sync(0xffffffffu, ms, x));
-                    mw = fmaxf(mw, __shfl_xor_sync(0xffffffffu, mw, x));
+                    a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, x));
+                    t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, x));
                 }
                 // sums without a finite reference so far are 0, or NaN
-                if (acc.m[nt][i] > -CUDART_INF_F) acc.l[nt][i] *= ex2_approx(acc.m[nt][i] - ms);
-                const float f = acc.t[nt][i] > -CUDART_INF_F ? ex2_approx(acc.t[nt][i] - mw) : 1.f;
-                acc.m[nt][i] = ms;
-                acc.t[nt][i] = mw;
+                if (acc.m[nt][i] > -CUDART_INF_F) acc.l[nt][i] *= ex2_approx(acc.m[nt][i] - a);
+                const float f = acc.t[nt][i] > -CUDART_INF_F ? ex2_approx(acc.t[nt][i] - t) : 1.f;
+                acc.m[nt][i] = a;
+                acc.t[nt][i] = t;
 #pragma unroll
                 for (int j = 0; j < DP / 16; ++j) { acc.o[nt][j][i] *= f; acc.o[nt][j][2 + i] *= f; }
             }
     }
-    uint32_t p0[NT], p1[NT], r0[NT], r1[NT];
+    uint32_t p0[B][NT], p1[B][NT], r0[B][NT], r1[B][NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const float m0 = acc.m[nt][0] > -CUDART_INF_F ? acc.m[nt][0] : 0.f, m1 = acc.m[nt][1] > -CUDART_INF_F ? acc.m[nt][1] : 0.f;
         const float t0 = acc.t[nt][0] > -CUDART_INF_F ? acc.t[nt][0] : 0.f, t1 = acc.t[nt][1] > -CUDART_INF_F ? acc.t[nt][1] : 0.f;
-        acc.l[nt][0] += ex2_approx(s[nt][0] - m0) + ex2_approx(s[nt][2] - m0);
-        acc.l[nt][1] += ex2_approx(s[nt][1] - m1) + ex2_approx(s[nt][3] - m1);
-        const float x0 = ex2_approx(w[nt][0] - t0), x1 = ex2_approx(w[nt][1] - t1), x2 = ex2_approx(w[nt][2] - t0), x3 = ex2_approx(w[nt][3] - t1);
-        const uint32_t a = pack2<__half>(x0, x1), b = pack2<__half>(x2, x3);
-        p0[nt] = transposed(a);
-        p1[nt] = transposed(b);
-        if (TWO) {
-            const float2 ra = unpack2<__half>(a), rb = unpack2<__half>(b);
-            r0[nt] = transposed(pack2<__half>(x0 - ra.x, x1 - ra.y));
-            r1[nt] = transposed(pack2<__half>(x2 - rb.x, x3 - rb.y));
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            acc.l[nt][0] += ex2_approx(s[b][nt][0] - m0) + ex2_approx(s[b][nt][2] - m0);
+            acc.l[nt][1] += ex2_approx(s[b][nt][1] - m1) + ex2_approx(s[b][nt][3] - m1);
+            const float x0 = ex2_approx(w[b][nt][0] - t0), x1 = ex2_approx(w[b][nt][1] - t1), x2 = ex2_approx(w[b][nt][2] - t0), x3 = ex2_approx(w[b][nt][3] - t1);
+            const uint32_t p = pack2<__half>(x0, x1), q = pack2<__half>(x2, x3);
+            p0[b][nt] = transposed(p);
+            p1[b][nt] = transposed(q);
+            if (TWO) {
+                const float2 rp = unpack2<__half>(p), rq = unpack2<__half>(q);
+                r0[b][nt] = transposed(pack2<__half>(x0 - rp.x, x1 - rp.y));
+                r1[b][nt] = transposed(pack2<__half>(x2 - rq.x, x3 - rq.y));
+            }
         }
     }
 #pragma unroll
-    for (int j = 0; j < DP / 32; ++j) {
-        uint32_t vf[4], a[4], b[4];
-        // matrices: tokens 0-7 at chunks 2 j and 2 j + 1, then tokens 8-15; each register two dims of two tokens
-        ldsm4t(stage + BLK * DP + held_chunk_at<DP>((lane & 7) + ((lane >> 4) << 3), 2 * j + ((lane >> 3) & 1)), vf);
-        value_codes<HELD>(vf[0], a[0], a[1]);
-        value_codes<HELD>(vf[2], a[2], a[3]);
-        value_codes<HELD>(vf[1], b[0], b[1]);
-        value_codes<HELD>(vf[3], b[2], b[3]);
+    for (int b = 0; b < B; ++b) {
+        if (B > 1 && tokens[b] == 0) continue;     // what its memory holds may be anything, and 0 times that NaN
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            mma16<__half>(acc.o[nt][2 * j], a, p0[nt], p1[nt]);
-            mma16<__half>(acc.o[nt][2 * j + 1], b, p0[nt], p1[nt]);
-            if (TWO) {
-                mma16<__half>(acc.o[nt][2 * j], a, r0[nt], r1[nt]);
-                mma16<__half>(acc.o[nt][2 * j + 1], b, r0[nt], r1[nt]);
+        for (int j = 0; j < DP / 32; ++j) {
+            uint32_t vf[4], x[4], y[4];
+            // matrices: tokens 0-7 at chunks 2 j and 2 j + 1, then tokens 8-15; each register two dims of two tokens
+            ldsm4t((stage[b] + BLK * DP + held_chunk_at<DP>((lane & 7) + ((lane >> 4) << 3), (lane >> 3) & 1)) ^ uint32_t(j << 5), vf);
+            value_codes<HELD>(vf[0], x[0], x[1]);
+            value_codes<HELD>(vf[2], x[2], x[3]);
+            value_codes<HELD>(vf[1], y[0], y[1]);
+            value_codes<HELD>(vf[3], y[2], y[3]);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                mma16<__half>(acc.o[nt][2 * j], x, p0[b][nt], p1[b][nt]);
+                mma16<__half>(acc.o[nt][2 * j + 1], y, p0[b][nt], p1[b][nt]);
+                if (TWO) {
+                    mma16<__half>(acc.o[nt][2 * j], x, r0[b][nt], r1[b][nt]);
+                    mma16<__half>(acc.o[nt][2 * j + 1], y, r0[b][nt], r1[b][nt]);
+                }
             }
         }
     }
