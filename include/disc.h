@@ -547,7 +547,8 @@ int disc_cache_write(const disc_cache_t* c, int32_t layer, const void* k, int64_
 /* Tokens of some rows out of layer `layer`, packed: token t = cu[i] + j of sequence i (row rows[i]; null: row i) is token
  * start[i] + j (null start: j) of its row; places before cu[0] and from cu[n_seqs] on are left as they are.
  *   cu       device, int32[n_seqs+1], ascending, cu[n_seqs] <= n_tokens
- *   k_out, v_out   device, [n_tokens][n_kv_heads][head_dim] contiguous, 32-byte aligned; zeros for tokens the row does not have */
+ *   k_out, v_out   device, [n_tokens][n_kv_heads][head_dim] contiguous, 32-byte aligned; zeros for tokens the row does not have
+ * Errors: DISC_ERR_ARG, DISC_ERR_UNSUPPORTED (also for tokens of more than 2^15 runs of 16 bytes). */
 int disc_cache_read(const disc_cache_t* c, int32_t layer, const int32_t* cu, int32_t n_seqs, const int32_t* rows, const int32_t* start, int64_t n_tokens,
                     void* k_out, void* v_out, void* stream);
 

@@ -537,7 +537,7 @@ struct JoinSmem {
 // next block's loads in flight under the present one's products (78 us without).
 // EXACT: the head dim is DP itself, and all strides and ends along it are known.
 template <typename T, int DP, bool EXACT, int HELD>
-__global__ void __launch_bounds__(JT, 3) attend_join_kernel(const AttendParams p, int heads_per_job) {
+__global__ void __launch_bounds__(JT, HELD ? 4 : 3) attend_join_kernel(const AttendParams p, int heads_per_job) {
     let_later_in();
     wait_for_earlier();
     using S = JoinSmem<DP, HELD>;
@@ -787,7 +787,7 @@ int launch_groups(const AttendParams& a, const CUtensorMap& q, const CUtensorMap
     if (const int rc = allow_smem(attend_join_kernel<T, DP, false, HELD>, join_bytes, done3)) return rc;
     int sms = 0;
     if (const int rc = device_sms(&sms)) return rc;
-    const int64_t places = int64_t(sms) * 3 * (JT / 32), units = int64_t(a.rows) * a.kv_heads;
+    const int64_t places = int64_t(sms) * (HELD ? 4 : 3) * (JT / 32), units = int64_t(a.rows) * a.kv_heads;
     // a warp takes two key heads of a row if that leaves a job for every warp that runs at a time: the row's books are read once
     // and the second head's blocks come in under the first's sums (4096 rows of 4 heads: 120.4 us for plan and attention; one
     // head 124.3, all four 123.4, as the warps are then through 2.3 times)

@@ -3,7 +3,7 @@
 //   disc_cache_fork     row r becomes what row parent[r] was, sharing its pages
 //   disc_cache_free     rows let go of their pages
 //   disc_cache_extend   room for new tokens: free pages, and private copies of shared last pages
-//   disc_cache_write    keys and values of new tokens into the pages (in 8 bits: disc_rope.cu)
+//   disc_cache_write    keys and values of new tokens into the pages
 //   disc_cache_read     tokens of a row back as packed keys and values
 //   disc_cache_compact  the live pages move to the front of the pool
 //
@@ -461,6 +461,84 @@ __global__ void __launch_bounds__(256) cache_write_kernel(Books b, WriteParams w
     }
 }
 
+// The same into 8 bits.  A warp has up to 32 tokens, which its lanes look up side by side, and goes through their heads, LPV lanes with 16
+// values each to a vector, keys and values of two heads of each lane in flight.  Bound by the bytes.
+template <typename T, int LPV, int HELD>
+__global__ void __launch_bounds__(256) cache_write_held_kernel(Books b, WriteParams w, int32_t D, int32_t per_warp, uint32_t of_token) {
+    let_later_in();
+    wait_for_earlier();
+    constexpr int SIDE = 32 / LPV;
+    const int64_t t0 = (int64_t(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5)) * per_warp;
+    const int lane = threadIdx.x & 31, c = lane % LPV;
+    if (t0 >= w.tokens) return;
+    const int n_tokens = int(min(int64_t(per_warp), w.tokens - t0));
+    int32_t my_page = -1, my_off = 0;
+    const int32_t mine = int32_t(t0) + lane;
+    if (lane < n_tokens && (!w.cu || (mine >= w.cu[0] && mine < w.cu[w.n]))) {
+        int32_t seq = mine, back = 1;
+        if (w.cu) {
+            int32_t lo = 0, hi = w.n;
+            while (hi - lo > 1) {
+                const int32_t m = lo + (hi - lo) / 2;
+                if (w.cu[m] <= mine) lo = m; else hi = m;
+            }
+            seq = lo;
+            back = w.cu[lo + 1] - mine;
+        }
+        const int32_t row = w.rows ? w.rows[seq] : seq;
+        if (row >= 0 && row < b.rows && !(w.status && w.status[row])) {
+            const int32_t pos = b.len[row] - back;
+            if (pos >= 0 && (pos >> b.shift) < b.width) {
+                my_page = b.table[size_t(row) * b.width + (pos >> b.shift)];
+                my_off = pos & (b.page_size - 1);
+                if (my_page >= b.pages) my_page = -1;
+            }
+        }
+    }
+    const int all = n_tokens * w.heads;
+    for (int i0 = 0; i0 < all; i0 += 2 * SIDE) {
+        uint4 x[2][2][2];              // step; keys, values; halves of the lane's 16 values
+        int64_t part[2];               // the page and head
+        int32_t place[2];              // in it
+        bool some[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int i = i0 + u * SIDE + lane / LPV, t = min(w.heads == 1 ? i : int(__umulhi(uint32_t(i), of_token)), n_tokens - 1), h = i - t * w.heads;
+            const int32_t page = __shfl_sync(FULL, my_page, t), off = __shfl_sync(FULL, my_off, t);
+            some[u] = i < all && page >= 0 && c * 16 < D;
+            part[u] = (int64_t(max(page, 0)) * w.heads + h) * w.head_bytes;
+            place[u] = off;
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv) {
+                const unsigned char* from = kv ? w.v + (t0 + t) * w.v_token + h * w.v_head : w.k + (t0 + t) * w.k_token + h * w.k_head;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    x[u][kv][e] = make_uint4(0, 0, 0, 0);
+                    if (some[u]) x[u][kv][e] = *reinterpret_cast<const uint4*>(from + c * 32 + e * 16);
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv) {
+                const uint32_t y[8] = {x[u][kv][0].x, x[u][kv][0].y, x[u][kv][0].z, x[u][kv][0].w, x[u][kv][1].x, x[u][kv][1].y, x[u][kv][1].z, x[u][kv][1].w};
+                float inv;
+                const int e = hold_exponent<HELD>(largest_bits<T, LPV, 8>(y), &inv);
+                uint4 code = make_uint4(0, 0, 0, 0);
+                if (e != NAN_EXP) {
+                    code.x = hold4<HELD>(unpack2<T>(y[0]), unpack2<T>(y[1]), inv);
+                    code.y = hold4<HELD>(unpack2<T>(y[2]), unpack2<T>(y[3]), inv);
+                    code.z = hold4<HELD>(unpack2<T>(y[4]), unpack2<T>(y[5]), inv);
+                    code.w = hold4<HELD>(unpack2<T>(y[6]), unpack2<T>(y[7]), inv);
+                }
+                unsigned char* plane = kv ? w.v_plane : w.k_plane;
+                if (some[u]) *reinterpret_cast<uint4*>(plane + part[u] + place[u] * D + c * 16) = code;
+                if (some[u] && c == 0) plane[part[u] + b.page_size * D + place[u]] = uint8_t(e);
+            }
+    }
+}
+
 // ---- read --------------------------------------------------------------------------------------------
 struct ReadParams {
     const unsigned char* k_plane;
@@ -471,60 +549,79 @@ struct ReadParams {
     const int32_t* rows;                        // [n] nullable: sequence i is row i
     const int32_t* start;                       // [n] nullable: from the row's first token
     int32_t n, tokens, heads, D, head_bytes;
+    int32_t per_warp;                           // tokens of a warp, up to 32
+    uint32_t of_token, of_head;                 // 2^32 over the runs of a token's keys, and over those of a vector, rounded up
 };
-// One warp per token: 16 values of a lane at a time, out of 16 codes, or 8 as they are.  Bound by the bytes.
+constexpr int READ_RUNS = 1 << 15;              // of a warp's tokens
+// A warp has up to 32 tokens, which its lanes look up side by side (a token to a warp: 34 us for 40,000 tokens of 4 heads, most of them
+// seven loads that wait for one another), and goes through their vectors in runs of 16 values out of 16 codes, or 8 as they are: two runs of keys
+// and two of values of each lane in flight.  Bound by the bytes.
 template <typename T, int HELD>
 __global__ void __launch_bounds__(256) cache_read_kernel(Books b, ReadParams r) {
     let_later_in();
     wait_for_earlier();
-    const int32_t t = int32_t((int64_t(blockIdx.x) * blockDim.x + threadIdx.x) >> 5);
+    const int64_t t0 = (int64_t(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5)) * r.per_warp;
     const int lane = threadIdx.x & 31;
-    if (t >= r.tokens) return;
-    int32_t page = -1, off = 0;
-    bool asked = false;
-    if (t >= r.cu[0] && t < r.cu[r.n]) {
-        asked = true;
-        int32_t lo = 0, hi = r.n;               // cu[lo] <= t < cu[hi]
+    if (t0 >= r.tokens) return;
+    const int n_tokens = int(min(int64_t(r.per_warp), r.tokens - t0));
+    // the lane's token: its page and the place in it; page -1: zeros, -2: left as it is
+    int32_t my_page = -2, my_off = 0;
+    const int32_t mine = int32_t(t0) + lane;
+    if (lane < n_tokens && mine >= r.cu[0] && mine < r.cu[r.n]) {
+        my_page = -1;
+        int32_t lo = 0, hi = r.n;               // cu[lo] <= mine < cu[hi]
         while (hi - lo > 1) {
             const int32_t m = lo + (hi - lo) / 2;
-            if (r.cu[m] <= t) lo = m; else hi = m;
+            if (r.cu[m] <= mine) lo = m; else hi = m;
         }
         const int32_t row = r.rows ? r.rows[lo] : lo;
-        const int64_t pos = int64_t(r.start ? r.start[lo] : 0) + (t - r.cu[lo]);
+        const int64_t pos = int64_t(r.start ? r.start[lo] : 0) + (mine - r.cu[lo]);
         if (row >= 0 && row < b.rows && pos >= 0 && pos < b.len[row] && (pos >> b.shift) < b.width) {
-            page = b.table[size_t(row) * b.width + (pos >> b.shift)];
-            off = int32_t(pos) & (b.page_size - 1);
-            if (page >= b.pages) page = -1;
+            my_page = b.table[size_t(row) * b.width + (pos >> b.shift)];
+            my_off = int32_t(pos) & (b.page_size - 1);
+            if (my_page < 0 || my_page >= b.pages) my_page = -1;
         }
     }
-    if (!asked) return;
-    constexpr int RUN = HELD ? 16 : 8;          // values of a lane
-    const int runs = r.D / RUN, all = runs * r.heads;
-    const int64_t out0 = int64_t(t) * r.heads * r.D * 2, in0 = int64_t(max(page, 0)) * r.heads * r.head_bytes;
-    for (int i0 = lane; i0 < 2 * all; i0 += 32 * 4) {          // four loads in flight
-        uint4 c[4];
-        int e[4];
+    constexpr int RUN = HELD ? 16 : 8;          // values of a run
+    const int runs = r.D / RUN, of_token = runs * r.heads, all = of_token * n_tokens;
+    const int64_t out0 = t0 * of_token;
+    for (int i0 = 0; i0 < all; i0 += 64) {
+        uint4 k[2], v[2];
+        int ek[2], ev[2], page[2];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int i = i0 + u * 32, j = i >= all ? i - all : i, h = j / runs, x = j - h * runs;
-            c[u] = make_uint4(0, 0, 0, 0);
-            e[u] = 0;
-            if (i >= 2 * all || page < 0) continue;
-            const unsigned char* from = (i >= all ? r.v_plane : r.k_plane) + in0 + int64_t(h) * r.head_bytes;
-            c[u] = *reinterpret_cast<const uint4*>(from + (off * r.D * (HELD ? 1 : 2)) + x * 16);
-            if (HELD) e[u] = reinterpret_cast<const signed char*>(from)[b.page_size * r.D + off];
+        for (int u = 0; u < 2; ++u) {
+            const int i = i0 + u * 32 + lane, t = min(of_token == 1 ? i : int(__umulhi(uint32_t(i), r.of_token)), n_tokens - 1), j = i - t * of_token;
+            const int h = runs == 1 ? j : int(__umulhi(uint32_t(j), r.of_head)), x = j - h * runs;
+            page[u] = __shfl_sync(FULL, my_page, t);
+            const int32_t off = __shfl_sync(FULL, my_off, t);
+            k[u] = v[u] = make_uint4(0, 0, 0, 0);
+            ek[u] = ev[u] = 0;
+            if (i < all && page[u] >= 0) {
+                const int64_t part = (int64_t(page[u]) * r.heads + h) * r.head_bytes;
+                const unsigned char *kp = r.k_plane + part, *vp = r.v_plane + part;
+                const int at = off * r.D * (HELD ? 1 : 2) + x * 16;
+                k[u] = *reinterpret_cast<const uint4*>(kp + at);
+                v[u] = *reinterpret_cast<const uint4*>(vp + at);
+                if (HELD) {
+                    ek[u] = reinterpret_cast<const signed char*>(kp)[b.page_size * r.D + off];
+                    ev[u] = reinterpret_cast<const signed char*>(vp)[b.page_size * r.D + off];
+                }
+            }
+            if (i >= all) page[u] = -2;
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int i = i0 + u * 32, j = i >= all ? i - all : i;
-            if (i >= 2 * all) continue;
-            unsigned char* to = (i >= all ? r.v : r.k) + out0 + int64_t(j) * RUN * 2;
+        for (int u = 0; u < 2; ++u) {
+            if (page[u] == -2) continue;
+            const int64_t to = (out0 + i0 + u * 32 + lane) * (RUN * 2);
             if (HELD) {
                 uint32_t x[8];
-                values16<T, HELD>(c[u], page < 0 ? 0.f : exponent_scale(e[u]), x);
-                st_global32(to, x);
+                any_values16<T, HELD>(k[u], ek[u], x);
+                st_global32(r.k + to, x);
+                any_values16<T, HELD>(v[u], ev[u], x);
+                st_global32(r.v + to, x);
             } else {
-                *reinterpret_cast<uint4*>(to) = c[u];
+                *reinterpret_cast<uint4*>(r.k + to) = k[u];
+                *reinterpret_cast<uint4*>(r.v + to) = v[u];
             }
         }
     }
@@ -635,11 +732,25 @@ __global__ void __launch_bounds__(256) cache_move_kernel(Books b, unsigned char*
     }
 }
 
+// tokens of a warp, at least one: as many as wanted while every SM has 32 warps; a lane looks up one
+int32_t tokens_of_warp(int64_t n_tokens, int64_t wanted, int sms) {
+    const int64_t most = n_tokens / (int64_t(sms) * 32), n = wanted < most ? wanted : most;
+    return int32_t(n < 1 ? 1 : n > 32 ? 32 : n);
+}
+
 int check_cache(const disc_cache_t* c) {
     if (!c || !c->pool || !c->table || !c->len || !c->ref || !c->scratch) return DISC_ERR_ARG;
     if (const int rc = disc::cache_sizes(c)) return rc;
     if (c->scratch_bytes < scratch_layout(c, nullptr)) return DISC_ERR_ARG;
     return DISC_OK;
+}
+
+template <typename T, int HELD>
+auto write_held_kernel(int32_t D) { return D <= 64 ? cache_write_held_kernel<T, 4, HELD> : cache_write_held_kernel<T, 8, HELD>; }
+auto write_held_kernel(const disc_cache_t* c) {
+    const bool bf = cache_type(c) == DISC_BF16;
+    return cache_held(c) == HELD_E4M3 ? (bf ? write_held_kernel<__nv_bfloat16, HELD_E4M3>(c->head_dim) : write_held_kernel<__half, HELD_E4M3>(c->head_dim))
+                                      : (bf ? write_held_kernel<__nv_bfloat16, HELD_I8>(c->head_dim) : write_held_kernel<__half, HELD_I8>(c->head_dim));
 }
 
 Books books(const disc_cache_t* c) {
@@ -736,18 +847,26 @@ int disc_cache_write(const disc_cache_t* c, int32_t layer, const void* k, int64_
     // 16-byte reads: the bases on 16-byte boundaries, the strides multiples of 8 values
     if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15u) return DISC_ERR_ARG;
     if ((k_token_stride | k_head_stride | v_token_stride | v_head_stride) & 7) return DISC_ERR_UNSUPPORTED;
-    if (cache_held(c))
-        return disc::write_held(c, layer, k, k_token_stride, k_head_stride, v, v_token_stride, v_head_stride, int32_t(n_tokens), cu, n_seqs, rows, status,
-                                static_cast<cudaStream_t>(stream));
     WriteParams w;
     w.k = static_cast<const unsigned char*>(k); w.v = static_cast<const unsigned char*>(v);
     w.k_token = k_token_stride * 2; w.k_head = k_head_stride * 2; w.v_token = v_token_stride * 2; w.v_head = v_head_stride * 2;
     w.cu = cu; w.rows = rows; w.status = status; w.n = n_seqs; w.tokens = int32_t(n_tokens);
-    w.heads = c->n_kv_heads; w.token_bytes = c->head_dim * 2; w.head_bytes = c->page_size * w.token_bytes;
-    const int64_t plane = int64_t(c->n_pages) * w.heads * w.head_bytes;
+    w.heads = c->n_kv_heads; w.token_bytes = cache_token_bytes(c); w.head_bytes = cache_head_bytes(c);
+    const int64_t plane = cache_plane_bytes(c);
     w.k_plane = static_cast<unsigned char*>(c->pool) + 2 * int64_t(layer) * plane;
     w.v_plane = w.k_plane + plane;
-    return launch_after(cache_write_kernel, unsigned((n_tokens * 32 + 255) / 256), 256, 0, static_cast<cudaStream_t>(stream), books(c), w);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (cache_held(c)) {
+        // vectors of a warp: quotients of numbers below 2^16
+        if (w.heads > (1 << 11)) return DISC_ERR_UNSUPPORTED;
+        int sms = 0;
+        if (const int rc = device_sms(&sms)) return rc;
+        const int32_t per_warp = tokens_of_warp(n_tokens, 32 / w.heads, sms);
+        const int64_t warps = (n_tokens + per_warp - 1) / per_warp;
+        return launch_after(write_held_kernel(c), unsigned((warps + 7) / 8), 256, 0, st, books(c), w, c->head_dim, per_warp,
+                            uint32_t(((uint64_t(1) << 32) + w.heads - 1) / w.heads));
+    }
+    return launch_after(cache_write_kernel, unsigned((n_tokens * 32 + 255) / 256), 256, 0, st, books(c), w);
 }
 
 int disc_cache_read(const disc_cache_t* c, int32_t layer, const int32_t* cu, int32_t n_seqs, const int32_t* rows, const int32_t* start, int64_t n_tokens,
@@ -764,11 +883,21 @@ int disc_cache_read(const disc_cache_t* c, int32_t layer, const int32_t* cu, int
     r.k = static_cast<unsigned char*>(k_out); r.v = static_cast<unsigned char*>(v_out);
     r.cu = cu; r.rows = rows; r.start = start; r.n = n_seqs; r.tokens = int32_t(n_tokens);
     r.heads = c->n_kv_heads; r.D = c->head_dim; r.head_bytes = cache_head_bytes(c);
+    // quotients of numbers below 2^16: a warp's tokens have READ_RUNS runs together at most
+    const int32_t runs = c->head_dim / (cache_held(c) ? 16 : 8), of_token = runs * c->n_kv_heads;
+    if (int64_t(runs) * c->n_kv_heads > READ_RUNS) return DISC_ERR_UNSUPPORTED;
+    r.of_head = uint32_t(((uint64_t(1) << 32) + runs - 1) / runs);
+    r.of_token = uint32_t(((uint64_t(1) << 32) + of_token - 1) / of_token);
+    int sms = 0;
+    if (const int rc = device_sms(&sms)) return rc;
+    // a warp: 128 runs of keys (twice as many: 57 us for 40,000 tokens of 8 heads instead of 50), fewer where there are not that many tokens
+    r.per_warp = tokens_of_warp(n_tokens, 128 / of_token, sms);
+    const int64_t warps = (n_tokens + r.per_warp - 1) / r.per_warp;
     const bool bf = cache_type(c) == DISC_BF16;
     auto kernel = cache_held(c) == HELD_PLAIN ? cache_read_kernel<__nv_bfloat16, HELD_PLAIN>
                   : cache_held(c) == HELD_E4M3 ? (bf ? cache_read_kernel<__nv_bfloat16, HELD_E4M3> : cache_read_kernel<__half, HELD_E4M3>)
                                                : (bf ? cache_read_kernel<__nv_bfloat16, HELD_I8> : cache_read_kernel<__half, HELD_I8>);
-    return launch_after(kernel, unsigned((n_tokens * 32 + 255) / 256), 256, 0, static_cast<cudaStream_t>(stream), books(c), r);
+    return launch_after(kernel, unsigned((warps + 7) / 8), 256, 0, static_cast<cudaStream_t>(stream), books(c), r);
 }
 
 int disc_cache_compact(const disc_cache_t* c, int32_t* live_out, void* stream) {

@@ -30,6 +30,19 @@ __device__ __forceinline__ int hold_exponent(uint32_t amax_bits, float* inv) {
     *inv = pow2f(-e);
     return e;
 }
+// The bits of the largest |value| of a vector that LPV lanes hold, N words of two values each: found among the 16-bit patterns
+// themselves, two at a time; without their signs they are in order, and infinities and NaN come last.
+template <typename T, int LPV, int N>
+__device__ __forceinline__ uint32_t largest_bits(const uint32_t* y) {
+    constexpr uint32_t ABS = 0x7fff7fffu;
+    uint32_t top = y[0] & ABS;
+#pragma unroll
+    for (int j = 1; j < N; ++j) top = __vmaxu2(top, y[j] & ABS);
+#pragma unroll
+    for (int o = 1; o < LPV; o <<= 1) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float2 f = unpack2<T>(top);
+    return max(__float_as_uint(f.x), __float_as_uint(f.y));
+}
 __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
     float2 d;
     asm("mul.rn.f32x2 %0, %1, %2;"
@@ -154,6 +167,12 @@ __device__ __forceinline__ void fast_values16(const uint4& c, uint32_t scale2, u
         out[2 * i] = mul16x2<T>(pattern2<T, HELD>(w[i], 0x1000u), scale2);                // codes 0 and 1 of the word
         out[2 * i + 1] = mul16x2<T>(pattern2<T, HELD>(w[i], 0x3020u), scale2);            // 2 and 3
     }
+}
+
+template <typename T, int HELD>
+__device__ __forceinline__ void any_values16(const uint4& c, int e, uint32_t* out) {
+    uint32_t scale2;
+    if (fast_scale<T, HELD>(e, &scale2)) fast_values16<T, HELD>(c, scale2, out); else values16<T, HELD>(c, exponent_scale(e), out);
 }
 
 }  // namespace disc

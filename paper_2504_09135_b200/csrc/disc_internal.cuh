@@ -223,10 +223,6 @@ inline int32_t cache_token_bytes(const disc_cache_t* c) { return cache_held(c) ?
 inline int32_t cache_head_bytes(const disc_cache_t* c) { return c->page_size * (cache_token_bytes(c) + (cache_held(c) ? 1 : 0)); }
 inline int64_t cache_plane_bytes(const disc_cache_t* c) { return int64_t(c->n_pages) * c->n_kv_heads * cache_head_bytes(c); }
 
-// Keys and values of new tokens into a cache held in 8 bits (disc_rope.cu); the arguments have been checked.  Strides in values.
-int write_held(const disc_cache_t* c, int32_t layer, const void* k, int64_t k_token, int64_t k_head, const void* v, int64_t v_token, int64_t v_head,
-               int32_t n_tokens, const int32_t* cu, int32_t n_seqs, const int32_t* rows, const uint8_t* status, cudaStream_t st);
-
 // top 23 bits k of a word -> u = (2k+1) * 2^-24, exact in fp32, as is 1-u
 __device__ __forceinline__ float uniform_from_bits(uint32_t r) {
     return float((r >> 9) * 2u + 1u) * 5.9604644775390625e-08f;

@@ -1,6 +1,6 @@
 // Queries and keys on their way to attention: each head's RMS norm and the rotation by the token's position in one pass
 // (disc_norm_rope), its gradient (disc_norm_rope_grad), and, with the keys and values going straight into a cache's pages,
-// disc_norm_rope_write.  The last is also how a cache held in 8 bits is written (disc_cache_write).
+// disc_norm_rope_write.
 //
 //   u = w x r,  r = 1 / sqrt(mean(x^2) + eps);   y_a = u_a cos t_i - u_b sin t_i,  y_b = u_b cos t_i + u_a sin t_i,
 //   t_i = position inv_freq_i,  (a, b) = (i, i + rot / 2) or (2 i, 2 i + 1)
@@ -35,6 +35,7 @@ constexpr int GRAD_BLOCKS = 3;
 constexpr int SMS = 148;
 constexpr int MAX_GRAD_BLOCKS = SMS * GRAD_BLOCKS;     // which each leave sums of their own
 constexpr int MOST_TOKENS = 32;        // of a warp, whose lanes look up one each
+constexpr int MOST_STEPS = 8;
 
 struct Vectors {                       // strides in bytes
     unsigned char* at;
@@ -308,13 +309,9 @@ __device__ __forceinline__ bool share_of(const Cut& cut, const RopeParams& p, in
     return true;
 }
 
-// HELD: -1 without a cache, else how it holds its vectors.  ROPE: there is a norm or a rotation; without, the kernel needs half the registers, and twice
-// as many warps run at a time (65,000 tokens x 16 vectors of 128 into 8 bits: MEASURED).  The largest |value| of a vector is found among the 16-bit patterns
-// themselves, two at a time: without their signs they are in order, and infinities and NaN come last.
-template <bool ROPE>
-__host__ __device__ constexpr int blocks_of() { return ROPE ? BLOCKS : 9; }
-template <typename T, int LPV, int RUN, int HELD, bool ROPE>
-__global__ void __launch_bounds__(THREADS, blocks_of<ROPE>()) norm_rope_kernel(const RopeParams p, const CacheParams w, const Cut cut) {
+// HELD: -1 without a cache, else how it holds its vectors.
+template <typename T, int LPV, int RUN, int HELD>
+__global__ void __launch_bounds__(THREADS, BLOCKS) norm_rope_kernel(const RopeParams p, const CacheParams w, const Cut cut) {
     let_later_in();
     wait_for_earlier();
     constexpr int STEP = step_bytes<RUN>();
@@ -328,7 +325,7 @@ __global__ void __launch_bounds__(THREADS, blocks_of<ROPE>()) norm_rope_kernel(c
     if (!share_of(cut, p, int64_t(blockIdx.x) * WARPS + (threadIdx.x >> 5), SIDE, &sh)) return;
     const int kind = sh.kind;
     const Place at = place_of<RUN>(p, c);
-    const bool rotated = ROPE && p.rot > 0 && kind < 2, normed = ROPE && p.norm && kind < 2;
+    const bool rotated = p.rot > 0 && kind < 2, normed = p.norm && kind < 2;
     const int steps = (sh.h1 - sh.h0 + SIDE - 1) / SIDE;           // of a token
 
     // loads, DEPTH - 1 steps ahead
@@ -431,15 +428,8 @@ __global__ void __launch_bounds__(THREADS, blocks_of<ROPE>()) norm_rope_kernel(c
                 if (real && written) store_raw<RUN>(out + off * w.token_bytes, at, y);
             } else {
                 // what is held is a vector of the type T
-                constexpr uint32_t ABS = 0x7fff7fffu;
-                uint32_t top = y.w[0] & ABS;
-#pragma unroll
-                for (int j = 1; j < RUN; ++j) top = __vmaxu2(top, y.w[j] & ABS);
-#pragma unroll
-                for (int o = 1; o < LPV; o <<= 1) top = __vmaxu2(top, __shfl_xor_sync(FULL, top, o));
-                const float2 tops = unpack2<T>(top);
                 float inv;
-                const int e = hold_exponent<HELD>(max(__float_as_uint(tops.x), __float_as_uint(tops.y)), &inv);
+                const int e = hold_exponent<HELD>(largest_bits<T, LPV, RUN>(y.w), &inv);
                 float2 x[RUN];
                 unpack<T, RUN>(y, x);
                 uint32_t code[RUN / 2];
@@ -622,17 +612,15 @@ __global__ void __launch_bounds__(1024) weight_grad_kernel(const float* part, in
 bool long_runs(int32_t D, int32_t rot) { return D % 16 == 0 && rot % 16 == 0; }
 int side_by_side(int32_t D, int32_t rot) { return (D <= 64 ? 4 : 2) * (long_runs(D, rot) ? 2 : 1); }
 
-// Equal shares of all steps for the warps that run at a time, as long as that is at least two steps and at most `most` (then several
-// shares one after the other): a second round of warps that only few take part in would cost as much as the first (65,000 tokens written
-// in 8 bits by 1.1 times as many warps as run at a time: 129 us).  A share is several tokens, or a part of one.  With norm or
-// rotation small shares in several rounds are better (16 steps: 60 us for 16384 tokens of 40 heads; one round of 55: 69 us); without,
-// where a token is less work than looking up its place, large ones (64 steps: 128 us; 4: 139).
-Cut cut_of(int64_t n, const int32_t* heads, int side, int64_t warps, int64_t most) {
+// Equal shares of all steps for the warps that run at a time, as long as that is at least two steps and at most MOST_STEPS (then several
+// shares one after the other): with many steps the warps that end late are then short ones (16384 tokens x 40 heads: 65 us; with one round of 55
+// steps 69, with 4 steps, half of a token's queries, 73).  A share is several tokens, or a part of one.
+Cut cut_of(int64_t n, const int32_t* heads, int side, int64_t warps) {
     Cut cut = {};
     int64_t steps[3], all = 0, end = 0;
     for (int k = 0; k < 3; ++k) all += n * (steps[k] = (heads[k] + side - 1) / side);
     int64_t share = (all + warps - 1) / warps;
-    share = share < 2 ? 2 : share > most ? most : share;
+    share = share < 2 ? 2 : share > MOST_STEPS ? MOST_STEPS : share;
     for (int k = 0; k < 3; ++k) {
         cut.tokens[k] = cut.per[k] = 1;
         if (steps[k] > 0) {
@@ -649,17 +637,11 @@ Cut cut_of(int64_t n, const int32_t* heads, int side, int64_t warps, int64_t mos
 
 template <typename T, int HELD>
 int launch(const RopeParams& p, const CacheParams& w, cudaStream_t st) {
-    const bool plain = HELD > HELD_PLAIN && !p.norm && p.rot == 0;
-    const Cut cut = cut_of(p.n, p.heads, side_by_side(p.D, p.rot), SMS * WARPS * (plain ? blocks_of<false>() : blocks_of<true>()), plain ? 64 : 16);
+    const Cut cut = cut_of(p.n, p.heads, side_by_side(p.D, p.rot), SMS * WARPS * BLOCKS);
     const int64_t blocks = (cut.end[2] + WARPS - 1) / WARPS;
     if (blocks >= (int64_t(1) << 31)) return DISC_ERR_UNSUPPORTED;
-    if (plain) {
-        // held vectors are made of 16 values
-        auto kernel = p.D <= 64 ? norm_rope_kernel<T, 4, 8, HELD, false> : norm_rope_kernel<T, 8, 8, HELD, false>;
-        return launch_after(kernel, unsigned(blocks), THREADS, 0, st, p, w, cut);
-    }
-    auto kernel = long_runs(p.D, p.rot) ? (p.D <= 64 ? norm_rope_kernel<T, 4, 8, HELD, true> : norm_rope_kernel<T, 8, 8, HELD, true>)
-                                        : (p.D <= 64 ? norm_rope_kernel<T, 8, 4, HELD, true> : norm_rope_kernel<T, 16, 4, HELD, true>);
+    auto kernel = long_runs(p.D, p.rot) ? (p.D <= 64 ? norm_rope_kernel<T, 4, 8, HELD> : norm_rope_kernel<T, 8, 8, HELD>)
+                                        : (p.D <= 64 ? norm_rope_kernel<T, 8, 4, HELD> : norm_rope_kernel<T, 16, 4, HELD>);
     return launch_after(kernel, unsigned(blocks), THREADS, 0, st, p, w, cut);
 }
 template <int HELD>
@@ -743,18 +725,6 @@ GradCut grad_cut(int64_t n, int32_t hq, int32_t hkv, int side) {
 }
 
 }  // namespace
-
-int disc::write_held(const disc_cache_t* c, int32_t layer, const void* k, int64_t k_token, int64_t k_head, const void* v, int64_t v_token, int64_t v_head,
-                     int32_t n_tokens, const int32_t* cu, int32_t n_seqs, const int32_t* rows, const uint8_t* status, cudaStream_t st) {
-    RopeParams p = {};
-    CacheParams w;
-    p.n = n_tokens; p.D = c->head_dim; p.inv_D = 1.f / float(p.D);
-    p.heads[1] = p.heads[2] = c->n_kv_heads;
-    p.x[1] = Vectors{static_cast<unsigned char*>(const_cast<void*>(k)), k_token * 2, k_head * 2};
-    p.x[2] = Vectors{static_cast<unsigned char*>(const_cast<void*>(v)), v_token * 2, v_head * 2};
-    cache_params(c, layer, cu, n_seqs, rows, status, &w);
-    return launch_cache(c, p, w, st);
-}
 
 extern "C" {
 
