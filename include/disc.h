@@ -445,39 +445,42 @@ int disc_attend_error(const uint32_t* error, void* stream);
  *   u = w x / sqrt(mean(x^2) + eps) with `norm` (a null weight counts as 1), u = x without
  *   y_a = u_a cos t_i - u_b sin t_i,  y_b = u_b cos t_i + u_a sin t_i,   t_i = position * inv_freq[i],  i < rot / 2
  * with (a, b) = (i, i + rot/2), or (2i, 2i + 1) with `interleaved`; values from rot on are not rotated.  Rounded once, at the end.
- * Angles are formed in 64 bits less their whole turns: as exact at position 10^6 as at 10. */
+ * Angles are formed less their whole turns, in whole numbers: as exact at position 10^6 as at 10.  Sums of squares are held in
+ * fp32: |x| up to about 10^18.
+ *
+ * The call's arguments, in host memory, read before the call returns; what a call does not mention is not looked at. */
 typedef struct {
-    const float* inv_freq;     /* device, float[rot / 2] (nullable with rot = 0)                        */
-    const void* q_weight;      /* device, head_dim values (nullable), 16-byte aligned                    */
-    const void* k_weight;
-    float eps;                 /* >= 0                                                                   */
-    int32_t rot;               /* a multiple of 8, at most head_dim; 0: no rotation                      */
-    int32_t interleaved, norm; /* 0 or 1                                                                 */
-    int32_t weight_dtype;      /* DISC_F32 or the vectors' type                                          */
-} disc_rope_t;
+    const void *q, *k, *v;     /* device, [n_tokens][heads][head_dim]: token t, head h at element offset t*token + h*head;           */
+    void *q_out, *k_out;       /* bases on 16-byte boundaries, strides multiples of 8 (over an axis of one: any)                     */
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head, q_out_token, q_out_head, k_out_token, k_out_head;
+    const int32_t* positions;  /* device, int32[n_tokens]                                                                            */
+    const float* inv_freq;     /* device, float[rot / 2] (nullable with rot = 0)                                                     */
+    const void *q_weight, *k_weight;   /* device, head_dim values (nullable), 16-byte aligned                                        */
+    int64_t n_tokens;
+    const int32_t *cu, *rows;  /* disc_norm_rope_write: as for disc_cache_write                                                      */
+    const uint8_t* status;
+    int32_t dtype;             /* DISC_BF16 or DISC_F16                                                                              */
+    int32_t n_q_heads, n_kv_heads;     /* 0: without queries, without keys                                                           */
+    int32_t head_dim;          /* a multiple of 8, at most DISC_MAX_HEAD_DIM                                                         */
+    int32_t rot;               /* a multiple of 8, at most head_dim; 0: no rotation                                                  */
+    int32_t interleaved, norm; /* 0 or 1                                                                                             */
+    int32_t weight_dtype;      /* DISC_F32 or the vectors' type                                                                      */
+    float eps;                 /* >= 0                                                                                               */
+    int32_t n_seqs;
+} disc_norm_rope_t;
 
-/* q [n_tokens][n_q_heads][head_dim] -> q_out, k [n_tokens][n_kv_heads][head_dim] -> k_out, by the tokens' positions.
- *   q, k, q_out, k_out   device, bf16 or f16; token t, head h at element offset t*token_stride + h*head_stride; bases on
- *               16-byte boundaries, strides multiples of 8.  An output may be its input (same strides), otherwise must
- *               not overlap it.  Either of q and k may be left out with 0 heads
- *   head_dim    a multiple of 8, at most DISC_MAX_HEAD_DIM
- *   positions   device, int32[n_tokens] (nullable with rot = 0)
- * Sums of squares are held in fp32: |x| up to about 10^18.
+/* q -> q_out, k -> k_out, by the tokens' positions (nullable with rot = 0).  An output may be its input (same strides), otherwise must
+ * not overlap it.
  * Errors: DISC_ERR_ARG, DISC_ERR_UNSUPPORTED (dtype, head_dim, rot, strides, weight_dtype). */
-int disc_norm_rope(const disc_rope_t* how, const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride,
-                   int64_t k_head_stride, disc_dtype_t dtype, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t n_tokens,
-                   const int32_t* positions, void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride, void* k_out,
-                   int64_t k_out_token_stride, int64_t k_out_head_stride, void* stream);
+int disc_norm_rope(const disc_norm_rope_t* a, void* stream);
 
-/* Its gradient: from d_q_out, d_k_out (strides as above, 0 allowed) those of q and k and, where not null, of the weights.
+/* Its gradient: q_out, k_out are the gradients of the results (read; strides of 0 allowed), from which come those of q and k
+ * and, where not null, of the weights.
  *   d_q, d_k    device, [n_tokens][heads][head_dim] contiguous, 16-byte aligned, of the vectors' type; must not overlap any input
  *   d_q_weight, d_k_weight   device, float[head_dim] (nullable; need `norm`): sums in fp32, the same every time
  *   scratch     device, disc_norm_rope_scratch_bytes() bytes, 4-byte aligned (nullable without weight gradients) */
 int64_t disc_norm_rope_scratch_bytes(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t n_tokens);
-int disc_norm_rope_grad(const disc_rope_t* how, const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride,
-                        int64_t k_head_stride, disc_dtype_t dtype, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t n_tokens,
-                        const int32_t* positions, const void* d_q_out, int64_t dq_token_stride, int64_t dq_head_stride, const void* d_k_out,
-                        int64_t dk_token_stride, int64_t dk_head_stride, void* d_q, void* d_k, float* d_q_weight, float* d_k_weight, void* scratch,
+int disc_norm_rope_grad(const disc_norm_rope_t* a, void* d_q, void* d_k, float* d_q_weight, float* d_k_weight, void* scratch,
                         int64_t scratch_bytes, void* stream);
 
 /* ---- the key-value cache ---------------------------------------------------------------------------
@@ -552,15 +555,12 @@ int disc_cache_write(const disc_cache_t* c, int32_t layer, const void* k, int64_
 int disc_cache_read(const disc_cache_t* c, int32_t layer, const int32_t* cu, int32_t n_seqs, const int32_t* rows, const int32_t* start, int64_t n_tokens,
                     void* k_out, void* v_out, void* stream);
 
-/* disc_norm_rope on the newest tokens' queries and keys with the cache's head_dim and type, and disc_cache_write of the resulting
- * keys and of v as they are, in one launch and bit for bit what the two give.
- *   positions   device, int32[n_tokens] (nullable: each token's place in its row, 0 for one that has none)
- *   n_q_heads   may be 0 (no queries)
+/* disc_norm_rope on the newest tokens' queries and keys (n_kv_heads, head_dim and dtype are the cache's), and disc_cache_write of the
+ * resulting keys and of v as they are, in one launch and bit for bit what the two give.
+ *   positions   nullable: each token's place in its row, 0 for one that has none
+ *   k_out       not used
  * cu, n_seqs, rows, status as for disc_cache_write; the queries of tokens that are not written are formed all the same. */
-int disc_norm_rope_write(const disc_cache_t* c, int32_t layer, const disc_rope_t* how, const void* q, int64_t q_token_stride, int64_t q_head_stride,
-                         int32_t n_q_heads, const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,
-                         int64_t v_head_stride, int64_t n_tokens, const int32_t* positions, const int32_t* cu, int32_t n_seqs, const int32_t* rows,
-                         const uint8_t* status, void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride, void* stream);
+int disc_norm_rope_write(const disc_cache_t* c, int32_t layer, const disc_norm_rope_t* a, void* stream);
 
 /* The n pages in use move to the ids 0 .. n-1 (those that are there already stay, the others go to
  * the free ids below n in order), contents of all layers with them.  live_out: device, int32: n. */

@@ -52,11 +52,6 @@ class _Cache(C.Structure):
                 ("table_width", C.c_int32), ("dtype", C.c_int32)]
 
 
-class _Rope(C.Structure):
-    _fields_ = [("inv_freq", C.c_void_p), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("eps", C.c_float), ("rot", C.c_int32),
-                ("interleaved", C.c_int32), ("norm", C.c_int32), ("weight_dtype", C.c_int32)]
-
-
 class _SetInfo(C.Structure):
     _fields_ = [("n_members", C.c_int64), ("n_entries", C.c_int64), ("n_nodes", C.c_int64),
                 ("vocab_size", C.c_int32), ("mask_words", C.c_int32), ("l_max", C.c_int32),
@@ -111,11 +106,10 @@ def lib():
     L.disc_cache_write.argtypes = [vp, i32, vp, i64, i64, vp, i64, i64, i64, vp, i32, vp, vp, vp]
     L.disc_cache_compact.argtypes = [vp, vp, vp]
     L.disc_cache_read.argtypes = [vp, i32, vp, i32, vp, vp, i64, vp, vp, vp]
-    L.disc_norm_rope.argtypes = [vp, vp, i64, i64, vp, i64, i64, C.c_int, i32, i32, i32, i64, vp, vp, i64, i64, vp, i64, i64, vp]
+    L.disc_norm_rope.argtypes = [C.c_char_p, vp]
+    L.disc_norm_rope_write.argtypes = [vp, i32, C.c_char_p, vp]
     L.disc_norm_rope_scratch_bytes.argtypes = [i32, i32, i32, i64]
-    L.disc_norm_rope_grad.argtypes = [vp, vp, i64, i64, vp, i64, i64, C.c_int, i32, i32, i32, i64, vp, vp, i64, i64, vp, i64, i64, vp, vp, vp, vp,
-                                      vp, i64, vp]
-    L.disc_norm_rope_write.argtypes = [vp, i32, vp, vp, i64, i64, i32, vp, i64, i64, vp, i64, i64, i64, vp, vp, i32, vp, vp, vp, i64, i64, vp]
+    L.disc_norm_rope_grad.argtypes = [C.c_char_p, vp, vp, vp, vp, vp, i64, vp]
     L.disc_attend_plan_bytes.argtypes = [vp, i32, i32]
     L.disc_attend_plan.argtypes = [vp, i32, i32, vp, i64, vp]
     L.disc_attend_cached.argtypes = [vp, i32, vp, i64, i64, i32, i32, f32, vp, i64, vp, vp, vp]

@@ -613,15 +613,13 @@ __global__ void __launch_bounds__(JT, HELD ? 4 : 3) attend_join_kernel(const Att
                 load_held_queries<T, DP, HELD>(qs, 0, p.q + row * p.q_row + (head * G + g0 + (lane >> 2)) * p.q_head, (lane >> 2) < heads, D, p.c2, lane);
                 HeldSums<DP, 1> acc;
                 clear_held(acc);
-                const bool in[1][1][2] = {{{true, true}}};
+                const bool in[1][2] = {{true, true}};
                 for (int i = 0; i < left; ++i, ++step) {
                     __syncwarp();                      // what the next loads overwrite has been read by all lanes
                     load_step(step + 1);
                     cp_wait<1>();
                     __syncwarp();
-                    const uint32_t stage[1] = {smem_u32(own) + (step & 1) * S::STEP_BYTES};
-                    const int tokens[1] = {min(BLK, len - (begin + i) * BLK)};
-                    add_held_blocks<T, DP, HELD, 1, 1>(acc, qs, stage, tokens, in, lane);
+                    add_held_block<T, DP, HELD, 1>(acc, qs, smem_u32(own) + (step & 1) * S::STEP_BYTES, min(BLK, len - (begin + i) * BLK), in, lane);
                 }
                 finish_held(acc);
 #pragma unroll

@@ -28,14 +28,11 @@ using namespace disc;
 
 constexpr int AT = 128;
 constexpr int WARPS = AT / 32;
-constexpr int RING_BLKS = 4;           // blocks of 16 tokens on their way to a warp, and those it is at
 
 template <int DP, int NT>
 struct HeldSmem {
-    static constexpr int B = 1;                      // blocks worked on together: as many as the registers have room for
-    static constexpr int STAGES = RING_BLKS / B;
-    static constexpr int BLOCK = held_stage_bytes<DP>();           // in its spare place: the block's tokens and owner
-    static constexpr int STAGE = B * BLOCK;
+    static constexpr int STAGES = DP == 128 ? 4 : 8;               // blocks on their way to a warp, and the one it is at
+    static constexpr int STAGE = held_stage_bytes<DP>();           // in its spare place: the block's tokens and owner
     static constexpr int RING = STAGES * STAGE;                    // of a warp
     static constexpr int SUMS = WARPS * NT * 8 * DP * 4;           // at the end, over the rings
     static constexpr int BYTES = WARPS * RING > SUMS ? WARPS * RING : SUMS;
@@ -46,7 +43,7 @@ __global__ void __launch_bounds__(AT, HELD_BLOCKS) attend_held_kernel(const Atte
     let_later_in();
     wait_for_earlier();
     using S = HeldSmem<DP, NT>;
-    constexpr int STAGES = S::STAGES, STAGE = S::STAGE, B = S::B;
+    constexpr int STAGES = S::STAGES, STAGE = S::STAGE;
     constexpr int CH = DP / 16;                                    // 16-byte chunks of a token's codes
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ float w_m[WARPS][NT * 8], w_l[WARPS][NT * 8], w_t[WARPS][NT * 8];
@@ -67,41 +64,32 @@ __global__ void __launch_bounds__(AT, HELD_BLOCKS) attend_held_kernel(const Atte
         const int2* list = p.plan.list + int64_t(g) * sh.list_ld;
         const int32_t* table = p.table + int64_t(r0) * p.width;
         const int32_t len = p.len[r0];
-        const int steps = (item.z - item.y - warp * B + WARPS * B - 1) / (WARPS * B);        // of this warp: B blocks of every 4 B
+        const int blocks = (item.z - item.y - warp + WARPS - 1) / WARPS;       // of this warp: warp, warp + 4, ...
 
         __syncthreads();                                           // the item before is done with the shared memory
-        struct Entries { int2 e[B]; };
-        auto entries = [&](int t) {
-            Entries x;
-#pragma unroll
-            for (int b = 0; b < B; ++b) {
-                const int i = item.y + (t * WARPS + warp) * B + b;
-                x.e[b] = i >= item.z ? make_int2(0, 0) : sh.per_group > 1 ? list[i]
-                         : make_int2(table[i >> blk_shift], (i & (sh.blks_per_page - 1)) | max(0, min(BLK, len - i * BLK)) << 8);
-            }
-            return x;
+        auto entry = [&](int t) {
+            const int i = item.y + t * WARPS + warp;
+            if (i >= item.z) return make_int2(0, 0);
+            if (sh.per_group > 1) return list[i];
+            return make_int2(table[i >> blk_shift], (i & (sh.blks_per_page - 1)) | max(0, min(BLK, len - i * BLK)) << 8);
         };
-        auto load = [&](uint32_t stage, const Entries& x) {
-#pragma unroll
-            for (int b = 0; b < B; ++b) {
-                int2 e = x.e[b];
-                // a plan older than the books: rows may have let go of their pages since, and -1 is no place to read from
-                if (unsigned(e.x) >= unsigned(p.pages)) e = make_int2(0, 0);
-                const int tokens = (e.y >> 8) & 255;
-                const int64_t off = (int64_t(e.x) * p.kv_heads + head) * p.head_bytes;
-                if (tokens) load_held_block<DP>(ring_at + stage + b * S::BLOCK, p.k + off, p.v + off, e.y & 255, tokens, p.D, p.page_size, lane);
-                if (lane == 0) *reinterpret_cast<volatile int*>(ring + stage + b * S::BLOCK + 2 * BLK * DP + HELD_SPARE) = e.y >> 8;
-            }
+        auto load = [&](uint32_t stage, int2 e) {
+            // a plan older than the books: rows may have let go of their pages since, and -1 is no place to read from
+            if (unsigned(e.x) >= unsigned(p.pages)) e = make_int2(0, 0);
+            const int tokens = (e.y >> 8) & 255;
+            const int64_t off = (int64_t(e.x) * p.kv_heads + head) * p.head_bytes;
+            if (tokens) load_held_block<DP>(ring_at + stage, p.k + off, p.v + off, e.y & 255, tokens, p.D, p.page_size, lane);
+            if (lane == 0) *reinterpret_cast<volatile int*>(ring + stage + 2 * BLK * DP + HELD_SPARE) = e.y >> 8;
         };
-        Entries first[STAGES];
+        int2 first[STAGES];
 #pragma unroll
-        for (int t = 0; t < STAGES; ++t) first[t] = entries(t);
+        for (int t = 0; t < STAGES; ++t) first[t] = entry(t);
 #pragma unroll
         for (int t = 0; t < STAGES - 1; ++t) {
-            if (t < steps) load(t * STAGE, first[t]);
+            if (t < blocks) load(t * STAGE, first[t]);
             cp_commit();
         }
-        Entries next = first[STAGES - 1];
+        int2 next = first[STAGES - 1];
 
         // query vectors: vector m is head m % G of row m / G
         HeldQueries<DP, NT> qs;
@@ -120,26 +108,19 @@ __global__ void __launch_bounds__(AT, HELD_BLOCKS) attend_held_kernel(const Atte
 
         uint32_t stage = 0;
 #pragma unroll 1
-        for (int t = 0; t < steps; ++t) {
+        for (int t = 0; t < blocks; ++t) {
             cp_wait<STAGES - 2>();
             __syncwarp();                                          // a warp works on what it has brought in itself
-            if (t + STAGES - 1 < steps) load(stage == 0 ? (STAGES - 1) * STAGE : stage - STAGE, next);
+            if (t + STAGES - 1 < blocks) load(stage == 0 ? (STAGES - 1) * STAGE : stage - STAGE, next);
             cp_commit();
-            next = entries(t + STAGES);
-            uint32_t at[B];
-            int tokens[B];
-            bool in[B][NT][2];
+            next = entry(t + STAGES);
+            const int meta = *reinterpret_cast<volatile int*>(ring + stage + 2 * BLK * DP + HELD_SPARE), owner = meta >> 8, tokens = meta & 255;
+            bool in[NT][2];
 #pragma unroll
-            for (int b = 0; b < B; ++b) {
-                at[b] = ring_at + stage + b * S::BLOCK;
-                const int meta = *reinterpret_cast<volatile int*>(ring + stage + b * S::BLOCK + 2 * BLK * DP + HELD_SPARE), owner = meta >> 8;
-                tokens[b] = meta & 255;
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) in[b][nt][e] = !owner || owner == owner_of[nt][e];
-            }
-            if (tokens[0] | tokens[B - 1]) add_held_blocks<T, DP, HELD, NT, B>(acc, qs, at, tokens, in, lane);
+                for (int e = 0; e < 2; ++e) in[nt][e] = !owner || owner == owner_of[nt][e];
+            if (tokens) add_held_block<T, DP, HELD, NT>(acc, qs, ring_at + stage, tokens, in, lane);
             stage = stage == (STAGES - 1) * STAGE ? 0 : stage + STAGE;
         }
         finish_held(acc);

@@ -154,69 +154,60 @@ __device__ __forceinline__ void finish_held(HeldSums<DP, NT>& a) {
             for (int e = 0; e < 2; ++e) a.l[nt][e] += __shfl_xor_sync(0xffffffffu, a.l[nt][e], x);
 }
 
-// B blocks at a time, of tokens[b] tokens each (none: the block is left out); in[b][nt][e]: the block's tokens are seen by this thread's
-// vectors.  Probabilities are rounded to f16 for the second product; where T is f16 what that leaves out goes through a second one,
-// so that the outputs' own rounding stays the larger.
-template <typename T, int DP, int HELD, int NT, int B>
-__device__ __forceinline__ void add_held_blocks(HeldSums<DP, NT>& acc, const HeldQueries<DP, NT>& qs, const uint32_t (&stage)[B], const int (&tokens)[B],
-                                                const bool (&in)[B][NT][2], int lane) {
+// A block of some tokens, at least one; in[nt][e]: they are seen by this thread's vectors.  Probabilities are rounded to f16 for the second
+// product; where T is f16 what that leaves out goes through a second one, so that the outputs' own rounding stays the larger.  (Two
+// blocks at a time, for more independent instructions, made no difference: 110 us for the 64 ragged rows both ways.)
+template <typename T, int DP, int HELD, int NT>
+__device__ __forceinline__ void add_held_block(HeldSums<DP, NT>& acc, const HeldQueries<DP, NT>& qs, uint32_t stage, int tokens, const bool (&in)[NT][2], int lane) {
     constexpr bool TWO = is_half<T>();
     // scores, and with the values' power of two; tokens lane / 4 ([0], [1]) and 8 further ([2], [3])
-    float s[B][NT][4], w[B][NT][4];
+    float s[NT][4], w[NT][4];
+    float s2[NT][4];               // two chains of products
 #pragma unroll
-    for (int b = 0; b < B; ++b) {
-        float s2[NT][4];               // two chains of products
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int i = 0; i < 4; ++i) s[nt][i] = s2[nt][i] = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[b][nt][i] = s2[nt][i] = 0.f;
+    for (int c = 0; c < DP / 32; ++c) {
+        uint32_t kf[4], x[4], y[4];
+        // matrices: tokens 0-7 and 8-15 at chunk 2 c, then at chunk 2 c + 1
+        ldsm4((stage + held_chunk_at<DP>(lane & 15, lane >> 4)) ^ uint32_t(c << 5), kf);
+        key_codes<HELD>(kf[0], x[0], x[2]);
+        key_codes<HELD>(kf[1], x[1], x[3]);
+        key_codes<HELD>(kf[2], y[0], y[2]);
+        key_codes<HELD>(kf[3], y[1], y[3]);
 #pragma unroll
-        for (int c = 0; c < DP / 32; ++c) {
-            uint32_t kf[4], x[4], y[4];
-            // matrices: tokens 0-7 and 8-15 at chunk 2 c, then at chunk 2 c + 1
-            ldsm4((stage[b] + held_chunk_at<DP>(lane & 15, lane >> 4)) ^ uint32_t(c << 5), kf);
-            key_codes<HELD>(kf[0], x[0], x[2]);
-            key_codes<HELD>(kf[1], x[1], x[3]);
-            key_codes<HELD>(kf[2], y[0], y[2]);
-            key_codes<HELD>(kf[3], y[1], y[3]);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                mma16<__half>(s[b][nt], x, qs.f[nt][2 * c][0], qs.f[nt][2 * c][1]);
-                mma16<__half>(s2[nt], y, qs.f[nt][2 * c + 1][0], qs.f[nt][2 * c + 1][1]);
-            }
+        for (int nt = 0; nt < NT; ++nt) {
+            mma16<__half>(s[nt], x, qs.f[nt][2 * c][0], qs.f[nt][2 * c][1]);
+            mma16<__half>(s2[nt], y, qs.f[nt][2 * c + 1][0], qs.f[nt][2 * c + 1][1]);
         }
-        const uint32_t exps = stage[b] + 2 * BLK * DP + (lane >> 2);
-        int e[4];                      // keys, values; token lane / 4, 8 further
-#pragma unroll
-        for (int i = 0; i < 4; ++i) asm volatile("ld.shared.s8 %0, [%1];" : "=r"(e[i]) : "r"(exps + i * 8) : "memory");
-        const float k0 = exponent_scale(e[0]), k1 = exponent_scale(e[1]);
-        const float v0 = e[2] == NAN_EXP ? CUDART_NAN_F : float(e[2]), v1 = e[3] == NAN_EXP ? CUDART_NAN_F : float(e[3]);
-        const bool some0 = (lane >> 2) < tokens[b], some1 = (lane >> 2) + 8 < tokens[b];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float x = (s[b][nt][i] + s2[nt][i]) * (qs.c2[nt][i] * k0), y = (s[b][nt][2 + i] + s2[nt][2 + i]) * (qs.c2[nt][i] * k1);
-                const bool p = some0 && in[b][nt][i], q = some1 && in[b][nt][i];
-                s[b][nt][i] = p ? x : -CUDART_INF_F;
-                s[b][nt][2 + i] = q ? y : -CUDART_INF_F;
-                w[b][nt][i] = p ? x + v0 : -CUDART_INF_F;
-                w[b][nt][2 + i] = q ? y + v1 : -CUDART_INF_F;
-            }
     }
+    const uint32_t exps = stage + 2 * BLK * DP + (lane >> 2);
+    int e[4];                          // keys, values; token lane / 4, 8 further
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm volatile("ld.shared.s8 %0, [%1];" : "=r"(e[i]) : "r"(exps + i * 8) : "memory");
+    const float k0 = exponent_scale(e[0]), k1 = exponent_scale(e[1]);
+    const float v0 = e[2] == NAN_EXP ? CUDART_NAN_F : float(e[2]), v1 = e[3] == NAN_EXP ? CUDART_NAN_F : float(e[3]);
+    const bool some0 = (lane >> 2) < tokens, some1 = (lane >> 2) + 8 < tokens;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float x = (s[nt][i] + s2[nt][i]) * (qs.c2[nt][i] * k0), y = (s[nt][2 + i] + s2[nt][2 + i]) * (qs.c2[nt][i] * k1);
+            const bool p = some0 && in[nt][i], q = some1 && in[nt][i];
+            s[nt][i] = p ? x : -CUDART_INF_F;
+            s[nt][2 + i] = q ? y : -CUDART_INF_F;
+            w[nt][i] = p ? x + v0 : -CUDART_INF_F;
+            w[nt][2 + i] = q ? y + v1 : -CUDART_INF_F;
+        }
     bool move = false;
     float ms[NT][2], mw[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            ms[nt][i] = fmaxf(s[0][nt][i], s[0][nt][2 + i]);
-            mw[nt][i] = fmaxf(w[0][nt][i], w[0][nt][2 + i]);
-#pragma unroll
-            for (int b = 1; b < B; ++b) {
-                ms[nt][i] = fmaxf(ms[nt][i], fmaxf(s[b][nt][i], s[b][nt][2 + i]));
-                mw[nt][i] = fmaxf(mw[nt][i], fmaxf(w[b][nt][i], w[b][nt][2 + i]));
-            }
+            ms[nt][i] = fmaxf(s[nt][i], s[nt][2 + i]);
+            mw[nt][i] = fmaxf(w[nt][i], w[nt][2 + i]);
             move = move || ms[nt][i] > acc.m[nt][i] + SLACK || mw[nt][i] > acc.t[nt][i] + SLACK;
         }
     if (__any_sync(0xffffffffu, move)) {
@@ -239,46 +230,39 @@ __device__ __forceinline__ void add_held_blocks(HeldSums<DP, NT>& acc, const Hel
                 for (int j = 0; j < DP / 16; ++j) { acc.o[nt][j][i] *= f; acc.o[nt][j][2 + i] *= f; }
             }
     }
-    uint32_t p0[B][NT], p1[B][NT], r0[B][NT], r1[B][NT];
+    uint32_t p0[NT], p1[NT], r0[NT], r1[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const float m0 = acc.m[nt][0] > -CUDART_INF_F ? acc.m[nt][0] : 0.f, m1 = acc.m[nt][1] > -CUDART_INF_F ? acc.m[nt][1] : 0.f;
         const float t0 = acc.t[nt][0] > -CUDART_INF_F ? acc.t[nt][0] : 0.f, t1 = acc.t[nt][1] > -CUDART_INF_F ? acc.t[nt][1] : 0.f;
-#pragma unroll
-        for (int b = 0; b < B; ++b) {
-            acc.l[nt][0] += ex2_approx(s[b][nt][0] - m0) + ex2_approx(s[b][nt][2] - m0);
-            acc.l[nt][1] += ex2_approx(s[b][nt][1] - m1) + ex2_approx(s[b][nt][3] - m1);
-            const float x0 = ex2_approx(w[b][nt][0] - t0), x1 = ex2_approx(w[b][nt][1] - t1), x2 = ex2_approx(w[b][nt][2] - t0), x3 = ex2_approx(w[b][nt][3] - t1);
-            const uint32_t p = pack2<__half>(x0, x1), q = pack2<__half>(x2, x3);
-            p0[b][nt] = transposed(p);
-            p1[b][nt] = transposed(q);
-            if (TWO) {
-                const float2 rp = unpack2<__half>(p), rq = unpack2<__half>(q);
-                r0[b][nt] = transposed(pack2<__half>(x0 - rp.x, x1 - rp.y));
-                r1[b][nt] = transposed(pack2<__half>(x2 - rq.x, x3 - rq.y));
-            }
+        acc.l[nt][0] += ex2_approx(s[nt][0] - m0) + ex2_approx(s[nt][2] - m0);
+        acc.l[nt][1] += ex2_approx(s[nt][1] - m1) + ex2_approx(s[nt][3] - m1);
+        const float x0 = ex2_approx(w[nt][0] - t0), x1 = ex2_approx(w[nt][1] - t1), x2 = ex2_approx(w[nt][2] - t0), x3 = ex2_approx(w[nt][3] - t1);
+        const uint32_t p = pack2<__half>(x0, x1), q = pack2<__half>(x2, x3);
+        p0[nt] = transposed(p);
+        p1[nt] = transposed(q);
+        if (TWO) {
+            const float2 rp = unpack2<__half>(p), rq = unpack2<__half>(q);
+            r0[nt] = transposed(pack2<__half>(x0 - rp.x, x1 - rp.y));
+            r1[nt] = transposed(pack2<__half>(x2 - rq.x, x3 - rq.y));
         }
     }
 #pragma unroll
-    for (int b = 0; b < B; ++b) {
-        if (B > 1 && tokens[b] == 0) continue;     // what its memory holds may be anything, and 0 times that NaN
+    for (int j = 0; j < DP / 32; ++j) {
+        uint32_t vf[4], x[4], y[4];
+        // matrices: tokens 0-7 at chunks 2 j and 2 j + 1, then tokens 8-15; each register two dims of two tokens
+        ldsm4t((stage + BLK * DP + held_chunk_at<DP>((lane & 7) + ((lane >> 4) << 3), (lane >> 3) & 1)) ^ uint32_t(j << 5), vf);
+        value_codes<HELD>(vf[0], x[0], x[1]);
+        value_codes<HELD>(vf[2], x[2], x[3]);
+        value_codes<HELD>(vf[1], y[0], y[1]);
+        value_codes<HELD>(vf[3], y[2], y[3]);
 #pragma unroll
-        for (int j = 0; j < DP / 32; ++j) {
-            uint32_t vf[4], x[4], y[4];
-            // matrices: tokens 0-7 at chunks 2 j and 2 j + 1, then tokens 8-15; each register two dims of two tokens
-            ldsm4t((stage[b] + BLK * DP + held_chunk_at<DP>((lane & 7) + ((lane >> 4) << 3), (lane >> 3) & 1)) ^ uint32_t(j << 5), vf);
-            value_codes<HELD>(vf[0], x[0], x[1]);
-            value_codes<HELD>(vf[2], x[2], x[3]);
-            value_codes<HELD>(vf[1], y[0], y[1]);
-            value_codes<HELD>(vf[3], y[2], y[3]);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                mma16<__half>(acc.o[nt][2 * j], x, p0[b][nt], p1[b][nt]);
-                mma16<__half>(acc.o[nt][2 * j + 1], y, p0[b][nt], p1[b][nt]);
-                if (TWO) {
-                    mma16<__half>(acc.o[nt][2 * j], x, r0[b][nt], r1[b][nt]);
-                    mma16<__half>(acc.o[nt][2 * j + 1], y, r0[b][nt], r1[b][nt]);
-                }
+        for (int nt = 0; nt < NT; ++nt) {
+            mma16<__half>(acc.o[nt][2 * j], x, p0[nt], p1[nt]);
+            mma16<__half>(acc.o[nt][2 * j + 1], y, p0[nt], p1[nt]);
+            if (TWO) {
+                mma16<__half>(acc.o[nt][2 * j], x, r0[nt], r1[nt]);
+                mma16<__half>(acc.o[nt][2 * j + 1], y, r0[nt], r1[nt]);
             }
         }
     }

@@ -656,20 +656,20 @@ int launch_cache(const disc_cache_t* c, const RopeParams& p, const CacheParams& 
 bool misaligned(const void* x) { return (reinterpret_cast<uintptr_t>(x) & 15u) != 0; }
 
 // what is done to the vectors; DISC_OK and p filled in, or an error
-int check_how(const disc_rope_t* how, disc_dtype_t dtype, int32_t D, RopeParams* p) {
-    if (!how) return DISC_ERR_ARG;
+int check_how(const disc_norm_rope_t* a, int32_t dtype, int32_t D, RopeParams* p) {
     if (dtype != DISC_BF16 && dtype != DISC_F16) return DISC_ERR_UNSUPPORTED;
-    if (D <= 0 || how->rot < 0 || how->rot > D || (how->rot > 0 && !how->inv_freq)) return DISC_ERR_ARG;
-    if (D % 8 || D > DISC_MAX_HEAD_DIM || how->rot % 8) return DISC_ERR_UNSUPPORTED;
-    if (how->norm && !(how->eps >= 0.f && how->eps <= 3.0e38f)) return DISC_ERR_ARG;
-    const bool weights = how->norm && (how->q_weight || how->k_weight);
-    if (weights && how->weight_dtype != DISC_F32 && how->weight_dtype != int32_t(dtype)) return DISC_ERR_UNSUPPORTED;
-    if (weights && (misaligned(how->q_weight) || misaligned(how->k_weight))) return DISC_ERR_ARG;
-    p->D = D; p->rot = how->rot; p->interleaved = how->interleaved != 0; p->norm = how->norm != 0;
-    p->weights_f32 = how->weight_dtype == DISC_F32;
-    p->w[0] = p->norm ? how->q_weight : nullptr; p->w[1] = p->norm ? how->k_weight : nullptr;
+    if (D <= 0 || a->rot < 0 || a->rot > D || (a->rot > 0 && !a->inv_freq)) return DISC_ERR_ARG;
+    if (D % 8 || D > DISC_MAX_HEAD_DIM || a->rot % 8) return DISC_ERR_UNSUPPORTED;
+    if (a->norm && !(a->eps >= 0.f && a->eps <= 3.0e38f)) return DISC_ERR_ARG;
+    const bool weights = a->norm && (a->q_weight || a->k_weight);
+    if (weights && a->weight_dtype != DISC_F32 && a->weight_dtype != dtype) return DISC_ERR_UNSUPPORTED;
+    if (weights && (misaligned(a->q_weight) || misaligned(a->k_weight))) return DISC_ERR_ARG;
+    if (a->n_q_heads < 0 || a->n_q_heads > (1 << 16) || a->n_kv_heads < 0 || a->n_kv_heads > (1 << 16) || a->n_tokens < 0 || a->n_tokens > (int64_t(1) << 30)) return DISC_ERR_ARG;
+    p->D = D; p->rot = a->rot; p->interleaved = a->interleaved != 0; p->norm = a->norm != 0;
+    p->weights_f32 = a->weight_dtype == DISC_F32;
+    p->w[0] = p->norm ? a->q_weight : nullptr; p->w[1] = p->norm ? a->k_weight : nullptr;
     p->inv_D = 1.f / float(D);
-    p->eps = how->eps; p->inv_freq = how->inv_freq;
+    p->eps = a->eps; p->inv_freq = a->inv_freq; p->pos = a->positions; p->n = int32_t(a->n_tokens);
     return DISC_OK;
 }
 // vectors [n][heads][D]: 16-byte boundaries, strides multiples of 8 values
@@ -677,7 +677,6 @@ int check_vectors(const void* x, int64_t token, int64_t head, int64_t n, int32_t
     *v = Vectors{nullptr, 0, 0};
     if (heads == 0) return DISC_OK;
     if (!x || misaligned(x)) return DISC_ERR_ARG;
-    // the stride over an axis of one is never used
     if (n == 1) token = 0;
     if (heads == 1) head = 0;
     if ((token | head) & 7) return DISC_ERR_UNSUPPORTED;
@@ -728,42 +727,39 @@ GradCut grad_cut(int64_t n, int32_t hq, int32_t hkv, int side) {
 
 extern "C" {
 
-int disc_norm_rope(const disc_rope_t* how, const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride,
-                   int64_t k_head_stride, disc_dtype_t dtype, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t n_tokens,
-                   const int32_t* positions, void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride, void* k_out,
-                   int64_t k_out_token_stride, int64_t k_out_head_stride, void* stream) {
+int disc_norm_rope(const disc_norm_rope_t* a, void* stream) {
     RopeParams p = {};
-    if (const int rc = check_how(how, dtype, head_dim, &p)) return rc;
-    if (n_q_heads < 0 || n_kv_heads < 0 || n_q_heads > (1 << 16) || n_kv_heads > (1 << 16) || n_q_heads + n_kv_heads == 0 || n_tokens < 0 || n_tokens > (int64_t(1) << 30)) return DISC_ERR_ARG;
-    if (n_tokens == 0) return DISC_OK;
-    if (p.rot > 0 && !positions) return DISC_ERR_ARG;
-    if (const int rc = check_vectors(q, q_token_stride, q_head_stride, n_tokens, n_q_heads, &p.x[0])) return rc;
-    if (const int rc = check_vectors(k, k_token_stride, k_head_stride, n_tokens, n_kv_heads, &p.x[1])) return rc;
-    if (const int rc = check_vectors(q_out, q_out_token_stride, q_out_head_stride, n_tokens, n_q_heads, &p.y[0])) return rc;
-    if (const int rc = check_vectors(k_out, k_out_token_stride, k_out_head_stride, n_tokens, n_kv_heads, &p.y[1])) return rc;
-    p.n = int32_t(n_tokens); p.heads[0] = n_q_heads; p.heads[1] = n_kv_heads; p.pos = positions;
-    return launch<-1>(dtype, p, CacheParams{}, static_cast<cudaStream_t>(stream));
+    if (!a) return DISC_ERR_ARG;
+    if (const int rc = check_how(a, a->dtype, a->head_dim, &p)) return rc;
+    const int64_t n = a->n_tokens;
+    if (a->n_q_heads + a->n_kv_heads == 0) return DISC_ERR_ARG;
+    if (n == 0) return DISC_OK;
+    if (p.rot > 0 && !a->positions) return DISC_ERR_ARG;
+    if (const int rc = check_vectors(a->q, a->q_token, a->q_head, n, a->n_q_heads, &p.x[0])) return rc;
+    if (const int rc = check_vectors(a->k, a->k_token, a->k_head, n, a->n_kv_heads, &p.x[1])) return rc;
+    if (const int rc = check_vectors(a->q_out, a->q_out_token, a->q_out_head, n, a->n_q_heads, &p.y[0])) return rc;
+    if (const int rc = check_vectors(a->k_out, a->k_out_token, a->k_out_head, n, a->n_kv_heads, &p.y[1])) return rc;
+    p.heads[0] = a->n_q_heads; p.heads[1] = a->n_kv_heads;
+    return launch<-1>(a->dtype, p, CacheParams{}, static_cast<cudaStream_t>(stream));
 }
 
-int disc_norm_rope_write(const disc_cache_t* c, int32_t layer, const disc_rope_t* how, const void* q, int64_t q_token_stride, int64_t q_head_stride,
-                         int32_t n_q_heads, const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,
-                         int64_t v_head_stride, int64_t n_tokens, const int32_t* positions, const int32_t* cu, int32_t n_seqs, const int32_t* rows,
-                         const uint8_t* status, void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride, void* stream) {
-    if (!c || !c->pool || !c->table || !c->len) return DISC_ERR_ARG;
+int disc_norm_rope_write(const disc_cache_t* c, int32_t layer, const disc_norm_rope_t* a, void* stream) {
+    if (!a || !c || !c->pool || !c->table || !c->len) return DISC_ERR_ARG;
     if (const int rc = disc::cache_sizes(c)) return rc;
     RopeParams p = {};
-    if (const int rc = check_how(how, disc_dtype_t(cache_type(c)), c->head_dim, &p)) return rc;
-    if (layer < 0 || layer >= c->n_layers || n_q_heads < 0 || n_q_heads > (1 << 16) || n_tokens < 0 || n_seqs < 0 || n_tokens > (int64_t(1) << 30)) return DISC_ERR_ARG;
-    if (!cu && n_tokens != n_seqs) return DISC_ERR_ARG;
-    if (!rows && n_seqs > c->n_rows) return DISC_ERR_ARG;
-    if (n_tokens == 0 || n_seqs == 0) return DISC_OK;
-    if (const int rc = check_vectors(q, q_token_stride, q_head_stride, n_tokens, n_q_heads, &p.x[0])) return rc;
-    if (const int rc = check_vectors(k, k_token_stride, k_head_stride, n_tokens, c->n_kv_heads, &p.x[1])) return rc;
-    if (const int rc = check_vectors(v, v_token_stride, v_head_stride, n_tokens, c->n_kv_heads, &p.x[2])) return rc;
-    if (const int rc = check_vectors(q_out, q_out_token_stride, q_out_head_stride, n_tokens, n_q_heads, &p.y[0])) return rc;
-    p.n = int32_t(n_tokens); p.heads[0] = n_q_heads; p.heads[1] = p.heads[2] = c->n_kv_heads; p.pos = positions;
+    if (const int rc = check_how(a, cache_type(c), c->head_dim, &p)) return rc;
+    const int64_t n = a->n_tokens;
+    if (layer < 0 || layer >= c->n_layers || a->n_seqs < 0 || a->dtype != cache_type(c) || a->head_dim != c->head_dim || a->n_kv_heads != c->n_kv_heads) return DISC_ERR_ARG;
+    if (!a->cu && n != a->n_seqs) return DISC_ERR_ARG;
+    if (!a->rows && a->n_seqs > c->n_rows) return DISC_ERR_ARG;
+    if (n == 0 || a->n_seqs == 0) return DISC_OK;
+    if (const int rc = check_vectors(a->q, a->q_token, a->q_head, n, a->n_q_heads, &p.x[0])) return rc;
+    if (const int rc = check_vectors(a->k, a->k_token, a->k_head, n, c->n_kv_heads, &p.x[1])) return rc;
+    if (const int rc = check_vectors(a->v, a->v_token, a->v_head, n, c->n_kv_heads, &p.x[2])) return rc;
+    if (const int rc = check_vectors(a->q_out, a->q_out_token, a->q_out_head, n, a->n_q_heads, &p.y[0])) return rc;
+    p.heads[0] = a->n_q_heads; p.heads[1] = p.heads[2] = c->n_kv_heads;
     CacheParams w;
-    cache_params(c, layer, cu, n_seqs, rows, status, &w);
+    cache_params(c, layer, a->cu, a->n_seqs, a->rows, a->status, &w);
     return launch_cache(c, p, w, static_cast<cudaStream_t>(stream));
 }
 
@@ -774,16 +770,14 @@ int64_t disc_norm_rope_scratch_bytes(int32_t n_q_heads, int32_t n_kv_heads, int3
     return int64_t(a > b ? a : b) * head_dim * 4;
 }
 
-int disc_norm_rope_grad(const disc_rope_t* how, const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride,
-                        int64_t k_head_stride, disc_dtype_t dtype, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t n_tokens,
-                        const int32_t* positions, const void* d_q_out, int64_t dq_token_stride, int64_t dq_head_stride, const void* d_k_out,
-                        int64_t dk_token_stride, int64_t dk_head_stride, void* d_q, void* d_k, float* d_q_weight, float* d_k_weight, void* scratch,
-                        int64_t scratch_bytes, void* stream) {
+int disc_norm_rope_grad(const disc_norm_rope_t* a, void* d_q, void* d_k, float* d_q_weight, float* d_k_weight, void* scratch, int64_t scratch_bytes, void* stream) {
     RopeParams p = {};
-    if (const int rc = check_how(how, dtype, head_dim, &p)) return rc;
-    const int64_t need = disc_norm_rope_scratch_bytes(n_q_heads, n_kv_heads, head_dim, n_tokens);
+    if (!a) return DISC_ERR_ARG;
+    if (const int rc = check_how(a, a->dtype, a->head_dim, &p)) return rc;
+    const int32_t head_dim = a->head_dim, n_q_heads = a->n_q_heads, n_kv_heads = a->n_kv_heads;
+    const int64_t n_tokens = a->n_tokens, need = disc_norm_rope_scratch_bytes(n_q_heads, n_kv_heads, head_dim, n_tokens);
     if (need < 0) return int(need);
-    if (n_tokens > 0 && p.rot > 0 && !positions) return DISC_ERR_ARG;
+    if (n_tokens > 0 && p.rot > 0 && !a->positions) return DISC_ERR_ARG;
     const bool weights = d_q_weight || d_k_weight;
     if (weights && (!p.norm || (n_tokens > 0 && (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 3u) || scratch_bytes < need)))) return DISC_ERR_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -792,15 +786,15 @@ int disc_norm_rope_grad(const disc_rope_t* how, const void* q, int64_t q_token_s
         if (d_k_weight) DISC_CUDA(cudaMemsetAsync(d_k_weight, 0, size_t(head_dim) * 4, st));
         return DISC_OK;
     }
-    if (const int rc = check_vectors(q, q_token_stride, q_head_stride, n_tokens, n_q_heads, &p.x[0])) return rc;
-    if (const int rc = check_vectors(k, k_token_stride, k_head_stride, n_tokens, n_kv_heads, &p.x[1])) return rc;
-    if (const int rc = check_vectors(d_q_out, dq_token_stride, dq_head_stride, n_tokens, n_q_heads, &p.y[0])) return rc;
-    if (const int rc = check_vectors(d_k_out, dk_token_stride, dk_head_stride, n_tokens, n_kv_heads, &p.y[1])) return rc;
+    if (const int rc = check_vectors(a->q, a->q_token, a->q_head, n_tokens, n_q_heads, &p.x[0])) return rc;
+    if (const int rc = check_vectors(a->k, a->k_token, a->k_head, n_tokens, n_kv_heads, &p.x[1])) return rc;
+    if (const int rc = check_vectors(a->q_out, a->q_out_token, a->q_out_head, n_tokens, n_q_heads, &p.y[0])) return rc;
+    if (const int rc = check_vectors(a->k_out, a->k_out_token, a->k_out_head, n_tokens, n_kv_heads, &p.y[1])) return rc;
     if ((n_q_heads && (!d_q || misaligned(d_q))) || (n_kv_heads && (!d_k || misaligned(d_k)))) return DISC_ERR_ARG;
-    p.n = int32_t(n_tokens); p.heads[0] = n_q_heads; p.heads[1] = n_kv_heads; p.pos = positions;
+    p.heads[0] = n_q_heads; p.heads[1] = n_kv_heads;
     const GradCut g = grad_cut(n_tokens, n_q_heads, n_kv_heads, side_by_side(head_dim, p.rot));
     float* part = weights ? static_cast<float*>(scratch) : nullptr;
-    const bool bf = dtype == DISC_BF16, small = head_dim <= 64;
+    const bool bf = a->dtype == DISC_BF16, small = head_dim <= 64;
     auto kernel = long_runs(head_dim, p.rot) ? (bf ? (small ? norm_rope_grad_kernel<__nv_bfloat16, 4, 8> : norm_rope_grad_kernel<__nv_bfloat16, 8, 8>)
                                                    : (small ? norm_rope_grad_kernel<__half, 4, 8> : norm_rope_grad_kernel<__half, 8, 8>))
                                              : (bf ? (small ? norm_rope_grad_kernel<__nv_bfloat16, 8, 4> : norm_rope_grad_kernel<__nv_bfloat16, 16, 4>)

@@ -9,10 +9,11 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+import struct
 
 import torch
 
-from .binding import DISC_BF16, DISC_F16, DISC_F32, DISC_HELD_E4M3, DISC_HELD_I8, DiscError, _Cache, _Rope, _check, _dev, _here, _stream_ptr, lib
+from .binding import DISC_BF16, DISC_F16, DISC_F32, DISC_HELD_E4M3, DISC_HELD_I8, DiscError, _Cache, _check, _dev, _here, _stream_ptr, lib
 
 _HALF = {torch.bfloat16: DISC_BF16, torch.float16: DISC_F16}
 _LOGIT = {torch.float32: DISC_F32, torch.bfloat16: DISC_BF16}
@@ -169,12 +170,16 @@ def _weights(dtype, d: int, norm, q_weight, k_weight):
     return _dev(q_weight, wt, "q_weight"), _dev(k_weight, wt, "k_weight"), DISC_F32 if wt is _F32 else _HALF[wt]
 
 
-def _how(dtype, d: int, inv_freq, norm, q_weight, k_weight, eps, interleaved) -> _Rope:
-    """What is done to the vectors, with the checks that need the tensors."""
+def _how(dtype, d: int, inv_freq, norm, q_weight, k_weight, interleaved):
+    """What is done to the vectors, with the checks that need the tensors: the three pointers, then rot, interleaved, norm, weight type."""
     qw, kw, wt = (0, 0, 0) if q_weight is None and k_weight is None else _weights(dtype, d, norm, q_weight, k_weight)
     if inv_freq is None:
-        return _Rope(None, qw, kw, eps, 0, 0, 1 if norm else 0, wt)
-    return _Rope(_dev(inv_freq, _F32, "inv_freq"), qw, kw, eps, 2 * inv_freq.numel(), 1 if interleaved else 0, 1 if norm else 0, wt)
+        return (0, qw, kw), (0, 0, 1 if norm else 0, wt)
+    return (_dev(inv_freq, _F32, "inv_freq"), qw, kw), (2 * inv_freq.numel(), 1 if interleaved else 0, 1 if norm else 0, wt)
+
+
+# disc_norm_rope_t
+_pack_call = struct.Struct("5Q10q4Qq3Q8ifi").pack
 
 
 def _positions(positions, n: int, inv_freq):
@@ -282,7 +287,7 @@ def disc_norm_rope(q, k, positions, inv_freq=None, *, norm: bool = True, q_weigh
     dtype, n, hq, hkv, d = _heads(q, k, "disc_norm_rope")
     qv = _NONE if q is None else _vectors(q, dtype, "q")
     kv = _NONE if k is None else _vectors(k, dtype, "k")
-    how = _how(dtype, d, inv_freq, norm, q_weight, k_weight, eps, interleaved)
+    ptrs, how = _how(dtype, d, inv_freq, norm, q_weight, k_weight, interleaved)
     pos = _positions(positions, n, inv_freq)
     if out is None:
         q_out, qo = (None, _NONE) if q is None else _dense(q, stream)
@@ -290,8 +295,9 @@ def disc_norm_rope(q, k, positions, inv_freq=None, *, norm: bool = True, q_weigh
     else:
         q_out, k_out = out
         qo, ko = _NONE if q is None else _given(q, q_out, "out"), _NONE if k is None else _given(k, k_out, "out")
-    rc = lib().disc_norm_rope(C.addressof(how), *qv, *kv, _HALF[dtype], hq, hkv, d, n, pos, *qo, *ko, _stream_ptr(stream))
-    _check(rc, "disc_norm_rope")
+    call = _pack_call(qv[0], kv[0], 0, qo[0], ko[0], qv[1], qv[2], kv[1], kv[2], 0, 0, qo[1], qo[2], ko[1], ko[2], pos, *ptrs, n, 0, 0, 0,
+                      _HALF[dtype], hq, hkv, d, *how, eps, 0)
+    _check(lib().disc_norm_rope(call, _stream_ptr(stream)), "disc_norm_rope")
     return (q_out if q is not None else None), (k_out if k is not None else None)
 
 
@@ -311,7 +317,7 @@ def disc_norm_rope_grad(q, k, positions, inv_freq, d_q, d_k, *, norm: bool = Tru
         for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight"), (inv_freq, "inv_freq")):
             if w is not None and w.requires_grad:
                 _without_grad(w, name)
-    how = _how(dtype, d, inv_freq, norm, q_weight, k_weight, eps, interleaved)
+    ptrs, how = _how(dtype, d, inv_freq, norm, q_weight, k_weight, interleaved)
     pos = _positions(positions, n, inv_freq)
     need = 0
     if q_weight is not None or k_weight is not None:
@@ -319,8 +325,9 @@ def disc_norm_rope_grad(q, k, positions, inv_freq, d_q, d_k, *, norm: bool = Tru
         if need < 0:
             raise DiscError(int(need), "disc_norm_rope_scratch_bytes")
     gq, gk, gqw, gkw, scratch = _alloc(stream, _grad_outputs, q, k, q_weight, k_weight, need)
-    _check(lib().disc_norm_rope_grad(C.addressof(how), *qv, *kv, _HALF[dtype], hq, hkv, d, n, pos, *gqv, *gkv, _own(gq), _own(gk), _own(gqw), _own(gkw),
-                                     _own(scratch), need, _stream_ptr(stream)), "disc_norm_rope_grad")
+    call = _pack_call(qv[0], kv[0], 0, gqv[0], gkv[0], qv[1], qv[2], kv[1], kv[2], 0, 0, gqv[1], gqv[2], gkv[1], gkv[2], pos, *ptrs, n, 0, 0, 0,
+                      _HALF[dtype], hq, hkv, d, *how, eps, 0)
+    _check(lib().disc_norm_rope_grad(call, _own(gq), _own(gk), _own(gqw), _own(gkw), _own(scratch), need, _stream_ptr(stream)), "disc_norm_rope_grad")
     return gq, gk, gqw, gkw
 
 
@@ -535,7 +542,7 @@ def disc_norm_rope_write(cache: DiscCache, layer: int, q, k: torch.Tensor, v: to
         for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight"), (inv_freq, "inv_freq")):
             if w is not None and w.requires_grad:
                 _without_grad(w, name)
-    how = _how(cache.dtype, d, inv_freq, norm, q_weight, k_weight, eps, interleaved)
+    ptrs, how = _how(cache.dtype, d, inv_freq, norm, q_weight, k_weight, interleaved)
     n_seqs = n if cu is None else cu.numel() - 1
     if rows is not None:
         _want(rows, n_seqs, "rows")
@@ -547,9 +554,10 @@ def disc_norm_rope_write(cache: DiscCache, layer: int, q, k: torch.Tensor, v: to
         out, qo = _dense(q, stream)
     else:
         qo = _given(q, out, "out")
-    _check(lib().disc_norm_rope_write(_books(cache), int(layer), C.addressof(how), *qv, hq, *kv, *vv, n, _dev(positions, torch.int32, "positions"),
-                                      _dev(cu, torch.int32, "cu"), n_seqs, _dev(rows, torch.int32, "rows"), _dev(status, torch.uint8, "status"), *qo,
-                                      _stream_ptr(stream)), "disc_norm_rope_write")
+    call = _pack_call(qv[0], kv[0], vv[0], qo[0], 0, qv[1], qv[2], kv[1], kv[2], vv[1], vv[2], qo[1], qo[2], 0, 0, _dev(positions, torch.int32, "positions"),
+                      *ptrs, n, _dev(cu, torch.int32, "cu"), _dev(rows, torch.int32, "rows"), _dev(status, torch.uint8, "status"),
+                      _HALF[cache.dtype], hq, h, d, *how, eps, n_seqs)
+    _check(lib().disc_norm_rope_write(_books(cache), int(layer), call, _stream_ptr(stream)), "disc_norm_rope_write")
     return out
 
 
