@@ -219,15 +219,15 @@ __device__ __forceinline__ void turn(float2* x, const float2* P, const float2* Q
         }
     }
 }
-// P and Q for weights w: forward, sign 1: y_a = w_a x_a c - w_b x_b s, y_b = w_b x_b c + w_a x_a s; back, sign -1
+// P and Q for weights w: y_a = w_a x_a c - w_b x_b s, y_b = w_b x_b c + w_a x_a s
 template <int RUN>
-__device__ __forceinline__ void coefficients(const Turns& t, int c, const float2* w, bool interleaved, float sign, float2* P, float2* Q) {
+__device__ __forceinline__ void coefficients(const Turns& t, int c, const float2* w, bool interleaved, float2* P, float2* Q) {
     float cs[RUN], sn[RUN];
     read_turns<RUN>(t, c, cs, sn);
     if (interleaved) {
 #pragma unroll
         for (int i = 0; i < RUN; ++i) {
-            const float s = sign * sn[i];
+            const float s = sn[i];
             P[i] = make_float2(w[i].x * cs[i], w[i].y * cs[i]);
             Q[i] = make_float2(-w[i].y * s, w[i].x * s);
         }
@@ -235,11 +235,26 @@ __device__ __forceinline__ void coefficients(const Turns& t, int c, const float2
         constexpr int H = RUN / 2;
 #pragma unroll
         for (int i = 0; i < H; ++i) {
-            const float2 cc = make_float2(cs[2 * i], cs[2 * i + 1]), ss = make_float2(sign * sn[2 * i], sign * sn[2 * i + 1]);
+            const float2 cc = make_float2(cs[2 * i], cs[2 * i + 1]), ss = make_float2(sn[2 * i], sn[2 * i + 1]);
             P[i] = mul2(w[i], cc);
             P[i + H] = mul2(w[i + H], cc);
             Q[i] = mul2(w[i + H], make_float2(-ss.x, -ss.y));
             Q[i + H] = mul2(w[i], ss);
+        }
+    }
+}
+// back by the angles, without weights: half the registers of P and Q
+template <int RUN>
+__device__ __forceinline__ void turn_back(float2* x, const float* cs, const float* sn, bool interleaved) {
+    if (interleaved) {
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) x[i] = fma2(x[i], make_float2(cs[i], cs[i]), mul2(swapped(x[i]), make_float2(sn[i], -sn[i])));
+    } else {
+#pragma unroll
+        for (int i = 0; i < RUN / 2; ++i) {
+            const float2 c = make_float2(cs[2 * i], cs[2 * i + 1]), t = make_float2(sn[2 * i], sn[2 * i + 1]), u = x[i], v = x[i + RUN / 2];
+            x[i] = fma2(u, c, mul2(v, t));
+            x[i + RUN / 2] = fma2(v, c, mul2(u, make_float2(-t.x, -t.y)));
         }
     }
 }
@@ -394,7 +409,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_rope_kernel(const RopePa
                     float2 f[RUN];
                     load_weights<T, RUN>(p, kind, at, f);
                     if (at.turned) {
-                        coefficients<RUN>(turns, c, f, p.interleaved, 1.f, P, Q);
+                        coefficients<RUN>(turns, c, f, p.interleaved, P, Q);
                     } else {
 #pragma unroll
                         for (int j = 0; j < RUN; ++j) P[j] = f[j];
@@ -526,15 +541,10 @@ __global__ void __launch_bounds__(THREADS, GRAD_BLOCKS) norm_rope_grad_kernel(co
     for (int64_t id = first; id < items; id += stride) {
         const int32_t t = int32_t(id / chunks);
         const int h0 = int(id % chunks) * per, h1 = min(heads, h0 + per);
-        float2 P[RUN], Q[RUN];
+        float cs[RUN], sn[RUN];
         if (rotated) {
             turn_to(p, p.pos[t], freq, turns, lane);
-            if (at.turned) {
-                float2 one[RUN];
-#pragma unroll
-                for (int j = 0; j < RUN; ++j) one[j] = make_float2(1.f, 1.f);
-                coefficients<RUN>(turns, c, one, p.interleaved, -1.f, P, Q);
-            }
+            if (at.turned) read_turns<RUN>(turns, c, cs, sn);
         }
         unsigned char* to = (kind ? dk : dq) + (int64_t(t) * heads + h0 + side) * p.D * 2;
         for (int h = h0 + side; h - side < h1; h += SIDE, to += SIDE * p.D * 2) {
@@ -545,7 +555,7 @@ __global__ void __launch_bounds__(THREADS, GRAD_BLOCKS) norm_rope_grad_kernel(co
             unpack<T, RUN>(load_raw<RUN>(mine + STEP, mine + STEP + 32 * RUN * 2), g);
             at_step = at_step == (GRAD_DEPTH - 1) * 2 * STEP ? 0 : at_step + 2 * STEP;
             fetch();
-            if (rotated && at.turned) turn<RUN>(g, P, Q, p.interleaved);
+            if (rotated && at.turned) turn_back<RUN>(g, cs, sn, p.interleaved);
             if (p.norm) {
                 const float r = inverse_norm<LPV, RUN>(p, x);
                 // vectors that are not there are zeros, but 0 times an infinite r (eps = 0) is not
@@ -694,7 +704,7 @@ void cache_params(const disc_cache_t* c, int32_t layer, const int32_t* cu, int32
     w->cu = cu; w->seq_rows = rows; w->status = status; w->n_seqs = n_seqs;
 }
 
-// The gradient's blocks, in proportion to the vectors of each kind.
+// The gradient's blocks for each kind of vectors.
 struct GradCut {
     Cut cut;
     int q_blocks, blocks;
@@ -710,12 +720,16 @@ GradCut grad_cut(int64_t n, int32_t hq, int32_t hkv, int side) {
         g.cut.per[k] = chunks ? int32_t((steps + chunks - 1) / chunks) : 1;
         g.cut.chunks[k] = int32_t((steps + g.cut.per[k] - 1) / g.cut.per[k]);
     }
-    const int64_t all = int64_t(hq) + hkv;
-    int64_t q = hq ? (MAX_GRAD_BLOCKS * int64_t(hq) + all / 2) / all : 0;
-    if (hq && q < 1) q = 1;
-    if (hkv && q > MAX_GRAD_BLOCKS - 1) q = MAX_GRAD_BLOCKS - 1;
+    // the blocks are dealt out so that the kind whose warps end last ends soonest; beginning an item costs as much as a step and a half
+    const int64_t items[2] = {n * g.cut.chunks[0], n * g.cut.chunks[1]}, cost[2] = {2 * g.cut.per[0] + 3, 2 * g.cut.per[1] + 3};
+    int64_t q = hkv ? 0 : MAX_GRAD_BLOCKS, best = int64_t(1) << 62;
+    for (int64_t x = 4; hq && hkv && x < MAX_GRAD_BLOCKS; x += 8) {
+        const int64_t wq = x * WARPS, wk = (MAX_GRAD_BLOCKS - x) * WARPS, cq = (items[0] + wq - 1) / wq * cost[0], ck = (items[1] + wk - 1) / wk * cost[1];
+        const int64_t end = cq > ck ? cq : ck;
+        if (end < best) { best = end; q = x; }
+    }
     int64_t k = hkv ? MAX_GRAD_BLOCKS - q : 0;
-    const int64_t need_q = (n * g.cut.chunks[0] + WARPS - 1) / WARPS, need_k = (n * g.cut.chunks[1] + WARPS - 1) / WARPS;
+    const int64_t need_q = (items[0] + WARPS - 1) / WARPS, need_k = (items[1] + WARPS - 1) / WARPS;
     if (q > need_q) q = need_q;
     if (k > need_k) k = need_k;
     g.q_blocks = int(q);
