@@ -49,7 +49,8 @@ __global__ void __launch_bounds__(AT, HELD_BLOCKS) attend_held_kernel(const Atte
     __shared__ float w_m[WARPS][NT * 8], w_l[WARPS][NT * 8], w_t[WARPS][NT * 8];
     __shared__ int s_last;
 
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    // by shuffle: the compiler then knows that the warp's number is the same for its lanes, and what hangs on it goes through uniform registers
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const PlanShape& sh = p.shape;
     const int G = sh.G, blk_shift = 31 - __clz(sh.blks_per_page);  // pages are powers of two
     const int lane_of = blockIdx.x / p.kv_heads, head = blockIdx.x % p.kv_heads;

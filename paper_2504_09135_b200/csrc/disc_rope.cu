@@ -26,12 +26,12 @@ namespace {
 using namespace disc;
 
 constexpr unsigned FULL = 0xffffffffu;
-constexpr int THREADS = 128;
+constexpr int THREADS = 128;           // of a block of the gradient
 constexpr int WARPS = THREADS / 32;
 constexpr int DEPTH = 6;               // steps of a warp in flight, and the one it is at
 constexpr int GRAD_DEPTH = 4;
-constexpr int BLOCKS = 5;              // on an SM
-constexpr int GRAD_BLOCKS = 3;
+constexpr int FORWARD_WARPS = 20;      // blocks of one warp, on an SM
+constexpr int GRAD_BLOCKS = 3;         // on an SM
 constexpr int SMS = 148;
 constexpr int MAX_GRAD_BLOCKS = SMS * GRAD_BLOCKS;     // which each leave sums of their own
 constexpr int MOST_TOKENS = 32;        // of a warp, whose lanes look up one each
@@ -324,27 +324,26 @@ __device__ __forceinline__ bool share_of(const Cut& cut, const RopeParams& p, in
     return true;
 }
 
-// HELD: -1 without a cache, else how it holds its vectors.
+// HELD: -1 without a cache, else how it holds its vectors.  Blocks of one warp: all that is the same for its lanes then goes by the block's number
+// and through the uniform registers (four warps to a block: 64 us for 16384 tokens x 40 heads instead of 59).
 template <typename T, int LPV, int RUN, int HELD>
-__global__ void __launch_bounds__(THREADS, BLOCKS) norm_rope_kernel(const RopeParams p, const CacheParams w, const Cut cut) {
+__global__ void __launch_bounds__(32, FORWARD_WARPS) norm_rope_kernel(const RopeParams p, const CacheParams w, const Cut cut) {
     let_later_in();
     wait_for_earlier();
     constexpr int STEP = step_bytes<RUN>();
-    __shared__ __align__(16) unsigned char s_ring[WARPS][DEPTH * STEP];
-    __shared__ Turns s_turns[WARPS];
+    __shared__ __align__(16) unsigned char ring[DEPTH * STEP];
+    __shared__ Turns turns;
     constexpr int SIDE = 32 / LPV;     // vectors side by side
     constexpr bool CACHE = HELD >= 0;
-    const int lane = threadIdx.x & 31, c = lane % LPV, side = lane / LPV;
-    Turns& turns = s_turns[threadIdx.x >> 5];
+    const int lane = threadIdx.x, c = lane % LPV, side = lane / LPV;
     Share sh;
-    if (!share_of(cut, p, int64_t(blockIdx.x) * WARPS + (threadIdx.x >> 5), SIDE, &sh)) return;
+    if (!share_of(cut, p, blockIdx.x, SIDE, &sh)) return;
     const int kind = sh.kind;
     const Place at = place_of<RUN>(p, c);
     const bool rotated = p.rot > 0 && kind < 2, normed = p.norm && kind < 2;
     const int steps = (sh.h1 - sh.h0 + SIDE - 1) / SIDE;           // of a token
 
     // loads, DEPTH - 1 steps ahead
-    unsigned char* ring = s_ring[threadIdx.x >> 5];
     const uint32_t ring_at = smem_u32(ring);
     const Vectors src = CACHE ? pick(p.x, kind) : pick2(p.x, kind);
     const unsigned char* in = src.at + sh.t0 * src.token + (sh.h0 + side) * src.head;
@@ -391,84 +390,82 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_rope_kernel(const RopePa
     int h = sh.h1 + side;              // at a token's end: the next begins
     int from = -1;                     // which of the warp's tokens
     for (int todo = sh.tokens * steps; todo > 0; --todo) {
-        {
-            if (h - side >= sh.h1) {
-                ++from;
-                h = sh.h0 + side;
-                if (to_cache) {
-                    const int32_t page = __shfl_sync(FULL, spots.page, from);
-                    off = __shfl_sync(FULL, spots.off, from);
-                    written = page >= 0;
-                    out = plane + max(page, 0) * page_bytes + first_out;
-                } else {
-                    out = dst.at + (int64_t(sh.t0) + from) * dst.token + first_out;
-                }
-                if (rotated) turn_to(p, __shfl_sync(FULL, spots.pos, from), freq, turns, lane);
-                // what the weights and the angles come to, where they change
-                if (rotated || (normed && from == 0)) {
-                    float2 f[RUN];
-                    load_weights<T, RUN>(p, kind, at, f);
-                    if (at.turned) {
-                        coefficients<RUN>(turns, c, f, p.interleaved, P, Q);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < RUN; ++j) P[j] = f[j];
-                    }
-                }
-            }
-            wait_for_all_but<DEPTH - 2>();
-            Raw<RUN> y = load_raw<RUN>(ring + at_step + lane * (RUN * 2), ring + at_step + (32 + lane) * (RUN * 2));
-            at_step = at_step == (DEPTH - 1) * STEP ? 0 : at_step + STEP;
-            fetch();
-            if (normed || rotated) {
-                float2 x[RUN];
-                unpack<T, RUN>(y, x);
-                if (normed) {
-                    const float r = inverse_norm<LPV, RUN>(p, x);
-#pragma unroll
-                    for (int j = 0; j < RUN; ++j) x[j] = mul2(x[j], make_float2(r, r));
-                }
-                if (at.turned && rotated) {
-                    turn<RUN>(x, P, Q, p.interleaved);
-                } else if (normed) {
-#pragma unroll
-                    for (int j = 0; j < RUN; ++j) x[j] = mul2(x[j], P[j]);
-                }
-                y = pack<T, RUN>(x);
-            }
-            const bool real = h < sh.h1 && at.some;
-            if (!to_cache) {
-                if (real) store_raw<RUN>(out, at, y);
-            } else if (HELD <= HELD_PLAIN) {
-                if (real && written) store_raw<RUN>(out + off * w.token_bytes, at, y);
+        if (h - side >= sh.h1) {
+            ++from;
+            h = sh.h0 + side;
+            if (to_cache) {
+                const int32_t page = __shfl_sync(FULL, spots.page, from);
+                off = __shfl_sync(FULL, spots.off, from);
+                written = page >= 0;
+                out = plane + max(page, 0) * page_bytes + first_out;
             } else {
-                // what is held is a vector of the type T
-                float inv;
-                const int e = hold_exponent<HELD>(largest_bits<T, LPV, RUN>(y.w), &inv);
-                float2 x[RUN];
-                unpack<T, RUN>(y, x);
-                uint32_t code[RUN / 2];
+                out = dst.at + (int64_t(sh.t0) + from) * dst.token + first_out;
+            }
+            if (rotated) turn_to(p, __shfl_sync(FULL, spots.pos, from), freq, turns, lane);
+            // what the weights and the angles come to, where they change
+            if (rotated || (normed && from == 0)) {
+                float2 f[RUN];
+                load_weights<T, RUN>(p, kind, at, f);
+                if (at.turned) {
+                    coefficients<RUN>(turns, c, f, p.interleaved, P, Q);
+                } else {
 #pragma unroll
-                for (int j = 0; j < RUN / 2; ++j) code[j] = hold4<HELD>(x[2 * j], x[2 * j + 1], inv);
-                if (e == NAN_EXP) {
-#pragma unroll
-                    for (int j = 0; j < RUN / 2; ++j) code[j] = 0;
-                }
-                if (real && written) {
-                    unsigned char* to = out + off * p.D;
-                    if constexpr (RUN == 8) {
-                        *reinterpret_cast<uint2*>(to + at.a) = make_uint2(code[0], code[1]);
-                        *reinterpret_cast<uint2*>(to + at.b) = make_uint2(code[2], code[3]);
-                    } else {
-                        *reinterpret_cast<uint32_t*>(to + at.a) = code[0];
-                        *reinterpret_cast<uint32_t*>(to + at.b) = code[1];
-                    }
-                    if (c == 0) out[w.page_size * p.D + off] = uint8_t(e);
+                    for (int j = 0; j < RUN; ++j) P[j] = f[j];
                 }
             }
-            h += SIDE;
-            out += out_step;
         }
+        wait_for_all_but<DEPTH - 2>();
+        Raw<RUN> y = load_raw<RUN>(ring + at_step + lane * (RUN * 2), ring + at_step + (32 + lane) * (RUN * 2));
+        at_step = at_step == (DEPTH - 1) * STEP ? 0 : at_step + STEP;
+        fetch();
+        if (normed || rotated) {
+            float2 x[RUN];
+            unpack<T, RUN>(y, x);
+            if (normed) {
+                const float r = inverse_norm<LPV, RUN>(p, x);
+#pragma unroll
+                for (int j = 0; j < RUN; ++j) x[j] = mul2(x[j], make_float2(r, r));
+            }
+            if (at.turned && rotated) {
+                turn<RUN>(x, P, Q, p.interleaved);
+            } else if (normed) {
+#pragma unroll
+                for (int j = 0; j < RUN; ++j) x[j] = mul2(x[j], P[j]);
+            }
+            y = pack<T, RUN>(x);
+        }
+        const bool real = h < sh.h1 && at.some;
+        if (!to_cache) {
+            if (real) store_raw<RUN>(out, at, y);
+        } else if (HELD <= HELD_PLAIN) {
+            if (real && written) store_raw<RUN>(out + off * w.token_bytes, at, y);
+        } else {
+            // what is held is a vector of the type T
+            float inv;
+            const int e = hold_exponent<HELD>(largest_bits<T, LPV, RUN>(y.w), &inv);
+            float2 x[RUN];
+            unpack<T, RUN>(y, x);
+            uint32_t code[RUN / 2];
+#pragma unroll
+            for (int j = 0; j < RUN / 2; ++j) code[j] = hold4<HELD>(x[2 * j], x[2 * j + 1], inv);
+            if (e == NAN_EXP) {
+#pragma unroll
+                for (int j = 0; j < RUN / 2; ++j) code[j] = 0;
+            }
+            if (real && written) {
+                unsigned char* to = out + off * p.D;
+                if constexpr (RUN == 8) {
+                    *reinterpret_cast<uint2*>(to + at.a) = make_uint2(code[0], code[1]);
+                    *reinterpret_cast<uint2*>(to + at.b) = make_uint2(code[2], code[3]);
+                } else {
+                    *reinterpret_cast<uint32_t*>(to + at.a) = code[0];
+                    *reinterpret_cast<uint32_t*>(to + at.b) = code[1];
+                }
+                if (c == 0) out[w.page_size * p.D + off] = uint8_t(e);
+            }
+        }
+        h += SIDE;
+        out += out_step;
     }
 }
 
@@ -485,7 +482,7 @@ __global__ void __launch_bounds__(THREADS, GRAD_BLOCKS) norm_rope_grad_kernel(co
     __shared__ Turns s_turns[WARPS];
     __shared__ float sums[WARPS][128];
     constexpr int SIDE = 32 / LPV;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane % LPV, side = lane / LPV;
+    const int lane = threadIdx.x & 31, warp = __shfl_sync(FULL, int(threadIdx.x >> 5), 0), c = lane % LPV, side = lane / LPV;
     Turns& turns = s_turns[warp];
     const Place at = place_of<RUN>(p, c);
     const int kind = int(blockIdx.x) < q_blocks ? 0 : 1, heads = kind ? p.heads[1] : p.heads[0];
@@ -647,12 +644,11 @@ Cut cut_of(int64_t n, const int32_t* heads, int side, int64_t warps) {
 
 template <typename T, int HELD>
 int launch(const RopeParams& p, const CacheParams& w, cudaStream_t st) {
-    const Cut cut = cut_of(p.n, p.heads, side_by_side(p.D, p.rot), SMS * WARPS * BLOCKS);
-    const int64_t blocks = (cut.end[2] + WARPS - 1) / WARPS;
-    if (blocks >= (int64_t(1) << 31)) return DISC_ERR_UNSUPPORTED;
+    const Cut cut = cut_of(p.n, p.heads, side_by_side(p.D, p.rot), SMS * FORWARD_WARPS);
+    if (cut.end[2] >= (int64_t(1) << 31)) return DISC_ERR_UNSUPPORTED;
     auto kernel = long_runs(p.D, p.rot) ? (p.D <= 64 ? norm_rope_kernel<T, 4, 8, HELD> : norm_rope_kernel<T, 8, 8, HELD>)
                                         : (p.D <= 64 ? norm_rope_kernel<T, 8, 4, HELD> : norm_rope_kernel<T, 16, 4, HELD>);
-    return launch_after(kernel, unsigned(blocks), THREADS, 0, st, p, w, cut);
+    return launch_after(kernel, unsigned(cut.end[2]), 32, 0, st, p, w, cut);
 }
 template <int HELD>
 int launch(int type, const RopeParams& p, const CacheParams& w, cudaStream_t st) {
