@@ -11,7 +11,8 @@ constexpr int GROUP_M = 128;           // query vectors that a group can have at
 constexpr int G_MAX = 64;              // query heads per key head
 constexpr int START = 8;               // what beginning an item costs, in blocks
 constexpr int PLACES = 148 * 2;        // blocks that run at a time: two to an SM
-constexpr int HELD_BLOCKS = 3;         // rows form over a cache held in 8 bits: three
+constexpr int HELD_BLOCKS = 3;         // rows form over a cache held in 8 bits, up to HELD_FEW query vectors: three
+constexpr int HELD_FEW = 8;
 
 struct PlanShape {
     int32_t G;                         // query heads per key head
@@ -70,7 +71,7 @@ inline int plan_shape(const disc_cache_t* c, int32_t hq, int32_t group, PlanShap
     s->blks_per_page = c->page_size / BLK;
     // blocks are counted in 32 bits
     if (int64_t(c->n_rows) * (int64_t(c->table_width) * s->blks_per_page + START) >= (int64_t(1) << 30)) return DISC_ERR_UNSUPPORTED;
-    const int32_t places = cache_held(c) && s->M <= ROWS_M ? PLACES / 2 * HELD_BLOCKS : PLACES;
+    const int32_t places = cache_held(c) && s->M <= HELD_FEW ? PLACES / 2 * HELD_BLOCKS : PLACES;
     s->lanes = places / c->n_kv_heads > 1 ? places / c->n_kv_heads : 1;
     // every border between two lanes makes one item two
     if (s->M <= ROWS_M) {

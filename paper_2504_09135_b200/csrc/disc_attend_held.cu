@@ -38,8 +38,10 @@ struct HeldSmem {
     static constexpr int BYTES = WARPS * RING > SUMS ? WARPS * RING : SUMS;
 };
 
+// Up to 8 query vectors fit three blocks' registers; with 16 they spilled there (64 ragged rows of 16 heads on each of 4 key heads: 200 us, with two
+// blocks to an SM 88).
 template <typename T, int DP, int HELD, int NT>
-__global__ void __launch_bounds__(AT, HELD_BLOCKS) attend_held_kernel(const AttendParams p) {
+__global__ void __launch_bounds__(AT, NT == 1 ? HELD_BLOCKS : 2) attend_held_kernel(const AttendParams p) {
     let_later_in();
     wait_for_earlier();
     using S = HeldSmem<DP, NT>;
@@ -204,7 +206,7 @@ int launch(const AttendParams& p, cudaStream_t st) {
 }
 template <typename T, int HELD>
 int launch(const AttendParams& p, cudaStream_t st) {
-    if (p.shape.M <= 8) return p.D <= 64 ? launch<T, 64, HELD, 1>(p, st) : launch<T, 128, HELD, 1>(p, st);
+    if (p.shape.M <= HELD_FEW) return p.D <= 64 ? launch<T, 64, HELD, 1>(p, st) : launch<T, 128, HELD, 1>(p, st);
     return p.D <= 64 ? launch<T, 64, HELD, 2>(p, st) : launch<T, 128, HELD, 2>(p, st);
 }
 
