@@ -223,15 +223,36 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
 template <typename T, int DP, int HELD>
 __device__ __forceinline__ void expand_tile(unsigned char* tile, const unsigned char* codes, int tokens, int D, int box_bytes, int thread) {
     const int t = thread >> 1, half = thread & 1;
-    if (t >= tokens) return;
-    const int e = reinterpret_cast<const signed char*>(codes)[TN * DP + t];
+    int e = reinterpret_cast<const signed char*>(codes)[TN * DP + t];
+    if (t >= tokens) e = 0;
     uint32_t scale2;
     const bool fast = fast_scale<T, HELD>(e, &scale2);
-    const float scale = exponent_scale(e);
     unsigned char* row = tile + t * (BOX * 2);
     const unsigned char* from = codes + t * D;
     const int turn = DP == 128 ? (t & 1) << 1 | (t >> 1 & 1) : t >> 1 & 1;
+    auto store = [&](int c, const uint32_t* x) {
+        unsigned char* box = row + c / 4 * box_bytes;
+        const int at = c % 4 * 2;
+        *reinterpret_cast<uint4*>(box + ((at ^ (t & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
+        *reinterpret_cast<uint4*>(box + (((at + 1) ^ (t & 7)) << 4)) = make_uint4(x[4], x[5], x[6], x[7]);
+    };
+    if (__all_sync(FULL, fast) && D == DP) {
+        // what is in order for a whole warp: no branches between one run of codes and the next (with them 64 us for the shared pages of 128 prompts, this way 61)
+        if (t >= tokens) return;
+        uint4 w[DP / 32];
 #pragma unroll
+        for (int j = 0; j < DP / 32; ++j) w[j] = *reinterpret_cast<const uint4*>(from + (2 * (j ^ turn) + half) * 16);
+#pragma unroll
+        for (int j = 0; j < DP / 32; ++j) {
+            uint32_t x[8];
+            fast_values16<T, HELD>(w[j], scale2, x);
+            store(2 * (j ^ turn) + half, x);
+        }
+        return;
+    }
+    if (t >= tokens) return;
+    const float scale = exponent_scale(e);
+#pragma unroll 1
     for (int j = 0; j < DP / 32; ++j) {
         const int c = 2 * (j ^ turn) + half;
         uint32_t x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -239,10 +260,7 @@ __device__ __forceinline__ void expand_tile(unsigned char* tile, const unsigned 
             const uint4 w = *reinterpret_cast<const uint4*>(from + c * 16);
             if (fast) fast_values16<T, HELD>(w, scale2, x); else values16<T, HELD>(w, scale, x);
         }
-        unsigned char* box = row + c / 4 * box_bytes;
-        const int at = c % 4 * 2;
-        *reinterpret_cast<uint4*>(box + ((at ^ (t & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
-        *reinterpret_cast<uint4*>(box + (((at + 1) ^ (t & 7)) << 4)) = make_uint4(x[4], x[5], x[6], x[7]);
+        store(c, x);
     }
 }
 
