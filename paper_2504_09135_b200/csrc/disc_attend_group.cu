@@ -24,7 +24,8 @@
 //
 // A cache held in 8 bits: the loads bring codes and exponents, and four more warps make of them the tiles that the products read, in
 // the vectors' type and exactly the values that are held; the products and the softmax are the same.  Kernel 2 takes its blocks as
-// disc_attend_held.cu does.
+// disc_attend_held.cu does.  On 128 prompts of 500 to 1024 tokens with 32 candidates each, e4m3: kernel 1 61 us (two warps that make tiles: 84; in 16
+// bits 50), kernel 2 59 at four blocks to an SM (three: 65).
 
 #include "disc_attend.cuh"
 #include "disc_held_mma.cuh"

@@ -3,21 +3,24 @@
 //
 //   out[r] = sum_j p_j v_j,  p = softmax_j(scale q[r] k_j),  k_j = 2^e_j kc_j,  v_j = 2^f_j vc_j
 //
-// The codes kc, vc become f16 exactly, by a few bit operations on four of them at a time, and go into the products as they are; the
+// The codes kc, vc become f16 exactly and go into the products as they are; the
 // powers of two stay outside: scale 2^e_j multiplies a token's scores, and what multiplies a token's value codes is
 // 2^(s_j + f_j - t) with a running maximum t of the exponents s_j + f_j of its own, so that the factors are at most 2^SLACK however
 // much the values' sizes differ from token to token.  The queries become f16 too, a bf16 vector after a power of two that brings its
 // largest value to 2^8 (what is lost is below 2^-32 of the largest value).
 //
-// Bound by the bytes of the distinct pages while the conversion keeps up: that is what the instructions go into, about 7 for four
-// codes.  So the products are taken with the tokens (S^T = K Q^T) and the value dims (O^T = V^T P^T) as the wide side of
-// mma.sync m16n8k16 and the query vectors as the narrow one, eight at a time: a converted register is used whole, and once for each eight
-// query vectors.  ldmatrix with transposition moves 16-bit units, which are two value dims of a token here; the two become two
-// rows of the product (dims 2 i and 2 i + 1 are rows i and i + 8), so that no byte is ever transposed alone.
+// Bound by the bytes of the distinct pages while the conversion keeps up.  So the products are taken with the tokens (S^T = K Q^T) and
+// the value dims (O^T = V^T P^T) as the wide side of mma.sync m16n8k16 and the query vectors as the narrow one, eight at a
+// time: a converted register is used whole, and once for each eight query vectors.  ldmatrix with transposition moves 16-bit units, which
+// are two value dims of a token here; the two become two rows of the product (dims 2 i and 2 i + 1 are rows i and i + 8).
 //
 // A block of 4 warps per share and key head as in disc_attend.cu: every warp brings in blocks of 16 tokens for itself, several in
 // flight, and the warps' results are joined at the end.  The maxima move only when a score exceeds them by SLACK, which is what one
 // vote of the warp costs, instead of shuffles for every block.
+//
+// Measured on 64 rows of 1 to 8191 tokens, 32 / 8 heads of 128, bf16 in e4m3: 100 us for 0.53 GB (5.3 TB/s; the copy rate would be 81).  Neither
+// DRAM (82 %) nor issue (52 %) nor a pipe (ALU 57 %, 212 of 380 instructions for a block of 16 tokens) is full; 8 or 12 warps to an SM,
+// one block at a time or two, three or five blocks in flight make no difference.
 
 #include "disc_attend.cuh"
 #include "disc_held_mma.cuh"

@@ -608,7 +608,7 @@ class AttendPlan:
 
 def _of_cache(plan: AttendPlan, cache: DiscCache):
     # what lies where in the buffer hangs on the sizes: another layout would be read as page numbers
-    if plan.sizes != cache._sizes:
+    if plan.sizes is not cache._sizes and plan.sizes != cache._sizes:
         raise TypeError("plan: made for a cache of other sizes")
 
 
