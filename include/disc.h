@@ -505,7 +505,8 @@ int disc_norm_rope_grad(const disc_norm_rope_t* a, void* d_q, void* d_k, float* 
  *   code    value * 2^-e rounded to the nearest, ties to even;  e is at least -126
  * so that an e4m3 code is off by at most 2^-4 of its value (or 2^-10 2^e), an i8 code by half of 2^e.  A held value, code * 2^e, is exact in the
  * vectors' type; one that exceeds the type's largest finite value (an e4m3 code rounded up) is given back as that.  A vector
- * with an infinite value or a NaN is held as e = -128 and reads as NaN throughout. */
+ * with an infinite value or a NaN is held as e = -128 and reads as NaN throughout.  In a pool that is filled otherwise, e4m3 codes of
+ * 0x7f and 0xff, which are no numbers, have no place. */
 #define DISC_HELD_E4M3 0x10
 #define DISC_HELD_I8 0x20
 typedef struct {
@@ -542,7 +543,8 @@ int disc_cache_extend(const disc_cache_t* c, const int32_t* add, uint8_t* status
  * the row was extended by.
  *   k, v    device, token t, head h at element offset t*token_stride + h*head_stride; bases on
  *           16-byte boundaries, strides multiples of 8
- *   status  device, uint8[n_rows] (nullable): rows with a status (disc_cache_extend) are skipped */
+ *   status  device, uint8[n_rows] (nullable): rows with a status (disc_cache_extend) are skipped
+ * Into 8 bits: DISC_ERR_UNSUPPORTED for more than 2048 key heads. */
 int disc_cache_write(const disc_cache_t* c, int32_t layer, const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v,
                      int64_t v_token_stride, int64_t v_head_stride, int64_t n_tokens, const int32_t* cu, int32_t n_seqs,
                      const int32_t* rows, const uint8_t* status, void* stream);
@@ -593,7 +595,10 @@ int disc_attend_plan(const disc_cache_t* c, int32_t n_q_heads, int32_t group, vo
  * Scores, sums and outputs are accumulated in fp32; the probabilities are rounded to the inputs' type for
  * the second product (up to 8 query vectors per group, min(group, n_rows) times the query heads of a key head: to twice its
  * digits), the outputs once at the end.  The result does not depend on the order in which the parts of
- * a row finish, and a row's non-finite values do not reach the other rows of its group. */
+ * a row finish, and a row's non-finite values do not reach the other rows of its group.
+ * Over a cache held in 8 bits the values that are held take part as they are.  Up to 16 query vectors per group the probabilities, times
+ * the values' powers of two, are rounded to f16 relative to the largest of them (q of type f16: to twice its digits), above that as over 16 bits;
+ * a vector held as NaN makes NaN of all outputs of the query heads that see it. */
 int disc_attend_cached(const disc_cache_t* c, int32_t layer, const void* q, int64_t q_row_stride, int64_t q_head_stride,
                        int32_t n_q_heads, int32_t group, float scale, void* plan, int64_t plan_bytes, void* out, float* lse_out,
                        void* stream);
