@@ -461,11 +461,12 @@ __global__ void __launch_bounds__(256) cache_write_kernel(Books b, WriteParams w
     }
 }
 
-// The same into 8 bits.  A warp has up to 32 tokens, which its lanes look up side by side, and goes through their heads, LPV lanes with 16
-// values each to a vector, keys and values of two heads of each lane in flight.  Bound by the bytes: 65,000 tokens x 8 heads of 128 85 us
-// (449 MB, 5.3 TB/s; through a ring in shared memory, as the norms go, 128: its instructions cost more than what they hide).
+// The same into 8 bits.  A warp has up to 32 tokens, which its lanes look up side by side, and goes through their vectors, LPV lanes with 16
+// values each to a vector, head after head and within one from token to token, as they lie in a page: what it writes at a time is then one run of
+// codes and one of exponents (token after token 85 us instead of 77).  Keys and values of two steps of each lane in flight.  Bound by the bytes: 65,000 tokens x 8 heads
+// of 128 77 us (449 MB, 5.8 TB/s; through a ring in shared memory, as the norms go, 128: its instructions cost more than what they hide).
 template <typename T, int LPV, int HELD>
-__global__ void __launch_bounds__(256) cache_write_held_kernel(Books b, WriteParams w, int32_t D, int32_t per_warp, uint32_t of_token) {
+__global__ void __launch_bounds__(256) cache_write_held_kernel(Books b, WriteParams w, int32_t D, int32_t per_warp, uint32_t of_head) {
     let_later_in();
     wait_for_earlier();
     constexpr int SIDE = 32 / LPV;
@@ -496,7 +497,7 @@ __global__ void __launch_bounds__(256) cache_write_held_kernel(Books b, WritePar
             }
         }
     }
-    const int all = n_tokens * w.heads;
+    const int all = per_warp * w.heads;
     for (int i0 = 0; i0 < all; i0 += 2 * SIDE) {
         uint4 x[2][2][2];              // step; keys, values; halves of the lane's 16 values
         int64_t part[2];               // the page and head
@@ -504,9 +505,9 @@ __global__ void __launch_bounds__(256) cache_write_held_kernel(Books b, WritePar
         bool some[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int i = i0 + u * SIDE + lane / LPV, t = min(w.heads == 1 ? i : int(__umulhi(uint32_t(i), of_token)), n_tokens - 1), h = i - t * w.heads;
+            const int i = i0 + u * SIDE + lane / LPV, h = per_warp == 1 ? i : int(__umulhi(uint32_t(i), of_head)), t = i - h * per_warp;
             const int32_t page = __shfl_sync(FULL, my_page, t), off = __shfl_sync(FULL, my_off, t);
-            some[u] = i < all && page >= 0 && c * 16 < D;
+            some[u] = h < w.heads && page >= 0 && c * 16 < D;     // tokens from n_tokens on have no page
             part[u] = (int64_t(max(page, 0)) * w.heads + h) * w.head_bytes;
             place[u] = off;
 #pragma unroll
@@ -862,10 +863,10 @@ int disc_cache_write(const disc_cache_t* c, int32_t layer, const void* k, int64_
         if (w.heads > (1 << 11)) return DISC_ERR_UNSUPPORTED;
         int sms = 0;
         if (const int rc = device_sms(&sms)) return rc;
-        const int32_t per_warp = tokens_of_warp(n_tokens, 32 / w.heads, sms);
+        const int32_t per_warp = tokens_of_warp(n_tokens, 32 / w.heads > 4 ? 32 / w.heads : 4, sms);
         const int64_t warps = (n_tokens + per_warp - 1) / per_warp;
         return launch_after(write_held_kernel(c), unsigned((warps + 7) / 8), 256, 0, st, books(c), w, c->head_dim, per_warp,
-                            uint32_t(((uint64_t(1) << 32) + w.heads - 1) / w.heads));
+                            uint32_t(((uint64_t(1) << 32) + per_warp - 1) / per_warp));
     }
     return launch_after(cache_write_kernel, unsigned((n_tokens * 32 + 255) / 256), 256, 0, st, books(c), w);
 }
