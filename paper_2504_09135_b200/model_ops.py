@@ -63,6 +63,12 @@ def _empty(shape, dtype, device):
     return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _two(shape, dtype, device):
+    """Two contiguous tensors of three axes."""
+    stride = (shape[1] * shape[2], shape[2], 1)
+    return torch.empty_strided(shape, stride, dtype=dtype, device=device), torch.empty_strided(shape, stride, dtype=dtype, device=device)
+
+
 def _alloc(stream, make, *args):
     """make(*args) with its memory from the stream the kernel runs on: memory of another stream may still be in use there."""
     if stream is None:
@@ -335,7 +341,7 @@ def _grad_outputs(q, k, q_weight, k_weight, need: int):
     like = torch.empty_like
     return (None if q is None else like(q, memory_format=_DENSE), None if k is None else like(k, memory_format=_DENSE),
             None if q_weight is None else like(q_weight, dtype=_F32), None if k_weight is None else like(k_weight, dtype=_F32),
-            torch.empty(need, dtype=torch.uint8, device=(k if q is None else q).device) if need else None)
+            torch.empty_strided((need,), (1,), dtype=torch.uint8, device=(k if q is None else q).device) if need else None)
 
 
 # ---- attention over prompts -------------------------------------------------------------------------
@@ -567,11 +573,13 @@ def disc_cache_read(cache: DiscCache, layer: int, cu: torch.Tensor, n_tokens: in
     (None: row i) -> (k, v) [n_tokens, kv heads, head dim]; zeros for tokens the row does not have.  n_tokens: cu[-1], or more
     (what lies behind is left as it is).  out: a pair of contiguous buffers of that shape."""
     n_seqs = cu.numel() - 1
-    for t, name in ((rows, "rows"), (start, "start")):
-        _want(t, n_seqs, name)
+    if rows is not None:
+        _want(rows, n_seqs, "rows")
+    if start is not None:
+        _want(start, n_seqs, "start")
     shape = (int(n_tokens), cache.n_kv_heads, cache.head_dim)
     if out is None:
-        k, v = _alloc(stream, lambda: (_empty(shape, cache.dtype, cache.pool.device), _empty(shape, cache.dtype, cache.pool.device)))
+        k, v = _alloc(stream, _two, shape, cache.dtype, cache.pool.device)
     else:
         k, v = out
         for t, name in ((k, "k"), (v, "v")):
