@@ -249,6 +249,25 @@ def _aligned(t, stream):
     return t
 
 
+def _leaves(node):
+    """Of a node of autograd's graph: the nodes behind it that add to a leaf's gradient."""
+    return [n for n, _ in node.next_functions if type(n).__name__ == "AccumulateGrad"]
+
+
+def _note_stream(node):
+    """A leaf's node lives as long as some graph of the leaf, and adds on the stream on which it came to be."""
+    for n in _leaves(node):
+        n.metadata.setdefault("disc_stream", torch.cuda.current_stream())
+
+
+def _same_stream(node):
+    """In a capture: a wait for another stream, which the leaf's node brings with it, would end the process from a thread of autograd's."""
+    for n in _leaves(node):
+        if n.metadata.get("disc_stream", torch.cuda.current_stream()) != torch.cuda.current_stream():
+            raise RuntimeError("disc_norm_rope: a backward pass is captured while results of an earlier call on another stream hold a graph of the same leaf; "
+                               "release them before the capture")
+
+
 class _NormRope(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, positions, inv_freq, q_weight, k_weight, norm, eps, interleaved, stream):
@@ -268,6 +287,8 @@ class _NormRope(torch.autograd.Function):
             k = kw = None
         if q is None and k is None:
             return (None,) * 10
+        if torch.cuda.is_current_stream_capturing():
+            _same_stream(ctx)
         d_q, d_k, d_qw, d_kw = disc_norm_rope_grad(q, k, positions, inv_freq, d_q, d_k, norm=norm, q_weight=qw, k_weight=kw, eps=eps, interleaved=interleaved)
         if d_qw is not None:
             d_qw = d_qw.to(qw.dtype)
@@ -282,14 +303,17 @@ def disc_norm_rope(q, k, positions, inv_freq=None, *, norm: bool = True, q_weigh
     projection are fine; either may be None), positions int32[n] -> (q', k').  inv_freq float32[rot / 2]: the first `rot` values
     of a vector are rotated (None: none); q_weight, k_weight [D] float32 or the vectors' type (None: 1).
     out: a pair of buffers of the same shapes, which may be q and k themselves.  Where an input or a weight requires a gradient the
-    results have one (disc_norm_rope_grad; its call goes to the current stream of this one), and `out` is refused."""
+    results have one (disc_norm_rope_grad; its call goes to the current stream of this one), and `out` is refused.  A backward pass
+    that is captured into a graph is refused while results of an earlier call on another stream hold on to the same leaf."""
     if torch.is_grad_enabled():
         if inv_freq is not None and inv_freq.requires_grad:
             _without_grad(inv_freq, "inv_freq")
         if any(t is not None and t.requires_grad for t in (q, k, q_weight, k_weight)):
             if out is not None:
                 raise TypeError("out: given buffers have no history; detach the inputs, or call under torch.no_grad()")
-            return _NormRope.apply(q, k, positions, inv_freq, q_weight, k_weight, norm, eps, interleaved, stream)
+            y = _NormRope.apply(q, k, positions, inv_freq, q_weight, k_weight, norm, eps, interleaved, stream)
+            _note_stream((y[1] if y[0] is None else y[0]).grad_fn)
+            return y
     dtype, n, hq, hkv, d = _heads(q, k, "disc_norm_rope")
     qv = _NONE if q is None else _vectors(q, dtype, "q")
     kv = _NONE if k is None else _vectors(k, dtype, "k")

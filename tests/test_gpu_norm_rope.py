@@ -224,6 +224,36 @@ def test_captured_and_on_another_stream():
         assert all(torch.equal(a, b) for a, b in zip(got + got_g, want + want_g))
 
 
+def test_a_captured_backward_pass_and_an_eager_graph_of_the_same_leaves():
+    q, k, pos, qw, _ = inputs(40, 4, 2, 64, torch.bfloat16)
+    freq, dy = frequencies(64), torch.randn((40, 4, 64), device=DEV).bfloat16()
+    want = disc.disc_norm_rope_grad(q, None, pos, freq, dy, None, q_weight=qw)
+    leaf, weight = q.clone().requires_grad_(), qw.clone().requires_grad_()
+
+    def both():
+        disc.disc_norm_rope(leaf, None, pos, freq, q_weight=weight)[0].backward(dy)
+
+    held = disc.disc_norm_rope(leaf, None, pos, freq, q_weight=weight)
+    torch.cuda.synchronize()
+    with pytest.raises(RuntimeError, match="release them"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            both()
+    assert leaf.grad is None and weight.grad is None
+    held[0].backward(dy)               # as before
+    assert torch.equal(leaf.grad, want[0]) and torch.equal(weight.grad, want[2])
+    del held
+    leaf.grad = weight.grad = None
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for scale in (2.0, 1.0):
+        dy.copy_(dy * scale)
+        graph.replay()
+    torch.cuda.synchronize()
+    want = disc.disc_norm_rope_grad(q, None, pos, freq, dy, None, q_weight=qw)
+    assert torch.equal(leaf.grad, want[0]) and torch.equal(weight.grad, want[2])
+
+
 def test_calls_that_are_refused():
     q, k, pos, qw, kw = inputs(4, 4, 2, 64, torch.bfloat16)
     freq = frequencies(64)
