@@ -11,8 +11,9 @@
 // lane holds 16 values of a vector, two runs of 8 that are rotated into one another (8 or 4 lanes a vector, 4 or 8 vectors side by side
 // in a warp; vectors that cannot be cut like that have runs of 4): loads and stores of 16 bytes, three or two shuffles for a sum of
 // squares.  A warp's vectors are all of one kind, queries, keys or values, and it goes from token to token, the next ones on their way
-// into a ring in shared memory, of which every lane fills and reads places of its own, while the present ones are worked on.  What a token's vectors have in common, weight times cosine and weight times sine, is formed once for
-// all of them: y = r (P x + Q x'), x' the other value of the pair.
+// into a ring in shared memory, of which every lane fills and reads places of its own, while the present ones are worked on.  What a
+// token's vectors have in common, weight times cosine and weight times sine, is formed once for all of them: y = r (P x + Q x'), x' the
+// other value of the pair.
 //
 // Angles: the fraction of a turn, position x inv_freq / 2 pi less its whole turns, is the product of two whole numbers modulo 2^64 (the
 // frequency as a 64-bit fraction of a turn, which wraps by itself), so that a position of a million is as exact as one of ten; an fp32
