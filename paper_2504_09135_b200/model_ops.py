@@ -257,15 +257,16 @@ def _leaves(node):
 def _note_stream(node):
     """A leaf's node lives as long as some graph of the leaf, and adds on the stream on which it came to be."""
     for n in _leaves(node):
-        n.metadata.setdefault("disc_stream", torch.cuda.current_stream())
+        n.metadata.setdefault("disc_default_stream", torch.cuda.current_stream().cuda_stream == 0)
 
 
-def _same_stream(node):
-    """In a capture: a wait for another stream, which the leaf's node brings with it, would end the process from a thread of autograd's."""
+def _not_default(node):
+    """In a capture: another stream joins it, but the default stream's wait, which the leaf's node brings with it, would end the process
+    from a thread of autograd's."""
     for n in _leaves(node):
-        if n.metadata.get("disc_stream", torch.cuda.current_stream()) != torch.cuda.current_stream():
-            raise RuntimeError("disc_norm_rope: a backward pass is captured while results of an earlier call on another stream hold a graph of the same leaf; "
-                               "release them before the capture")
+        if n.metadata.get("disc_default_stream", False):
+            raise RuntimeError("disc_norm_rope: a backward pass is captured while results of an earlier call on the default stream hold a graph of the "
+                               "same leaf; release them before the capture")
 
 
 class _NormRope(torch.autograd.Function):
@@ -288,7 +289,7 @@ class _NormRope(torch.autograd.Function):
         if q is None and k is None:
             return (None,) * 10
         if torch.cuda.is_current_stream_capturing():
-            _same_stream(ctx)
+            _not_default(ctx)
         d_q, d_k, d_qw, d_kw = disc_norm_rope_grad(q, k, positions, inv_freq, d_q, d_k, norm=norm, q_weight=qw, k_weight=kw, eps=eps, interleaved=interleaved)
         if d_qw is not None:
             d_qw = d_qw.to(qw.dtype)
@@ -304,7 +305,7 @@ def disc_norm_rope(q, k, positions, inv_freq=None, *, norm: bool = True, q_weigh
     of a vector are rotated (None: none); q_weight, k_weight [D] float32 or the vectors' type (None: 1).
     out: a pair of buffers of the same shapes, which may be q and k themselves.  Where an input or a weight requires a gradient the
     results have one (disc_norm_rope_grad; its call goes to the current stream of this one), and `out` is refused.  A backward pass
-    that is captured into a graph is refused while results of an earlier call on another stream hold on to the same leaf."""
+    that is captured into a graph is refused while results of an earlier call on the default stream hold on to the same leaf."""
     if torch.is_grad_enabled():
         if inv_freq is not None and inv_freq.requires_grad:
             _without_grad(inv_freq, "inv_freq")

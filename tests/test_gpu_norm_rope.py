@@ -254,6 +254,24 @@ def test_a_captured_backward_pass_and_an_eager_graph_of_the_same_leaves():
     assert torch.equal(leaf.grad, want[0]) and torch.equal(weight.grad, want[2])
 
 
+def test_a_captured_backward_pass_after_eager_ones_on_a_stream_of_their_own():
+    q, _, pos, qw, _ = inputs(40, 4, 2, 64, torch.bfloat16)
+    freq, dy = frequencies(64), torch.randn((40, 4, 64), device=DEV).bfloat16()
+    want = disc.disc_norm_rope_grad(q, None, pos, freq, dy, None, q_weight=qw)
+    leaf, weight = q.clone().requires_grad_(), qw.clone().requires_grad_()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        held = disc.disc_norm_rope(leaf, None, pos, freq, q_weight=weight)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            disc.disc_norm_rope(leaf, None, pos, freq, q_weight=weight)[0].backward(dy)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert held[0].grad_fn is not None
+    assert torch.equal(leaf.grad, want[0]) and torch.equal(weight.grad, want[2])
+
+
 def test_calls_that_are_refused():
     q, k, pos, qw, kw = inputs(4, 4, 2, 64, torch.bfloat16)
     freq = frequencies(64)
