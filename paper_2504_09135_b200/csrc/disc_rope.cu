@@ -5,7 +5,8 @@
 //   u = w x r,  r = 1 / sqrt(mean(x^2) + eps);   y_a = u_a cos t_i - u_b sin t_i,  y_b = u_b cos t_i + u_a sin t_i,
 //   t_i = position inv_freq_i,  (a, b) = (i, i + rot / 2) or (2 i, 2 i + 1)
 //
-// Backward, with g = dy rotated by -t and c = w g:  dw = sum g x r,  dx = r c - x r^3 mean(c x).
+// Backward, with g = dy rotated by -t, c = w g and z = x r:  dw = sum g z,  dx = r (c - z mean(c z)).  The vectors are normed first: r^3, which
+// r c - x r^3 mean(c x) has, leaves the range of fp32 where |x| is 10^15, or 10^-13 with eps = 0.
 //
 // Bound by the bytes: every vector is read once and written once, and what stands in the way are the instructions around them.  So a
 // lane holds 16 values of a vector, two runs of 8 that are rotated into one another (8 or 4 lanes a vector, 4 or 8 vectors side by side
@@ -563,14 +564,14 @@ __global__ void __launch_bounds__(THREADS, GRAD_BLOCKS) norm_rope_grad_kernel(co
                 float2 dot = make_float2(0.f, 0.f);
 #pragma unroll
                 for (int j = 0; j < RUN; ++j) {
-                    const float2 gx = mul2(g[j], x[j]);
-                    acc[j] = fma2(gx, make_float2(ra, ra), acc[j]);
-                    dot = fma2(gx, f[j], dot);
+                    x[j] = mul2(x[j], make_float2(ra, ra));
+                    acc[j] = fma2(g[j], x[j], acc[j]);
                     g[j] = mul2(g[j], f[j]);
+                    dot = fma2(g[j], x[j], dot);
                 }
-                const float m = -sum_of<LPV>(dot.x + dot.y) * p.inv_D * (r * r * r);
+                const float m = -sum_of<LPV>(dot.x + dot.y) * p.inv_D;
 #pragma unroll
-                for (int j = 0; j < RUN; ++j) g[j] = fma2(x[j], make_float2(m, m), mul2(g[j], make_float2(r, r)));
+                for (int j = 0; j < RUN; ++j) g[j] = mul2(fma2(x[j], make_float2(m, m), g[j]), make_float2(r, r));
             }
             if (h < h1 && at.some) store_raw<RUN>(to, at, pack<T, RUN>(g));
         }
