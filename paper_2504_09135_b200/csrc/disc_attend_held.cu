@@ -5,8 +5,8 @@
 //
 // The codes kc, vc become f16 exactly and go into the products as they are; the
 // powers of two stay outside: scale 2^e_j multiplies a token's scores, and what multiplies a token's value codes is
-// 2^(s_j + f_j - t) with a running maximum t of the exponents s_j + f_j of its own, so that the factors are at most 2^SLACK however
-// much the values' sizes differ from token to token.  The queries become f16 too, a bf16 vector after a power of two that brings its
+// 2^(s_j + f_j - t) with a running maximum t of the exponents s_j + f_j of its own, so that the factors are at most 2^SLACK (and HEADROOM more, up to
+// the end of f16's range) however much the values' sizes differ from token to token.  The queries become f16 too, a bf16 vector after a power of two that brings its
 // largest value to 2^8 (what is lost is below 2^-32 of the largest value).
 //
 // Bound by the bytes of the distinct pages while the conversion keeps up.  So the products are taken with the tokens (S^T = K Q^T) and
@@ -165,9 +165,10 @@ __global__ void __launch_bounds__(AT, NT == 1 ? HELD_BLOCKS : 2) attend_held_ker
                 x.z += w_t[w][m] > -CUDART_INF_F ? f * y.z : y.z; x.w += w_t[w][m] > -CUDART_INF_F ? f * y.w : y.w;
                 ll += w_m[w][m] > -CUDART_INF_F ? ex2_approx(w_m[w][m] - mm) * w_l[w][m] : w_l[w][m];
             }
-            float inv = ll > 0.f ? 1.f / ll : (ll == 0.f ? 0.f : ll);
-            if (tt > -CUDART_INF_F && ll > 0.f) inv *= exp2f(tt - mm);
-            x.x *= inv; x.y *= inv; x.z *= inv; x.w *= inv;
+            const float inv = ll > 0.f ? 1.f / ll : (ll == 0.f ? 0.f : ll);
+            // in two halves: with the smallest of the values' powers of two the factor itself has few digits
+            const float f = tt > -CUDART_INF_F && ll > 0.f ? exp2f(0.5f * (tt - mm)) : 1.f;
+            x.x = x.x * inv * f * f; x.y = x.y * inv * f * f; x.z = x.z * inv * f * f; x.w = x.w * inv * f * f;
             float lse2 = ll > 0.f ? mm + log2f(ll) : (ll == 0.f ? -CUDART_INF_F : ll);
             if (n_rows > 1 && p.len[r0 + m / G] == 0) {           // beside rows whose shared pages it does not hold
                 x = make_float4(0.f, 0.f, 0.f, 0.f);

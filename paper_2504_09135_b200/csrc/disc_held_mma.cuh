@@ -7,6 +7,11 @@
 
 namespace disc {
 
+// Probability times the values' power of two is at most 2^SLACK of its reference and goes into the products in f16, which ends above 2^15 and has
+// steps of 2^-24 at its lower end.  So it gets this many powers of two more, of which the sums are rid at the end: what is lost of a small one
+// is then 2^-32 of the reference, and not 2^-25, which 2^17 tokens of a warp, each of that probability beside a large one, made 0.0017 of 1.
+constexpr float HEADROOM = 15.f - SLACK;
+
 // shared memory of a block: keys [16][DP] | values [16][DP] | exponents of the keys [16] | of the values [16] | the user's, from HELD_SPARE on
 constexpr int HELD_SPARE = 2 * BLK;
 template <int DP>
@@ -132,7 +137,7 @@ template <int DP, int NT>
 struct HeldSums {                      // this thread's vectors: 2 (lane % 4) and the next of each eight
     float o[NT][DP / 16][4];           // dims 16 j + 2 (lane / 4) of the two vectors, then the next dim of both, times 2^-t
     float m[NT][2], l[NT][2];          // reference and sum of the probabilities
-    float t[NT][2];                    // reference of probability times the values' power of two
+    float t[NT][2];                    // reference of probability times the values' power of two; from finish_held on what o is times 2^-t of
 };
 template <int DP, int NT>
 __device__ __forceinline__ void clear_held(HeldSums<DP, NT>& a) {
@@ -152,6 +157,10 @@ __device__ __forceinline__ void finish_held(HeldSums<DP, NT>& a) {
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 2; ++e) a.l[nt][e] += __shfl_xor_sync(0xffffffffu, a.l[nt][e], x);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) a.t[nt][e] -= HEADROOM;
 }
 
 // A block of some tokens, at least one; in[nt][e]: they are seen by this thread's vectors.  Probabilities are rounded to f16 for the second
@@ -234,7 +243,7 @@ __device__ __forceinline__ void add_held_block(HeldSums<DP, NT>& acc, const Held
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const float m0 = acc.m[nt][0] > -CUDART_INF_F ? acc.m[nt][0] : 0.f, m1 = acc.m[nt][1] > -CUDART_INF_F ? acc.m[nt][1] : 0.f;
-        const float t0 = acc.t[nt][0] > -CUDART_INF_F ? acc.t[nt][0] : 0.f, t1 = acc.t[nt][1] > -CUDART_INF_F ? acc.t[nt][1] : 0.f;
+        const float t0 = acc.t[nt][0] > -CUDART_INF_F ? acc.t[nt][0] - HEADROOM : 0.f, t1 = acc.t[nt][1] > -CUDART_INF_F ? acc.t[nt][1] - HEADROOM : 0.f;
         acc.l[nt][0] += ex2_approx(s[nt][0] - m0) + ex2_approx(s[nt][2] - m0);
         acc.l[nt][1] += ex2_approx(s[nt][1] - m1) + ex2_approx(s[nt][3] - m1);
         const float x0 = ex2_approx(w[nt][0] - t0), x1 = ex2_approx(w[nt][1] - t1), x2 = ex2_approx(w[nt][2] - t0), x3 = ex2_approx(w[nt][3] - t1);
