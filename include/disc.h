@@ -445,8 +445,8 @@ int disc_attend_error(const uint32_t* error, void* stream);
  *   u = w x / sqrt(mean(x^2) + eps) with `norm` (a null weight counts as 1), u = x without
  *   y_a = u_a cos t_i - u_b sin t_i,  y_b = u_b cos t_i + u_a sin t_i,   t_i = position * inv_freq[i],  i < rot / 2
  * with (a, b) = (i, i + rot/2), or (2i, 2i + 1) with `interleaved`; values from rot on are not rotated.  Rounded once, at the end.
- * Angles are formed less their whole turns, in whole numbers: as exact at position 10^6 as at 10.  Sums of squares are held in
- * fp32: |x| up to about 10^18, and with eps = 0 from about 10^-18.
+ * Angles are formed less their whole turns, in whole numbers: as exact at position 10^6 as at 10; a pair whose frequency is not finite
+ * becomes NaN.  Sums of squares are held in fp32: |x| up to about 10^18, and with eps = 0 from about 10^-18.
  *
  * The call's arguments, in host memory, read before the call returns; what a call does not mention is not looked at. */
 typedef struct {

@@ -172,7 +172,7 @@ struct Turns {
     float c[64], s[64];
 };
 struct Frequencies {
-    uint64_t f[2];                     // of pairs lane and lane + 32, as 64-bit fractions of a turn
+    uint64_t f[2];                     // of pairs lane and lane + 32, as fractions of a turn of 63 bits; the last bit says that it is not finite
 };
 __device__ __forceinline__ Frequencies frequencies_of(const RopeParams& p, int lane) {
     Frequencies q;
@@ -180,8 +180,9 @@ __device__ __forceinline__ Frequencies frequencies_of(const RopeParams& p, int l
     for (int i = 0; i < 2; ++i) {
         q.f[i] = 0;
         if (2 * (lane + 32 * i) >= p.rot) continue;
-        const double turns = double(p.inv_freq[lane + 32 * i]) * 0.15915494309189533577;          // 1 / 2 pi
-        q.f[i] = uint64_t((turns - floor(turns)) * 18446744073709551616.0);
+        const float inv_freq = p.inv_freq[lane + 32 * i];
+        const double turns = double(inv_freq) * 0.15915494309189533577;          // 1 / 2 pi
+        q.f[i] = fabsf(inv_freq) < CUDART_INF_F ? uint64_t((turns - floor(turns)) * 18446744073709551616.0) & ~uint64_t(1) : 1;
     }
     return q;
 }
@@ -192,7 +193,7 @@ __device__ __forceinline__ void turn_to(const RopeParams& p, int32_t pos, const 
         if (64 * i >= p.rot) break;
         const int32_t part = int32_t(uint32_t((uint64_t(int64_t(pos)) * q.f[i]) >> 32));          // of 2^32, from -1/2 to 1/2 of a turn
         float s, c;
-        sincospif(float(part) * 0x1p-31f, &s, &c);
+        sincospif(q.f[i] & 1 ? CUDART_NAN_F : float(part) * 0x1p-31f, &s, &c);
         out.c[lane + 32 * i] = c;
         out.s[lane + 32 * i] = s;
     }
