@@ -168,9 +168,10 @@ __device__ __forceinline__ void load_weights(const RopeParams& p, int kind, cons
 }
 
 // Cosines and sines of a warp's token: each of the rot / 2 <= 64 pairs by one lane, through shared memory.
-struct Turns {
+struct __align__(16) Turns {           // read four at a time
     float c[64], s[64];
 };
+static_assert(alignof(Turns) == 16 && sizeof(Turns) % 16 == 0, "read_turns");
 struct Frequencies {
     uint64_t f[2];                     // of pairs lane and lane + 32, as fractions of a turn of 63 bits; the last bit says that it is not finite
 };
