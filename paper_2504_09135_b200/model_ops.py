@@ -282,15 +282,17 @@ class _NormRope(torch.autograd.Function):
     def backward(ctx, d_q, d_k):
         q, k, positions, inv_freq, qw, kw = ctx.saved_tensors
         norm, eps, interleaved = ctx.how
-        if d_q is None:
-            q = qw = None
-        if d_k is None:
-            k = kw = None
+        need_q, need_k, _, _, need_qw, need_kw = ctx.needs_input_grad[:6]
+        if d_q is None or not (need_q or need_qw):
+            q = d_q = qw = None
+        if d_k is None or not (need_k or need_kw):
+            k = d_k = kw = None
         if q is None and k is None:
             return (None,) * 10
         if torch.cuda.is_current_stream_capturing():
             _not_default(ctx)
-        d_q, d_k, d_qw, d_kw = disc_norm_rope_grad(q, k, positions, inv_freq, d_q, d_k, norm=norm, q_weight=qw, k_weight=kw, eps=eps, interleaved=interleaved)
+        d_q, d_k, d_qw, d_kw = disc_norm_rope_grad(q, k, positions, inv_freq, d_q, d_k, norm=norm, q_weight=qw, k_weight=kw, eps=eps, interleaved=interleaved,
+                                                   q_weight_grad=need_qw, k_weight_grad=need_kw)
         if d_qw is not None:
             d_qw = d_qw.to(qw.dtype)
         if d_kw is not None:
@@ -333,9 +335,9 @@ def disc_norm_rope(q, k, positions, inv_freq=None, *, norm: bool = True, q_weigh
 
 
 def disc_norm_rope_grad(q, k, positions, inv_freq, d_q, d_k, *, norm: bool = True, q_weight=None, k_weight=None, eps: float = 1e-6,
-                        interleaved: bool = False, stream=None):
+                        interleaved: bool = False, q_weight_grad: bool = True, k_weight_grad: bool = True, stream=None):
     """From the gradients d_q, d_k of disc_norm_rope's results those of its inputs: (dq, dk, dq_weight, dk_weight), the weights' in
-    float32 (None for a weight that is not given)."""
+    float32 (None for a weight that is not given, or whose gradient is not asked for)."""
     dtype, n, hq, hkv, d = _heads(q, k, "disc_norm_rope_grad")
     if (q is None) != (d_q is None) or (q is not None and d_q.shape != q.shape):
         raise TypeError("d_q: expected the shape of the queries")
@@ -351,6 +353,11 @@ def disc_norm_rope_grad(q, k, positions, inv_freq, d_q, d_k, *, norm: bool = Tru
     ptrs, how = _how(dtype, d, inv_freq, norm, q_weight, k_weight, interleaved)
     pos = _positions(positions, n, inv_freq)
     need = 0
+    # the call's pointers are taken: from here on the weights stand for their gradients
+    if not q_weight_grad:
+        q_weight = None
+    if not k_weight_grad:
+        k_weight = None
     if q_weight is not None or k_weight is not None:
         need = lib().disc_norm_rope_scratch_bytes(hq, hkv, d, n)
         if need < 0:
