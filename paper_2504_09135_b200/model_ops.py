@@ -12,6 +12,7 @@ import math
 import struct
 
 import torch
+from torch.autograd.graph import increment_version as _written      # what kernels write through a pointer, a graph that has saved it has to be told
 
 from .binding import DISC_BF16, DISC_F16, DISC_F32, DISC_HELD_E4M3, DISC_HELD_I8, DiscError, _Cache, _check, _dev, _here, _stream_ptr, lib
 
@@ -123,7 +124,8 @@ def disc_logprobs(logits: torch.Tensor, targets: torch.Tensor | None = None, *, 
     ptr, dt, ld = _rows(logits, "disc_logprobs")
     n, V = logits.shape
     _want(targets, n, "targets")
-    if out is None:
+    given = out is not None
+    if not given:
         out = _alloc(stream, _logprobs_outputs, n, top, targets is not None, logits.device)
     else:
         for k in _LOGPROBS:
@@ -133,6 +135,8 @@ def disc_logprobs(logits: torch.Tensor, targets: torch.Tensor | None = None, *, 
                              _own(out["logp"]), _own(out["entropy"]), _own(out["lse"]), _own(out["top_ids"]),
                              _own(out["top_logp"]), _own(out["status"]), _stream_ptr(stream))
     _check(rc, "disc_logprobs")
+    if given:
+        _written([out[k] for k in _LOGPROBS if out[k] is not None])
     return out
 
 
@@ -148,7 +152,8 @@ def disc_logprobs_grad(logits: torch.Tensor, targets, lse: torch.Tensor, entropy
         if t is not None and (t.requires_grad or t.numel() != n):
             _want(t, n, name)
             _without_grad(t, name)
-    if out is None:
+    given = out is not None
+    if not given:
         out = _alloc(stream, _empty, (n, V), logits.dtype, logits.device)
     elif out.shape != logits.shape or out.dtype != logits.dtype:
         raise TypeError("out: expected the shape and dtype of the logits")
@@ -158,6 +163,8 @@ def disc_logprobs_grad(logits: torch.Tensor, targets, lse: torch.Tensor, entropy
                                   _dev(d_logp, torch.float32, "d_logp"), _dev(d_entropy, torch.float32, "d_entropy"),
                                   optr, old, _stream_ptr(stream))
     _check(rc, "disc_logprobs_grad")
+    if given:
+        _written(out)
     return out
 
 
@@ -331,6 +338,8 @@ def disc_norm_rope(q, k, positions, inv_freq=None, *, norm: bool = True, q_weigh
     call = _pack_call(qv[0], kv[0], 0, qo[0], ko[0], qv[1], qv[2], kv[1], kv[2], 0, 0, qo[1], qo[2], ko[1], ko[2], pos, *ptrs, n, 0, 0, 0,
                       _HALF[dtype], hq, hkv, d, *how, eps, 0)
     _check(lib().disc_norm_rope(call, _stream_ptr(stream)), "disc_norm_rope")
+    if out is not None:
+        _written([o for t, o in ((q, q_out), (k, k_out)) if t is not None])
     return (q_out if q is not None else None), (k_out if k is not None else None)
 
 
@@ -425,12 +434,15 @@ def disc_attend_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: 
     n_seqs = cu_q.numel() - 1
     if cu_k is not None:
         _want(cu_k, n_seqs + 1, "cu_k")
+    given = [t for t in (out, lse) if t is not None]
     out, lse = _alloc(stream, _attend_outputs, q, out, lse)
     rc = lib().disc_attend_prompt(qp, qt, qh, kp, kt, kh, vp, vt, vh, dt, hq, hkv, d, n_q, n_k, _dev(cu_q, torch.int32, "cu_q"), _dev(cu_k, torch.int32, "cu_k"), n_seqs,
                                   int(max_len), int(causal), 1.0 / math.sqrt(d) if scale is None else float(scale),
                                   _own(out), _own(lse), attend_error_word(q.device).data_ptr(),
                                   _stream_ptr(stream))
     _check(rc, "disc_attend_prompt")
+    if given:
+        _written(given)
     return out, lse
 
 
@@ -586,16 +598,19 @@ def disc_norm_rope_write(cache: DiscCache, layer: int, q, k: torch.Tensor, v: to
         _want(rows, n_seqs, "rows")
     _want(status, cache.n_rows, "status")
     _want(positions, n, "positions")
+    given = q is not None and out is not None
     if q is None:
         out, qo = None, _NONE
-    elif out is None:
-        out, qo = _dense(q, stream)
-    else:
+    elif given:
         qo = _given(q, out, "out")
+    else:
+        out, qo = _dense(q, stream)
     call = _pack_call(qv[0], kv[0], vv[0], qo[0], 0, qv[1], qv[2], kv[1], kv[2], vv[1], vv[2], qo[1], qo[2], 0, 0, _dev(positions, torch.int32, "positions"),
                       *ptrs, n, _dev(cu, torch.int32, "cu"), _dev(rows, torch.int32, "rows"), _dev(status, torch.uint8, "status"),
                       _HALF[cache.dtype], hq, h, d, *how, eps, n_seqs)
     _check(lib().disc_norm_rope_write(_books(cache), int(layer), call, _stream_ptr(stream)), "disc_norm_rope_write")
+    if given:
+        _written(out)
     return out
 
 
@@ -620,6 +635,8 @@ def disc_cache_read(cache: DiscCache, layer: int, cu: torch.Tensor, n_tokens: in
                 raise TypeError(f"{name}: expected [n_tokens, kv heads, head dim]")
     _check(lib().disc_cache_read(_books(cache), int(layer), _dev(cu, torch.int32, "cu"), n_seqs, _dev(rows, torch.int32, "rows"),
                                  _dev(start, torch.int32, "start"), int(n_tokens), k.data_ptr(), v.data_ptr(), _stream_ptr(stream)), "disc_cache_read")
+    if out is not None:
+        _written(out)
     return k, v
 
 
@@ -682,9 +699,12 @@ def disc_attend_cached(cache: DiscCache, layer: int, q: torch.Tensor, plan: Atte
     _of_cache(plan, cache)
     if not plan.made:
         raise TypeError("plan: not made yet (disc_attend_plan)")
+    given = [t for t in (out, lse) if t is not None]
     out, lse = _alloc(stream, _attend_outputs, q, out, lse)
     _check(lib().disc_attend_cached(_books(cache), int(layer), qp, qr, qh, plan.n_q_heads, plan.group,
                                     1.0 / math.sqrt(cache.head_dim) if scale is None else float(scale), plan.buf.data_ptr(),
                                     plan.nbytes, _own(out), _own(lse),
                                     _stream_ptr(stream)), "disc_attend_cached")
+    if given:
+        _written(given)
     return out, lse
