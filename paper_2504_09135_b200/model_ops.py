@@ -12,6 +12,7 @@ import math
 import struct
 
 import torch
+import torch.autograd.forward_ad as _forward
 from torch.autograd.graph import increment_version as _written      # what kernels write through a pointer, a graph that has saved it has to be told
 
 from .binding import DISC_BF16, DISC_F16, DISC_F32, DISC_HELD_E4M3, DISC_HELD_I8, DiscError, _Cache, _check, _dev, _here, _stream_ptr, lib
@@ -25,11 +26,18 @@ def _without_grad(t, name: str):
         raise TypeError(f"{name}: requires a gradient, which this call does not give; detach it, or call under torch.no_grad()")
 
 
+def _without_tangent(t, name: str):
+    if t is not None and _forward.unpack_dual(t).tangent is not None:
+        raise TypeError(f"{name}: has a tangent, which this call's results would not have; take its primal")
+
+
 def _vectors(t: torch.Tensor, dtype, name: str):
     """A CUDA tensor [tokens, heads, head_dim] whose innermost axis is contiguous: (pointer, the two strides)."""
     if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype:
         if t.requires_grad:
             _without_grad(t, name)
+        if _forward._current_level >= 0:
+            _without_tangent(t, name)
         st = t.stride()
         if len(st) == 3 and (st[2] == 1 or t.shape[2] == 1):
             return _here(t, name), st[0], st[1]
@@ -47,6 +55,8 @@ def _rows(t: torch.Tensor, name: str):
         raise TypeError(f"{name}: expected a CUDA tensor [n, V] with unit inner stride")
     if t.dtype not in _LOGIT:
         raise DiscError(-7, name)
+    if _forward._current_level >= 0:
+        _without_tangent(t, name)
     return _here(t, name), _LOGIT[t.dtype], t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
@@ -152,6 +162,8 @@ def disc_logprobs_grad(logits: torch.Tensor, targets, lse: torch.Tensor, entropy
         if t is not None and (t.requires_grad or t.numel() != n):
             _want(t, n, name)
             _without_grad(t, name)
+        if _forward._current_level >= 0:
+            _without_tangent(t, name)
     given = out is not None
     if not given:
         out = _alloc(stream, _empty, (n, V), logits.dtype, logits.device)
@@ -186,6 +198,9 @@ def _weights(dtype, d: int, norm, q_weight, k_weight):
 def _how(dtype, d: int, inv_freq, norm, q_weight, k_weight, interleaved):
     """What is done to the vectors, with the checks that need the tensors: the three pointers, then rot, interleaved, norm, weight type."""
     qw, kw, wt = (0, 0, 0) if q_weight is None and k_weight is None else _weights(dtype, d, norm, q_weight, k_weight)
+    if _forward._current_level >= 0:
+        for t, name in ((inv_freq, "inv_freq"), (q_weight, "q_weight"), (k_weight, "k_weight")):
+            _without_tangent(t, name)
     if inv_freq is None:
         return (0, qw, kw), (0, 0, 1 if norm else 0, wt)
     return (_dev(inv_freq, _F32, "inv_freq"), qw, kw), (2 * inv_freq.numel(), 1 if interleaved else 0, 1 if norm else 0, wt)
