@@ -271,24 +271,55 @@ def _aligned(t, stream):
     return t
 
 
+# A backward pass that is captured into a graph.  A leaf's node in autograd's graph lives as long as something holds it, and adds on the stream on
+# which it came to be.  Another stream joins the capture, but the default stream's wait would end the process from a thread of autograd's.  So
+# the node has a note: True for the default stream, False for another one, None where it is not known.
+_NOTE, _ALIVE = "disc_default_stream", "disc_alive"
+
+
 def _leaves(node):
     """Of a node of autograd's graph: the nodes behind it that add to a leaf's gradient."""
     return [n for n, _ in node.next_functions if type(n).__name__ == "AccumulateGrad"]
 
 
-def _note_stream(node):
-    """A leaf's node lives as long as some graph of the leaf, and adds on the stream on which it came to be."""
+def _leaf_node(t):
+    return torch.autograd.graph.get_gradient_edge(t).node
+
+
+def _note_foreign(*tensors) -> bool:
+    """Before a call: notes the leaves among `tensors` whose nodes something else holds, made who knows where, and says whether there are any.
+    What is put on a node that nothing holds goes with it."""
+    some = False
+    for t in tensors:
+        if t is not None and t.requires_grad and t.is_leaf:
+            _leaf_node(t).metadata[_ALIVE] = True
+            if _leaf_node(t).metadata.pop(_ALIVE, False):
+                _leaf_node(t).metadata.setdefault(_NOTE, None)
+                some = True
+    return some
+
+
+def _note_new(node, on_default: bool):
+    """After a call: leaves without a note."""
     for n in _leaves(node):
-        n.metadata.setdefault("disc_default_stream", torch.cuda.current_stream().cuda_stream == 0)
+        n.metadata.setdefault(_NOTE, on_default)
+
+
+def _find_out(node):
+    """In a backward pass that is not captured, before the leaves' nodes run: which stream they run on."""
+    for n in _leaves(node):
+        notes = n.metadata
+        if notes.get(_NOTE, False) is None:
+            n.register_prehook(lambda grads, notes=notes: notes.__setitem__(_NOTE, _stream_ptr() == 0))
 
 
 def _not_default(node):
-    """In a capture: another stream joins it, but the default stream's wait, which the leaf's node brings with it, would end the process
-    from a thread of autograd's."""
+    """In a captured one."""
     for n in _leaves(node):
-        if n.metadata.get("disc_default_stream", False):
-            raise RuntimeError("disc_norm_rope: a backward pass is captured while results of an earlier call on the default stream hold a graph of the "
-                               "same leaf; release them before the capture")
+        if n.metadata.get(_NOTE, False) is not False:
+            raise RuntimeError("disc_norm_rope: a backward pass is captured while results of an earlier call, or something else, hold graphs of the same leaf that "
+                               "were made on the default stream, or nobody knows where; release them before the capture, or run a backward pass on another "
+                               "stream before it, which finds out")
 
 
 class _NormRope(torch.autograd.Function):
@@ -296,7 +327,7 @@ class _NormRope(torch.autograd.Function):
     def forward(ctx, q, k, positions, inv_freq, q_weight, k_weight, norm, eps, interleaved, stream):
         ctx.set_materialize_grads(False)
         ctx.save_for_backward(q, k, positions, inv_freq, q_weight, k_weight)
-        ctx.how = (norm, eps, interleaved)
+        ctx.how, ctx.foreign = (norm, eps, interleaved), False
         return disc_norm_rope(q, k, positions, inv_freq, norm=norm, q_weight=q_weight, k_weight=k_weight, eps=eps, interleaved=interleaved, stream=stream)
 
     @staticmethod
@@ -313,6 +344,8 @@ class _NormRope(torch.autograd.Function):
             return (None,) * 10
         if torch.cuda.is_current_stream_capturing():
             _not_default(ctx)
+        elif ctx.foreign:
+            _find_out(ctx)
         d_q, d_k, d_qw, d_kw = disc_norm_rope_grad(q, k, positions, inv_freq, d_q, d_k, norm=norm, q_weight=qw, k_weight=kw, eps=eps, interleaved=interleaved,
                                                    q_weight_grad=need_qw, k_weight_grad=need_kw)
         if d_qw is not None:
@@ -329,15 +362,21 @@ def disc_norm_rope(q, k, positions, inv_freq=None, *, norm: bool = True, q_weigh
     of a vector are rotated (None: none); q_weight, k_weight [D] float32 or the vectors' type (None: 1).
     out: a pair of buffers of the same shapes, which may be q and k themselves.  Where an input or a weight requires a gradient the
     results have one (disc_norm_rope_grad; its call goes to the current stream of this one), and `out` is refused.  A backward pass
-    that is captured into a graph is refused while results of an earlier call on the default stream hold on to the same leaf."""
+    that is captured into a graph is refused while something holds a graph of the same leaf, given to this call as it is, that was made on
+    the default stream, or before a call of this one on another stream has had a backward pass, which shows where it was made.  (With leaves
+    that reach the call through other operations it is not seen, and ends the process, as it does under torch's own operations.)"""
     if torch.is_grad_enabled():
         if inv_freq is not None and inv_freq.requires_grad:
             _without_grad(inv_freq, "inv_freq")
         if any(t is not None and t.requires_grad for t in (q, k, q_weight, k_weight)):
             if out is not None:
                 raise TypeError("out: given buffers have no history; detach the inputs, or call under torch.no_grad()")
+            on_default = _stream_ptr() == 0
+            foreign = not on_default and _note_foreign(q, k, q_weight, k_weight)
             y = _NormRope.apply(q, k, positions, inv_freq, q_weight, k_weight, norm, eps, interleaved, stream)
-            _note_stream((y[1] if y[0] is None else y[0]).grad_fn)
+            node = (y[1] if y[0] is None else y[0]).grad_fn
+            node.foreign = foreign
+            _note_new(node, on_default)
             return y
     dtype, n, hq, hkv, d = _heads(q, k, "disc_norm_rope")
     qv = _NONE if q is None else _vectors(q, dtype, "q")
