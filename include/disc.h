@@ -596,9 +596,9 @@ int disc_attend_plan(const disc_cache_t* c, int32_t n_q_heads, int32_t group, vo
  * the second product (up to 8 query vectors per group, min(group, n_rows) times the query heads of a key head: to twice its
  * digits), the outputs once at the end.  The result does not depend on the order in which the parts of
  * a row finish, and a row's non-finite values do not reach the other rows of its group.
- * Over a cache held in 8 bits the values that are held take part as they are.  Up to 16 query vectors per group the probabilities, times
- * the values' powers of two, are rounded to f16 relative to 2^7 times the largest of them (what is below 2^-32 of that one is lost; q of type
- * f16: to twice its digits), above that as over 16 bits;
+ * Over a cache held in 8 bits the values that are held take part as they are; outputs beyond f16's largest value are given as that.  Up to
+ * 16 query vectors per group the probabilities, times the values' powers of two, are rounded to f16 relative to 2^7 times the largest of
+ * them (what is below 2^-32 of that one is lost; q of type f16: to twice its digits), above that as over 16 bits;
  * a vector held as NaN makes NaN of all outputs of the query heads that see it. */
 int disc_attend_cached(const disc_cache_t* c, int32_t layer, const void* q, int64_t q_row_stride, int64_t q_head_stride,
                        int32_t n_q_heads, int32_t group, float scale, void* plan, int64_t plan_bytes, void* out, float* lse_out,

@@ -205,6 +205,16 @@ struct AttendParams {
 
 constexpr float LN2_F = 0.6931471805599453f;
 
+// Two outputs.  In f16 a value held in 8 bits can exceed the type's largest one by the rounding of its code; reading it gives the largest, and so
+// does a mean of such values, which would else be infinite.  Infinities themselves, which 16 bits can hold, stay.
+template <typename T>
+__device__ __forceinline__ uint32_t pack_out(float a, float b) { return pack2<T>(a, b); }
+template <>
+__device__ __forceinline__ uint32_t pack_out<__half>(float a, float b) {
+    auto within = [](float x) { return fabsf(x) < CUDART_INF_F ? fminf(fmaxf(x, -65504.f), 65504.f) : x; };
+    return pack2<__half>(within(a), within(b));
+}
+
 // The items of a group, joined in their order by the block of threads that finished last: one pass, eight parts on their way at
 // a time.  slot: the group's first part; M query vectors of the rows from r0 on, DP >= D values.
 template <typename T, int DP, int THREADS>
@@ -240,7 +250,7 @@ __device__ __forceinline__ void join_items(const AttendParams& p, int32_t slot, 
         }
         const float inv = total > 0.f ? 1.f / total : (total == 0.f ? 0.f : total);
         const int64_t at = int64_t(r0 + m / G) * p.kv_heads * G + head * G + m % G;
-        *reinterpret_cast<uint2*>(p.out + (at * p.D + d) * 2) = make_uint2(pack2<T>(x.x * inv, x.y * inv), pack2<T>(x.z * inv, x.w * inv));
+        *reinterpret_cast<uint2*>(p.out + (at * p.D + d) * 2) = make_uint2(pack_out<T>(x.x * inv, x.y * inv), pack_out<T>(x.z * inv, x.w * inv));
         if (d == 0 && p.lse) p.lse[at] = total > 0.f ? (top + log2f(total)) * LN2_F : (total == 0.f ? -CUDART_INF_F : total);
     }
 }

@@ -786,7 +786,7 @@ __global__ void __launch_bounds__(JT, HELD ? 4 : 3) attend_join_kernel(const Att
                 }
                 const float inv = total[a] > 0.f ? 1.f / total[a] : (total[a] == 0.f ? 0.f : total[a]);
                 *reinterpret_cast<uint2*>(p.out + ((out_at + g0 + h[a]) * D + d) * 2) =
-                    make_uint2(pack2<T>(x[a].x * inv, x[a].y * inv), pack2<T>(x[a].z * inv, x[a].w * inv));
+                    make_uint2(pack_out<T>(x[a].x * inv, x[a].y * inv), pack_out<T>(x[a].z * inv, x[a].w * inv));
                 if (d == 0 && p.lse) p.lse[out_at + g0 + h[a]] = total[a] > 0.f ? (m[a] + log2f(total[a])) * LN2_F : (total[a] == 0.f ? -CUDART_INF_F : total[a]);
             }
         }

@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(AT, NT == 1 ? HELD_BLOCKS : 2) attend_held_ker
                 if (d == 0) p.plan.part_lse[slot + m] = lse2;
             } else {
                 const int64_t at = int64_t(r0 + m / G) * p.kv_heads * G + head * G + m % G;
-                *reinterpret_cast<uint2*>(p.out + (at * p.D + d) * 2) = make_uint2(pack2<T>(x.x, x.y), pack2<T>(x.z, x.w));
+                *reinterpret_cast<uint2*>(p.out + (at * p.D + d) * 2) = make_uint2(pack_out<T>(x.x, x.y), pack_out<T>(x.z, x.w));
                 if (d == 0 && p.lse) p.lse[at] = lse2 * LN2_F;
             }
         }
