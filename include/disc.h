@@ -469,9 +469,9 @@ typedef struct {
     int32_t n_seqs;
 } disc_norm_rope_t;
 
-/* q -> q_out, k -> k_out, by the tokens' positions (nullable with rot = 0).  An output may be its input (same strides), otherwise must
- * not overlap it.
- * Errors: DISC_ERR_ARG, DISC_ERR_UNSUPPORTED (dtype, head_dim, rot, strides, weight_dtype). */
+/* q -> q_out, k -> k_out, by the tokens' positions (nullable with rot = 0).  An output may be its own input (same strides); otherwise it
+ * must not overlap any input, nor the other output.
+ * Errors: DISC_ERR_ARG (also for an output that begins where another input does), DISC_ERR_UNSUPPORTED (dtype, head_dim, rot, strides, weight_dtype). */
 int disc_norm_rope(const disc_norm_rope_t* a, void* stream);
 
 /* Its gradient: q_out, k_out are the gradients of the results (read; strides of 0 allowed), from which come those of q and k

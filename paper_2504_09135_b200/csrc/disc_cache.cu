@@ -878,7 +878,7 @@ int disc_cache_read(const disc_cache_t* c, int32_t layer, const int32_t* cu, int
     if (layer < 0 || layer >= c->n_layers || n_tokens < 0 || n_seqs < 0 || n_tokens > (int64_t(1) << 30)) return DISC_ERR_ARG;
     if (!rows && n_seqs > c->n_rows) return DISC_ERR_ARG;
     if (n_tokens == 0 || n_seqs == 0) return DISC_OK;
-    if (!cu || !k_out || !v_out || ((reinterpret_cast<uintptr_t>(k_out) | reinterpret_cast<uintptr_t>(v_out)) & 31u)) return DISC_ERR_ARG;
+    if (!cu || !k_out || !v_out || k_out == v_out || ((reinterpret_cast<uintptr_t>(k_out) | reinterpret_cast<uintptr_t>(v_out)) & 31u)) return DISC_ERR_ARG;
     ReadParams r;
     r.k_plane = static_cast<const unsigned char*>(c->pool) + 2 * int64_t(layer) * cache_plane_bytes(c);
     r.v_plane = r.k_plane + cache_plane_bytes(c);

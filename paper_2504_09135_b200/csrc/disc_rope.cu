@@ -696,6 +696,17 @@ int check_vectors(const void* x, int64_t token, int64_t head, int64_t n, int32_t
     return DISC_OK;
 }
 
+// An output may lie on its own input, place for place; on another one it would be written while that is still read.  Told by where they begin.
+int check_places(const RopeParams& p) {
+    for (int k = 0; k < 2; ++k) {
+        const Vectors &y = p.y[k], &x = p.x[k];
+        if (!y.at) continue;
+        if (y.at == x.at && (y.token != x.token || y.head != x.head)) return DISC_ERR_ARG;
+        if (y.at == p.x[1 - k].at || y.at == p.x[2].at || y.at == p.y[1 - k].at) return DISC_ERR_ARG;
+    }
+    return DISC_OK;
+}
+
 void cache_params(const disc_cache_t* c, int32_t layer, const int32_t* cu, int32_t n_seqs, const int32_t* rows, const uint8_t* status, CacheParams* w) {
     w->plane[0] = static_cast<unsigned char*>(c->pool) + 2 * int64_t(layer) * cache_plane_bytes(c);
     w->plane[1] = w->plane[0] + cache_plane_bytes(c);
@@ -763,6 +774,7 @@ int disc_norm_rope(const disc_norm_rope_t* a, void* stream) {
     if (const int rc = check_vectors(a->k, a->k_token, a->k_head, n, a->n_kv_heads, &p.x[1])) return rc;
     if (const int rc = check_vectors(a->q_out, a->q_out_token, a->q_out_head, n, a->n_q_heads, &p.y[0])) return rc;
     if (const int rc = check_vectors(a->k_out, a->k_out_token, a->k_out_head, n, a->n_kv_heads, &p.y[1])) return rc;
+    if (const int rc = check_places(p)) return rc;
     p.heads[0] = a->n_q_heads; p.heads[1] = a->n_kv_heads;
     return launch<-1>(a->dtype, p, CacheParams{}, static_cast<cudaStream_t>(stream));
 }
@@ -781,6 +793,7 @@ int disc_norm_rope_write(const disc_cache_t* c, int32_t layer, const disc_norm_r
     if (const int rc = check_vectors(a->k, a->k_token, a->k_head, n, c->n_kv_heads, &p.x[1])) return rc;
     if (const int rc = check_vectors(a->v, a->v_token, a->v_head, n, c->n_kv_heads, &p.x[2])) return rc;
     if (const int rc = check_vectors(a->q_out, a->q_out_token, a->q_out_head, n, a->n_q_heads, &p.y[0])) return rc;
+    if (const int rc = check_places(p)) return rc;
     p.heads[0] = a->n_q_heads; p.heads[1] = p.heads[2] = c->n_kv_heads;
     CacheParams w;
     cache_params(c, layer, a->cu, a->n_seqs, a->rows, a->status, &w);
