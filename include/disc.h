@@ -592,8 +592,8 @@ int disc_attend_plan(const disc_cache_t* c, int32_t n_q_heads, int32_t group, vo
  *           it, so calls that share a plan must not overlap
  *   out     device, [n_rows][n_q_heads][head_dim] contiguous, 16-byte aligned
  *   lse_out device, float[n_rows][n_q_heads] (nullable)
- * Scores, sums and outputs are accumulated in fp32; the probabilities are rounded to the inputs' type for
- * the second product (up to 8 query vectors per group, min(group, n_rows) times the query heads of a key head: to twice its
+ * Scores, sums and outputs are accumulated in fp32; the probabilities are rounded to the inputs' type (f16: with steps of 2^-24 of the
+ * largest at their lower end) for the second product (up to 8 query vectors per group, min(group, n_rows) times the query heads of a key head: to twice its
  * digits), the outputs once at the end.  The result does not depend on the order in which the parts of
  * a row finish, and a row's non-finite values do not reach the other rows of its group.
  * Over a cache held in 8 bits the values that are held take part as they are; outputs beyond f16's largest value are given as that.  Up to

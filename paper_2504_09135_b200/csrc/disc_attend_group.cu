@@ -18,14 +18,14 @@
 // one the MMAs.  Tensor memory: S 64 columns | O.  Tiles of 64 tokens, so that five of keys or values are on their way at a
 // time (with two of 128 tokens the loads came too late: 54 us against 50 on 128 prompts of 500 to 1024 tokens).  A last tile of fewer than 4 blocks takes fewer steps of the
 // second product, and its missing scores are masked, so that nothing stale is ever multiplied.  P is rounded to the inputs' type, the
-// operand type of the second product; sums of the remainders apart from O, as the rows form has them, would need 320 of the 256
-// columns of tensor memory that a block can have with two to an SM.
-
+// operand type of the second product: outputs are off by 0.0022 (bf16) and 0.00027 (f16) relative to their size instead of the 0.0017 and 0.00021 that
+// their own rounding makes.  The remainders could lie in S's other 32 columns and their product be added to the same sums.  Over 8 bits that
+// gives 0.0017, and takes 146 us instead of 138 for 128 prompts with 32 candidates each (kernel 1 an eighth longer), so it was left out.
 //
 // A cache held in 8 bits: the loads bring codes and exponents, and four more warps make of them the tiles that the products read, in
 // the vectors' type and exactly the values that are held; the products and the softmax are the same.  Kernel 2 takes its blocks as
-// disc_attend_held.cu does.  On 128 prompts of 500 to 1024 tokens with 32 candidates each, e4m3: kernel 1 61 us (two warps that make tiles: 84; in 16
-// bits 50), kernel 2 59 at four blocks to an SM (three: 65).
+// disc_attend_held.cu does.  On 128 prompts of 500 to 1024 tokens with 32 candidates each, e4m3: kernel 1 60 us (with two warps that make tiles 84; in
+// 16 bits 50), kernel 2 58 at four blocks to an SM (three: 65).
 
 #include "disc_attend.cuh"
 #include "disc_held_mma.cuh"
@@ -238,7 +238,7 @@ __device__ __forceinline__ void expand_tile(unsigned char* tile, const unsigned 
         *reinterpret_cast<uint4*>(box + (((at + 1) ^ (t & 7)) << 4)) = make_uint4(x[4], x[5], x[6], x[7]);
     };
     if (__all_sync(FULL, fast) && D == DP) {
-        // what is in order for a whole warp: no branches between one run of codes and the next (with them 64 us for the shared pages of 128 prompts, this way 61)
+        // what is in order for a whole warp: no branches between one run of codes and the next (with them 5 % longer for the shared pages of 128 prompts)
         if (t >= tokens) return;
         uint4 w[DP / 32];
 #pragma unroll

@@ -18,7 +18,7 @@
 // flight, and the warps' results are joined at the end.  The maxima move only when a score exceeds them by SLACK, which is what one
 // vote of the warp costs, instead of shuffles for every block.
 //
-// Measured on 64 rows of 1 to 8191 tokens, 32 / 8 heads of 128, bf16 in e4m3: 100 us for 0.53 GB (5.3 TB/s; the copy rate would be 81).  Neither
+// Measured on 64 rows of 1 to 8191 tokens, 32 / 8 heads of 128, bf16 in e4m3: 98 us for 0.53 GB (5.4 TB/s; the copy rate would be 81).  Neither
 // DRAM (82 %) nor issue (52 %) nor a pipe (ALU 57 %, 212 of 380 instructions for a block of 16 tokens) is full; 8 or 12 warps to an SM,
 // one block at a time or two, three or five blocks in flight make no difference.
 
@@ -41,8 +41,8 @@ struct HeldSmem {
     static constexpr int BYTES = WARPS * RING > SUMS ? WARPS * RING : SUMS;
 };
 
-// Up to 8 query vectors fit three blocks' registers; with 16 they spilled there (64 ragged rows of 16 heads on each of 4 key heads: 200 us, with two
-// blocks to an SM 88).
+// Up to 8 query vectors fit three blocks' registers; with 16 they spilled there and took more than twice as long.  The 64 rows with 16 heads
+// on each of 4 key heads: 77 us for 0.27 GB, which the copy rate would move in 41; eight warps to an SM are too few for the chain of a block.
 template <typename T, int DP, int HELD, int NT>
 __global__ void __launch_bounds__(AT, NT == 1 ? HELD_BLOCKS : 2) attend_held_kernel(const AttendParams p) {
     let_later_in();

@@ -53,8 +53,8 @@ __device__ __forceinline__ void load_held_block(uint32_t stage, const unsigned c
     if (lane < 2) cp16(stage + 2 * BLK * DP + lane * BLK, (lane ? v : k) + page_size * D + blk * BLK, true);
 }
 
-// Codes as f16, exactly.  e4m3: the conversion instruction takes two neighbouring codes, 49 of them a clock and SM (with shifts and masks,
-// seven operations for four codes, the 64 ragged rows took 183 us).  i8: a code, its top bit turned over, is the last byte of the f16
+// Codes as f16, exactly.  e4m3: the conversion instruction takes two neighbouring codes, 49 of them a clock and SM (with shifts and masks
+// it is seven operations for four codes).  i8: a code, its top bit turned over, is the last byte of the f16
 // 1024 + 128 + code; that gives codes 0 and 2, and 1 and 3.
 __device__ __forceinline__ uint32_t e4m3_f16(uint32_t two) {
     uint32_t x;
@@ -165,7 +165,7 @@ __device__ __forceinline__ void finish_held(HeldSums<DP, NT>& a) {
 
 // A block of some tokens, at least one; in[nt][e]: they are seen by this thread's vectors.  Probabilities are rounded to f16 for the second
 // product; where T is f16 what that leaves out goes through a second one, so that the outputs' own rounding stays the larger.  (Two
-// blocks at a time, for more independent instructions, made no difference: 110 us for the 64 ragged rows both ways.)
+// blocks at a time, for more independent instructions, made no difference.)
 template <typename T, int DP, int HELD, int NT>
 __device__ __forceinline__ void add_held_block(HeldSums<DP, NT>& acc, const HeldQueries<DP, NT>& qs, uint32_t stage, int tokens, const bool (&in)[NT][2], int lane) {
     constexpr bool TWO = is_half<T>();

@@ -21,7 +21,8 @@
 // product would be off by 0.03 there.  Then sin and cos of that fraction in fp32, each pair's by one lane, and through shared memory to the lanes
 // that turn it.
 //
-// Measured, bf16, heads of 128: 16384 tokens x 40 heads 60 us (336 MB, 5.6 TB/s), the gradient of 8191 tokens x 40 heads 50 us (252 MB, 5.0 TB/s).
+// Measured, bf16, heads of 128: 16384 tokens x 40 heads 57 to 60 us (336 MB, 5.6 to 5.9 TB/s), the gradient of 8191 tokens x 40 heads 51 us (252 MB,
+// 4.9 TB/s).  Heads of 80 take as long as heads of 96, 56 and 51 us: five or six of a vector's eight lanes have values.
 
 #include "disc_held.cuh"
 
@@ -331,7 +332,7 @@ __device__ __forceinline__ bool share_of(const Cut& cut, const RopeParams& p, in
 }
 
 // HELD: -1 without a cache, else how it holds its vectors.  Blocks of one warp: all that is the same for its lanes then goes by the block's number
-// and through the uniform registers (four warps to a block: 64 us for 16384 tokens x 40 heads instead of 59).
+// and through the uniform registers (four warps to a block: 7 % longer for 16384 tokens x 40 heads).
 template <typename T, int LPV, int RUN, int HELD>
 __global__ void __launch_bounds__(32, FORWARD_WARPS) norm_rope_kernel(const RopeParams p, const CacheParams w, const Cut cut) {
     let_later_in();
@@ -626,8 +627,8 @@ bool long_runs(int32_t D, int32_t rot) { return D % 16 == 0 && rot % 16 == 0; }
 int side_by_side(int32_t D, int32_t rot) { return (D <= 64 ? 4 : 2) * (long_runs(D, rot) ? 2 : 1); }
 
 // Equal shares of all steps for the warps that run at a time, as long as that is at least two steps and at most MOST_STEPS (then several
-// shares one after the other): with many steps the warps that end late are then short ones (16384 tokens x 40 heads: 65 us; with one round of 55
-// steps 69, with 4 steps, half of a token's queries, 73).  A share is several tokens, or a part of one.
+// shares one after the other): with many steps the warps that end late are then short ones (16384 tokens x 40 heads: with one round of 55
+// steps 6 % longer, with 4 steps, half of a token's queries, 12 %).  A share is several tokens, or a part of one.
 Cut cut_of(int64_t n, const int32_t* heads, int side, int64_t warps) {
     Cut cut = {};
     int64_t steps[3], all = 0, end = 0;
