@@ -360,11 +360,12 @@ def disc_norm_rope(q, k, positions, inv_freq=None, *, norm: bool = True, q_weigh
     """Each head's RMS norm and the rotation by the token's position: q [n, Hq, D], k [n, Hkv, D] (bf16 or f16, slices of a fused
     projection are fine; either may be None), positions int32[n] -> (q', k').  inv_freq float32[rot / 2]: the first `rot` values
     of a vector are rotated (None: none); q_weight, k_weight [D] float32 or the vectors' type (None: 1).
-    out: a pair of buffers of the same shapes, which may be q and k themselves, each its own, and otherwise overlap nothing.  Where an input or a weight requires a gradient the
-    results have one (disc_norm_rope_grad; its call goes to the current stream of this one), and `out` is refused.  A backward pass
-    that is captured into a graph is refused while something holds a graph of the same leaf, given to this call as it is, that was made on
-    the default stream, or before a call of this one on another stream has had a backward pass, which shows where it was made.  (With leaves
-    that reach the call through other operations it is not seen, and ends the process, as it does under torch's own operations.)"""
+    out: a pair of buffers of the same shapes, which may be q and k themselves, each its own, and otherwise overlap nothing.  Where
+    an input or a weight requires a gradient the results have one (disc_norm_rope_grad; its call goes to the current stream of this
+    one), and `out` is refused.  A backward pass that is captured into a graph is refused while something holds a graph of the same
+    leaf, given to this call as it is, that was made on the default stream, or nobody knows where until a call on another stream
+    has had a backward pass.  (Leaves that reach the call through other operations are not seen: the default stream's wait then ends
+    the process, as it does under torch's own operations.)"""
     if torch.is_grad_enabled():
         if inv_freq is not None and inv_freq.requires_grad:
             _without_grad(inv_freq, "inv_freq")
